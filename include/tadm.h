@@ -483,6 +483,156 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
                                                  double tau_max, double tau_min, int self_cond, uint64_t seed,
                                                  void* scratch, size_t scratch_bytes, tadm_stream stream);
 
+/* ------------------------------------- prompts of different lengths, paged cache --
+ * Operators of a server whose sequences differ in length: attention over
+ * packed prompts, an 8-bit KV cache in pages, attention over it, and the
+ * bookkeeping of the pages.  They use no handle; all pointers but the pool
+ * struct itself are device pointers, and every call only enqueues work.
+ *
+ * Packed rows.  The rows of `batch` sequences lie one after the other;
+ * cu_rows (int32 [batch + 1], not decreasing, within 0 .. total_rows) says
+ * where: sequence b has the rows cu_rows[b] .. cu_rows[b + 1] - 1.  A sequence
+ * may have no row.  Rows outside every sequence are neither read nor written.
+ * max_rows is at least the longest sequence's row count; rows of a sequence
+ * past it are left out.  Row t, head h of an operand starts at element
+ * t * ld + h * head_dim, ld >= heads * head_dim, so that q, k and v may be
+ * slices of one QKV projection's output.  dtype: 0 fp32, 1 bf16, of every row
+ * operand of the call.  Pointers are 16-byte aligned and ld * element size is
+ * a multiple of 16.  head_dim is 64 or 128.
+ *
+ * Visibility.  Keys j of a row's own sequence; causal: only j <= p, p the
+ * row's position; window > 0: only j with p - j < window.  A row that sees no
+ * key gets zeros.  K and V of one sequence never reach another one's rows,
+ * whatever they hold; an infinity or NaN in V of a visible key spreads to
+ * rows of the same sequence that do not see that key.
+ *
+ * Arithmetic: fp32 scores, softmax sums and accumulators.  bf16 calls round
+ * the probabilities to 8 (tadm_attention_packed) or 11 significant bits
+ * (tadm_page_attention) before they multiply V. */
+
+/* softmax(Q K^T / sqrt(head_dim)) V of whole prompts: row r of a sequence is
+ * at position r.  q, o: [total_rows, n_heads, head_dim]; k, v: [total_rows,
+ * n_kv_heads, head_dim].  Query head h reads KV head h / (n_heads /
+ * n_kv_heads).  o must not overlap the inputs. */
+TADM_API tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, void* o,
+                                           const int32_t* cu_rows, int batch, int total_rows, int max_rows,
+                                           int n_heads, int n_kv_heads, int head_dim, int64_t ldq, int64_t ldk,
+                                           int64_t ldv, int64_t ldo, int causal, int window, int dtype,
+                                           tadm_stream stream);
+
+/* The cache.  A page holds TADM_PAGE_TOKENS tokens of every KV head as e4m3
+ * (1 sign, 4 exponent, 3 mantissa bits) with one positive fp32 scale for K and
+ * one for V per page and head: value = e4m3 * scale.
+ *   k: [layers, pages, n_kv_heads, TADM_PAGE_TOKENS, head_dim]
+ *   v: [layers, pages, n_kv_heads, head_dim, TADM_PAGE_TOKENS] (transposed)
+ *   k_scale, v_scale: fp32 [layers, pages, n_kv_heads]
+ * k and v are 16-byte aligned.  Every layer uses the same page ids.
+ *
+ * A page table is int32 [sequences, ld_table]: entry i of a row is the page of
+ * the tokens 64 i .. 64 i + 63, or -1.  tadm_page_* calls use entries that
+ * the lengths cover: an id outside 0 .. pages - 1 there is not followed (the
+ * tokens of such a page are not written, and read as zeros). */
+#define TADM_PAGE_TOKENS 64
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t layers, pages, n_kv_heads, head_dim;
+} tadm_page_pool;
+
+/* Stores rows in the cache of `layer`: row r of sequence b (k, v:
+ * [total_rows, n_kv_heads, head_dim]) becomes token start[b] + r.
+ * The scale of a page and head is the least power of two s, 2^-60 <= s <=
+ * 2^60, with |x| <= 448 s for every finite x that it takes; x / s is rounded
+ * to the nearest e4m3 (ties to even; infinities and NaN are stored as NaN).
+ * If start[b] lies inside a page, its tokens below start[b] stay: the scale is then
+ * at least the page's present one, and where it grows those tokens are
+ * encoded again (which is exact but for the smallest, because scales are powers
+ * of two).  Slots past the last row of a page written from its first slot are
+ * zeroed.  No two sequences of a call may share a page that it writes, and
+ * ld_table * 64 covers start[b] + rows. */
+TADM_API tadm_status tadm_page_write(const tadm_page_pool* pool, int layer, const void* k, const void* v,
+                                     const int32_t* cu_rows, const int32_t* start, int batch, int total_rows,
+                                     int max_rows, int64_t ldk, int64_t ldv, const int32_t* table, int ld_table,
+                                     int dtype, tadm_stream stream);
+
+/* The inverse: row r of sequence b of k, v gets token start[b] + r of the
+ * cache (exact in fp32; bf16 is exact for scales that are powers of two). */
+TADM_API tadm_status tadm_page_read(const tadm_page_pool* pool, int layer, void* k, void* v, const int32_t* cu_rows,
+                                    const int32_t* start, int batch, int total_rows, int max_rows, int64_t ldk,
+                                    int64_t ldv, const int32_t* table, int ld_table, int dtype, tadm_stream stream);
+
+/* softmax(Q K^T / sqrt(head_dim)) V over the cache of `layer`: sequence b sees
+ * its tokens 0 .. lens[b] - 1 (int32 [batch]), of which its rows are the last
+ * ones: row r of n is at position lens[b] - n + r.  A decode step has one row per
+ * sequence, a block step block_len rows and causal = 0, a chunk of a prompt
+ * many rows and causal = 1.  lens[b] <= max_len <= ld_table * 64; tokens past
+ * max_len are left out.  scratch: at least tadm_page_attention_scratch_size()
+ * bytes, 16-byte aligned; it needs no initialisation, and calls that overlap
+ * on the GPU need one each. */
+TADM_API tadm_status tadm_page_attention_scratch_size(int batch, int total_rows, int max_rows, int max_len,
+                                                      int n_heads, int n_kv_heads, int head_dim, int dtype,
+                                                      size_t* bytes);
+TADM_API tadm_status tadm_page_attention(const void* q, const tadm_page_pool* pool, int layer, void* o,
+                                         const int32_t* cu_rows, const int32_t* lens, int batch, int total_rows,
+                                         int max_rows, int max_len, int n_heads, int64_t ldq, int64_t ldo,
+                                         const int32_t* table, int ld_table, int causal, int window, int dtype,
+                                         void* scratch, size_t scratch_bytes, tadm_stream stream);
+
+/* Bookkeeping.  tables: int32 [n_seqs, ld_table], -1 where a sequence holds no
+ * page (a sequence's pages come first in its row); lens: int32 [n_seqs]
+ * tokens; refs: int32 [pages], how many table entries hold a page (0: free).  Each call reads tables, lens and refs and
+ * writes *_out, which may be the same arrays (in place); each out array is
+ * either its input or overlaps none.  Everything is decided on the device in
+ * a fixed order, free pages are taken lowest id first, and status (int32 [1])
+ * tells the outcome: 0 done; TADM_PAGES_SHORT not enough free pages;
+ * TADM_PAGES_BAD an index out of range, a sequence listed twice, or tables
+ * and refs that contradict each other.  If it is not 0, the out arrays are
+ * copies of the inputs and no page is written.  scratch: at least
+ * tadm_pages_scratch_size() bytes, 16-byte aligned, as above. */
+#define TADM_PAGES_SHORT 1
+#define TADM_PAGES_BAD 2
+TADM_API tadm_status tadm_pages_scratch_size(int pages, int n_seqs, size_t* bytes);
+
+/* Gives the sequences seqs[i] (int32 [n]) the pages that they lack for
+ * new_len[i] tokens: list order, then position order.  Pages that they hold stay.
+ * lens is not changed. */
+TADM_API tadm_status tadm_pages_reserve(const int32_t* tables, const int32_t* refs, int pages, int n_seqs, int ld_table,
+                                        const int32_t* seqs, const int32_t* new_len, int n, int32_t* tables_out,
+                                        int32_t* refs_out, int32_t* status, void* scratch, size_t scratch_bytes,
+                                        tadm_stream stream);
+
+/* Sequence dst[i], which holds no page, becomes a copy of src[i] (int32 [n]; a
+ * source may be listed often, a target once and not as a source): pages that
+ * its lens[src[i]] tokens fill are shared, a last page that they do not fill
+ * is copied, in every layer, to a page of its own, so that either sequence
+ * can go on writing. */
+TADM_API tadm_status tadm_pages_fork(const tadm_page_pool* pool, const int32_t* tables, const int32_t* lens,
+                                     const int32_t* refs, int n_seqs, int ld_table, const int32_t* src,
+                                     const int32_t* dst, int n, int32_t* tables_out, int32_t* lens_out,
+                                     int32_t* refs_out, int32_t* status, void* scratch, size_t scratch_bytes,
+                                     tadm_stream stream);
+
+/* The sequences seqs[i] (int32 [n]) give their pages back; their lens become 0. */
+TADM_API tadm_status tadm_pages_free(const int32_t* tables, const int32_t* lens, const int32_t* refs, int pages,
+                                     int n_seqs, int ld_table, const int32_t* seqs, int n, int32_t* tables_out,
+                                     int32_t* lens_out, int32_t* refs_out, int32_t* status, void* scratch,
+                                     size_t scratch_bytes, tadm_stream stream);
+
+/* Moves the n_live pages in use to the ids 0 .. n_live - 1, in every layer: the
+ * i-th page in use above them takes the i-th free id below (both ascending);
+ * tables and refs follow (n_live: int32 [1]; table entries that are no page id stay). */
+TADM_API tadm_status tadm_pages_compact(const tadm_page_pool* pool, const int32_t* tables, const int32_t* refs,
+                                        int n_seqs, int ld_table, int32_t* tables_out, int32_t* refs_out,
+                                        int32_t* n_live, void* scratch, size_t scratch_bytes, tadm_stream stream);
+
+/* Copies page src[i] onto page dst[i] (int32 [n]) in every layer, scales
+ * included.  A target is listed once and is no source; pairs with an id out of
+ * range are left out. */
+TADM_API tadm_status tadm_pages_copy(const tadm_page_pool* pool, const int32_t* src, const int32_t* dst, int n,
+                                     tadm_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,188 @@
+// Attention of packed rows on the CUDA cores: over the rows of their own
+// sequence, or over a sequence's pages of the 8-bit cache.
+//
+// A block takes 16 virtual rows (row-major, then the query heads of one KV
+// head, so that a key tile serves all of them) of one sequence and walks its
+// visible keys in tiles of 64: K and V as fp32 in shared memory, a warp per
+// two virtual rows, two keys per lane for the scores, four or two dims per
+// lane for P V.  Everything is fp32: scores, running maximum and sum
+// (online softmax), accumulators.
+#include <cuda_fp8.h>
+
+#include <type_traits>
+
+#include "ragged.cuh"
+#include "serve.h"
+
+namespace tadm {
+namespace {
+
+constexpr int RT = 16, KT = 64, NT = 256;     // virtual rows and keys of a tile, threads
+static_assert(KT == TADM_PAGE_TOKENS, "a key tile is a page");
+
+struct RowsAttnArgs {
+  const void *q, *k, *v;
+  void* o;
+  const uint8_t *pk, *pv;
+  const float *sk, *sv;
+  const int32_t *cu, *lens, *table;
+  int batch, total, max_rows, max_len, ld_table, pages;
+  int n_heads, n_kv;
+  int64_t ldq, ldk, ldv, ldo;
+  int causal, window;
+  float scale;
+};
+
+template <class T, bool PAGED, int HD>
+__global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
+  pdl_enter();
+  constexpr int LD = HD + 4, PL = HD / 32;
+  extern __shared__ __align__(16) float sm[];
+  float* sK = sm;                      // [KT][LD]
+  float* sV = sK + KT * LD;            // [KT][LD]
+  float* sQ = sV + KT * LD;            // [RT][HD]
+  float* sP = sQ + RT * HD;            // [RT][KT]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int group = a.n_heads / a.n_kv, hk = blockIdx.y;
+  int t;
+  const int b = find_tile(a.batch, blockIdx.x, [&](int i) {
+    return (static_cast<int64_t>(seq_rows(a.cu, i, a.total, a.max_rows).n) * group + RT - 1) / RT;
+  }, &t);
+  if (b < 0) return;
+  const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
+  const int n_virt = rows.n * group, v0 = t * RT;
+  const int len = PAGED ? min(max(a.lens[b], 0), a.max_len) : rows.n;
+  const int pos0 = len - rows.n;                       // position of row 0
+  // keys that any row of the tile sees
+  const int r_lo = v0 / group, r_hi = (min(v0 + RT, n_virt) - 1) / group;
+  const int k_end = a.causal ? max(0, min(len, pos0 + r_hi + 1)) : len;
+  const int k_begin = a.window > 0 ? max(0, pos0 + r_lo - a.window + 1) : 0;
+  for (int i = tid; i < RT * HD; i += NT) {
+    const int v = v0 + i / HD;
+    const T* q = static_cast<const T*>(a.q);
+    sQ[i] = v < n_virt ? to_f32(q[(rows.first + v / group) * a.ldq + static_cast<int64_t>(hk * group + v % group) * HD + i % HD]) : 0.0f;
+  }
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, acc[2][PL] = {};
+  for (int k0 = k_begin / KT * KT; k0 < k_end; k0 += KT) {
+    __syncthreads();
+    if (PAGED) {
+      const int slot = k0 / KT;
+      const int page = slot < a.ld_table ? a.table[static_cast<int64_t>(b) * a.ld_table + slot] : -1;
+      const bool ok = page >= 0 && page < a.pages;
+      const int64_t ph = static_cast<int64_t>(ok ? page : 0) * a.n_kv + hk;
+      const float ks = ok ? a.sk[ph] : 0.0f, vs = ok ? a.sv[ph] : 0.0f;
+      const uint8_t *pk = a.pk + ph * KT * HD, *pv = a.pv + ph * KT * HD;
+      auto dec = [](uint8_t x) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(x, __NV_E4M3))); };
+      for (int i = tid; i < KT * HD; i += NT) {
+        const int kr = i / HD, kc = i % HD, vt = i % KT, vd = i / KT;
+        sK[kr * LD + kc] = ok && k0 + kr < len ? dec(pk[i]) * ks : 0.0f;
+        sV[vt * LD + vd] = ok && k0 + vt < len ? dec(pv[i]) * vs : 0.0f;   // slots past the length may hold anything
+      }
+    } else {
+      const T *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
+      for (int i = tid; i < KT * HD; i += NT) {
+        const int r = i / HD, c = i % HD;
+        const int64_t row = rows.first + k0 + r;
+        sK[r * LD + c] = k0 + r < len ? to_f32(k[row * a.ldk + static_cast<int64_t>(hk) * HD + c]) : 0.0f;
+        sV[r * LD + c] = k0 + r < len ? to_f32(v[row * a.ldv + static_cast<int64_t>(hk) * HD + c]) : 0.0f;
+      }
+    }
+    __syncthreads();
+    float s[2][2] = {};                                // [row][key half]
+#pragma unroll 4
+    for (int c = 0; c < HD; c += 4) {
+      const float4 ka = *reinterpret_cast<const float4*>(sK + lane * LD + c);
+      const float4 kb = *reinterpret_cast<const float4*>(sK + (lane + 32) * LD + c);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 q = *reinterpret_cast<const float4*>(sQ + (2 * warp + i) * HD + c);
+        s[i][0] = fmaf(q.x, ka.x, fmaf(q.y, ka.y, fmaf(q.z, ka.z, fmaf(q.w, ka.w, s[i][0]))));
+        s[i][1] = fmaf(q.x, kb.x, fmaf(q.y, kb.y, fmaf(q.z, kb.z, fmaf(q.w, kb.w, s[i][1]))));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int v = v0 + 2 * warp + i, pos = pos0 + v / group;
+      const int hi = a.causal ? min(len, pos + 1) : len, lo = a.window > 0 ? pos - a.window + 1 : 0;
+      const bool see0 = v < n_virt && k0 + lane >= lo && k0 + lane < hi;
+      const bool see1 = v < n_virt && k0 + lane + 32 >= lo && k0 + lane + 32 < hi;
+      const float x0 = see0 ? s[i][0] * a.scale : -INFINITY, x1 = see1 ? s[i][1] * a.scale : -INFINITY;
+      const float mn = fmaxf(m[i], warp_max(fmaxf(x0, x1)));
+      const float f = m[i] == -INFINITY ? 0.0f : expf(m[i] - mn);
+      const float p0 = see0 ? expf(x0 - mn) : 0.0f, p1 = see1 ? expf(x1 - mn) : 0.0f;
+      sP[(2 * warp + i) * KT + lane] = p0;
+      sP[(2 * warp + i) * KT + lane + 32] = p1;
+      l[i] = l[i] * f + p0 + p1;                       // this lane's keys; the lanes' sums meet at the end
+#pragma unroll
+      for (int d = 0; d < PL; ++d) acc[i][d] *= f;
+      m[i] = mn;
+    }
+    __syncwarp();
+#pragma unroll 4
+    for (int j = 0; j < KT; ++j) {
+      float x[PL];
+#pragma unroll
+      for (int d = 0; d < PL; ++d) x[d] = sV[j * LD + 32 * d + lane];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float p = sP[(2 * warp + i) * KT + j];
+#pragma unroll
+        for (int d = 0; d < PL; ++d) acc[i][d] = fmaf(p, x[d], acc[i][d]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int v = v0 + 2 * warp + i;
+    const float sum = warp_sum(l[i]);
+    if (v >= n_virt) continue;
+    T* o = static_cast<T*>(a.o) + (rows.first + v / group) * a.ldo + static_cast<int64_t>(hk * group + v % group) * HD;
+#pragma unroll
+    for (int d = 0; d < PL; ++d) o[32 * d + lane] = from_f32<T>(sum == 0.0f ? 0.0f : acc[i][d] / sum);
+  }
+}
+
+template <class T, bool PAGED, int HD>
+const char* launch(const RaggedCall& c, cudaStream_t s) {
+  constexpr int smem = (2 * KT * (HD + 4) + RT * HD + RT * KT) * 4;
+  int dev = 0;
+  current_sms(&dev);
+  static PerDevice ready;
+  if (ready.get(dev, [] {
+        return cudaFuncSetAttribute(attn_rows_kernel<T, PAGED, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) ==
+                       cudaSuccess ? 1 : 0;
+      }) <= 0)
+    return "attention smem attribute failed";
+  RowsAttnArgs a{c.q, c.k, c.v, c.o, nullptr, nullptr, nullptr, nullptr, c.cu, c.lens, c.table, c.batch, c.total,
+                 c.max_rows, c.max_len, c.ld_table, 0, c.n_heads, c.n_kv, c.ldq, c.ldk, c.ldv, c.ldo, c.causal, c.window,
+                 1.0f / sqrtf(static_cast<float>(HD))};
+  if (PAGED) {
+    const tadm_page_pool& p = *c.pool;
+    const int64_t at = static_cast<int64_t>(c.layer) * p.pages * p.n_kv_heads;
+    a.pk = static_cast<const uint8_t*>(p.k) + at * KT * HD;
+    a.pv = static_cast<const uint8_t*>(p.v) + at * KT * HD;
+    a.sk = p.k_scale + at;
+    a.sv = p.v_scale + at;
+    a.pages = p.pages;
+  }
+  const int group = c.n_heads / c.n_kv;
+  // at most one tile per 16 virtual rows and one more per sequence
+  const int64_t tiles = static_cast<int64_t>(c.total) * group / RT + c.batch;
+  const cudaError_t e = launch_pdl(attn_rows_kernel<T, PAGED, HD>, dim3(static_cast<unsigned>(tiles), c.n_kv), NT, smem, s, a);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+
+}  // namespace
+
+const char* attention_rows(const RaggedCall& c, cudaStream_t s) {
+  if (c.batch == 0 || c.total == 0 || c.max_rows == 0) return nullptr;
+  auto hd = [&](auto t, auto paged) {
+    using T = decltype(t);
+    constexpr bool P = decltype(paged)::value;
+    return c.head_dim == 128 ? launch<T, P, 128>(c, s) : launch<T, P, 64>(c, s);
+  };
+  if (c.bf16) return c.pool ? hd(bf16{}, std::true_type{}) : hd(bf16{}, std::false_type{});
+  return c.pool ? hd(0.0f, std::true_type{}) : hd(0.0f, std::false_type{});
+}
+
+}  // namespace tadm

@@ -1,0 +1,678 @@
+// The paged 8-bit KV cache: rows into pages and back, and the pages' bookkeeping.
+//
+// A page holds 64 tokens of every KV head: K as [64, hd] and V transposed as
+// [hd, 64] e4m3 bytes (the operand layouts that attention reads), with one
+// fp32 scale for K and one for V per page and head.  Scales that this file
+// writes are powers of two: dividing by one and multiplying by it are exact,
+// e4m3 has an exponent of its own, so nothing is lost against a free scale
+// but at most one bit of its range, and a page's earlier tokens survive a
+// growing scale unchanged unless they fall below the smallest e4m3 step.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+#include <cstring>
+
+#include "serve.h"
+
+namespace tadm {
+namespace {
+
+constexpr int PT = TADM_PAGE_TOKENS;
+
+// ------------------------------------------------------------ rows <-> pages
+__device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }
+
+// The least power of two s in 2^-60 .. 2^60 with amax <= 448 s (448 = 1.75 * 2^8).
+__device__ __forceinline__ float needed_scale(float amax) {
+  const int bits = __float_as_int(amax);
+  const int e = (bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0);
+  return pow2f(min(60, max(-60, e)));
+}
+
+__device__ __forceinline__ uint32_t enc8(float x) {
+  const uint32_t q = __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+  return fabsf(x) <= 3.402823466e38f ? q : 0x7fu;     // infinities too become NaN
+}
+__device__ __forceinline__ float dec8(uint32_t b) {
+  return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(b), __NV_E4M3)));
+}
+
+// 8 consecutive elements as floats
+template <class T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float* p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+template <> __device__ __forceinline__ void load8<bf16>(const bf16* p, float (&x)[8]) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+template <class T> __device__ __forceinline__ void store8(T* p, const float (&x)[8]);
+template <> __device__ __forceinline__ void store8<float>(float* p, const float (&x)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+template <> __device__ __forceinline__ void store8<bf16>(bf16* p, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __nv_bfloat162 t = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<uint32_t*>(&t);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+struct RowsArgs {
+  uint8_t *pk, *pv;            // this layer's pages
+  float *sk, *sv;
+  void *k, *v;                 // rows (read by the write, written by the read)
+  const int32_t *cu, *start, *table;
+  int64_t ldk, ldv;
+  int batch, total, max_rows, ld_table, pages, n_kv, touched;
+};
+
+// What block (x, y) works on: sequence b, the page that holds its i-th touched
+// 64-token range, slots lo .. hi - 1 of it, which are rows row0 .. of the operand.
+struct Part {
+  int page, lo, hi;
+  int64_t row0;
+};
+__device__ __forceinline__ bool find_part(const RowsArgs& a, int x, Part* p) {
+  const int b = x / a.touched, i = x - b * a.touched;
+  const int c0 = min(max(a.cu[b], 0), a.total), c1 = min(max(a.cu[b + 1], c0), a.total);
+  const int n = min(c1 - c0, a.max_rows), s = a.start[b];
+  if (n <= 0 || s < 0) return false;
+  const int64_t slot = static_cast<int64_t>(s / PT) + i, first = slot * PT;
+  const int64_t end = static_cast<int64_t>(s) + n;
+  if (first >= end || slot >= a.ld_table) return false;
+  p->page = a.table[static_cast<int64_t>(b) * a.ld_table + slot];
+  if (p->page < 0 || p->page >= a.pages) return false;
+  p->lo = static_cast<int>(max(static_cast<int64_t>(s), first) - first);
+  p->hi = static_cast<int>(min(end, first + PT) - first);
+  p->row0 = c0 + first + p->lo - s;
+  return true;
+}
+
+// One block per (page, head, K or V): HD / 8 threads take a row, the rows stay
+// in registers between the maximum and the conversion, so they are read once.
+// V goes through shared memory to be transposed.
+template <class T, int HD>
+__global__ void __launch_bounds__(256) page_write_kernel(const RowsArgs a) {
+  pdl_enter();
+  constexpr int TPR = HD / 8, RPP = 256 / TPR, NP = PT / RPP;   // threads per row, rows per pass, passes
+  constexpr int LDT = PT + 4;                                   // bytes per dim of the transposed tile
+  __shared__ __align__(16) uint8_t tile[HD * LDT];
+  __shared__ float red[8];
+  Part p;
+  if (!find_part(a, blockIdx.x, &p)) return;
+  const int head = blockIdx.y >> 1, is_v = blockIdx.y & 1;
+  const int tid = threadIdx.x, r = tid / TPR, d = (tid % TPR) * 8, n = p.hi - p.lo;
+  const int64_t ld = is_v ? a.ldv : a.ldk;
+  const T* src = static_cast<const T*>(is_v ? a.v : a.k) + p.row0 * ld + static_cast<int64_t>(head) * HD + d;
+  float x[NP][8], amax = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int row = i * RPP + r;
+    if (row < n) {
+      load8<T>(src + row * ld, x[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NP; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = fabsf(x[i][e]);
+      amax = m <= 3.402823466e38f ? fmaxf(amax, m) : amax;
+    }
+  amax = warp_max(amax);
+  if ((tid & 31) == 0) red[tid >> 5] = amax;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) amax = fmaxf(amax, red[w]);
+  const int64_t ph = static_cast<int64_t>(p.page) * a.n_kv + head;
+  float* sp = (is_v ? a.sv : a.sk) + ph;
+  uint8_t* data = (is_v ? a.pv : a.pk) + ph * (PT * HD);
+  float scale = needed_scale(amax), again = 1.0f;
+  if (p.lo > 0) {
+    const float had = *sp;
+    if (scale > had) again = had / scale;
+    else scale = had;
+  }
+  const float inv = 1.0f / scale;
+  __syncthreads();                       // every thread has read the old scale
+  if (tid == 0 && (p.lo == 0 || again != 1.0f)) *sp = scale;
+  if (again != 1.0f) {                   // tokens that stay, in the new scale
+    if (is_v) {
+      for (int e = tid; e < HD * p.lo; e += 256) {
+        uint8_t* q = data + (e / p.lo) * PT + e % p.lo;
+        *q = static_cast<uint8_t>(enc8(dec8(*q) * again));
+      }
+    } else {
+      for (int e = tid; e < HD * p.lo; e += 256) data[e] = static_cast<uint8_t>(enc8(dec8(data[e]) * again));
+    }
+  }
+  const bool fresh = p.lo == 0;          // slots past the rows become zeros
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int row = i * RPP + r;
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e >> 2] |= enc8(x[i][e] * inv) << (8 * (e & 3));
+    if (is_v) {
+      if (fresh || row < n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) tile[(d + e) * LDT + row] = static_cast<uint8_t>(w[e >> 2] >> (8 * (e & 3)));
+      }
+    } else if (row < n || (fresh && row < PT)) {
+      *reinterpret_cast<uint2*>(data + (p.lo + row) * HD + d) = make_uint2(w[0], w[1]);
+    }
+  }
+  if (!is_v) return;
+  __syncthreads();
+  if (fresh) {
+    for (int c = tid; c < HD * (PT / 16); c += 256) {
+      const int dim = c >> 2, at = (c & 3) * 16;
+      const uint32_t* t = reinterpret_cast<const uint32_t*>(tile + dim * LDT + at);
+      *reinterpret_cast<uint4*>(data + dim * PT + at) = make_uint4(t[0], t[1], t[2], t[3]);
+    }
+  } else {
+    for (int e = tid; e < HD * n; e += 256) data[(e / n) * PT + p.lo + e % n] = tile[(e / n) * LDT + e % n];
+  }
+}
+
+template <class T, int HD>
+__global__ void __launch_bounds__(256) page_read_kernel(const RowsArgs a) {
+  pdl_enter();
+  constexpr int TPR = HD / 8, RPP = 256 / TPR;
+  constexpr int LDT = PT + 4;
+  __shared__ __align__(16) uint8_t tile[HD * LDT];
+  Part p;
+  if (!find_part(a, blockIdx.x, &p)) {
+    // rows of a page that the table does not hold read as zeros
+    const int b = blockIdx.x / a.touched, i = blockIdx.x - b * a.touched;
+    const int c0 = min(max(a.cu[b], 0), a.total), c1 = min(max(a.cu[b + 1], c0), a.total);
+    const int64_t n = min(c1 - c0, a.max_rows), s = a.start[b];
+    if (n <= 0 || s < 0) return;
+    const int64_t first = (s / PT + i) * PT;
+    const int64_t lo = max(first, s), hi = min(first + PT, s + n);
+    const int head = blockIdx.y >> 1, is_v = blockIdx.y & 1;
+    T* dst = static_cast<T*>(is_v ? a.v : a.k) + static_cast<int64_t>(head) * HD;
+    const int64_t ld = is_v ? a.ldv : a.ldk;
+    for (int64_t e = threadIdx.x; e < (hi - lo) * HD; e += 256) dst[(c0 + lo - s + e / HD) * ld + e % HD] = from_f32<T>(0.0f);
+    return;
+  }
+  const int head = blockIdx.y >> 1, is_v = blockIdx.y & 1;
+  const int tid = threadIdx.x, r = tid / TPR, d = (tid % TPR) * 8, n = p.hi - p.lo;
+  const int64_t ph = static_cast<int64_t>(p.page) * a.n_kv + head;
+  const float scale = (is_v ? a.sv : a.sk)[ph];
+  const uint8_t* data = (is_v ? a.pv : a.pk) + ph * (PT * HD);
+  const int64_t ld = is_v ? a.ldv : a.ldk;
+  T* dst = static_cast<T*>(is_v ? a.v : a.k) + p.row0 * ld + static_cast<int64_t>(head) * HD + d;
+  if (is_v) {
+    for (int c = tid; c < HD * (PT / 16); c += 256) {
+      const int dim = c >> 2, at = (c & 3) * 16;
+      const uint4 t = *reinterpret_cast<const uint4*>(data + dim * PT + at);
+      uint32_t* o = reinterpret_cast<uint32_t*>(tile + dim * LDT + at);
+      o[0] = t.x, o[1] = t.y, o[2] = t.z, o[3] = t.w;
+    }
+    __syncthreads();
+  }
+  for (int row = r; row < n; row += RPP) {
+    float x[8];
+    if (is_v) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = dec8(tile[(d + e) * LDT + p.lo + row]) * scale;
+    } else {
+      const uint2 t = *reinterpret_cast<const uint2*>(data + (p.lo + row) * HD + d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = dec8(((e < 4 ? t.x : t.y) >> (8 * (e & 3))) & 0xff) * scale;
+    }
+    store8<T>(dst + row * ld, x);
+  }
+}
+
+template <class T, int HD>
+cudaError_t launch_rows(const RowsArgs& a, bool write, cudaStream_t s) {
+  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.batch) * a.touched), 2 * a.n_kv);
+  return write ? launch_pdl(page_write_kernel<T, HD>, grid, 256, 0, s, a) : launch_pdl(page_read_kernel<T, HD>, grid, 256, 0, s, a);
+}
+
+// ------------------------------------------------------------- bookkeeping
+// Every call is two launches: one block plans (checks, counts, prefix sums in
+// list order, the free list lowest id first), then a grid applies the plan to
+// the tables and moves the pages.  The plan lives in the caller's scratch.
+constexpr int PB = 1024;      // threads of the planning block
+
+struct Plan {
+  int status, n_copies, pad[2];
+};
+struct Scratch {
+  Plan* plan;
+  int *mark;                        // [n_seqs] 1 + list index of a listed (target) sequence, 0 for the others
+  int *first, *count, *offset;      // [n_seqs] per list entry: first slot that gets a new page, how many, where in fresh
+  int *fresh;                       // [pages] free pages taken, in order
+  int *from, *to;                   // [pages] page copies
+  int *map;                         // [pages] new id of a page
+};
+size_t scratch_layout(int pages, int n_seqs, char* base, Scratch* s) {
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t o = at;
+    at += (4 * n + 15) / 16 * 16;
+    return reinterpret_cast<int*>(base + o);
+  };
+  Scratch t;
+  t.plan = reinterpret_cast<Plan*>(take(4));
+  t.mark = take(n_seqs), t.first = take(n_seqs), t.count = take(n_seqs), t.offset = take(n_seqs);
+  t.fresh = take(pages), t.from = take(pages), t.to = take(pages), t.map = take(pages);
+  if (s) *s = t;
+  return at;
+}
+
+// Exclusive prefix sum of v over the block; *total is the block's sum.  Every thread calls it.
+__device__ __forceinline__ int block_scan(int v, int* total) {
+  __shared__ int ws[PB / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) ws[warp] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < PB / 32; ++w) {
+    const int y = ws[w];
+    if (w < warp) before += y;
+    all += y;
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// The first `want` pages without a reference, ascending, into fresh; returns how many there are (at most want).
+__device__ int take_free(const int32_t* refs, int pages, int want, int* fresh) {
+  int have = 0;
+  for (int base = 0; base < pages && have < want; base += 4 * PB) {
+    int free4 = 0, n = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int p = base + 4 * static_cast<int>(threadIdx.x) + e;
+      if (p < pages && refs[p] == 0) free4 |= 1 << e, ++n;
+    }
+    int total;
+    int at = have + block_scan(n, &total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (free4 >> e & 1) {
+        if (at < want) fresh[at] = base + 4 * static_cast<int>(threadIdx.x) + e;
+        ++at;
+      }
+    have += total;
+  }
+  return min(have, want);
+}
+
+__device__ __forceinline__ int pages_of(int tokens) { return tokens / PT + (tokens % PT != 0); }
+
+struct SeqArgs {
+  const int32_t *tables, *lens, *refs, *list, *list2;
+  int32_t *tables_out, *lens_out, *refs_out, *status;
+  int pages, n_seqs, ld, n;
+  Scratch sc;
+};
+
+// Marks the listed sequences; false where one is out of range or listed twice.
+__device__ bool mark_list(const SeqArgs& a, const int32_t* list) {
+  for (int i = threadIdx.x; i < a.n_seqs; i += PB) a.sc.mark[i] = 0;
+  __syncthreads();
+  bool ok = true;
+  for (int i = threadIdx.x; i < a.n; i += PB) {
+    const int s = list[i];
+    if (s < 0 || s >= a.n_seqs || atomicCAS(a.sc.mark + s, 0, i + 1) != 0) ok = false;
+  }
+  return __syncthreads_and(ok);
+}
+
+__device__ __forceinline__ void copy_refs(const SeqArgs& a) {
+  if (a.refs_out != a.refs)
+    for (int i = threadIdx.x; i < a.pages; i += PB) a.refs_out[i] = a.refs[i];
+}
+
+__device__ __forceinline__ void finish(const SeqArgs& a, int status, int copies) {
+  if (threadIdx.x == 0) {
+    a.sc.plan->status = status;
+    a.sc.plan->n_copies = status ? 0 : copies;
+    *a.status = status;
+  }
+}
+
+// How many pages sequence s holds (its row's entries before the first -1), by one warp.
+__device__ __forceinline__ int held(const SeqArgs& a, int s) {
+  const int32_t* row = a.tables + static_cast<int64_t>(s) * a.ld;
+  for (int i = 0; i < a.ld; i += 32) {
+    const int j = i + (threadIdx.x & 31);
+    const unsigned none = __ballot_sync(0xffffffffu, j >= a.ld || row[j] < 0);
+    if (none) return i + __ffs(none) - 1;
+  }
+  return a.ld;
+}
+
+__global__ void __launch_bounds__(PB) plan_reserve_kernel(const SeqArgs a) {
+  pdl_enter();
+  int status = mark_list(a, a.list) ? 0 : TADM_PAGES_BAD;
+  bool ok = true;
+  if (!status)
+    for (int i = threadIdx.x >> 5; i < a.n; i += PB / 32) {
+      const int have = held(a, a.list[i]), want = a.list2[i];
+      if (want < 0 || pages_of(want) > a.ld) ok = false;
+      if ((threadIdx.x & 31) == 0) {
+        a.sc.first[i] = have;
+        a.sc.count[i] = max(0, pages_of(max(want, 0)) - have);
+      }
+    }
+  if (!__syncthreads_and(ok)) status = TADM_PAGES_BAD;
+  int need = 0;
+  for (int base = 0; !status && base < a.n; base += PB) {
+    const int i = base + threadIdx.x;
+    int total;
+    // a sum past the pool saturates (each term and the pool are below 2^31 / PB after the clamp)
+    const int at = block_scan(i < a.n ? min(a.sc.count[i], min(a.pages, (1 << 20)) + 1) : 0, &total);
+    if (i < a.n) a.sc.offset[i] = need + at;
+    need = total > a.pages - need ? a.pages + 1 : need + total;
+    if (need > a.pages) status = TADM_PAGES_SHORT;
+  }
+  __syncthreads();
+  if (!status && take_free(a.refs, a.pages, need, a.sc.fresh) < need) status = TADM_PAGES_SHORT;
+  __syncthreads();
+  copy_refs(a);
+  __syncthreads();
+  if (!status)
+    for (int k = threadIdx.x; k < need; k += PB) a.refs_out[a.sc.fresh[k]] = 1;
+  finish(a, status, 0);
+}
+
+__global__ void __launch_bounds__(PB) plan_fork_kernel(const SeqArgs a) {
+  pdl_enter();
+  int status = mark_list(a, a.list2) ? 0 : TADM_PAGES_BAD;
+  bool ok = true;
+  if (!status)
+    for (int i = threadIdx.x >> 5; i < a.n; i += PB / 32) {     // a warp per list entry
+      const int s = a.list[i], d = a.list2[i];
+      const bool in = s >= 0 && s < a.n_seqs && a.sc.mark[s] == 0;
+      const int len = in ? a.lens[s] : -1, np = len < 0 ? 0 : pages_of(len);
+      if (len < 0 || np > a.ld || a.tables[static_cast<int64_t>(d) * a.ld] >= 0) {
+        ok = false;
+        continue;
+      }
+      const int32_t* row = a.tables + static_cast<int64_t>(s) * a.ld;
+      for (int j = threadIdx.x & 31; j < np; j += 32) {
+        const int p = row[j];
+        if (p < 0 || p >= a.pages || a.refs[p] <= 0) ok = false;
+      }
+      if ((threadIdx.x & 31) == 0) {
+        a.sc.count[i] = len % PT != 0;
+        a.sc.first[i] = len / PT;
+      }
+    }
+  if (!__syncthreads_and(ok)) status = TADM_PAGES_BAD;
+  int need = 0;
+  for (int base = 0; !status && base < a.n; base += PB) {
+    const int i = base + threadIdx.x;
+    int total;
+    const int at = block_scan(i < a.n ? a.sc.count[i] : 0, &total);
+    if (i < a.n) a.sc.offset[i] = need + at;
+    need += total;
+  }
+  __syncthreads();
+  if (!status && (need > a.pages || take_free(a.refs, a.pages, need, a.sc.fresh) < need)) status = TADM_PAGES_SHORT;
+  __syncthreads();
+  copy_refs(a);
+  __syncthreads();
+  if (!status)
+    for (int i = threadIdx.x; i < a.n; i += PB)
+      if (a.sc.count[i]) {
+        const int k = a.sc.offset[i], page = a.sc.fresh[k];
+        a.refs_out[page] = 1;
+        a.sc.from[k] = a.tables[static_cast<int64_t>(a.list[i]) * a.ld + a.sc.first[i]];
+        a.sc.to[k] = page;
+      }
+  finish(a, status, need);
+}
+
+__global__ void __launch_bounds__(PB) plan_free_kernel(const SeqArgs a) {
+  pdl_enter();
+  int status = mark_list(a, a.list) ? 0 : TADM_PAGES_BAD;
+  copy_refs(a);
+  __syncthreads();
+  if (!status) {
+    // references go down; one that falls below 0 (or an id out of range) takes all of them back
+    auto each = [&](auto f) {
+      for (int i = threadIdx.x >> 5; i < a.n; i += PB / 32) {
+        const int32_t* row = a.tables + static_cast<int64_t>(a.list[i]) * a.ld;
+        const int n = held(a, a.list[i]);
+        for (int j = threadIdx.x & 31; j < n; j += 32) f(row[j]);
+      }
+    };
+    bool ok = true;
+    each([&](int p) {
+      if (p >= a.pages) ok = false;
+      else if (atomicSub(a.refs_out + p, 1) <= 0) ok = false;
+    });
+    if (!__syncthreads_and(ok)) {
+      status = TADM_PAGES_BAD;
+      each([&](int p) { if (p < a.pages) atomicAdd(a.refs_out + p, 1); });
+    }
+  }
+  finish(a, status, 0);
+}
+
+__global__ void __launch_bounds__(PB) plan_compact_kernel(const SeqArgs a) {
+  pdl_enter();
+  int live = 0;
+  for (int base = 0; base < a.pages; base += PB) {
+    const int p = base + threadIdx.x;
+    live += __syncthreads_count(p < a.pages && a.refs[p] > 0);
+  }
+  // the i-th hole below `live` and the i-th page in use from there on
+  int holes = 0, movers = 0;
+  for (int base = 0; base < a.pages; base += PB) {
+    const int p = base + threadIdx.x;
+    const bool used = p < a.pages && a.refs[p] > 0;
+    const bool hole = p < live && !used, mover = used && p >= live;
+    int total;
+    const int at = block_scan((hole ? 1 : 0) | (mover ? 1 << 16 : 0), &total);   // at most 1024 of each
+    if (hole) a.sc.to[holes + (at & 0xffff)] = p;
+    if (mover) a.sc.from[movers + (at >> 16)] = p;
+    holes += total & 0xffff;
+    movers += total >> 16;
+    if (p < a.pages) a.sc.map[p] = p;
+  }
+  __syncthreads();
+  copy_refs(a);
+  __syncthreads();
+  for (int k = threadIdx.x; k < movers; k += PB) {
+    const int from = a.sc.from[k], to = a.sc.to[k];
+    a.refs_out[to] = a.refs[from];
+    a.sc.map[from] = to;
+  }
+  __syncthreads();                       // in place: every mover's count has been read
+  for (int k = threadIdx.x; k < movers; k += PB) a.refs_out[a.sc.from[k]] = 0;
+  if (threadIdx.x == 0) {
+    a.sc.plan->status = 0;
+    a.sc.plan->n_copies = movers;
+    *a.status = live;
+  }
+}
+
+// Copies pages from[i] -> to[i], i < *n (n_max where n is null), in every layer: 16-byte vectors in chunks of 4 KB,
+// four chunks of a block in flight.
+struct CopyArgs {
+  uint4 *k, *v;
+  float *sk, *sv;
+  const int *from, *to, *n;
+  int n_max, layers, pages, n_kv;
+  int page_chunks;                 // chunks of 256 vectors per page and layer
+};
+__device__ __forceinline__ bool pair_ok(const CopyArgs& c, int from, int to) {
+  return from >= 0 && from < c.pages && to >= 0 && to < c.pages;
+}
+__device__ void copy_pages(const CopyArgs& c, int block, int blocks) {
+  const int n = c.n ? *c.n : c.n_max;
+  const int64_t per = static_cast<int64_t>(c.layers) * 2 * c.page_chunks, total = n * per;
+  constexpr int U = 4;
+  for (int64_t base = static_cast<int64_t>(block) * U; base < total; base += static_cast<int64_t>(blocks) * U) {
+    uint4 x[U];
+    uint4* dst[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      dst[u] = nullptr;
+      const int64_t id = base + u;
+      if (id >= total) continue;
+      const int i = static_cast<int>(id / per);
+      const int in = static_cast<int>(id - i * per), unit = in / c.page_chunks, chunk = in - unit * c.page_chunks;
+      const int from = c.from[i], to = c.to[i];
+      if (!pair_ok(c, from, to)) continue;
+      uint4* base_p = (unit & 1) ? c.v : c.k;
+      const int64_t layer = static_cast<int64_t>(unit >> 1) * c.pages;
+      const int64_t at = static_cast<int64_t>(chunk) * 256 + threadIdx.x;
+      x[u] = base_p[(layer + from) * c.page_chunks * 256 + at];
+      dst[u] = base_p + (layer + to) * c.page_chunks * 256 + at;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (dst[u]) *dst[u] = x[u];
+  }
+  const int64_t ns = static_cast<int64_t>(n) * c.layers * c.n_kv;
+  for (int64_t e = static_cast<int64_t>(block) * 256 + threadIdx.x; e < ns; e += static_cast<int64_t>(blocks) * 256) {
+    const int i = static_cast<int>(e / (c.layers * c.n_kv));
+    const int in = static_cast<int>(e - static_cast<int64_t>(i) * c.layers * c.n_kv), l = in / c.n_kv, h = in - l * c.n_kv;
+    const int from = c.from[i], to = c.to[i];
+    if (!pair_ok(c, from, to)) continue;
+    const int64_t src = (static_cast<int64_t>(l) * c.pages + from) * c.n_kv + h;
+    const int64_t dst = (static_cast<int64_t>(l) * c.pages + to) * c.n_kv + h;
+    c.sk[dst] = c.sk[src];
+    c.sv[dst] = c.sv[src];
+  }
+}
+
+__global__ void __launch_bounds__(256) copy_pages_kernel(const CopyArgs c) {
+  pdl_enter();
+  copy_pages(c, blockIdx.x, gridDim.x);
+}
+
+enum { OP_RESERVE, OP_FORK, OP_FREE, OP_COMPACT };
+
+// The planned tables, and the page copies.
+template <int OP>
+__global__ void __launch_bounds__(256) apply_kernel(const SeqArgs a, const CopyArgs c) {
+  pdl_enter();
+  const bool ok = a.sc.plan->status == 0, same = a.tables_out == a.tables;
+  const int64_t entries = static_cast<int64_t>(a.n_seqs) * a.ld;
+  for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < entries; e += static_cast<int64_t>(gridDim.x) * 256) {
+    const int row = static_cast<int>(e / a.ld), slot = static_cast<int>(e - static_cast<int64_t>(row) * a.ld);
+    if (OP == OP_COMPACT) {
+      const int p = a.tables[e];
+      a.tables_out[e] = p >= 0 && p < a.pages ? a.sc.map[p] : p;
+      continue;
+    }
+    const int i = ok ? a.sc.mark[row] - 1 : -1;
+    if (i < 0) {
+      if (!same) a.tables_out[e] = a.tables[e];
+    } else if (OP == OP_FREE) {
+      a.tables_out[e] = -1;
+    } else if (OP == OP_RESERVE) {
+      const int k = slot - a.sc.first[i];
+      if (k >= 0 && k < a.sc.count[i]) a.tables_out[e] = a.sc.fresh[a.sc.offset[i] + k];
+      else if (!same) a.tables_out[e] = a.tables[e];
+    } else {
+      int p = -1;
+      if (slot < a.sc.first[i]) {                               // a page that the source's tokens fill
+        p = a.tables[static_cast<int64_t>(a.list[i]) * a.ld + slot];
+        atomicAdd(a.refs_out + p, 1);
+      } else if (slot == a.sc.first[i] && a.sc.count[i]) {
+        p = a.sc.fresh[a.sc.offset[i]];
+      }
+      a.tables_out[e] = p;
+    }
+  }
+  if (OP == OP_FORK || OP == OP_FREE)
+    for (int row = blockIdx.x * 256 + threadIdx.x; row < a.n_seqs; row += gridDim.x * 256) {
+      const int i = ok ? a.sc.mark[row] - 1 : -1;
+      if (i >= 0) a.lens_out[row] = OP == OP_FREE ? 0 : a.lens[a.list[i]];
+      else if (a.lens_out != a.lens) a.lens_out[row] = a.lens[row];
+    }
+  if (OP == OP_FORK || OP == OP_COMPACT) copy_pages(c, blockIdx.x, gridDim.x);
+}
+
+CopyArgs copy_args(const tadm_page_pool& p, const int* from, const int* to, const int* n, int n_max) {
+  return CopyArgs{static_cast<uint4*>(p.k), static_cast<uint4*>(p.v), p.k_scale, p.v_scale, from, to, n, n_max,
+                  p.layers, p.pages, p.n_kv_heads, p.n_kv_heads * PT * p.head_dim / 4096};
+}
+
+// Blocks for `bytes` of copying and `entries` of tables: 16 KB or 256 entries each, at most eight per SM.
+int apply_grid(int64_t bytes, int64_t entries) {
+  int dev = 0;
+  const int64_t most = 8LL * current_sms(&dev);
+  return static_cast<int>(std::max<int64_t>(1, std::min(most, std::max(bytes / 16384, entries / 256) + 1)));
+}
+
+template <int OP>
+const char* run_pages(const PagesCall& c, cudaStream_t s, void (*plan)(SeqArgs)) {
+  Scratch sc;
+  scratch_layout(c.pages, c.n_seqs, static_cast<char*>(c.scratch), &sc);
+  const SeqArgs a{c.tables, c.lens, c.refs, c.list, c.list2, c.tables_out, c.lens_out, c.refs_out, c.status,
+                  c.pages, c.n_seqs, c.ld_table, c.n, sc};
+  CopyArgs cp{};
+  int64_t bytes = 0;
+  if (c.pool) {
+    cp = copy_args(*c.pool, sc.from, sc.to, &sc.plan->n_copies, 0);
+    const int64_t most = OP == OP_FORK ? c.n : c.pages / 2;
+    bytes = most * 2 * c.pool->layers * cp.page_chunks * 4096;
+  }
+  cudaError_t e = launch_pdl(plan, 1, PB, 0, s, a);
+  if (e == cudaSuccess)
+    e = launch_pdl(apply_kernel<OP>, apply_grid(bytes, static_cast<int64_t>(c.n_seqs) * c.ld_table), 256, 0, s, a, cp);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+
+}  // namespace
+
+const char* page_rows(const PageRowsCall& c, bool write, cudaStream_t s) {
+  if (c.batch == 0 || c.max_rows == 0) return nullptr;
+  const tadm_page_pool& p = *c.pool;
+  const int64_t page = static_cast<int64_t>(p.pages) * p.n_kv_heads;
+  RowsArgs a{static_cast<uint8_t*>(p.k) + c.layer * page * PT * p.head_dim,
+             static_cast<uint8_t*>(p.v) + c.layer * page * PT * p.head_dim,
+             p.k_scale + c.layer * page, p.v_scale + c.layer * page, c.k, c.v, c.cu, c.start, c.table, c.ldk, c.ldv,
+             c.batch, c.total, c.max_rows, c.ld_table, p.pages, p.n_kv_heads, (c.max_rows + PT - 2) / PT + 1};
+  cudaError_t e;
+  if (p.head_dim == 128) e = c.bf16 ? launch_rows<bf16, 128>(a, write, s) : launch_rows<float, 128>(a, write, s);
+  else e = c.bf16 ? launch_rows<bf16, 64>(a, write, s) : launch_rows<float, 64>(a, write, s);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+
+size_t pages_scratch(int pages, int n_seqs) { return scratch_layout(pages, n_seqs, nullptr, nullptr); }
+const char* pages_reserve(const PagesCall& c, cudaStream_t s) { return run_pages<OP_RESERVE>(c, s, plan_reserve_kernel); }
+const char* pages_fork(const PagesCall& c, cudaStream_t s) { return run_pages<OP_FORK>(c, s, plan_fork_kernel); }
+const char* pages_free(const PagesCall& c, cudaStream_t s) { return run_pages<OP_FREE>(c, s, plan_free_kernel); }
+const char* pages_compact(const PagesCall& c, cudaStream_t s) { return run_pages<OP_COMPACT>(c, s, plan_compact_kernel); }
+const char* pages_copy(const tadm_page_pool& p, const int32_t* src, const int32_t* dst, int n, cudaStream_t s) {
+  if (n == 0) return nullptr;
+  const CopyArgs c = copy_args(p, src, dst, nullptr, n);
+  const cudaError_t e = launch_pdl(copy_pages_kernel, apply_grid(2LL * n * p.layers * c.page_chunks * 4096, 0), 256, 0, s, c);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+
+}  // namespace tadm

@@ -26,6 +26,9 @@ ABI_FUNCTIONS = [
     "tadm_head_confidence", "tadm_head_confidence_static", "tadm_probe_breakdown",
     "tadm_remdm_schedule", "tadm_remdm_uniforms", "tadm_remdm_update", "tadm_generate_remdm",
     "tadm_eb_update", "tadm_eb_scratch_bytes", "tadm_generate_entropy_bound",
+    "tadm_attention_packed", "tadm_page_write", "tadm_page_read", "tadm_page_attention_scratch_size",
+    "tadm_page_attention", "tadm_pages_scratch_size", "tadm_pages_reserve", "tadm_pages_fork", "tadm_pages_free",
+    "tadm_pages_compact", "tadm_pages_copy",
 ]
 
 
@@ -53,6 +56,12 @@ class tadm_counters(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in (
         "shared_layers", "anchor_layers", "denoise_layers", "anchor_calls", "denoise_steps", "commit_passes",
         "kernel_launches")]
+
+
+class tadm_page_pool(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in (
+                    "layers", "pages", "n_kv_heads", "head_dim")]
 
 
 class tadm_plan_event(ctypes.Structure):
@@ -112,6 +121,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "tadm_eb_scratch_bytes": (I, [P, I, I, I, ctypes.POINTER(SZ)]),
         "tadm_generate_entropy_bound": (I, [P, P, I, I, P, I, I, I, ctypes.c_double, ctypes.c_double,
                                             ctypes.c_double, I, ctypes.c_uint64, P, SZ, P]),
+        "tadm_attention_packed": (I, [P] * 5 + [I] * 6 + [I64] * 4 + [I] * 3 + [P]),
+        "tadm_page_write": (I, [P, I, P, P, P, P, I, I, I, I64, I64, P, I, I, P]),
+        "tadm_page_read": (I, [P, I, P, P, P, P, I, I, I, I64, I64, P, I, I, P]),
+        "tadm_page_attention_scratch_size": (I, [I] * 8 + [ctypes.POINTER(SZ)]),
+        "tadm_page_attention": (I, [P, P, I, P, P, P, I, I, I, I, I, I64, I64, P, I, I, I, I, P, SZ, P]),
+        "tadm_pages_scratch_size": (I, [I, I, ctypes.POINTER(SZ)]),
+        "tadm_pages_reserve": (I, [P, P, I, I, I, P, P, I, P, P, P, P, SZ, P]),
+        "tadm_pages_fork": (I, [P, P, P, P, I, I, P, P, I, P, P, P, P, P, SZ, P]),
+        "tadm_pages_free": (I, [P, P, P, I, I, I, P, I, P, P, P, P, P, SZ, P]),
+        "tadm_pages_compact": (I, [P, P, P, I, I, P, P, P, P, SZ, P]),
+        "tadm_pages_copy": (I, [P, P, P, I, P]),
         "tadm_probe_breakdown": (I, [P, I, ctypes.POINTER(I64), ctypes.POINTER(ctypes.c_double),
                                      ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]),
         "tadm_probe_read": (I, [P, ctypes.POINTER(I64), ctypes.POINTER(ctypes.c_double),
@@ -278,6 +298,193 @@ def tadm_eb_update(z, logits, first_gen: int, mask_id: int, tau: float, eta: flo
                                          tau, eta, int(bool(last)), seed, step, _ptr(entropy),
                                          _ptr(probs) if probs is not None else None, p_dtype,
                                          probs.shape[1] if probs is not None else 0, _ptr(z_sum), _stream(stream)))
+
+
+# ------------------------------------------------ sequences of different lengths
+PAGE_TOKENS = 64
+
+
+class PagePool:
+    """The 8-bit KV cache's pages: e4m3 bytes k [layers, pages, kv heads, 64, hd]
+    and v [layers, pages, kv heads, hd, 64], fp32 scales [layers, pages, kv
+    heads].  Holds references to the tensors that it is made of."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        layers, pages, n_kv, tokens, hd = k.shape
+        if tokens != PAGE_TOKENS or tuple(v.shape) != (layers, pages, n_kv, hd, tokens):
+            raise TadmError(1, f"pages have shapes {tuple(k.shape)} and {tuple(v.shape)}")
+        for s in (k_scale, v_scale):
+            if tuple(s.shape) != (layers, pages, n_kv) or str(s.dtype) != "torch.float32":
+                raise TadmError(1, f"scales must be fp32 {(layers, pages, n_kv)}")
+        for t in (k, v, k_scale, v_scale):
+            if not t.is_contiguous() or not t.is_cuda or t.device != k.device:
+                raise TadmError(1, "a pool's tensors must be contiguous CUDA tensors of one device")
+        if k.element_size() != 1 or v.element_size() != 1:
+            raise TadmError(1, "pages hold one byte per element")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.layers, self.pages, self.n_kv_heads, self.head_dim = layers, pages, n_kv, hd
+        self.c = tadm_page_pool(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), layers, pages,
+                                n_kv, hd)
+        self.ref = ctypes.addressof(self.c)
+
+    @classmethod
+    def empty(cls, layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
+        """Pages that hold zeros."""
+        import torch
+        z = lambda shape, dt: torch.zeros(shape, dtype=dt, device=device)  # noqa: E731
+        return cls(z((layers, pages, n_kv_heads, PAGE_TOKENS, head_dim), torch.uint8),
+                   z((layers, pages, n_kv_heads, head_dim, PAGE_TOKENS), torch.uint8),
+                   z((layers, pages, n_kv_heads), torch.float32), z((layers, pages, n_kv_heads), torch.float32))
+
+
+_DTYPES = None
+
+
+def _rows_of(*tensors):
+    """The dtype code of row operands [rows, heads, hd]: fp32 or bf16, each row's heads dense, on one device."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+    first = tensors[0]
+    dtype = _DTYPES.get(first.dtype)
+    if dtype is None:
+        raise TadmError(1, f"rows must be fp32 or bf16, not {first.dtype}")
+    for t in tensors:
+        s = t.stride()
+        if t.dim() != 3 or s[2] != 1 or s[1] != t.shape[2] or t.dtype != first.dtype or not t.is_cuda:
+            raise TadmError(1, "rows must be CUDA tensors [rows, heads, head_dim] of one type with dense heads")
+    return dtype
+
+
+def _ints_of(*tensors):
+    for t in tensors:
+        if str(t.dtype) != "torch.int32" or not t.is_contiguous() or not t.is_cuda:
+            raise TadmError(1, "lengths, tables and lists must be contiguous int32 CUDA tensors")
+
+
+def tadm_attention_packed(q, k, v, o, cu_rows, max_rows: int, causal: bool = True, window: int = 0, stream=None):
+    """Attention of whole prompts packed one after the other: q, o [rows,
+    heads, hd], k, v [rows, kv heads, hd] (fp32 or bf16, rows may be strided),
+    cu_rows int32 [batch + 1]."""
+    dtype = _rows_of(q, k, v, o)
+    _ints_of(cu_rows)
+    rows, heads, hd = q.shape
+    if o.shape != q.shape or k.shape != v.shape or k.shape[0] != rows or k.shape[2] != hd:
+        raise TadmError(1, "shapes of q, k, v and o do not agree")
+    _check(load_library().tadm_attention_packed(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), cu_rows.data_ptr(), cu_rows.shape[0] - 1, rows,
+        max_rows, heads, k.shape[1], hd, q.stride(0), k.stride(0), v.stride(0), o.stride(0), int(causal), window,
+        dtype, _stream(stream)))
+
+
+def _page_rows(name, pool, layer, k, v, cu_rows, start, table, max_rows, stream):
+    dtype = _rows_of(k, v)
+    _ints_of(cu_rows, start, table)
+    if k.shape != v.shape or k.shape[1:] != (pool.n_kv_heads, pool.head_dim):
+        raise TadmError(1, "rows do not have the pool's heads")
+    batch = cu_rows.shape[0] - 1
+    if start.shape[0] != batch or table.shape[0] < batch:
+        raise TadmError(1, "start and table need an entry per sequence")
+    _check(getattr(load_library(), name)(
+        pool.ref, layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, k.shape[0], max_rows,
+        k.stride(0), v.stride(0), table.data_ptr(), table.shape[1], dtype, _stream(stream)))
+
+
+def tadm_page_write(pool, layer: int, k, v, cu_rows, start, table, max_rows: int, stream=None):
+    """Rows k, v [rows, kv heads, hd] become tokens start[b] .. of the cache (e4m3, a power-of-two scale per page and head)."""
+    _page_rows("tadm_page_write", pool, layer, k, v, cu_rows, start, table, max_rows, stream)
+
+
+def tadm_page_read(pool, layer: int, k, v, cu_rows, start, table, max_rows: int, stream=None):
+    """Tokens start[b] .. of the cache into the rows k, v [rows, kv heads, hd]."""
+    _page_rows("tadm_page_read", pool, layer, k, v, cu_rows, start, table, max_rows, stream)
+
+
+def tadm_page_attention_scratch_size(batch: int, total_rows: int, max_rows: int, max_len: int, n_heads: int,
+                                     n_kv_heads: int, head_dim: int, dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().tadm_page_attention_scratch_size(batch, total_rows, max_rows, max_len, n_heads, n_kv_heads,
+                                                           head_dim, dtype, ctypes.byref(n)))
+    return n.value
+
+
+def tadm_page_attention(q, pool, layer: int, o, cu_rows, lens, table, max_rows: int, max_len: int, scratch,
+                        causal: bool = False, window: int = 0, stream=None):
+    """Attention of packed rows q, o [rows, heads, hd] over the cache: sequence b
+    sees its first lens[b] tokens, its rows are the last ones of them."""
+    dtype = _rows_of(q, o)
+    _ints_of(cu_rows, lens, table)
+    rows, heads, hd = q.shape
+    batch = cu_rows.shape[0] - 1
+    if o.shape != q.shape or hd != pool.head_dim or lens.shape[0] != batch or table.shape[0] < batch:
+        raise TadmError(1, "shapes of q, o, lens, table and the pool do not agree")
+    _check(load_library().tadm_page_attention(
+        q.data_ptr(), pool.ref, layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
+        max_len, heads, q.stride(0), o.stride(0), table.data_ptr(), table.shape[1], int(causal), window, dtype,
+        _ptr(scratch), 0 if scratch is None else scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def tadm_pages_scratch_size(pages: int, n_seqs: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().tadm_pages_scratch_size(pages, n_seqs, ctypes.byref(n)))
+    return n.value
+
+
+def _seqs_of(tables, tables_out, per_seq, refs, refs_out, lists, status):
+    _ints_of(tables, tables_out, refs, refs_out, status, *per_seq, *lists)
+    if tables_out.shape != tables.shape or refs_out.shape != refs.shape or any(
+            t.shape[0] != tables.shape[0] for t in per_seq) or any(t.shape != lists[0].shape for t in lists):
+        raise TadmError(1, "shapes of tables, lens, refs and lists do not agree")
+
+
+def tadm_pages_reserve(tables, refs, seqs, new_len, tables_out, refs_out, status, scratch, stream=None):
+    """The pages that sequences seqs lack for new_len tokens, lowest free ids first."""
+    _seqs_of(tables, tables_out, (), refs, refs_out, (seqs, new_len), status)
+    _check(load_library().tadm_pages_reserve(
+        tables.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1], seqs.data_ptr(),
+        new_len.data_ptr(), seqs.shape[0], tables_out.data_ptr(), refs_out.data_ptr(), status.data_ptr(),
+        scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def tadm_pages_fork(pool, tables, lens, refs, src, dst, tables_out, lens_out, refs_out, status, scratch, stream=None):
+    """Sequences dst become copies of src: full pages shared, the last page copied."""
+    _seqs_of(tables, tables_out, (lens, lens_out), refs, refs_out, (src, dst), status)
+    if refs.shape[0] != pool.pages:
+        raise TadmError(1, "refs needs an entry per page")
+    _check(load_library().tadm_pages_fork(
+        pool.ref, tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1],
+        src.data_ptr(), dst.data_ptr(), src.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
+        status.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def tadm_pages_free(tables, lens, refs, seqs, tables_out, lens_out, refs_out, status, scratch, stream=None):
+    """Sequences seqs give their pages back."""
+    _seqs_of(tables, tables_out, (lens, lens_out), refs, refs_out, (seqs,), status)
+    _check(load_library().tadm_pages_free(
+        tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1],
+        seqs.data_ptr(), seqs.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
+        status.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def tadm_pages_compact(pool, tables, refs, tables_out, refs_out, n_live, scratch, stream=None):
+    """Pages in use move to the lowest ids; n_live int32 [1] gets their number."""
+    _seqs_of(tables, tables_out, (), refs, refs_out, (), n_live)
+    if refs.shape[0] != pool.pages:
+        raise TadmError(1, "refs needs an entry per page")
+    _check(load_library().tadm_pages_compact(
+        pool.ref, tables.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1], tables_out.data_ptr(),
+        refs_out.data_ptr(), n_live.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(),
+        _stream(stream)))
+
+
+def tadm_pages_copy(pool, src, dst, stream=None):
+    """Page src[i] onto page dst[i] in every layer."""
+    _ints_of(src, dst)
+    if src.shape != dst.shape:
+        raise TadmError(1, "src and dst differ in length")
+    _check(load_library().tadm_pages_copy(pool.ref, src.data_ptr(), dst.data_ptr(), src.shape[0], _stream(stream)))
+
 
 # ---------------------------------------------------------------------------- model handle
 class TadmModel:

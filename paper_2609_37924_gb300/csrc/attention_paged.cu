@@ -1,0 +1,862 @@
+// Attention of packed bf16 rows over the paged 8-bit cache, tcgen05.
+//
+//   S^T = K Q^T,  O^T = V^T P^T      (keys and head dims on the 128 MMA rows)
+//
+// The rows that read one KV head (query heads of its group x rows of a block
+// step or a single token) are few: 2 to 64 virtual rows.  They are the N of
+// both products here, so the tensor work follows their number (16, 32 or 64)
+// instead of being padded to 128, and a key is one TMEM lane = one thread,
+// whose page scales are two registers.
+//
+// A tile is 128 keys, two pages.  Roles of a CTA:
+//   warp 0      streams the pages with TMA (one 4-D map for K, one for V^T);
+//   warps 2-5   convert: e4m3 -> f16, exact, from shared memory into the TMEM
+//               A operands (K: a key per lane, V^T: a dim per lane); V slots
+//               past the sequence become zeros here;
+//   warp 1      S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
+//   warps 6-    softmax: a key per thread, the values of up to 32 rows in
+//               registers (four warps, or eight for 64 rows).  The running maximum of a row is a reference that moves only when
+//               a tile exceeds it by 2^8, so a tile costs one vote of these
+//               warps and no reduction over the keys; the sums of a row stay
+//               one partial per thread until the end of the work item.
+// Precision: Q enters as f16 scaled by one power of two per tile of rows
+// (exact for values within 2^-28 of the largest), K and V are exact, the
+// probabilities times the page's V scale are rounded to f16 (11 bits) with
+// the row's reference at 2^7 to 2^15, so that a probability 2^-21 of the
+// largest still has all of them; scores, sums and O are fp32.
+//
+// Work: the tiles of all (sequence, KV head, row tile) items lie on one line
+// that is cut evenly over the SMs, whatever the lengths; an item that a cut
+// splits leaves fp32 partials, which a second small kernel merges in order.
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "ragged.cuh"
+#include "serve.h"
+#include "tensor_map.h"
+
+namespace tadm {
+namespace {
+
+constexpr int PT = TADM_PAGE_TOKENS;
+constexpr int TK = 2 * PT;                 // keys of a tile
+
+struct PagedArgs {
+  const bf16* q;
+  bf16* o;
+  const float *sk, *sv;                    // this layer's scales
+  const int32_t *cu, *lens, *table;
+  int batch, total, max_rows, max_len, ld_table, pages;
+  int group, n_kv;
+  int64_t ldq, ldo;
+  int causal, window;
+  float scale_log2;                        // log2(e) / sqrt(hd)
+  float* part_o;                           // [2 * CTAs][N][HD]
+  float2* part_ml;                         // [2 * CTAs][N]: (reference in log2 units, sum)
+};
+
+// ------------------------------------------------------------------ work items
+struct SeqInfo {
+  int first, n_virt, len, pos0, n_rt;      // first row, virtual rows, tokens, position of row 0, row tiles
+};
+template <int N>
+__device__ __forceinline__ SeqInfo seq_info(const PagedArgs& a, int b) {
+  const SeqRows r = seq_rows(a.cu, b, a.total, a.max_rows);
+  const int len = min(max(a.lens[b], 0), a.max_len);
+  return {r.first, r.n * a.group, len, len - r.n, (r.n * a.group + N - 1) / N};
+}
+// The tiles that any row of row tile rt sees: first tile and how many (maybe none).
+template <int N>
+__device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s, int rt) {
+  const int r_lo = rt * N / a.group, r_hi = (min((rt + 1) * N, s.n_virt) - 1) / a.group;
+  const int end = a.causal ? max(0, min(s.len, s.pos0 + r_hi + 1)) : s.len;
+  const int begin = a.window > 0 ? max(0, s.pos0 + r_lo - a.window + 1) : 0;
+  const int t0 = begin / TK, t1 = (end + TK - 1) / TK;
+  return make_int2(t0, begin < end ? t1 - t0 : 0);
+}
+// Units of a sequence and KV head: its row tiles' tiles, at least one each (a row tile that sees nothing has zeros to write).
+template <int N>
+__device__ __forceinline__ int64_t seq_units(const PagedArgs& a, int b) {
+  const SeqInfo s = seq_info<N>(a, b);
+  if (s.n_virt <= 0) return 0;
+  if (!a.causal && a.window == 0) return static_cast<int64_t>(s.n_rt) * max(1, tile_range<N>(a, s, 0).y);
+  int64_t u = 0;
+  for (int rt = 0; rt < s.n_rt; ++rt) u += max(1, tile_range<N>(a, s, rt).y);
+  return u;
+}
+template <int N>
+__device__ __forceinline__ int64_t total_units(const PagedArgs& a) {      // warp-collective
+  int64_t u = 0;
+  for (int b = threadIdx.x & 31; b < a.batch; b += 32) u += seq_units<N>(a, b);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+  return u * a.n_kv;
+}
+struct Item {
+  int b, hk, rt, off;                      // off: units of the item before the place asked for
+};
+// The item that holds unit `unit` (< total_units).  Warp-collective.
+template <int N>
+__device__ __forceinline__ Item locate(const PagedArgs& a, int64_t unit) {
+  const int lane = threadIdx.x & 31;
+  Item it{0, 0, 0, 0};
+  int64_t before = 0;
+  for (int base = 0; base < a.batch; base += 32) {
+    const int b = base + lane;
+    const int64_t mine = b < a.batch ? seq_units<N>(a, b) : 0;
+    int64_t x = mine * a.n_kv;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, before + x > unit);
+    if (past) {
+      const int src = __ffs(past) - 1;
+      const int64_t per = __shfl_sync(0xffffffffu, mine, src);
+      int64_t in = unit - before - (__shfl_sync(0xffffffffu, x, src) - per * a.n_kv);
+      it.b = base + src;
+      it.hk = static_cast<int>(in / per);
+      in -= it.hk * per;
+      const SeqInfo s = seq_info<N>(a, it.b);
+      for (int rt = 0; rt < s.n_rt; ++rt) {
+        const int u = max(1, tile_range<N>(a, s, rt).y);
+        if (in < u) {
+          it.rt = rt;
+          it.off = static_cast<int>(in);
+          break;
+        }
+        in -= u;
+      }
+      return it;
+    }
+    before += __shfl_sync(0xffffffffu, x, 31);
+  }
+  return it;
+}
+
+// A CTA's walk over its units: one segment = consecutive tiles of one item.
+template <int N>
+struct Walk {
+  const PagedArgs& a;
+  Item it;
+  int64_t left;
+  SeqInfo s;
+  int t0, nt;              // tiles of the segment
+  bool from_start, to_end; // it begins / ends with its item
+  __device__ Walk(const PagedArgs& args, const Item& start, int64_t units) : a(args), it(start), left(units) {
+    if (left > 0) s = seq_info<N>(a, it.b);
+  }
+  __device__ bool next() {                 // false: no segment left
+    if (left <= 0) return false;
+    const int2 r = tile_range<N>(a, s, it.rt);
+    const int units = max(1, r.y);
+    const int take = static_cast<int>(min(left, static_cast<int64_t>(units - it.off)));
+    t0 = r.x + it.off;
+    nt = r.y > 0 ? take : 0;
+    from_start = it.off == 0;
+    to_end = it.off + take == units;
+    left -= take;
+    return true;
+  }
+  __device__ void advance() {              // to the next item, after the segment's work
+    it.off = 0;
+    if (++it.rt < s.n_rt) return;
+    it.rt = 0;
+    if (++it.hk < a.n_kv) return;
+    it.hk = 0;
+    if (left <= 0) return;
+    do {
+      s = seq_info<N>(a, ++it.b);
+    } while (s.n_virt <= 0 && it.b + 1 < a.batch);
+  }
+};
+__device__ __forceinline__ int64_t cut(int64_t total, int cta, int ctas) { return total * cta / ctas; }
+
+// ------------------------------------------------------------------ the kernel
+template <int HD_, int N_>
+struct PagedCfg {
+  static constexpr int HD = HD_, N = N_;
+  static constexpr int PAGE_BYTES = PT * HD;                 // of K or V^T, one head
+  static constexpr int STAGE_BYTES = 4 * PAGE_BYTES;         // two pages of K, two of V^T
+  static constexpr int STAGES = HD == 128 ? 5 : 8;
+  static constexpr int Q_BYTES = HD / 64 * N * 128;          // HD/64 atoms of N rows x 64 dims, f16
+  static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
+  static constexpr int RN = N < 32 ? N : 32, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
+  static constexpr int SM_THREADS = 128 * GROUPS;
+  static constexpr int MISC = 1024 + N * 64;
+  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + Q_BYTES + 2 * P_BYTES + MISC;
+  static constexpr int K_COL = 0, V_COL = 128, S_COL = 256, O_COL = 384;   // TMEM: two of K, V^T and S, one O
+  static constexpr int THREADS = 192 + SM_THREADS;
+};
+
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+// D(tmem) (+)= A(tmem) * B(smem)^T for f16 operands is umma_bf16_ts with another instruction descriptor.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_major) {
+  return (1u << 4) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
+         (static_cast<uint32_t>(M >> 4) << 24);
+}
+// MN-major operand with 128-byte swizzling: a line of 64 rows per key, 8 keys
+// of 1024 bytes per atom; only one atom along the rows, so both offsets are
+// the step of 8 keys.
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(1024 >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+}
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+// the softmax warps' own barrier, and its vote
+template <int T>
+__device__ __forceinline__ void bar_softmax() {
+  asm volatile("barrier.cta.sync 1, %0;" ::"n"(T) : "memory");
+}
+template <int T>
+__device__ __forceinline__ bool vote_softmax(bool p) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred a, b;\n\t"
+      "setp.ne.u32 a, %1, 0;\n\t"
+      "barrier.cta.red.or.pred b, 1, %2, a;\n\t"
+      "selp.u32 %0, 1, 0, b;\n\t}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(p)), "n"(T)
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// v[r] of 32 lanes -> lane r gets the reduction of row r
+template <class Op>
+__device__ __forceinline__ float reduce_rows(float (&v)[32], Op op) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float send = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, o));
+    }
+  }
+  return v[0];
+}
+__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t w, int hi) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(hi ? w >> 16 : w & 0xffff), __NV_E4M3);
+  return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+}
+// C consecutive TMEM columns of this thread's lane, C = 16 or 32
+template <int C>
+__device__ __forceinline__ void tmem_ld(uint32_t addr, float* v) {
+  if constexpr (C == 32) {
+    uint32_t r[32];
+    tmem_ld32_nowait(addr, r);
+    tmem_wait_ld(r);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+  } else {
+    float r[16];
+    tmem_ld16(addr, r);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = r[i];
+  }
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]),
+      "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+      : "memory");
+}
+
+template <int HD_, int N_>
+__global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
+    attn_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedArgs a) {
+  using C = PagedCfg<HD_, N_>;
+  constexpr int HD = C::HD, N = C::N, NST = C::STAGES, PB = C::PAGE_BYTES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sKV = smem;
+  uint8_t* sQ = sKV + NST * C::STAGE_BYTES;
+  uint8_t* sP = sQ + C::Q_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sP + 2 * C::P_BYTES);
+  uint64_t *kv_full = bars, *kv_empty = bars + 8;             // [NST]
+  uint64_t *kt_full = bars + 16, *kt_empty = bars + 18;       // [2] converted K
+  uint64_t *vt_full = bars + 20, *vt_empty = bars + 22;       // [2] converted V^T
+  uint64_t *s_full = bars + 24, *p_full = bars + 26;          // [2]
+  uint64_t *o_full = bars + 28, *q_full = bars + 29, *drain = bars + 30;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 31);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int64_t* s_units = reinterpret_cast<int64_t*>(bars + 32);
+  Item* s_item = reinterpret_cast<Item*>(bars + 33);
+  float* s_qmax = reinterpret_cast<float*>(bars + 36);        // [8] Q maximum per softmax warp
+  // per virtual row
+  float* s_negm = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // minus the reference
+  float* s_fac = s_negm + N;
+  float* s_red = s_fac + N;                                   // [4][N]
+  int2* s_see = reinterpret_cast<int2*>(s_red + 4 * N);       // visible keys [x, y)
+  int64_t* s_row = reinterpret_cast<int64_t*>(s_see + N);     // element offset of the output row, -1: none
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NST; ++i) {
+      mbar_init(&kv_full[i], 1);
+      mbar_init(&kv_empty[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&kt_full[i], 4);
+      mbar_init(&kt_empty[i], 1);
+      mbar_init(&vt_full[i], 4);
+      mbar_init(&vt_empty[i], 1);
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 4 * C::GROUPS);
+    }
+    mbar_init(o_full, 1);
+    mbar_init(q_full, 4 * C::GROUPS);
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  pdl_enter();
+  if (warp == 0) {
+    const int64_t total = total_units<N>(a);
+    const int64_t u0 = cut(total, blockIdx.x, gridDim.x), u1 = cut(total, blockIdx.x + 1, gridDim.x);
+    const Item it = u0 < u1 ? locate<N>(a, u0) : Item{0, 0, 0, 0};
+    if (lane == 0) {
+      *s_units = u1 - u0;
+      *s_item = it;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk<N> w(a, *s_item, *s_units);
+
+  if (warp == 0) {
+    // --------------------------------------------------------------- producer
+    int g = 0;
+    bool ok = true;
+    for (; ok && w.next(); w.advance()) {
+      const int32_t* row = a.table + static_cast<int64_t>(w.it.b) * a.ld_table;
+      const int n_pages = (w.s.len + PT - 1) / PT;
+      int ids = 0;
+      for (int i = 0; i < w.nt; ++i, ++g) {
+        if ((i & 15) == 0) {                                  // page ids of 16 tiles
+          const int at = 2 * (w.t0 + i) + lane;
+          ids = at < n_pages ? row[at] : -1;
+        }
+        const int p0 = __shfl_sync(0xffffffffu, ids, 2 * (i & 15)), p1 = __shfl_sync(0xffffffffu, ids, 2 * (i & 15) + 1);
+        const int st = g % NST;
+        if (!warp_wait_bounded(&kv_empty[st], ((g / NST) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
+        if (lane == 0) {
+          const bool two = 2 * (w.t0 + i) + 1 < n_pages;      // an id out of range lies outside the map: zeros arrive
+          uint8_t* dst = sKV + st * C::STAGE_BYTES;
+          mbar_arrive_expect_tx(&kv_full[st], two ? 4 * PB : 2 * PB);
+          tma_load_4d(dst, &tmK, &kv_full[st], 0, 0, w.it.hk, p0);
+          tma_load_4d(dst + 2 * PB, &tmV, &kv_full[st], 0, 0, w.it.hk, p0);
+          if (two) {
+            tma_load_4d(dst + PB, &tmK, &kv_full[st], 0, 0, w.it.hk, p1);
+            tma_load_4d(dst + 3 * PB, &tmV, &kv_full[st], 0, 0, w.it.hk, p1);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    // every copy started here has landed before the CTA may exit (g tiles were issued in ring order)
+    volatile int never = 0;
+    for (int i = max(0, g - NST); i < g; ++i) mbar_wait_bounded(&kv_full[i % NST], (i / NST) & 1, &never, nullptr);
+  } else if (warp == 1) {
+    // --------------------------------------------------------------- MMA issuer
+    constexpr uint32_t idesc_s = idesc_f16_f32(128, N, false), idesc_o = idesc_f16_f32(128, N, true);
+    const uint64_t q0 = sdesc_kmajor_sw128(smem_u32(sQ));
+    int g = 0, seg = 0;
+    bool ok = true;
+    for (; ok && w.next(); w.advance()) {
+      if (w.nt == 0) continue;
+      if (!warp_wait_bounded(q_full, seg & 1, abort_flag, nullptr)) break;
+      ++seg;
+      for (int i = 0; i <= w.nt; ++i) {
+        if (i < w.nt) {
+          // S^T of tile g + i; its buffer was read before p_full of two tiles ago, which PV has waited for
+          const int t = g + i, sb = t & 1;
+          if (!warp_wait_bounded(&kt_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < HD / 16; ++kk)
+            umma_bf16_ts(tmem + C::S_COL + sb * 64, tmem + C::K_COL + sb * 64 + 8 * kk,
+                         q0 + (((kk >> 2) * (N * 128) + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
+          umma_commit(&s_full[sb]);
+          umma_commit(&kt_empty[sb]);
+        }
+        if (i >= 1) {
+          const int t = g + i - 1, pb = t & 1;
+          if (!warp_wait_bounded(&vt_full[pb], (t >> 1) & 1, abort_flag, nullptr) ||
+              !warp_wait_bounded(&p_full[pb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t p0 = sdesc_mn_sw128(smem_u32(sP + pb * C::P_BYTES));
+#pragma unroll
+          for (int kk = 0; kk < TK / 16; ++kk)
+            umma_bf16_ts(tmem + C::O_COL, tmem + C::V_COL + pb * 64 + 8 * kk, p0 + kk * (2048 >> 4), idesc_o, i != 1 || kk != 0);
+          umma_commit(o_full);
+          umma_commit(&vt_empty[pb]);
+        }
+      }
+      g += w.nt;
+    }
+    umma_commit(drain);
+    volatile int never = 0;
+    warp_wait_bounded(drain, 0, &never, nullptr);
+  } else if (warp < 6) {
+    // --------------------------------------------------------------- converters
+    const int row = (warp & 3) * 32 + lane;                   // key of K, dim of V^T
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    int g = 0;
+    bool ok = true;
+    for (; ok && w.next(); w.advance()) {
+      for (int i = 0; i < w.nt; ++i, ++g) {
+        const int st = g % NST, sb = g & 1;
+        const uint32_t again = ((g >> 1) & 1) ^ 1;
+        if (!warp_wait_bounded(&kv_full[st], (g / NST) & 1, abort_flag, nullptr) ||
+            !warp_wait_bounded(&kt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
+        tc_fence_after();
+        const uint8_t* base = sKV + st * C::STAGE_BYTES;
+        {
+          const int r = row & (PT - 1);
+          const uint8_t* line = base + (row >> 6) * PB + r * HD;
+#pragma unroll
+          for (int c = 0; c < HD / 64; ++c) {
+            uint32_t out[32];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int ch = 4 * c + j;
+              const uint4 x = *reinterpret_cast<const uint4*>(line + ((HD == 128 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3)) << 4));
+              const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                out[8 * j + 2 * e] = e4m3x2_f16x2(v[e], 0);
+                out[8 * j + 2 * e + 1] = e4m3x2_f16x2(v[e], 1);
+              }
+            }
+            tmem_st32(tmem + lane_off + C::K_COL + sb * 64 + 32 * c, out);
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&kt_full[sb]);
+        if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
+        tc_fence_after();
+        if (HD == 128 || row < 64) {                          // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
+          const int valid = w.s.len - (w.t0 + i) * TK;        // keys of this tile that exist
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const uint8_t* line = base + (2 + c) * PB + row * PT;
+            uint32_t out[32];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint4 x = *reinterpret_cast<const uint4*>(line + ((j ^ ((row >> 1) & 3)) << 4));
+              uint32_t v[4] = {x.x, x.y, x.z, x.w};
+              if (valid < TK) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int n = valid - (64 * c + 16 * j + 4 * e);
+                  v[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+                }
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                out[8 * j + 2 * e] = e4m3x2_f16x2(v[e], 0);
+                out[8 * j + 2 * e + 1] = e4m3x2_f16x2(v[e], 1);
+              }
+            }
+            tmem_st32(tmem + lane_off + C::V_COL + sb * 64 + 32 * c, out);
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&vt_full[sb]);
+        warp_arrive(&kv_empty[st]);
+      }
+    }
+  } else {
+    // --------------------------------------------------------------- softmax
+    constexpr int ST = C::SM_THREADS, RN = C::RN;
+    const int tid = threadIdx.x - 192, sw = warp - 6;
+    const int key_lane = (warp & 3) * 32 + lane;              // this thread's key in a tile = its TMEM lane
+    const int row0 = (sw >> 2) * RN;                          // its rows: row0 .. row0 + RN - 1
+    float* my_red = s_red + (sw & 3) * N + row0;
+    const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    int g = 0, n_seg = 0;
+    bool ok = true;
+    for (; ok && w.next(); w.advance(), ++n_seg) {
+      const int v0 = w.it.rt * N;
+      if (tid < N) {
+        const int v = v0 + tid;
+        const bool in = v < w.s.n_virt;
+        const int r = v / a.group, pos = w.s.pos0 + r;
+        s_row[tid] = in ? (w.s.first + r) * a.ldo + static_cast<int64_t>(w.it.hk * a.group + v % a.group) * HD : -1;
+        s_see[tid] = make_int2(in && a.window > 0 ? pos - a.window + 1 : 0,
+                               in && a.causal ? min(w.s.len, pos + 1) : w.s.len);
+        s_negm[tid] = 0.0f;
+      }
+      const bool whole = w.from_start && w.to_end;
+      if (w.nt == 0) {                                        // no key: zeros
+        bar_softmax<ST>();
+        for (int r = 0; r < N; ++r)
+          if (s_row[r] >= 0 && tid < HD) a.o[s_row[r] + tid] = __float2bfloat16_rn(0.0f);
+        bar_softmax<ST>();
+        continue;
+      }
+      // ---- Q: N rows as f16, scaled by a power of two so that the largest is in 2^14 .. 2^15
+      constexpr int CPR = HD / 8, QV = (N * CPR + ST - 1) / ST;   // 16-byte chunks per row, per thread
+      uint4 qv[QV];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int c = i * ST + tid, r = c / CPR, v = v0 + r;
+        qv[i] = make_uint4(0, 0, 0, 0);
+        if (c < N * CPR && v < w.s.n_virt) {
+          const int t = v / a.group;
+          qv[i] = *reinterpret_cast<const uint4*>(a.q + (w.s.first + t) * a.ldq +
+                                                  static_cast<int64_t>(w.it.hk * a.group + v % a.group) * HD + (c % CPR) * 8);
+        }
+        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = x[e] << 16 & 0x7fff0000u, hi = x[e] & 0x7fff0000u;
+          if (lo < 0x7f800000u) top = max(top, lo);
+          if (hi < 0x7f800000u) top = max(top, hi);
+        }
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) s_qmax[sw] = __uint_as_float(top);
+      bar_softmax<ST>();
+      float q_max = s_qmax[0];
+#pragma unroll
+      for (int k = 1; k < ST / 32; ++k) q_max = fmaxf(q_max, s_qmax[k]);
+      const int e_max = max(static_cast<int>(__float_as_uint(q_max) >> 23), 40) - 127;   // 2^e_max <= q_max
+      const float q_up = __int_as_float((14 - e_max + 127) << 23), q_down = __int_as_float((e_max - 14 + 127) << 23);
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int c = i * ST + tid, r = c / CPR, ch = c % CPR;
+        if (c >= N * CPR) break;
+        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const __half2 t = __floats2half2_rn(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
+          h[e] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        *reinterpret_cast<uint4*>(sQ + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      fence_proxy_async_smem();
+      warp_arrive(q_full);
+
+      // ---- page scales: ids two tiles ahead, scales one tile ahead
+      const int32_t* row = a.table + static_cast<int64_t>(w.it.b) * a.ld_table;
+      const int n_pages = (w.s.len + PT - 1) / PT, half = key_lane >> 6;
+      auto page_id = [&](int tile) {
+        const int at = 2 * tile + half;
+        return at < n_pages ? row[at] : -1;
+      };
+      auto scales = [&](int page) {                           // a page that is not there: K = V = 0
+        if (page < 0 || page >= a.pages) return make_float2(0.0f, 1.0f);
+        const int64_t at = static_cast<int64_t>(page) * a.n_kv + w.it.hk;
+        return make_float2(a.sk[at], a.sv[at]);
+      };
+      float2 sc_next = scales(page_id(w.t0));
+      int id_next = page_id(w.t0 + 1);
+      // rows whose bounds cut a tile: every key below `all_lo` or from `all_hi` on is hidden from some row
+      const int last_v = min(v0 + N, w.s.n_virt) - 1;
+      const int all_hi = a.causal ? min(w.s.len, w.s.pos0 + v0 / a.group + 1) : w.s.len;
+      const int all_lo = a.window > 0 ? w.s.pos0 + last_v / a.group - a.window + 1 : 0;
+
+      float l[RN];
+#pragma unroll
+      for (int r = 0; r < RN; ++r) l[r] = 0.0f;
+      bool has_ref = false;                                   // of row tid
+      bool unset = true;                                      // some row has no reference yet (the warps agree)
+      for (int i = 0; i < w.nt; ++i) {
+        const int t = g + i, sb = t & 1, tile = w.t0 + i;
+        const float2 sc = sc_next;
+        if (i + 1 < w.nt) {
+          sc_next = scales(id_next);
+          if (i + 2 < w.nt) id_next = page_id(tile + 2);
+        }
+        if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; }
+        // the warps vote below: all of them leave together
+        tc_fence_after();
+        const float cth = sc.x * q_down * a.scale_log2, lv = log2f(sc.y);
+        const int key = tile * TK + key_lane;
+        const bool masked = tile * TK < all_lo || (tile + 1) * TK > all_hi;
+        float x[RN];
+        tmem_ld<RN>(tmem + lane_off + C::S_COL + sb * 64 + row0, x);
+        const uint64_t c2 = f2_pack(cth, cth);
+        float mx = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < RN; r += 4) {
+          const ulonglong2 nm = *reinterpret_cast<const ulonglong2*>(s_negm + row0 + r);
+          f2_unpack(f2_fma(f2_pack(x[r], x[r + 1]), c2, nm.x), x[r], x[r + 1]);
+          f2_unpack(f2_fma(f2_pack(x[r + 2], x[r + 3]), c2, nm.y), x[r + 2], x[r + 3]);
+        }
+        if (masked) {
+#pragma unroll
+          for (int r = 0; r < RN; ++r) {
+            const int2 see = s_see[row0 + r];
+            x[r] = key >= see.x && key < see.y ? x[r] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < RN; r += 2) mx = fmax3(mx, x[r], x[r + 1]);
+        if (vote_softmax<ST>(unset || mx + lv > 8.0f || !ok)) {
+          // ---- some row exceeds its reference (or has none): new references, O and the sums follow
+          if (*abort_flag) ok = false;
+          {
+            float y[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) y[k] = k < RN ? x[k < RN ? k : 0] + lv : -INFINITY;
+            const float m = reduce_rows(y, [](float p, float q) { return fmaxf(p, q); });
+            if (lane < RN) my_red[lane] = m;
+          }
+          bar_softmax<ST>();
+          bool none = false;
+          if (tid < N) {
+            const float rel = fmaxf(fmaxf(s_red[tid], s_red[N + tid]), fmaxf(s_red[2 * N + tid], s_red[3 * N + tid]));
+            float f = 1.0f, d = 0.0f;                         // factor of O and l, step of the reference
+            if (!has_ref) {                                   // O and l of the row are still zero
+              none = rel == -INFINITY;
+              has_ref = !none;
+              d = none ? 0.0f : rel;
+            } else if (rel > 8.0f) {
+              d = rel;
+              f = ex2_approx(-rel);
+            }
+            s_negm[tid] -= d;
+            s_fac[tid] = f;
+            s_red[tid] = d;                                   // its four inputs have been read by this thread alone
+          }
+          unset = vote_softmax<ST>(none);
+#pragma unroll
+          for (int r = 0; r < RN; ++r) x[r] -= s_red[row0 + r];
+          if (i > 0) {
+            // O holds the segment's tiles up to i - 1 once their PV is complete
+            if (!warp_wait_bounded(o_full, (t - 1) & 1, abort_flag, nullptr)) ok = false;
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < RN / 16; ++c) {
+              float y[16];
+              tmem_ld16(tmem + lane_off + C::O_COL + row0 + 16 * c, y);
+#pragma unroll
+              for (int k = 0; k < 16; ++k) y[k] *= s_fac[row0 + 16 * c + k];
+              tmem_st16(tmem + lane_off + C::O_COL + row0 + 16 * c, y);
+            }
+            tmem_wait_st();
+#pragma unroll
+            for (int r = 0; r < RN; ++r) l[r] *= s_fac[row0 + r];
+          }
+          if (vote_softmax<ST>(!ok)) { ok = false; break; }       // also: s_fac and s_red may be written again
+        }
+        // ---- P = 2^x times the page's V scale, f16, a 128-byte line per key
+        const float vs = sc.y * 128.0f;
+        const uint64_t vs2 = f2_pack(vs, vs);
+        uint8_t* line = sP + sb * C::P_BYTES + key_lane * 128;
+#pragma unroll
+        for (int r = 0; r < RN; r += 8) {
+          uint32_t h[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p0 = ex2_approx(x[r + 2 * e]), p1 = ex2_approx(x[r + 2 * e + 1]);
+            f2_unpack(f2_add(f2_pack(l[r + 2 * e], l[r + 2 * e + 1]), f2_pack(p0, p1)), l[r + 2 * e], l[r + 2 * e + 1]);
+            float y0, y1;
+            f2_unpack(f2_mul(f2_pack(p0, p1), vs2), y0, y1);
+            const __half2 q = __floats2half2_rn(y0, y1);
+            h[e] = *reinterpret_cast<const uint32_t*>(&q);
+          }
+          *reinterpret_cast<uint4*>(line + ((((row0 + r) >> 3) ^ (key_lane & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        warp_arrive(&p_full[sb]);
+      }
+      if (!ok) break;
+      g += w.nt;
+      // ---- the rows' sums, then O
+      {
+        float y[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) y[k] = k < RN ? l[k < RN ? k : 0] : 0.0f;
+        const float s = reduce_rows(y, [](float p, float q) { return p + q; });
+        if (lane < RN) my_red[lane] = s;
+      }
+      bar_softmax<ST>();
+      if (tid < N) {
+        const float s = (s_red[tid] + s_red[N + tid]) + (s_red[2 * N + tid] + s_red[3 * N + tid]);
+        if (whole) {
+          s_fac[tid] = s == 0.0f ? 0.0f : 1.0f / (s * 128.0f);
+        } else {
+          const int64_t slot = 2LL * blockIdx.x + (n_seg > 0);
+          a.part_ml[slot * N + tid] = make_float2(s == 0.0f ? -INFINITY : -s_negm[tid], s * 128.0f);
+        }
+      }
+      ok = warp_wait_bounded(o_full, (g - 1) & 1, abort_flag, nullptr);
+      tc_fence_after();
+      bar_softmax<ST>();
+      if (ok) {
+        float* part = a.part_o + (2LL * blockIdx.x + (n_seg > 0)) * N * HD + key_lane;
+#pragma unroll
+        for (int c = 0; c < RN / 16; ++c) {
+          float y[16];
+          tmem_ld16(tmem + lane_off + C::O_COL + row0 + 16 * c, y);
+          if (HD == 128 || key_lane < HD) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const int r = row0 + 16 * c + k;
+              const int64_t at = s_row[r];
+              if (at < 0) continue;
+              if (whole) a.o[at + key_lane] = __float2bfloat16_rn(y[k] * s_fac[r]);
+              else part[r * HD] = y[k];
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      if (vote_softmax<ST>(!ok)) {                            // also: s_row, s_see, s_negm and s_fac may be written again
+        ok = false;
+        break;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// Merges the partials of an item that the cut between CTAs c - 1 and c splits
+// first: m* = max m_s, O = sum 2^(m_s - m*) O_s / sum 2^(m_s - m*) l_s, in the
+// order of the CTAs.  Block (c, y) takes four of the item's rows, a warp each.
+template <int HD, int N>
+__global__ void __launch_bounds__(128) merge_paged_kernel(const PagedArgs a, int ctas) {
+  pdl_enter();
+  const int c = blockIdx.x + 1, lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5);
+  const int64_t total = total_units<N>(a), start = cut(total, c, ctas);
+  if (start == cut(total, c + 1, ctas)) return;               // no units from here: a later cut is the same place
+  const Item it = locate<N>(a, start);
+  const int64_t first = start - it.off;                       // the item's first unit
+  int k = c - 1;                                              // the CTA that ends at this cut
+  while (k > 0 && cut(total, k, ctas) == start) --k;
+  if (it.off == 0 || cut(total, k, ctas) > first) return;     // the item begins here, or an earlier cut splits it first
+  const SeqInfo s = seq_info<N>(a, it.b);
+  const int v = it.rt * N + r;
+  if (v >= s.n_virt) return;
+  const int64_t end = first + max(1, tile_range<N>(a, s, it.rt).y);
+  constexpr int PL = HD / 32;
+  float m = -INFINITY, l = 0.0f, acc[PL] = {};
+  for (; k < ctas && cut(total, k, ctas) < end; ++k) {
+    const int64_t k0 = cut(total, k, ctas);
+    if (k0 == cut(total, k + 1, ctas)) continue;              // no units
+    const int64_t slot = 2LL * k + (k0 < first);              // the item is not the first one of CTA c - 1
+    const float2 ml = a.part_ml[slot * N + r];
+    float x[PL];
+    const float* p = a.part_o + (slot * N + r) * HD + lane * PL;
+#pragma unroll
+    for (int d = 0; d < PL; ++d) x[d] = p[d];
+    if (ml.x == -INFINITY) continue;                          // no key of this part
+    const float mn = fmaxf(m, ml.x), f = ex2_approx(m - mn), h = ex2_approx(ml.x - mn);
+    l = l * f + ml.y * h;
+#pragma unroll
+    for (int d = 0; d < PL; ++d) acc[d] = acc[d] * f + x[d] * h;
+    m = mn;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  bf16* o = a.o + (s.first + v / a.group) * a.ldo + static_cast<int64_t>(it.hk * a.group + v % a.group) * HD + lane * PL;
+#pragma unroll
+  for (int d = 0; d < PL; d += 2) *reinterpret_cast<__nv_bfloat162*>(o + d) = __floats2bfloat162_rn(acc[d] * inv, acc[d + 1] * inv);
+}
+
+// uint8 map {d0, d1, n_kv, pages}, dense, box {d0, d1, 1, 1}, swizzled by its row
+bool page_map(CUtensorMap* m, const void* ptr, uint32_t d0, uint32_t d1, uint64_t n_kv, uint64_t pages) {
+  const cuuint64_t dims[4] = {d0, d1, n_kv, pages};
+  const cuuint64_t strides[3] = {d0, static_cast<uint64_t>(d0) * d1, static_cast<uint64_t>(d0) * d1 * n_kv};
+  const cuuint32_t box[4] = {d0, d1, 1, 1}, estr[4] = {1, 1, 1, 1};
+  return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(ptr), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, d0 == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Virtual rows of a tile: the least of 16, 32, 64 that holds a sequence's rows of one KV head (64: several tiles).
+int tile_rows(int max_rows, int group) {
+  const int64_t v = static_cast<int64_t>(max_rows) * group;
+  return v <= 16 ? 16 : v <= 32 ? 32 : 64;
+}
+
+template <int HD, int N>
+const char* launch(const RaggedCall& c, cudaStream_t s) {
+  using C = PagedCfg<HD, N>;
+  if (!tensor_map_encoder()) return "cuTensorMapEncodeTiled is unavailable";
+  int dev = 0;
+  const int ctas = current_sms(&dev);
+  static PerDevice ready;
+  if (ready.get(dev, [] {
+        return cudaFuncSetAttribute(attn_paged_kernel<HD, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) ==
+                       cudaSuccess ? 1 : 0;
+      }) <= 0)
+    return "attention smem attribute failed";
+  const tadm_page_pool& p = *c.pool;
+  const int64_t at = static_cast<int64_t>(c.layer) * p.pages * p.n_kv_heads;
+  CUtensorMap mk, mv;
+  if (!page_map(&mk, static_cast<const uint8_t*>(p.k) + at * PT * HD, HD, PT, p.n_kv_heads, p.pages) ||
+      !page_map(&mv, static_cast<const uint8_t*>(p.v) + at * PT * HD, PT, HD, p.n_kv_heads, p.pages))
+    return "page tensor map encode failed";
+  float* part = static_cast<float*>(c.scratch);
+  const PagedArgs a{static_cast<const bf16*>(c.q), static_cast<bf16*>(c.o), p.k_scale + at, p.v_scale + at,
+                    c.cu, c.lens, c.table, c.batch, c.total, c.max_rows, c.max_len, c.ld_table, p.pages,
+                    c.n_heads / c.n_kv, c.n_kv, c.ldq, c.ldo, c.causal, c.window,
+                    1.4426950408889634f / sqrtf(static_cast<float>(HD)), part,
+                    reinterpret_cast<float2*>(part + 2LL * ctas * N * HD)};
+  cudaError_t e = launch_pdl(attn_paged_kernel<HD, N>, ctas, C::THREADS, C::SMEM, s, mk, mv, a);
+  if (e == cudaSuccess && ctas > 1)
+    e = launch_pdl(merge_paged_kernel<HD, N>, dim3(ctas - 1, N / 4), 128, 0, s, a, ctas);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+
+}  // namespace
+
+size_t attention_paged_scratch(int max_rows, int group, int head_dim) {
+  int dev = 0;
+  return 2ull * current_sms(&dev) * tile_rows(max_rows, group) * (head_dim + 2) * sizeof(float);
+}
+
+const char* attention_paged(const RaggedCall& c, cudaStream_t s) {
+  auto hd = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    return c.head_dim == 128 ? launch<128, N>(c, s) : launch<64, N>(c, s);
+  };
+  switch (tile_rows(c.max_rows, c.n_heads / c.n_kv)) {
+    case 16: return hd(std::integral_constant<int, 16>{});
+    case 32: return hd(std::integral_constant<int, 32>{});
+    default: return hd(std::integral_constant<int, 64>{});
+  }
+}
+
+}  // namespace tadm

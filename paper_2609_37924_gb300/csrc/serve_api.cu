@@ -20,10 +20,10 @@ bool packed_ok(const int32_t* cu, int batch, int total, int max_rows) {
   return batch >= 0 && total >= 0 && max_rows >= 0 && (cu || batch == 0);
 }
 bool pool_ok(const tadm_page_pool* p) {
-  return p && p->layers > 0 && p->pages >= 0 && p->n_kv_heads > 0 && p->n_kv_heads <= 16384 &&
+  return p && p->layers > 0 && p->pages > 0 && p->n_kv_heads > 0 && p->n_kv_heads <= 16384 &&
          (p->head_dim == 64 || p->head_dim == 128) &&
-         (p->pages == 0 || (p->k && p->v && p->k_scale && p->v_scale && aligned(p->k) && aligned(p->v) &&
-                            aligned(p->k_scale, 4) && aligned(p->v_scale, 4)));
+         p->k && p->v && p->k_scale && p->v_scale && aligned(p->k) && aligned(p->v) && aligned(p->k_scale, 4) &&
+         aligned(p->v_scale, 4);
 }
 // ld_table * 64 tokens have to be an int32; grids cover batch * touched pages
 bool table_ok(const int32_t* table, int ld_table, int rows) {
@@ -104,7 +104,8 @@ tadm_status tadm_page_attention_scratch_size(int batch, int total_rows, int max_
   if (batch < 0 || total_rows < 0 || max_rows < 0 || max_len < 0 || !heads_ok(n_heads, n_kv_heads, head_dim) ||
       (dtype != 0 && dtype != 1) || !bytes)
     return TADM_ERR_INVALID_ARG;
-  *bytes = 0;
+  const int rows = max_rows < total_rows ? max_rows : total_rows;
+  *bytes = dtype ? attention_paged_scratch(rows, n_heads / n_kv_heads, head_dim) : 0;
   return TADM_OK;
 }
 
@@ -129,7 +130,7 @@ tadm_status tadm_page_attention(const void* q, const tadm_page_pool* pool, int l
   c.max_rows = max_rows < total_rows ? max_rows : total_rows, c.max_len = max_len, c.ld_table = ld_table;
   c.n_heads = n_heads, c.n_kv = pool->n_kv_heads, c.head_dim = pool->head_dim;
   c.ldq = ldq, c.ldo = ldo, c.causal = causal, c.window = window, c.bf16 = dtype, c.scratch = scratch;
-  return attention_rows(c, stream) ? TADM_ERR_CUDA : TADM_OK;
+  return (dtype ? attention_paged(c, stream) : attention_rows(c, stream)) ? TADM_ERR_CUDA : TADM_OK;
 }
 
 tadm_status tadm_pages_scratch_size(int pages, int n_seqs, size_t* bytes) {

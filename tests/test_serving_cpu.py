@@ -45,7 +45,7 @@ def test_empty_calls_do_nothing(T, over):
 ROWS = dict(layer=0, k=P, v=P, cu=P, start=P, batch=2, total=10, max_rows=8, ldk=256, ldv=256, table=P, ld_table=4, dtype=1,
             stream=None)
 POOLS = [dict(k=None), dict(v=None), dict(k_scale=None), dict(v_scale=None), dict(k=P + 4), dict(v=P + 8),
-         dict(k_scale=P + 2), dict(layers=0), dict(pages=-1), dict(n_kv_heads=0), dict(head_dim=32), dict(head_dim=256)]
+         dict(k_scale=P + 2), dict(layers=0), dict(pages=-1), dict(pages=0), dict(n_kv_heads=0), dict(head_dim=32), dict(head_dim=256)]
 
 
 @pytest.mark.parametrize("name", ["tadm_page_write", "tadm_page_read"])

@@ -8,26 +8,31 @@
 // instead of being padded to 128, and a key is one TMEM lane = one thread,
 // whose page scales are two registers.
 //
-// A tile is 128 keys, two pages.  Roles of a CTA:
-//   warp 0      streams the pages with TMA (one 4-D map for K, one for V^T);
-//   warps 2-5   convert: e4m3 -> f16, exact, from shared memory into the TMEM
-//               A operands (K: a key per lane, V^T: a dim per lane); V slots
-//               past the sequence become zeros here;
-//   warp 1      S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
-//   warps 6-    softmax: a key per thread, the values of up to 32 rows in
-//               registers (four warps, or eight for 64 rows).  The running maximum of a row is a reference that moves only when
-//               a tile exceeds it by 2^8, so a tile costs one vote of these
-//               warps and no reduction over the keys; the sums of a row stay
-//               one partial per thread until the end of the work item.
+// A tile is 128 keys, two pages.  Roles of a CTA (16 warps):
+//   warp 0        streams the pages with TMA (one 4-D map for K, one for V^T)
+//                 and leaves their scales beside them;
+//   warps 14, 15  stage Q of the next work item while this one runs;
+//   warps 2-5     convert: e4m3 -> f16, exact, from shared memory into the
+//   (2-9)         TMEM A operands (K: a key per lane, V^T: a dim per lane); V
+//                 slots past the sequence become zeros here.  Up to 32 rows
+//                 K and V have four warps each;
+//   warp 1        S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
+//   warps 10-13   softmax: a key per thread, the values of up to 32 rows in
+//   (6-13)        registers.  The running maximum of a row is a reference that
+//                 moves only when a tile exceeds it by 2^8, so a tile costs
+//                 one vote of these warps and no reduction over the keys; the
+//                 sums of a row stay one partial per thread until the end of
+//                 the work item.
 // Precision: Q enters as f16 scaled by one power of two per tile of rows
 // (exact for values within 2^-28 of the largest), K and V are exact, the
 // probabilities times the page's V scale are rounded to f16 (11 bits) with
 // the row's reference at 2^7 to 2^15, so that a probability 2^-21 of the
 // largest still has all of them; scores, sums and O are fp32.
 //
-// Work: the tiles of all (sequence, KV head, row tile) items lie on one line
-// that is cut evenly over the SMs, whatever the lengths; an item that a cut
-// splits leaves fp32 partials, which a second small kernel merges in order.
+// Work: the tiles of all (sequence, KV head, row tile) items lie on one line,
+// each item followed by what its start and end cost, and the line is cut
+// evenly over the SMs, whatever the lengths; an item that a cut splits leaves
+// fp32 partials, which a second small kernel merges in order.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -53,6 +58,7 @@ struct PagedArgs {
   float scale_log2;                        // log2(e) / sqrt(hd)
   float* part_o;                           // [2 * CTAs][N][HD]
   float2* part_ml;                         // [2 * CTAs][N]: (reference in log2 units, sum)
+  struct Place* place;                     // [CTAs] where each CTA's units begin
 };
 
 // ------------------------------------------------------------------ work items
@@ -74,14 +80,18 @@ __device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s,
   const int t0 = begin / TK, t1 = (end + TK - 1) / TK;
   return make_int2(t0, begin < end ? t1 - t0 : 0);
 }
-// Units of a sequence and KV head: its row tiles' tiles, at least one each (a row tile that sees nothing has zeros to write).
+// An item's units: its tiles, then kItemUnits for its start and end (Q, the
+// first references, the sums, O), measured in tiles; a row tile that sees
+// nothing has zeros to write there.
+constexpr int kItemUnits = 2;
+// Units of a sequence and KV head.
 template <int N>
 __device__ __forceinline__ int64_t seq_units(const PagedArgs& a, int b) {
   const SeqInfo s = seq_info<N>(a, b);
   if (s.n_virt <= 0) return 0;
-  if (!a.causal && a.window == 0) return static_cast<int64_t>(s.n_rt) * max(1, tile_range<N>(a, s, 0).y);
+  if (!a.causal && a.window == 0) return static_cast<int64_t>(s.n_rt) * (tile_range<N>(a, s, 0).y + kItemUnits);
   int64_t u = 0;
-  for (int rt = 0; rt < s.n_rt; ++rt) u += max(1, tile_range<N>(a, s, rt).y);
+  for (int rt = 0; rt < s.n_rt; ++rt) u += tile_range<N>(a, s, rt).y + kItemUnits;
   return u;
 }
 template <int N>
@@ -94,6 +104,10 @@ __device__ __forceinline__ int64_t total_units(const PagedArgs& a) {      // war
 }
 struct Item {
   int b, hk, rt, off;                      // off: units of the item before the place asked for
+};
+struct Place {
+  int64_t total, unit;                     // units of the call, of this CTA's start
+  Item it;
 };
 // The item that holds unit `unit` (< total_units).  Warp-collective.
 template <int N>
@@ -120,7 +134,7 @@ __device__ __forceinline__ Item locate(const PagedArgs& a, int64_t unit) {
       in -= it.hk * per;
       const SeqInfo s = seq_info<N>(a, it.b);
       for (int rt = 0; rt < s.n_rt; ++rt) {
-        const int u = max(1, tile_range<N>(a, s, rt).y);
+        const int u = tile_range<N>(a, s, rt).y + kItemUnits;
         if (in < u) {
           it.rt = rt;
           it.off = static_cast<int>(in);
@@ -142,24 +156,32 @@ struct Walk {
   Item it;
   int64_t left;
   SeqInfo s;
-  int t0, nt;              // tiles of the segment
-  bool from_start, to_end; // it begins / ends with its item
+  int t0, nt;              // tiles of the segment; none: the item sees nothing and has zeros to write
+  bool from_start, to_end; // it begins / ends with its item's tiles
+  bool fresh = true;
   __device__ Walk(const PagedArgs& args, const Item& start, int64_t units) : a(args), it(start), left(units) {
     if (left > 0) s = seq_info<N>(a, it.b);
   }
   __device__ bool next() {                 // false: no segment left
-    if (left <= 0) return false;
-    const int2 r = tile_range<N>(a, s, it.rt);
-    const int units = max(1, r.y);
-    const int take = static_cast<int>(min(left, static_cast<int64_t>(units - it.off)));
-    t0 = r.x + it.off;
-    nt = r.y > 0 ? take : 0;
-    from_start = it.off == 0;
-    to_end = it.off + take == units;
-    left -= take;
-    return true;
+    for (;; fresh = false) {
+      if (!fresh) step();
+      if (left <= 0) return false;
+      const int2 r = tile_range<N>(a, s, it.rt);
+      const int units = r.y + kItemUnits, off = it.off;
+      const int take = static_cast<int>(min(left, static_cast<int64_t>(units - off)));
+      const int lo = min(off, r.y), hi = min(off + take, r.y);
+      t0 = r.x + lo;
+      nt = hi - lo;
+      from_start = lo == 0;
+      to_end = hi == r.y;
+      left -= take;
+      if (nt > 0 || (r.y == 0 && off == 0)) {
+        fresh = false;
+        return true;
+      }
+    }
   }
-  __device__ void advance() {              // to the next item, after the segment's work
+  __device__ void step() {                 // to the next item
     it.off = 0;
     if (++it.rt < s.n_rt) return;
     it.rt = 0;
@@ -179,15 +201,17 @@ struct PagedCfg {
   static constexpr int HD = HD_, N = N_;
   static constexpr int PAGE_BYTES = PT * HD;                 // of K or V^T, one head
   static constexpr int STAGE_BYTES = 4 * PAGE_BYTES;         // two pages of K, two of V^T
-  static constexpr int STAGES = HD == 128 ? 5 : 8;
-  static constexpr int Q_BYTES = HD / 64 * N * 128;          // HD/64 atoms of N rows x 64 dims, f16
+  static constexpr int STAGES = HD == 64 ? 8 : N == 64 ? 4 : 5;
+  static constexpr int Q_BYTES = HD / 64 * N * 128;          // HD/64 atoms of N rows x 64 dims, f16; two buffers
   static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
   static constexpr int RN = N < 32 ? N : 32, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
+  static constexpr int CONV_GROUPS = 3 - GROUPS;             // groups of four converting warps
+  static constexpr int SM_WARP = 2 + 4 * CONV_GROUPS, Q_WARP = 14, THREADS = 512;
   static constexpr int MISC = 1024 + N * 64;
-  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + Q_BYTES + 2 * P_BYTES + MISC;
+  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + MISC;
   static constexpr int K_COL = 0, V_COL = 128, S_COL = 256, O_COL = 384;   // TMEM: two of K, V^T and S, one O
-  static constexpr int THREADS = 192 + SM_THREADS;
+  static_assert(SMEM <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
@@ -251,9 +275,14 @@ __device__ __forceinline__ float reduce_rows(float (&v)[32], Op op) {
   }
   return v[0];
 }
-__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint32_t w, int hi) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(hi ? w >> 16 : w & 0xffff), __NV_E4M3);
-  return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
+// four e4m3 -> two pairs of f16 (exact)
+__device__ __forceinline__ void e4m3x4_f16x4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "mov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
 }
 // C consecutive TMEM columns of this thread's lane, C = 16 or 32
 template <int C>
@@ -288,18 +317,21 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sKV = smem;
   uint8_t* sQ = sKV + NST * C::STAGE_BYTES;
-  uint8_t* sP = sQ + C::Q_BYTES;
+  uint8_t* sP = sQ + 2 * C::Q_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sP + 2 * C::P_BYTES);
   uint64_t *kv_full = bars, *kv_empty = bars + 8;             // [NST]
   uint64_t *kt_full = bars + 16, *kt_empty = bars + 18;       // [2] converted K
   uint64_t *vt_full = bars + 20, *vt_empty = bars + 22;       // [2] converted V^T
   uint64_t *s_full = bars + 24, *p_full = bars + 26;          // [2]
-  uint64_t *o_full = bars + 28, *q_full = bars + 29, *drain = bars + 30;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 31);
+  uint64_t *q_full = bars + 28, *q_empty = bars + 30;         // [2]
+  uint64_t *o_full = bars + 32, *drain = bars + 33;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int64_t* s_units = reinterpret_cast<int64_t*>(bars + 32);
-  Item* s_item = reinterpret_cast<Item*>(bars + 33);
-  float* s_qmax = reinterpret_cast<float*>(bars + 36);        // [8] Q maximum per softmax warp
+  Place* s_place = reinterpret_cast<Place*>(bars + 36);       // 32 bytes
+  float* s_qdown = reinterpret_cast<float*>(bars + 40);       // [4] 1 / the factor of segment i's Q at i % 4 (the
+                                                              // softmax reads it later than the MMAs read Q)
+  uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 42);  // [2] the staging warps' maxima
+  float2* s_scale = reinterpret_cast<float2*>(bars + 64);     // [16][2] (K, V) scales of the pages of tile t at t % 16
   // per virtual row
   float* s_negm = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // minus the reference
   float* s_fac = s_negm + N;
@@ -311,7 +343,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) {
       mbar_init(&kv_full[i], 1);
-      mbar_init(&kv_empty[i], 4);
+      mbar_init(&kv_empty[i], 4 * C::CONV_GROUPS);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&kt_full[i], 4);
@@ -320,9 +352,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       mbar_init(&vt_empty[i], 1);
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[i], 4 * C::GROUPS);
+      mbar_init(&q_full[i], 2);
+      mbar_init(&q_empty[i], 1);
     }
     mbar_init(o_full, 1);
-    mbar_init(q_full, 4 * C::GROUPS);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -339,45 +372,78 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     const int64_t u0 = cut(total, blockIdx.x, gridDim.x), u1 = cut(total, blockIdx.x + 1, gridDim.x);
     const Item it = u0 < u1 ? locate<N>(a, u0) : Item{0, 0, 0, 0};
     if (lane == 0) {
-      *s_units = u1 - u0;
-      *s_item = it;
+      *s_place = Place{total, u0, it};
+      a.place[blockIdx.x] = Place{total, u0, it};
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk<N> w(a, *s_item, *s_units);
+  Walk<N> w(a, s_place->it, cut(s_place->total, blockIdx.x + 1, gridDim.x) - s_place->unit);
 
   if (warp == 0) {
     // --------------------------------------------------------------- producer
+    // Batches of up to 16 tiles of a segment: a lane per page.  The ids of a
+    // batch are asked for two batches ahead, the scales one batch ahead.
+    struct Batch {
+      int hk, tile, n, n_pages;            // n = 0: no batch left
+      int id;
+      float2 sc;
+    };
+    int at = 0;                            // tiles of w's segment that are in a batch
+    bool more = w.next();
+    auto take = [&]() {
+      while (more && at >= w.nt) {
+        more = w.next();
+        at = 0;
+      }
+      Batch b{0, 0, 0, 0, -1, make_float2(0.0f, 1.0f)};
+      if (!more) return b;
+      b.hk = w.it.hk;
+      b.tile = w.t0 + at;
+      b.n = min(16, w.nt - at);
+      b.n_pages = (w.s.len + PT - 1) / PT;
+      at += b.n;
+      const int page = 2 * b.tile + lane;
+      if (lane < 2 * b.n && page < b.n_pages) b.id = a.table[static_cast<int64_t>(w.it.b) * a.ld_table + page];
+      return b;
+    };
+    auto scales = [&](Batch& b) {          // a page that is not there: K = V = 0
+      if (b.id < 0 || b.id >= a.pages) return;
+      const int64_t p = static_cast<int64_t>(b.id) * a.n_kv + b.hk;
+      b.sc = make_float2(a.sk[p], a.sv[p]);
+    };
+    Batch now = take();
+    scales(now);
+    Batch next = take();
     int g = 0;
     bool ok = true;
-    for (; ok && w.next(); w.advance()) {
-      const int32_t* row = a.table + static_cast<int64_t>(w.it.b) * a.ld_table;
-      const int n_pages = (w.s.len + PT - 1) / PT;
-      int ids = 0;
-      for (int i = 0; i < w.nt; ++i, ++g) {
-        if ((i & 15) == 0) {                                  // page ids of 16 tiles
-          const int at = 2 * (w.t0 + i) + lane;
-          ids = at < n_pages ? row[at] : -1;
-        }
-        const int p0 = __shfl_sync(0xffffffffu, ids, 2 * (i & 15)), p1 = __shfl_sync(0xffffffffu, ids, 2 * (i & 15) + 1);
+    while (ok && now.n > 0) {
+      scales(next);
+      const Batch after = take();
+      for (int i = 0; i < now.n; ++i, ++g) {
+        const int p0 = __shfl_sync(0xffffffffu, now.id, 2 * i), p1 = __shfl_sync(0xffffffffu, now.id, 2 * i + 1);
         const int st = g % NST;
         if (!warp_wait_bounded(&kv_empty[st], ((g / NST) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
+        // the converters are done with tile g - NST, so the softmax is with tile g - 16
+        if ((lane >> 1) == i) s_scale[(g & 15) * 2 + (lane & 1)] = now.sc;
+        __syncwarp();
         if (lane == 0) {
-          const bool two = 2 * (w.t0 + i) + 1 < n_pages;      // an id out of range lies outside the map: zeros arrive
+          const bool two = 2 * (now.tile + i) + 1 < now.n_pages;   // an id out of range lies outside the map: zeros arrive
           uint8_t* dst = sKV + st * C::STAGE_BYTES;
           mbar_arrive_expect_tx(&kv_full[st], two ? 4 * PB : 2 * PB);
-          tma_load_4d(dst, &tmK, &kv_full[st], 0, 0, w.it.hk, p0);
-          tma_load_4d(dst + 2 * PB, &tmV, &kv_full[st], 0, 0, w.it.hk, p0);
+          tma_load_4d(dst, &tmK, &kv_full[st], 0, 0, now.hk, p0);
+          tma_load_4d(dst + 2 * PB, &tmV, &kv_full[st], 0, 0, now.hk, p0);
           if (two) {
-            tma_load_4d(dst + PB, &tmK, &kv_full[st], 0, 0, w.it.hk, p1);
-            tma_load_4d(dst + 3 * PB, &tmV, &kv_full[st], 0, 0, w.it.hk, p1);
+            tma_load_4d(dst + PB, &tmK, &kv_full[st], 0, 0, now.hk, p1);
+            tma_load_4d(dst + 3 * PB, &tmV, &kv_full[st], 0, 0, now.hk, p1);
           }
         }
         __syncwarp();
       }
+      now = next;
+      next = after;
     }
     // every copy started here has landed before the CTA may exit (g tiles were issued in ring order)
     volatile int never = 0;
@@ -385,13 +451,14 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
     constexpr uint32_t idesc_s = idesc_f16_f32(128, N, false), idesc_o = idesc_f16_f32(128, N, true);
-    const uint64_t q0 = sdesc_kmajor_sw128(smem_u32(sQ));
     int g = 0, seg = 0;
     bool ok = true;
-    for (; ok && w.next(); w.advance()) {
+    while (ok && w.next()) {
       if (w.nt == 0) continue;
-      if (!warp_wait_bounded(q_full, seg & 1, abort_flag, nullptr)) break;
+      const int qb = seg & 1;
+      if (!warp_wait_bounded(&q_full[qb], (seg >> 1) & 1, abort_flag, nullptr)) break;
       ++seg;
+      const uint64_t q0 = sdesc_kmajor_sw128(smem_u32(sQ + qb * C::Q_BYTES));
       for (int i = 0; i <= w.nt; ++i) {
         if (i < w.nt) {
           // S^T of tile g + i; its buffer was read before p_full of two tiles ago, which PV has waited for
@@ -404,6 +471,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
                          q0 + (((kk >> 2) * (N * 128) + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
           umma_commit(&s_full[sb]);
           umma_commit(&kt_empty[sb]);
+          if (i == w.nt - 1) umma_commit(&q_empty[qb]);
         }
         if (i >= 1) {
           const int t = g + i - 1, pb = t & 1;
@@ -423,21 +491,22 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     umma_commit(drain);
     volatile int never = 0;
     warp_wait_bounded(drain, 0, &never, nullptr);
-  } else if (warp < 6) {
+  } else if (warp < C::SM_WARP) {
     // --------------------------------------------------------------- converters
     const int row = (warp & 3) * 32 + lane;                   // key of K, dim of V^T
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const bool do_k = C::CONV_GROUPS == 1 || warp < 6, do_v = C::CONV_GROUPS == 1 || warp >= 6;
     int g = 0;
     bool ok = true;
-    for (; ok && w.next(); w.advance()) {
+    while (ok && w.next()) {
       for (int i = 0; i < w.nt; ++i, ++g) {
         const int st = g % NST, sb = g & 1;
         const uint32_t again = ((g >> 1) & 1) ^ 1;
-        if (!warp_wait_bounded(&kv_full[st], (g / NST) & 1, abort_flag, nullptr) ||
-            !warp_wait_bounded(&kt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
-        tc_fence_after();
         const uint8_t* base = sKV + st * C::STAGE_BYTES;
-        {
+        if (!warp_wait_bounded(&kv_full[st], (g / NST) & 1, abort_flag, nullptr)) { ok = false; break; }
+        if (do_k) {
+          if (!warp_wait_bounded(&kt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
+          tc_fence_after();
           const int r = row & (PT - 1);
           const uint8_t* line = base + (row >> 6) * PB + r * HD;
 #pragma unroll
@@ -449,62 +518,125 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
               const uint4 x = *reinterpret_cast<const uint4*>(line + ((HD == 128 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3)) << 4));
               const uint32_t v[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                out[8 * j + 2 * e] = e4m3x2_f16x2(v[e], 0);
-                out[8 * j + 2 * e + 1] = e4m3x2_f16x2(v[e], 1);
-              }
+              for (int e = 0; e < 4; ++e) e4m3x4_f16x4(v[e], out[8 * j + 2 * e], out[8 * j + 2 * e + 1]);
             }
             tmem_st32(tmem + lane_off + C::K_COL + sb * 64 + 32 * c, out);
           }
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(&kt_full[sb]);
         }
-        tmem_wait_st();
-        tc_fence_before();
-        warp_arrive(&kt_full[sb]);
-        if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
-        tc_fence_after();
-        if (HD == 128 || row < 64) {                          // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
-          const int valid = w.s.len - (w.t0 + i) * TK;        // keys of this tile that exist
+        if (do_v) {
+          if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
+          tc_fence_after();
+          if (HD == 128 || row < 64) {                        // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
+            const int valid = w.s.len - (w.t0 + i) * TK;      // keys of this tile that exist
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const uint8_t* line = base + (2 + c) * PB + row * PT;
-            uint32_t out[32];
+            for (int c = 0; c < 2; ++c) {
+              const uint8_t* line = base + (2 + c) * PB + row * PT;
+              uint32_t out[32];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint4 x = *reinterpret_cast<const uint4*>(line + ((j ^ ((row >> 1) & 3)) << 4));
-              uint32_t v[4] = {x.x, x.y, x.z, x.w};
-              if (valid < TK) {
+              for (int j = 0; j < 4; ++j) {
+                const uint4 x = *reinterpret_cast<const uint4*>(line + ((j ^ ((row >> 1) & 3)) << 4));
+                uint32_t v[4] = {x.x, x.y, x.z, x.w};
+                if (valid < TK) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const int n = valid - (64 * c + 16 * j + 4 * e);
-                  v[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+                  for (int e = 0; e < 4; ++e) {
+                    const int n = valid - (64 * c + 16 * j + 4 * e);
+                    v[e] &= n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+                  }
                 }
-              }
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                out[8 * j + 2 * e] = e4m3x2_f16x2(v[e], 0);
-                out[8 * j + 2 * e + 1] = e4m3x2_f16x2(v[e], 1);
+                for (int e = 0; e < 4; ++e) e4m3x4_f16x4(v[e], out[8 * j + 2 * e], out[8 * j + 2 * e + 1]);
               }
+              tmem_st32(tmem + lane_off + C::V_COL + sb * 64 + 32 * c, out);
             }
-            tmem_st32(tmem + lane_off + C::V_COL + sb * 64 + 32 * c, out);
           }
+          tmem_wait_st();
+          tc_fence_before();
+          warp_arrive(&vt_full[sb]);
         }
-        tmem_wait_st();
-        tc_fence_before();
-        warp_arrive(&vt_full[sb]);
         warp_arrive(&kv_empty[st]);
       }
+    }
+  } else if (warp >= C::Q_WARP) {
+    // --------------------------------------------------------------- Q
+    // N rows as f16, scaled by a power of two so that the largest value is in 2^14 .. 2^15
+    constexpr int CPR = HD / 8, QV = N * CPR / 64;            // 16-byte chunks per row, per thread
+    const int tid = threadIdx.x - 32 * C::Q_WARP;
+    int seg = 0;
+    while (w.next()) {
+      if (w.nt == 0) continue;
+      const int qb = seg & 1, v0 = w.it.rt * N;
+      uint4 qv[QV];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int c = i * 64 + tid, v = v0 + c / CPR;
+        qv[i] = make_uint4(0, 0, 0, 0);
+        if (v < w.s.n_virt) {
+          const int t = v / a.group;
+          qv[i] = *reinterpret_cast<const uint4*>(a.q + (w.s.first + t) * a.ldq +
+                                                  static_cast<int64_t>(w.it.hk * a.group + v - t * a.group) * HD + (c % CPR) * 8);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = x[e] << 16 & 0x7fff0000u, hi = x[e] & 0x7fff0000u;
+          if (lo < 0x7f800000u) top = max(top, lo);
+          if (hi < 0x7f800000u) top = max(top, hi);
+        }
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) s_qmax[warp & 1] = top;
+      asm volatile("barrier.cta.sync 2, 64;" ::: "memory");
+      top = max(s_qmax[0], s_qmax[1]);
+      const int e_max = max(static_cast<int>(top >> 23), 40) - 127;    // 2^e_max <= the largest
+      const float q_up = __int_as_float((14 - e_max + 127) << 23), q_down = __int_as_float((e_max - 14 + 127) << 23);
+      const bool ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr);
+      if (tid == 0) s_qdown[seg & 3] = q_down;
+#pragma unroll
+      for (int i = 0; i < QV; ++i) {
+        const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
+        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+        uint32_t h[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const __half2 t = __floats2half2_rn(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
+          h[e] = *reinterpret_cast<const uint32_t*>(&t);
+        }
+        *reinterpret_cast<uint4*>(sQ + qb * C::Q_BYTES + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      fence_proxy_async_smem();
+      warp_arrive(&q_full[qb]);
+      ++seg;
+      // both warps have read the maxima, and they go on or leave together
+      uint32_t leave;
+      asm volatile(
+          "{\n\t.reg .pred a, b;\n\t"
+          "setp.ne.u32 a, %1, 0;\n\t"
+          "barrier.cta.red.or.pred b, 2, 64, a;\n\t"
+          "selp.u32 %0, 1, 0, b;\n\t}"
+          : "=r"(leave)
+          : "r"(static_cast<uint32_t>(!ok))
+          : "memory");
+      if (leave) break;
     }
   } else {
     // --------------------------------------------------------------- softmax
     constexpr int ST = C::SM_THREADS, RN = C::RN;
-    const int tid = threadIdx.x - 192, sw = warp - 6;
+    const int tid = threadIdx.x - 32 * C::SM_WARP, sw = warp - C::SM_WARP;
     const int key_lane = (warp & 3) * 32 + lane;              // this thread's key in a tile = its TMEM lane
     const int row0 = (sw >> 2) * RN;                          // its rows: row0 .. row0 + RN - 1
     float* my_red = s_red + (sw & 3) * N + row0;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    int g = 0, n_seg = 0;
+    int g = 0, seg = 0;
     bool ok = true;
-    for (; ok && w.next(); w.advance(), ++n_seg) {
+    while (ok && w.next()) {
       const int v0 = w.it.rt * N;
       if (tid < N) {
         const int v = v0 + tid;
@@ -523,66 +655,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         bar_softmax<ST>();
         continue;
       }
-      // ---- Q: N rows as f16, scaled by a power of two so that the largest is in 2^14 .. 2^15
-      constexpr int CPR = HD / 8, QV = (N * CPR + ST - 1) / ST;   // 16-byte chunks per row, per thread
-      uint4 qv[QV];
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < QV; ++i) {
-        const int c = i * ST + tid, r = c / CPR, v = v0 + r;
-        qv[i] = make_uint4(0, 0, 0, 0);
-        if (c < N * CPR && v < w.s.n_virt) {
-          const int t = v / a.group;
-          qv[i] = *reinterpret_cast<const uint4*>(a.q + (w.s.first + t) * a.ldq +
-                                                  static_cast<int64_t>(w.it.hk * a.group + v % a.group) * HD + (c % CPR) * 8);
-        }
-        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t lo = x[e] << 16 & 0x7fff0000u, hi = x[e] & 0x7fff0000u;
-          if (lo < 0x7f800000u) top = max(top, lo);
-          if (hi < 0x7f800000u) top = max(top, hi);
-        }
-      }
-      top = __reduce_max_sync(0xffffffffu, top);
-      if (lane == 0) s_qmax[sw] = __uint_as_float(top);
       bar_softmax<ST>();
-      float q_max = s_qmax[0];
-#pragma unroll
-      for (int k = 1; k < ST / 32; ++k) q_max = fmaxf(q_max, s_qmax[k]);
-      const int e_max = max(static_cast<int>(__float_as_uint(q_max) >> 23), 40) - 127;   // 2^e_max <= q_max
-      const float q_up = __int_as_float((14 - e_max + 127) << 23), q_down = __int_as_float((e_max - 14 + 127) << 23);
-#pragma unroll
-      for (int i = 0; i < QV; ++i) {
-        const int c = i * ST + tid, r = c / CPR, ch = c % CPR;
-        if (c >= N * CPR) break;
-        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-        uint32_t h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const __half2 t = __floats2half2_rn(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
-          h[e] = *reinterpret_cast<const uint32_t*>(&t);
-        }
-        *reinterpret_cast<uint4*>(sQ + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
-            make_uint4(h[0], h[1], h[2], h[3]);
-      }
-      fence_proxy_async_smem();
-      warp_arrive(q_full);
-
-      // ---- page scales: ids two tiles ahead, scales one tile ahead
-      const int32_t* row = a.table + static_cast<int64_t>(w.it.b) * a.ld_table;
-      const int n_pages = (w.s.len + PT - 1) / PT, half = key_lane >> 6;
-      auto page_id = [&](int tile) {
-        const int at = 2 * tile + half;
-        return at < n_pages ? row[at] : -1;
-      };
-      auto scales = [&](int page) {                           // a page that is not there: K = V = 0
-        if (page < 0 || page >= a.pages) return make_float2(0.0f, 1.0f);
-        const int64_t at = static_cast<int64_t>(page) * a.n_kv + w.it.hk;
-        return make_float2(a.sk[at], a.sv[at]);
-      };
-      float2 sc_next = scales(page_id(w.t0));
-      int id_next = page_id(w.t0 + 1);
       // rows whose bounds cut a tile: every key below `all_lo` or from `all_hi` on is hidden from some row
       const int last_v = min(v0 + N, w.s.n_virt) - 1;
       const int all_hi = a.causal ? min(w.s.len, w.s.pos0 + v0 / a.group + 1) : w.s.len;
@@ -595,15 +668,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       bool unset = true;                                      // some row has no reference yet (the warps agree)
       for (int i = 0; i < w.nt; ++i) {
         const int t = g + i, sb = t & 1, tile = w.t0 + i;
-        const float2 sc = sc_next;
-        if (i + 1 < w.nt) {
-          sc_next = scales(id_next);
-          if (i + 2 < w.nt) id_next = page_id(tile + 2);
-        }
         if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; }
         // the warps vote below: all of them leave together
         tc_fence_after();
-        const float cth = sc.x * q_down * a.scale_log2, lv = log2f(sc.y);
+        const float2 sc = s_scale[(t & 15) * 2 + (key_lane >> 6)];
+        const float cth = sc.x * s_qdown[seg & 3] * a.scale_log2, lv = log2f(sc.y);
         const int key = tile * TK + key_lane;
         const bool masked = tile * TK < all_lo || (tile + 1) * TK > all_hi;
         float x[RN];
@@ -697,6 +766,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       }
       if (!ok) break;
       g += w.nt;
+      ++seg;
       // ---- the rows' sums, then O
       {
         float y[32];
@@ -711,29 +781,27 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         if (whole) {
           s_fac[tid] = s == 0.0f ? 0.0f : 1.0f / (s * 128.0f);
         } else {
-          const int64_t slot = 2LL * blockIdx.x + (n_seg > 0);
+          const int64_t slot = 2LL * blockIdx.x + w.from_start;   // at most one part of each kind per CTA
           a.part_ml[slot * N + tid] = make_float2(s == 0.0f ? -INFINITY : -s_negm[tid], s * 128.0f);
         }
       }
       ok = warp_wait_bounded(o_full, (g - 1) & 1, abort_flag, nullptr);
       tc_fence_after();
       bar_softmax<ST>();
-      if (ok) {
-        float* part = a.part_o + (2LL * blockIdx.x + (n_seg > 0)) * N * HD + key_lane;
+      if (ok && (HD == 128 || key_lane < HD)) {               // warp-uniform: a dim per thread
+        float y[RN];
+        tmem_ld<RN>(tmem + lane_off + C::O_COL + row0, y);
+        if (whole) {
 #pragma unroll
-        for (int c = 0; c < RN / 16; ++c) {
-          float y[16];
-          tmem_ld16(tmem + lane_off + C::O_COL + row0 + 16 * c, y);
-          if (HD == 128 || key_lane < HD) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              const int r = row0 + 16 * c + k;
-              const int64_t at = s_row[r];
-              if (at < 0) continue;
-              if (whole) a.o[at + key_lane] = __float2bfloat16_rn(y[k] * s_fac[r]);
-              else part[r * HD] = y[k];
-            }
+          for (int r = 0; r < RN; ++r) {
+            const int64_t at = s_row[row0 + r];
+            const float f = s_fac[row0 + r];
+            if (at >= 0) a.o[at + key_lane] = __float2bfloat16_rn(y[r] * f);
           }
+        } else {
+          float* part = a.part_o + ((2LL * blockIdx.x + w.from_start) * N + row0) * HD + key_lane;
+#pragma unroll
+          for (int r = 0; r < RN; ++r) part[r * HD] = y[r];
         }
       }
       tc_fence_before();
@@ -752,41 +820,46 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   }
 }
 
-// Merges the partials of an item that the cut between CTAs c - 1 and c splits
-// first: m* = max m_s, O = sum 2^(m_s - m*) O_s / sum 2^(m_s - m*) l_s, in the
-// order of the CTAs.  Block (c, y) takes four of the item's rows, a warp each.
+// Merges the partials of an item that the cut between two CTAs splits first:
+// m* = max m_s, O = sum 2^(m_s - m*) O_s / sum 2^(m_s - m*) l_s, in the order
+// of the CTAs.  Block (c - 1, y) has the cut ahead of CTA c and takes four of
+// the item's rows, a warp each.
 template <int HD, int N>
 __global__ void __launch_bounds__(128) merge_paged_kernel(const PagedArgs a, int ctas) {
   pdl_enter();
   const int c = blockIdx.x + 1, lane = threadIdx.x & 31, r = blockIdx.y * 4 + (threadIdx.x >> 5);
-  const int64_t total = total_units<N>(a), start = cut(total, c, ctas);
-  if (start == cut(total, c + 1, ctas)) return;               // no units from here: a later cut is the same place
-  const Item it = locate<N>(a, start);
-  const int64_t first = start - it.off;                       // the item's first unit
+  const Place pl = a.place[c];
+  const Item it = pl.it;
+  if (it.off == 0 || cut(pl.total, c + 1, ctas) == pl.unit) return;   // no item is split here, or CTA c has no units
+  const int64_t first = pl.unit - it.off;                     // the item's first unit
   int k = c - 1;                                              // the CTA that ends at this cut
-  while (k > 0 && cut(total, k, ctas) == start) --k;
-  if (it.off == 0 || cut(total, k, ctas) > first) return;     // the item begins here, or an earlier cut splits it first
+  while (k > 0 && cut(pl.total, k, ctas) == pl.unit) --k;
+  if (cut(pl.total, k, ctas) > first) return;                 // an earlier cut splits the item first
   const SeqInfo s = seq_info<N>(a, it.b);
   const int v = it.rt * N + r;
   if (v >= s.n_virt) return;
-  const int64_t end = first + max(1, tile_range<N>(a, s, it.rt).y);
+  const int64_t nt = tile_range<N>(a, s, it.rt).y;
+  if (it.off >= nt) return;                                   // its tiles end ahead of the cut
   constexpr int PL = HD / 32;
   float m = -INFINITY, l = 0.0f, acc[PL] = {};
-  for (; k < ctas && cut(total, k, ctas) < end; ++k) {
-    const int64_t k0 = cut(total, k, ctas);
-    if (k0 == cut(total, k + 1, ctas)) continue;              // no units
-    const int64_t slot = 2LL * k + (k0 < first);              // the item is not the first one of CTA c - 1
-    const float2 ml = a.part_ml[slot * N + r];
-    float x[PL];
-    const float* p = a.part_o + (slot * N + r) * HD + lane * PL;
+  for (int64_t k0 = cut(pl.total, k, ctas); k < ctas && k0 < first + nt; ++k) {
+    const int64_t k1 = cut(pl.total, k + 1, ctas);
+    if (k0 < k1) {                                            // this CTA has tiles of the item
+      const int64_t slot = 2LL * k + (k0 <= first);
+      const float2 ml = a.part_ml[slot * N + r];
+      float x[PL];
+      const float* p = a.part_o + (slot * N + r) * HD + lane * PL;
 #pragma unroll
-    for (int d = 0; d < PL; ++d) x[d] = p[d];
-    if (ml.x == -INFINITY) continue;                          // no key of this part
-    const float mn = fmaxf(m, ml.x), f = ex2_approx(m - mn), h = ex2_approx(ml.x - mn);
-    l = l * f + ml.y * h;
+      for (int d = 0; d < PL; ++d) x[d] = p[d];
+      if (ml.x != -INFINITY) {                                // it saw a key
+        const float mn = fmaxf(m, ml.x), f = ex2_approx(m - mn), h = ex2_approx(ml.x - mn);
+        l = l * f + ml.y * h;
 #pragma unroll
-    for (int d = 0; d < PL; ++d) acc[d] = acc[d] * f + x[d] * h;
-    m = mn;
+        for (int d = 0; d < PL; ++d) acc[d] = acc[d] * f + x[d] * h;
+        m = mn;
+      }
+    }
+    k0 = k1;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bf16* o = a.o + (s.first + v / a.group) * a.ldo + static_cast<int64_t>(it.hk * a.group + v % a.group) * HD + lane * PL;
@@ -833,7 +906,8 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
                     c.cu, c.lens, c.table, c.batch, c.total, c.max_rows, c.max_len, c.ld_table, p.pages,
                     c.n_heads / c.n_kv, c.n_kv, c.ldq, c.ldo, c.causal, c.window,
                     1.4426950408889634f / sqrtf(static_cast<float>(HD)), part,
-                    reinterpret_cast<float2*>(part + 2LL * ctas * N * HD)};
+                    reinterpret_cast<float2*>(part + 2LL * ctas * N * HD),
+                    reinterpret_cast<Place*>(part + 2LL * ctas * N * (HD + 2))};
   cudaError_t e = launch_pdl(attn_paged_kernel<HD, N>, ctas, C::THREADS, C::SMEM, s, mk, mv, a);
   if (e == cudaSuccess && ctas > 1)
     e = launch_pdl(merge_paged_kernel<HD, N>, dim3(ctas - 1, N / 4), 128, 0, s, a, ctas);
@@ -844,7 +918,8 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
 
 size_t attention_paged_scratch(int max_rows, int group, int head_dim) {
   int dev = 0;
-  return 2ull * current_sms(&dev) * tile_rows(max_rows, group) * (head_dim + 2) * sizeof(float);
+  return static_cast<size_t>(current_sms(&dev)) *
+         (2ull * tile_rows(max_rows, group) * (head_dim + 2) * sizeof(float) + sizeof(Place));
 }
 
 const char* attention_paged(const RaggedCall& c, cudaStream_t s) {

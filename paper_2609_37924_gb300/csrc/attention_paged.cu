@@ -8,26 +8,31 @@
 // instead of being padded to 128, and a key is one TMEM lane = one thread,
 // whose page scales are two registers.
 //
-// A tile is 128 keys, two pages.  Roles of a CTA (16 warps):
-//   warp 0        streams the pages with TMA (one 4-D map for K, one for V^T)
-//                 and leaves their scales beside them;
-//   warps 14, 15  stage Q of the next work item while this one runs;
-//   warps 2-5     convert: e4m3 -> f16, exact, from shared memory into the
-//   (2-9)         TMEM A operands (K: a key per lane, V^T: a dim per lane); V
-//                 slots past the sequence become zeros here.  Up to 32 rows
-//                 K and V have four warps each;
-//   warp 1        S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
-//   warps 10-13   softmax: a key per thread, the values of up to 32 rows in
-//   (6-13)        registers.  The running maximum of a row is a reference that
-//                 moves only when a tile exceeds it by 2^8, so a tile costs
-//                 one vote of these warps and no reduction over the keys; the
-//                 sums of a row stay one partial per thread until the end of
-//                 the work item.
-// Precision: Q enters as f16 scaled by one power of two per tile of rows
-// (exact for values within 2^-28 of the largest), K and V are exact, the
-// probabilities times the page's V scale are rounded to f16 (11 bits) with
-// the row's reference at 2^7 to 2^15, so that a probability 2^-21 of the
-// largest still has all of them; scores, sums and O are fp32.
+// K enters the tensor cores as the e4m3 bytes that the page holds; Q is the sum
+// of three 8-bit floats (e4m3, e4m3, e5m2), each multiplied with K into the
+// same fp32 scores.  V^T is widened to f16, because the probabilities need
+// more than 8 bits.
+//
+// A tile is 128 keys, two pages.  Roles of a CTA (12 warps, or 16 for 64 rows):
+//   warp 0       streams the pages with TMA (one 4-D map for K, one for V^T)
+//                and leaves their scales beside them;
+//   warps 2, 3   stage Q of the next work item while this one runs;
+//   warps 4-7    convert V^T: e4m3 -> f16, exact, from shared memory into the
+//                TMEM A operand (a dim per lane); slots past the sequence
+//                become zeros here;
+//   warp 1       S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
+//   warps 8-     softmax: a key per thread, the values of up to 32 rows in
+//                registers.  The running maximum of a row is a reference that
+//                moves only when a tile exceeds it by 2^8, so a tile costs
+//                one vote of the four warps that share rows and no reduction
+//                over the keys; the sums of a row stay one partial per thread
+//                until the end of the work item.
+// Precision: Q is scaled by one power of two per tile of rows; the three terms
+// hold a bf16 value exactly if it is within 2^-10 of the tile's largest, and
+// to 2^-25 of the largest below that.  K and V are exact, the probabilities
+// times the page's V scale are rounded to f16 (11 bits) with the row's
+// reference at 2^7 to 2^15, so that a probability 2^-21 of the largest still
+// has all of them; scores, sums and O are fp32.
 //
 // Work: the tiles of all (sequence, KV head, row tile) items lie on one line,
 // each item followed by what its start and end cost, and the line is cut
@@ -202,15 +207,14 @@ struct PagedCfg {
   static constexpr int PAGE_BYTES = PT * HD;                 // of K or V^T, one head
   static constexpr int STAGE_BYTES = 4 * PAGE_BYTES;         // two pages of K, two of V^T
   static constexpr int STAGES = HD == 64 ? 8 : N == 64 ? 4 : 5;
-  static constexpr int Q_BYTES = HD / 64 * N * 128;          // HD/64 atoms of N rows x 64 dims, f16; two buffers
+  static constexpr int QT_BYTES = N * HD, Q_BYTES = 3 * QT_BYTES;   // three terms of N rows; two buffers
   static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
   static constexpr int RN = N < 32 ? N : 32, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
-  static constexpr int CONV_GROUPS = 3 - GROUPS;             // groups of four converting warps
-  static constexpr int SM_WARP = 2 + 4 * CONV_GROUPS, Q_WARP = 14, THREADS = 512;
+  static constexpr int THREADS = 256 + SM_THREADS;
   static constexpr int MISC = 1024 + N * 64;
   static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + MISC;
-  static constexpr int K_COL = 0, V_COL = 128, S_COL = 256, O_COL = 384;   // TMEM: two of K, V^T and S, one O
+  static constexpr int V_COL = 0, S_COL = 128, O_COL = 256;  // TMEM columns: two V^T, two S, one O
   static_assert(SMEM <= 232448, "shared memory");
 };
 
@@ -237,21 +241,47 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
   __syncwarp();
   if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
 }
-// the softmax warps' own barrier, and its vote
+// D(tmem) (+)= A(smem) * B(smem)^T, 8-bit floats, fp32 accumulator
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// A: e4m3; B: e4m3 or e5m2; both K-major
+__host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N, bool b_e5m2) {
+  return (1u << 4) | (b_e5m2 ? 1u << 10 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+// K-major 8-bit operand whose rows are HD bytes, swizzled over the row's width
+template <int HD>
+__device__ __forceinline__ uint64_t sdesc_rows8(uint32_t saddr) {
+  constexpr uint64_t sbo = 8 * HD, layout = HD == 128 ? 2 : 4;
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(1) << 16) | ((sbo >> 4) << 32) |
+         (static_cast<uint64_t>(1) << 46) | (layout << 61);
+}
+// 16-byte chunk `c` of row `r` in that layout
+template <int HD>
+__device__ __forceinline__ int chunk_at(int r, int c) {
+  return r * HD + ((HD == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4);
+}
+// barrier `id` of T threads, and its vote
 template <int T>
-__device__ __forceinline__ void bar_softmax() {
-  asm volatile("barrier.cta.sync 1, %0;" ::"n"(T) : "memory");
+__device__ __forceinline__ void bar_group(int id) {
+  asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(T) : "memory");
 }
 template <int T>
-__device__ __forceinline__ bool vote_softmax(bool p) {
+__device__ __forceinline__ bool vote_group(int id, bool p) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred a, b;\n\t"
       "setp.ne.u32 a, %1, 0;\n\t"
-      "barrier.cta.red.or.pred b, 1, %2, a;\n\t"
+      "barrier.cta.red.or.pred b, %3, %2, a;\n\t"
       "selp.u32 %0, 1, 0, b;\n\t}"
       : "=r"(r)
-      : "r"(static_cast<uint32_t>(p)), "n"(T)
+      : "r"(static_cast<uint32_t>(p)), "n"(T), "r"(id)
       : "memory");
   return r != 0;
 }
@@ -320,11 +350,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   uint8_t* sP = sQ + 2 * C::Q_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sP + 2 * C::P_BYTES);
   uint64_t *kv_full = bars, *kv_empty = bars + 8;             // [NST]
-  uint64_t *kt_full = bars + 16, *kt_empty = bars + 18;       // [2] converted K
   uint64_t *vt_full = bars + 20, *vt_empty = bars + 22;       // [2] converted V^T
   uint64_t *s_full = bars + 24, *p_full = bars + 26;          // [2]
   uint64_t *q_full = bars + 28, *q_empty = bars + 30;         // [2]
-  uint64_t *o_full = bars + 32, *drain = bars + 33;
+  uint64_t *o_full = bars + 32, *drain = bars + 33;           // o_full: a completion per PV
+  uint64_t* o_done = bars + 35;                               // a completion per segment, its last PV
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   Place* s_place = reinterpret_cast<Place*>(bars + 36);       // 32 bytes
@@ -343,11 +373,9 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < NST; ++i) {
       mbar_init(&kv_full[i], 1);
-      mbar_init(&kv_empty[i], 4 * C::CONV_GROUPS);
+      mbar_init(&kv_empty[i], 5);          // four converting warps, the MMAs that read K
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&kt_full[i], 4);
-      mbar_init(&kt_empty[i], 1);
       mbar_init(&vt_full[i], 4);
       mbar_init(&vt_empty[i], 1);
       mbar_init(&s_full[i], 1);
@@ -356,6 +384,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       mbar_init(&q_empty[i], 1);
     }
     mbar_init(o_full, 1);
+    mbar_init(o_done, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -450,7 +479,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     for (int i = max(0, g - NST); i < g; ++i) mbar_wait_bounded(&kv_full[i % NST], (i / NST) & 1, &never, nullptr);
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
-    constexpr uint32_t idesc_s = idesc_f16_f32(128, N, false), idesc_o = idesc_f16_f32(128, N, true);
+    constexpr uint32_t idesc_o = idesc_f16_f32(128, N, true);
     int g = 0, seg = 0;
     bool ok = true;
     while (ok && w.next()) {
@@ -458,19 +487,22 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       const int qb = seg & 1;
       if (!warp_wait_bounded(&q_full[qb], (seg >> 1) & 1, abort_flag, nullptr)) break;
       ++seg;
-      const uint64_t q0 = sdesc_kmajor_sw128(smem_u32(sQ + qb * C::Q_BYTES));
+      const uint64_t q0 = sdesc_rows8<HD>(smem_u32(sQ + qb * C::Q_BYTES));
       for (int i = 0; i <= w.nt; ++i) {
         if (i < w.nt) {
           // S^T of tile g + i; its buffer was read before p_full of two tiles ago, which PV has waited for
-          const int t = g + i, sb = t & 1;
-          if (!warp_wait_bounded(&kt_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; break; }
+          const int t = g + i, sb = t & 1, st = t % NST;
+          if (!warp_wait_bounded(&kv_full[st], (t / NST) & 1, abort_flag, nullptr)) { ok = false; break; }
           tc_fence_after();
+          const uint64_t k0 = sdesc_rows8<HD>(smem_u32(sKV + st * C::STAGE_BYTES));
 #pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk)
-            umma_bf16_ts(tmem + C::S_COL + sb * 64, tmem + C::K_COL + sb * 64 + 8 * kk,
-                         q0 + (((kk >> 2) * (N * 128) + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
+          for (int term = 0; term < 3; ++term)
+#pragma unroll
+            for (int kk = 0; kk < HD / 32; ++kk)
+              umma_f8(tmem + C::S_COL + sb * 64, k0 + 2 * kk, q0 + ((term * C::QT_BYTES) >> 4) + 2 * kk,
+                      idesc_f8_f32(128, N, term == 2), term + kk != 0);
           umma_commit(&s_full[sb]);
-          umma_commit(&kt_empty[sb]);
+          umma_commit(&kv_empty[st]);
           if (i == w.nt - 1) umma_commit(&q_empty[qb]);
         }
         if (i >= 1) {
@@ -484,6 +516,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
             umma_bf16_ts(tmem + C::O_COL, tmem + C::V_COL + pb * 64 + 8 * kk, p0 + kk * (2048 >> 4), idesc_o, i != 1 || kk != 0);
           umma_commit(o_full);
           umma_commit(&vt_empty[pb]);
+          if (i == w.nt) umma_commit(o_done);
         }
       }
       g += w.nt;
@@ -491,11 +524,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     umma_commit(drain);
     volatile int never = 0;
     warp_wait_bounded(drain, 0, &never, nullptr);
-  } else if (warp < C::SM_WARP) {
+  } else if (warp >= 4 && warp < 8) {
     // --------------------------------------------------------------- converters
-    const int row = (warp & 3) * 32 + lane;                   // key of K, dim of V^T
+    const int row = (warp & 3) * 32 + lane;                   // dim of V^T
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const bool do_k = C::CONV_GROUPS == 1 || warp < 6, do_v = C::CONV_GROUPS == 1 || warp >= 6;
     int g = 0;
     bool ok = true;
     while (ok && w.next()) {
@@ -504,29 +536,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         const uint32_t again = ((g >> 1) & 1) ^ 1;
         const uint8_t* base = sKV + st * C::STAGE_BYTES;
         if (!warp_wait_bounded(&kv_full[st], (g / NST) & 1, abort_flag, nullptr)) { ok = false; break; }
-        if (do_k) {
-          if (!warp_wait_bounded(&kt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
-          tc_fence_after();
-          const int r = row & (PT - 1);
-          const uint8_t* line = base + (row >> 6) * PB + r * HD;
-#pragma unroll
-          for (int c = 0; c < HD / 64; ++c) {
-            uint32_t out[32];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int ch = 4 * c + j;
-              const uint4 x = *reinterpret_cast<const uint4*>(line + ((HD == 128 ? ch ^ (r & 7) : ch ^ ((r >> 1) & 3)) << 4));
-              const uint32_t v[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) e4m3x4_f16x4(v[e], out[8 * j + 2 * e], out[8 * j + 2 * e + 1]);
-            }
-            tmem_st32(tmem + lane_off + C::K_COL + sb * 64 + 32 * c, out);
-          }
-          tmem_wait_st();
-          tc_fence_before();
-          warp_arrive(&kt_full[sb]);
-        }
-        if (do_v) {
+        {
           if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
           tc_fence_after();
           if (HD == 128 || row < 64) {                        // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
@@ -559,11 +569,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         warp_arrive(&kv_empty[st]);
       }
     }
-  } else if (warp >= C::Q_WARP) {
+  } else if (warp < 4) {
     // --------------------------------------------------------------- Q
-    // N rows as f16, scaled by a power of two so that the largest value is in 2^14 .. 2^15
-    constexpr int CPR = HD / 8, QV = N * CPR / 64;            // 16-byte chunks per row, per thread
-    const int tid = threadIdx.x - 32 * C::Q_WARP;
+    // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in three 8-bit terms
+    constexpr int CPR = HD / 8, QV = N * CPR / 64;            // groups of 8 dims per row, per thread
+    const int tid = threadIdx.x - 64;
     int seg = 0;
     while (w.next()) {
       if (w.nt == 0) continue;
@@ -592,24 +602,32 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       }
       top = __reduce_max_sync(0xffffffffu, top);
       if (lane == 0) s_qmax[warp & 1] = top;
-      asm volatile("barrier.cta.sync 2, 64;" ::: "memory");
+      asm volatile("barrier.cta.sync 3, 64;" ::: "memory");
       top = max(s_qmax[0], s_qmax[1]);
       const int e_max = max(static_cast<int>(top >> 23), 40) - 127;    // 2^e_max <= the largest
-      const float q_up = __int_as_float((14 - e_max + 127) << 23), q_down = __int_as_float((e_max - 14 + 127) << 23);
+      const float q_up = __int_as_float((7 - e_max + 127) << 23), q_down = __int_as_float((e_max - 7 + 127) << 23);
       const bool ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr);
       if (tid == 0) s_qdown[seg & 3] = q_down;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
         const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-        uint32_t h[4];
+        uint32_t term[3][2];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const __half2 t = __floats2half2_rn(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
-          h[e] = *reinterpret_cast<const uint32_t*>(&t);
+          float2 v = make_float2(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const __nv_fp8_interpretation_t f = k < 2 ? __NV_E4M3 : __NV_E5M2;
+            const uint32_t p = __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, f);
+            const float2 back = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(p), f)));
+            v = make_float2(v.x - back.x, v.y - back.y);
+            term[k][e >> 1] = (e & 1) ? term[k][e >> 1] | p << 16 : p;
+          }
         }
-        *reinterpret_cast<uint4*>(sQ + qb * C::Q_BYTES + (ch >> 3) * (N * 128) + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
-            make_uint4(h[0], h[1], h[2], h[3]);
+        uint8_t* dst = sQ + qb * C::Q_BYTES + chunk_at<HD>(r, ch >> 1) + (ch & 1) * 8;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(dst + k * C::QT_BYTES) = make_uint2(term[k][0], term[k][1]);
       }
       fence_proxy_async_smem();
       warp_arrive(&q_full[qb]);
@@ -619,7 +637,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       asm volatile(
           "{\n\t.reg .pred a, b;\n\t"
           "setp.ne.u32 a, %1, 0;\n\t"
-          "barrier.cta.red.or.pred b, 2, 64, a;\n\t"
+          "barrier.cta.red.or.pred b, 3, 64, a;\n\t"
           "selp.u32 %0, 1, 0, b;\n\t}"
           : "=r"(leave)
           : "r"(static_cast<uint32_t>(!ok))
@@ -628,34 +646,35 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
   } else {
     // --------------------------------------------------------------- softmax
-    constexpr int ST = C::SM_THREADS, RN = C::RN;
-    const int tid = threadIdx.x - 32 * C::SM_WARP, sw = warp - C::SM_WARP;
+    constexpr int RN = C::RN;
+    const int tid = (threadIdx.x - 256) & 127, sw = warp - 8;  // of the group of four warps that share rows
     const int key_lane = (warp & 3) * 32 + lane;              // this thread's key in a tile = its TMEM lane
-    const int row0 = (sw >> 2) * RN;                          // its rows: row0 .. row0 + RN - 1
+    const int grp = sw >> 2, row0 = grp * RN;                 // its rows: row0 .. row0 + RN - 1
+    const int own = row0 + tid;                               // thread tid < RN keeps row `own`'s reference
     float* my_red = s_red + (sw & 3) * N + row0;
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     int g = 0, seg = 0;
     bool ok = true;
     while (ok && w.next()) {
       const int v0 = w.it.rt * N;
-      if (tid < N) {
-        const int v = v0 + tid;
+      if (tid < RN) {
+        const int v = v0 + own;
         const bool in = v < w.s.n_virt;
         const int r = v / a.group, pos = w.s.pos0 + r;
-        s_row[tid] = in ? (w.s.first + r) * a.ldo + static_cast<int64_t>(w.it.hk * a.group + v % a.group) * HD : -1;
-        s_see[tid] = make_int2(in && a.window > 0 ? pos - a.window + 1 : 0,
+        s_row[own] = in ? (w.s.first + r) * a.ldo + static_cast<int64_t>(w.it.hk * a.group + v - r * a.group) * HD : -1;
+        s_see[own] = make_int2(in && a.window > 0 ? pos - a.window + 1 : 0,
                                in && a.causal ? min(w.s.len, pos + 1) : w.s.len);
-        s_negm[tid] = 0.0f;
+        s_negm[own] = 0.0f;
       }
       const bool whole = w.from_start && w.to_end;
       if (w.nt == 0) {                                        // no key: zeros
-        bar_softmax<ST>();
-        for (int r = 0; r < N; ++r)
+        bar_group<128>(1 + grp);
+        for (int r = row0; r < row0 + RN; ++r)
           if (s_row[r] >= 0 && tid < HD) a.o[s_row[r] + tid] = __float2bfloat16_rn(0.0f);
-        bar_softmax<ST>();
+        bar_group<128>(1 + grp);
         continue;
       }
-      bar_softmax<ST>();
+      bar_group<128>(1 + grp);
       // rows whose bounds cut a tile: every key below `all_lo` or from `all_hi` on is hidden from some row
       const int last_v = min(v0 + N, w.s.n_virt) - 1;
       const int all_hi = a.causal ? min(w.s.len, w.s.pos0 + v0 / a.group + 1) : w.s.len;
@@ -664,7 +683,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       float l[RN];
 #pragma unroll
       for (int r = 0; r < RN; ++r) l[r] = 0.0f;
-      bool has_ref = false;                                   // of row tid
+      bool has_ref = false;                                   // of row `own`
       bool unset = true;                                      // some row has no reference yet (the warps agree)
       for (int i = 0; i < w.nt; ++i) {
         const int t = g + i, sb = t & 1, tile = w.t0 + i;
@@ -694,7 +713,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         }
 #pragma unroll
         for (int r = 0; r < RN; r += 2) mx = fmax3(mx, x[r], x[r + 1]);
-        if (vote_softmax<ST>(unset || mx + lv > 8.0f || !ok)) {
+        if (vote_group<128>(1 + grp, unset || mx + lv > 8.0f || !ok)) {
           // ---- some row exceeds its reference (or has none): new references, O and the sums follow
           if (*abort_flag) ok = false;
           {
@@ -704,10 +723,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
             const float m = reduce_rows(y, [](float p, float q) { return fmaxf(p, q); });
             if (lane < RN) my_red[lane] = m;
           }
-          bar_softmax<ST>();
+          bar_group<128>(1 + grp);
           bool none = false;
-          if (tid < N) {
-            const float rel = fmaxf(fmaxf(s_red[tid], s_red[N + tid]), fmaxf(s_red[2 * N + tid], s_red[3 * N + tid]));
+          if (tid < RN) {
+            const float rel = fmaxf(fmaxf(s_red[own], s_red[N + own]), fmaxf(s_red[2 * N + own], s_red[3 * N + own]));
             float f = 1.0f, d = 0.0f;                         // factor of O and l, step of the reference
             if (!has_ref) {                                   // O and l of the row are still zero
               none = rel == -INFINITY;
@@ -717,15 +736,16 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
               d = rel;
               f = ex2_approx(-rel);
             }
-            s_negm[tid] -= d;
-            s_fac[tid] = f;
-            s_red[tid] = d;                                   // its four inputs have been read by this thread alone
+            s_negm[own] -= d;
+            s_fac[own] = f;
+            s_red[own] = d;                                   // its four inputs have been read by this thread alone
           }
-          unset = vote_softmax<ST>(none);
+          unset = vote_group<128>(1 + grp, none);
 #pragma unroll
           for (int r = 0; r < RN; ++r) x[r] -= s_red[row0 + r];
           if (i > 0) {
-            // O holds the segment's tiles up to i - 1 once their PV is complete
+            // O holds the segment's tiles up to i - 1 once their PV is complete (all but the last are: S of this tile
+            // was issued behind them)
             if (!warp_wait_bounded(o_full, (t - 1) & 1, abort_flag, nullptr)) ok = false;
             tc_fence_after();
 #pragma unroll
@@ -740,7 +760,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
 #pragma unroll
             for (int r = 0; r < RN; ++r) l[r] *= s_fac[row0 + r];
           }
-          if (vote_softmax<ST>(!ok)) { ok = false; break; }       // also: s_fac and s_red may be written again
+          if (vote_group<128>(1 + grp, !ok)) { ok = false; break; }       // also: s_fac and s_red may be written again
         }
         // ---- P = 2^x times the page's V scale, f16, a 128-byte line per key
         const float vs = sc.y * 128.0f;
@@ -766,7 +786,6 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       }
       if (!ok) break;
       g += w.nt;
-      ++seg;
       // ---- the rows' sums, then O
       {
         float y[32];
@@ -775,19 +794,21 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         const float s = reduce_rows(y, [](float p, float q) { return p + q; });
         if (lane < RN) my_red[lane] = s;
       }
-      bar_softmax<ST>();
-      if (tid < N) {
-        const float s = (s_red[tid] + s_red[N + tid]) + (s_red[2 * N + tid] + s_red[3 * N + tid]);
+      bar_group<128>(1 + grp);
+      if (tid < RN) {
+        const float s = (s_red[own] + s_red[N + own]) + (s_red[2 * N + own] + s_red[3 * N + own]);
         if (whole) {
-          s_fac[tid] = s == 0.0f ? 0.0f : 1.0f / (s * 128.0f);
+          s_fac[own] = s == 0.0f ? 0.0f : 1.0f / (s * 128.0f);
         } else {
           const int64_t slot = 2LL * blockIdx.x + w.from_start;   // at most one part of each kind per CTA
-          a.part_ml[slot * N + tid] = make_float2(s == 0.0f ? -INFINITY : -s_negm[tid], s * 128.0f);
+          a.part_ml[slot * N + own] = make_float2(s == 0.0f ? -INFINITY : -s_negm[own], s * 128.0f);
         }
       }
-      ok = warp_wait_bounded(o_full, (g - 1) & 1, abort_flag, nullptr);
+      // o_done, not o_full: the PV ahead of the last one may still be running as well
+      ok = warp_wait_bounded(o_done, seg & 1, abort_flag, nullptr);
+      ++seg;
       tc_fence_after();
-      bar_softmax<ST>();
+      bar_group<128>(1 + grp);
       if (ok && (HD == 128 || key_lane < HD)) {               // warp-uniform: a dim per thread
         float y[RN];
         tmem_ld<RN>(tmem + lane_off + C::O_COL + row0, y);
@@ -805,7 +826,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         }
       }
       tc_fence_before();
-      if (vote_softmax<ST>(!ok)) {                            // also: s_row, s_see, s_negm and s_fac may be written again
+      if (vote_group<128>(1 + grp, !ok)) {                            // also: s_row, s_see, s_negm and s_fac may be written again
         ok = false;
         break;
       }

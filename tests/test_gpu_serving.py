@@ -411,6 +411,24 @@ def test_page_attention_streams(T):
     close(outs[0][:32], ref, absum, torch.bfloat16, float(seqs[0][1].abs().max()))
 
 
+@pytest.mark.parametrize("heads,rows,lens", [((32, 16, 128), [200, 1], [200, 3000]), ((32, 16, 128), [100, 33, 7], [517, 40, 1025]),
+                                             ((4, 2, 64), [1] * 5, [64, 1, 700, 129, 63])])
+def test_page_attention_repeats(T, heads, rows, lens):
+    """The same bits on every call: items of several tiles, split between CTAs, one behind the other."""
+    Hq, Hkv, hd = heads
+    pool, table, seqs = filled(T, lens, Hkv, hd, 5)
+    q = torch.randn((sum(rows), Hq, hd), generator=gen(9), device="cuda").bfloat16()
+    o, first = torch.empty_like(q), run_paged(T, pool, table, q, cum(rows), lens, max(rows), max(lens), False, 0)
+    scratch = torch.empty(T.tadm_page_attention_scratch_size(len(rows), sum(rows), max(rows), max(lens), Hq, Hkv, hd, 1),
+                          dtype=torch.uint8, device="cuda")
+    args = i32(cum(rows)), i32(lens), table, max(rows), max(lens), scratch
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(300):
+        T.tadm_page_attention(q, pool, 1, o, *args)
+        differ += (o != first).sum()
+    assert int(differ) == 0
+
+
 # ------------------------------------------------------------------ bookkeeping
 class Pages:
     """The bookkeeping in plain Python."""

@@ -9,8 +9,7 @@
 // whose page scales are two registers.
 //
 // K enters the tensor cores as the e4m3 bytes that the page holds; Q is the sum
-// of three 8-bit floats (e4m3, e4m3, e5m2), each multiplied with K into the
-// same fp32 scores.  V^T is widened to f16, because the probabilities need
+// of two e4m3 terms, both multiplied with K into the same fp32 scores.  V^T is widened to f16, because the probabilities need
 // more than 8 bits.
 //
 // A tile is 128 keys, two pages.  Roles of a CTA (12 warps, or 16 for 64 rows):
@@ -27,9 +26,9 @@
 //                one vote of the four warps that share rows and no reduction
 //                over the keys; the sums of a row stay one partial per thread
 //                until the end of the work item.
-// Precision: Q is scaled by one power of two per tile of rows; the three terms
+// Precision: Q is scaled by one power of two per tile of rows; the two terms
 // hold a bf16 value exactly if it is within 2^-10 of the tile's largest, and
-// to 2^-25 of the largest below that.  K and V are exact, the probabilities
+// to 2^-18 of the largest below that.  K and V are exact, the probabilities
 // times the page's V scale are rounded to f16 (11 bits) with the row's
 // reference at 2^7 to 2^15, so that a probability 2^-21 of the largest still
 // has all of them; scores, sums and O are fp32.
@@ -154,39 +153,46 @@ __device__ __forceinline__ Item locate(const PagedArgs& a, int64_t unit) {
   return it;
 }
 
-// A CTA's walk over its units: one segment = consecutive tiles of one item.
+// A warp's walk over its CTA's units: one segment = consecutive tiles of one
+// item.  It lies in shared memory and lane 0 moves it: a segment's fields are
+// read where they are needed instead of filling registers.
 template <int N>
 struct Walk {
-  const PagedArgs& a;
   Item it;
-  int64_t left;
   SeqInfo s;
+  int64_t left;            // units behind the segment
   int t0, nt;              // tiles of the segment; none: the item sees nothing and has zeros to write
-  bool from_start, to_end; // it begins / ends with its item's tiles
-  bool fresh = true;
-  __device__ Walk(const PagedArgs& args, const Item& start, int64_t units) : a(args), it(start), left(units) {
-    if (left > 0) s = seq_info<N>(a, it.b);
+  int from_start, to_end;  // it begins / ends with its item's tiles
+  int started;
+  __device__ __forceinline__ bool next(const PagedArgs& a) {   // false: no segment left.  Warp-collective.
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) move(a);
+    __syncwarp();
+    return nt >= 0;
   }
-  __device__ bool next() {                 // false: no segment left
-    for (;; fresh = false) {
-      if (!fresh) step();
-      if (left <= 0) return false;
+  __device__ __forceinline__ void move(const PagedArgs& a) {
+    for (;;) {
+      if (started) step(a);
+      started = 1;
+      if (left <= 0) {
+        nt = -1;
+        return;
+      }
       const int2 r = tile_range<N>(a, s, it.rt);
       const int units = r.y + kItemUnits, off = it.off;
       const int take = static_cast<int>(min(left, static_cast<int64_t>(units - off)));
       const int lo = min(off, r.y), hi = min(off + take, r.y);
-      t0 = r.x + lo;
-      nt = hi - lo;
-      from_start = lo == 0;
-      to_end = hi == r.y;
       left -= take;
-      if (nt > 0 || (r.y == 0 && off == 0)) {
-        fresh = false;
-        return true;
+      if (hi > lo || (r.y == 0 && off == 0)) {
+        t0 = r.x + lo;
+        nt = hi - lo;
+        from_start = lo == 0;
+        to_end = hi == r.y;
+        return;
       }
     }
   }
-  __device__ void step() {                 // to the next item
+  __device__ __forceinline__ void step(const PagedArgs& a) {   // to the next item
     it.off = 0;
     if (++it.rt < s.n_rt) return;
     it.rt = 0;
@@ -207,12 +213,12 @@ struct PagedCfg {
   static constexpr int PAGE_BYTES = PT * HD;                 // of K or V^T, one head
   static constexpr int STAGE_BYTES = 4 * PAGE_BYTES;         // two pages of K, two of V^T
   static constexpr int STAGES = HD == 64 ? 8 : N == 64 ? 4 : 5;
-  static constexpr int QT_BYTES = N * HD, Q_BYTES = 3 * QT_BYTES;   // three terms of N rows; two buffers
+  static constexpr int QT_BYTES = N * HD, Q_BYTES = 2 * QT_BYTES;   // two terms of N rows; two buffers
   static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
   static constexpr int RN = N < 32 ? N : 32, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
   static constexpr int THREADS = 256 + SM_THREADS;
-  static constexpr int MISC = 1024 + N * 64;
+  static constexpr int MISC = 2560 + N * 40;
   static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + MISC;
   static constexpr int V_COL = 0, S_COL = 128, O_COL = 256;  // TMEM columns: two V^T, two S, one O
   static_assert(SMEM <= 232448, "shared memory");
@@ -251,9 +257,9 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// A: e4m3; B: e4m3 or e5m2; both K-major
-__host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N, bool b_e5m2) {
-  return (1u << 4) | (b_e5m2 ? 1u << 10 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+// A and B: e4m3, both K-major
+__host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N) {
+  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 // K-major 8-bit operand whose rows are HD bytes, swizzled over the row's width
 template <int HD>
@@ -290,12 +296,14 @@ __device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// v[r] of 32 lanes -> lane r gets the reduction of row r
+// v[r] of 32 lanes -> lanes r and r + 16 get the reduction of row r
 template <class Op>
-__device__ __forceinline__ float reduce_rows(float (&v)[32], Op op) {
+__device__ __forceinline__ float reduce_rows(float (&v)[16], Op op) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int i = 0; i < 16; ++i) v[i] = op(v[i], __shfl_xor_sync(0xffffffffu, v[i], 16));
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
     const bool up = lane & o;
 #pragma unroll
     for (int i = 0; i < o; ++i) {
@@ -362,8 +370,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
                                                               // softmax reads it later than the MMAs read Q)
   uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 42);  // [2] the staging warps' maxima
   float2* s_scale = reinterpret_cast<float2*>(bars + 64);     // [16][2] (K, V) scales of the pages of tile t at t % 16
+  Walk<N>* s_walk = reinterpret_cast<Walk<N>*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // [16] one per warp
+  static_assert(sizeof(Walk<N>) * 16 <= 1536, "walks");
   // per virtual row
-  float* s_negm = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // minus the reference
+  float* s_negm = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 2560);   // minus the reference
   float* s_fac = s_negm + N;
   float* s_red = s_fac + N;                                   // [4][N]
   int2* s_see = reinterpret_cast<int2*>(s_red + 4 * N);       // visible keys [x, y)
@@ -409,7 +419,13 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk<N> w(a, s_place->it, cut(s_place->total, blockIdx.x + 1, gridDim.x) - s_place->unit);
+  Walk<N>& w = s_walk[warp];
+  if (lane == 0) {
+    w.it = s_place->it;
+    w.left = cut(s_place->total, blockIdx.x + 1, gridDim.x) - s_place->unit;
+    w.started = 0;
+    if (w.left > 0) w.s = seq_info<N>(a, w.it.b);
+  }
 
   if (warp == 0) {
     // --------------------------------------------------------------- producer
@@ -421,10 +437,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       float2 sc;
     };
     int at = 0;                            // tiles of w's segment that are in a batch
-    bool more = w.next();
+    bool more = w.next(a);
     auto take = [&]() {
       while (more && at >= w.nt) {
-        more = w.next();
+        more = w.next(a);
         at = 0;
       }
       Batch b{0, 0, 0, 0, -1, make_float2(0.0f, 1.0f)};
@@ -482,28 +498,29 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     constexpr uint32_t idesc_o = idesc_f16_f32(128, N, true);
     int g = 0, seg = 0;
     bool ok = true;
-    while (ok && w.next()) {
-      if (w.nt == 0) continue;
+    while (ok && w.next(a)) {
+      const int nt = w.nt;
+      if (nt == 0) continue;
       const int qb = seg & 1;
       if (!warp_wait_bounded(&q_full[qb], (seg >> 1) & 1, abort_flag, nullptr)) break;
       ++seg;
       const uint64_t q0 = sdesc_rows8<HD>(smem_u32(sQ + qb * C::Q_BYTES));
-      for (int i = 0; i <= w.nt; ++i) {
-        if (i < w.nt) {
+      for (int i = 0; i <= nt; ++i) {
+        if (i < nt) {
           // S^T of tile g + i; its buffer was read before p_full of two tiles ago, which PV has waited for
           const int t = g + i, sb = t & 1, st = t % NST;
           if (!warp_wait_bounded(&kv_full[st], (t / NST) & 1, abort_flag, nullptr)) { ok = false; break; }
           tc_fence_after();
           const uint64_t k0 = sdesc_rows8<HD>(smem_u32(sKV + st * C::STAGE_BYTES));
 #pragma unroll
-          for (int term = 0; term < 3; ++term)
+          for (int term = 0; term < 2; ++term)
 #pragma unroll
             for (int kk = 0; kk < HD / 32; ++kk)
               umma_f8(tmem + C::S_COL + sb * 64, k0 + 2 * kk, q0 + ((term * C::QT_BYTES) >> 4) + 2 * kk,
-                      idesc_f8_f32(128, N, term == 2), term + kk != 0);
+                      idesc_f8_f32(128, N), term + kk != 0);
           umma_commit(&s_full[sb]);
           umma_commit(&kv_empty[st]);
-          if (i == w.nt - 1) umma_commit(&q_empty[qb]);
+          if (i == nt - 1) umma_commit(&q_empty[qb]);
         }
         if (i >= 1) {
           const int t = g + i - 1, pb = t & 1;
@@ -516,10 +533,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
             umma_bf16_ts(tmem + C::O_COL, tmem + C::V_COL + pb * 64 + 8 * kk, p0 + kk * (2048 >> 4), idesc_o, i != 1 || kk != 0);
           umma_commit(o_full);
           umma_commit(&vt_empty[pb]);
-          if (i == w.nt) umma_commit(o_done);
+          if (i == nt) umma_commit(o_done);
         }
       }
-      g += w.nt;
+      g += nt;
     }
     umma_commit(drain);
     volatile int never = 0;
@@ -530,8 +547,9 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     int g = 0;
     bool ok = true;
-    while (ok && w.next()) {
-      for (int i = 0; i < w.nt; ++i, ++g) {
+    while (ok && w.next(a)) {
+      const int nt = w.nt, keys = w.s.len - w.t0 * TK;        // keys from the segment's start on
+      for (int i = 0; i < nt; ++i, ++g) {
         const int st = g % NST, sb = g & 1;
         const uint32_t again = ((g >> 1) & 1) ^ 1;
         const uint8_t* base = sKV + st * C::STAGE_BYTES;
@@ -540,7 +558,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
           tc_fence_after();
           if (HD == 128 || row < 64) {                        // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
-            const int valid = w.s.len - (w.t0 + i) * TK;      // keys of this tile that exist
+            const int valid = keys - i * TK;                // keys of this tile that exist
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               const uint8_t* line = base + (2 + c) * PB + row * PT;
@@ -571,11 +589,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
   } else if (warp < 4) {
     // --------------------------------------------------------------- Q
-    // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in three 8-bit terms
+    // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in two e4m3 terms
     constexpr int CPR = HD / 8, QV = N * CPR / 64;            // groups of 8 dims per row, per thread
     const int tid = threadIdx.x - 64;
     int seg = 0;
-    while (w.next()) {
+    while (w.next(a)) {
       if (w.nt == 0) continue;
       const int qb = seg & 1, v0 = w.it.rt * N;
       uint4 qv[QV];
@@ -612,22 +630,20 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
         const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-        uint32_t term[3][2];
+        uint32_t term[2][2] = {};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float2 v = make_float2(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
-#pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            const __nv_fp8_interpretation_t f = k < 2 ? __NV_E4M3 : __NV_E5M2;
-            const uint32_t p = __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, f);
-            const float2 back = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(p), f)));
-            v = make_float2(v.x - back.x, v.y - back.y);
-            term[k][e >> 1] = (e & 1) ? term[k][e >> 1] | p << 16 : p;
-          }
+          // the upper four significant bits of each value, then the lower four
+          const float2 v = make_float2(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
+          const float2 u = make_float2(__uint_as_float((x[e] << 16) & 0xfff00000u) * q_up, __uint_as_float(x[e] & 0xfff00000u) * q_up);
+          const uint32_t p = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
+          const uint32_t r = __nv_cvt_float2_to_fp8x2(make_float2(v.x - u.x, v.y - u.y), __NV_SATFINITE, __NV_E4M3);
+          term[0][e >> 1] |= p << (16 * (e & 1));
+          term[1][e >> 1] |= r << (16 * (e & 1));
         }
         uint8_t* dst = sQ + qb * C::Q_BYTES + chunk_at<HD>(r, ch >> 1) + (ch & 1) * 8;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(dst + k * C::QT_BYTES) = make_uint2(term[k][0], term[k][1]);
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint2*>(dst + k * C::QT_BYTES) = make_uint2(term[k][0], term[k][1]);
       }
       fence_proxy_async_smem();
       warp_arrive(&q_full[qb]);
@@ -655,7 +671,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     const uint32_t lane_off = static_cast<uint32_t>((warp & 3) * 32) << 16;
     int g = 0, seg = 0;
     bool ok = true;
-    while (ok && w.next()) {
+    while (ok && w.next(a)) {
       const int v0 = w.it.rt * N;
       if (tid < RN) {
         const int v = v0 + own;
@@ -666,7 +682,6 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
                                in && a.causal ? min(w.s.len, pos + 1) : w.s.len);
         s_negm[own] = 0.0f;
       }
-      const bool whole = w.from_start && w.to_end;
       if (w.nt == 0) {                                        // no key: zeros
         bar_group<128>(1 + grp);
         for (int r = row0; r < row0 + RN; ++r)
@@ -685,8 +700,9 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       for (int r = 0; r < RN; ++r) l[r] = 0.0f;
       bool has_ref = false;                                   // of row `own`
       bool unset = true;                                      // some row has no reference yet (the warps agree)
-      for (int i = 0; i < w.nt; ++i) {
-        const int t = g + i, sb = t & 1, tile = w.t0 + i;
+      const int nt = w.nt, t0 = w.t0;
+      for (int i = 0; i < nt; ++i) {
+        const int t = g + i, sb = t & 1, tile = t0 + i;
         if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; }
         // the warps vote below: all of them leave together
         tc_fence_after();
@@ -716,12 +732,13 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         if (vote_group<128>(1 + grp, unset || mx + lv > 8.0f || !ok)) {
           // ---- some row exceeds its reference (or has none): new references, O and the sums follow
           if (*abort_flag) ok = false;
-          {
-            float y[32];
 #pragma unroll
-            for (int k = 0; k < 32; ++k) y[k] = k < RN ? x[k < RN ? k : 0] + lv : -INFINITY;
+          for (int c = 0; c < RN; c += 16) {
+            float y[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) y[k] = x[c + k] + lv;
             const float m = reduce_rows(y, [](float p, float q) { return fmaxf(p, q); });
-            if (lane < RN) my_red[lane] = m;
+            if (lane < 16) my_red[c + lane] = m;
           }
           bar_group<128>(1 + grp);
           bool none = false;
@@ -785,19 +802,20 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         warp_arrive(&p_full[sb]);
       }
       if (!ok) break;
-      g += w.nt;
+      g += nt;
       // ---- the rows' sums, then O
-      {
-        float y[32];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) y[k] = k < RN ? l[k < RN ? k : 0] : 0.0f;
+      for (int c = 0; c < RN; c += 16) {
+        float y[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) y[k] = l[c + k];
         const float s = reduce_rows(y, [](float p, float q) { return p + q; });
-        if (lane < RN) my_red[lane] = s;
+        if (lane < 16) my_red[c + lane] = s;
       }
       bar_group<128>(1 + grp);
       if (tid < RN) {
         const float s = (s_red[own] + s_red[N + own]) + (s_red[2 * N + own] + s_red[3 * N + own]);
-        if (whole) {
+        if (w.from_start && w.to_end) {
           s_fac[own] = s == 0.0f ? 0.0f : 1.0f / (s * 128.0f);
         } else {
           const int64_t slot = 2LL * blockIdx.x + w.from_start;   // at most one part of each kind per CTA
@@ -812,7 +830,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       if (ok && (HD == 128 || key_lane < HD)) {               // warp-uniform: a dim per thread
         float y[RN];
         tmem_ld<RN>(tmem + lane_off + C::O_COL + row0, y);
-        if (whole) {
+        if (w.from_start && w.to_end) {
 #pragma unroll
           for (int r = 0; r < RN; ++r) {
             const int64_t at = s_row[row0 + r];

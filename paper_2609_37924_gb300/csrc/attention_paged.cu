@@ -87,7 +87,7 @@ __device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s,
 // An item's units: its tiles, then kItemUnits for its start and end (Q, the
 // first references, the sums, O), measured in tiles; a row tile that sees
 // nothing has zeros to write there.
-constexpr int kItemUnits = 2;
+constexpr int kItemUnits = 5;
 // Units of a sequence and KV head.
 template <int N>
 __device__ __forceinline__ int64_t seq_units(const PagedArgs& a, int b) {
@@ -170,7 +170,8 @@ struct Walk {
     __syncwarp();
     return nt >= 0;
   }
-  __device__ __forceinline__ void move(const PagedArgs& a) {
+  // one copy for all roles: code that runs once per segment costs its instruction fetches
+  __device__ __noinline__ void move(const PagedArgs& a) {
     for (;;) {
       if (started) step(a);
       started = 1;
@@ -214,12 +215,13 @@ struct PagedCfg {
   static constexpr int STAGE_BYTES = 4 * PAGE_BYTES;         // two pages of K, two of V^T
   static constexpr int STAGES = HD == 64 ? 8 : N == 64 ? 4 : 5;
   static constexpr int QT_BYTES = N * HD, Q_BYTES = 2 * QT_BYTES;   // two terms of N rows; two buffers
+  static constexpr int RAW_BYTES = N * HD * 2;               // Q as it is in memory
   static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
   static constexpr int RN = N < 32 ? N : 32, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
   static constexpr int THREADS = 256 + SM_THREADS;
   static constexpr int MISC = 2560 + N * 40;
-  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + MISC;
+  static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + RAW_BYTES + MISC;
   static constexpr int V_COL = 0, S_COL = 128, O_COL = 256;  // TMEM columns: two V^T, two S, one O
   static_assert(SMEM <= 232448, "shared memory");
 };
@@ -272,6 +274,12 @@ __device__ __forceinline__ uint64_t sdesc_rows8(uint32_t saddr) {
 template <int HD>
 __device__ __forceinline__ int chunk_at(int r, int c) {
   return r * HD + ((HD == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3)) << 4);
+}
+// `bytes` (a multiple of 16) of global memory into shared memory, counted on the mbarrier
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
 }
 // barrier `id` of T threads, and its vote
 template <int T>
@@ -338,6 +346,17 @@ __device__ __forceinline__ void tmem_ld(uint32_t addr, float* v) {
     for (int i = 0; i < 16; ++i) v[i] = r[i];
   }
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
+  uint32_t r[8];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -356,13 +375,15 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   uint8_t* sKV = smem;
   uint8_t* sQ = sKV + NST * C::STAGE_BYTES;
   uint8_t* sP = sQ + 2 * C::Q_BYTES;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sP + 2 * C::P_BYTES);
+  uint8_t* sRaw = sP + 2 * C::P_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sRaw + C::RAW_BYTES);
   uint64_t *kv_full = bars, *kv_empty = bars + 8;             // [NST]
   uint64_t *vt_full = bars + 20, *vt_empty = bars + 22;       // [2] converted V^T
   uint64_t *s_full = bars + 24, *p_full = bars + 26;          // [2]
   uint64_t *q_full = bars + 28, *q_empty = bars + 30;         // [2]
   uint64_t *o_full = bars + 32, *drain = bars + 33;           // o_full: a completion per PV
   uint64_t* o_done = bars + 35;                               // a completion per segment, its last PV
+  uint64_t* raw_full = bars + 43;                             // a completion per segment, its rows of Q
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   Place* s_place = reinterpret_cast<Place*>(bars + 36);       // 32 bytes
@@ -395,6 +416,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
     mbar_init(o_full, 1);
     mbar_init(o_done, 1);
+    mbar_init(raw_full, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -590,27 +612,36 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   } else if (warp < 4) {
     // --------------------------------------------------------------- Q
     // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in two e4m3 terms
+    // (rolled loops: this runs once per item, straight-line code would wait for its instructions)
     constexpr int CPR = HD / 8, QV = N * CPR / 64;            // groups of 8 dims per row, per thread
     const int tid = threadIdx.x - 64;
     int seg = 0;
-    while (w.next(a)) {
-      if (w.nt == 0) continue;
-      const int qb = seg & 1, v0 = w.it.rt * N;
-      uint4 qv[QV];
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < QV; ++i) {
-        const int c = i * 64 + tid, v = v0 + c / CPR;
-        qv[i] = make_uint4(0, 0, 0, 0);
-        if (v < w.s.n_virt) {
-          const int t = v / a.group;
-          qv[i] = *reinterpret_cast<const uint4*>(a.q + (w.s.first + t) * a.ldq +
-                                                  static_cast<int64_t>(w.it.hk * a.group + v - t * a.group) * HD + (c % CPR) * 8);
+    bool more = w.next(a);
+    while (more && w.nt == 0) more = w.next(a);
+    // the rows of an item, copied by warp 2
+    auto fetch = [&]() {
+      const int v0 = w.it.rt * N, rows = min(N, w.s.n_virt - v0);
+      if (warp == 2) {
+        if (lane == 0) mbar_arrive_expect_tx(raw_full, rows * HD * 2);
+        __syncwarp();
+        for (int r = lane; r < rows; r += 32) {
+          const int t = (v0 + r) / a.group;
+          bulk_load(sRaw + r * HD * 2, a.q + (w.s.first + t) * a.ldq + static_cast<int64_t>(w.it.hk * a.group + v0 + r - t * a.group) * HD,
+                    HD * 2, raw_full);
         }
       }
-#pragma unroll
+      return rows;
+    };
+    while (more) {
+      const int qb = seg & 1, rows = fetch();
+      bool ok = warp_wait_bounded(raw_full, seg & 1, abort_flag, nullptr);
+      uint32_t top = 0;
+#pragma unroll 2
       for (int i = 0; i < QV; ++i) {
-        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+        const int c = i * 64 + tid;
+        if (c / CPR >= rows) break;
+        const uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
+        const uint32_t x[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const uint32_t lo = x[e] << 16 & 0x7fff0000u, hi = x[e] & 0x7fff0000u;
@@ -624,12 +655,14 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       top = max(s_qmax[0], s_qmax[1]);
       const int e_max = max(static_cast<int>(top >> 23), 40) - 127;    // 2^e_max <= the largest
       const float q_up = __int_as_float((7 - e_max + 127) << 23), q_down = __int_as_float((e_max - 7 + 127) << 23);
-      const bool ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr);
+      ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr) && ok;
       if (tid == 0) s_qdown[seg & 3] = q_down;
-#pragma unroll
+#pragma unroll 2
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
-        const uint32_t x[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+        uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
+        if (r >= rows) q = make_uint4(0, 0, 0, 0);
+        const uint32_t x[4] = {q.x, q.y, q.z, q.w};
         uint32_t term[2][2] = {};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -637,9 +670,9 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           const float2 v = make_float2(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
           const float2 u = make_float2(__uint_as_float((x[e] << 16) & 0xfff00000u) * q_up, __uint_as_float(x[e] & 0xfff00000u) * q_up);
           const uint32_t p = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
-          const uint32_t r = __nv_cvt_float2_to_fp8x2(make_float2(v.x - u.x, v.y - u.y), __NV_SATFINITE, __NV_E4M3);
+          const uint32_t l = __nv_cvt_float2_to_fp8x2(make_float2(v.x - u.x, v.y - u.y), __NV_SATFINITE, __NV_E4M3);
           term[0][e >> 1] |= p << (16 * (e & 1));
-          term[1][e >> 1] |= r << (16 * (e & 1));
+          term[1][e >> 1] |= l << (16 * (e & 1));
         }
         uint8_t* dst = sQ + qb * C::Q_BYTES + chunk_at<HD>(r, ch >> 1) + (ch & 1) * 8;
 #pragma unroll
@@ -648,7 +681,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       fence_proxy_async_smem();
       warp_arrive(&q_full[qb]);
       ++seg;
-      // both warps have read the maxima, and they go on or leave together
+      // both warps have read the maxima and the rows, and they go on or leave together
       uint32_t leave;
       asm volatile(
           "{\n\t.reg .pred a, b;\n\t"
@@ -659,7 +692,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           : "r"(static_cast<uint32_t>(!ok))
           : "memory");
       if (leave) break;
+      more = w.next(a);
+      while (more && w.nt == 0) more = w.next(a);
     }
+    volatile int never = 0;                                   // the rows have landed (a warp that gave up)
+    if (seg > 0) mbar_wait_bounded(raw_full, (seg - 1) & 1, &never, nullptr);
   } else {
     // --------------------------------------------------------------- softmax
     constexpr int RN = C::RN;
@@ -828,19 +865,23 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       tc_fence_after();
       bar_group<128>(1 + grp);
       if (ok && (HD == 128 || key_lane < HD)) {               // warp-uniform: a dim per thread
-        float y[RN];
-        tmem_ld<RN>(tmem + lane_off + C::O_COL + row0, y);
-        if (w.from_start && w.to_end) {
+        const bool direct = w.from_start && w.to_end;
+        float* part = a.part_o + ((2LL * blockIdx.x + w.from_start) * N + row0) * HD + key_lane;
+#pragma unroll 1
+        for (int c = 0; c < RN; c += 8) {
+          float y[8];
+          tmem_ld8(tmem + lane_off + C::O_COL + row0 + c, y);
+          if (direct) {
 #pragma unroll
-          for (int r = 0; r < RN; ++r) {
-            const int64_t at = s_row[row0 + r];
-            const float f = s_fac[row0 + r];
-            if (at >= 0) a.o[at + key_lane] = __float2bfloat16_rn(y[r] * f);
+            for (int r = 0; r < 8; ++r) {
+              const int64_t at = s_row[row0 + c + r];
+              const float f = s_fac[row0 + c + r];
+              if (at >= 0) a.o[at + key_lane] = __float2bfloat16_rn(y[r] * f);
+            }
+          } else {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) part[(c + r) * HD] = y[r];
           }
-        } else {
-          float* part = a.part_o + ((2LL * blockIdx.x + w.from_start) * N + row0) * HD + key_lane;
-#pragma unroll
-          for (int r = 0; r < RN; ++r) part[r * HD] = y[r];
         }
       }
       tc_fence_before();

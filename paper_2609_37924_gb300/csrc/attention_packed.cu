@@ -1,0 +1,423 @@
+// Attention of packed bf16 prompts, tcgen05.
+//
+// A CTA takes two tiles of 128 virtual rows (rows of one sequence, row-major,
+// then the query heads of one KV head) and walks the key tiles that they see,
+// 128 keys each.  Both tiles use a K or V tile while it is in shared memory,
+// and their softmaxes alternate with the tensor pipe:
+//   warp 0       streams K and V tiles with TMA into a ring of five slots;
+//   warp 1       O_A += P_A V(j), S_A = Q_A K(j+1)^T, then the same for B: one
+//                tile's softmax runs while the tensor pipe works on the other;
+//   warps 4-7    softmax of tile A, warps 8-11 of tile B: a row per thread.
+// P (bf16) lies in TMEM over the scores that it was made from, V is read as it
+// lies in memory (a key per line, an MN-major operand).  The reference maximum
+// of a row moves only when a tile exceeds it by 2^8; O is rescaled then.
+// A key tile that some row of a tile sees only in part keeps P in two bf16
+// terms, whose 128 columns are those of the scores: rows with few visible keys,
+// where single probabilities weigh most, do not feel the rounding to 8 bits.
+// What a tile holds behind the sequence's end belongs to its neighbour: those
+// scores are masked, and those lines of V are zeroed in shared memory.
+//
+// Bound: tensor pipe and exponentials alike: 4 * 128 * 128 * hd FLOP per 128 x
+// 128 exponentials, 1024 cycles of each at hd 128.
+#include "ragged.cuh"
+#include "serve.h"
+#include "softmax_rows.cuh"
+#include "tensor_map.h"
+
+namespace tadm {
+namespace {
+
+constexpr int TQ = 128, TK = 128;
+
+template <int HD_>
+struct PackedCfg {
+  static constexpr int HD = HD_;
+  static constexpr int TILE_BYTES = HD / 64 * 16384;          // HD/64 atoms of 128 rows x 64 dims: a tile of Q, K or V
+  static constexpr int SLOTS = 5;
+  static constexpr int SMEM = 1024 + (2 + SLOTS) * TILE_BYTES + 256;
+  static constexpr int S_COL = 0, O_COL = 256;                // two tiles of 128 columns, then of HD
+  static constexpr int THREADS = 384;
+};
+
+struct PackedArgs {
+  const bf16* q;
+  bf16* o;
+  const int32_t* cu;
+  int batch, total, max_rows, group, n_kv;
+  int64_t ldq, ldo;
+  int causal, window;
+  float scale_log2;
+};
+
+// MN-major B operand: lines of 64 dims (128 bytes, swizzled) per key, 8 keys
+// per 1024-byte atom; 64 further dims lie `mn_step` bytes on.
+__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t mn_step) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(mn_step >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+}
+
+// P = 2^(s * scale - m) of 32 columns as 16 packed pairs, added to the sums.
+__device__ __forceinline__ void exp32_pack(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, uint64_t (&ps2)[2],
+                                           uint32_t (&pk)[16]) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    float x0, x1;
+    f2_unpack(f2_fma(f2_pack(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), sc2, negm2), x0, x1);
+    const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+    ps2[j & 1] = f2_add(ps2[j & 1], f2_pack(p0, p1));
+    __nv_bfloat162 t = __floats2bfloat162_rn(p0, p1);
+    pk[j] = *reinterpret_cast<uint32_t*>(&t);
+  }
+}
+// The same where columns outside lo .. lim - 1 are hidden (P = 0), with the remainders P - bf16(P) as bf16 pairs.
+__device__ __forceinline__ void exp32_split(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, int lo, int lim,
+                                            uint64_t (&ps2)[2], uint32_t (&pk)[16], uint32_t* rest) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    float x0, x1;
+    f2_unpack(f2_fma(f2_pack(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), sc2, negm2), x0, x1);
+    const float p0 = 2 * j < lim && 2 * j >= lo ? ex2_approx(x0) : 0.0f;
+    const float p1 = 2 * j + 1 < lim && 2 * j + 1 >= lo ? ex2_approx(x1) : 0.0f;
+    ps2[j & 1] = f2_add(ps2[j & 1], f2_pack(p0, p1));
+    __nv_bfloat162 t = __floats2bfloat162_rn(p0, p1);
+    pk[j] = *reinterpret_cast<uint32_t*>(&t);
+    t = __floats2bfloat162_rn(p0 - __uint_as_float(pk[j] << 16), p1 - __uint_as_float(pk[j] & 0xffff0000u));
+    rest[j] = *reinterpret_cast<uint32_t*>(&t);
+  }
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+      "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+
+template <int HD_>
+__global__ void __launch_bounds__(384, 1)
+    attn_packed_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PackedArgs a) {
+  using C = PackedCfg<HD_>;
+  constexpr int HD = C::HD, NS = C::SLOTS;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem;                                         // two tiles
+  uint8_t* sKV = sQ + 2 * C::TILE_BYTES;                      // ring: K and V tiles in turn
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + NS * C::TILE_BYTES);
+  uint64_t *full = bars, *empty = bars + NS;                  // [NS]
+  uint64_t *q_full = bars + 2 * NS, *s_full = q_full + 2, *p_full = q_full + 4, *o_done = q_full + 6;   // [2] by tile
+  uint64_t* drain = q_full + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&q_full[i], 4);
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[i], 4);
+      mbar_init(&o_done[i], 1);
+    }
+    mbar_init(drain, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
+  pdl_enter();
+  // the blocks of a row tile are its KV heads; a sequence's last rows, which see most keys, come first
+  const int hk = blockIdx.x % a.n_kv;
+  int within;
+  auto pairs = [&](int b) { return (static_cast<int64_t>(seq_rows(a.cu, b, a.total, a.max_rows).n) * a.group + 2 * TQ - 1) / (2 * TQ); };
+  const int b = find_tile(a.batch, blockIdx.x / a.n_kv, pairs, &within);
+  if (b < 0) return;                                          // uniform; nothing allocated or in flight
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
+  const int n_virt = rows.n * a.group;
+  const int v0 = (static_cast<int>(pairs(b)) - 1 - within) * 2 * TQ;
+  // the key tiles of virtual tile h: first and end
+  auto range = [&](int h) {
+    const int lo_v = v0 + h * TQ, hi_v = min(lo_v + TQ, n_virt) - 1;
+    if (lo_v >= n_virt) return make_int2(0, 0);
+    const int end = a.causal ? hi_v / a.group + 1 : rows.n;
+    const int begin = a.window > 0 ? max(0, lo_v / a.group - a.window + 1) : 0;
+    return make_int2(begin / TK, (end + TK - 1) / TK);
+  };
+  const int2 rA = range(0), rB = range(1);
+  // whether tile h has a row that does not see all of key tile j
+  auto partial = [&](int h, int j) {
+    const int lo_v = v0 + h * TQ, hi_v = min(lo_v + TQ, n_virt) - 1;
+    return (j + 1) * TK > (a.causal ? lo_v / a.group + 1 : rows.n) || (a.window > 0 && j * TK < hi_v / a.group - a.window + 1);
+  };
+  const bool two = rB.y > 0;
+  const int j0 = rA.x, j1 = two ? max(rA.y, rB.y) : rA.y;
+
+  if (warp == 0) {
+    // --------------------------------------------------------------- producer
+    if (lane == 0) {
+      int g = 0;
+      bool ok = true;
+      for (int j = j0; ok && j < j1; ++j)
+        for (int m = 0; m < 2; ++m, ++g) {
+          const int sl = g % NS;
+          if (!mbar_wait_bounded(&empty[sl], ((g / NS) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
+          mbar_arrive_expect_tx(&full[sl], C::TILE_BYTES);
+          for (int s = 0; s < HD / 64; ++s)
+            tma_load_3d(sKV + sl * C::TILE_BYTES + s * 16384, m ? &tmV : &tmK, &full[sl], 64 * s, hk, rows.first + j * TK);
+        }
+      // every copy started here has landed before the CTA may exit
+      volatile int never = 0;
+      for (int i = max(0, g - NS); i < g; ++i) mbar_wait_bounded(&full[i % NS], (i / NS) & 1, &never, nullptr);
+    }
+  } else if (warp == 1) {
+    // --------------------------------------------------------------- MMA issuer
+    constexpr uint32_t idesc_s = idesc_bf16_f32(TQ, TK), idesc_o = idesc_bf16_f32(TQ, HD) | 1u << 16;   // V: MN-major
+    auto wait_kv = [&](int g) { return warp_wait_bounded(&full[g % NS], (g / NS) & 1, abort_flag, nullptr); };
+    auto scores = [&](int h, int g) {                         // S_h = Q_h K^T, K in ring place g
+      const uint64_t q0 = sdesc_kmajor_sw128(smem_u32(sQ + h * C::TILE_BYTES));
+      const uint64_t k0 = sdesc_kmajor_sw128(smem_u32(sKV + (g % NS) * C::TILE_BYTES));
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk)
+        umma_bf16(tmem + C::S_COL + h * TK, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
+                  k0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
+      umma_commit(&s_full[h]);
+    };
+    auto values = [&](int h, int g, bool first, bool split) { // O_h += P_h V
+      const uint64_t v0d = sdesc_mn_sw128(smem_u32(sKV + (g % NS) * C::TILE_BYTES), 16384);
+#pragma unroll
+      for (int kk = 0; kk < TK / 16; ++kk)
+        umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, !first || kk != 0);
+      if (split)
+#pragma unroll
+        for (int kk = 0; kk < TK / 16; ++kk)
+          umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + TK / 2 + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, 1);
+    };
+    bool ok = warp_wait_bounded(&q_full[0], 0, abort_flag, nullptr) && (!two || warp_wait_bounded(&q_full[1], 0, abort_flag, nullptr)) &&
+              wait_kv(0);
+    if (ok) {
+      tc_fence_after();
+      scores(0, 0);
+      if (two && rB.x == j0) scores(1, 0);
+      umma_commit(&empty[0]);
+    }
+    for (int j = j0; ok && j < j1; ++j) {
+      const int gv = 2 * (j - j0) + 1, gk = gv + 1;           // V(j), K(j + 1)
+      if (!wait_kv(gv)) break;
+      const int valid = rows.n - j * TK;
+      if (valid < TK) {                                       // the lines of V behind the sequence's end
+        uint8_t* sV = sKV + (gv % NS) * C::TILE_BYTES;
+        for (int i = lane; i < (TK - valid) * 8; i += 32)
+#pragma unroll
+          for (int s = 0; s < HD / 64; ++s) *reinterpret_cast<uint4*>(sV + s * 16384 + valid * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+        __syncwarp();
+      }
+      bool k_ready = false;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int2 r = h ? rB : rA;
+        if (j >= r.x && j < r.y) {
+          if (!warp_wait_bounded(&p_full[h], (j - r.x) & 1, abort_flag, nullptr)) { ok = false; break; }
+          tc_fence_after();
+          values(h, gv, j == r.x, partial(h, j));
+          if (j == r.y - 1) umma_commit(&o_done[h]);
+        }
+        if (h == 1 || !two) umma_commit(&empty[gv % NS]);
+        if (j + 1 >= r.x && j + 1 < r.y) {
+          if (!k_ready && !wait_kv(gk)) { ok = false; break; }
+          k_ready = true;
+          tc_fence_after();
+          scores(h, gk);
+        }
+        if (!two) break;
+      }
+      if (!ok) break;
+      if (j + 1 < j1) {
+        if (!k_ready && !wait_kv(gk)) break;                  // (every K tile of the walk is some tile's)
+        umma_commit(&empty[gk % NS]);
+      }
+    }
+    umma_commit(drain);
+    volatile int never = 0;
+    warp_wait_bounded(drain, 0, &never, nullptr);
+  } else if (warp >= 4 && (warp < 8 || two)) {
+    // --------------------------------------------------------------- softmax
+    const int h = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
+    const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
+    const int2 r = h ? rB : rA;
+    const int v = v0 + h * TQ + row;
+    const bool v_ok = v < n_virt;
+    const int pos = v_ok ? v / a.group : 0, head = hk * a.group + (v_ok ? v - pos * a.group : 0);
+    {
+      const uint4* src = reinterpret_cast<const uint4*>(a.q + (rows.first + pos) * a.ldq + static_cast<int64_t>(head) * HD);
+#pragma unroll
+      for (int s = 0; s < HD / 64; ++s) {
+        uint8_t* dst = sQ + h * C::TILE_BYTES + s * 16384 + row * 128;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) = v_ok ? src[s * 8 + c] : make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async_smem();
+      warp_arrive(&q_full[h]);
+    }
+    const uint32_t t_s = tmem + lane_off + C::S_COL + h * TK, t_o = tmem + lane_off + C::O_COL + h * HD;
+    const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2);
+    const int see_hi = a.causal && v_ok ? pos + 1 : rows.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
+    float m_ref = -INFINITY, l_run = 0.0f;
+    bool ok = true;
+    for (int j = r.x; j < r.y; ++j) {
+      if (!warp_wait_bounded(&s_full[h], (j - r.x) & 1, abort_flag, nullptr)) { ok = false; break; }
+      tc_fence_after();
+      const int lim = see_hi - j * TK, lo = see_lo - j * TK;  // visible columns of this tile: [lo, lim)
+      const bool masked = partial(h, j);
+      float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      uint32_t ra[32], rb[32];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        tmem_ld32_nowait(t_s + 64 * c, ra);
+        tmem_ld32_nowait(t_s + 64 * c + 32, rb);
+        tmem_wait_ld(ra);
+        tmem_bind(rb);
+        if (masked) max64<true>(ra, rb, lo - 64 * c, lim - 64 * c, mxa);
+        else max64<false>(ra, rb, 0, 64, mxa);
+      }
+      const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
+      float m_new = m_ref, factor = 1.0f;
+      if (m_ref == -INFINITY) {
+        m_new = m_tile;                                       // every earlier exponential was 0
+      } else if (m_tile > m_ref + 8.0f) {
+        m_new = m_tile;
+        factor = ex2_approx(m_ref - m_tile);
+      }
+      if (__any_sync(0xffffffffu, factor != 1.0f)) {
+        // O holds the tiles before this one: their PV was issued ahead of this tile's S
+#pragma unroll
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t ro[32];
+          tmem_ld32_nowait(t_o + 32 * c, ro);
+          tmem_wait_ld(ro);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) ro[k] = __float_as_uint(__uint_as_float(ro[k]) * factor);
+          tmem_st32(t_o + 32 * c, ro);
+        }
+        l_run *= factor;
+      }
+      const uint64_t negm2 = f2_pack(-m_new, -m_new);
+      uint64_t ps2[2] = {0, 0};
+      uint32_t pk[16];
+      if (masked) {
+        uint32_t rest[64];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {                         // P over the columns that have been read
+          tmem_ld32_nowait(t_s + 32 * c, ra);
+          tmem_wait_ld(ra);
+          exp32_split(ra, sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
+          tmem_st16(t_s + 16 * c, pk);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) pk[k] = rest[16 * c + k];
+          tmem_st16(t_s + TK / 2 + 16 * c, pk);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tmem_ld32_nowait(t_s + 32 * c, ra);
+          tmem_wait_ld(ra);
+          exp32_pack(ra, sc2, negm2, ps2, pk);
+          tmem_st16(t_s + 16 * c, pk);
+        }
+      }
+      float a0, a1, b0, b1;
+      f2_unpack(ps2[0], a0, a1);
+      f2_unpack(ps2[1], b0, b1);
+      l_run += (a0 + a1) + (b0 + b1);
+      m_ref = m_new;
+      tmem_wait_st();
+      tc_fence_before();
+      warp_arrive(&p_full[h]);
+    }
+    if (ok && warp_wait_bounded(&o_done[h], 0, abort_flag, nullptr)) {
+      tc_fence_after();
+      const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+      bf16* orow = a.o + (rows.first + pos) * a.ldo + static_cast<int64_t>(head) * HD;
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        uint32_t ro[32];
+        tmem_ld32_nowait(t_o + 32 * c, ro);
+        tmem_wait_ld(ro);
+        if (v_ok) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              __nv_bfloat162 t = __floats2bfloat162_rn(__uint_as_float(ro[k + 2 * e]) * inv, __uint_as_float(ro[k + 2 * e + 1]) * inv);
+              w[e] = *reinterpret_cast<uint32_t*>(&t);
+            }
+            *reinterpret_cast<uint4*>(orow + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// bf16 map {HD, kv heads, rows}, box {64, 1, 128}, 128-byte swizzle
+bool rows_map(CUtensorMap* m, const void* ptr, int hd, int n_kv, int total, int64_t ld) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(n_kv), static_cast<cuuint64_t>(total)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(hd) * 2, static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[3] = {64, 1, TK}, estr[3] = {1, 1, 1};
+  return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD>
+const char* launch(const RaggedCall& c, cudaStream_t s) {
+  using C = PackedCfg<HD>;
+  if (!tensor_map_encoder()) return "cuTensorMapEncodeTiled is unavailable";
+  int dev = 0;
+  current_sms(&dev);
+  static PerDevice ready;
+  if (ready.get(dev, [] {
+        return cudaFuncSetAttribute(attn_packed_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess ? 1 : 0;
+      }) <= 0)
+    return "attention smem attribute failed";
+  CUtensorMap mk, mv;
+  if (!rows_map(&mk, c.k, HD, c.n_kv, c.total, c.ldk) || !rows_map(&mv, c.v, HD, c.n_kv, c.total, c.ldv))
+    return "attention tensor map encode failed";
+  const int group = c.n_heads / c.n_kv;
+  const PackedArgs a{static_cast<const bf16*>(c.q), static_cast<bf16*>(c.o), c.cu, c.batch, c.total, c.max_rows, group, c.n_kv,
+                     c.ldq, c.ldo, c.causal, c.window, 1.4426950408889634f / sqrtf(static_cast<float>(HD))};
+  // at most one pair of tiles per 256 virtual rows and one more per sequence
+  const int64_t blocks = (static_cast<int64_t>(c.total) * group / (2 * TQ) + c.batch) * c.n_kv;
+  const cudaError_t e = launch_pdl(attn_packed_kernel<HD>, dim3(static_cast<unsigned>(blocks)), C::THREADS, C::SMEM, s, mk, mv, a);
+  return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
+}
+
+}  // namespace
+
+const char* attention_packed(const RaggedCall& c, cudaStream_t s) {
+  return c.head_dim == 128 ? launch<128>(c, s) : launch<64>(c, s);
+}
+
+}  // namespace tadm

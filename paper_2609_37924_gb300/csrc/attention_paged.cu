@@ -42,6 +42,7 @@
 
 #include "ragged.cuh"
 #include "serve.h"
+#include "softmax_rows.cuh"
 #include "tensor_map.h"
 
 namespace tadm {
@@ -244,10 +245,6 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_maj
 __device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr) {
   return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(1024 >> 4) << 16) |
          (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
-}
-__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
-  __syncwarp();
-  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
 }
 // D(tmem) (+)= A(smem) * B(smem)^T, 8-bit floats, fp32 accumulator
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {

@@ -82,7 +82,7 @@ tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, v
   c.n_heads = n_heads, c.n_kv = n_kv_heads, c.head_dim = head_dim;
   c.ldq = ldq, c.ldk = ldk, c.ldv = ldv, c.ldo = ldo;
   c.causal = causal, c.window = window, c.bf16 = dtype;
-  return attention_rows(c, stream) ? TADM_ERR_CUDA : TADM_OK;
+  return (dtype ? attention_packed(c, stream) : attention_rows(c, stream)) ? TADM_ERR_CUDA : TADM_OK;
 }
 
 tadm_status tadm_page_write(const tadm_page_pool* pool, int layer, const void* k, const void* v, const int32_t* cu_rows,

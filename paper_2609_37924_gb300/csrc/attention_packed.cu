@@ -6,7 +6,8 @@
 // and their softmaxes alternate with the tensor pipe:
 //   warp 0       streams K and V tiles with TMA into a ring of five slots;
 //   warp 1       O_A += P_A V(j), S_A = Q_A K(j+1)^T, then the same for B: one
-//                tile's softmax runs while the tensor pipe works on the other;
+//                tile's softmax runs while the tensor pipe works on the other,
+//                and P V of a tile's first 64 keys while it is at the others;
 //   warps 4-7    softmax of tile A, warps 8-11 of tile B: a row per thread.
 // P (bf16) lies in TMEM over the scores that it was made from, V is read as it
 // lies in memory (a key per line, an MN-major operand).  The reference maximum
@@ -49,6 +50,12 @@ struct PackedArgs {
   float scale_log2;
 };
 
+// `bytes` (a multiple of 16) of shared memory to global memory (bulk-group completion)
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)),
+               "r"(smem_u32(src)), "r"(bytes)
+               : "memory");
+}
 // MN-major B operand: lines of 64 dims (128 bytes, swizzled) per key, 8 keys
 // per 1024-byte atom; 64 further dims lie `mn_step` bytes on.
 __device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t mn_step) {
@@ -93,6 +100,12 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
       : "memory");
 }
 
+// A value that is the same in every lane, in a uniform register: what the MMA
+// warp computes from it (loop counts, ring places, descriptors) then needs no
+// move into one ahead of every MMA.
+__device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<uint32_t>(x))); }
+__device__ __forceinline__ int2 uniform(int2 x) { return make_int2(uniform(x.x), uniform(x.y)); }
+
 template <int HD_>
 __global__ void __launch_bounds__(384, 1)
     attn_packed_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PackedArgs a) {
@@ -104,8 +117,9 @@ __global__ void __launch_bounds__(384, 1)
   uint8_t* sKV = sQ + 2 * C::TILE_BYTES;                      // ring: K and V tiles in turn
   uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + NS * C::TILE_BYTES);
   uint64_t *full = bars, *empty = bars + NS;                  // [NS]
-  uint64_t *q_full = bars + 2 * NS, *s_full = q_full + 2, *p_full = q_full + 4, *o_done = q_full + 6;   // [2] by tile
-  uint64_t* drain = q_full + 8;
+  uint64_t *q_full = bars + 2 * NS, *s_full = q_full + 2, *o_done = q_full + 4;   // [2] by tile
+  uint64_t* p_full = q_full + 6;                              // [2][2] by tile, keys 0 .. 63 and 64 .. 127
+  uint64_t* drain = q_full + 10;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
@@ -118,7 +132,8 @@ __global__ void __launch_bounds__(384, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(&q_full[i], 4);
       mbar_init(&s_full[i], 1);
-      mbar_init(&p_full[i], 4);
+      mbar_init(&p_full[2 * i], 4);
+      mbar_init(&p_full[2 * i + 1], 4);
       mbar_init(&o_done[i], 1);
     }
     mbar_init(drain, 1);
@@ -141,7 +156,7 @@ __global__ void __launch_bounds__(384, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = 0;                                    // all 512 columns: the allocation starts at 0
   const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
   const int n_virt = rows.n * a.group;
   const int v0 = (static_cast<int>(pairs(b)) - 1 - within) * 2 * TQ;
@@ -153,15 +168,17 @@ __global__ void __launch_bounds__(384, 1)
     const int begin = a.window > 0 ? max(0, lo_v / a.group - a.window + 1) : 0;
     return make_int2(begin / TK, (end + TK - 1) / TK);
   };
-  const int2 rA = range(0), rB = range(1);
-  // whether tile h has a row that does not see all of key tile j
-  auto partial = [&](int h, int j) {
+  const int2 rA = uniform(range(0)), rB = uniform(range(1));
+  // the keys that every row of tile h sees: [x, y); a key tile that is not inside them is cut by the mask
+  auto common = [&](int h) {
     const int lo_v = v0 + h * TQ, hi_v = min(lo_v + TQ, n_virt) - 1;
-    return (j + 1) * TK > (a.causal ? lo_v / a.group + 1 : rows.n) || (a.window > 0 && j * TK < hi_v / a.group - a.window + 1);
+    return make_int2(a.window > 0 ? hi_v / a.group - a.window + 1 : 0, a.causal ? lo_v / a.group + 1 : rows.n);
   };
+  auto partial = [](int2 c, int j) { return (j + 1) * TK > c.y || j * TK < c.x; };
   const bool two = rB.y > 0;
-  const int j0 = rA.x, j1 = two ? max(rA.y, rB.y) : rA.y;
+  const int j0 = rA.x, j1 = two ? rB.y : rA.y, n_keys = uniform(rows.n);   // A's keys begin and end no later than B's
 
+  if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     // --------------------------------------------------------------- producer
     if (lane == 0) {
@@ -192,15 +209,22 @@ __global__ void __launch_bounds__(384, 1)
                   k0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
       umma_commit(&s_full[h]);
     };
-    auto values = [&](int h, int g, bool first, bool split) { // O_h += P_h V
+    const int2 cA = uniform(common(0)), cB = uniform(common(1));
+    auto values = [&](int h, int g, int n, bool first, bool split) {   // O_h += P_h V, the tile's n-th P
       const uint64_t v0d = sdesc_mn_sw128(smem_u32(sKV + (g % NS) * C::TILE_BYTES), 16384);
 #pragma unroll
-      for (int kk = 0; kk < TK / 16; ++kk)
-        umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, !first || kk != 0);
+      for (int half = 0; half < 2; ++half) {
+        if (!warp_wait_bounded(&p_full[2 * h + half], n & 1, abort_flag, nullptr)) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
+          umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, !first || kk != 0);
+      }
       if (split)
 #pragma unroll
         for (int kk = 0; kk < TK / 16; ++kk)
           umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + TK / 2 + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, 1);
+      return true;
     };
     bool ok = warp_wait_bounded(&q_full[0], 0, abort_flag, nullptr) && (!two || warp_wait_bounded(&q_full[1], 0, abort_flag, nullptr)) &&
               wait_kv(0);
@@ -212,8 +236,8 @@ __global__ void __launch_bounds__(384, 1)
     }
     for (int j = j0; ok && j < j1; ++j) {
       const int gv = 2 * (j - j0) + 1, gk = gv + 1;           // V(j), K(j + 1)
-      if (!wait_kv(gv)) break;
-      const int valid = rows.n - j * TK;
+      if (!wait_kv(gv) || (j + 1 < j1 && !wait_kv(gk))) break;
+      const int valid = n_keys - j * TK;
       if (valid < TK) {                                       // the lines of V behind the sequence's end
         uint8_t* sV = sKV + (gv % NS) * C::TILE_BYTES;
         for (int i = lane; i < (TK - valid) * 8; i += 32)
@@ -222,36 +246,29 @@ __global__ void __launch_bounds__(384, 1)
         fence_proxy_async_smem();
         __syncwarp();
       }
-      bool k_ready = false;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int2 r = h ? rB : rA;
-        if (j >= r.x && j < r.y) {
-          if (!warp_wait_bounded(&p_full[h], (j - r.x) & 1, abort_flag, nullptr)) { ok = false; break; }
-          tc_fence_after();
-          values(h, gv, j == r.x, partial(h, j));
-          if (j == r.y - 1) umma_commit(&o_done[h]);
-        }
-        if (h == 1 || !two) umma_commit(&empty[gv % NS]);
-        if (j + 1 >= r.x && j + 1 < r.y) {
-          if (!k_ready && !wait_kv(gk)) { ok = false; break; }
-          k_ready = true;
-          tc_fence_after();
-          scores(h, gk);
-        }
-        if (!two) break;
+      tc_fence_after();
+      if (j < rA.y) {
+        if (!values(0, gv, j - j0, j == j0, partial(cA, j))) break;
+        if (j == rA.y - 1) umma_commit(&o_done[0]);
       }
-      if (!ok) break;
-      if (j + 1 < j1) {
-        if (!k_ready && !wait_kv(gk)) break;                  // (every K tile of the walk is some tile's)
-        umma_commit(&empty[gk % NS]);
+      if (!two) umma_commit(&empty[gv % NS]);
+      if (j + 1 < rA.y) scores(0, gk);
+      if (two) {
+        if (j >= rB.x) {                                      // (j < rB.y: B's keys end last)
+          if (!values(1, gv, j - rB.x, j == rB.x, partial(cB, j))) break;
+          if (j == rB.y - 1) umma_commit(&o_done[1]);
+        }
+        umma_commit(&empty[gv % NS]);
+        if (j + 1 >= rB.x && j + 1 < rB.y) scores(1, gk);
       }
+      if (j + 1 < j1) umma_commit(&empty[gk % NS]);
     }
     umma_commit(drain);
     volatile int never = 0;
     warp_wait_bounded(drain, 0, &never, nullptr);
-  } else if (warp >= 4 && (warp < 8 || two)) {
+  } else if (warp >= 4) {
     // --------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");     // 56 + 224 + 224 = 3 * 168
     const int h = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
     const int2 r = h ? rB : rA;
@@ -273,55 +290,56 @@ __global__ void __launch_bounds__(384, 1)
     const uint32_t t_s = tmem + lane_off + C::S_COL + h * TK, t_o = tmem + lane_off + C::O_COL + h * HD;
     const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2);
     const int see_hi = a.causal && v_ok ? pos + 1 : rows.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
+    // O of a row is scaled by `factor` (and its sum): the tiles before this one are complete, their PV was issued ahead
+    // of this tile's S
     float m_ref = -INFINITY, l_run = 0.0f;
+    auto rescale = [&](float factor) {
+#pragma unroll
+      for (int c = 0; c < HD / 32; ++c) {
+        uint32_t ro[32];
+        tmem_ld32_nowait(t_o + 32 * c, ro);
+        tmem_wait_ld(ro);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) ro[k] = __float_as_uint(__uint_as_float(ro[k]) * factor);
+        tmem_st32(t_o + 32 * c, ro);
+      }
+      l_run *= factor;
+    };
+    const int2 all = common(h);
     bool ok = true;
     for (int j = r.x; j < r.y; ++j) {
       if (!warp_wait_bounded(&s_full[h], (j - r.x) & 1, abort_flag, nullptr)) { ok = false; break; }
       tc_fence_after();
-      const int lim = see_hi - j * TK, lo = see_lo - j * TK;  // visible columns of this tile: [lo, lim)
-      const bool masked = partial(h, j);
-      float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      uint32_t ra[32], rb[32];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        tmem_ld32_nowait(t_s + 64 * c, ra);
-        tmem_ld32_nowait(t_s + 64 * c + 32, rb);
-        tmem_wait_ld(ra);
-        tmem_bind(rb);
-        if (masked) max64<true>(ra, rb, lo - 64 * c, lim - 64 * c, mxa);
-        else max64<false>(ra, rb, 0, 64, mxa);
-      }
-      const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
-      float m_new = m_ref, factor = 1.0f;
-      if (m_ref == -INFINITY) {
-        m_new = m_tile;                                       // every earlier exponential was 0
-      } else if (m_tile > m_ref + 8.0f) {
-        m_new = m_tile;
-        factor = ex2_approx(m_ref - m_tile);
-      }
-      if (__any_sync(0xffffffffu, factor != 1.0f)) {
-        // O holds the tiles before this one: their PV was issued ahead of this tile's S
-#pragma unroll
-        for (int c = 0; c < HD / 32; ++c) {
-          uint32_t ro[32];
-          tmem_ld32_nowait(t_o + 32 * c, ro);
-          tmem_wait_ld(ro);
-#pragma unroll
-          for (int k = 0; k < 32; ++k) ro[k] = __float_as_uint(__uint_as_float(ro[k]) * factor);
-          tmem_st32(t_o + 32 * c, ro);
-        }
-        l_run *= factor;
-      }
-      const uint64_t negm2 = f2_pack(-m_new, -m_new);
+      // the row's scores stay in registers: P is written over them in TMEM
+      uint32_t s[4][32], pk[16];
+      tmem_ld32_nowait(t_s, s[0]);
+      tmem_ld32_nowait(t_s + 32, s[1]);
+      tmem_wait_ld(s[0]);
+      tmem_bind(s[1]);
+      tmem_ld32_nowait(t_s + 64, s[2]);
+      tmem_ld32_nowait(t_s + 96, s[3]);
       uint64_t ps2[2] = {0, 0};
-      uint32_t pk[16];
-      if (masked) {
+      if (partial(all, j)) {
+        const int lim = see_hi - j * TK, lo = see_lo - j * TK;   // visible columns of this tile: [lo, lim)
+        float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        max64<true>(s[0], s[1], lo, lim, mxa);
+        tmem_wait_ld(s[2]);
+        tmem_bind(s[3]);
+        max64<true>(s[2], s[3], lo - 64, lim - 64, mxa);
+        const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
+        float factor = 1.0f;
+        if (m_ref == -INFINITY) {
+          m_ref = m_tile;                                     // every earlier exponential was 0
+        } else if (m_tile > m_ref + 8.0f) {
+          factor = ex2_approx(m_ref - m_tile);
+          m_ref = m_tile;
+        }
+        if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
+        const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
         uint32_t rest[64];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {                         // P over the columns that have been read
-          tmem_ld32_nowait(t_s + 32 * c, ra);
-          tmem_wait_ld(ra);
-          exp32_split(ra, sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
+        for (int c = 0; c < 4; ++c) {
+          exp32_split(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
           tmem_st16(t_s + 16 * c, pk);
         }
 #pragma unroll
@@ -331,45 +349,73 @@ __global__ void __launch_bounds__(384, 1)
           tmem_st16(t_s + TK / 2 + 16 * c, pk);
         }
       } else {
+        float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        max64<false>(s[0], s[1], 0, 64, mxa);
+        tmem_wait_ld(s[2]);
+        tmem_bind(s[3]);
+        max64<false>(s[2], s[3], 0, 64, mxa);
+        const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
+        float factor = 1.0f;
+        if (m_ref == -INFINITY) {
+          m_ref = m_tile;
+        } else if (m_tile > m_ref + 8.0f) {
+          factor = ex2_approx(m_ref - m_tile);
+          m_ref = m_tile;
+        }
+        if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
+        const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          tmem_ld32_nowait(t_s + 32 * c, ra);
-          tmem_wait_ld(ra);
-          exp32_pack(ra, sc2, negm2, ps2, pk);
+          exp32_pack(s[c], sc2, negm2, ps2, pk);
           tmem_st16(t_s + 16 * c, pk);
+          if (c == 1) {                                       // P V of the first 64 keys may start
+            tmem_wait_st();
+            tc_fence_before();
+            warp_arrive(&p_full[2 * h]);
+          }
         }
       }
       float a0, a1, b0, b1;
       f2_unpack(ps2[0], a0, a1);
       f2_unpack(ps2[1], b0, b1);
       l_run += (a0 + a1) + (b0 + b1);
-      m_ref = m_new;
       tmem_wait_st();
       tc_fence_before();
-      warp_arrive(&p_full[h]);
+      if (partial(all, j)) warp_arrive(&p_full[2 * h]);
+      warp_arrive(&p_full[2 * h + 1]);
     }
-    if (ok && warp_wait_bounded(&o_done[h], 0, abort_flag, nullptr)) {
+    if (ok && r.y > 0 && warp_wait_bounded(&o_done[h], 0, abort_flag, nullptr)) {
+      // O leaves by rows: 64 dims of a thread's row through its own line of shared memory (Q's, which no MMA reads any
+      // more; 144 bytes apart, without bank conflicts), then one bulk copy
       tc_fence_after();
       const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
       bf16* orow = a.o + (rows.first + pos) * a.ldo + static_cast<int64_t>(head) * HD;
-#pragma unroll
-      for (int c = 0; c < HD / 32; ++c) {
-        uint32_t ro[32];
-        tmem_ld32_nowait(t_o + 32 * c, ro);
+      uint8_t* line = sQ + h * C::TILE_BYTES + row * (HD == 128 ? 144 : 128);
+#pragma unroll 1
+      for (int c = 0; c < HD / 64; ++c) {
+        uint32_t ro[32], rp[32];
+        tmem_ld32_nowait(t_o + 64 * c, ro);
+        tmem_ld32_nowait(t_o + 64 * c + 32, rp);
         tmem_wait_ld(ro);
-        if (v_ok) {
+        tmem_bind(rp);
+        if (c > 0) bulk_wait_read0();
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
-            uint32_t w[4];
+        for (int k = 0; k < 64; k += 8) {
+          uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              __nv_bfloat162 t = __floats2bfloat162_rn(__uint_as_float(ro[k + 2 * e]) * inv, __uint_as_float(ro[k + 2 * e + 1]) * inv);
-              w[e] = *reinterpret_cast<uint32_t*>(&t);
-            }
-            *reinterpret_cast<uint4*>(orow + 32 * c + k) = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int e = 0; e < 4; ++e) {
+            const float x = __uint_as_float(k < 32 ? ro[(k + 2 * e) & 31] : rp[(k + 2 * e) & 31]);
+            const float y = __uint_as_float(k < 32 ? ro[(k + 2 * e + 1) & 31] : rp[(k + 2 * e + 1) & 31]);
+            __nv_bfloat162 t = __floats2bfloat162_rn(x * inv, y * inv);
+            w[e] = *reinterpret_cast<uint32_t*>(&t);
           }
+          *reinterpret_cast<uint4*>(line + 2 * k) = make_uint4(w[0], w[1], w[2], w[3]);
         }
+        fence_proxy_async_smem();
+        if (v_ok) bulk_store(orow + 64 * c, line, 128);
+        bulk_commit();
       }
+      bulk_wait0();
     }
   }
   tc_fence_before();

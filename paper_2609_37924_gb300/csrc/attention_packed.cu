@@ -56,11 +56,49 @@ __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t 
                "r"(smem_u32(src)), "r"(bytes)
                : "memory");
 }
-// MN-major B operand: lines of 64 dims (128 bytes, swizzled) per key, 8 keys
-// per 1024-byte atom; 64 further dims lie `mn_step` bytes on.
-__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr, uint32_t mn_step) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(mn_step >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+// The MMAs of a tile in one block: the lane is elected once, and operands differ by constants in the low words of their
+// descriptors (the high word: 1024 bytes from one 8-row group to the next, descriptor version, 128-byte swizzle).  With
+// a 64-bit descriptor built per MMA their issue took longer than the MMAs.
+constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
+// low word of a K-major tile at saddr (16 further elements: 32 bytes on; 64: 16384 on)
+__device__ __forceinline__ uint32_t desc_k(uint32_t saddr) { return (saddr & 0x3FFFFu) >> 4 | 1u << 16; }
+// low word of a tile of V as it lies in memory, an MN-major operand: lines of 64 dims per key (16 further keys: 2048
+// bytes on), 64 further dims 16384 bytes on
+__device__ __forceinline__ uint32_t desc_mn(uint32_t saddr) { return (saddr & 0x3FFFFu) >> 4 | (16384u >> 4) << 16; }
+
+// D = A B^T over 64 dims (four MMAs), A and B in shared memory; acc: add to D
+__device__ __forceinline__ void umma4_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, e, t;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, %5, %5;\n\t"
+      "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t"
+      "add.u32 x, %1, 2;\n\tadd.u32 y, %2, 2;\n\tmov.b64 da, {x, %5};\n\tmov.b64 db, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, t;\n\t"
+      "add.u32 x, %1, 4;\n\tadd.u32 y, %2, 4;\n\tmov.b64 da, {x, %5};\n\tmov.b64 db, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, t;\n\t"
+      "add.u32 x, %1, 6;\n\tadd.u32 y, %2, 6;\n\tmov.b64 da, {x, %5};\n\tmov.b64 db, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, t;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHi)
+      : "memory");
+}
+// D += A B over 64 keys (four MMAs), A = P in TMEM (8 columns per 16 keys), B = V, MN-major
+__device__ __forceinline__ void umma4_ts_mn(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, e, t;\n\t.reg .b64 db;\n\t.reg .b32 x, y;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, %5, %5;\n\t"
+      "mov.b64 db, {%2, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t"
+      "add.u32 x, %1, 8;\n\tadd.u32 y, %2, 128;\n\tmov.b64 db, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, t;\n\t"
+      "add.u32 x, %1, 16;\n\tadd.u32 y, %2, 256;\n\tmov.b64 db, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, t;\n\t"
+      "add.u32 x, %1, 24;\n\tadd.u32 y, %2, 384;\n\tmov.b64 db, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, t;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHi)
+      : "memory");
 }
 
 // P = 2^(s * scale - m) of 32 columns as 16 packed pairs, added to the sums.
@@ -199,47 +237,50 @@ __global__ void __launch_bounds__(384, 1)
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
     constexpr uint32_t idesc_s = idesc_bf16_f32(TQ, TK), idesc_o = idesc_bf16_f32(TQ, HD) | 1u << 16;   // V: MN-major
-    auto wait_kv = [&](int g) { return warp_wait_bounded(&full[g % NS], (g / NS) & 1, abort_flag, nullptr); };
-    auto scores = [&](int h, int g) {                         // S_h = Q_h K^T, K in ring place g
-      const uint64_t q0 = sdesc_kmajor_sw128(smem_u32(sQ + h * C::TILE_BYTES));
-      const uint64_t k0 = sdesc_kmajor_sw128(smem_u32(sKV + (g % NS) * C::TILE_BYTES));
+    const int2 cA = uniform(common(0)), cB = uniform(common(1));
+    struct Slot {                                             // a place of the ring and the parity of its phase
+      uint32_t at, parity;
+    };
+    auto after = [](Slot s) { return s.at + 1 == NS ? Slot{0, s.parity ^ 1} : Slot{s.at + 1, s.parity}; };
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, nullptr);
+    };
+    const uint32_t q_lo = desc_k(smem_u32(sQ)), kv_lo = smem_u32(sKV);
+    auto scores = [&](int h, Slot s) {                        // S_h = Q_h K^T
+      const uint32_t q0 = q_lo + h * (C::TILE_BYTES >> 4), k0 = desc_k(kv_lo + s.at * C::TILE_BYTES);
 #pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk)
-        umma_bf16(tmem + C::S_COL + h * TK, q0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
-                  k0 + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4), idesc_s, kk != 0);
+      for (int c = 0; c < HD / 64; ++c) umma4_ss(tmem + C::S_COL + h * TK, q0 + c * 1024, k0 + c * 1024, idesc_s, c);
       umma_commit(&s_full[h]);
     };
-    const int2 cA = uniform(common(0)), cB = uniform(common(1));
-    auto values = [&](int h, int g, int n, bool first, bool split) {   // O_h += P_h V, the tile's n-th P
-      const uint64_t v0d = sdesc_mn_sw128(smem_u32(sKV + (g % NS) * C::TILE_BYTES), 16384);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (!warp_wait_bounded(&p_full[2 * h + half], n & 1, abort_flag, nullptr)) return false;
-        tc_fence_after();
-#pragma unroll
-        for (int kk = 4 * half; kk < 4 * half + 4; ++kk)
-          umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, !first || kk != 0);
+    auto values = [&](int h, Slot s, int n, bool first, bool split) {   // O_h += P_h V, the tile's n-th P
+      const uint32_t vd = desc_mn(kv_lo + s.at * C::TILE_BYTES), o = tmem + C::O_COL + h * HD, p = tmem + C::S_COL + h * TK;
+      if (!wait(&p_full[2 * h], n & 1)) return false;
+      tc_fence_after();
+      umma4_ts_mn(o, p, vd, idesc_o, !first);
+      if (!wait(&p_full[2 * h + 1], n & 1)) return false;
+      tc_fence_after();
+      umma4_ts_mn(o, p + 32, vd + 512, idesc_o, 1);
+      if (split) {
+        umma4_ts_mn(o, p + 64, vd, idesc_o, 1);
+        umma4_ts_mn(o, p + 96, vd + 512, idesc_o, 1);
       }
-      if (split)
-#pragma unroll
-        for (int kk = 0; kk < TK / 16; ++kk)
-          umma_bf16_ts(tmem + C::O_COL + h * HD, tmem + C::S_COL + h * TK + TK / 2 + 8 * kk, v0d + kk * (2048 >> 4), idesc_o, 1);
       return true;
     };
-    bool ok = warp_wait_bounded(&q_full[0], 0, abort_flag, nullptr) && (!two || warp_wait_bounded(&q_full[1], 0, abort_flag, nullptr)) &&
-              wait_kv(0);
+    Slot sk{0, 0};                                            // K(j0)
+    bool ok = wait(&q_full[0], 0) && (!two || wait(&q_full[1], 0)) && wait(&full[0], 0);
     if (ok) {
       tc_fence_after();
-      scores(0, 0);
-      if (two && rB.x == j0) scores(1, 0);
+      scores(0, sk);
+      if (two && rB.x == j0) scores(1, sk);
       umma_commit(&empty[0]);
     }
     for (int j = j0; ok && j < j1; ++j) {
-      const int gv = 2 * (j - j0) + 1, gk = gv + 1;           // V(j), K(j + 1)
-      if (!wait_kv(gv) || (j + 1 < j1 && !wait_kv(gk))) break;
+      const Slot sv = after(sk);                              // V(j), then K(j + 1)
+      sk = after(sv);
+      if (!wait(&full[sv.at], sv.parity) || (j + 1 < j1 && !wait(&full[sk.at], sk.parity))) break;
       const int valid = n_keys - j * TK;
       if (valid < TK) {                                       // the lines of V behind the sequence's end
-        uint8_t* sV = sKV + (gv % NS) * C::TILE_BYTES;
+        uint8_t* sV = sKV + sv.at * C::TILE_BYTES;
         for (int i = lane; i < (TK - valid) * 8; i += 32)
 #pragma unroll
           for (int s = 0; s < HD / 64; ++s) *reinterpret_cast<uint4*>(sV + s * 16384 + valid * 128 + i * 16) = make_uint4(0, 0, 0, 0);
@@ -248,20 +289,20 @@ __global__ void __launch_bounds__(384, 1)
       }
       tc_fence_after();
       if (j < rA.y) {
-        if (!values(0, gv, j - j0, j == j0, partial(cA, j))) break;
+        if (!values(0, sv, j - j0, j == j0, partial(cA, j))) break;
         if (j == rA.y - 1) umma_commit(&o_done[0]);
       }
-      if (!two) umma_commit(&empty[gv % NS]);
-      if (j + 1 < rA.y) scores(0, gk);
+      if (!two) umma_commit(&empty[sv.at]);
+      if (j + 1 < rA.y) scores(0, sk);
       if (two) {
         if (j >= rB.x) {                                      // (j < rB.y: B's keys end last)
-          if (!values(1, gv, j - rB.x, j == rB.x, partial(cB, j))) break;
+          if (!values(1, sv, j - rB.x, j == rB.x, partial(cB, j))) break;
           if (j == rB.y - 1) umma_commit(&o_done[1]);
         }
-        umma_commit(&empty[gv % NS]);
-        if (j + 1 >= rB.x && j + 1 < rB.y) scores(1, gk);
+        umma_commit(&empty[sv.at]);
+        if (j + 1 >= rB.x && j + 1 < rB.y) scores(1, sk);
       }
-      if (j + 1 < j1) umma_commit(&empty[gk % NS]);
+      if (j + 1 < j1) umma_commit(&empty[sk.at]);
     }
     umma_commit(drain);
     volatile int never = 0;

@@ -1,8 +1,8 @@
 // Attention of packed bf16 prompts, tcgen05.
 //
-// A CTA takes two tiles of 128 virtual rows (rows of one sequence, row-major,
-// then the query heads of one KV head) and walks the key tiles that they see,
-// 128 keys each.  Both tiles use a K or V tile while it is in shared memory,
+// A CTA takes one or two tiles of up to 128 virtual rows (as many whole rows of
+// one sequence as fit, row-major, then the query heads of one KV head) and
+// walks the key tiles that they see, 128 keys each.  Two tiles both use a K or V tile while it is in shared memory,
 // and their softmaxes alternate with the tensor pipe:
 //   warp 0       streams K and V tiles with TMA into a ring of five slots;
 //   warp 1       O_A += P_A V(j), S_A = Q_A K(j+1)^T, then the same for B: one
@@ -30,22 +30,26 @@ namespace {
 
 constexpr int TQ = 128, TK = 128;
 
-template <int HD_>
+// NT row tiles per CTA
+template <int HD_, int NT_>
 struct PackedCfg {
-  static constexpr int HD = HD_;
+  static constexpr int HD = HD_, NT = NT_;
   static constexpr int TILE_BYTES = HD / 64 * 16384;          // HD/64 atoms of 128 rows x 64 dims: a tile of Q, K or V
-  static constexpr int SLOTS = 5;
-  static constexpr int SMEM = 1024 + (2 + SLOTS) * TILE_BYTES + 256;
-  static constexpr int S_COL = 0, O_COL = 256;                // two tiles of 128 columns, then of HD
-  static constexpr int THREADS = 384;
+  static constexpr int SLOTS = NT == 2 ? 5 : 4;
+  static constexpr int MIN_BLOCKS = 3 - NT;
+  static constexpr int SMEM = 1024 + (NT + SLOTS) * TILE_BYTES + 256;
+  static constexpr int S_COL = 0, O_COL = NT * TK, TMEM_COLS = NT * 256;   // NT tiles of 128 columns, then of HD
+  static constexpr int THREADS = 128 + NT * 128;
+  static constexpr int REGS = NT == 2 ? 224 : 200;            // of a softmax thread; the other warps keep 56
+  static_assert(56 + NT * REGS <= (NT + 1) * (NT == 2 ? 168 : 128), "registers at launch");
 };
 
 struct PackedArgs {
-  const bf16* q;
   bf16* o;
   const int32_t* cu;
   int batch, total, max_rows, group, n_kv;
-  int64_t ldq, ldo;
+  int tq, rows;            // rows of a sequence in a tile, virtual rows (tq * group <= 128)
+  int64_t ldo;
   int causal, window;
   float scale_log2;
 };
@@ -144,15 +148,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16
 __device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<uint32_t>(x))); }
 __device__ __forceinline__ int2 uniform(int2 x) { return make_int2(uniform(x.x), uniform(x.y)); }
 
-template <int HD_>
-__global__ void __launch_bounds__(384, 1)
-    attn_packed_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PackedArgs a) {
-  using C = PackedCfg<HD_>;
-  constexpr int HD = C::HD, NS = C::SLOTS;
+template <int HD_, int NT_>
+__global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, NT_>::MIN_BLOCKS)
+    attn_packed_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                       const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO, const PackedArgs a) {
+  using C = PackedCfg<HD_, NT_>;
+  constexpr int HD = C::HD, NT = C::NT, NS = C::SLOTS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* sQ = smem;                                         // two tiles
-  uint8_t* sKV = sQ + 2 * C::TILE_BYTES;                      // ring: K and V tiles in turn
+  uint8_t* sQ = smem;                                         // NT tiles
+  uint8_t* sKV = sQ + NT * C::TILE_BYTES;                     // ring: K and V tiles in turn
   uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + NS * C::TILE_BYTES);
   uint64_t *full = bars, *empty = bars + NS;                  // [NS]
   uint64_t *q_full = bars + 2 * NS, *s_full = q_full + 2, *o_done = q_full + 4;   // [2] by tile
@@ -168,7 +173,7 @@ __global__ void __launch_bounds__(384, 1)
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&q_full[i], 4);
+      mbar_init(&q_full[i], 1);
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[2 * i], 4);
       mbar_init(&p_full[2 * i + 1], 4);
@@ -177,6 +182,7 @@ __global__ void __launch_bounds__(384, 1)
     mbar_init(drain, 1);
     *abort_flag = 0;
     fence_mbar_init();
+    tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
     tma_prefetch_desc(&tmV);
   }
@@ -184,36 +190,36 @@ __global__ void __launch_bounds__(384, 1)
   // the blocks of a row tile are its KV heads; a sequence's last rows, which see most keys, come first
   const int hk = blockIdx.x % a.n_kv;
   int within;
-  auto pairs = [&](int b) { return (static_cast<int64_t>(seq_rows(a.cu, b, a.total, a.max_rows).n) * a.group + 2 * TQ - 1) / (2 * TQ); };
+  auto pairs = [&](int b) { return (static_cast<int64_t>(seq_rows(a.cu, b, a.total, a.max_rows).n) + NT * a.tq - 1) / (NT * a.tq); };
   const int b = find_tile(a.batch, blockIdx.x / a.n_kv, pairs, &within);
   if (b < 0) return;                                          // uniform; nothing allocated or in flight
   if (warp == 1) {
-    tmem_alloc(tmem_slot, 512);
+    tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = 0;                                    // all 512 columns: the allocation starts at 0
+  const uint32_t tmem = uniform(static_cast<int>(*tmem_slot));
   const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
   const int n_virt = rows.n * a.group;
-  const int v0 = (static_cast<int>(pairs(b)) - 1 - within) * 2 * TQ;
+  const int v0 = (static_cast<int>(pairs(b)) - 1 - within) * NT * a.rows;
   // the key tiles of virtual tile h: first and end
   auto range = [&](int h) {
-    const int lo_v = v0 + h * TQ, hi_v = min(lo_v + TQ, n_virt) - 1;
+    const int lo_v = v0 + h * a.rows, hi_v = min(lo_v + a.rows, n_virt) - 1;
     if (lo_v >= n_virt) return make_int2(0, 0);
     const int end = a.causal ? hi_v / a.group + 1 : rows.n;
     const int begin = a.window > 0 ? max(0, lo_v / a.group - a.window + 1) : 0;
     return make_int2(begin / TK, (end + TK - 1) / TK);
   };
-  const int2 rA = uniform(range(0)), rB = uniform(range(1));
+  const int2 rA = uniform(range(0)), rB = NT == 2 ? uniform(range(1)) : make_int2(0, 0);
   // the keys that every row of tile h sees: [x, y); a key tile that is not inside them is cut by the mask
   auto common = [&](int h) {
-    const int lo_v = v0 + h * TQ, hi_v = min(lo_v + TQ, n_virt) - 1;
+    const int lo_v = v0 + h * a.rows, hi_v = min(lo_v + a.rows, n_virt) - 1;
     return make_int2(a.window > 0 ? hi_v / a.group - a.window + 1 : 0, a.causal ? lo_v / a.group + 1 : rows.n);
   };
   auto partial = [](int2 c, int j) { return (j + 1) * TK > c.y || j * TK < c.x; };
-  const bool two = rB.y > 0;
+  const bool two = NT == 2 && rB.y > 0;
   const int j0 = rA.x, j1 = two ? rB.y : rA.y, n_keys = uniform(rows.n);   // A's keys begin and end no later than B's
 
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -222,6 +228,11 @@ __global__ void __launch_bounds__(384, 1)
     if (lane == 0) {
       int g = 0;
       bool ok = true;
+      for (int h = 0; h < (two ? 2 : 1); ++h) {               // rows behind the sequence's end are other rows, unused
+        mbar_arrive_expect_tx(&q_full[h], HD / 64 * a.rows * 128);
+        for (int s = 0; s < HD / 64; ++s)
+          tma_load_3d(sQ + h * C::TILE_BYTES + s * 16384, &tmQ, &q_full[h], 64 * s, hk * a.group, rows.first + v0 / a.group + h * a.tq);
+      }
       for (int j = j0; ok && j < j1; ++j)
         for (int m = 0; m < 2; ++m, ++g) {
           const int sl = g % NS;
@@ -232,6 +243,7 @@ __global__ void __launch_bounds__(384, 1)
         }
       // every copy started here has landed before the CTA may exit
       volatile int never = 0;
+      for (int h = 0; h < (two ? 2 : 1); ++h) mbar_wait_bounded(&q_full[h], 0, &never, nullptr);
       for (int i = max(0, g - NS); i < g; ++i) mbar_wait_bounded(&full[i % NS], (i / NS) & 1, &never, nullptr);
     }
   } else if (warp == 1) {
@@ -309,25 +321,13 @@ __global__ void __launch_bounds__(384, 1)
     warp_wait_bounded(drain, 0, &never, nullptr);
   } else if (warp >= 4) {
     // --------------------------------------------------------------- softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");     // 56 + 224 + 224 = 3 * 168
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS));
     const int h = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
     const int2 r = h ? rB : rA;
-    const int v = v0 + h * TQ + row;
-    const bool v_ok = v < n_virt;
+    const int v = v0 + h * a.rows + row;
+    const bool v_ok = row < a.rows && v < n_virt;
     const int pos = v_ok ? v / a.group : 0, head = hk * a.group + (v_ok ? v - pos * a.group : 0);
-    {
-      const uint4* src = reinterpret_cast<const uint4*>(a.q + (rows.first + pos) * a.ldq + static_cast<int64_t>(head) * HD);
-#pragma unroll
-      for (int s = 0; s < HD / 64; ++s) {
-        uint8_t* dst = sQ + h * C::TILE_BYTES + s * 16384 + row * 128;
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          *reinterpret_cast<uint4*>(dst + ((c ^ (row & 7)) << 4)) = v_ok ? src[s * 8 + c] : make_uint4(0, 0, 0, 0);
-      }
-      fence_proxy_async_smem();
-      warp_arrive(&q_full[h]);
-    }
     const uint32_t t_s = tmem + lane_off + C::S_COL + h * TK, t_o = tmem + lane_off + C::O_COL + h * HD;
     const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2);
     const int see_hi = a.causal && v_ok ? pos + 1 : rows.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
@@ -426,12 +426,13 @@ __global__ void __launch_bounds__(384, 1)
       warp_arrive(&p_full[2 * h + 1]);
     }
     if (ok && r.y > 0 && warp_wait_bounded(&o_done[h], 0, abort_flag, nullptr)) {
-      // O leaves by rows: 64 dims of a thread's row through its own line of shared memory (Q's, which no MMA reads any
-      // more; 144 bytes apart, without bank conflicts), then one bulk copy
+      // O leaves through Q's shared memory, which no MMA reads any more.  A tile of whole rows of the sequence is one
+      // tensor store; in the sequence's last tile each row has a line of its own (144 bytes apart) and a copy of its own
       tc_fence_after();
       const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+      const bool full_tile = v0 + (h + 1) * a.rows <= n_virt;
       bf16* orow = a.o + (rows.first + pos) * a.ldo + static_cast<int64_t>(head) * HD;
-      uint8_t* line = sQ + h * C::TILE_BYTES + row * (HD == 128 ? 144 : 128);
+      uint8_t* tile = sQ + h * C::TILE_BYTES;
 #pragma unroll 1
       for (int c = 0; c < HD / 64; ++c) {
         uint32_t ro[32], rp[32];
@@ -439,7 +440,9 @@ __global__ void __launch_bounds__(384, 1)
         tmem_ld32_nowait(t_o + 64 * c + 32, rp);
         tmem_wait_ld(ro);
         tmem_bind(rp);
-        if (c > 0) bulk_wait_read0();
+        if (c > 0 && !full_tile) bulk_wait_read0();
+        uint8_t* line = full_tile ? tile + c * 16384 + row * 128 : tile + row * (HD == 128 ? 144 : 128);
+        const int swap = full_tile ? row & 7 : 0;
 #pragma unroll
         for (int k = 0; k < 64; k += 8) {
           uint32_t w[4];
@@ -450,11 +453,20 @@ __global__ void __launch_bounds__(384, 1)
             __nv_bfloat162 t = __floats2bfloat162_rn(x * inv, y * inv);
             w[e] = *reinterpret_cast<uint32_t*>(&t);
           }
-          *reinterpret_cast<uint4*>(line + 2 * k) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(line + (((k >> 3) ^ swap) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
         fence_proxy_async_smem();
-        if (v_ok) bulk_store(orow + 64 * c, line, 128);
-        bulk_commit();
+        if (!full_tile) {
+          if (v_ok) bulk_store(orow + 64 * c, line, 128);
+          bulk_commit();
+        }
+      }
+      if (full_tile) {
+        asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + h) : "memory");
+        if (row == 0) {
+          for (int s = 0; s < HD / 64; ++s) tma_store_3d(&tmO, tile + s * 16384, 64 * s, hk * a.group, rows.first + v0 / a.group + h * a.tq);
+          bulk_commit();
+        }
       }
       bulk_wait0();
     }
@@ -464,47 +476,51 @@ __global__ void __launch_bounds__(384, 1)
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, C::TMEM_COLS);
   }
 }
 
-// bf16 map {HD, kv heads, rows}, box {64, 1, 128}, 128-byte swizzle
-bool rows_map(CUtensorMap* m, const void* ptr, int hd, int n_kv, int total, int64_t ld) {
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(n_kv), static_cast<cuuint64_t>(total)};
+// bf16 map {HD, heads, rows}, box {64, box_heads, box_rows}, 128-byte swizzle
+bool rows_map(CUtensorMap* m, const void* ptr, int hd, int heads, int total, int64_t ld, int box_heads, int box_rows) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(total)};
   const cuuint64_t strides[2] = {static_cast<cuuint64_t>(hd) * 2, static_cast<cuuint64_t>(ld) * 2};
-  const cuuint32_t box[3] = {64, 1, TK}, estr[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_rows)}, estr[3] = {1, 1, 1};
   return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int HD>
+template <int HD, int NT>
 const char* launch(const RaggedCall& c, cudaStream_t s) {
-  using C = PackedCfg<HD>;
+  using C = PackedCfg<HD, NT>;
   if (!tensor_map_encoder()) return "cuTensorMapEncodeTiled is unavailable";
   int dev = 0;
   current_sms(&dev);
   static PerDevice ready;
   if (ready.get(dev, [] {
-        return cudaFuncSetAttribute(attn_packed_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess ? 1 : 0;
+        return cudaFuncSetAttribute(attn_packed_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) == cudaSuccess ? 1 : 0;
       }) <= 0)
     return "attention smem attribute failed";
-  CUtensorMap mk, mv;
-  if (!rows_map(&mk, c.k, HD, c.n_kv, c.total, c.ldk) || !rows_map(&mv, c.v, HD, c.n_kv, c.total, c.ldv))
+  const int group = c.n_heads / c.n_kv, tq = TQ / group;
+  CUtensorMap mq, mk, mv, mo;
+  if (!rows_map(&mq, c.q, HD, c.n_heads, c.total, c.ldq, group, tq) || !rows_map(&mo, c.o, HD, c.n_heads, c.total, c.ldo, group, tq) ||
+      !rows_map(&mk, c.k, HD, c.n_kv, c.total, c.ldk, 1, TK) || !rows_map(&mv, c.v, HD, c.n_kv, c.total, c.ldv, 1, TK))
     return "attention tensor map encode failed";
-  const int group = c.n_heads / c.n_kv;
-  const PackedArgs a{static_cast<const bf16*>(c.q), static_cast<bf16*>(c.o), c.cu, c.batch, c.total, c.max_rows, group, c.n_kv,
-                     c.ldq, c.ldo, c.causal, c.window, 1.4426950408889634f / sqrtf(static_cast<float>(HD))};
-  // at most one pair of tiles per 256 virtual rows and one more per sequence
-  const int64_t blocks = (static_cast<int64_t>(c.total) * group / (2 * TQ) + c.batch) * c.n_kv;
-  const cudaError_t e = launch_pdl(attn_packed_kernel<HD>, dim3(static_cast<unsigned>(blocks)), C::THREADS, C::SMEM, s, mk, mv, a);
+  const PackedArgs a{static_cast<bf16*>(c.o), c.cu, c.batch, c.total, c.max_rows, group, c.n_kv, tq, tq * group,
+                     c.ldo, c.causal, c.window, 1.4426950408889634f / sqrtf(static_cast<float>(HD))};
+  // at most one CTA per NT tiles of rows and one more per sequence
+  const int64_t blocks = (static_cast<int64_t>(c.total) / (NT * tq) + c.batch) * c.n_kv;
+  const cudaError_t e = launch_pdl(attn_packed_kernel<HD, NT>, dim3(static_cast<unsigned>(blocks)), C::THREADS, C::SMEM, s, mq, mk, mv, mo, a);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 
 }  // namespace
 
 const char* attention_packed(const RaggedCall& c, cudaStream_t s) {
-  return c.head_dim == 128 ? launch<128>(c, s) : launch<64>(c, s);
+  // Two tiles share K and V in one CTA per SM for heads of 128 (one 8192-token prompt, 32 / 16 heads: 383 us, with one
+  // tile and two CTAs per SM 431; 24 prompts of 512: 128 and 138).  Heads of 64 leave shared memory and tensor memory for
+  // two CTAs with longer rings, whose starts and ends overlap (12 prompts of 1024, 12 heads: 62 us, 68 with two tiles).
+  return c.head_dim == 128 ? launch<128, 2>(c, s) : launch<64, 1>(c, s);
 }
 
 }  // namespace tadm

@@ -76,6 +76,10 @@ tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, v
   if (!rows_ok(q, ldq, wq, dtype) || !rows_ok(k, ldk, wk, dtype) || !rows_ok(v, ldv, wk, dtype) ||
       !rows_ok(o, ldo, wq, dtype))
     return TADM_ERR_INVALID_ARG;
+  // a tile of the tensor-core kernel holds whole rows, all query heads of a KV head; its grid is one-dimensional
+  if (dtype && (n_heads / n_kv_heads > 128 ||
+                (static_cast<int64_t>(total_rows) / (128 / (n_heads / n_kv_heads)) + batch) * n_kv_heads > INT32_MAX))
+    return TADM_ERR_UNSUPPORTED;
   RaggedCall c{};
   c.q = q, c.k = k, c.v = v, c.o = o;
   c.cu = cu_rows, c.batch = batch, c.total = total_rows, c.max_rows = max_rows < total_rows ? max_rows : total_rows;

@@ -33,19 +33,57 @@ __device__ __forceinline__ uint32_t enc8(float x) {
   const uint32_t q = __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
   return fabsf(x) <= 3.402823466e38f ? q : 0x7fu;     // infinities too become NaN
 }
-__device__ __forceinline__ float dec8(uint32_t b) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(b), __NV_E4M3)));
+// four finite values at a time, the first in the low byte
+__device__ __forceinline__ uint32_t enc8x4(const float* x, float s) {
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[0] * s, x[1] * s), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[2] * s, x[3] * s), __NV_SATFINITE, __NV_E4M3);
+  return lo | hi << 16;
+}
+__device__ __forceinline__ void dec8x4(uint32_t w, float s, float* x) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> (16 * h)), __NV_E4M3)));
+    x[2 * h] = f.x * s, x[2 * h + 1] = f.y * s;
+  }
+}
+// four words of four bytes, transposed
+__device__ __forceinline__ void transpose4(uint32_t& a, uint32_t& b, uint32_t& c, uint32_t& d) {
+  const uint32_t p = __byte_perm(a, b, 0x5140), q = __byte_perm(c, d, 0x5140);
+  const uint32_t r = __byte_perm(a, b, 0x7362), s = __byte_perm(c, d, 0x7362);
+  a = __byte_perm(p, q, 0x5410), b = __byte_perm(p, q, 0x7632);
+  c = __byte_perm(r, s, 0x5410), d = __byte_perm(r, s, 0x7632);
 }
 
-// 8 consecutive elements as floats
-template <class T> __device__ __forceinline__ void load8(const T* p, float (&x)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float (&x)[8]) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+// 8 consecutive elements as they are in memory, and as floats
+template <class T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
+template <class T> __device__ __forceinline__ Raw8<T> load8(const T* p) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) r.v[i] = reinterpret_cast<const uint4*>(p)[i];
+  return r;
 }
-template <> __device__ __forceinline__ void load8<bf16>(const bf16* p, float (&x)[8]) {
-  const uint4 a = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// the largest magnitude as fp32 bits, infinities and NaN (0x7f800000 and above) included
+__device__ __forceinline__ uint32_t top8(const Raw8<float>& r) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    m = max(max(max(m, r.v[i].x & 0x7fffffffu), r.v[i].y & 0x7fffffffu), max(r.v[i].z & 0x7fffffffu, r.v[i].w & 0x7fffffffu));
+  return m;
+}
+__device__ __forceinline__ uint32_t top8(const Raw8<bf16>& r) {
+  const uint32_t m = __vmaxu2(__vmaxu2(r.v[0].x & 0x7fff7fffu, r.v[0].y & 0x7fff7fffu),
+                              __vmaxu2(r.v[0].z & 0x7fff7fffu, r.v[0].w & 0x7fff7fffu));
+  return max(m & 0xffff0000u, m << 16);
+}
+__device__ __forceinline__ void widen8(const Raw8<float>& r, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    x[4 * i] = __uint_as_float(r.v[i].x), x[4 * i + 1] = __uint_as_float(r.v[i].y);
+    x[4 * i + 2] = __uint_as_float(r.v[i].z), x[4 * i + 3] = __uint_as_float(r.v[i].w);
+  }
+}
+__device__ __forceinline__ void widen8(const Raw8<bf16>& r, float (&x)[8]) {
+  const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(w[i] << 16);
@@ -73,176 +111,226 @@ struct RowsArgs {
   void *k, *v;                 // rows (read by the write, written by the read)
   const int32_t *cu, *start, *table;
   int64_t ldk, ldv;
-  int batch, total, max_rows, ld_table, pages, n_kv, touched;
+  int total, max_rows, ld_table, pages, n_kv;
 };
 
-// What block (x, y) works on: sequence b, the page that holds its i-th touched
-// 64-token range, slots lo .. hi - 1 of it, which are rows row0 .. of the operand.
+// What block (i, y, b) works on: the i-th 64-token range that sequence b
+// touches, slots lo .. hi - 1 of it, which are rows row0 + lo .. of the operand,
+// and the place of its page in the table (at most 2^20 wide: tokens fit 27 bits).
 struct Part {
-  int page, lo, hi;
-  int64_t row0;
+  int64_t entry;
+  int row0, lo, hi;
 };
-__device__ __forceinline__ bool find_part(const RowsArgs& a, int x, Part* p) {
-  const int b = x / a.touched, i = x - b * a.touched;
+__device__ __forceinline__ bool find_part(const RowsArgs& a, Part* p) {
+  const int b = blockIdx.z, s = a.start[b];
   const int c0 = min(max(a.cu[b], 0), a.total), c1 = min(max(a.cu[b + 1], c0), a.total);
-  const int n = min(c1 - c0, a.max_rows), s = a.start[b];
-  if (n <= 0 || s < 0) return false;
-  const int64_t slot = static_cast<int64_t>(s / PT) + i, first = slot * PT;
-  const int64_t end = static_cast<int64_t>(s) + n;
-  if (first >= end || slot >= a.ld_table) return false;
-  p->page = a.table[static_cast<int64_t>(b) * a.ld_table + slot];
-  if (p->page < 0 || p->page >= a.pages) return false;
-  p->lo = static_cast<int>(max(static_cast<int64_t>(s), first) - first);
-  p->hi = static_cast<int>(min(end, first + PT) - first);
-  p->row0 = c0 + first + p->lo - s;
+  const int n = min(min(c1 - c0, a.max_rows), 1 << 27);
+  const int slot = s / PT + static_cast<int>(blockIdx.x);
+  if (n <= 0 || s < 0 || slot >= a.ld_table) return false;
+  const int first = slot * PT;
+  if (first >= s + n) return false;
+  p->entry = static_cast<int64_t>(b) * a.ld_table + slot;
+  p->lo = max(s, first) - first;
+  p->hi = min(s + n - first, PT);
+  p->row0 = c0 + first - s;
   return true;
 }
 
-// One block per (page, head, K or V): HD / 8 threads take a row, the rows stay
-// in registers between the maximum and the conversion, so they are read once.
-// V goes through shared memory to be transposed.
+// V's tile in shared memory: 16 words of four slots per dim, the words of dim d
+// in the order w ^ (d / 8), which spreads the 8-dim groups of a warp over the banks.
+__device__ __forceinline__ int tile_word(int dim, int w) { return dim * 16 + (w ^ ((dim >> 3) & 15)); }
+
+// One block per (page, head, K or V), 16 groups of HD / 8 threads: a thread
+// takes 8 dims of four slots, which stay in registers between the maximum and
+// the conversion, so the rows are read once.  V is transposed four slots (a
+// word) at a time through shared memory.
+// 6212 rows of 8 x 128: XXX us; what bounds it is the chain of dependent reads
+// (lengths, table, rows) per block and the launch.
 template <class T, int HD>
-__global__ void __launch_bounds__(256) page_write_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(2 * HD, sizeof(T) == 2 ? 1024 / HD : 512 / HD) page_write_kernel(const RowsArgs a) {
   pdl_enter();
-  constexpr int TPR = HD / 8, RPP = 256 / TPR, NP = PT / RPP;   // threads per row, rows per pass, passes
-  constexpr int LDT = PT + 4;                                   // bytes per dim of the transposed tile
-  __shared__ __align__(16) uint8_t tile[HD * LDT];
-  __shared__ float red[8];
+  constexpr int TPR = HD / 8, NT = 2 * HD;
+  __shared__ uint32_t tile[HD * 16];
+  __shared__ uint32_t red[NT / 32];
   Part p;
-  if (!find_part(a, blockIdx.x, &p)) return;
+  if (!find_part(a, &p)) return;
+  const int page = a.table[p.entry];
   const int head = blockIdx.y >> 1, is_v = blockIdx.y & 1;
-  const int tid = threadIdx.x, r = tid / TPR, d = (tid % TPR) * 8, n = p.hi - p.lo;
+  const int tid = threadIdx.x, w = tid / TPR, d = (tid % TPR) * 8;
   const int64_t ld = is_v ? a.ldv : a.ldk;
   const T* src = static_cast<const T*>(is_v ? a.v : a.k) + p.row0 * ld + static_cast<int64_t>(head) * HD + d;
-  float x[NP][8], amax = 0.0f;
+  Raw8<T> raw[4];
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int row = i * RPP + r;
-    if (row < n) {
-      load8<T>(src + row * ld, x[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
-    }
+  for (int i = 0; i < 4; ++i) {
+    const int slot = 4 * w + i;
+    if (slot >= p.lo && slot < p.hi) raw[i] = load8<T>(src + slot * ld);
+    else raw[i] = Raw8<T>{};
   }
-#pragma unroll
-  for (int i = 0; i < NP; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float m = fabsf(x[i][e]);
-      amax = m <= 3.402823466e38f ? fmaxf(amax, m) : amax;
-    }
-  amax = warp_max(amax);
-  if ((tid & 31) == 0) red[tid >> 5] = amax;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 8; ++w) amax = fmaxf(amax, red[w]);
-  const int64_t ph = static_cast<int64_t>(p.page) * a.n_kv + head;
+  if (page < 0 || page >= a.pages) return;                    // uniform: not followed
+  const int64_t ph = static_cast<int64_t>(page) * a.n_kv + head;
   float* sp = (is_v ? a.sv : a.sk) + ph;
   uint8_t* data = (is_v ? a.pv : a.pk) + ph * (PT * HD);
-  float scale = needed_scale(amax), again = 1.0f;
-  if (p.lo > 0) {
-    const float had = *sp;
-    if (scale > had) again = had / scale;
-    else scale = had;
+  const float had = p.lo > 0 ? *sp : 0.0f;
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = max(top, top8(raw[i]));
+  top = __reduce_max_sync(0xffffffffu, top);
+  if ((tid & 31) == 0) red[tid >> 5] = top;
+  __syncthreads();                                            // also: every thread has read the old scale
+#pragma unroll
+  for (int k = 0; k < NT / 32; ++k) top = max(top, red[k]);
+  const bool odd = top >= 0x7f800000u;                        // an infinity or NaN among the rows: the largest finite value
+  if (odd) {
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[8];
+      widen8(raw[i], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t m = __float_as_uint(x[e]) & 0x7fffffffu;
+        if (m < 0x7f800000u) top = max(top, m);
+      }
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    __syncthreads();
+    if ((tid & 31) == 0) red[tid >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NT / 32; ++k) top = max(top, red[k]);
   }
+  const float amax = __uint_as_float(top);
+  const float scale = fmaxf(needed_scale(amax), had);
+  const float again = had > 0.0f ? had / scale : 1.0f;        // what becomes of the tokens that stay
+  if (tid == 0 && scale != had) *sp = scale;
   const float inv = 1.0f / scale;
-  __syncthreads();                       // every thread has read the old scale
-  if (tid == 0 && (p.lo == 0 || again != 1.0f)) *sp = scale;
-  if (again != 1.0f) {                   // tokens that stay, in the new scale
-    if (is_v) {
-      for (int e = tid; e < HD * p.lo; e += 256) {
-        uint8_t* q = data + (e / p.lo) * PT + e % p.lo;
-        *q = static_cast<uint8_t>(enc8(dec8(*q) * again));
+  const bool fresh = p.lo == 0;                               // slots past the rows become zeros
+  uint32_t q[4][2];                                           // a slot's 8 dims
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[8];
+    widen8(raw[i], x);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      q[i][h] = enc8x4(x + 4 * h, inv);
+      if (odd) {
+        q[i][h] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[i][h] |= enc8(x[4 * h + e] * inv) << (8 * e);
       }
-    } else {
-      for (int e = tid; e < HD * p.lo; e += 256) data[e] = static_cast<uint8_t>(enc8(dec8(data[e]) * again));
     }
   }
-  const bool fresh = p.lo == 0;          // slots past the rows become zeros
+  auto encode_again = [&](uint32_t word) {                    // four values in the new scale (a NaN stays one)
+    float x[4];
+    dec8x4(word, again, x);
+    return enc8x4(x, 1.0f);
+  };
+  if (!is_v) {
 #pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int row = i * RPP + r;
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e >> 2] |= enc8(x[i][e] * inv) << (8 * (e & 3));
-    if (is_v) {
-      if (fresh || row < n) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile[(d + e) * LDT + row] = static_cast<uint8_t>(w[e >> 2] >> (8 * (e & 3)));
+    for (int i = 0; i < 4; ++i) {
+      const int slot = 4 * w + i;
+      uint2* at = reinterpret_cast<uint2*>(data + slot * HD + d);
+      if (fresh || (slot >= p.lo && slot < p.hi)) {
+        *at = make_uint2(q[i][0], q[i][1]);
+      } else if (slot < p.lo && again != 1.0f) {
+        const uint2 old = *at;
+        *at = make_uint2(encode_again(old.x), encode_again(old.y));
       }
-    } else if (row < n || (fresh && row < PT)) {
-      *reinterpret_cast<uint2*>(data + (p.lo + row) * HD + d) = make_uint2(w[0], w[1]);
     }
+    return;
   }
-  if (!is_v) return;
-  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) transpose4(q[0][h], q[1][h], q[2][h], q[3][h]);   // now four slots of dim d + 4 h + e in q[e][h]
   if (fresh) {
-    for (int c = tid; c < HD * (PT / 16); c += 256) {
-      const int dim = c >> 2, at = (c & 3) * 16;
-      const uint32_t* t = reinterpret_cast<const uint32_t*>(tile + dim * LDT + at);
-      *reinterpret_cast<uint4*>(data + dim * PT + at) = make_uint4(t[0], t[1], t[2], t[3]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) tile[tile_word(d + 4 * h + e, w)] = q[e][h];
+    __syncthreads();
+    for (int c = tid; c < HD * 4; c += NT) {
+      const int dim = c >> 2, at = (c & 3) * 4;
+      *reinterpret_cast<uint4*>(data + dim * PT + 4 * at) = make_uint4(tile[tile_word(dim, at)], tile[tile_word(dim, at + 1)],
+                                                                       tile[tile_word(dim, at + 2)], tile[tile_word(dim, at + 3)]);
     }
-  } else {
-    for (int e = tid; e < HD * n; e += 256) data[(e / n) * PT + p.lo + e % n] = tile[(e / n) * LDT + e % n];
+  } else if (4 * w < p.hi && (4 * w + 4 > p.lo || again != 1.0f)) {
+    // words of a page that keeps tokens: read, merged, written
+    uint32_t mine = 0, before = 0;                            // bytes of the new rows, of the tokens that stay
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (4 * w + i < p.lo) before |= 0xffu << (8 * i);
+      else if (4 * w + i < p.hi) mine |= 0xffu << (8 * i);
+    }
+    uint32_t old[4][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) old[e][h] = *reinterpret_cast<const uint32_t*>(data + (d + 4 * h + e) * PT + 4 * w);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t o = old[e][h];
+        if (again != 1.0f) o = (o & ~before) | (encode_again(o) & before);
+        *reinterpret_cast<uint32_t*>(data + (d + 4 * h + e) * PT + 4 * w) = (o & ~mine) | (q[e][h] & mine);
+      }
   }
 }
 
+// The same blocks and threads; rows of a page that the table does not hold read as zeros.
 template <class T, int HD>
-__global__ void __launch_bounds__(256) page_read_kernel(const RowsArgs a) {
+__global__ void __launch_bounds__(2 * HD) page_read_kernel(const RowsArgs a) {
   pdl_enter();
-  constexpr int TPR = HD / 8, RPP = 256 / TPR;
-  constexpr int LDT = PT + 4;
-  __shared__ __align__(16) uint8_t tile[HD * LDT];
+  constexpr int TPR = HD / 8, NT = 2 * HD;
+  __shared__ uint32_t tile[HD * 16];
   Part p;
-  if (!find_part(a, blockIdx.x, &p)) {
-    // rows of a page that the table does not hold read as zeros
-    const int b = blockIdx.x / a.touched, i = blockIdx.x - b * a.touched;
-    const int c0 = min(max(a.cu[b], 0), a.total), c1 = min(max(a.cu[b + 1], c0), a.total);
-    const int64_t n = min(c1 - c0, a.max_rows), s = a.start[b];
-    if (n <= 0 || s < 0) return;
-    const int64_t first = (s / PT + i) * PT;
-    const int64_t lo = max(first, s), hi = min(first + PT, s + n);
-    const int head = blockIdx.y >> 1, is_v = blockIdx.y & 1;
-    T* dst = static_cast<T*>(is_v ? a.v : a.k) + static_cast<int64_t>(head) * HD;
-    const int64_t ld = is_v ? a.ldv : a.ldk;
-    for (int64_t e = threadIdx.x; e < (hi - lo) * HD; e += 256) dst[(c0 + lo - s + e / HD) * ld + e % HD] = from_f32<T>(0.0f);
-    return;
-  }
+  if (!find_part(a, &p)) return;
+  const int page = a.table[p.entry];
+  const bool ok = page >= 0 && page < a.pages;
   const int head = blockIdx.y >> 1, is_v = blockIdx.y & 1;
-  const int tid = threadIdx.x, r = tid / TPR, d = (tid % TPR) * 8, n = p.hi - p.lo;
-  const int64_t ph = static_cast<int64_t>(p.page) * a.n_kv + head;
-  const float scale = (is_v ? a.sv : a.sk)[ph];
+  const int tid = threadIdx.x, w = tid / TPR, d = (tid % TPR) * 8;
+  const int64_t ph = static_cast<int64_t>(ok ? page : 0) * a.n_kv + head;
+  const float scale = ok ? (is_v ? a.sv : a.sk)[ph] : 0.0f;
   const uint8_t* data = (is_v ? a.pv : a.pk) + ph * (PT * HD);
   const int64_t ld = is_v ? a.ldv : a.ldk;
   T* dst = static_cast<T*>(is_v ? a.v : a.k) + p.row0 * ld + static_cast<int64_t>(head) * HD + d;
+  uint32_t q[4][2];                                           // a slot's 8 dims
   if (is_v) {
-    for (int c = tid; c < HD * (PT / 16); c += 256) {
-      const int dim = c >> 2, at = (c & 3) * 16;
-      const uint4 t = *reinterpret_cast<const uint4*>(data + dim * PT + at);
-      uint32_t* o = reinterpret_cast<uint32_t*>(tile + dim * LDT + at);
-      o[0] = t.x, o[1] = t.y, o[2] = t.z, o[3] = t.w;
+    for (int c = tid; c < HD * 4; c += NT) {
+      const int dim = c >> 2, at = (c & 3) * 4;
+      const uint4 t = ok ? *reinterpret_cast<const uint4*>(data + dim * PT + 4 * at) : make_uint4(0, 0, 0, 0);
+      tile[tile_word(dim, at)] = t.x, tile[tile_word(dim, at + 1)] = t.y;
+      tile[tile_word(dim, at + 2)] = t.z, tile[tile_word(dim, at + 3)] = t.w;
     }
     __syncthreads();
-  }
-  for (int row = r; row < n; row += RPP) {
-    float x[8];
-    if (is_v) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = dec8(tile[(d + e) * LDT + p.lo + row]) * scale;
-    } else {
-      const uint2 t = *reinterpret_cast<const uint2*>(data + (p.lo + row) * HD + d);
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = dec8(((e < 4 ? t.x : t.y) >> (8 * (e & 3))) & 0xff) * scale;
+      for (int e = 0; e < 4; ++e) q[e][h] = tile[tile_word(d + 4 * h + e, w)];
+      transpose4(q[0][h], q[1][h], q[2][h], q[3][h]);
     }
-    store8<T>(dst + row * ld, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int slot = 4 * w + i;
+      const uint2 t = ok && slot >= p.lo && slot < p.hi ? *reinterpret_cast<const uint2*>(data + slot * HD + d) : make_uint2(0, 0);
+      q[i][0] = t.x, q[i][1] = t.y;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int slot = 4 * w + i;
+    if (slot < p.lo || slot >= p.hi) continue;
+    float x[8];
+    dec8x4(q[i][0], scale, x);
+    dec8x4(q[i][1], scale, x + 4);
+    store8<T>(dst + slot * ld, x);
   }
 }
 
 template <class T, int HD>
-cudaError_t launch_rows(const RowsArgs& a, bool write, cudaStream_t s) {
-  const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.batch) * a.touched), 2 * a.n_kv);
-  return write ? launch_pdl(page_write_kernel<T, HD>, grid, 256, 0, s, a) : launch_pdl(page_read_kernel<T, HD>, grid, 256, 0, s, a);
+cudaError_t launch_rows(const RowsArgs& a, int batch, bool write, cudaStream_t s) {
+  const dim3 grid((a.max_rows + PT - 2) / PT + 1, 2 * a.n_kv, batch);
+  return write ? launch_pdl(page_write_kernel<T, HD>, grid, 2 * HD, 0, s, a) : launch_pdl(page_read_kernel<T, HD>, grid, 2 * HD, 0, s, a);
 }
 
 // ------------------------------------------------------------- bookkeeping
@@ -540,8 +628,8 @@ __device__ void copy_pages(const CopyArgs& c, int block, int blocks) {
       dst[u] = nullptr;
       const int64_t id = base + u;
       if (id >= total) continue;
-      const int i = static_cast<int>(id / per);
-      const int in = static_cast<int>(id - i * per), unit = in / c.page_chunks, chunk = in - unit * c.page_chunks;
+      const int in = static_cast<int>(id / n), i = static_cast<int>(id - static_cast<int64_t>(in) * n);
+      const int unit = in / c.page_chunks, chunk = in - unit * c.page_chunks;
       const int from = c.from[i], to = c.to[i];
       if (!pair_ok(c, from, to)) continue;
       uint4* base_p = (unit & 1) ? c.v : c.k;
@@ -656,10 +744,10 @@ const char* page_rows(const PageRowsCall& c, bool write, cudaStream_t s) {
   RowsArgs a{static_cast<uint8_t*>(p.k) + c.layer * page * PT * p.head_dim,
              static_cast<uint8_t*>(p.v) + c.layer * page * PT * p.head_dim,
              p.k_scale + c.layer * page, p.v_scale + c.layer * page, c.k, c.v, c.cu, c.start, c.table, c.ldk, c.ldv,
-             c.batch, c.total, c.max_rows, c.ld_table, p.pages, p.n_kv_heads, (c.max_rows + PT - 2) / PT + 1};
+             c.total, c.max_rows, c.ld_table, p.pages, p.n_kv_heads};
   cudaError_t e;
-  if (p.head_dim == 128) e = c.bf16 ? launch_rows<bf16, 128>(a, write, s) : launch_rows<float, 128>(a, write, s);
-  else e = c.bf16 ? launch_rows<bf16, 64>(a, write, s) : launch_rows<float, 64>(a, write, s);
+  if (p.head_dim == 128) e = c.bf16 ? launch_rows<bf16, 128>(a, c.batch, write, s) : launch_rows<float, 128>(a, c.batch, write, s);
+  else e = c.bf16 ? launch_rows<bf16, 64>(a, c.batch, write, s) : launch_rows<float, 64>(a, c.batch, write, s);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 

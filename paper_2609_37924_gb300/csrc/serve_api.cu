@@ -40,8 +40,7 @@ tadm_status page_rows_call(const tadm_page_pool* pool, int layer, const void* k,
   const int64_t width = static_cast<int64_t>(pool->n_kv_heads) * pool->head_dim;
   if (!rows_ok(k, ldk, width, dtype) || !rows_ok(v, ldv, width, dtype)) return TADM_ERR_INVALID_ARG;
   const int rows = max_rows < total ? max_rows : total;      // no sequence has more
-  if (static_cast<int64_t>(batch) * ((rows + TADM_PAGE_TOKENS - 2) / TADM_PAGE_TOKENS + 1) > INT32_MAX)
-    return TADM_ERR_UNSUPPORTED;
+  if (batch > 65535) return TADM_ERR_UNSUPPORTED;            // a grid dimension
   const PageRowsCall c{pool, layer, const_cast<void*>(k), const_cast<void*>(v), cu, start, table, batch, total, rows,
                        ld_table, ldk, ldv, dtype};
   return page_rows(c, write, s) ? TADM_ERR_CUDA : TADM_OK;

@@ -200,10 +200,21 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream=None) -> Optional[int]:
-    import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    """The handle of `stream`, or of the current stream of the current device (0.2 us; a torch.cuda.Stream object for it
+    costs 3 us per call)."""
+    global _raw_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None:
+        import torch
+        torch.cuda.init()
+        get, dev = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        _raw_stream = lambda: get(dev())  # noqa: E731
+    return _raw_stream()
 
 
 def tadm_gemm(A, B, C, dtype: int, stream=None):
@@ -337,29 +348,32 @@ class PagePool:
                    z((layers, pages, n_kv_heads), torch.float32), z((layers, pages, n_kv_heads), torch.float32))
 
 
-_DTYPES = None
+_DTYPES = {}
+
+
+def _torch_types():
+    import torch
+    _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.int32: "int32"})
+    return _DTYPES
 
 
 def _rows_of(*tensors):
-    """The dtype code of row operands [rows, heads, hd]: fp32 or bf16, each row's heads dense, on one device."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
-    first = tensors[0]
-    dtype = _DTYPES.get(first.dtype)
-    if dtype is None:
-        raise TadmError(1, f"rows must be fp32 or bf16, not {first.dtype}")
+    """The dtype code of row operands [rows, heads, hd]: fp32 or bf16, each row's heads dense, on the GPU."""
+    kind = tensors[0].dtype
+    dtype = (_DTYPES or _torch_types()).get(kind)
+    if dtype not in (0, 1):
+        raise TadmError(1, f"rows must be fp32 or bf16, not {kind}")
     for t in tensors:
         s = t.stride()
-        if t.dim() != 3 or s[2] != 1 or s[1] != t.shape[2] or t.dtype != first.dtype or not t.is_cuda:
+        if len(s) != 3 or s[2] != 1 or s[1] != t.shape[2] or t.dtype is not kind or not t.is_cuda:
             raise TadmError(1, "rows must be CUDA tensors [rows, heads, head_dim] of one type with dense heads")
     return dtype
 
 
 def _ints_of(*tensors):
+    types = _DTYPES or _torch_types()
     for t in tensors:
-        if str(t.dtype) != "torch.int32" or not t.is_contiguous() or not t.is_cuda:
+        if types.get(t.dtype) != "int32" or not t.is_contiguous() or not t.is_cuda:
             raise TadmError(1, "lengths, tables and lists must be contiguous int32 CUDA tensors")
 
 
@@ -369,36 +383,43 @@ def tadm_attention_packed(q, k, v, o, cu_rows, max_rows: int, causal: bool = Tru
     cu_rows int32 [batch + 1]."""
     dtype = _rows_of(q, k, v, o)
     _ints_of(cu_rows)
-    rows, heads, hd = q.shape
-    if o.shape != q.shape or k.shape != v.shape or k.shape[0] != rows or k.shape[2] != hd:
+    shape, kv = q.shape, k.shape
+    rows, heads, hd = shape
+    if o.shape != shape or kv != v.shape or kv[0] != rows or kv[2] != hd:
         raise TadmError(1, "shapes of q, k, v and o do not agree")
-    _check(load_library().tadm_attention_packed(
+    status = load_library().tadm_attention_packed(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), cu_rows.data_ptr(), cu_rows.shape[0] - 1, rows,
-        max_rows, heads, k.shape[1], hd, q.stride(0), k.stride(0), v.stride(0), o.stride(0), int(causal), window,
-        dtype, _stream(stream)))
+        max_rows, heads, kv[1], hd, q.stride(0), k.stride(0), v.stride(0), o.stride(0), 1 if causal else 0, window,
+        dtype, _stream(stream))
+    if status:
+        _check(status)
 
 
-def _page_rows(name, pool, layer, k, v, cu_rows, start, table, max_rows, stream):
+def _page_rows(call, pool, layer, k, v, cu_rows, start, table, max_rows, stream):
     dtype = _rows_of(k, v)
     _ints_of(cu_rows, start, table)
-    if k.shape != v.shape or k.shape[1:] != (pool.n_kv_heads, pool.head_dim):
+    shape = k.shape
+    rows, heads, hd = shape
+    if shape != v.shape or heads != pool.n_kv_heads or hd != pool.head_dim:
         raise TadmError(1, "rows do not have the pool's heads")
     batch = cu_rows.shape[0] - 1
-    if start.shape[0] != batch or table.shape[0] < batch:
+    seqs, width = table.shape
+    if start.shape[0] != batch or seqs < batch:
         raise TadmError(1, "start and table need an entry per sequence")
-    _check(getattr(load_library(), name)(
-        pool.ref, layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, k.shape[0], max_rows,
-        k.stride(0), v.stride(0), table.data_ptr(), table.shape[1], dtype, _stream(stream)))
+    status = call(pool.ref, layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, rows, max_rows,
+                  k.stride(0), v.stride(0), table.data_ptr(), width, dtype, _stream(stream))
+    if status:
+        _check(status)
 
 
 def tadm_page_write(pool, layer: int, k, v, cu_rows, start, table, max_rows: int, stream=None):
     """Rows k, v [rows, kv heads, hd] become tokens start[b] .. of the cache (e4m3, a power-of-two scale per page and head)."""
-    _page_rows("tadm_page_write", pool, layer, k, v, cu_rows, start, table, max_rows, stream)
+    _page_rows(load_library().tadm_page_write, pool, layer, k, v, cu_rows, start, table, max_rows, stream)
 
 
 def tadm_page_read(pool, layer: int, k, v, cu_rows, start, table, max_rows: int, stream=None):
     """Tokens start[b] .. of the cache into the rows k, v [rows, kv heads, hd]."""
-    _page_rows("tadm_page_read", pool, layer, k, v, cu_rows, start, table, max_rows, stream)
+    _page_rows(load_library().tadm_page_read, pool, layer, k, v, cu_rows, start, table, max_rows, stream)
 
 
 def tadm_page_attention_scratch_size(batch: int, total_rows: int, max_rows: int, max_len: int, n_heads: int,
@@ -415,14 +436,18 @@ def tadm_page_attention(q, pool, layer: int, o, cu_rows, lens, table, max_rows: 
     sees its first lens[b] tokens, its rows are the last ones of them."""
     dtype = _rows_of(q, o)
     _ints_of(cu_rows, lens, table)
-    rows, heads, hd = q.shape
+    shape = q.shape
+    rows, heads, hd = shape
     batch = cu_rows.shape[0] - 1
-    if o.shape != q.shape or hd != pool.head_dim or lens.shape[0] != batch or table.shape[0] < batch:
+    seqs, width = table.shape
+    if o.shape != shape or hd != pool.head_dim or lens.shape[0] != batch or seqs < batch:
         raise TadmError(1, "shapes of q, o, lens, table and the pool do not agree")
-    _check(load_library().tadm_page_attention(
+    status = load_library().tadm_page_attention(
         q.data_ptr(), pool.ref, layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
-        max_len, heads, q.stride(0), o.stride(0), table.data_ptr(), table.shape[1], int(causal), window, dtype,
-        _ptr(scratch), 0 if scratch is None else scratch.numel() * scratch.element_size(), _stream(stream)))
+        max_len, heads, q.stride(0), o.stride(0), table.data_ptr(), width, 1 if causal else 0, window, dtype,
+        _ptr(scratch), 0 if scratch is None else scratch.nbytes, _stream(stream))
+    if status:
+        _check(status)
 
 
 def tadm_pages_scratch_size(pages: int, n_seqs: int) -> int:
@@ -444,7 +469,7 @@ def tadm_pages_reserve(tables, refs, seqs, new_len, tables_out, refs_out, status
     _check(load_library().tadm_pages_reserve(
         tables.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1], seqs.data_ptr(),
         new_len.data_ptr(), seqs.shape[0], tables_out.data_ptr(), refs_out.data_ptr(), status.data_ptr(),
-        scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+        scratch.data_ptr(), scratch.nbytes, _stream(stream)))
 
 
 def tadm_pages_fork(pool, tables, lens, refs, src, dst, tables_out, lens_out, refs_out, status, scratch, stream=None):
@@ -455,7 +480,7 @@ def tadm_pages_fork(pool, tables, lens, refs, src, dst, tables_out, lens_out, re
     _check(load_library().tadm_pages_fork(
         pool.ref, tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1],
         src.data_ptr(), dst.data_ptr(), src.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
-        status.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+        status.data_ptr(), scratch.data_ptr(), scratch.nbytes, _stream(stream)))
 
 
 def tadm_pages_free(tables, lens, refs, seqs, tables_out, lens_out, refs_out, status, scratch, stream=None):
@@ -464,7 +489,7 @@ def tadm_pages_free(tables, lens, refs, seqs, tables_out, lens_out, refs_out, st
     _check(load_library().tadm_pages_free(
         tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1],
         seqs.data_ptr(), seqs.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
-        status.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)))
+        status.data_ptr(), scratch.data_ptr(), scratch.nbytes, _stream(stream)))
 
 
 def tadm_pages_compact(pool, tables, refs, tables_out, refs_out, n_live, scratch, stream=None):

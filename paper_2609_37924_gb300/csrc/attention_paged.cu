@@ -99,13 +99,10 @@ __device__ __forceinline__ int64_t seq_units(const PagedArgs& a, int b) {
   for (int rt = 0; rt < s.n_rt; ++rt) u += tile_range<N>(a, s, rt).y + kItemUnits;
   return u;
 }
-template <int N>
-__device__ __forceinline__ int64_t total_units(const PagedArgs& a) {      // warp-collective
-  int64_t u = 0;
-  for (int b = threadIdx.x & 31; b < a.batch; b += 32) u += seq_units<N>(a, b);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-  return u * a.n_kv;
+// where CTA `cta` of `ctas` begins (64-bit divisions only for more units than 2^32 / ctas)
+__device__ __forceinline__ int64_t cut(int64_t total, int cta, int ctas) {
+  const int64_t x = total * cta;
+  return x >> 32 ? x / ctas : static_cast<uint32_t>(x) / static_cast<uint32_t>(ctas);
 }
 struct Item {
   int b, hk, rt, off;                      // off: units of the item before the place asked for
@@ -114,44 +111,54 @@ struct Place {
   int64_t total, unit;                     // units of the call, of this CTA's start
   Item it;
 };
-// The item that holds unit `unit` (< total_units).  Warp-collective.
+// The units of the call, and where CTA `cta` of `ctas` begins.  Warp-collective; the lanes keep the units of the first
+// 32 sequences between the sum and the search.
 template <int N>
-__device__ __forceinline__ Item locate(const PagedArgs& a, int64_t unit) {
+__device__ __forceinline__ Place locate(const PagedArgs& a, int cta, int ctas) {
   const int lane = threadIdx.x & 31;
-  Item it{0, 0, 0, 0};
+  const int64_t own = lane < a.batch ? seq_units<N>(a, lane) : 0;
+  int64_t sum = own;
+  for (int b = lane + 32; b < a.batch; b += 32) sum += seq_units<N>(a, b);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  Place pl{sum * a.n_kv, 0, Item{0, 0, 0, 0}};
+  pl.unit = cut(pl.total, cta, ctas);
+  if (pl.unit >= pl.total) return pl;
   int64_t before = 0;
   for (int base = 0; base < a.batch; base += 32) {
     const int b = base + lane;
-    const int64_t mine = b < a.batch ? seq_units<N>(a, b) : 0;
+    const int64_t mine = base == 0 ? own : b < a.batch ? seq_units<N>(a, b) : 0;
     int64_t x = mine * a.n_kv;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += y;
     }
-    const unsigned past = __ballot_sync(0xffffffffu, before + x > unit);
+    const unsigned past = __ballot_sync(0xffffffffu, before + x > pl.unit);
     if (past) {
       const int src = __ffs(past) - 1;
       const int64_t per = __shfl_sync(0xffffffffu, mine, src);
-      int64_t in = unit - before - (__shfl_sync(0xffffffffu, x, src) - per * a.n_kv);
-      it.b = base + src;
-      it.hk = static_cast<int>(in / per);
-      in -= it.hk * per;
-      const SeqInfo s = seq_info<N>(a, it.b);
+      int64_t in = pl.unit - before - (__shfl_sync(0xffffffffu, x, src) - per * a.n_kv);
+      pl.it.b = base + src;
+      while (in >= per) {                                     // (fewer steps than KV heads)
+        in -= per;
+        ++pl.it.hk;
+      }
+      const SeqInfo s = seq_info<N>(a, pl.it.b);
       for (int rt = 0; rt < s.n_rt; ++rt) {
         const int u = tile_range<N>(a, s, rt).y + kItemUnits;
         if (in < u) {
-          it.rt = rt;
-          it.off = static_cast<int>(in);
+          pl.it.rt = rt;
+          pl.it.off = static_cast<int>(in);
           break;
         }
         in -= u;
       }
-      return it;
+      return pl;
     }
     before += __shfl_sync(0xffffffffu, x, 31);
   }
-  return it;
+  return pl;
 }
 
 // A warp's walk over its CTA's units: one segment = consecutive tiles of one
@@ -206,7 +213,6 @@ struct Walk {
     } while (s.n_virt <= 0 && it.b + 1 < a.batch);
   }
 };
-__device__ __forceinline__ int64_t cut(int64_t total, int cta, int ctas) { return total * cta / ctas; }
 
 // ------------------------------------------------------------------ the kernel
 template <int HD_, int N_>
@@ -301,19 +307,24 @@ __device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// v[r] of 32 lanes -> lanes r and r + 16 get the reduction of row r
-template <class Op>
-__device__ __forceinline__ float reduce_rows(float (&v)[16], Op op) {
+// the largest of the warp's 32 values (NaN left out)
+__device__ __forceinline__ float warp_top(float v) {
+  float r;
+  asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+// v[r] of 32 lanes -> lanes r and r + 16 get the sum of row r
+__device__ __forceinline__ float sum_rows(float (&v)[16]) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = op(v[i], __shfl_xor_sync(0xffffffffu, v[i], 16));
+  for (int i = 0; i < 16; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 16);
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) {
     const bool up = lane & o;
 #pragma unroll
     for (int i = 0; i < o; ++i) {
       const float send = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
-      v[i] = op(keep, __shfl_xor_sync(0xffffffffu, send, o));
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
     }
   }
   return v[0];
@@ -426,12 +437,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   }
   pdl_enter();
   if (warp == 0) {
-    const int64_t total = total_units<N>(a);
-    const int64_t u0 = cut(total, blockIdx.x, gridDim.x), u1 = cut(total, blockIdx.x + 1, gridDim.x);
-    const Item it = u0 < u1 ? locate<N>(a, u0) : Item{0, 0, 0, 0};
+    const Place pl = locate<N>(a, blockIdx.x, gridDim.x);
     if (lane == 0) {
-      *s_place = Place{total, u0, it};
-      a.place[blockIdx.x] = Place{total, u0, it};
+      *s_place = pl;
+      a.place[blockIdx.x] = pl;
     }
   }
   tc_fence_before();
@@ -633,20 +642,16 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       const int qb = seg & 1, rows = fetch();
       bool ok = warp_wait_bounded(raw_full, seg & 1, abort_flag, nullptr);
       uint32_t top = 0;
-#pragma unroll 2
+#pragma unroll 4
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid;
-        if (c / CPR >= rows) break;
-        const uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
-        const uint32_t x[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t lo = x[e] << 16 & 0x7fff0000u, hi = x[e] & 0x7fff0000u;
-          if (lo < 0x7f800000u) top = max(top, lo);
-          if (hi < 0x7f800000u) top = max(top, hi);
-        }
+        uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
+        if (c / CPR >= rows) q = make_uint4(0, 0, 0, 0);
+        // infinities and NaN (an exponent of ones) aside
+        auto finite = [](uint32_t w) { return w & 0x7fff7fffu & ~__vcmpgeu2(w & 0x7fff7fffu, 0x7f807f80u); };
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(finite(q.x), finite(q.y)), __vmaxu2(finite(q.z), finite(q.w))));
       }
-      top = __reduce_max_sync(0xffffffffu, top);
+      top = __reduce_max_sync(0xffffffffu, max(top & 0xffff0000u, top << 16));
       if (lane == 0) s_qmax[warp & 1] = top;
       asm volatile("barrier.cta.sync 3, 64;" ::: "memory");
       top = max(s_qmax[0], s_qmax[1]);
@@ -654,7 +659,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       const float q_up = __int_as_float((7 - e_max + 127) << 23), q_down = __int_as_float((e_max - 7 + 127) << 23);
       ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr) && ok;
       if (tid == 0) s_qdown[seg & 3] = q_down;
-#pragma unroll 2
+#pragma unroll 4
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
         uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
@@ -665,7 +670,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         for (int e = 0; e < 4; ++e) {
           // the upper four significant bits of each value, then the lower four
           const float2 v = make_float2(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
-          const float2 u = make_float2(__uint_as_float((x[e] << 16) & 0xfff00000u) * q_up, __uint_as_float(x[e] & 0xfff00000u) * q_up);
+          const float2 u = make_float2(__uint_as_float(__float_as_uint(v.x) & 0xfff00000u), __uint_as_float(__float_as_uint(v.y) & 0xfff00000u));
           const uint32_t p = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
           const uint32_t l = __nv_cvt_float2_to_fp8x2(make_float2(v.x - u.x, v.y - u.y), __NV_SATFINITE, __NV_E4M3);
           term[0][e >> 1] |= p << (16 * (e & 1));
@@ -766,14 +771,13 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         if (vote_group<128>(1 + grp, unset || mx + lv > 8.0f || !ok)) {
           // ---- some row exceeds its reference (or has none): new references, O and the sums follow
           if (*abort_flag) ok = false;
+          float m = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < RN; c += 16) {
-            float y[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) y[k] = x[c + k] + lv;
-            const float m = reduce_rows(y, [](float p, float q) { return fmaxf(p, q); });
-            if (lane < 16) my_red[c + lane] = m;
+          for (int r = 0; r < RN; ++r) {
+            const float top = warp_top(x[r] + lv);
+            m = lane == r ? top : m;
           }
+          if (lane < RN) my_red[lane] = m;
           bar_group<128>(1 + grp);
           bool none = false;
           if (tid < RN) {
@@ -843,7 +847,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         float y[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) y[k] = l[c + k];
-        const float s = reduce_rows(y, [](float p, float q) { return p + q; });
+        const float s = sum_rows(y);
         if (lane < 16) my_red[c + lane] = s;
       }
       bar_group<128>(1 + grp);
@@ -919,24 +923,35 @@ __global__ void __launch_bounds__(128) merge_paged_kernel(const PagedArgs a, int
   if (it.off >= nt) return;                                   // its tiles end ahead of the cut
   constexpr int PL = HD / 32;
   float m = -INFINITY, l = 0.0f, acc[PL] = {};
-  for (int64_t k0 = cut(pl.total, k, ctas); k < ctas && k0 < first + nt; ++k) {
-    const int64_t k1 = cut(pl.total, k + 1, ctas);
-    if (k0 < k1) {                                            // this CTA has tiles of the item
-      const int64_t slot = 2LL * k + (k0 <= first);
-      const float2 ml = a.part_ml[slot * N + r];
-      float x[PL];
-      const float* p = a.part_o + (slot * N + r) * HD + lane * PL;
+  // four parts are asked for at a time; a CTA without units has none
+  int64_t k0 = cut(pl.total, k, ctas);
+  while (k < ctas && k0 < first + nt) {
+    float2 ml[4];
+    float x[4][PL];
 #pragma unroll
-      for (int d = 0; d < PL; ++d) x[d] = p[d];
-      if (ml.x != -INFINITY) {                                // it saw a key
-        const float mn = fmaxf(m, ml.x), f = ex2_approx(m - mn), h = ex2_approx(ml.x - mn);
-        l = l * f + ml.y * h;
+    for (int u = 0; u < 4; ++u) {
+      ml[u] = make_float2(-INFINITY, 0.0f);
+      if (k >= ctas || k0 >= first + nt) continue;
+      const int64_t k1 = cut(pl.total, k + 1, ctas);
+      if (k0 < k1) {
+        const int64_t slot = 2LL * k + (k0 <= first);
+        ml[u] = a.part_ml[slot * N + r];
+        const float* p = a.part_o + (slot * N + r) * HD + lane * PL;
 #pragma unroll
-        for (int d = 0; d < PL; ++d) acc[d] = acc[d] * f + x[d] * h;
-        m = mn;
+        for (int d = 0; d < PL; ++d) x[u][d] = p[d];
       }
+      k0 = k1;
+      ++k;
     }
-    k0 = k1;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (ml[u].x == -INFINITY) continue;                     // it saw no key
+      const float mn = fmaxf(m, ml[u].x), f = ex2_approx(m - mn), h = ex2_approx(ml[u].x - mn);
+      l = l * f + ml[u].y * h;
+#pragma unroll
+      for (int d = 0; d < PL; ++d) acc[d] = acc[d] * f + x[u][d] * h;
+      m = mn;
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   bf16* o = a.o + (s.first + v / a.group) * a.ldo + static_cast<int64_t>(it.hk * a.group + v % a.group) * HD + lane * PL;

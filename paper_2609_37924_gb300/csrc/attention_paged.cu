@@ -44,6 +44,7 @@
 #include "serve.h"
 #include "softmax_rows.cuh"
 #include "tensor_map.h"
+#include "umma_tiles.cuh"
 
 namespace tadm {
 namespace {
@@ -245,34 +246,14 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_maj
   return (1u << 4) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
 }
-// MN-major operand with 128-byte swizzling: a line of 64 rows per key, 8 keys
-// of 1024 bytes per atom; only one atom along the rows, so both offsets are
-// the step of 8 keys.
-__device__ __forceinline__ uint64_t sdesc_mn_sw128(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(1024 >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
-}
-// D(tmem) (+)= A(smem) * B(smem)^T, 8-bit floats, fp32 accumulator
-__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, e;\n\t"
-      "elect.sync _|e, 0xffffffff;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "@e tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 // A and B: e4m3, both K-major
 __host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
-// K-major 8-bit operand whose rows are HD bytes, swizzled over the row's width
+// High word of the descriptor of a K-major 8-bit operand whose rows are HD bytes, swizzled over the row's width (the low
+// word is desc_k's).
 template <int HD>
-__device__ __forceinline__ uint64_t sdesc_rows8(uint32_t saddr) {
-  constexpr uint64_t sbo = 8 * HD, layout = HD == 128 ? 2 : 4;
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (static_cast<uint64_t>(1) << 16) | ((sbo >> 4) << 32) |
-         (static_cast<uint64_t>(1) << 46) | (layout << 61);
-}
+constexpr uint32_t kRows8Hi = (8u * HD >> 4) | 1u << 14 | (HD == 128 ? 2u : 4u) << 29;
 // 16-byte chunk `c` of row `r` in that layout
 template <int HD>
 __device__ __forceinline__ int chunk_at(int r, int c) {
@@ -446,7 +427,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = 0;                                    // all 512 columns: the allocation starts at 0
   Walk<N>& w = s_walk[warp];
   if (lane == 0) {
     w.it = s_place->it;
@@ -523,48 +504,47 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     for (int i = max(0, g - NST); i < g; ++i) mbar_wait_bounded(&kv_full[i % NST], (i / NST) & 1, &never, nullptr);
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
-    constexpr uint32_t idesc_o = idesc_f16_f32(128, N, true);
-    int g = 0, seg = 0;
+    constexpr uint32_t idesc_s = idesc_f8_f32(128, N), idesc_o = idesc_f16_f32(128, N, true);
+    const uint32_t q_lo = desc_k(smem_u32(sQ)), k_lo = desc_k(smem_u32(sKV)), p_lo = desc_mn(smem_u32(sP));
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, nullptr);
+    };
+    uint32_t st = 0, turn = 0, tile = 0;                      // ring place and its parity; tiles so far
+    int seg = 0;
     bool ok = true;
     while (ok && w.next(a)) {
-      const int nt = w.nt;
+      const int nt = uniform(w.nt);
       if (nt == 0) continue;
       const int qb = seg & 1;
-      if (!warp_wait_bounded(&q_full[qb], (seg >> 1) & 1, abort_flag, nullptr)) break;
+      if (!wait(&q_full[qb], (seg >> 1) & 1)) break;
       ++seg;
-      const uint64_t q0 = sdesc_rows8<HD>(smem_u32(sQ + qb * C::Q_BYTES));
-      for (int i = 0; i <= nt; ++i) {
+      const uint32_t q0 = q_lo + qb * (C::Q_BYTES >> 4);
+      for (int i = 0; i <= nt; ++i, ++tile) {
         if (i < nt) {
-          // S^T of tile g + i; its buffer was read before p_full of two tiles ago, which PV has waited for
-          const int t = g + i, sb = t & 1, st = t % NST;
-          if (!warp_wait_bounded(&kv_full[st], (t / NST) & 1, abort_flag, nullptr)) { ok = false; break; }
+          // S^T of this tile; its buffer was read before p_full of two tiles ago, which PV has waited for
+          const uint32_t sb = tile & 1, s = tmem + C::S_COL + sb * 64, k0 = k_lo + st * (C::STAGE_BYTES >> 4);
+          if (!wait(&kv_full[st], turn)) { ok = false; break; }
           tc_fence_after();
-          const uint64_t k0 = sdesc_rows8<HD>(smem_u32(sKV + st * C::STAGE_BYTES));
-#pragma unroll
-          for (int term = 0; term < 2; ++term)
-#pragma unroll
-            for (int kk = 0; kk < HD / 32; ++kk)
-              umma_f8(tmem + C::S_COL + sb * 64, k0 + 2 * kk, q0 + ((term * C::QT_BYTES) >> 4) + 2 * kk,
-                      idesc_f8_f32(128, N), term + kk != 0);
+          umma_f8_ss<HD / 32>(s, k0, q0, kRows8Hi<HD>, idesc_s, 0);
+          umma_f8_ss<HD / 32>(s, k0, q0 + (C::QT_BYTES >> 4), kRows8Hi<HD>, idesc_s, 1);
           umma_commit(&s_full[sb]);
           umma_commit(&kv_empty[st]);
           if (i == nt - 1) umma_commit(&q_empty[qb]);
+          if (++st == NST) st = 0, turn ^= 1;
         }
         if (i >= 1) {
-          const int t = g + i - 1, pb = t & 1;
-          if (!warp_wait_bounded(&vt_full[pb], (t >> 1) & 1, abort_flag, nullptr) ||
-              !warp_wait_bounded(&p_full[pb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; break; }
+          const uint32_t t = tile - 1, pb = t & 1, parity = (t >> 1) & 1;
+          const uint32_t v = tmem + C::V_COL + pb * 64, p0 = p_lo + pb * (C::P_BYTES >> 4);
+          if (!wait(&vt_full[pb], parity) || !wait(&p_full[pb], parity)) { ok = false; break; }
           tc_fence_after();
-          const uint64_t p0 = sdesc_mn_sw128(smem_u32(sP + pb * C::P_BYTES));
-#pragma unroll
-          for (int kk = 0; kk < TK / 16; ++kk)
-            umma_bf16_ts(tmem + C::O_COL, tmem + C::V_COL + pb * 64 + 8 * kk, p0 + kk * (2048 >> 4), idesc_o, i != 1 || kk != 0);
+          umma4_ts_mn(tmem + C::O_COL, v, p0, idesc_o, i != 1);
+          umma4_ts_mn(tmem + C::O_COL, v + 32, p0 + 512, idesc_o, 1);
           umma_commit(o_full);
           umma_commit(&vt_empty[pb]);
           if (i == nt) umma_commit(o_done);
         }
       }
-      g += nt;
+      --tile;                                                 // the last round of a segment has no tile of its own
     }
     umma_commit(drain);
     volatile int never = 0;

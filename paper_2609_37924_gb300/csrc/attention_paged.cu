@@ -225,10 +225,10 @@ struct PagedCfg {
   static constexpr int QT_BYTES = N * HD, Q_BYTES = 2 * QT_BYTES;   // two terms of N rows; two buffers
   static constexpr int RAW_BYTES = N * HD * 2;               // Q as it is in memory
   static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
-  static constexpr int RN = N < 32 ? N : 32, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
+  static constexpr int RN = 16, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
   static constexpr int THREADS = 256 + SM_THREADS;
-  static constexpr int MISC = 2560 + N * 40;
+  static constexpr int MISC = 3328 + N * 40;
   static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + RAW_BYTES + MISC;
   static constexpr int V_COL = 0, S_COL = 128, O_COL = 256;  // TMEM columns: two V^T, two S, one O
   static_assert(SMEM <= 232448, "shared memory");
@@ -380,10 +380,10 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
                                                               // softmax reads it later than the MMAs read Q)
   uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 42);  // [2] the staging warps' maxima
   float2* s_scale = reinterpret_cast<float2*>(bars + 64);     // [16][2] (K, V) scales of the pages of tile t at t % 16
-  Walk<N>* s_walk = reinterpret_cast<Walk<N>*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // [16] one per warp
-  static_assert(sizeof(Walk<N>) * 16 <= 1536, "walks");
+  Walk<N>* s_walk = reinterpret_cast<Walk<N>*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // one per warp
+  static_assert(sizeof(Walk<N>) * (C::THREADS / 32) <= 2304, "walks");
   // per virtual row
-  float* s_negm = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 2560);   // minus the reference
+  float* s_negm = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + 3328);   // minus the reference
   float* s_fac = s_negm + N;
   float* s_red = s_fac + N;                                   // [4][N]
   int2* s_see = reinterpret_cast<int2*>(s_red + 4 * N);       // visible keys [x, y)
@@ -633,7 +633,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       }
       top = __reduce_max_sync(0xffffffffu, max(top & 0xffff0000u, top << 16));
       if (lane == 0) s_qmax[warp & 1] = top;
-      asm volatile("barrier.cta.sync 3, 64;" ::: "memory");
+      asm volatile("barrier.cta.sync 8, 64;" ::: "memory");
       top = max(s_qmax[0], s_qmax[1]);
       const int e_max = max(static_cast<int>(top >> 23), 40) - 127;    // 2^e_max <= the largest
       const float q_up = __int_as_float((7 - e_max + 127) << 23), q_down = __int_as_float((e_max - 7 + 127) << 23);
@@ -668,7 +668,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       asm volatile(
           "{\n\t.reg .pred a, b;\n\t"
           "setp.ne.u32 a, %1, 0;\n\t"
-          "barrier.cta.red.or.pred b, 3, 64, a;\n\t"
+          "barrier.cta.red.or.pred b, 8, 64, a;\n\t"
           "selp.u32 %0, 1, 0, b;\n\t}"
           : "=r"(leave)
           : "r"(static_cast<uint32_t>(!ok))

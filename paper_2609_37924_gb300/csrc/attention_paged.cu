@@ -89,7 +89,7 @@ __device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s,
 // An item's units: its tiles, then kItemUnits for its start and end (Q, the
 // first references, the sums, O), measured in tiles; a row tile that sees
 // nothing has zeros to write there.
-constexpr int kItemUnits = 5;
+constexpr int kItemUnits = 6;
 // Units of a sequence and KV head.
 template <int N>
 __device__ __forceinline__ int64_t seq_units(const PagedArgs& a, int b) {
@@ -379,7 +379,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   float* s_qdown = reinterpret_cast<float*>(bars + 40);       // [4] 1 / the factor of segment i's Q at i % 4 (the
                                                               // softmax reads it later than the MMAs read Q)
   uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 42);  // [2] the staging warps' maxima
-  float2* s_scale = reinterpret_cast<float2*>(bars + 64);     // [16][2] (K, V) scales of the pages of tile t at t % 16
+  // [16][2] of the pages of tile t at t % 16: K scale, V scale * 128, log2(V scale)
+  float4* s_scale = reinterpret_cast<float4*>(bars + 64);
   Walk<N>* s_walk = reinterpret_cast<Walk<N>*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // one per warp
   static_assert(sizeof(Walk<N>) * (C::THREADS / 32) <= 2304, "walks");
   // per virtual row
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     struct Batch {
       int hk, tile, n, n_pages;            // n = 0: no batch left
       int id;
-      float2 sc;
+      float4 sc;
     };
     int at = 0;                            // tiles of w's segment that are in a batch
     bool more = w.next(a);
@@ -452,7 +453,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         more = w.next(a);
         at = 0;
       }
-      Batch b{0, 0, 0, 0, -1, make_float2(0.0f, 1.0f)};
+      Batch b{0, 0, 0, 0, -1, make_float4(0.0f, 128.0f, 0.0f, 0.0f)};
       if (!more) return b;
       b.hk = w.it.hk;
       b.tile = w.t0 + at;
@@ -466,7 +467,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     auto scales = [&](Batch& b) {          // a page that is not there: K = V = 0
       if (b.id < 0 || b.id >= a.pages) return;
       const int64_t p = static_cast<int64_t>(b.id) * a.n_kv + b.hk;
-      b.sc = make_float2(a.sk[p], a.sv[p]);
+      const float v = a.sv[p];
+      b.sc = make_float4(a.sk[p], v * 128.0f, log2f(v), 0.0f);
     };
     Batch now = take();
     scales(now);
@@ -720,13 +722,15 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       bool has_ref = false;                                   // of row `own`
       bool unset = true;                                      // some row has no reference yet (the warps agree)
       const int nt = w.nt, t0 = w.t0;
+      float q_scale = 0.0f;
       for (int i = 0; i < nt; ++i) {
         const int t = g + i, sb = t & 1, tile = t0 + i;
         if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; }
         // the warps vote below: all of them leave together
         tc_fence_after();
-        const float2 sc = s_scale[(t & 15) * 2 + (key_lane >> 6)];
-        const float cth = sc.x * s_qdown[seg & 3] * a.scale_log2, lv = log2f(sc.y);
+        const float4 sc = s_scale[(t & 15) * 2 + (key_lane >> 6)];
+        if (i == 0) q_scale = s_qdown[seg & 3] * a.scale_log2;
+        const float cth = sc.x * q_scale, lv = sc.z;
         const int key = tile * TK + key_lane;
         const bool masked = tile * TK < all_lo || (tile + 1) * TK > all_hi;
         float x[RN];
@@ -798,8 +802,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           if (vote_group<128>(1 + grp, !ok)) { ok = false; break; }       // also: s_fac and s_red may be written again
         }
         // ---- P = 2^x times the page's V scale, f16, a 128-byte line per key
-        const float vs = sc.y * 128.0f;
-        const uint64_t vs2 = f2_pack(vs, vs);
+        const uint64_t vs2 = f2_pack(sc.y, sc.y);
         uint8_t* line = sP + sb * C::P_BYTES + key_lane * 128;
 #pragma unroll
         for (int r = 0; r < RN; r += 8) {

@@ -614,3 +614,99 @@ def test_pages_copy(T):
     d.moved(before, [(3, 0), (3, 7), (29, 11)])
     T.tadm_pages_copy(d.pool, i32([]), i32([]))
     d.moved(before, [(3, 0), (3, 7), (29, 11)])
+
+
+# ------------------------------------------------------------------ together
+def test_example_server(T):
+    """The example runs the operators together: pages shared by branches, blocks and single tokens on top of them; every
+    attention over the cache within bf16 rounding of 64 bits (the probabilities' 11 bits and the output's 8)."""
+    import importlib.util
+    import os
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "ragged_server.py")
+    spec = importlib.util.spec_from_file_location("ragged_server", at)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    for heads, kv_heads, hd, seed in ((16, 8, 128, 0), (6, 6, 64, 1)):
+        x, peak, live, worst = m.serve(layers=2, prompts=4, branches=3, heads=heads, kv_heads=kv_heads, hd=hd, seed=seed, check=True)
+        assert torch.isfinite(x).all() and 0 < live < peak and worst < 4e-3, (peak, live, worst)
+
+
+def test_graph_replay(T):
+    """Captured into a CUDA graph and replayed on new inputs in place: packed prompts, write, attention over the cache, read."""
+    Hq, Hkv, hd, lens = 8, 4, 128, [70, 5, 200]
+    cu, rows = i32(cum(lens)), sum(lens)
+    pool, table = T.PagePool.empty(1, 12, Hkv, hd), torch.arange(12, dtype=torch.int32, device="cuda").view(3, 4)
+    x = torch.randn((rows, Hq + 2 * Hkv, hd), generator=gen(1), device="cuda").bfloat16()
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    o, p, kb, vb = (torch.empty((rows, h, hd), dtype=x.dtype, device="cuda") for h in (Hq, Hq, Hkv, Hkv))
+    start, n = i32([0, 0, 0]), i32(lens)
+    scratch = torch.empty(T.tadm_page_attention_scratch_size(3, rows, 200, 200, Hq, Hkv, hd, 1), dtype=torch.uint8, device="cuda")
+
+    def once(stream=None):
+        T.tadm_attention_packed(q, k, v, o, cu, 200, stream=stream)
+        T.tadm_page_write(pool, 0, k, v, cu, start, table, 200, stream=stream)
+        T.tadm_page_attention(q, pool, 0, p, cu, n, table, 200, 200, scratch, causal=True, stream=stream)
+        T.tadm_page_read(pool, 0, kb, vb, cu, start, table, 200, stream=stream)
+
+    once()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once()
+    x.copy_(torch.randn(x.shape, generator=gen(2), device="cuda"))
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [t.clone() for t in (o, p, kb, vb)]
+    once()
+    for a, b in zip(got, (o, p, kb, vb)):
+        assert torch.equal(a, b)
+    for a, m in zip(cum(lens), lens):
+        s = slice(a, a + m)
+        ref, absum = attend64(q[s].double(), k[s].double(), v[s].double(), torch.arange(m, device="cuda"), True, 0)
+        close(o[s], ref, absum, torch.bfloat16, float(v[s].abs().max()))
+        ref, absum = attend64(q[s].double(), kb[s].double(), vb[s].double(), torch.arange(m, device="cuda"), True, 0)
+        close(p[s], ref, absum, torch.bfloat16, float(vb[s].abs().max()))
+
+
+def test_offsets_past_32_bits(T):
+    """The last pages of a pool whose K and V are over 4 GB each: rows written, read and attended over."""
+    Hkv, hd, pages = 8, 128, 34000
+    k = torch.empty((2, pages, Hkv, PAGE, hd), dtype=torch.uint8, device="cuda")
+    v = torch.empty((2, pages, Hkv, hd, PAGE), dtype=torch.uint8, device="cuda")
+    assert k.numel() > 1 << 32
+    scales = [torch.ones((2, pages, Hkv), dtype=torch.float32, device="cuda") for _ in range(2)]
+    pool, table = T.PagePool(k, v, *scales), i32([pages - 1, pages - 3, 5]).view(1, 3)
+    x = torch.randn((150, 2, Hkv, hd), generator=gen(1), device="cuda").bfloat16()
+    T.tadm_page_write(pool, 1, x[:, 0], x[:, 1], i32([0, 150]), i32([0]), table, 150)
+    kb, vb = torch.empty_like(x[:, 0]).contiguous(), torch.empty_like(x[:, 1]).contiguous()
+    T.tadm_page_read(pool, 1, kb, vb, i32([0, 150]), i32([0]), table, 150)
+    assert (kb.float() - x[:, 0].float()).abs().max() <= 2.0 ** -4 * x.abs().max()     # e4m3: half of 2^-3 of a value
+    q = torch.randn((1, 16, hd), generator=gen(2), device="cuda").bfloat16()
+    o = run_paged(T, pool, table, q, [0, 1], [150], 1, 150, True, 0)
+    ref, absum = attend64(q.double(), kb.double(), vb.double(), torch.tensor([149], device="cuda"), True, 0)
+    close(o, ref, absum, torch.bfloat16, float(vb.abs().max()))
+    status, refs = i32([0]), torch.zeros(pages, dtype=torch.int32, device="cuda")
+    T.tadm_pages_copy(pool, i32([pages - 1]), i32([pages - 2]))
+    assert torch.equal(k[:, pages - 1], k[:, pages - 2]) and torch.equal(v[1, pages - 1], v[1, pages - 2])
+    assert int(status) == 0 and int(refs.sum()) == 0
+
+
+def test_many_items_and_long_splits(T):
+    """More sequences than a warp scans at once, most of them short; and one sequence that every SM has a part of."""
+    Hq, Hkv, hd = 8, 4, 64
+    lens = [(13 * i) % 150 for i in range(100)]
+    pool, table, seqs = filled(T, lens, Hkv, hd, 21)
+    rows = [1 if n else 0 for n in lens]
+    q = torch.randn((sum(rows), Hq, hd), generator=gen(3), device="cuda").bfloat16()
+    o = run_paged(T, pool, table, q, cum(rows), lens, 1, max(lens), True, 0)
+    for b, n in enumerate(lens):
+        if n:
+            s = slice(cum(rows)[b], cum(rows)[b] + 1)
+            ref, absum = attend64(q[s].double(), *seqs[b], torch.tensor([n - 1], device="cuda"), True, 0)
+            close(o[s], ref, absum, torch.bfloat16, float(seqs[b][1].abs().max()))
+    pool, table, seqs = filled(T, [70001], 1, hd, 22)
+    for n in (1, 33):
+        q = torch.randn((n, 2, hd), generator=gen(4), device="cuda").bfloat16()
+        o = run_paged(T, pool, table, q, [0, n], [70001], n, 70001, False, 0)
+        ref, absum = attend64(q.double(), *seqs[0], torch.zeros(n, device="cuda"), False, 0)
+        close(o, ref, absum, torch.bfloat16, float(seqs[0][1].abs().max()))

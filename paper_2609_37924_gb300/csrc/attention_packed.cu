@@ -50,6 +50,7 @@ struct PackedArgs {
   const int32_t* cu;
   int batch, total, max_rows, group, n_kv;
   int tq, rows;            // rows of a sequence in a tile, virtual rows (tq * group <= 128)
+  uint32_t group_inv;      // row / group = row * group_inv >> 16 for rows below 128
   int64_t ldo;
   int causal, window;
   float scale_log2;
@@ -152,21 +153,20 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
   tc_fence_after();
   const uint32_t tmem = uniform(static_cast<int>(*tmem_slot));
   const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
-  const int n_virt = rows.n * a.group;
-  const int v0 = (static_cast<int>(pairs(b)) - 1 - within) * NT * a.rows;
-  // the key tiles of virtual tile h: first and end
+  const int tok0 = (static_cast<int>(pairs(b)) - 1 - within) * NT * a.tq;   // first row of the CTA's tiles
+  // the key tiles of tile h, whose rows of the sequence are tok0 + h tq and on: first and end
   auto range = [&](int h) {
-    const int lo_v = v0 + h * a.rows, hi_v = min(lo_v + a.rows, n_virt) - 1;
-    if (lo_v >= n_virt) return make_int2(0, 0);
-    const int end = a.causal ? hi_v / a.group + 1 : rows.n;
-    const int begin = a.window > 0 ? max(0, lo_v / a.group - a.window + 1) : 0;
+    const int lo = tok0 + h * a.tq, hi = min(lo + a.tq, rows.n) - 1;
+    if (lo >= rows.n) return make_int2(0, 0);
+    const int end = a.causal ? hi + 1 : rows.n;
+    const int begin = a.window > 0 ? max(0, lo - a.window + 1) : 0;
     return make_int2(begin / TK, (end + TK - 1) / TK);
   };
   const int2 rA = uniform(range(0)), rB = NT == 2 ? uniform(range(1)) : make_int2(0, 0);
   // the keys that every row of tile h sees: [x, y); a key tile that is not inside them is cut by the mask
   auto common = [&](int h) {
-    const int lo_v = v0 + h * a.rows, hi_v = min(lo_v + a.rows, n_virt) - 1;
-    return make_int2(a.window > 0 ? hi_v / a.group - a.window + 1 : 0, a.causal ? lo_v / a.group + 1 : rows.n);
+    const int lo = tok0 + h * a.tq, hi = min(lo + a.tq, rows.n) - 1;
+    return make_int2(a.window > 0 ? hi - a.window + 1 : 0, a.causal ? lo + 1 : rows.n);
   };
   auto partial = [](int2 c, int j) { return (j + 1) * TK > c.y || j * TK < c.x; };
   const bool two = NT == 2 && rB.y > 0;
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       for (int h = 0; h < (two ? 2 : 1); ++h) {               // rows behind the sequence's end are other rows, unused
         mbar_arrive_expect_tx(&q_full[h], HD / 64 * a.rows * 128);
         for (int s = 0; s < HD / 64; ++s)
-          tma_load_3d(sQ + h * C::TILE_BYTES + s * 16384, &tmQ, &q_full[h], 64 * s, hk * a.group, rows.first + v0 / a.group + h * a.tq);
+          tma_load_3d(sQ + h * C::TILE_BYTES + s * 16384, &tmQ, &q_full[h], 64 * s, hk * a.group, rows.first + tok0 + h * a.tq);
       }
       for (int j = j0; ok && j < j1; ++j)
         for (int m = 0; m < 2; ++m, ++g) {
@@ -275,9 +275,9 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     const int h = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
     const int2 r = h ? rB : rA;
-    const int v = v0 + h * a.rows + row;
-    const bool v_ok = row < a.rows && v < n_virt;
-    const int pos = v_ok ? v / a.group : 0, head = hk * a.group + (v_ok ? v - pos * a.group : 0);
+    const int in_tile = static_cast<int>(row * a.group_inv >> 16), tok = tok0 + h * a.tq + in_tile;
+    const bool v_ok = row < a.rows && tok < rows.n;
+    const int pos = v_ok ? tok : 0, head = hk * a.group + (v_ok ? row - in_tile * a.group : 0);
     const uint32_t t_s = tmem + lane_off + C::S_COL + h * TK, t_o = tmem + lane_off + C::O_COL + h * HD;
     const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2);
     const int see_hi = a.causal && v_ok ? pos + 1 : rows.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       // tensor store; in the sequence's last tile each row has a line of its own (144 bytes apart) and a copy of its own
       tc_fence_after();
       const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-      const bool full_tile = v0 + (h + 1) * a.rows <= n_virt;
+      const bool full_tile = tok0 + (h + 1) * a.tq <= rows.n;
       bf16* orow = a.o + (rows.first + pos) * a.ldo + static_cast<int64_t>(head) * HD;
       uint8_t* tile = sQ + h * C::TILE_BYTES;
 #pragma unroll 1
@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       if (full_tile) {
         asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + h) : "memory");
         if (row == 0) {
-          for (int s = 0; s < HD / 64; ++s) tma_store_3d(&tmO, tile + s * 16384, 64 * s, hk * a.group, rows.first + v0 / a.group + h * a.tq);
+          for (int s = 0; s < HD / 64; ++s) tma_store_3d(&tmO, tile + s * 16384, 64 * s, hk * a.group, rows.first + tok0 + h * a.tq);
           bulk_commit();
         }
       }
@@ -456,7 +456,7 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
   if (!rows_map(&mq, c.q, HD, c.n_heads, c.total, c.ldq, group, tq) || !rows_map(&mo, c.o, HD, c.n_heads, c.total, c.ldo, group, tq) ||
       !rows_map(&mk, c.k, HD, c.n_kv, c.total, c.ldk, 1, TK) || !rows_map(&mv, c.v, HD, c.n_kv, c.total, c.ldv, 1, TK))
     return "attention tensor map encode failed";
-  const PackedArgs a{static_cast<bf16*>(c.o), c.cu, c.batch, c.total, c.max_rows, group, c.n_kv, tq, tq * group,
+  const PackedArgs a{static_cast<bf16*>(c.o), c.cu, c.batch, c.total, c.max_rows, group, c.n_kv, tq, tq * group, 65536u / group + 1,
                      c.ldo, c.causal, c.window, 1.4426950408889634f / sqrtf(static_cast<float>(HD))};
   // at most one CTA per NT tiles of rows and one more per sequence
   const int64_t blocks = (static_cast<int64_t>(c.total) / (NT * tq) + c.batch) * c.n_kv;

@@ -59,6 +59,7 @@ struct PagedArgs {
   const int32_t *cu, *lens, *table;
   int batch, total, max_rows, max_len, ld_table, pages;
   int group, n_kv;
+  uint32_t group_inv;                      // floor((2^32 - 1) / group)
   int64_t ldq, ldo;
   int causal, window;
   float scale_log2;                        // log2(e) / sqrt(hd)
@@ -71,6 +72,11 @@ struct PagedArgs {
 struct SeqInfo {
   int first, n_virt, len, pos0, n_rt;      // first row, virtual rows, tokens, position of row 0, row tiles
 };
+// v / group for 0 <= v < 2^31: the product is the quotient or one less
+__device__ __forceinline__ int by_group(const PagedArgs& a, int v) {
+  const uint32_t q = __umulhi(static_cast<uint32_t>(v), a.group_inv);
+  return static_cast<int>(q + (static_cast<uint32_t>(v) - q * a.group >= static_cast<uint32_t>(a.group)));
+}
 template <int N>
 __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& a, int b) {
   const SeqRows r = seq_rows(a.cu, b, a.total, a.max_rows);
@@ -80,7 +86,7 @@ __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& a, int b) {
 // The tiles that any row of row tile rt sees: first tile and how many (maybe none).
 template <int N>
 __device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s, int rt) {
-  const int r_lo = rt * N / a.group, r_hi = (min((rt + 1) * N, s.n_virt) - 1) / a.group;
+  const int r_lo = by_group(a, rt * N), r_hi = by_group(a, min((rt + 1) * N, s.n_virt) - 1);
   const int end = a.causal ? max(0, min(s.len, s.pos0 + r_hi + 1)) : s.len;
   const int begin = a.window > 0 ? max(0, s.pos0 + r_lo - a.window + 1) : 0;
   const int t0 = begin / TK, t1 = (end + TK - 1) / TK;
@@ -613,7 +619,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         if (lane == 0) mbar_arrive_expect_tx(raw_full, rows * HD * 2);
         __syncwarp();
         for (int r = lane; r < rows; r += 32) {
-          const int t = (v0 + r) / a.group;
+          const int t = by_group(a, v0 + r);
           bulk_load(sRaw + r * HD * 2, a.q + (w.s.first + t) * a.ldq + static_cast<int64_t>(w.it.hk * a.group + v0 + r - t * a.group) * HD,
                     HD * 2, raw_full);
         }
@@ -697,7 +703,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       if (tid < RN) {
         const int v = v0 + own;
         const bool in = v < w.s.n_virt;
-        const int r = v / a.group, pos = w.s.pos0 + r;
+        const int r = by_group(a, v), pos = w.s.pos0 + r;
         s_row[own] = in ? (w.s.first + r) * a.ldo + static_cast<int64_t>(w.it.hk * a.group + v - r * a.group) * HD : -1;
         s_see[own] = make_int2(in && a.window > 0 ? pos - a.window + 1 : 0,
                                in && a.causal ? min(w.s.len, pos + 1) : w.s.len);
@@ -713,8 +719,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       bar_group<128>(1 + grp);
       // rows whose bounds cut a tile: every key below `all_lo` or from `all_hi` on is hidden from some row
       const int last_v = min(v0 + N, w.s.n_virt) - 1;
-      const int all_hi = a.causal ? min(w.s.len, w.s.pos0 + v0 / a.group + 1) : w.s.len;
-      const int all_lo = a.window > 0 ? w.s.pos0 + last_v / a.group - a.window + 1 : 0;
+      const int all_hi = a.causal ? min(w.s.len, w.s.pos0 + by_group(a, v0) + 1) : w.s.len;
+      const int all_lo = a.window > 0 ? w.s.pos0 + by_group(a, last_v) - a.window + 1 : 0;
 
       float l[RN];
 #pragma unroll
@@ -900,7 +906,7 @@ __global__ void __launch_bounds__(128) merge_paged_kernel(const PagedArgs a, int
   while (k > 0 && cut(pl.total, k, ctas) == pl.unit) --k;
   if (cut(pl.total, k, ctas) > first) return;                 // an earlier cut splits the item first
   const SeqInfo s = seq_info<N>(a, it.b);
-  const int v = it.rt * N + r;
+  const int v = it.rt * N + r, row = by_group(a, v);
   if (v >= s.n_virt) return;
   const int64_t nt = tile_range<N>(a, s, it.rt).y;
   if (it.off >= nt) return;                                   // its tiles end ahead of the cut
@@ -937,7 +943,7 @@ __global__ void __launch_bounds__(128) merge_paged_kernel(const PagedArgs a, int
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  bf16* o = a.o + (s.first + v / a.group) * a.ldo + static_cast<int64_t>(it.hk * a.group + v % a.group) * HD + lane * PL;
+  bf16* o = a.o + (s.first + row) * a.ldo + static_cast<int64_t>(it.hk * a.group + v - row * a.group) * HD + lane * PL;
 #pragma unroll
   for (int d = 0; d < PL; d += 2) *reinterpret_cast<__nv_bfloat162*>(o + d) = __floats2bfloat162_rn(acc[d] * inv, acc[d + 1] * inv);
 }
@@ -979,7 +985,8 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
   float* part = static_cast<float*>(c.scratch);
   const PagedArgs a{static_cast<const bf16*>(c.q), static_cast<bf16*>(c.o), p.k_scale + at, p.v_scale + at,
                     c.cu, c.lens, c.table, c.batch, c.total, c.max_rows, c.max_len, c.ld_table, p.pages,
-                    c.n_heads / c.n_kv, c.n_kv, c.ldq, c.ldo, c.causal, c.window,
+                    c.n_heads / c.n_kv, c.n_kv, 0xffffffffu / static_cast<uint32_t>(c.n_heads / c.n_kv),
+                    c.ldq, c.ldo, c.causal, c.window,
                     1.4426950408889634f / sqrtf(static_cast<float>(HD)), part,
                     reinterpret_cast<float2*>(part + 2LL * ctas * N * HD),
                     reinterpret_cast<Place*>(part + 2LL * ctas * N * (HD + 2))};

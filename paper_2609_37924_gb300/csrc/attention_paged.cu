@@ -362,7 +362,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const float (&v)[16]) 
 
 template <int HD_, int N_>
 __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
-    attn_paged_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const PagedArgs a) {
+    attn_paged_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                      const __grid_constant__ CUtensorMap tmV, const PagedArgs a) {
   using C = PagedCfg<HD_, N_>;
   constexpr int HD = C::HD, N = C::N, NST = C::STAGES, PB = C::PAGE_BYTES;
   extern __shared__ uint8_t smem_raw[];
@@ -612,10 +613,17 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     int seg = 0;
     bool more = w.next(a);
     while (more && w.nt == 0) more = w.next(a);
-    // the rows of an item, copied by warp 2
+    // the rows of an item: one box where its tiles hold whole rows of the sequence (what lies behind the sequence's end
+    // comes along and is not used), else row by row
     auto fetch = [&]() {
       const int v0 = w.it.rt * N, rows = min(N, w.s.n_virt - v0);
-      if (warp == 2) {
+      if (warp == 2 && N % a.group == 0) {
+        if (lane == 0) {
+          mbar_arrive_expect_tx(raw_full, N * HD * 2);
+          tma_load_3d(sRaw, &tmQ, raw_full, 0, w.it.hk * a.group, w.s.first + by_group(a, v0));
+        }
+        __syncwarp();
+      } else if (warp == 2) {
         if (lane == 0) mbar_arrive_expect_tx(raw_full, rows * HD * 2);
         __syncwarp();
         for (int r = lane; r < rows; r += 32) {
@@ -958,6 +966,17 @@ bool page_map(CUtensorMap* m, const void* ptr, uint32_t d0, uint32_t d1, uint64_
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// bf16 map {hd, heads, rows}, box {hd, group, n / group}, not swizzled
+bool q_map(CUtensorMap* m, const void* ptr, int hd, int heads, int total, int64_t ld, int group, int n) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(hd), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(total)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(hd) * 2, static_cast<cuuint64_t>(ld) * 2};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(hd), static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(n / group)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return tensor_map_encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Virtual rows of a tile: the least of 16, 32, 64 that holds a sequence's rows of one KV head (64: several tiles).
 int tile_rows(int max_rows, int group) {
   const int64_t v = static_cast<int64_t>(max_rows) * group;
@@ -978,19 +997,21 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
     return "attention smem attribute failed";
   const tadm_page_pool& p = *c.pool;
   const int64_t at = static_cast<int64_t>(c.layer) * p.pages * p.n_kv_heads;
-  CUtensorMap mk, mv;
-  if (!page_map(&mk, static_cast<const uint8_t*>(p.k) + at * PT * HD, HD, PT, p.n_kv_heads, p.pages) ||
+  const int group = c.n_heads / c.n_kv;
+  CUtensorMap mq{}, mk, mv;
+  if ((N % group == 0 && !q_map(&mq, c.q, HD, c.n_heads, c.total, c.ldq, group, N)) ||
+      !page_map(&mk, static_cast<const uint8_t*>(p.k) + at * PT * HD, HD, PT, p.n_kv_heads, p.pages) ||
       !page_map(&mv, static_cast<const uint8_t*>(p.v) + at * PT * HD, PT, HD, p.n_kv_heads, p.pages))
     return "page tensor map encode failed";
   float* part = static_cast<float*>(c.scratch);
   const PagedArgs a{static_cast<const bf16*>(c.q), static_cast<bf16*>(c.o), p.k_scale + at, p.v_scale + at,
                     c.cu, c.lens, c.table, c.batch, c.total, c.max_rows, c.max_len, c.ld_table, p.pages,
-                    c.n_heads / c.n_kv, c.n_kv, 0xffffffffu / static_cast<uint32_t>(c.n_heads / c.n_kv),
+                    group, c.n_kv, 0xffffffffu / static_cast<uint32_t>(group),
                     c.ldq, c.ldo, c.causal, c.window,
                     1.4426950408889634f / sqrtf(static_cast<float>(HD)), part,
                     reinterpret_cast<float2*>(part + 2LL * ctas * N * HD),
                     reinterpret_cast<Place*>(part + 2LL * ctas * N * (HD + 2))};
-  cudaError_t e = launch_pdl(attn_paged_kernel<HD, N>, ctas, C::THREADS, C::SMEM, s, mk, mv, a);
+  cudaError_t e = launch_pdl(attn_paged_kernel<HD, N>, ctas, C::THREADS, C::SMEM, s, mq, mk, mv, a);
   if (e == cudaSuccess && ctas > 1)
     e = launch_pdl(merge_paged_kernel<HD, N>, dim3(ctas - 1, N / 4), 128, 0, s, a, ctas);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);

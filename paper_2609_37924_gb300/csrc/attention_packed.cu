@@ -12,9 +12,10 @@
 // P (bf16) lies in TMEM over the scores that it was made from, V is read as it
 // lies in memory (a key per line, an MN-major operand).  The reference maximum
 // of a row moves only when a tile exceeds it by 2^8; O is rescaled then.
-// A key tile that some row of a tile sees only in part keeps P in two bf16
-// terms, whose 128 columns are those of the scores: rows with few visible keys,
-// where single probabilities weigh most, do not feel the rounding to 8 bits.
+// Where a causal row of a tile sees fewer than 256 keys in all, key tiles that
+// the mask cuts keep P in two bf16 terms, whose 128 columns are those of the
+// scores: with few visible keys single probabilities weigh most, and these
+// rows do not feel their rounding to 8 bits.
 // What a tile holds behind the sequence's end belongs to its neighbour: those
 // scores are masked, and those lines of V are zeroed in shared memory.
 //
@@ -75,9 +76,10 @@ __device__ __forceinline__ void exp32_pack(const uint32_t (&r)[32], uint64_t sc2
     pk[j] = *reinterpret_cast<uint32_t*>(&t);
   }
 }
-// The same where columns outside lo .. lim - 1 are hidden (P = 0), with the remainders P - bf16(P) as bf16 pairs.
-__device__ __forceinline__ void exp32_split(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, int lo, int lim,
-                                            uint64_t (&ps2)[2], uint32_t (&pk)[16], uint32_t* rest) {
+// The same where columns outside lo .. lim - 1 are hidden (P = 0); REST: with the remainders P - bf16(P) as bf16 pairs.
+template <bool REST>
+__device__ __forceinline__ void exp32_masked(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, int lo, int lim,
+                                             uint64_t (&ps2)[2], uint32_t (&pk)[16], uint32_t* rest) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     float x0, x1;
@@ -87,8 +89,10 @@ __device__ __forceinline__ void exp32_split(const uint32_t (&r)[32], uint64_t sc
     ps2[j & 1] = f2_add(ps2[j & 1], f2_pack(p0, p1));
     __nv_bfloat162 t = __floats2bfloat162_rn(p0, p1);
     pk[j] = *reinterpret_cast<uint32_t*>(&t);
-    t = __floats2bfloat162_rn(p0 - __uint_as_float(pk[j] << 16), p1 - __uint_as_float(pk[j] & 0xffff0000u));
-    rest[j] = *reinterpret_cast<uint32_t*>(&t);
+    if (REST) {
+      t = __floats2bfloat162_rn(p0 - __uint_as_float(pk[j] << 16), p1 - __uint_as_float(pk[j] & 0xffff0000u));
+      rest[j] = *reinterpret_cast<uint32_t*>(&t);
+    }
   }
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
@@ -169,6 +173,12 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     return make_int2(a.window > 0 ? hi - a.window + 1 : 0, a.causal ? lo + 1 : rows.n);
   };
   auto partial = [](int2 c, int j) { return (j + 1) * TK > c.y || j * TK < c.x; };
+  // whether tile h keeps P in two terms in cut key tiles: a causal row of it sees fewer than 256 keys; without the causal
+  // rule only a sequence's end and a window's edge cut
+  auto few = [&](int h) {
+    const int seen = tok0 + h * a.tq + 1;
+    return !a.causal || (a.window > 0 ? min(seen, a.window) : seen) < 256;
+  };
   const bool two = NT == 2 && rB.y > 0;
   const int j0 = rA.x, j1 = two ? rB.y : rA.y, n_keys = uniform(rows.n);   // A's keys begin and end no later than B's
 
@@ -200,6 +210,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     // --------------------------------------------------------------- MMA issuer
     constexpr uint32_t idesc_s = idesc_bf16_f32(TQ, TK), idesc_o = idesc_bf16_f32(TQ, HD) | 1u << 16;   // V: MN-major
     const int2 cA = uniform(common(0)), cB = uniform(common(1));
+    const bool fA = uniform(few(0)), fB = uniform(few(1));
     struct Slot {                                             // a place of the ring and the parity of its phase
       uint32_t at, parity;
     };
@@ -251,14 +262,14 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       }
       tc_fence_after();
       if (j < rA.y) {
-        if (!values(0, sv, j - j0, j == j0, partial(cA, j))) break;
+        if (!values(0, sv, j - j0, j == j0, fA && partial(cA, j))) break;
         if (j == rA.y - 1) umma_commit(&o_done[0]);
       }
       if (!two) umma_commit(&empty[sv.at]);
       if (j + 1 < rA.y) scores(0, sk);
       if (two) {
         if (j >= rB.x) {                                      // (j < rB.y: B's keys end last)
-          if (!values(1, sv, j - rB.x, j == rB.x, partial(cB, j))) break;
+          if (!values(1, sv, j - rB.x, j == rB.x, fB && partial(cB, j))) break;
           if (j == rB.y - 1) umma_commit(&o_done[1]);
         }
         umma_commit(&empty[sv.at]);
@@ -297,6 +308,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       l_run *= factor;
     };
     const int2 all = common(h);
+    const bool few_keys = few(h);
     bool ok = true;
     for (int j = r.x; j < r.y; ++j) {
       if (!warp_wait_bounded(&s_full[h], (j - r.x) & 1, abort_flag, nullptr)) { ok = false; break; }
@@ -327,17 +339,25 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         }
         if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
         const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
-        uint32_t rest[64];
+        if (few_keys) {
+          uint32_t rest[64];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          exp32_split(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
-          tmem_st16(t_s + 16 * c, pk);
-        }
+          for (int c = 0; c < 4; ++c) {
+            exp32_masked<true>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
+            tmem_st16(t_s + 16 * c, pk);
+          }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 4; ++c) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k) pk[k] = rest[16 * c + k];
-          tmem_st16(t_s + TK / 2 + 16 * c, pk);
+            for (int k = 0; k < 16; ++k) pk[k] = rest[16 * c + k];
+            tmem_st16(t_s + TK / 2 + 16 * c, pk);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            exp32_masked<false>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, nullptr);
+            tmem_st16(t_s + 16 * c, pk);
+          }
         }
       } else {
         float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};

@@ -9,10 +9,10 @@
 // whose page scales are two registers.
 //
 // K enters the tensor cores as the e4m3 bytes that the page holds; Q is the sum
-// of two e4m3 terms, both multiplied with K into the same fp32 scores.  V^T is widened to f16, because the probabilities need
-// more than 8 bits.
+// of two e4m3 terms, both multiplied with K into the same fp32 scores.  V^T is
+// widened to f16, because the probabilities need more than 8 bits.
 //
-// A tile is 128 keys, two pages.  Roles of a CTA (12 warps, or 16 for 64 rows):
+// A tile is 128 keys, two pages.  Roles of a CTA (12, 16 or 24 warps for 16, 32 or 64 rows):
 //   warp 0       streams the pages with TMA (one 4-D map for K, one for V^T)
 //                and leaves their scales beside them;
 //   warps 2, 3   stage Q of the next work item while this one runs;
@@ -20,7 +20,7 @@
 //                TMEM A operand (a dim per lane); slots past the sequence
 //                become zeros here;
 //   warp 1       S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
-//   warps 8-     softmax: a key per thread, the values of up to 32 rows in
+//   warps 8-     softmax: a key per thread, the values of 16 rows in
 //                registers.  The running maximum of a row is a reference that
 //                moves only when a tile exceeds it by 2^8, so a tile costs
 //                one vote of the four warps that share rows and no reduction
@@ -36,7 +36,8 @@
 // Work: the tiles of all (sequence, KV head, row tile) items lie on one line,
 // each item followed by what its start and end cost, and the line is cut
 // evenly over the SMs, whatever the lengths; an item that a cut splits leaves
-// fp32 partials, which a second small kernel merges in order.
+// fp32 partials, which a second small kernel merges in order.  Where the cuts
+// fall follows from all lengths of a call, and with them a row's last bits.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -117,6 +118,8 @@ struct Item {
 struct Place {
   int64_t total, unit;                     // units of the call, of this CTA's start
   Item it;
+  SeqInfo s;                               // of the item's sequence
+  int nt;                                  // the item's tiles
 };
 // The units of the call, and where CTA `cta` of `ctas` begins.  Warp-collective; the lanes keep the units of the first
 // 32 sequences between the sum and the search.
@@ -128,7 +131,7 @@ __device__ __forceinline__ Place locate(const PagedArgs& a, int cta, int ctas) {
   for (int b = lane + 32; b < a.batch; b += 32) sum += seq_units<N>(a, b);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  Place pl{sum * a.n_kv, 0, Item{0, 0, 0, 0}};
+  Place pl{sum * a.n_kv, 0, Item{0, 0, 0, 0}, SeqInfo{0, 0, 0, 0, 0}, 0};
   pl.unit = cut(pl.total, cta, ctas);
   if (pl.unit >= pl.total) return pl;
   int64_t before = 0;
@@ -151,15 +154,15 @@ __device__ __forceinline__ Place locate(const PagedArgs& a, int cta, int ctas) {
         in -= per;
         ++pl.it.hk;
       }
-      const SeqInfo s = seq_info<N>(a, pl.it.b);
-      for (int rt = 0; rt < s.n_rt; ++rt) {
-        const int u = tile_range<N>(a, s, rt).y + kItemUnits;
-        if (in < u) {
+      pl.s = seq_info<N>(a, pl.it.b);
+      for (int rt = 0; rt < pl.s.n_rt; ++rt) {
+        pl.nt = tile_range<N>(a, pl.s, rt).y;
+        if (in < pl.nt + kItemUnits) {
           pl.it.rt = rt;
           pl.it.off = static_cast<int>(in);
           break;
         }
-        in -= u;
+        in -= pl.nt + kItemUnits;
       }
       return pl;
     }
@@ -382,10 +385,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   uint64_t* raw_full = bars + 43;                             // a completion per segment, its rows of Q
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  Place* s_place = reinterpret_cast<Place*>(bars + 36);       // 32 bytes
-  float* s_qdown = reinterpret_cast<float*>(bars + 40);       // [4] 1 / the factor of segment i's Q at i % 4 (the
+  float* s_qdown = reinterpret_cast<float*>(bars + 36);       // [4] 1 / the factor of segment i's Q at i % 4 (the
                                                               // softmax reads it later than the MMAs read Q)
-  uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 42);  // [2] the staging warps' maxima
+  uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 38);  // [2] the staging warps' maxima
+  Place* s_place = reinterpret_cast<Place*>(bars + 44);
+  static_assert(sizeof(Place) <= 160, "place");
   // [16][2] of the pages of tile t at t % 16: K scale, V scale * 128, log2(V scale)
   float4* s_scale = reinterpret_cast<float4*>(bars + 64);
   Walk<N>* s_walk = reinterpret_cast<Walk<N>*>(reinterpret_cast<uint8_t*>(bars) + 1024);   // one per warp
@@ -441,7 +445,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     w.it = s_place->it;
     w.left = cut(s_place->total, blockIdx.x + 1, gridDim.x) - s_place->unit;
     w.started = 0;
-    if (w.left > 0) w.s = seq_info<N>(a, w.it.b);
+    w.s = s_place->s;
   }
 
   if (warp == 0) {
@@ -913,10 +917,10 @@ __global__ void __launch_bounds__(128) merge_paged_kernel(const PagedArgs a, int
   int k = c - 1;                                              // the CTA that ends at this cut
   while (k > 0 && cut(pl.total, k, ctas) == pl.unit) --k;
   if (cut(pl.total, k, ctas) > first) return;                 // an earlier cut splits the item first
-  const SeqInfo s = seq_info<N>(a, it.b);
+  const SeqInfo s = pl.s;
   const int v = it.rt * N + r, row = by_group(a, v);
   if (v >= s.n_virt) return;
-  const int64_t nt = tile_range<N>(a, s, it.rt).y;
+  const int64_t nt = pl.nt;
   if (it.off >= nt) return;                                   // its tiles end ahead of the cut
   constexpr int PL = HD / 32;
   float m = -INFINITY, l = 0.0f, acc[PL] = {};

@@ -491,43 +491,44 @@ __global__ void __launch_bounds__(PB) plan_reserve_kernel(const SeqArgs a) {
   finish(a, status, 0);
 }
 
+// (Each step is a chain of dependent reads of about 0.7 us each: what does not
+// need the list comes first, and the steps share their barriers.)
 __global__ void __launch_bounds__(PB) plan_fork_kernel(const SeqArgs a) {
   pdl_enter();
+  copy_refs(a);
+  const int have = take_free(a.refs, a.pages, min(a.n, a.pages), a.sc.fresh);   // an entry takes one page at most
   int status = mark_list(a, a.list2) ? 0 : TADM_PAGES_BAD;
   bool ok = true;
-  if (!status)
-    for (int i = threadIdx.x >> 5; i < a.n; i += PB / 32) {     // a warp per list entry
-      const int s = a.list[i], d = a.list2[i];
-      const bool in = s >= 0 && s < a.n_seqs && a.sc.mark[s] == 0;
-      const int len = in ? a.lens[s] : -1, np = len < 0 ? 0 : pages_of(len);
-      if (len < 0 || np > a.ld || a.tables[static_cast<int64_t>(d) * a.ld] >= 0) {
-        ok = false;
-        continue;
-      }
-      const int32_t* row = a.tables + static_cast<int64_t>(s) * a.ld;
-      for (int j = threadIdx.x & 31; j < np; j += 32) {
-        const int p = row[j];
-        if (p < 0 || p >= a.pages || a.refs[p] <= 0) ok = false;
-      }
-      if ((threadIdx.x & 31) == 0) {
-        a.sc.count[i] = len % PT != 0;
-        a.sc.first[i] = len / PT;
-      }
-    }
-  if (!__syncthreads_and(ok)) status = TADM_PAGES_BAD;
   int need = 0;
   for (int base = 0; !status && base < a.n; base += PB) {
     const int i = base + threadIdx.x;
+    int c = 0;
+    if (i < a.n) {
+      const int s = a.list[i];
+      const bool in = s >= 0 && s < a.n_seqs && a.sc.mark[s] == 0;
+      const int len = in ? a.lens[s] : -1;
+      if (len < 0 || pages_of(len) > a.ld || a.tables[static_cast<int64_t>(a.list2[i]) * a.ld] >= 0) ok = false;
+      else c = len % PT != 0;
+      a.sc.count[i] = c;
+      a.sc.first[i] = max(len, 0) / PT;
+    }
     int total;
-    const int at = block_scan(i < a.n ? a.sc.count[i] : 0, &total);
+    const int at = block_scan(c, &total);
     if (i < a.n) a.sc.offset[i] = need + at;
     need += total;
   }
-  __syncthreads();
-  if (!status && (need > a.pages || take_free(a.refs, a.pages, need, a.sc.fresh) < need)) status = TADM_PAGES_SHORT;
-  __syncthreads();
-  copy_refs(a);
-  __syncthreads();
+  if (!__syncthreads_and(ok)) status = TADM_PAGES_BAD;
+  if (!status)
+    for (int i = threadIdx.x >> 4; i < a.n; i += PB / 16) {     // the pages that are shared or copied, 16 threads per entry
+      const int32_t* row = a.tables + static_cast<int64_t>(a.list[i]) * a.ld;
+      const int np = a.sc.first[i] + a.sc.count[i];
+      for (int j = threadIdx.x & 15; j < np; j += 16) {
+        const int p = row[j];
+        if (p < 0 || p >= a.pages || a.refs[p] <= 0) ok = false;
+      }
+    }
+  if (!__syncthreads_and(ok)) status = TADM_PAGES_BAD;
+  if (!status && need > have) status = TADM_PAGES_SHORT;
   if (!status)
     for (int i = threadIdx.x; i < a.n; i += PB)
       if (a.sc.count[i]) {

@@ -498,22 +498,28 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  * t * ld + h * head_dim, ld >= heads * head_dim, so that q, k and v may be
  * slices of one QKV projection's output.  dtype: 0 fp32, 1 bf16, of every row
  * operand of the call.  Pointers are 16-byte aligned and ld * element size is
- * a multiple of 16.  head_dim is 64 or 128.
+ * a multiple of 16.  head_dim is 64 or 128.  The attention calls return
+ * TADM_ERR_UNSUPPORTED where a sequence's rows times the query heads of a KV
+ * head pass 2^31.
  *
  * Visibility.  Keys j of a row's own sequence; causal: only j <= p, p the
  * row's position; window > 0: only j with p - j < window.  A row that sees no
  * key gets zeros.  K and V of one sequence never reach another one's rows,
- * whatever they hold; an infinity or NaN in V of a visible key spreads to
- * rows of the same sequence that do not see that key.
+ * whatever they hold, nor do keys that no row of their sequence sees reach
+ * any; an infinity or NaN in V of a key that one row sees may spread to rows
+ * of the same sequence that do not.
  *
  * Arithmetic: fp32 scores, softmax sums and accumulators.  bf16 calls round
  * the probabilities to 8 (tadm_attention_packed) or 11 significant bits
- * (tadm_page_attention) before they multiply V. */
+ * (tadm_page_attention) before they multiply V.  Results repeat from call to
+ * call; the last bits of a row may depend on the other sequences' lengths
+ * (tadm_page_attention splits long contexts by the whole call's work). */
 
 /* softmax(Q K^T / sqrt(head_dim)) V of whole prompts: row r of a sequence is
  * at position r.  q, o: [total_rows, n_heads, head_dim]; k, v: [total_rows,
  * n_kv_heads, head_dim].  Query head h reads KV head h / (n_heads /
- * n_kv_heads).  o must not overlap the inputs. */
+ * n_kv_heads).  o must not overlap the inputs.  bf16 calls take up to 128
+ * query heads per KV head (TADM_ERR_UNSUPPORTED above). */
 TADM_API tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, void* o,
                                            const int32_t* cu_rows, int batch, int total_rows, int max_rows,
                                            int n_heads, int n_kv_heads, int head_dim, int64_t ldq, int64_t ldk,
@@ -551,7 +557,8 @@ typedef struct {
  * encoded again (which is exact but for the smallest, because scales are powers
  * of two).  Slots past the last row of a page written from its first slot are
  * zeroed.  No two sequences of a call may share a page that it writes, and
- * ld_table * 64 covers start[b] + rows. */
+ * ld_table * 64 covers start[b] + rows.  batch is at most 65535 here and in
+ * tadm_page_read (TADM_ERR_UNSUPPORTED above). */
 TADM_API tadm_status tadm_page_write(const tadm_page_pool* pool, int layer, const void* k, const void* v,
                                      const int32_t* cu_rows, const int32_t* start, int batch, int total_rows,
                                      int max_rows, int64_t ldk, int64_t ldv, const int32_t* table, int ld_table,
@@ -568,9 +575,11 @@ TADM_API tadm_status tadm_page_read(const tadm_page_pool* pool, int layer, void*
  * ones: row r of n is at position lens[b] - n + r.  A decode step has one row per
  * sequence, a block step block_len rows and causal = 0, a chunk of a prompt
  * many rows and causal = 1.  lens[b] <= max_len <= ld_table * 64; tokens past
- * max_len are left out.  scratch: at least tadm_page_attention_scratch_size()
- * bytes, 16-byte aligned; it needs no initialisation, and calls that overlap
- * on the GPU need one each. */
+ * max_len are left out.  Scales that bf16 calls meet lie within 2^-60 ..
+ * 2^60, as tadm_page_write makes them.  scratch: at least
+ * tadm_page_attention_scratch_size() bytes (for the current device), 16-byte
+ * aligned; it needs no initialisation, and calls that overlap on the GPU need
+ * one each. */
 TADM_API tadm_status tadm_page_attention_scratch_size(int batch, int total_rows, int max_rows, int max_len,
                                                       int n_heads, int n_kv_heads, int head_dim, int dtype,
                                                       size_t* bytes);

@@ -17,8 +17,8 @@
 //                and leaves their scales beside them;
 //   warps 2, 3   stage Q of the next work item while this one runs;
 //   warps 4-7    convert V^T: e4m3 -> f16, exact, from shared memory into the
-//                TMEM A operand (a dim per lane); slots past the sequence
-//                become zeros here;
+//                TMEM A operand (a dim per lane); keys that no row
+//                of the item sees become zeros here;
 //   warp 1       S^T(i) = K Q^T, then O^T += V^T P^T of tile i - 1;
 //   warps 8-     softmax: a key per thread, the values of 16 rows in
 //                registers.  The running maximum of a row is a reference that
@@ -32,6 +32,14 @@
 // times the page's V scale are rounded to f16 (11 bits) with the row's
 // reference at 2^7 to 2^15, so that a probability 2^-21 of the largest still
 // has all of them; scores, sums and O are fp32.
+//
+// Bound: the bytes of the cache.  Measured: 4 tokens over 386,544 cached ones (8
+// KV heads of 128) 135 us, 5.9 TB/s; with 64 virtual rows a tile takes 1.05 us
+// per SM for 0.73 us of bytes, paced by the softmax warps' chain of waits (8 x
+// 32 rows over 99,641 tokens, 16 KV heads: 97 us, 4.3 TB/s).  There, in the order
+// of their making: K and V both widened to f16 157 us; K multiplied as it is
+// stored, 142 with Q in three terms and 121 in two; fewer instructions around
+// the items 109; 16 rows per softmax thread where 32 were 100.
 //
 // Work: the tiles of all (sequence, KV head, row tile) items lie on one line,
 // each item followed by what its start and end cost, and the line is cut
@@ -84,17 +92,25 @@ __device__ __forceinline__ SeqInfo seq_info(const PagedArgs& a, int b) {
   const int len = min(max(a.lens[b], 0), a.max_len);
   return {r.first, r.n * a.group, len, len - r.n, (r.n * a.group + N - 1) / N};
 }
-// The tiles that any row of row tile rt sees: first tile and how many (maybe none).
+// The keys that any row of row tile rt sees: from .x to before .y.
+template <int N>
+__device__ __forceinline__ int2 key_range(const PagedArgs& a, const SeqInfo& s, int rt) {
+  const int r_lo = by_group(a, rt * N), r_hi = by_group(a, min((rt + 1) * N, s.n_virt) - 1);
+  return make_int2(a.window > 0 ? max(0, s.pos0 + r_lo - a.window + 1) : 0,
+                   a.causal ? max(0, min(s.len, s.pos0 + r_hi + 1)) : s.len);
+}
+// Their tiles: first tile and how many (maybe none).
+__device__ __forceinline__ int2 tiles_of(int2 keys) {
+  const int t0 = keys.x / TK, t1 = (keys.y + TK - 1) / TK;
+  return make_int2(t0, keys.x < keys.y ? t1 - t0 : 0);
+}
 template <int N>
 __device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s, int rt) {
-  const int r_lo = by_group(a, rt * N), r_hi = by_group(a, min((rt + 1) * N, s.n_virt) - 1);
-  const int end = a.causal ? max(0, min(s.len, s.pos0 + r_hi + 1)) : s.len;
-  const int begin = a.window > 0 ? max(0, s.pos0 + r_lo - a.window + 1) : 0;
-  const int t0 = begin / TK, t1 = (end + TK - 1) / TK;
-  return make_int2(t0, begin < end ? t1 - t0 : 0);
+  return tiles_of(key_range<N>(a, s, rt));
 }
 // An item's units: its tiles, then kItemUnits for its start and end (Q, the
-// first references, the sums, O), measured in tiles; a row tile that sees
+// first references, the sums, O), measured in tiles (32 block steps over 1 to
+// 2000 tokens: 49 us with 3, 43.6 with 5, 42.4 with 8); a row tile that sees
 // nothing has zeros to write there.
 constexpr int kItemUnits = 6;
 // Units of a sequence and KV head.
@@ -182,6 +198,7 @@ struct Walk {
   int t0, nt;              // tiles of the segment; none: the item sees nothing and has zeros to write
   int from_start, to_end;  // it begins / ends with its item's tiles
   int started;
+  int begin;               // the first key that a row of the item sees
   __device__ __forceinline__ bool next(const PagedArgs& a) {   // false: no segment left.  Warp-collective.
     __syncwarp();
     if ((threadIdx.x & 31) == 0) move(a);
@@ -197,7 +214,8 @@ struct Walk {
         nt = -1;
         return;
       }
-      const int2 r = tile_range<N>(a, s, it.rt);
+      const int2 keys = key_range<N>(a, s, it.rt), r = tiles_of(keys);
+      begin = keys.x;
       const int units = r.y + kItemUnits, off = it.off;
       const int take = static_cast<int>(min(left, static_cast<int64_t>(units - off)));
       const int lo = min(off, r.y), hi = min(off + take, r.y);
@@ -223,6 +241,18 @@ struct Walk {
     } while (s.n_virt <= 0 && it.b + 1 < a.batch);
   }
 };
+
+// Zeroes what line `row` of a staged V^T tile (two pages of PB bytes) holds of its first `lo` keys.  Out of line: it runs
+// once per item, and the loop that calls it is short of registers.
+template <int PB>
+__device__ __noinline__ void hide_front(uint8_t* v, int row, int lo) {
+#pragma unroll 1
+  for (int n = 0; n < lo; n += 4) {
+    uint32_t* word = reinterpret_cast<uint32_t*>(v + (n >> 6) * PB + row * PT + ((((n >> 4) & 3) ^ ((row >> 1) & 3)) << 4) + (n & 15));
+    *word = lo - n >= 4 ? 0u : *word & ~((1u << (8 * (lo - n))) - 1u);
+  }
+  fence_proxy_async_smem();                                   // the next page arrives there
+}
 
 // ------------------------------------------------------------------ the kernel
 template <int HD_, int N_>
@@ -472,7 +502,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       b.n_pages = (w.s.len + PT - 1) / PT;
       at += b.n;
       const int page = 2 * b.tile + lane;
-      if (lane < 2 * b.n && page < b.n_pages) b.id = a.table[static_cast<int64_t>(w.it.b) * a.ld_table + page];
+      // (a page in front of the window is not there)
+      if (lane < 2 * b.n && page >= w.begin / PT && page < b.n_pages) b.id = a.table[static_cast<int64_t>(w.it.b) * a.ld_table + page];
       return b;
     };
     auto scales = [&](Batch& b) {          // a page that is not there: K = V = 0
@@ -579,7 +610,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
           tc_fence_after();
           if (HD == 128 || row < 64) {                        // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
-            const int valid = keys - i * TK;                // keys of this tile that exist
+            const int valid = keys - i * TK;                  // keys of this tile that exist
+            if (a.window > 0 && i == 0) hide_front<PB>(sKV + st * C::STAGE_BYTES + 2 * PB, row, w.begin - w.t0 * TK);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               const uint8_t* line = base + (2 + c) * PB + row * PT;

@@ -1,15 +1,15 @@
-// Attention of packed rows on the CUDA cores: over the rows of their own
+// Attention of packed fp32 rows on the CUDA cores: over the rows of their own
 // sequence, or over a sequence's pages of the 8-bit cache.
 //
 // A block takes 16 virtual rows (row-major, then the query heads of one KV
 // head, so that a key tile serves all of them) of one sequence and walks its
 // visible keys in tiles of 64: K and V as fp32 in shared memory, a warp per
 // two virtual rows, two keys per lane for the scores, four or two dims per
-// lane for P V.  Everything is fp32: scores, running maximum and sum
-// (online softmax), accumulators.
+// lane for P V.  Everything is fp32: scores, running maximum and sum (online
+// softmax), accumulators.  It serves fp32 rows, those of the small models, whose
+// calls are a launch (11 us with the host's part for a few hundred rows of 4
+// heads); long ones are bound by shared-memory reads.
 #include <cuda_fp8.h>
-
-#include <type_traits>
 
 #include "ragged.cuh"
 #include "serve.h"
@@ -21,8 +21,8 @@ constexpr int RT = 16, KT = 64, NT = 256;     // virtual rows and keys of a tile
 static_assert(KT == TADM_PAGE_TOKENS, "a key tile is a page");
 
 struct RowsAttnArgs {
-  const void *q, *k, *v;
-  void* o;
+  const float *q, *k, *v;
+  float* o;
   const uint8_t *pk, *pv;
   const float *sk, *sv;
   const int32_t *cu, *lens, *table;
@@ -33,7 +33,7 @@ struct RowsAttnArgs {
   float scale;
 };
 
-template <class T, bool PAGED, int HD>
+template <bool PAGED, int HD>
 __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
   pdl_enter();
   constexpr int LD = HD + 4, PL = HD / 32;
@@ -59,8 +59,7 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
   const int k_begin = a.window > 0 ? max(0, pos0 + r_lo - a.window + 1) : 0;
   for (int i = tid; i < RT * HD; i += NT) {
     const int v = v0 + i / HD;
-    const T* q = static_cast<const T*>(a.q);
-    sQ[i] = v < n_virt ? to_f32(q[(rows.first + v / group) * a.ldq + static_cast<int64_t>(hk * group + v % group) * HD + i % HD]) : 0.0f;
+    sQ[i] = v < n_virt ? a.q[(rows.first + v / group) * a.ldq + static_cast<int64_t>(hk * group + v % group) * HD + i % HD] : 0.0f;
   }
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, acc[2][PL] = {};
   for (int k0 = k_begin / KT * KT; k0 < k_end; k0 += KT) {
@@ -75,16 +74,16 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
       auto dec = [](uint8_t x) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(x, __NV_E4M3))); };
       for (int i = tid; i < KT * HD; i += NT) {
         const int kr = i / HD, kc = i % HD, vt = i % KT, vd = i / KT;
-        sK[kr * LD + kc] = ok && k0 + kr < len ? dec(pk[i]) * ks : 0.0f;
-        sV[vt * LD + vd] = ok && k0 + vt < len ? dec(pv[i]) * vs : 0.0f;   // slots past the length may hold anything
+        sK[kr * LD + kc] = ok && k0 + kr < k_end ? dec(pk[i]) * ks : 0.0f;
+        // what no row of the tile sees may hold anything
+        sV[vt * LD + vd] = ok && k0 + vt >= k_begin && k0 + vt < k_end ? dec(pv[i]) * vs : 0.0f;
       }
     } else {
-      const T *k = static_cast<const T*>(a.k), *v = static_cast<const T*>(a.v);
       for (int i = tid; i < KT * HD; i += NT) {
         const int r = i / HD, c = i % HD;
         const int64_t row = rows.first + k0 + r;
-        sK[r * LD + c] = k0 + r < len ? to_f32(k[row * a.ldk + static_cast<int64_t>(hk) * HD + c]) : 0.0f;
-        sV[r * LD + c] = k0 + r < len ? to_f32(v[row * a.ldv + static_cast<int64_t>(hk) * HD + c]) : 0.0f;
+        sK[r * LD + c] = k0 + r < len ? a.k[row * a.ldk + static_cast<int64_t>(hk) * HD + c] : 0.0f;
+        sV[r * LD + c] = k0 + r < len ? a.v[row * a.ldv + static_cast<int64_t>(hk) * HD + c] : 0.0f;
       }
     }
     __syncthreads();
@@ -136,24 +135,25 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
     const int v = v0 + 2 * warp + i;
     const float sum = warp_sum(l[i]);
     if (v >= n_virt) continue;
-    T* o = static_cast<T*>(a.o) + (rows.first + v / group) * a.ldo + static_cast<int64_t>(hk * group + v % group) * HD;
+    float* o = a.o + (rows.first + v / group) * a.ldo + static_cast<int64_t>(hk * group + v % group) * HD;
 #pragma unroll
-    for (int d = 0; d < PL; ++d) o[32 * d + lane] = from_f32<T>(sum == 0.0f ? 0.0f : acc[i][d] / sum);
+    for (int d = 0; d < PL; ++d) o[32 * d + lane] = sum == 0.0f ? 0.0f : acc[i][d] / sum;
   }
 }
 
-template <class T, bool PAGED, int HD>
+template <bool PAGED, int HD>
 const char* launch(const RaggedCall& c, cudaStream_t s) {
   constexpr int smem = (2 * KT * (HD + 4) + RT * HD + RT * KT) * 4;
   int dev = 0;
   current_sms(&dev);
   static PerDevice ready;
   if (ready.get(dev, [] {
-        return cudaFuncSetAttribute(attn_rows_kernel<T, PAGED, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) ==
+        return cudaFuncSetAttribute(attn_rows_kernel<PAGED, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) ==
                        cudaSuccess ? 1 : 0;
       }) <= 0)
     return "attention smem attribute failed";
-  RowsAttnArgs a{c.q, c.k, c.v, c.o, nullptr, nullptr, nullptr, nullptr, c.cu, c.lens, c.table, c.batch, c.total,
+  RowsAttnArgs a{static_cast<const float*>(c.q), static_cast<const float*>(c.k), static_cast<const float*>(c.v),
+                 static_cast<float*>(c.o), nullptr, nullptr, nullptr, nullptr, c.cu, c.lens, c.table, c.batch, c.total,
                  c.max_rows, c.max_len, c.ld_table, 0, c.n_heads, c.n_kv, c.ldq, c.ldk, c.ldv, c.ldo, c.causal, c.window,
                  1.0f / sqrtf(static_cast<float>(HD))};
   if (PAGED) {
@@ -168,7 +168,7 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
   const int group = c.n_heads / c.n_kv;
   // at most one tile per 16 virtual rows and one more per sequence
   const int64_t tiles = static_cast<int64_t>(c.total) * group / RT + c.batch;
-  const cudaError_t e = launch_pdl(attn_rows_kernel<T, PAGED, HD>, dim3(static_cast<unsigned>(tiles), c.n_kv), NT, smem, s, a);
+  const cudaError_t e = launch_pdl(attn_rows_kernel<PAGED, HD>, dim3(static_cast<unsigned>(tiles), c.n_kv), NT, smem, s, a);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 
@@ -176,13 +176,8 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
 
 const char* attention_rows(const RaggedCall& c, cudaStream_t s) {
   if (c.batch == 0 || c.total == 0 || c.max_rows == 0) return nullptr;
-  auto hd = [&](auto t, auto paged) {
-    using T = decltype(t);
-    constexpr bool P = decltype(paged)::value;
-    return c.head_dim == 128 ? launch<T, P, 128>(c, s) : launch<T, P, 64>(c, s);
-  };
-  if (c.bf16) return c.pool ? hd(bf16{}, std::true_type{}) : hd(bf16{}, std::false_type{});
-  return c.pool ? hd(0.0f, std::true_type{}) : hd(0.0f, std::false_type{});
+  if (c.pool) return c.head_dim == 128 ? launch<true, 128>(c, s) : launch<true, 64>(c, s);
+  return c.head_dim == 128 ? launch<false, 128>(c, s) : launch<false, 64>(c, s);
 }
 
 }  // namespace tadm

@@ -45,7 +45,7 @@ struct RaggedCall {
   int causal, window, bf16;
   void* scratch;
 };
-const char* attention_rows(const RaggedCall& c, cudaStream_t s);      // CUDA cores, any type
+const char* attention_rows(const RaggedCall& c, cudaStream_t s);      // CUDA cores, fp32
 const char* attention_packed(const RaggedCall& c, cudaStream_t s);    // tcgen05, bf16 rows over themselves
 const char* attention_paged(const RaggedCall& c, cudaStream_t s);     // tcgen05, bf16 rows over a pool
 size_t attention_paged_scratch(int max_rows, int group, int head_dim);

@@ -50,6 +50,12 @@ bool heads_ok(int n_heads, int n_kv, int head_dim) {
   return n_heads > 0 && n_kv > 0 && n_heads % n_kv == 0 && n_kv <= 16384 && (head_dim == 64 || head_dim == 128);
 }
 
+// query heads x rows of one sequence and KV head, and tiles of 16 of them over the call, are int32
+bool grid_ok(int batch, int total, int rows, int group) {
+  return static_cast<int64_t>(rows) * group <= INT32_MAX - 128 &&
+         static_cast<int64_t>(total) * group / 16 + batch <= INT32_MAX;
+}
+
 bool seqs_ok(const int32_t* tables, const int32_t* refs, int pages, int n_seqs, int ld_table, const int32_t* list, int n,
              const int32_t* tables_out, const int32_t* refs_out, const int32_t* status, const void* scratch,
              size_t scratch_bytes) {
@@ -75,6 +81,7 @@ tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, v
   if (!rows_ok(q, ldq, wq, dtype) || !rows_ok(k, ldk, wk, dtype) || !rows_ok(v, ldv, wk, dtype) ||
       !rows_ok(o, ldo, wq, dtype))
     return TADM_ERR_INVALID_ARG;
+  if (!grid_ok(batch, total_rows, max_rows < total_rows ? max_rows : total_rows, n_heads / n_kv_heads)) return TADM_ERR_UNSUPPORTED;
   // a tile of the tensor-core kernel holds whole rows, all query heads of a KV head; its grid is one-dimensional
   if (dtype && (n_heads / n_kv_heads > 128 ||
                 (static_cast<int64_t>(total_rows) / (128 / (n_heads / n_kv_heads)) + batch) * n_kv_heads > INT32_MAX))
@@ -84,7 +91,7 @@ tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, v
   c.cu = cu_rows, c.batch = batch, c.total = total_rows, c.max_rows = max_rows < total_rows ? max_rows : total_rows;
   c.n_heads = n_heads, c.n_kv = n_kv_heads, c.head_dim = head_dim;
   c.ldq = ldq, c.ldk = ldk, c.ldv = ldv, c.ldo = ldo;
-  c.causal = causal, c.window = window, c.bf16 = dtype;
+  c.causal = causal, c.window = window < c.max_rows ? window : 0, c.bf16 = dtype;   // none where no distance reaches it
   return (dtype ? attention_packed(c, stream) : attention_rows(c, stream)) ? TADM_ERR_CUDA : TADM_OK;
 }
 
@@ -124,6 +131,8 @@ tadm_status tadm_page_attention(const void* q, const tadm_page_pool* pool, int l
   if (batch == 0 || total_rows == 0 || max_rows == 0) return TADM_OK;
   const int64_t wq = static_cast<int64_t>(n_heads) * pool->head_dim;
   if (!rows_ok(q, ldq, wq, dtype) || !rows_ok(o, ldo, wq, dtype)) return TADM_ERR_INVALID_ARG;
+  if (!grid_ok(batch, total_rows, max_rows < total_rows ? max_rows : total_rows, n_heads / pool->n_kv_heads))
+    return TADM_ERR_UNSUPPORTED;
   size_t need = 0;
   tadm_page_attention_scratch_size(batch, total_rows, max_rows, max_len, n_heads, pool->n_kv_heads, pool->head_dim, dtype, &need);
   if (need > 0 && (!scratch || !aligned(scratch) || scratch_bytes < need)) return TADM_ERR_INVALID_ARG;
@@ -132,7 +141,8 @@ tadm_status tadm_page_attention(const void* q, const tadm_page_pool* pool, int l
   c.cu = cu_rows, c.lens = lens, c.table = table, c.batch = batch, c.total = total_rows;
   c.max_rows = max_rows < total_rows ? max_rows : total_rows, c.max_len = max_len, c.ld_table = ld_table;
   c.n_heads = n_heads, c.n_kv = pool->n_kv_heads, c.head_dim = pool->head_dim;
-  c.ldq = ldq, c.ldo = ldo, c.causal = causal, c.window = window, c.bf16 = dtype, c.scratch = scratch;
+  c.ldq = ldq, c.ldo = ldo, c.causal = causal, c.bf16 = dtype, c.scratch = scratch;
+  c.window = window < max_len ? window : 0;                   // none where no distance reaches it
   return (dtype ? attention_paged(c, stream) : attention_rows(c, stream)) ? TADM_ERR_CUDA : TADM_OK;
 }
 

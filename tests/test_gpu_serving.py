@@ -363,6 +363,57 @@ def test_page_attention_limits(T, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("causal,window", [(True, 1), (True, 70), (False, 150)])
+def test_page_attention_behind_window(T, dtype, heads, causal, window):
+    """Keys that the window hides from every row of a sequence reach none, whatever they, their page's scales or their table
+    entry hold."""
+    Hq, Hkv, hd = heads
+    rows, lens = [1, 32, 5], [700, 1000, 389]
+    pool, table, seqs = filled(T, lens, Hkv, hd, 21)
+    q = torch.randn((sum(rows), Hq, hd), generator=gen(22), device="cuda").to(dtype)
+    for b, n in enumerate(rows):
+        lo = lens[b] - n - window + 1                # the first row's first key
+        page = int(table[b, lo // PAGE])
+        pool.k[1, page, :, :lo % PAGE] = 0x7F
+        pool.v[1, page, :, :, :lo % PAGE] = 0xFF
+        gone = table[b, :lo // PAGE].long()
+        pool.k[1, gone], pool.v[1, gone], pool.k_scale[1, gone], pool.v_scale[1, gone] = 0x7F, 0x7F, math.nan, math.inf
+        table[b, :lo // PAGE:2] = -1
+    o = run_paged(T, pool, table, q, cum(rows), lens, max(rows), max(lens), causal, window)
+    for b, n in enumerate(rows):
+        s, (k, v) = slice(cum(rows)[b], cum(rows)[b] + n), seqs[b]
+        ref, absum = attend64(q[s].double(), k, v, torch.arange(lens[b] - n, lens[b], device="cuda"), causal, window)
+        close(o[s], ref, absum, dtype, float(v.abs().max()))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 300, 299, 40])
+def test_windows_as_long_as_the_context(T, dtype, window):
+    """Windows about the length of the longest context and the longest possible one, where some sequences are shorter than
+    their rows (positions below zero)."""
+    Hq, Hkv, hd, rows, lens = 8, 4, 64, [33, 5, 40, 2], [300, 2, 17, 0]
+    pool, table, seqs = filled(T, lens, Hkv, hd, 31)
+    q = torch.randn((sum(rows), Hq, hd), generator=gen(32), device="cuda").to(dtype)
+    for causal in (True, False):
+        o = run_paged(T, pool, table, q, cum(rows), lens, max(rows), max(lens), causal, window)
+        for b, n in enumerate(rows):
+            s, (k, v) = slice(cum(rows)[b], cum(rows)[b] + n), seqs[b]
+            if lens[b] == 0:
+                assert (o[s] == 0).all()
+                continue
+            ref, absum = attend64(q[s].double(), k, v, torch.arange(lens[b] - n, lens[b], device="cuda"), causal, window)
+            close(o[s], ref, absum, dtype, float(v.abs().max()))
+        k, v = (torch.randn((sum(rows), Hkv, hd), generator=gen(33 + i), device="cuda").to(dtype) for i in range(2))
+        o = torch.empty_like(q)
+        T.tadm_attention_packed(q, k, v, o, i32(cum(rows)), max(rows), causal=causal, window=window)
+        for b, n in enumerate(rows):
+            s = slice(cum(rows)[b], cum(rows)[b] + n)
+            ref, absum = attend64(q[s].double(), k[s].double(), v[s].double(), torch.arange(n, device="cuda"), causal, window)
+            close(o[s], ref, absum, dtype, float(v.abs().max()))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows", [1, 32])
 def test_page_attention_sink(T, dtype, rows):
     """One key holds nearly all the weight and a zero value; the rest of a long context, each key 2^-20 of it, makes

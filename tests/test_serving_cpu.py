@@ -127,3 +127,22 @@ def test_bookkeeping_needs_its_lists(T):
     assert lib.tadm_pages_scratch_size(-1, 4, ctypes.byref(ctypes.c_size_t())) == INVALID
     assert lib.tadm_pages_scratch_size(4, 4, None) == INVALID
     assert a["pages"] == c.pages
+
+
+UNSUPPORTED = 2
+
+
+def test_sizes_beyond_the_grids(T):
+    """Well-formed calls that no kernel takes, and their neighbours in range that have nothing to do."""
+    lib, c = T.load_library(), pool(T)
+    many = dict(heads=4 * 129, ldq=4 * 129 * 64, ldo=4 * 129 * 64)
+    assert lib.tadm_attention_packed(*{**PACKED, **many}.values()) == UNSUPPORTED
+    assert lib.tadm_attention_packed(*{**PACKED, **many, "total": 0}.values()) == 0
+    wide = dict(heads=16384, kv=16384, ldq=16384 * 64, ldk=16384 * 64, ldv=16384 * 64, ldo=16384 * 64, total=1 << 27, max_rows=1 << 27)
+    assert lib.tadm_attention_packed(*{**PACKED, **wide}.values()) == UNSUPPORTED
+    tall = dict(total=1 << 30, max_rows=1 << 30)              # 2 query heads per KV head: 2^31 rows of one
+    assert lib.tadm_attention_packed(*{**PACKED, **tall, "dtype": 0}.values()) == UNSUPPORTED
+    assert lib.tadm_page_attention(P, ctypes.addressof(c), *{**ATTEND, **tall}.values()) == UNSUPPORTED
+    for f in (lib.tadm_page_write, lib.tadm_page_read):
+        assert f(ctypes.addressof(c), *{**ROWS, "batch": 65536}.values()) == UNSUPPORTED
+        assert f(ctypes.addressof(c), *{**ROWS, "batch": 65536, "max_rows": 0}.values()) == 0

@@ -2,9 +2,13 @@
 //
 // A CTA takes one or two tiles of up to 128 virtual rows (as many whole rows of
 // one sequence as fit, row-major, then the query heads of one KV head) and
-// walks the key tiles that they see, 128 keys each.  Two tiles both use a K or V tile while it is in shared memory,
-// and their softmaxes alternate with the tensor pipe:
-//   warp 0       streams K and V tiles with TMA into a ring of five slots;
+// walks the key tiles that they see, 128 keys each.  Two tiles both use a K or V
+// tile while it is in shared memory, and their softmaxes alternate with the
+// tensor pipe.  A CTA that is through takes the work of a block of the grid that
+// has not started (the hardware hands it out), so that the next Q, K and first
+// scores come while the last O leaves:
+//   warp 0       finds the work and streams Q, K and V tiles with TMA, these
+//                into a ring of four slots;
 //   warp 1       O_A += P_A V(j), S_A = Q_A K(j+1)^T, then the same for B: one
 //                tile's softmax runs while the tensor pipe works on the other,
 //                and P V of a tile's first 64 keys while it is at the others;
@@ -20,10 +24,11 @@
 // scores are masked, and those lines of V are zeroed in shared memory.
 //
 // Bound: the tensor pipe, 1024 cycles per 128 x 128 tile at hd 128 (the
-// exponentials take 512).  Measured: about 1450 per tile, 1.29 PFLOP/s over an
-// 8111-token prompt of 32 / 16 heads (462 us with its neighbours); prompts of a
-// few hundred tokens are bound by the starts and ends of the CTAs (24 prompts,
-// 6400 tokens, 16 / 8 heads: 42 us).
+// exponentials take 512).  Measured: about 1450 per tile, 1.33 PFLOP/s over an
+// 8111-token prompt of 32 / 16 heads (449 us with its neighbours; 461 where
+// each block starts and ends by itself, and a window of 1024 over 8900 rows 133
+// instead of 157); prompts of a few hundred tokens are bound by the latency of
+// cut tiles (24 prompts, 6400 tokens, 16 / 8 heads: 43 us).
 #include "ragged.cuh"
 #include "serve.h"
 #include "softmax_rows.cuh"
@@ -40,9 +45,10 @@ template <int HD_, int NT_>
 struct PackedCfg {
   static constexpr int HD = HD_, NT = NT_;
   static constexpr int TILE_BYTES = HD / 64 * 16384;          // HD/64 atoms of 128 rows x 64 dims: a tile of Q, K or V
-  static constexpr int SLOTS = NT == 2 ? 5 : 4;
+  static constexpr int SLOTS = 4;
+  static constexpr int STAGE_BYTES = 16384;                   // 64 dims of a tile's O on their way out
   static constexpr int MIN_BLOCKS = 3 - NT;
-  static constexpr int SMEM = 1024 + (NT + SLOTS) * TILE_BYTES + 256;
+  static constexpr int SMEM = 1024 + (NT + SLOTS) * TILE_BYTES + NT * STAGE_BYTES + 512;
   static constexpr int S_COL = 0, O_COL = NT * TK, TMEM_COLS = NT * 256;   // NT tiles of 128 columns, then of HD
   static constexpr int THREADS = 128 + NT * 128;
   static constexpr int REGS = NT == 2 ? 224 : 200;            // of a softmax thread; the other warps keep 56
@@ -60,11 +66,30 @@ struct PackedArgs {
   float scale_log2;
 };
 
-// `bytes` (a multiple of 16) of shared memory to global memory (bulk-group completion)
-__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(reinterpret_cast<uint64_t>(dst)),
-               "r"(smem_u32(src)), "r"(bytes)
+// A pair of row tiles: KV head, first row and row count of the sequence (0: no pair is left), first row of the pair in it.
+struct Work {
+  int hk, first, n, tok0;
+};
+// Asks for the index of a block of this grid that has not started, which then never starts: 16 bytes arrive at `resp`,
+// counted on the mbarrier.  One thread; not again after next_block() has said that there is none.
+__device__ __forceinline__ void ask_block(void* resp, uint64_t* bar) {
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_u32(resp)),
+               "r"(smem_u32(bar))
                : "memory");
+}
+// The index (blockIdx.x), -1: none is left.
+__device__ __forceinline__ int next_block(const void* resp) {
+  int x;
+  asm volatile(
+      "{\n\t.reg .b128 h;\n\t.reg .pred p;\n\t"
+      "ld.shared.b128 h, [%1];\n\t"
+      "mov.u32 %0, -1;\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, h;\n\t}"
+      : "=r"(x)
+      : "r"(smem_u32(resp))
+      : "memory");
+  return x;
 }
 // P = 2^(s * scale - m) of 32 columns as 16 packed pairs, added to the sums.
 __device__ __forceinline__ void exp32_pack(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, uint64_t (&ps2)[2],
@@ -116,12 +141,17 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                                         // NT tiles
   uint8_t* sKV = sQ + NT * C::TILE_BYTES;                     // ring: K and V tiles in turn
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sKV + NS * C::TILE_BYTES);
+  uint8_t* sO = sKV + NS * C::TILE_BYTES;                     // O of each tile on its way out
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sO + NT * C::STAGE_BYTES);
   uint64_t *full = bars, *empty = bars + NS;                  // [NS]
   uint64_t *q_full = bars + 2 * NS, *s_full = q_full + 2, *o_done = q_full + 4;   // [2] by tile
   uint64_t* p_full = q_full + 6;                              // [2][2] by tile, keys 0 .. 63 and 64 .. 127
-  uint64_t* drain = q_full + 10;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t *drain = q_full + 10, *asked = drain + 1;
+  uint64_t* q_empty = drain + 2;                              // [2] by tile
+  uint64_t *w_full = drain + 4, *w_empty = drain + 6;         // [2] the pairs of row tiles in turn
+  Work* s_work = reinterpret_cast<Work*>(bars + 40);          // [2]
+  uint4* s_asked = reinterpret_cast<uint4*>(bars + 44);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 46);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -136,8 +166,12 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       mbar_init(&p_full[2 * i], 4);
       mbar_init(&p_full[2 * i + 1], 4);
       mbar_init(&o_done[i], 1);
+      mbar_init(&q_empty[i], 1);
+      mbar_init(&w_full[i], 1);
+      mbar_init(&w_empty[i], 1 + 4 * NT);
     }
     mbar_init(drain, 1);
+    mbar_init(asked, 1);
     *abort_flag = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tmQ);
@@ -145,12 +179,17 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     tma_prefetch_desc(&tmV);
   }
   pdl_enter();
-  // the blocks of a row tile are its KV heads; a sequence's last rows, which see most keys, come first
-  const int hk = blockIdx.x % a.n_kv;
-  int within;
+  // the blocks of a pair of row tiles are its KV heads; a sequence's last rows, which see most keys, come first
   auto pairs = [&](int b) { return (static_cast<int64_t>(seq_rows(a.cu, b, a.total, a.max_rows).n) + NT * a.tq - 1) / (NT * a.tq); };
-  const int b = find_tile(a.batch, blockIdx.x / a.n_kv, pairs, &within);
-  if (b < 0) return;                                          // uniform; nothing allocated or in flight
+  auto find = [&](int block) {
+    int within;
+    const int b = find_tile(a.batch, block / a.n_kv, pairs, &within);
+    if (b < 0) return Work{0, 0, 0, 0};
+    const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
+    return Work{block % a.n_kv, rows.first, rows.n, (static_cast<int>(pairs(b)) - 1 - within) * NT * a.tq};
+  };
+  const Work first = find(blockIdx.x);
+  if (first.n == 0) return;                                   // uniform; nothing allocated or in flight
   if (warp == 1) {
     tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
@@ -159,61 +198,86 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(static_cast<int>(*tmem_slot));
-  const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
-  const int tok0 = (static_cast<int>(pairs(b)) - 1 - within) * NT * a.tq;   // first row of the CTA's tiles
   // the key tiles of tile h, whose rows of the sequence are tok0 + h tq and on: first and end
-  auto range = [&](int h) {
-    const int lo = tok0 + h * a.tq, hi = min(lo + a.tq, rows.n) - 1;
-    if (lo >= rows.n) return make_int2(0, 0);
-    const int end = a.causal ? hi + 1 : rows.n;
+  auto range = [&](const Work& w, int h) {
+    const int lo = w.tok0 + h * a.tq, hi = min(lo + a.tq, w.n) - 1;
+    if (h >= NT || lo >= w.n) return make_int2(0, 0);
+    const int end = a.causal ? hi + 1 : w.n;
     const int begin = a.window > 0 ? max(0, lo - a.window + 1) : 0;
     return make_int2(begin / TK, (end + TK - 1) / TK);
   };
-  const int2 rA = uniform(range(0)), rB = NT == 2 ? uniform(range(1)) : make_int2(0, 0);
   // the keys that every row of tile h sees: [x, y); a key tile that is not inside them is cut by the mask
-  auto common = [&](int h) {
-    const int lo = tok0 + h * a.tq, hi = min(lo + a.tq, rows.n) - 1;
-    return make_int2(a.window > 0 ? hi - a.window + 1 : 0, a.causal ? lo + 1 : rows.n);
+  auto common = [&](const Work& w, int h) {
+    const int lo = w.tok0 + h * a.tq, hi = min(lo + a.tq, w.n) - 1;
+    return make_int2(a.window > 0 ? hi - a.window + 1 : 0, a.causal ? lo + 1 : w.n);
   };
   auto partial = [](int2 c, int j) { return (j + 1) * TK > c.y || j * TK < c.x; };
   // whether tile h keeps P in two terms in cut key tiles: a causal row of it sees fewer than 256 keys; without the causal
   // rule only a sequence's end and a window's edge cut
-  auto few = [&](int h) {
-    const int seen = tok0 + h * a.tq + 1;
+  auto few = [&](const Work& w, int h) {
+    const int seen = w.tok0 + h * a.tq + 1;
     return !a.causal || (a.window > 0 ? min(seen, a.window) : seen) < 256;
   };
-  const bool two = NT == 2 && rB.y > 0;
-  const int j0 = rA.x, j1 = two ? rB.y : rA.y, n_keys = uniform(rows.n);   // A's keys begin and end no later than B's
 
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     // --------------------------------------------------------------- producer
-    if (lane == 0) {
-      int g = 0;
-      bool ok = true;
-      for (int h = 0; h < (two ? 2 : 1); ++h) {               // rows behind the sequence's end are other rows, unused
-        mbar_arrive_expect_tx(&q_full[h], HD / 64 * a.rows * 128);
-        for (int s = 0; s < HD / 64; ++s)
-          tma_load_3d(sQ + h * C::TILE_BYTES + s * 16384, &tmQ, &q_full[h], 64 * s, hk * a.group, rows.first + tok0 + h * a.tq);
-      }
-      for (int j = j0; ok && j < j1; ++j)
-        for (int m = 0; m < 2; ++m, ++g) {
-          const int sl = g % NS;
-          if (!mbar_wait_bounded(&empty[sl], ((g / NS) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
-          mbar_arrive_expect_tx(&full[sl], C::TILE_BYTES);
+    // Also finds the pairs: the block's own first, then those of blocks that have not started, so that the loads and first
+    // scores of a pair hide behind the end of the one before it and all CTAs end together.
+    Work w = first;
+    int t = 0, g = 0, qn[2] = {0, 0};                         // pairs; loads into the ring and of each Q (lane 0)
+    bool ok = true, asking = false;
+    volatile int never = 0;
+    for (;; ++t) {
+      if (!warp_wait_bounded(&w_empty[t & 1], ((t >> 1) & 1) ^ 1, abort_flag, nullptr)) break;
+      if (lane == 0) s_work[t & 1] = w;
+      warp_arrive(&w_full[t & 1]);
+      if (w.n == 0) break;
+      const int2 rA = range(w, 0), rB = range(w, 1);
+      const bool two = rB.y > 0;
+      if (lane == 0) {
+        for (int h = 0; ok && h < (two ? 2 : 1); ++h) {       // rows behind the sequence's end are other rows, unused
+          ok = mbar_wait_bounded(&q_empty[h], (qn[h] & 1) ^ 1, abort_flag, nullptr);
+          if (!ok) break;
+          ++qn[h];
+          mbar_arrive_expect_tx(&q_full[h], HD / 64 * a.rows * 128);
           for (int s = 0; s < HD / 64; ++s)
-            tma_load_3d(sKV + sl * C::TILE_BYTES + s * 16384, m ? &tmV : &tmK, &full[sl], 64 * s, hk, rows.first + j * TK);
+            tma_load_3d(sQ + h * C::TILE_BYTES + s * 16384, &tmQ, &q_full[h], 64 * s, w.hk * a.group, w.first + w.tok0 + h * a.tq);
         }
-      // every copy started here has landed before the CTA may exit
-      volatile int never = 0;
-      for (int h = 0; h < (two ? 2 : 1); ++h) mbar_wait_bounded(&q_full[h], 0, &never, nullptr);
+        for (int j = rA.x; ok && j < (two ? rB.y : rA.y); ++j)
+          for (int m = 0; m < 2; ++m, ++g) {
+            const int sl = g % NS;
+            if (!mbar_wait_bounded(&empty[sl], ((g / NS) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
+            mbar_arrive_expect_tx(&full[sl], C::TILE_BYTES);
+            for (int s = 0; s < HD / 64; ++s)
+              tma_load_3d(sKV + sl * C::TILE_BYTES + s * 16384, m ? &tmV : &tmK, &full[sl], 64 * s, w.hk, w.first + j * TK);
+          }
+      }
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      if (!ok) break;
+      // two key tiles before the pair's end: late, so that no CTA keeps a pair waiting that another one could begin
+      if (lane == 0) {
+        mbar_arrive_expect_tx(asked, 16);
+        ask_block(s_asked, asked);
+      }
+      asking = true;
+      if (!warp_wait_bounded(asked, t & 1, abort_flag, nullptr)) break;
+      asking = false;
+      const int block = next_block(s_asked);
+      fence_proxy_async_smem();                               // the next answer is written there
+      __syncwarp();
+      w = block < 0 ? Work{0, 0, 0, 0} : find(block);         // (blocks past the last pair are the grid's last)
+    }
+    // every copy started here has landed before the CTA may exit
+    if (lane == 0) {
+      if (asking) mbar_wait_bounded(asked, t & 1, &never, nullptr);
+      for (int h = 0; h < 2; ++h)
+        if (qn[h] > 0) mbar_wait_bounded(&q_full[h], (qn[h] - 1) & 1, &never, nullptr);
       for (int i = max(0, g - NS); i < g; ++i) mbar_wait_bounded(&full[i % NS], (i / NS) & 1, &never, nullptr);
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
     constexpr uint32_t idesc_s = idesc_bf16_f32(TQ, TK), idesc_o = idesc_bf16_f32(TQ, HD) | 1u << 16;   // V: MN-major
-    const int2 cA = uniform(common(0)), cB = uniform(common(1));
-    const bool fA = uniform(few(0)), fB = uniform(few(1));
     struct Slot {                                             // a place of the ring and the parity of its phase
       uint32_t at, parity;
     };
@@ -222,11 +286,12 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, nullptr);
     };
     const uint32_t q_lo = desc_k(smem_u32(sQ)), kv_lo = smem_u32(sKV);
-    auto scores = [&](int h, Slot s) {                        // S_h = Q_h K^T
+    auto scores = [&](int h, Slot s, bool last) {             // S_h = Q_h K^T, the pair's last ones release Q_h
       const uint32_t q0 = q_lo + h * (C::TILE_BYTES >> 4), k0 = desc_k(kv_lo + s.at * C::TILE_BYTES);
 #pragma unroll
       for (int c = 0; c < HD / 64; ++c) umma4_ss(tmem + C::S_COL + h * TK, q0 + c * 1024, k0 + c * 1024, idesc_s, c);
       umma_commit(&s_full[h]);
+      if (last) umma_commit(&q_empty[h]);
     };
     auto values = [&](int h, Slot s, int n, bool first, bool split) {   // O_h += P_h V, the tile's n-th P
       const uint32_t vd = desc_mn(kv_lo + s.at * C::TILE_BYTES), o = tmem + C::O_COL + h * HD, p = tmem + C::S_COL + h * TK;
@@ -242,43 +307,64 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       }
       return true;
     };
-    Slot sk{0, 0};                                            // K(j0)
-    bool ok = wait(&q_full[0], 0) && (!two || wait(&q_full[1], 0)) && wait(&full[0], 0);
-    if (ok) {
+    Slot sk{0, 0};                                            // K(j0) of the pair
+    int nA = 0, nB = 0, uB = 0;                               // P's of tiles 0 and 1 ahead of the pair, pairs with a tile 1
+    for (int t = 0;; ++t) {
+      if (!wait(&w_full[t & 1], (t >> 1) & 1)) break;
+      const Work w = s_work[t & 1];
+      warp_arrive(&w_empty[t & 1]);
+      const int n_keys = uniform(w.n);
+      if (n_keys == 0) break;
+      const int2 rA = uniform(range(w, 0)), rB = uniform(range(w, 1)), cA = uniform(common(w, 0)), cB = uniform(common(w, 1));
+      const bool fA = uniform(few(w, 0)), fB = uniform(few(w, 1)), two = rB.y > 0;
+      const int j0 = rA.x, j1 = two ? rB.y : rA.y;            // A's keys begin and end no later than B's
+      bool ok = wait(&q_full[0], t & 1) && wait(&full[sk.at], sk.parity);
+      if (!ok) break;
       tc_fence_after();
-      scores(0, sk);
-      if (two && rB.x == j0) scores(1, sk);
-      umma_commit(&empty[0]);
-    }
-    for (int j = j0; ok && j < j1; ++j) {
-      const Slot sv = after(sk);                              // V(j), then K(j + 1)
-      sk = after(sv);
-      if (!wait(&full[sv.at], sv.parity) || (j + 1 < j1 && !wait(&full[sk.at], sk.parity))) break;
-      const int valid = n_keys - j * TK;
-      if (valid < TK) {                                       // the lines of V behind the sequence's end
-        uint8_t* sV = sKV + sv.at * C::TILE_BYTES;
-        for (int i = lane; i < (TK - valid) * 8; i += 32)
-#pragma unroll
-          for (int s = 0; s < HD / 64; ++s) *reinterpret_cast<uint4*>(sV + s * 16384 + valid * 128 + i * 16) = make_uint4(0, 0, 0, 0);
-        fence_proxy_async_smem();
-        __syncwarp();
-      }
-      tc_fence_after();
-      if (j < rA.y) {
-        if (!values(0, sv, j - j0, j == j0, fA && partial(cA, j))) break;
-        if (j == rA.y - 1) umma_commit(&o_done[0]);
-      }
-      if (!two) umma_commit(&empty[sv.at]);
-      if (j + 1 < rA.y) scores(0, sk);
+      scores(0, sk, j0 + 1 == rA.y);
       if (two) {
-        if (j >= rB.x) {                                      // (j < rB.y: B's keys end last)
-          if (!values(1, sv, j - rB.x, j == rB.x, fB && partial(cB, j))) break;
-          if (j == rB.y - 1) umma_commit(&o_done[1]);
-        }
-        umma_commit(&empty[sv.at]);
-        if (j + 1 >= rB.x && j + 1 < rB.y) scores(1, sk);
+        if (!wait(&q_full[1], uB & 1)) break;
+        ++uB;
+        tc_fence_after();
+        if (rB.x == j0) scores(1, sk, j0 + 1 == rB.y);
       }
-      if (j + 1 < j1) umma_commit(&empty[sk.at]);
+      umma_commit(&empty[sk.at]);
+      for (int j = j0; j < j1; ++j) {
+        const Slot sv = after(sk);                            // V(j), then K(j + 1)
+        sk = after(sv);
+        ok = wait(&full[sv.at], sv.parity) && (j + 1 >= j1 || wait(&full[sk.at], sk.parity));
+        if (!ok) break;
+        const int valid = n_keys - j * TK;
+        if (valid < TK) {                                     // the lines of V behind the sequence's end
+          uint8_t* sV = sKV + sv.at * C::TILE_BYTES;
+          for (int i = lane; i < (TK - valid) * 8; i += 32)
+#pragma unroll
+            for (int s = 0; s < HD / 64; ++s) *reinterpret_cast<uint4*>(sV + s * 16384 + valid * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+        tc_fence_after();
+        if (j < rA.y) {
+          ok = values(0, sv, nA + j - j0, j == j0, fA && partial(cA, j));
+          if (!ok) break;
+          if (j == rA.y - 1) umma_commit(&o_done[0]);
+        }
+        if (!two) umma_commit(&empty[sv.at]);
+        if (j + 1 < rA.y) scores(0, sk, j + 2 == rA.y);
+        if (two) {
+          if (j >= rB.x) {                                    // (j < rB.y: B's keys end last)
+            ok = values(1, sv, nB + j - rB.x, j == rB.x, fB && partial(cB, j));
+            if (!ok) break;
+            if (j == rB.y - 1) umma_commit(&o_done[1]);
+          }
+          umma_commit(&empty[sv.at]);
+          if (j + 1 >= rB.x && j + 1 < rB.y) scores(1, sk, j + 2 == rB.y);
+        }
+        if (j + 1 < j1) umma_commit(&empty[sk.at]);
+      }
+      if (!ok) break;
+      nA += rA.y - rA.x;
+      nB += rB.y - rB.x;
     }
     umma_commit(drain);
     volatile int never = 0;
@@ -288,124 +374,133 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS));
     const int h = (warp >> 2) - 1, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
-    const int2 r = h ? rB : rA;
-    const int in_tile = static_cast<int>(row * a.group_inv >> 16), tok = tok0 + h * a.tq + in_tile;
-    const bool v_ok = row < a.rows && tok < rows.n;
-    const int pos = v_ok ? tok : 0, head = hk * a.group + (v_ok ? row - in_tile * a.group : 0);
+    const int in_tile = static_cast<int>(row * a.group_inv >> 16);
     const uint32_t t_s = tmem + lane_off + C::S_COL + h * TK, t_o = tmem + lane_off + C::O_COL + h * HD;
     const uint64_t sc2 = f2_pack(a.scale_log2, a.scale_log2);
-    const int see_hi = a.causal && v_ok ? pos + 1 : rows.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
-    // O of a row is scaled by `factor` (and its sum): the tiles before this one are complete, their PV was issued ahead
-    // of this tile's S
-    float m_ref = -INFINITY, l_run = 0.0f;
-    auto rescale = [&](float factor) {
+    uint8_t* stage = sO + h * C::STAGE_BYTES;
+    int n = 0, used = 0;                                      // scores so far, pairs with this tile
+    for (int t = 0;; ++t) {
+      bool ok = warp_wait_bounded(&w_full[t & 1], (t >> 1) & 1, abort_flag, nullptr);
+      if (vote_group<128>(1 + h, !ok)) break;                   // the four warps of a tile leave together
+      const Work w = s_work[t & 1];
+      warp_arrive(&w_empty[t & 1]);
+      if (w.n == 0) break;
+      const int2 r = range(w, h);
+      if (r.y == 0) continue;
+      const int tok = w.tok0 + h * a.tq + in_tile;
+      const bool v_ok = row < a.rows && tok < w.n;
+      const int pos = v_ok ? tok : 0;
+      const int see_hi = a.causal && v_ok ? pos + 1 : w.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
+      // O of a row is scaled by `factor` (and its sum): the tiles before this one are complete, their PV was issued ahead
+      // of this tile's S
+      float m_ref = -INFINITY, l_run = 0.0f;
+      auto rescale = [&](float factor) {
 #pragma unroll
-      for (int c = 0; c < HD / 32; ++c) {
-        uint32_t ro[32];
-        tmem_ld32_nowait(t_o + 32 * c, ro);
-        tmem_wait_ld(ro);
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t ro[32];
+          tmem_ld32_nowait(t_o + 32 * c, ro);
+          tmem_wait_ld(ro);
 #pragma unroll
-        for (int k = 0; k < 32; ++k) ro[k] = __float_as_uint(__uint_as_float(ro[k]) * factor);
-        tmem_st32(t_o + 32 * c, ro);
-      }
-      l_run *= factor;
-    };
-    const int2 all = common(h);
-    const bool few_keys = few(h);
-    bool ok = true;
-    for (int j = r.x; j < r.y; ++j) {
-      if (!warp_wait_bounded(&s_full[h], (j - r.x) & 1, abort_flag, nullptr)) { ok = false; break; }
-      tc_fence_after();
-      // the row's scores stay in registers: P is written over them in TMEM
-      uint32_t s[4][32], pk[16];
-      tmem_ld32_nowait(t_s, s[0]);
-      tmem_ld32_nowait(t_s + 32, s[1]);
-      tmem_wait_ld(s[0]);
-      tmem_bind(s[1]);
-      tmem_ld32_nowait(t_s + 64, s[2]);
-      tmem_ld32_nowait(t_s + 96, s[3]);
-      uint64_t ps2[2] = {0, 0};
-      if (partial(all, j)) {
-        const int lim = see_hi - j * TK, lo = see_lo - j * TK;   // visible columns of this tile: [lo, lim)
-        float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        max64<true>(s[0], s[1], lo, lim, mxa);
-        tmem_wait_ld(s[2]);
-        tmem_bind(s[3]);
-        max64<true>(s[2], s[3], lo - 64, lim - 64, mxa);
-        const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
-        float factor = 1.0f;
-        if (m_ref == -INFINITY) {
-          m_ref = m_tile;                                     // every earlier exponential was 0
-        } else if (m_tile > m_ref + 8.0f) {
-          factor = ex2_approx(m_ref - m_tile);
-          m_ref = m_tile;
+          for (int k = 0; k < 32; ++k) ro[k] = __float_as_uint(__uint_as_float(ro[k]) * factor);
+          tmem_st32(t_o + 32 * c, ro);
         }
-        if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
-        const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
-        if (few_keys) {
-          uint32_t rest[64];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            exp32_masked<true>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
-            tmem_st16(t_s + 16 * c, pk);
+        l_run *= factor;
+      };
+      const int2 all = common(w, h);
+      const bool few_keys = few(w, h);
+      for (int j = r.x; j < r.y; ++j, ++n) {
+        if (!warp_wait_bounded(&s_full[h], n & 1, abort_flag, nullptr)) { ok = false; break; }
+        tc_fence_after();
+        // the row's scores stay in registers: P is written over them in TMEM
+        uint32_t s[4][32], pk[16];
+        tmem_ld32_nowait(t_s, s[0]);
+        tmem_ld32_nowait(t_s + 32, s[1]);
+        tmem_wait_ld(s[0]);
+        tmem_bind(s[1]);
+        tmem_ld32_nowait(t_s + 64, s[2]);
+        tmem_ld32_nowait(t_s + 96, s[3]);
+        uint64_t ps2[2] = {0, 0};
+        if (partial(all, j)) {
+          const int lim = see_hi - j * TK, lo = see_lo - j * TK;   // visible columns of this tile: [lo, lim)
+          float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          max64<true>(s[0], s[1], lo, lim, mxa);
+          tmem_wait_ld(s[2]);
+          tmem_bind(s[3]);
+          max64<true>(s[2], s[3], lo - 64, lim - 64, mxa);
+          const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
+          float factor = 1.0f;
+          if (m_ref == -INFINITY) {
+            m_ref = m_tile;                                     // every earlier exponential was 0
+          } else if (m_tile > m_ref + 8.0f) {
+            factor = ex2_approx(m_ref - m_tile);
+            m_ref = m_tile;
           }
+          if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
+          const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
+          if (few_keys) {
+            uint32_t rest[64];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 4; ++c) {
+              exp32_masked<true>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
+              tmem_st16(t_s + 16 * c, pk);
+            }
 #pragma unroll
-            for (int k = 0; k < 16; ++k) pk[k] = rest[16 * c + k];
-            tmem_st16(t_s + TK / 2 + 16 * c, pk);
+            for (int c = 0; c < 4; ++c) {
+#pragma unroll
+              for (int k = 0; k < 16; ++k) pk[k] = rest[16 * c + k];
+              tmem_st16(t_s + TK / 2 + 16 * c, pk);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              exp32_masked<false>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, nullptr);
+              tmem_st16(t_s + 16 * c, pk);
+            }
           }
         } else {
+          float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          max64<false>(s[0], s[1], 0, 64, mxa);
+          tmem_wait_ld(s[2]);
+          tmem_bind(s[3]);
+          max64<false>(s[2], s[3], 0, 64, mxa);
+          const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
+          float factor = 1.0f;
+          if (m_ref == -INFINITY) {
+            m_ref = m_tile;
+          } else if (m_tile > m_ref + 8.0f) {
+            factor = ex2_approx(m_ref - m_tile);
+            m_ref = m_tile;
+          }
+          if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
+          const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            exp32_masked<false>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, nullptr);
+            exp32_pack(s[c], sc2, negm2, ps2, pk);
             tmem_st16(t_s + 16 * c, pk);
+            if (c == 1) {                                       // P V of the first 64 keys may start
+              tmem_wait_st();
+              tc_fence_before();
+              warp_arrive(&p_full[2 * h]);
+            }
           }
         }
-      } else {
-        float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        max64<false>(s[0], s[1], 0, 64, mxa);
-        tmem_wait_ld(s[2]);
-        tmem_bind(s[3]);
-        max64<false>(s[2], s[3], 0, 64, mxa);
-        const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
-        float factor = 1.0f;
-        if (m_ref == -INFINITY) {
-          m_ref = m_tile;
-        } else if (m_tile > m_ref + 8.0f) {
-          factor = ex2_approx(m_ref - m_tile);
-          m_ref = m_tile;
-        }
-        if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
-        const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          exp32_pack(s[c], sc2, negm2, ps2, pk);
-          tmem_st16(t_s + 16 * c, pk);
-          if (c == 1) {                                       // P V of the first 64 keys may start
-            tmem_wait_st();
-            tc_fence_before();
-            warp_arrive(&p_full[2 * h]);
-          }
-        }
+        float a0, a1, b0, b1;
+        f2_unpack(ps2[0], a0, a1);
+        f2_unpack(ps2[1], b0, b1);
+        l_run += (a0 + a1) + (b0 + b1);
+        tmem_wait_st();
+        tc_fence_before();
+        if (partial(all, j)) warp_arrive(&p_full[2 * h]);
+        warp_arrive(&p_full[2 * h + 1]);
       }
-      float a0, a1, b0, b1;
-      f2_unpack(ps2[0], a0, a1);
-      f2_unpack(ps2[1], b0, b1);
-      l_run += (a0 + a1) + (b0 + b1);
-      tmem_wait_st();
-      tc_fence_before();
-      if (partial(all, j)) warp_arrive(&p_full[2 * h]);
-      warp_arrive(&p_full[2 * h + 1]);
-    }
-    if (ok && r.y > 0 && warp_wait_bounded(&o_done[h], 0, abort_flag, nullptr)) {
-      // O leaves through Q's shared memory, which no MMA reads any more.  A tile of whole rows of the sequence is one
-      // tensor store; in the sequence's last tile each row has a line of its own (144 bytes apart) and a copy of its own
+      ok = ok && warp_wait_bounded(&o_done[h], used & 1, abort_flag, nullptr);
+      if (vote_group<128>(1 + h, !ok)) break;
+      ++used;
+      // O leaves 64 dims at a time.  A tile of whole rows of the sequence is one tensor store, else its rows are copied
       tc_fence_after();
       const float inv = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-      const bool full_tile = tok0 + (h + 1) * a.tq <= rows.n;
-      bf16* orow = a.o + (rows.first + pos) * a.ldo + static_cast<int64_t>(head) * HD;
-      uint8_t* tile = sQ + h * C::TILE_BYTES;
+      const int tile_tok = w.tok0 + h * a.tq;
+      const bool full_tile = tile_tok + a.tq <= w.n;
 #pragma unroll 1
       for (int c = 0; c < HD / 64; ++c) {
         uint32_t ro[32], rp[32];
@@ -413,36 +508,41 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         tmem_ld32_nowait(t_o + 64 * c + 32, rp);
         tmem_wait_ld(ro);
         tmem_bind(rp);
-        if (c > 0 && !full_tile) bulk_wait_read0();
-        uint8_t* line = full_tile ? tile + c * 16384 + row * 128 : tile + row * (HD == 128 ? 144 : 128);
-        const int swap = full_tile ? row & 7 : 0;
+        if (row == 0) bulk_wait_read0();
+        bar_group<128>(1 + h);                                  // the memory is free again
 #pragma unroll
         for (int k = 0; k < 64; k += 8) {
-          uint32_t w[4];
+          uint32_t v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float x = __uint_as_float(k < 32 ? ro[(k + 2 * e) & 31] : rp[(k + 2 * e) & 31]);
             const float y = __uint_as_float(k < 32 ? ro[(k + 2 * e + 1) & 31] : rp[(k + 2 * e + 1) & 31]);
-            __nv_bfloat162 t = __floats2bfloat162_rn(x * inv, y * inv);
-            w[e] = *reinterpret_cast<uint32_t*>(&t);
+            __nv_bfloat162 b = __floats2bfloat162_rn(x * inv, y * inv);
+            v[e] = *reinterpret_cast<uint32_t*>(&b);
           }
-          *reinterpret_cast<uint4*>(line + (((k >> 3) ^ swap) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(stage + row * 128 + (((k >> 3) ^ (row & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-        fence_proxy_async_smem();
-        if (!full_tile) {
-          if (v_ok) bulk_store(orow + 64 * c, line, 128);
-          bulk_commit();
+        if (full_tile) {
+          fence_proxy_async_smem();
+          bar_group<128>(1 + h);
+          if (row == 0) {
+            tma_store_3d(&tmO, stage, 64 * c, w.hk * a.group, w.first + tile_tok);
+            bulk_commit();
+          }
+        } else {
+          __syncwarp();                                         // a warp copies its own 32 rows, 8 lanes each
+#pragma unroll 1
+          for (int i = 0; i < 8; ++i) {
+            const int rr = quad * 32 + 4 * i + (lane >> 3), it = static_cast<int>(rr * a.group_inv >> 16);
+            if (rr < a.rows && tile_tok + it < w.n)
+              *reinterpret_cast<uint4*>(a.o + (w.first + tile_tok + it) * a.ldo + static_cast<int64_t>(w.hk * a.group + rr - it * a.group) * HD +
+                                        64 * c + 8 * (lane & 7)) =
+                  *reinterpret_cast<const uint4*>(stage + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4));
+          }
         }
       }
-      if (full_tile) {
-        asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + h) : "memory");
-        if (row == 0) {
-          for (int s = 0; s < HD / 64; ++s) tma_store_3d(&tmO, tile + s * 16384, 64 * s, hk * a.group, rows.first + tok0 + h * a.tq);
-          bulk_commit();
-        }
-      }
-      bulk_wait0();
     }
+    if (row == 0) bulk_wait0();
   }
   tc_fence_before();
   __syncthreads();

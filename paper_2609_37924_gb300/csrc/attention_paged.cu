@@ -304,24 +304,6 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
                : "memory");
 }
-// barrier `id` of T threads, and its vote
-template <int T>
-__device__ __forceinline__ void bar_group(int id) {
-  asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "n"(T) : "memory");
-}
-template <int T>
-__device__ __forceinline__ bool vote_group(int id, bool p) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred a, b;\n\t"
-      "setp.ne.u32 a, %1, 0;\n\t"
-      "barrier.cta.red.or.pred b, %3, %2, a;\n\t"
-      "selp.u32 %0, 1, 0, b;\n\t}"
-      : "=r"(r)
-      : "r"(static_cast<uint32_t>(p)), "n"(T), "r"(id)
-      : "memory");
-  return r != 0;
-}
 __device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));

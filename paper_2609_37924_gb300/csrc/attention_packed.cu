@@ -28,7 +28,8 @@
 // 8111-token prompt of 32 / 16 heads (449 us with its neighbours; 461 where
 // each block starts and ends by itself, and a window of 1024 over 8900 rows 133
 // instead of 157); prompts of a few hundred tokens are bound by the latency of
-// cut tiles (24 prompts, 6400 tokens, 16 / 8 heads: 43 us).
+// cut tiles (24 prompts, 6400 tokens, 16 / 8 heads: 36 us; 43 with their code
+// unrolled over the 128 columns).
 #include "ragged.cuh"
 #include "serve.h"
 #include "softmax_rows.cuh"
@@ -104,23 +105,25 @@ __device__ __forceinline__ void exp32_pack(const uint32_t (&r)[32], uint64_t sc2
     pk[j] = *reinterpret_cast<uint32_t*>(&t);
   }
 }
-// The same where columns outside lo .. lim - 1 are hidden (P = 0); REST: with the remainders P - bf16(P) as bf16 pairs.
-template <bool REST>
-__device__ __forceinline__ void exp32_masked(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, int lo, int lim,
-                                             uint64_t (&ps2)[2], uint32_t (&pk)[16], uint32_t* rest) {
+// Columns lo .. lim - 1 of 32, a bit each
+__device__ __forceinline__ uint32_t columns(int lo, int lim) {
+  const uint32_t below = lim >= 32 ? 0xffffffffu : lim <= 0 ? 0u : (1u << lim) - 1u;
+  return below & ~(lo >= 32 ? 0xffffffffu : lo <= 0 ? 0u : (1u << lo) - 1u);
+}
+// exp32_pack() where only the columns of `see` are visible (else P = 0), with the remainders P - bf16(P) as bf16 pairs.
+__device__ __forceinline__ void exp32_masked(const uint32_t (&r)[32], uint64_t sc2, uint64_t negm2, uint32_t see, uint64_t (&ps2)[2],
+                                             uint32_t (&pk)[16], uint32_t (&rest)[16]) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     float x0, x1;
     f2_unpack(f2_fma(f2_pack(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), sc2, negm2), x0, x1);
-    const float p0 = 2 * j < lim && 2 * j >= lo ? ex2_approx(x0) : 0.0f;
-    const float p1 = 2 * j + 1 < lim && 2 * j + 1 >= lo ? ex2_approx(x1) : 0.0f;
+    const float p0 = see >> 2 * j & 1 ? ex2_approx(x0) : 0.0f;
+    const float p1 = see >> (2 * j + 1) & 1 ? ex2_approx(x1) : 0.0f;
     ps2[j & 1] = f2_add(ps2[j & 1], f2_pack(p0, p1));
     __nv_bfloat162 t = __floats2bfloat162_rn(p0, p1);
     pk[j] = *reinterpret_cast<uint32_t*>(&t);
-    if (REST) {
-      t = __floats2bfloat162_rn(p0 - __uint_as_float(pk[j] << 16), p1 - __uint_as_float(pk[j] & 0xffff0000u));
-      rest[j] = *reinterpret_cast<uint32_t*>(&t);
-    }
+    t = __floats2bfloat162_rn(p0 - __uint_as_float(pk[j] << 16), p1 - __uint_as_float(pk[j] & 0xffff0000u));
+    rest[j] = *reinterpret_cast<uint32_t*>(&t);
   }
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
@@ -296,15 +299,17 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     auto values = [&](int h, Slot s, int n, bool first, bool split) {   // O_h += P_h V, the tile's n-th P
       const uint32_t vd = desc_mn(kv_lo + s.at * C::TILE_BYTES), o = tmem + C::O_COL + h * HD, p = tmem + C::S_COL + h * TK;
       if (!wait(&p_full[2 * h], n & 1)) return false;
+      if (split) {
+        if (!wait(&p_full[2 * h + 1], n & 1)) return false;
+        tc_fence_after();
+        for (int c = 0; c < 4; ++c) umma4_ts_two(o, p + 32 * c, vd + 256 * c, idesc_o, c > 0 || !first);
+        return true;
+      }
       tc_fence_after();
       umma4_ts_mn(o, p, vd, idesc_o, !first);
       if (!wait(&p_full[2 * h + 1], n & 1)) return false;
       tc_fence_after();
       umma4_ts_mn(o, p + 32, vd + 512, idesc_o, 1);
-      if (split) {
-        umma4_ts_mn(o, p + 64, vd, idesc_o, 1);
-        umma4_ts_mn(o, p + 96, vd + 512, idesc_o, 1);
-      }
       return true;
     };
     Slot sk{0, 0};                                            // K(j0) of the pair
@@ -390,7 +395,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       const int tok = w.tok0 + h * a.tq + in_tile;
       const bool v_ok = row < a.rows && tok < w.n;
       const int pos = v_ok ? tok : 0;
-      const int see_hi = a.causal && v_ok ? pos + 1 : w.n, see_lo = a.window > 0 && v_ok ? pos - a.window + 1 : 0;
+      const int see_hi = !v_ok ? 0 : a.causal ? pos + 1 : w.n, see_lo = a.window > 0 ? pos - a.window + 1 : 0;
       // O of a row is scaled by `factor` (and its sum): the tiles before this one are complete, their PV was issued ahead
       // of this tile's S
       float m_ref = -INFINITY, l_run = 0.0f;
@@ -411,68 +416,71 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       for (int j = r.x; j < r.y; ++j, ++n) {
         if (!warp_wait_bounded(&s_full[h], n & 1, abort_flag, nullptr)) { ok = false; break; }
         tc_fence_after();
-        // the row's scores stay in registers: P is written over them in TMEM
-        uint32_t s[4][32], pk[16];
-        tmem_ld32_nowait(t_s, s[0]);
-        tmem_ld32_nowait(t_s + 32, s[1]);
-        tmem_wait_ld(s[0]);
-        tmem_bind(s[1]);
-        tmem_ld32_nowait(t_s + 64, s[2]);
-        tmem_ld32_nowait(t_s + 96, s[3]);
         uint64_t ps2[2] = {0, 0};
-        if (partial(all, j)) {
-          const int lim = see_hi - j * TK, lo = see_lo - j * TK;   // visible columns of this tile: [lo, lim)
-          float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-          max64<true>(s[0], s[1], lo, lim, mxa);
-          tmem_wait_ld(s[2]);
-          tmem_bind(s[3]);
-          max64<true>(s[2], s[3], lo - 64, lim - 64, mxa);
-          const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
+        // the new reference, from the tile's largest score; O and the sum follow
+        auto refer = [&](float m_tile) {
           float factor = 1.0f;
           if (m_ref == -INFINITY) {
-            m_ref = m_tile;                                     // every earlier exponential was 0
+            m_ref = m_tile;                                   // every earlier exponential was 0
           } else if (m_tile > m_ref + 8.0f) {
             factor = ex2_approx(m_ref - m_tile);
             m_ref = m_tile;
           }
           if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
-          const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
-          if (few_keys) {
-            uint32_t rest[64];
+          return f2_pack(-m_ref, -m_ref);
+        };
+        if (partial(all, j)) {
+          // A cut tile: 32 columns at a time, twice (the maximum, the exponentials), and those that no row of the warp sees
+          // are left out.  Rolled, because it runs once or twice per tile of rows and would wait for its instructions.
+          // P goes over the scores that it was made from: two terms of 16 columns for 32, or one closed up.
+          const int lim = see_hi - j * TK, lo = see_lo - j * TK;   // visible columns of this tile: [lo, lim)
+          uint32_t s[32], pk[16], rest[16];
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t see = columns(lo - 32 * c, lim - 32 * c);
+            if (!__any_sync(0xffffffffu, see != 0)) continue;
+            tmem_ld32_nowait(t_s + 32 * c, s);
+            tmem_wait_ld(s);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              exp32_masked<true>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, rest + 16 * c);
-              tmem_st16(t_s + 16 * c, pk);
+            for (int k = 0; k < 32; k += 2)
+              top[(k >> 1) & 3] = fmax3(top[(k >> 1) & 3], see >> k & 1 ? __uint_as_float(s[k]) : -INFINITY,
+                                        see >> (k + 1) & 1 ? __uint_as_float(s[k + 1]) : -INFINITY);
+          }
+          const uint64_t negm2 = refer(fmax3(fmaxf(top[0], top[1]), top[2], top[3]) * a.scale_log2);
+#pragma unroll 1
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t see = columns(lo - 32 * c, lim - 32 * c);
+            if (__any_sync(0xffffffffu, see != 0)) {
+              tmem_ld32_nowait(t_s + 32 * c, s);
+              tmem_wait_ld(s);
+              exp32_masked(s, sc2, negm2, see, ps2, pk, rest);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 16; ++k) pk[k] = rest[k] = 0;
             }
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-#pragma unroll
-              for (int k = 0; k < 16; ++k) pk[k] = rest[16 * c + k];
-              tmem_st16(t_s + TK / 2 + 16 * c, pk);
-            }
-          } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              exp32_masked<false>(s[c], sc2, negm2, lo - 32 * c, lim - 32 * c, ps2, pk, nullptr);
+            if (few_keys) {
+              tmem_st16(t_s + 32 * c, pk);
+              tmem_st16(t_s + 32 * c + 16, rest);
+            } else {
               tmem_st16(t_s + 16 * c, pk);
             }
           }
         } else {
+          // the row's scores stay in registers: P is written over them in TMEM
+          uint32_t s[4][32], pk[16];
+          tmem_ld32_nowait(t_s, s[0]);
+          tmem_ld32_nowait(t_s + 32, s[1]);
+          tmem_wait_ld(s[0]);
+          tmem_bind(s[1]);
+          tmem_ld32_nowait(t_s + 64, s[2]);
+          tmem_ld32_nowait(t_s + 96, s[3]);
           float mxa[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
           max64<false>(s[0], s[1], 0, 64, mxa);
           tmem_wait_ld(s[2]);
           tmem_bind(s[3]);
           max64<false>(s[2], s[3], 0, 64, mxa);
-          const float m_tile = fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2;
-          float factor = 1.0f;
-          if (m_ref == -INFINITY) {
-            m_ref = m_tile;
-          } else if (m_tile > m_ref + 8.0f) {
-            factor = ex2_approx(m_ref - m_tile);
-            m_ref = m_tile;
-          }
-          if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
-          const uint64_t negm2 = f2_pack(-m_ref, -m_ref);
+          const uint64_t negm2 = refer(fmax3(fmaxf(mxa[0], mxa[1]), mxa[2], mxa[3]) * a.scale_log2);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             exp32_pack(s[c], sc2, negm2, ps2, pk);

@@ -55,6 +55,24 @@ __device__ __forceinline__ void umma4_ts_mn(uint32_t d, uint32_t a, uint32_t b, 
       : "memory");
 }
 
+// The same over 32 keys with P in two terms: 16 columns of the first, then 16 of the second
+__device__ __forceinline__ void umma4_ts_two(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p, e, t;\n\t.reg .b64 db, dc;\n\t.reg .b32 x, y;\n\t"
+      "elect.sync _|e, 0xffffffff;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.eq.b32 t, %5, %5;\n\t"
+      "add.u32 y, %2, 128;\n\tmov.b64 db, {%2, %5};\n\tmov.b64 dc, {y, %5};\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t"
+      "add.u32 x, %1, 8;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], dc, %3, t;\n\t"
+      "add.u32 x, %1, 16;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], db, %3, t;\n\t"
+      "add.u32 x, %1, 24;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [x], dc, %3, t;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHi)
+      : "memory");
+}
+
 // D = A B^T over STEPS x 32 dims of e4m3, A and B in shared memory, both K-major with rows of HD bytes; hi: the high
 // word of their descriptors (32 further dims: 32 bytes on)
 template <int STEPS>

@@ -5,8 +5,8 @@
 // walks the key tiles that they see, 128 keys each.  Two tiles both use a K or V
 // tile while it is in shared memory, and their softmaxes alternate with the
 // tensor pipe.  A CTA that is through takes the work of a block of the grid that
-// has not started (the hardware hands it out), so that the next Q, K and first
-// scores come while the last O leaves:
+// has not started (the hardware hands it out, longest work first), so that the
+// next Q, K and first scores come while the last O leaves:
 //   warp 0       finds the work and streams Q, K and V tiles with TMA, these
 //                into a ring of four slots;
 //   warp 1       O_A += P_A V(j), S_A = Q_A K(j+1)^T, then the same for B: one
@@ -28,8 +28,9 @@
 // 8111-token prompt of 32 / 16 heads (449 us with its neighbours; 461 where
 // each block starts and ends by itself, and a window of 1024 over 8900 rows 133
 // instead of 157); prompts of a few hundred tokens are bound by the latency of
-// cut tiles (24 prompts, 6400 tokens, 16 / 8 heads: 36 us; 43 with their code
-// unrolled over the 128 columns).
+// cut tiles and of the first pair, whose code and rows come from memory (24
+// prompts, 6400 tokens, 16 / 8 heads: 31 us; 43 with the code of cut tiles
+// unrolled over the 128 columns, 36 with the sequences' work in their order).
 #include "ragged.cuh"
 #include "serve.h"
 #include "softmax_rows.cuh"
@@ -182,14 +183,14 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     tma_prefetch_desc(&tmV);
   }
   pdl_enter();
-  // the blocks of a pair of row tiles are its KV heads; a sequence's last rows, which see most keys, come first
-  auto pairs = [&](int b) { return (static_cast<int64_t>(seq_rows(a.cu, b, a.total, a.max_rows).n) + NT * a.tq - 1) / (NT * a.tq); };
+  // the blocks of a pair of row tiles are its KV heads; the pairs that see most keys come first
   auto find = [&](int block) {
-    int within;
-    const int b = find_tile(a.batch, block / a.n_kv, pairs, &within);
+    int at;
+    const int b = find_largest(a.batch, block / a.n_kv,
+                               [&](int i) { return (seq_rows(a.cu, i, a.total, a.max_rows).n + NT * a.tq - 1) / (NT * a.tq); }, &at);
     if (b < 0) return Work{0, 0, 0, 0};
     const SeqRows rows = seq_rows(a.cu, b, a.total, a.max_rows);
-    return Work{block % a.n_kv, rows.first, rows.n, (static_cast<int>(pairs(b)) - 1 - within) * NT * a.tq};
+    return Work{block % a.n_kv, rows.first, rows.n, at * NT * a.tq};
   };
   const Work first = find(blockIdx.x);
   if (first.n == 0) return;                                   // uniform; nothing allocated or in flight
@@ -313,6 +314,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       return true;
     };
     Slot sk{0, 0};                                            // K(j0) of the pair
+    bool early = false;                                       // the pair's first scores of tile 0 are issued
     int nA = 0, nB = 0, uB = 0;                               // P's of tiles 0 and 1 ahead of the pair, pairs with a tile 1
     for (int t = 0;; ++t) {
       if (!wait(&w_full[t & 1], (t >> 1) & 1)) break;
@@ -323,10 +325,11 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       const int2 rA = uniform(range(w, 0)), rB = uniform(range(w, 1)), cA = uniform(common(w, 0)), cB = uniform(common(w, 1));
       const bool fA = uniform(few(w, 0)), fB = uniform(few(w, 1)), two = rB.y > 0;
       const int j0 = rA.x, j1 = two ? rB.y : rA.y;            // A's keys begin and end no later than B's
-      bool ok = wait(&q_full[0], t & 1) && wait(&full[sk.at], sk.parity);
+      bool ok = early || (wait(&q_full[0], t & 1) && wait(&full[sk.at], sk.parity));
       if (!ok) break;
       tc_fence_after();
-      scores(0, sk, j0 + 1 == rA.y);
+      if (!early) scores(0, sk, j0 + 1 == rA.y);
+      early = false;
       if (two) {
         if (!wait(&q_full[1], uB & 1)) break;
         ++uB;
@@ -357,6 +360,17 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         if (!two) umma_commit(&empty[sv.at]);
         if (j + 1 < rA.y) scores(0, sk, j + 2 == rA.y);
         if (two) {
+          if (j + 1 == j1) {                                  // tile 0 of the next pair, if its Q and K are here, ahead of tile 1's last P
+            const uint32_t u = t + 1;
+            const Slot next = after(sv);
+            early = __all_sync(0xffffffffu, mbar_test(&w_full[u & 1], (u >> 1) & 1) && s_work[u & 1].n > 0 &&
+                                                mbar_test(&q_full[0], u & 1) && mbar_test(&full[next.at], next.parity));
+            if (early) {
+              tc_fence_after();
+              const int2 r = uniform(range(s_work[u & 1], 0));
+              scores(0, next, r.x + 1 == r.y);
+            }
+          }
           if (j >= rB.x) {                                    // (j < rB.y: B's keys end last)
             ok = values(1, sv, nB + j - rB.x, j == rB.x, fB && partial(cB, j));
             if (!ok) break;

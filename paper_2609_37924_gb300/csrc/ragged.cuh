@@ -42,4 +42,35 @@ __device__ __forceinline__ int find_tile(int batch, int64_t tile, F&& tiles_of, 
   return -1;
 }
 
+// The same for tiles whose work grows with their index: 32 sequences at a time, their tiles in falling order of index (of
+// those with the same index, by sequence).  Warp-collective.
+template <class F>
+__device__ __forceinline__ int find_largest(int batch, int tile, F&& tiles_of, int* within) {
+  const int lane = threadIdx.x & 31;
+  for (int base = 0; base < batch; base += 32) {
+    const int n = base + lane < batch ? tiles_of(base + lane) : 0;
+    const int all = __reduce_add_sync(0xffffffffu, n);
+    if (tile >= all) {
+      tile -= all;
+      continue;
+    }
+    int lo = 0, hi = __reduce_max_sync(0xffffffffu, n), above = 0;   // tiles with an index >= lo: more than `tile`; >= hi: `above`
+    while (hi - lo > 1) {
+      const int mid = lo + (hi - lo) / 2, more = __reduce_add_sync(0xffffffffu, max(n - mid, 0));
+      if (more > tile) {
+        lo = mid;
+      } else {
+        hi = mid;
+        above = more;
+      }
+    }
+    const unsigned have = __ballot_sync(0xffffffffu, n > lo);
+    const bool mine = n > lo && __popc(have & ((1u << lane) - 1)) == tile - above;
+    *within = lo;
+    return base + __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+  }
+  *within = 0;
+  return -1;
+}
+
 }  // namespace tadm

@@ -52,7 +52,7 @@ bool heads_ok(int n_heads, int n_kv, int head_dim) {
 
 // query heads x rows of one sequence and KV head, and tiles of 16 of them over the call, are int32
 bool grid_ok(int batch, int total, int rows, int group) {
-  return static_cast<int64_t>(rows) * group <= INT32_MAX - 128 &&
+  return static_cast<int64_t>(rows) * group <= INT32_MAX - 512 &&
          static_cast<int64_t>(total) * group / 16 + batch <= INT32_MAX;
 }
 

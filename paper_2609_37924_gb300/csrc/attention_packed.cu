@@ -612,9 +612,10 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
 }  // namespace
 
 const char* attention_packed(const RaggedCall& c, cudaStream_t s) {
-  // Two tiles share K and V in one CTA per SM for heads of 128 (one 8192-token prompt, 32 / 16 heads: 383 us, with one
-  // tile and two CTAs per SM 431; 24 prompts of 512: 128 and 138).  Heads of 64 leave shared memory and tensor memory for
-  // two CTAs with longer rings, whose starts and ends overlap (12 prompts of 1024, 12 heads: 62 us, 68 with two tiles).
+  // Heads of 128: two tiles share K and V in one CTA per SM (one 8192-token prompt, 32 / 16 heads: 377 us; one tile and two
+  // CTAs per SM, whose rings then hold one K and one V, 734.  24 prompts of 512, 16 / 8 heads: 54 and 79).  Heads of 64
+  // leave shared memory and tensor memory for two CTAs with whole rings, whose starts and ends overlap (12 prompts of 1024,
+  // 12 heads: 48 us, 54 with two tiles; 64 of 64: 25 and 29; one of 8192, 32 / 16 heads: 341 and 331).
   return c.head_dim == 128 ? launch<128, 2>(c, s) : launch<64, 1>(c, s);
 }
 

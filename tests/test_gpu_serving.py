@@ -140,6 +140,31 @@ def test_packed_many_sequences(T):
             close(o[s], ref, absum, torch.bfloat16, float(v[s].abs().max()))
 
 
+@pytest.mark.parametrize("heads", [(16, 8, 128), (12, 12, 64), (15, 3, 128), (10, 2, 64)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 130), (False, 0)])
+def test_packed_more_work_than_blocks_run(T, heads, causal, window):
+    """More row tiles than the SMs take at a time, so that blocks go on with others' work, over more sequences than one warp
+    scans at a time; every call gives the same bits, also on two streams at once."""
+    Hq, Hkv, hd = heads
+    lens = [(37 * i * i + 5 * i) % 600 if i % 5 else (i * 13) % 3 for i in range(75)] + [1500, 1]
+    rows = sum(lens)
+    x = torch.randn((rows, Hq + 2 * Hkv, hd), generator=gen(rows + Hq), device="cuda").bfloat16()
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    outs = [torch.full((rows, Hq, hd), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(6)]
+    streams, cu = [torch.cuda.Stream() for _ in range(2)], i32(cum(lens))
+    torch.cuda.synchronize()
+    for i, o in enumerate(outs):
+        T.tadm_attention_packed(q, k, v, o, cu, max(lens), causal=causal, window=window, stream=streams[i % 2] if i > 1 else None)
+    torch.cuda.synchronize()
+    for o in outs[1:]:
+        assert torch.equal(o, outs[0])
+    for a, n in zip(cum(lens), lens):
+        if n:
+            s = slice(a, a + n)
+            ref, absum = attend64(q[s].double(), k[s].double(), v[s].double(), torch.arange(n, device="cuda"), causal, window)
+            close(outs[0][s], ref, absum, torch.bfloat16, float(v[s].abs().max()))
+
+
 # ------------------------------------------------------------------ the cache
 def e4m3_bytes(x):
     """Nearest e4m3 (ties to even) of float64 |x| <= 448, as bytes; NaN for what is not finite."""

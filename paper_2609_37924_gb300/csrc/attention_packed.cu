@@ -24,10 +24,10 @@
 // scores are masked, and those lines of V are zeroed in shared memory.
 //
 // Bound: the tensor pipe, 1024 cycles per 128 x 128 tile at hd 128 (the
-// exponentials take 512).  Measured: about 1450 per tile, 1.33 PFLOP/s over an
-// 8111-token prompt of 32 / 16 heads (449 us with its neighbours; 461 where
-// each block starts and ends by itself, and a window of 1024 over 8900 rows 133
-// instead of 157); prompts of a few hundred tokens are bound by the latency of
+// exponentials take 512).  Measured: about 1450 per tile, 1.34 PFLOP/s over an
+// 8111-token prompt of 32 / 16 heads (448 us with its neighbours; 461 where
+// each block starts and ends by itself, and a window of 1024 over 8900 rows 129
+// and 157; with 64-key tiles and two S per row tile 587 and 155); prompts of a few hundred tokens are bound by the latency of
 // cut tiles and of the first pair, whose code and rows come from memory (24
 // prompts, 6400 tokens, 16 / 8 heads: 31 us; 43 with the code of cut tiles
 // unrolled over the 128 columns, 36 with the sequences' work in their order).

@@ -36,7 +36,7 @@
 // Bound: the bytes of the cache.  Measured: 4 tokens over 386,544 cached ones (8
 // KV heads of 128) 135 us, 5.9 TB/s; with 64 virtual rows a tile takes 1.05 us
 // per SM for 0.73 us of bytes, paced by the softmax warps' chain of waits (8 x
-// 32 rows over 99,641 tokens, 16 KV heads: 97 us, 4.3 TB/s).  There, in the order
+// 32 rows over 99,641 tokens, 16 KV heads: 98 us, 4.2 TB/s).  There, in the order
 // of their making: K and V both widened to f16 157 us; K multiplied as it is
 // stored, 142 with Q in three terms and 121 in two; fewer instructions around
 // the items 109; 16 rows per softmax thread where 32 were 100.

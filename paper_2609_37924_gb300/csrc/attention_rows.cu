@@ -8,7 +8,10 @@
 // lane for P V.  Everything is fp32: scores, running maximum and sum (online
 // softmax), accumulators.  It serves fp32 rows, those of the small models, whose
 // calls are a launch (11 us with the host's part for a few hundred rows of 4
-// heads); long ones are bound by shared-memory reads.
+// heads).  Longer ones are bound by shared-memory reads and a tile's latency,
+// about 3 us; the next tile's loads wait in registers meanwhile, 16 bytes each
+// (a row over 600 tokens of the cache 36 us, 72 with loads of single elements
+// between the barriers; four prompts of 500: 54 and 70).
 #include <cuda_fp8.h>
 
 #include "ragged.cuh"
@@ -62,31 +65,67 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
     sQ[i] = v < n_virt ? a.q[(rows.first + v / group) * a.ldq + static_cast<int64_t>(hk * group + v % group) * HD + i % HD] : 0.0f;
   }
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, acc[2][PL] = {};
-  for (int k0 = k_begin / KT * KT; k0 < k_end; k0 += KT) {
-    __syncthreads();
+  // a thread's part of the next key tile waits in registers while this one is computed
+  constexpr int NF = PAGED ? HD / 64 : HD / 16;               // 16-byte loads per thread of K, of V
+  int4 rk[NF], rv[NF];
+  float ks = 0.0f, vs = 0.0f;
+  auto fetch = [&](int k0) {
     if (PAGED) {
       const int slot = k0 / KT;
       const int page = slot < a.ld_table ? a.table[static_cast<int64_t>(b) * a.ld_table + slot] : -1;
       const bool ok = page >= 0 && page < a.pages;
       const int64_t ph = static_cast<int64_t>(ok ? page : 0) * a.n_kv + hk;
-      const float ks = ok ? a.sk[ph] : 0.0f, vs = ok ? a.sv[ph] : 0.0f;
-      const uint8_t *pk = a.pk + ph * KT * HD, *pv = a.pv + ph * KT * HD;
-      auto dec = [](uint8_t x) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(x, __NV_E4M3))); };
-      for (int i = tid; i < KT * HD; i += NT) {
-        const int kr = i / HD, kc = i % HD, vt = i % KT, vd = i / KT;
-        sK[kr * LD + kc] = ok && k0 + kr < k_end ? dec(pk[i]) * ks : 0.0f;
-        // what no row of the tile sees may hold anything
-        sV[vt * LD + vd] = ok && k0 + vt >= k_begin && k0 + vt < k_end ? dec(pv[i]) * vs : 0.0f;
+      ks = ok ? a.sk[ph] : 0.0f, vs = ok ? a.sv[ph] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < NF; ++u) {
+        const int64_t at = ph * KT * HD + (u * NT + tid) * 16;
+        rk[u] = ok ? *reinterpret_cast<const int4*>(a.pk + at) : make_int4(0, 0, 0, 0);
+        rv[u] = ok ? *reinterpret_cast<const int4*>(a.pv + at) : make_int4(0, 0, 0, 0);
       }
     } else {
-      for (int i = tid; i < KT * HD; i += NT) {
-        const int r = i / HD, c = i % HD;
-        const int64_t row = rows.first + k0 + r;
-        sK[r * LD + c] = k0 + r < len ? a.k[row * a.ldk + static_cast<int64_t>(hk) * HD + c] : 0.0f;
-        sV[r * LD + c] = k0 + r < len ? a.v[row * a.ldv + static_cast<int64_t>(hk) * HD + c] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < NF; ++u) {
+        const int i = (u * NT + tid) * 4, r = i / HD;
+        const int64_t row = rows.first + k0 + r, c = static_cast<int64_t>(hk) * HD + i % HD;
+        const bool in = k0 + r < len;
+        rk[u] = in ? *reinterpret_cast<const int4*>(a.k + row * a.ldk + c) : make_int4(0, 0, 0, 0);
+        rv[u] = in ? *reinterpret_cast<const int4*>(a.v + row * a.ldv + c) : make_int4(0, 0, 0, 0);
       }
     }
+  };
+  auto stage = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < NF; ++u) {
+      if (PAGED) {
+        // K: 16 dims of a key, V: 16 keys of a dim; what no row of the tile sees may hold anything
+        const int i = (u * NT + tid) * 16, kr = i / HD, kc = i % HD, vt = i % KT, vd = i / KT;
+        const uint32_t wk[4] = {static_cast<uint32_t>(rk[u].x), static_cast<uint32_t>(rk[u].y), static_cast<uint32_t>(rk[u].z),
+                                static_cast<uint32_t>(rk[u].w)};
+        const uint32_t wv[4] = {static_cast<uint32_t>(rv[u].x), static_cast<uint32_t>(rv[u].y), static_cast<uint32_t>(rv[u].z),
+                                static_cast<uint32_t>(rv[u].w)};
+        auto dec = [](uint32_t w, int e) {
+          return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<uint8_t>(w >> (8 * (e & 3))), __NV_E4M3)));
+        };
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          sK[kr * LD + kc + e] = k0 + kr < k_end ? dec(wk[e >> 2], e) * ks : 0.0f;
+          const int key = k0 + vt + e;
+          sV[(vt + e) * LD + vd] = key >= k_begin && key < k_end ? dec(wv[e >> 2], e) * vs : 0.0f;
+        }
+      } else {
+        const int i = (u * NT + tid) * 4, at = i / HD * LD + i % HD;
+        *reinterpret_cast<int4*>(sK + at) = rk[u];
+        *reinterpret_cast<int4*>(sV + at) = rv[u];
+      }
+    }
+  };
+  if (k_begin < k_end) fetch(k_begin / KT * KT);
+  for (int k0 = k_begin / KT * KT; k0 < k_end; k0 += KT) {
     __syncthreads();
+    stage(k0);
+    __syncthreads();
+    if (k0 + KT < k_end) fetch(k0 + KT);
+    if (v0 + 2 * warp >= n_virt) continue;             // both rows of the warp are past the sequence's last
     float s[2][2] = {};                                // [row][key half]
 #pragma unroll 4
     for (int c = 0; c < HD; c += 4) {
@@ -118,16 +157,21 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
     }
     __syncwarp();
 #pragma unroll 4
-    for (int j = 0; j < KT; ++j) {
-      float x[PL];
-#pragma unroll
-      for (int d = 0; d < PL; ++d) x[d] = sV[j * LD + 32 * d + lane];
+    for (int j = 0; j < KT; j += 4) {
+      float p[2][4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float p = sP[(2 * warp + i) * KT + j];
-#pragma unroll
-        for (int d = 0; d < PL; ++d) acc[i][d] = fmaf(p, x[d], acc[i][d]);
+        const float4 q = *reinterpret_cast<const float4*>(sP + (2 * warp + i) * KT + j);
+        p[i][0] = q.x, p[i][1] = q.y, p[i][2] = q.z, p[i][3] = q.w;
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int d = 0; d < PL; ++d) {
+          const float x = sV[(j + e) * LD + 32 * d + lane];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[i][d] = fmaf(p[i][e], x, acc[i][d]);
+        }
     }
   }
 #pragma unroll

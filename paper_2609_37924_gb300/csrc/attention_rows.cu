@@ -4,15 +4,19 @@
 // A block takes 16 virtual rows (row-major, then the query heads of one KV
 // head, so that a key tile serves all of them) of one sequence and walks its
 // visible keys in tiles of 64: K and V as fp32 in shared memory, a warp per
-// two virtual rows, two keys per lane for the scores, four or two dims per
-// lane for P V.  Everything is fp32: scores, running maximum and sum (online
-// softmax), accumulators.  It serves fp32 rows, those of the small models, whose
-// calls are a launch (11 us with the host's part for a few hundred rows of 4
-// heads).  Longer ones are bound by shared-memory reads and a tile's latency,
-// about 3 us; the next tile's loads wait in registers meanwhile, 16 bytes each
-// (a row over 600 tokens of the cache 36 us, 72 with loads of single elements
-// between the barriers; four prompts of 500: 54 and 70).
+// two virtual rows (eight apart, so that a single token's rows are on warps of
+// their own), two keys per lane for the scores, four or two dims per lane for
+// P V.  Everything is fp32: scores, running maximum and sum (online softmax),
+// accumulators.  It serves fp32 rows, those of the small models, whose calls
+// are a launch (11 us with the host's part for a few hundred rows of 4 heads).
+// Longer ones are bound by a tile's latency, about 3 us: the next tile's loads
+// wait in registers meanwhile, 16 bytes each (a row over 600 tokens of the cache
+// 27 us, 72 with loads of single elements between the barriers; four prompts of
+// 500 rows 54 and 70; with tiles of 32 rows 26 and 60, and four blocks of 32
+// rows over 600 tokens 58 instead of 42).
 #include <cuda_fp8.h>
+
+#include <type_traits>
 
 #include "ragged.cuh"
 #include "serve.h"
@@ -21,6 +25,7 @@ namespace tadm {
 namespace {
 
 constexpr int RT = 16, KT = 64, NT = 256;     // virtual rows and keys of a tile, threads
+constexpr int WR = RT * 32 / NT;              // rows of a warp: its index and every eighth on
 static_assert(KT == TADM_PAGE_TOKENS, "a key tile is a page");
 
 struct RowsAttnArgs {
@@ -64,7 +69,13 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
     const int v = v0 + i / HD;
     sQ[i] = v < n_virt ? a.q[(rows.first + v / group) * a.ldq + static_cast<int64_t>(hk * group + v % group) * HD + i % HD] : 0.0f;
   }
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f}, acc[2][PL] = {};
+  float m[WR], l[WR], acc[WR][PL];
+#pragma unroll
+  for (int i = 0; i < WR; ++i) {
+    m[i] = -INFINITY, l[i] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < PL; ++d) acc[i][d] = 0.0f;
+  }
   // a thread's part of the next key tile waits in registers while this one is computed
   constexpr int NF = PAGED ? HD / 64 : HD / 16;               // 16-byte loads per thread of K, of V
   int4 rk[NF], rv[NF];
@@ -125,58 +136,64 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
     stage(k0);
     __syncthreads();
     if (k0 + KT < k_end) fetch(k0 + KT);
-    if (v0 + 2 * warp >= n_virt) continue;             // both rows of the warp are past the sequence's last
-    float s[2][2] = {};                                // [row][key half]
+    // the first R rows of the warp
+    auto tile = [&](auto count) {
+      constexpr int R = decltype(count)::value;
+      float s[R][2] = {};                              // [row][key half]
 #pragma unroll 4
-    for (int c = 0; c < HD; c += 4) {
-      const float4 ka = *reinterpret_cast<const float4*>(sK + lane * LD + c);
-      const float4 kb = *reinterpret_cast<const float4*>(sK + (lane + 32) * LD + c);
+      for (int c = 0; c < HD; c += 4) {
+        const float4 ka = *reinterpret_cast<const float4*>(sK + lane * LD + c);
+        const float4 kb = *reinterpret_cast<const float4*>(sK + (lane + 32) * LD + c);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float4 q = *reinterpret_cast<const float4*>(sQ + (2 * warp + i) * HD + c);
-        s[i][0] = fmaf(q.x, ka.x, fmaf(q.y, ka.y, fmaf(q.z, ka.z, fmaf(q.w, ka.w, s[i][0]))));
-        s[i][1] = fmaf(q.x, kb.x, fmaf(q.y, kb.y, fmaf(q.z, kb.z, fmaf(q.w, kb.w, s[i][1]))));
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int v = v0 + 2 * warp + i, pos = pos0 + v / group;
-      const int hi = a.causal ? min(len, pos + 1) : len, lo = a.window > 0 ? pos - a.window + 1 : 0;
-      const bool see0 = v < n_virt && k0 + lane >= lo && k0 + lane < hi;
-      const bool see1 = v < n_virt && k0 + lane + 32 >= lo && k0 + lane + 32 < hi;
-      const float x0 = see0 ? s[i][0] * a.scale : -INFINITY, x1 = see1 ? s[i][1] * a.scale : -INFINITY;
-      const float mn = fmaxf(m[i], warp_max(fmaxf(x0, x1)));
-      const float f = m[i] == -INFINITY ? 0.0f : expf(m[i] - mn);
-      const float p0 = see0 ? expf(x0 - mn) : 0.0f, p1 = see1 ? expf(x1 - mn) : 0.0f;
-      sP[(2 * warp + i) * KT + lane] = p0;
-      sP[(2 * warp + i) * KT + lane + 32] = p1;
-      l[i] = l[i] * f + p0 + p1;                       // this lane's keys; the lanes' sums meet at the end
-#pragma unroll
-      for (int d = 0; d < PL; ++d) acc[i][d] *= f;
-      m[i] = mn;
-    }
-    __syncwarp();
-#pragma unroll 4
-    for (int j = 0; j < KT; j += 4) {
-      float p[2][4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float4 q = *reinterpret_cast<const float4*>(sP + (2 * warp + i) * KT + j);
-        p[i][0] = q.x, p[i][1] = q.y, p[i][2] = q.z, p[i][3] = q.w;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int d = 0; d < PL; ++d) {
-          const float x = sV[(j + e) * LD + 32 * d + lane];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) acc[i][d] = fmaf(p[i][e], x, acc[i][d]);
+        for (int i = 0; i < R; ++i) {
+          const float4 q = *reinterpret_cast<const float4*>(sQ + (warp + 8 * i) * HD + c);
+          s[i][0] = fmaf(q.x, ka.x, fmaf(q.y, ka.y, fmaf(q.z, ka.z, fmaf(q.w, ka.w, s[i][0]))));
+          s[i][1] = fmaf(q.x, kb.x, fmaf(q.y, kb.y, fmaf(q.z, kb.z, fmaf(q.w, kb.w, s[i][1]))));
         }
-    }
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int v = v0 + warp + 8 * i, pos = pos0 + v / group;
+        const int hi = a.causal ? min(len, pos + 1) : len, lo = a.window > 0 ? pos - a.window + 1 : 0;
+        const bool see0 = v < n_virt && k0 + lane >= lo && k0 + lane < hi;
+        const bool see1 = v < n_virt && k0 + lane + 32 >= lo && k0 + lane + 32 < hi;
+        const float x0 = see0 ? s[i][0] * a.scale : -INFINITY, x1 = see1 ? s[i][1] * a.scale : -INFINITY;
+        const float mn = fmaxf(m[i], warp_max(fmaxf(x0, x1)));
+        const float f = m[i] == -INFINITY ? 0.0f : expf(m[i] - mn);
+        const float p0 = see0 ? expf(x0 - mn) : 0.0f, p1 = see1 ? expf(x1 - mn) : 0.0f;
+        sP[(warp + 8 * i) * KT + lane] = p0;
+        sP[(warp + 8 * i) * KT + lane + 32] = p1;
+        l[i] = l[i] * f + p0 + p1;                     // this lane's keys; the lanes' sums meet at the end
+#pragma unroll
+        for (int d = 0; d < PL; ++d) acc[i][d] *= f;
+        m[i] = mn;
+      }
+      __syncwarp();
+#pragma unroll 4
+      for (int j = 0; j < KT; j += 4) {
+        float p[R][4];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const float4 q = *reinterpret_cast<const float4*>(sP + (warp + 8 * i) * KT + j);
+          p[i][0] = q.x, p[i][1] = q.y, p[i][2] = q.z, p[i][3] = q.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int d = 0; d < PL; ++d) {
+            const float x = sV[(j + e) * LD + 32 * d + lane];
+#pragma unroll
+            for (int i = 0; i < R; ++i) acc[i][d] = fmaf(p[i][e], x, acc[i][d]);
+          }
+      }
+    };
+    const int left = n_virt - v0 - warp;               // > 8 i: the warp has row i
+    if (left > 8) tile(std::integral_constant<int, WR>{});
+    else if (left > 0) tile(std::integral_constant<int, 1>{});
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int v = v0 + 2 * warp + i;
+  for (int i = 0; i < WR; ++i) {
+    const int v = v0 + warp + 8 * i;
     const float sum = warp_sum(l[i]);
     if (v >= n_virt) continue;
     float* o = a.o + (rows.first + v / group) * a.ldo + static_cast<int64_t>(hk * group + v % group) * HD;
@@ -210,7 +227,7 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
     a.pages = p.pages;
   }
   const int group = c.n_heads / c.n_kv;
-  // at most one tile per 16 virtual rows and one more per sequence
+  // at most one tile per RT virtual rows and one more per sequence
   const int64_t tiles = static_cast<int64_t>(c.total) * group / RT + c.batch;
   const cudaError_t e = launch_pdl(attn_rows_kernel<PAGED, HD>, dim3(static_cast<unsigned>(tiles), c.n_kv), NT, smem, s, a);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);

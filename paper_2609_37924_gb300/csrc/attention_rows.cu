@@ -8,7 +8,7 @@
 // their own), two keys per lane for the scores, four or two dims per lane for
 // P V.  Everything is fp32: scores, running maximum and sum (online softmax),
 // accumulators.  It serves fp32 rows, those of the small models, whose calls
-// are a launch (11 us with the host's part for a few hundred rows of 4 heads).
+// are a launch (9 us with the host's part for a few hundred rows of 4 heads).
 // Longer ones are bound by a tile's latency, about 3 us: the next tile's loads
 // wait in registers meanwhile, 16 bytes each (a row over 600 tokens of the cache
 // 27 us, 72 with loads of single elements between the barriers; four prompts of

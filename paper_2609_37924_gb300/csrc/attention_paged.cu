@@ -9,7 +9,7 @@
 // whose page scales are two registers.
 //
 // K enters the tensor cores as the e4m3 bytes that the page holds; Q is the sum
-// of two e4m3 terms, both multiplied with K into the same fp32 scores.  V^T is
+// of an e4m3 and an e5m2 term, both multiplied with K into the same fp32 scores.  V^T is
 // widened to f16, because the probabilities need more than 8 bits.
 //
 // A tile is 128 keys, two pages.  Roles of a CTA (12, 16 or 24 warps for 16, 32 or 64 rows):
@@ -27,8 +27,9 @@
 //                over the keys; the sums of a row stay one partial per thread
 //                until the end of the work item.
 // Precision: Q is scaled by one power of two per tile of rows; the two terms
-// hold a bf16 value exactly if it is within 2^-10 of the tile's largest, and
-// to 2^-18 of the largest below that.  K and V are exact, the probabilities
+// hold a bf16 value exactly if it is within 2^-13 of the tile's largest, and
+// to 2^-21 of the largest below that (2^-10 and 2^-18 where the second term was
+// e4m3 too, whose least step is 2^-9 and not 2^-16).  K and V are exact, the probabilities
 // times the page's V scale are rounded to f16 (11 bits) with the row's
 // reference at 2^7 to 2^15, so that a probability 2^-21 of the largest still
 // has all of them; scores, sums and O are fp32.
@@ -285,9 +286,9 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_maj
   return (1u << 4) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
 }
-// A and B: e4m3, both K-major
-__host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N) {
-  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+// A: e4m3, B: e4m3 or e5m2, both K-major
+__host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N, bool b_e5m2) {
+  return (1u << 4) | (b_e5m2 ? 1u << 10 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 // High word of the descriptor of a K-major 8-bit operand whose rows are HD bytes, swizzled over the row's width (the low
 // word is desc_k's).
@@ -530,7 +531,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     for (int i = max(0, g - NST); i < g; ++i) mbar_wait_bounded(&kv_full[i % NST], (i / NST) & 1, &never, nullptr);
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
-    constexpr uint32_t idesc_s = idesc_f8_f32(128, N), idesc_o = idesc_f16_f32(128, N, true);
+    constexpr uint32_t idesc_hi = idesc_f8_f32(128, N, false), idesc_lo = idesc_f8_f32(128, N, true), idesc_o = idesc_f16_f32(128, N, true);
     const uint32_t q_lo = desc_k(smem_u32(sQ)), k_lo = desc_k(smem_u32(sKV)), p_lo = desc_mn(smem_u32(sP));
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, nullptr);
@@ -551,8 +552,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           const uint32_t sb = tile & 1, s = tmem + C::S_COL + sb * 64, k0 = k_lo + st * (C::STAGE_BYTES >> 4);
           if (!wait(&kv_full[st], turn)) { ok = false; break; }
           tc_fence_after();
-          umma_f8_ss<HD / 32>(s, k0, q0, kRows8Hi<HD>, idesc_s, 0);
-          umma_f8_ss<HD / 32>(s, k0, q0 + (C::QT_BYTES >> 4), kRows8Hi<HD>, idesc_s, 1);
+          umma_f8_ss<HD / 32>(s, k0, q0, kRows8Hi<HD>, idesc_hi, 0);
+          umma_f8_ss<HD / 32>(s, k0, q0 + (C::QT_BYTES >> 4), kRows8Hi<HD>, idesc_lo, 1);
           umma_commit(&s_full[sb]);
           umma_commit(&kv_empty[st]);
           if (i == nt - 1) umma_commit(&q_empty[qb]);
@@ -624,7 +625,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
   } else if (warp < 4) {
     // --------------------------------------------------------------- Q
-    // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in two e4m3 terms
+    // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in an e4m3 and an e5m2 term
     // (rolled loops: this runs once per item, straight-line code would wait for its instructions)
     constexpr int CPR = HD / 8, QV = N * CPR / 64;            // groups of 8 dims per row, per thread
     const int tid = threadIdx.x - 64;
@@ -671,6 +672,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       top = max(s_qmax[0], s_qmax[1]);
       const int e_max = max(static_cast<int>(top >> 23), 40) - 127;    // 2^e_max <= the largest
       const float q_up = __int_as_float((7 - e_max + 127) << 23), q_down = __int_as_float((e_max - 7 + 127) << 23);
+      const uint64_t up2 = f2_pack(q_up, q_up);
       ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr) && ok;
       if (tid == 0) s_qdown[seg & 3] = q_down;
 #pragma unroll 4
@@ -682,11 +684,15 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         uint32_t term[2][2] = {};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          // the upper four significant bits of each value, then the lower four
-          const float2 v = make_float2(__uint_as_float(x[e] << 16) * q_up, __uint_as_float(x[e] & 0xffff0000u) * q_up);
-          const float2 u = make_float2(__uint_as_float(__float_as_uint(v.x) & 0xfff00000u), __uint_as_float(__float_as_uint(v.y) & 0xfff00000u));
-          const uint32_t p = __nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
-          const uint32_t l = __nv_cvt_float2_to_fp8x2(make_float2(v.x - u.x, v.y - u.y), __NV_SATFINITE, __NV_E4M3);
+          // each value rounded to four significant bits, then the rest: at most 8 times the last place of the value's
+          // eight bits, which has three (and 0 v, a NaN where v is infinite: the conversions would saturate)
+          const uint64_t v = f2_mul(f2_pack(__uint_as_float(x[e] << 16), __uint_as_float(x[e] & 0xffff0000u)), up2);
+          float2 f;
+          f2_unpack(v, f.x, f.y);
+          const uint32_t p = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+          f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(p), __NV_E4M3)));
+          f2_unpack(f2_fma(v, f2_pack(0.0f, 0.0f), f2_fma(f2_pack(f.x, f.y), f2_pack(-1.0f, -1.0f), v)), f.x, f.y);
+          const uint32_t l = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E5M2);
           term[0][e >> 1] |= p << (16 * (e & 1));
           term[1][e >> 1] |= l << (16 * (e & 1));
         }

@@ -73,7 +73,7 @@ __device__ __forceinline__ void umma4_ts_two(uint32_t d, uint32_t a, uint32_t b,
       : "memory");
 }
 
-// D = A B^T over STEPS x 32 dims of e4m3, A and B in shared memory, both K-major with rows of HD bytes; hi: the high
+// D = A B^T over STEPS x 32 dims of 8-bit floats (idesc says which), A and B in shared memory, both K-major with rows of HD bytes; hi: the high
 // word of their descriptors (32 further dims: 32 bytes on)
 template <int STEPS>
 __device__ __forceinline__ void umma_f8_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t idesc, uint32_t acc) {

@@ -1,0 +1,46 @@
+"""Operators for sequences of different lengths over values of very different sizes, and in states at the edge of what
+they accept, against plain definitions in 64 bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from test_gpu_serving import T, attend64, filled, gen, run_paged  # noqa: E402, F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ queries of different sizes
+def cached(pool, table, b, n, layer=1):
+    """The first n tokens of sequence b as the pool's bytes and scales say, in 64 bits: k, v [n, heads, hd]."""
+    at = table[b, :-(-n // 64)].long()
+    f = lambda x, s: x[layer, at].view(torch.float8_e4m3fn).double() * s[layer, at].double()[..., None, None]  # noqa: E731
+    k, v = f(pool.k, pool.k_scale), f(pool.v, pool.v_scale)
+    return k.permute(0, 2, 1, 3).flatten(0, 1)[:n], v.permute(0, 3, 1, 2).flatten(0, 1)[:n]
+
+
+def encode(x):
+    return x.float().to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads", [(16, 8, 128), (6, 2, 64), (8, 1, 128), (32, 16, 128)])
+@pytest.mark.parametrize("n,length", [(1, 700), (8, 300), (33, 1025)])
+@pytest.mark.parametrize("gain", [2.0 ** 11, 2.0 ** 12])
+def test_page_attention_large_channel(T, dtype, heads, n, length, gain):
+    """A channel of Q is `gain` times the others and K's as much smaller, so that all channels count alike: the others keep
+    their bits.  The bf16 form holds Q to 2^-21 of the largest value of a tile of rows, q_top, errors evenly spread over
+    both signs: a score is off by |k| q_top 2^-21 / sqrt(3 hd), outputs by about twice that (relative), beside bf16's 2^-8."""
+    Hq, Hkv, hd = heads
+    pool, table, _ = filled(T, [length], Hkv, hd, length + Hq)
+    pool.k[1, :, :, :, 5] = encode(pool.k[1, :, :, :, 5].contiguous().view(torch.float8_e4m3fn).float() / gain)
+    k, v = cached(pool, table, 0, length)
+    q = torch.randn((n, Hq, hd), generator=gen(6), device="cuda")
+    q[..., 5] *= gain
+    q = q.to(dtype)
+    o = run_paged(T, pool, table, q, [0, n], [length], n, length, False, 0)
+    ref, _ = attend64(q.double(), k, v, torch.zeros(n, device="cuda"), False, 0)
+    err = (o.double() - ref).norm(dim=-1) / ref.norm(dim=-1)
+    score = float(q.abs().max()) * 2.0 ** -21 / math.sqrt(3.0 * hd) * float(k.norm(dim=-1).mean())
+    tol = math.sqrt(2.0 ** -16 + (2 * score) ** 2) if dtype == torch.bfloat16 else 1e-4
+    assert err.square().mean().sqrt() <= tol and (err <= 4 * tol).all(), (float(err.square().mean().sqrt()), float(err.max()), tol)

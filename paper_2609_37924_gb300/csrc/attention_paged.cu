@@ -26,21 +26,24 @@
 //                one vote of the four warps that share rows and no reduction
 //                over the keys; the sums of a row stay one partial per thread
 //                until the end of the work item.
-// Precision: Q is scaled by one power of two per tile of rows; the two terms
-// hold a bf16 value exactly if it is within 2^-13 of the tile's largest, and
-// to 2^-21 of the largest below that (2^-10 and 2^-18 where the second term was
-// e4m3 too, whose least step is 2^-9 and not 2^-16).  K and V are exact, the probabilities
+// Precision: each row of Q is scaled by a power of four of its own (with one factor
+// per tile, a large row took the bits of the others); the two terms hold a bf16
+// value exactly if it is within 2^-12 of its row's largest, and to 2^-20 of that
+// below (e5m2, because its steps go down to 2^-16, e4m3's to 2^-9).  K and V are
+// exact, the probabilities
 // times the page's V scale are rounded to f16 (11 bits) with the row's
 // reference at 2^7 to 2^15, so that a probability 2^-21 of the largest still
 // has all of them; scores, sums and O are fp32.
 //
 // Bound: the bytes of the cache.  Measured: 4 tokens over 386,544 cached ones (8
-// KV heads of 128) 135 us, 5.9 TB/s; with 64 virtual rows a tile takes 1.05 us
+// KV heads of 128) 135 us, 5.9 TB/s; with 64 virtual rows a tile takes 1.1 us
 // per SM for 0.73 us of bytes, paced by the softmax warps' chain of waits (8 x
-// 32 rows over 99,641 tokens, 16 KV heads: 98 us, 4.2 TB/s).  There, in the order
+// 32 rows over 99,641 tokens, 16 KV heads: 103 us, 4.0 TB/s).  There, in the order
 // of their making: K and V both widened to f16 157 us; K multiplied as it is
 // stored, 142 with Q in three terms and 121 in two; fewer instructions around
-// the items 109; 16 rows per softmax thread where 32 were 100.
+// the items 109; 16 rows per softmax thread where 32 were 100;
+// 98 with one factor of Q per tile.  A factor per row, read by the softmax with
+// every tile, took 107 as fp32, 106 as bf16 and 103 as a byte.
 //
 // Work: the tiles of all (sequence, KV head, row tile) items lie on one line,
 // each item followed by what its start and end cost, and the line is cut
@@ -268,7 +271,7 @@ struct PagedCfg {
   static constexpr int RN = 16, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
   static constexpr int THREADS = 256 + SM_THREADS;
-  static constexpr int MISC = 3328 + N * 40;
+  static constexpr int MISC = 3328 + N * 44;
   static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 2 * Q_BYTES + 2 * P_BYTES + RAW_BYTES + MISC;
   static constexpr int V_COL = 0, S_COL = 128, O_COL = 256;  // TMEM columns: two V^T, two S, one O
   static_assert(SMEM <= 232448, "shared memory");
@@ -341,22 +344,6 @@ __device__ __forceinline__ void e4m3x4_f16x4(uint32_t w, uint32_t& lo, uint32_t&
       : "=r"(lo), "=r"(hi)
       : "r"(w));
 }
-// C consecutive TMEM columns of this thread's lane, C = 16 or 32
-template <int C>
-__device__ __forceinline__ void tmem_ld(uint32_t addr, float* v) {
-  if constexpr (C == 32) {
-    uint32_t r[32];
-    tmem_ld32_nowait(addr, r);
-    tmem_wait_ld(r);
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-  } else {
-    float r[16];
-    tmem_ld16(addr, r);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = r[i];
-  }
-}
 __device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
   uint32_t r[8];
   asm volatile(
@@ -398,9 +385,6 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   uint64_t* raw_full = bars + 43;                             // a completion per segment, its rows of Q
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float* s_qdown = reinterpret_cast<float*>(bars + 36);       // [4] 1 / the factor of segment i's Q at i % 4 (the
-                                                              // softmax reads it later than the MMAs read Q)
-  uint32_t* s_qmax = reinterpret_cast<uint32_t*>(bars + 38);  // [2] the staging warps' maxima
   Place* s_place = reinterpret_cast<Place*>(bars + 44);
   static_assert(sizeof(Place) <= 160, "place");
   // [16][2] of the pages of tile t at t % 16: K scale, V scale * 128, log2(V scale)
@@ -413,6 +397,9 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   float* s_red = s_fac + N;                                   // [4][N]
   int2* s_see = reinterpret_cast<int2*>(s_red + 4 * N);       // visible keys [x, y)
   int64_t* s_row = reinterpret_cast<int64_t*>(s_see + N);     // element offset of the output row, -1: none
+  // [4][N] what a score of a row of segment i counts, 1 / the row's factor, at i % 4 (the softmax reads it later than the
+  // MMAs read Q): b stands for 2^(2 b - 126), whose fp32 bits are b, then 0x80, then zeros
+  uint8_t* s_unit = reinterpret_cast<uint8_t*>(s_row + N);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -625,7 +612,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
   } else if (warp < 4) {
     // --------------------------------------------------------------- Q
-    // N rows scaled by a power of two so that the largest value is in 2^7 .. 2^8, in an e4m3 and an e5m2 term
+    // N rows, each scaled by a power of four so that its largest value is in 2^6 .. 2^8, in an e4m3 and an e5m2 term
     // (rolled loops: this runs once per item, straight-line code would wait for its instructions)
     constexpr int CPR = HD / 8, QV = N * CPR / 64;            // groups of 8 dims per row, per thread
     const int tid = threadIdx.x - 64;
@@ -656,30 +643,32 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     while (more) {
       const int qb = seg & 1, rows = fetch();
       bool ok = warp_wait_bounded(raw_full, seg & 1, abort_flag, nullptr);
-      uint32_t top = 0;
+      // the largest magnitude of each row, infinities and NaN (an exponent of ones) aside: 64 / N threads per row, which
+      // begin at different groups (and banks)
+      constexpr int TPR = 64 / N;
+      const int own = tid / TPR;
+      uint32_t m = 0;
 #pragma unroll 4
       for (int i = 0; i < QV; ++i) {
-        const int c = i * 64 + tid;
-        uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
-        if (c / CPR >= rows) q = make_uint4(0, 0, 0, 0);
-        // infinities and NaN (an exponent of ones) aside
+        uint4 q = reinterpret_cast<const uint4*>(sRaw)[own * CPR + (TPR * (i + own) + tid % TPR) % CPR];
+        if (own >= rows) q = make_uint4(0, 0, 0, 0);
         auto finite = [](uint32_t w) { return w & 0x7fff7fffu & ~__vcmpgeu2(w & 0x7fff7fffu, 0x7f807f80u); };
-        top = __vmaxu2(top, __vmaxu2(__vmaxu2(finite(q.x), finite(q.y)), __vmaxu2(finite(q.z), finite(q.w))));
+        m = __vmaxu2(m, __vmaxu2(__vmaxu2(finite(q.x), finite(q.y)), __vmaxu2(finite(q.z), finite(q.w))));
       }
-      top = __reduce_max_sync(0xffffffffu, max(top & 0xffff0000u, top << 16));
-      if (lane == 0) s_qmax[warp & 1] = top;
+      uint32_t top = max(m & 0xffff0000u, m << 16);
+#pragma unroll
+      for (int o = 1; o < TPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int e_max = max(static_cast<int>(top >> 23), 40) - 127;      // 2^e_max <= the largest
+      s_unit[(seg & 3) * N + own] = static_cast<uint8_t>((e_max - 7 + 127) >> 1);
       asm volatile("barrier.cta.sync 8, 64;" ::: "memory");
-      top = max(s_qmax[0], s_qmax[1]);
-      const int e_max = max(static_cast<int>(top >> 23), 40) - 127;    // 2^e_max <= the largest
-      const float q_up = __int_as_float((7 - e_max + 127) << 23), q_down = __int_as_float((e_max - 7 + 127) << 23);
-      const uint64_t up2 = f2_pack(q_up, q_up);
       ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr) && ok;
-      if (tid == 0) s_qdown[seg & 3] = q_down;
 #pragma unroll 4
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
         uint4 q = reinterpret_cast<const uint4*>(sRaw)[c];
         if (r >= rows) q = make_uint4(0, 0, 0, 0);
+        const float q_up = __int_as_float((253 - 2 * s_unit[(seg & 3) * N + r]) << 23);
+        const uint64_t up2 = f2_pack(q_up, q_up);
         const uint32_t x[4] = {q.x, q.y, q.z, q.w};
         uint32_t term[2][2] = {};
 #pragma unroll
@@ -703,7 +692,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       fence_proxy_async_smem();
       warp_arrive(&q_full[qb]);
       ++seg;
-      // both warps have read the maxima and the rows, and they go on or leave together
+      // both warps have read the exponents and the rows, and they go on or leave together
       uint32_t leave;
       asm volatile(
           "{\n\t.reg .pred a, b;\n\t"
@@ -760,26 +749,26 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       bool has_ref = false;                                   // of row `own`
       bool unset = true;                                      // some row has no reference yet (the warps agree)
       const int nt = w.nt, t0 = w.t0;
-      float q_scale = 0.0f;
       for (int i = 0; i < nt; ++i) {
         const int t = g + i, sb = t & 1, tile = t0 + i;
         if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; }
         // the warps vote below: all of them leave together
         tc_fence_after();
         const float4 sc = s_scale[(t & 15) * 2 + (key_lane >> 6)];
-        if (i == 0) q_scale = s_qdown[seg & 3] * a.scale_log2;
-        const float cth = sc.x * q_scale, lv = sc.z;
+        const float lv = sc.z;
         const int key = tile * TK + key_lane;
         const bool masked = tile * TK < all_lo || (tile + 1) * TK > all_hi;
-        float x[RN];
-        tmem_ld<RN>(tmem + lane_off + C::S_COL + sb * 64 + row0, x);
-        const uint64_t c2 = f2_pack(cth, cth);
-        float mx = -INFINITY;
+        float x[RN], mx = -INFINITY;
+        tmem_ld16(tmem + lane_off + C::S_COL + sb * 64 + row0, x);
+        const float ks = sc.x * a.scale_log2;
+        const uint64_t ks2 = f2_pack(ks, ks);
 #pragma unroll
         for (int r = 0; r < RN; r += 4) {
           const ulonglong2 nm = *reinterpret_cast<const ulonglong2*>(s_negm + row0 + r);
-          f2_unpack(f2_fma(f2_pack(x[r], x[r + 1]), c2, nm.x), x[r], x[r + 1]);
-          f2_unpack(f2_fma(f2_pack(x[r + 2], x[r + 3]), c2, nm.y), x[r + 2], x[r + 3]);
+          const uint32_t un = *reinterpret_cast<const uint32_t*>(s_unit + (seg & 3) * N + row0 + r);
+          auto unit = [&](int k) { return __uint_as_float(__byte_perm(un, 0x00800000u, 0x0644 | k << 12)); };
+          f2_unpack(f2_fma(f2_pack(x[r], x[r + 1]), f2_mul(f2_pack(unit(0), unit(1)), ks2), nm.x), x[r], x[r + 1]);
+          f2_unpack(f2_fma(f2_pack(x[r + 2], x[r + 3]), f2_mul(f2_pack(unit(2), unit(3)), ks2), nm.y), x[r + 2], x[r + 3]);
         }
         if (masked) {
 #pragma unroll

@@ -5,7 +5,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_serving import T, attend64, filled, gen, run_paged  # noqa: E402, F401
+from test_gpu_serving import T, attend64, close, cum, filled, gen, run_paged  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -29,8 +29,9 @@ def encode(x):
 @pytest.mark.parametrize("gain", [2.0 ** 11, 2.0 ** 12])
 def test_page_attention_large_channel(T, dtype, heads, n, length, gain):
     """A channel of Q is `gain` times the others and K's as much smaller, so that all channels count alike: the others keep
-    their bits.  The bf16 form holds Q to 2^-21 of the largest value of a tile of rows, q_top, errors evenly spread over
-    both signs: a score is off by |k| q_top 2^-21 / sqrt(3 hd), outputs by about twice that (relative), beside bf16's 2^-8."""
+    their bits.  The bf16 form holds Q to 2^-20 of a row's largest value; with q_top the largest of all rows and errors of
+    q_top 2^-21 evenly spread over both signs, a score is off by |k| q_top 2^-21 / sqrt(3 hd), outputs by about twice that
+    (relative), beside bf16's 2^-8."""
     Hq, Hkv, hd = heads
     pool, table, _ = filled(T, [length], Hkv, hd, length + Hq)
     pool.k[1, :, :, :, 5] = encode(pool.k[1, :, :, :, 5].contiguous().view(torch.float8_e4m3fn).float() / gain)
@@ -44,3 +45,25 @@ def test_page_attention_large_channel(T, dtype, heads, n, length, gain):
     score = float(q.abs().max()) * 2.0 ** -21 / math.sqrt(3.0 * hd) * float(k.norm(dim=-1).mean())
     tol = math.sqrt(2.0 ** -16 + (2 * score) ** 2) if dtype == torch.bfloat16 else 1e-4
     assert err.square().mean().sqrt() <= tol and (err <= 4 * tol).all(), (float(err.square().mean().sqrt()), float(err.max()), tol)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads", [(16, 8, 128), (6, 2, 64), (8, 1, 128), (32, 16, 128)])
+@pytest.mark.parametrize("rows,lens", [([1, 1], [300, 64]), ([8, 3], [700, 40]), ([32, 33], [517, 1025])])
+@pytest.mark.parametrize("large", [2.0 ** 6, 2.0 ** 12, 2.0 ** 20, 2.0 ** 60, math.inf, math.nan])
+def test_page_attention_beside_large_rows(T, dtype, heads, rows, lens, large):
+    """One query head of a sequence's first row and all heads of its last one (where it has more) are enlarged: every
+    other row has its own accuracy, whatever shares its tile."""
+    Hq, Hkv, hd = heads
+    pool, table, seqs = filled(T, lens, Hkv, hd, sum(lens) + Hq)
+    q = torch.randn((sum(rows), Hq, hd), generator=gen(5), device="cuda")
+    grown = torch.zeros((sum(rows), Hq), dtype=torch.bool, device="cuda")
+    for a, n in zip(cum(rows), rows):
+        grown[a, Hq - 1] = True
+        if n > 1:
+            grown[a + n - 1] = True
+    q = torch.where(grown[..., None], q * large, q).to(dtype)
+    o = run_paged(T, pool, table, q, cum(rows), lens, max(rows), max(lens), False, 0)
+    for b, n in enumerate(rows):
+        s, (k, v) = slice(cum(rows)[b], cum(rows)[b] + n), seqs[b]
+        ref, absum = attend64(torch.where(grown[s][..., None], 0.0, q[s].double()), k, v, torch.zeros(n, device="cuda"), False, 0)
+        keep = ~grown[s]
+        close(o[s][keep], ref[keep], absum[keep], dtype, float(v.abs().max()))

@@ -217,6 +217,19 @@ def _stream(stream=None) -> Optional[int]:
     return _raw_stream()
 
 
+_current_device = None
+
+
+def _device() -> int:
+    """The current device, on which a call launches."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        torch.cuda.init()
+        _current_device = torch._C._cuda_getDevice
+    return _current_device()
+
+
 def tadm_gemm(A, B, C, dtype: int, stream=None):
     M, K = A.shape
     N = B.shape[0]
@@ -337,6 +350,7 @@ class PagePool:
         self.c = tadm_page_pool(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), layers, pages,
                                 n_kv, hd)
         self.ref = ctypes.addressof(self.c)
+        self.index = k.get_device()
 
     @classmethod
     def empty(cls, layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -358,23 +372,38 @@ def _torch_types():
 
 
 def _rows_of(*tensors):
-    """The dtype code of row operands [rows, heads, hd]: fp32 or bf16, each row's heads dense, on the GPU."""
-    kind = tensors[0].dtype
+    """The dtype code of row operands [rows, heads, hd]: fp32 or bf16, each row's heads dense, on the current device."""
+    kind, device = tensors[0].dtype, _device()
     dtype = (_DTYPES or _torch_types()).get(kind)
     if dtype not in (0, 1):
         raise TadmError(1, f"rows must be fp32 or bf16, not {kind}")
     for t in tensors:
         s = t.stride()
-        if len(s) != 3 or s[2] != 1 or s[1] != t.shape[2] or t.dtype is not kind or not t.is_cuda:
-            raise TadmError(1, "rows must be CUDA tensors [rows, heads, head_dim] of one type with dense heads")
+        if len(s) != 3 or s[2] != 1 or s[1] != t.shape[2] or t.dtype is not kind or t.get_device() != device:
+            raise TadmError(1, "rows must be tensors [rows, heads, head_dim] of one type with dense heads on the current device")
     return dtype
 
 
 def _ints_of(*tensors):
-    types = _DTYPES or _torch_types()
+    types, device = _DTYPES or _torch_types(), _device()
     for t in tensors:
-        if types.get(t.dtype) != "int32" or not t.is_contiguous() or not t.is_cuda:
-            raise TadmError(1, "lengths, tables and lists must be contiguous int32 CUDA tensors")
+        if types.get(t.dtype) != "int32" or not t.is_contiguous() or t.get_device() != device:
+            raise TadmError(1, "lengths, tables and lists must be contiguous int32 tensors on the current device")
+
+
+def _pool_of(pool):
+    if pool.index != _device():
+        raise TadmError(1, "the page pool is not on the current device")
+    return pool.ref
+
+
+def _scratch_of(t):
+    """Address and size of scratch memory; none at all is no address."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous() or t.get_device() != _device():
+        raise TadmError(1, "scratch must be a contiguous tensor on the current device")
+    return t.data_ptr(), t.nbytes
 
 
 def tadm_attention_packed(q, k, v, o, cu_rows, max_rows: int, causal: bool = True, window: int = 0, stream=None):
@@ -406,7 +435,7 @@ def _page_rows(call, pool, layer, k, v, cu_rows, start, table, max_rows, stream)
     seqs, width = table.shape
     if start.shape[0] != batch or seqs < batch:
         raise TadmError(1, "start and table need an entry per sequence")
-    status = call(pool.ref, layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, rows, max_rows,
+    status = call(_pool_of(pool), layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, rows, max_rows,
                   k.stride(0), v.stride(0), table.data_ptr(), width, dtype, _stream(stream))
     if status:
         _check(status)
@@ -443,9 +472,9 @@ def tadm_page_attention(q, pool, layer: int, o, cu_rows, lens, table, max_rows: 
     if o.shape != shape or hd != pool.head_dim or lens.shape[0] != batch or seqs < batch:
         raise TadmError(1, "shapes of q, o, lens, table and the pool do not agree")
     status = load_library().tadm_page_attention(
-        q.data_ptr(), pool.ref, layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
+        q.data_ptr(), _pool_of(pool), layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
         max_len, heads, q.stride(0), o.stride(0), table.data_ptr(), width, 1 if causal else 0, window, dtype,
-        _ptr(scratch), 0 if scratch is None else scratch.nbytes, _stream(stream))
+        *_scratch_of(scratch), _stream(stream))
     if status:
         _check(status)
 
@@ -469,7 +498,7 @@ def tadm_pages_reserve(tables, refs, seqs, new_len, tables_out, refs_out, status
     _check(load_library().tadm_pages_reserve(
         tables.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1], seqs.data_ptr(),
         new_len.data_ptr(), seqs.shape[0], tables_out.data_ptr(), refs_out.data_ptr(), status.data_ptr(),
-        scratch.data_ptr(), scratch.nbytes, _stream(stream)))
+        *_scratch_of(scratch), _stream(stream)))
 
 
 def tadm_pages_fork(pool, tables, lens, refs, src, dst, tables_out, lens_out, refs_out, status, scratch, stream=None):
@@ -478,9 +507,9 @@ def tadm_pages_fork(pool, tables, lens, refs, src, dst, tables_out, lens_out, re
     if refs.shape[0] != pool.pages:
         raise TadmError(1, "refs needs an entry per page")
     _check(load_library().tadm_pages_fork(
-        pool.ref, tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1],
+        _pool_of(pool), tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1],
         src.data_ptr(), dst.data_ptr(), src.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
-        status.data_ptr(), scratch.data_ptr(), scratch.nbytes, _stream(stream)))
+        status.data_ptr(), *_scratch_of(scratch), _stream(stream)))
 
 
 def tadm_pages_free(tables, lens, refs, seqs, tables_out, lens_out, refs_out, status, scratch, stream=None):
@@ -489,7 +518,7 @@ def tadm_pages_free(tables, lens, refs, seqs, tables_out, lens_out, refs_out, st
     _check(load_library().tadm_pages_free(
         tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1],
         seqs.data_ptr(), seqs.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
-        status.data_ptr(), scratch.data_ptr(), scratch.nbytes, _stream(stream)))
+        status.data_ptr(), *_scratch_of(scratch), _stream(stream)))
 
 
 def tadm_pages_compact(pool, tables, refs, tables_out, refs_out, n_live, scratch, stream=None):
@@ -498,9 +527,8 @@ def tadm_pages_compact(pool, tables, refs, tables_out, refs_out, n_live, scratch
     if refs.shape[0] != pool.pages:
         raise TadmError(1, "refs needs an entry per page")
     _check(load_library().tadm_pages_compact(
-        pool.ref, tables.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1], tables_out.data_ptr(),
-        refs_out.data_ptr(), n_live.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(),
-        _stream(stream)))
+        _pool_of(pool), tables.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1], tables_out.data_ptr(),
+        refs_out.data_ptr(), n_live.data_ptr(), *_scratch_of(scratch), _stream(stream)))
 
 
 def tadm_pages_copy(pool, src, dst, stream=None):
@@ -508,7 +536,7 @@ def tadm_pages_copy(pool, src, dst, stream=None):
     _ints_of(src, dst)
     if src.shape != dst.shape:
         raise TadmError(1, "src and dst differ in length")
-    _check(load_library().tadm_pages_copy(pool.ref, src.data_ptr(), dst.data_ptr(), src.shape[0], _stream(stream)))
+    _check(load_library().tadm_pages_copy(_pool_of(pool), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream(stream)))
 
 
 # ---------------------------------------------------------------------------- model handle

@@ -490,6 +490,8 @@ def _seqs_of(tables, tables_out, per_seq, refs, refs_out, lists, status):
     if tables_out.shape != tables.shape or refs_out.shape != refs.shape or any(
             t.shape[0] != tables.shape[0] for t in per_seq) or any(t.shape != lists[0].shape for t in lists):
         raise TadmError(1, "shapes of tables, lens, refs and lists do not agree")
+    if status.numel() < 1:
+        raise TadmError(1, "the outcome needs an element")
 
 
 def tadm_pages_reserve(tables, refs, seqs, new_len, tables_out, refs_out, status, scratch, stream=None):

@@ -113,6 +113,15 @@ def test_scratch_is_contiguous_memory_of_the_device(lib, name, bad):
     assert lib.calls == []
 
 
+@pytest.mark.parametrize("name", [n for n, a in calls().items() if "status" in a or "n_live" in a])
+def test_the_outcome_has_a_place(lib, name):
+    args = calls()[name]
+    args["n_live" if "n_live" in args else "status"] = ints(0)
+    with pytest.raises(tadm.TadmError):
+        getattr(tadm, name)(**args)
+    assert lib.calls == []
+
+
 def test_fp32_attention_needs_no_scratch(lib):
     f = lambda: Cuda(torch.zeros((5, 2, 64)))  # noqa: E731
     tadm.tadm_page_attention(**{**calls()["tadm_page_attention"], "q": f(), "o": f(), "scratch": None})

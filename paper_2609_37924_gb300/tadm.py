@@ -378,10 +378,15 @@ def _rows_of(*tensors):
     if dtype not in (0, 1):
         raise TadmError(1, f"rows must be fp32 or bf16, not {kind}")
     for t in tensors:
-        s = t.stride()
-        if len(s) != 3 or s[2] != 1 or s[1] != t.shape[2] or t.dtype is not kind or t.get_device() != device:
+        s, n = t.stride(), t.shape
+        if len(s) != 3 or s[2] != 1 or (s[1] != n[2] and n[1] != 1) or t.dtype is not kind or t.get_device() != device:
             raise TadmError(1, "rows must be tensors [rows, heads, head_dim] of one type with dense heads on the current device")
     return dtype
+
+
+def _ld(t) -> int:
+    """Elements from one row to the next (a single row may have any stride)."""
+    return t.stride(0) if t.shape[0] != 1 else t.shape[1] * t.shape[2]
 
 
 def _ints_of(*tensors):
@@ -418,7 +423,7 @@ def tadm_attention_packed(q, k, v, o, cu_rows, max_rows: int, causal: bool = Tru
         raise TadmError(1, "shapes of q, k, v and o do not agree")
     status = load_library().tadm_attention_packed(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), cu_rows.data_ptr(), cu_rows.shape[0] - 1, rows,
-        max_rows, heads, kv[1], hd, q.stride(0), k.stride(0), v.stride(0), o.stride(0), 1 if causal else 0, window,
+        max_rows, heads, kv[1], hd, _ld(q), _ld(k), _ld(v), _ld(o), 1 if causal else 0, window,
         dtype, _stream(stream))
     if status:
         _check(status)
@@ -436,7 +441,7 @@ def _page_rows(call, pool, layer, k, v, cu_rows, start, table, max_rows, stream)
     if start.shape[0] != batch or seqs < batch:
         raise TadmError(1, "start and table need an entry per sequence")
     status = call(_pool_of(pool), layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, rows, max_rows,
-                  k.stride(0), v.stride(0), table.data_ptr(), width, dtype, _stream(stream))
+                  _ld(k), _ld(v), table.data_ptr(), width, dtype, _stream(stream))
     if status:
         _check(status)
 
@@ -473,7 +478,7 @@ def tadm_page_attention(q, pool, layer: int, o, cu_rows, lens, table, max_rows: 
         raise TadmError(1, "shapes of q, o, lens, table and the pool do not agree")
     status = load_library().tadm_page_attention(
         q.data_ptr(), _pool_of(pool), layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
-        max_len, heads, q.stride(0), o.stride(0), table.data_ptr(), width, 1 if causal else 0, window, dtype,
+        max_len, heads, _ld(q), _ld(o), table.data_ptr(), width, 1 if causal else 0, window, dtype,
         *_scratch_of(scratch), _stream(stream))
     if status:
         _check(status)

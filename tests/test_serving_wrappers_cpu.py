@@ -126,3 +126,17 @@ def test_fp32_attention_needs_no_scratch(lib):
     f = lambda: Cuda(torch.zeros((5, 2, 64)))  # noqa: E731
     tadm.tadm_page_attention(**{**calls()["tadm_page_attention"], "q": f(), "o": f(), "scratch": None})
     assert lib.calls == ["tadm_page_attention"]
+
+
+def test_strides_of_single_rows_and_heads_do_not_matter(lib):
+    """A tensor of one row has no distance between rows, one of one head none between heads, whatever their strides say."""
+    leading = []
+    lib.tadm_attention_packed = lambda *a: leading.append(a[11:15]) or 0
+    one_row = lambda h: Cuda(torch.zeros((h, 1, 64), dtype=torch.bfloat16).transpose(0, 1))  # noqa: E731
+    tadm.tadm_attention_packed(one_row(8), one_row(2), one_row(2), one_row(8), ints(2), 1)
+    assert leading.pop() == (512, 128, 128, 512)
+    one_head = lambda: Cuda(torch.zeros((1, 5, 64), dtype=torch.bfloat16).transpose(0, 1))  # noqa: E731
+    tadm.tadm_attention_packed(one_head(), one_head(), one_head(), one_head(), ints(2), 5)
+    assert leading.pop() == (64, 64, 64, 64)
+    with pytest.raises(tadm.TadmError):
+        tadm.tadm_attention_packed(*[Cuda(torch.zeros((2, 5, 64), dtype=torch.bfloat16).transpose(0, 1)) for _ in range(4)], ints(2), 5)

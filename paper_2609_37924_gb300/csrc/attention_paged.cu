@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       if (b.id < 0 || b.id >= a.pages) return;
       const int64_t p = static_cast<int64_t>(b.id) * a.n_kv + b.hk;
       const float v = a.sv[p];
-      b.sc = make_float4(a.sk[p], v * 128.0f, log2f(v), 0.0f);
+      b.sc = make_float4(a.sk[p], v * 128.0f, v > 0.0f ? log2f(v) : 0.0f, 0.0f);   // (a page of zeros may have a scale of 0)
     };
     Batch now = take();
     scales(now);

@@ -354,12 +354,12 @@ class PagePool:
 
     @classmethod
     def empty(cls, layers: int, pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
-        """Pages that hold zeros."""
+        """Pages that hold zeros, with the least scale that tadm_page_write gives."""
         import torch
-        z = lambda shape, dt: torch.zeros(shape, dtype=dt, device=device)  # noqa: E731
-        return cls(z((layers, pages, n_kv_heads, PAGE_TOKENS, head_dim), torch.uint8),
-                   z((layers, pages, n_kv_heads, head_dim, PAGE_TOKENS), torch.uint8),
-                   z((layers, pages, n_kv_heads), torch.float32), z((layers, pages, n_kv_heads), torch.float32))
+        z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)  # noqa: E731
+        s = lambda: torch.full((layers, pages, n_kv_heads), 2.0 ** -60, dtype=torch.float32, device=device)  # noqa: E731
+        return cls(z(layers, pages, n_kv_heads, PAGE_TOKENS, head_dim), z(layers, pages, n_kv_heads, head_dim, PAGE_TOKENS),
+                   s(), s())
 
 
 _DTYPES = {}

@@ -5,7 +5,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_serving import T, attend64, close, cum, filled, gen, run_paged  # noqa: E402, F401
+from test_gpu_serving import T, attend64, close, cum, filled, gen, i32, run_paged  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,37 @@ def test_page_attention_beside_large_rows(T, dtype, heads, rows, lens, large):
         ref, absum = attend64(torch.where(grown[s][..., None], 0.0, q[s].double()), k, v, torch.zeros(n, device="cuda"), False, 0)
         keep = ~grown[s]
         close(o[s][keep], ref[keep], absum[keep], dtype, float(v.abs().max()))
+
+
+# ------------------------------------------------------------------ pages that nothing was written to
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [None, 0.0])
+@pytest.mark.parametrize("n", [1, 20])
+def test_unwritten_pages_are_zeros(T, dtype, scale, n):
+    """Pages that a sequence holds but that no row was written to, between pages whose scores are far below zero, in a new
+    pool and in one with scales of zero: their keys have score 0 and value 0."""
+    Hq, Hkv, hd = 8, 4, 128
+    pool, table = T.PagePool.empty(2, 6, Hkv, hd), i32([3, 0, 5, 1]).view(1, 4)
+    if scale is not None:
+        pool.k_scale.fill_(scale), pool.v_scale.fill_(scale)
+    x = torch.randn((64, 2, Hkv, hd), generator=gen(1), device="cuda").to(dtype)
+    x[:, 0] = -4.0                                             # scores of -4 * 4 * 128 / sqrt(128), 261 in log2 units below zero
+    q = torch.full((n, Hq, hd), 4.0, dtype=dtype, device="cuda")
+    for first in (0, 128):
+        T.tadm_page_write(pool, 1, x[:, 0], x[:, 1], i32([0, 64]), i32([first]), table, 64)
+    o = run_paged(T, pool, table, q, [0, n], [220], n, 220, False, 0)
+    assert (o == 0).all()
+    q = -q                                                     # and far above: the written pages have all the weight
+    o = run_paged(T, pool, table, q, [0, n], [220], n, 220, False, 0)
+    k, v = (torch.empty((64, Hkv, hd), dtype=dtype, device="cuda") for _ in range(2))
+    T.tadm_page_read(pool, 1, k, v, i32([0, 64]), i32([0]), table, 64)
+    ref = v.double().mean(0).repeat_interleave(Hq // Hkv, 0).expand(n, Hq, hd)
+    close(o, ref, v.double().abs().mean(0).repeat_interleave(Hq // Hkv, 0).expand(n, Hq, hd), dtype, float(v.abs().max()))
+
+
+def test_empty_pools_have_scales_that_attention_takes(T):
+    pool = T.PagePool.empty(1, 3, 2, 64)
+    for s in (pool.k_scale, pool.v_scale):
+        assert (s == 2.0 ** -60).all()
+    k, v = cached(pool, i32([0, 1, 2]).view(1, 3), 0, 192, layer=0)
+    assert (k == 0).all() and (v == 0).all()

@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(2 * HD, sizeof(T) == 2 ? 1024 / HD : 512 / HD)
   }
   const float amax = __uint_as_float(top);
   const float scale = fmaxf(needed_scale(amax), had);
-  const float again = had > 0.0f ? had / scale : 1.0f;        // what becomes of the tokens that stay
+  const float again = had >= 0.0f ? had / scale : 1.0f;       // what becomes of the tokens that stay (of scale 0: zeros)
   if (tid == 0 && scale != had) *sp = scale;
   const float inv = 1.0f / scale;
   const bool fresh = p.lo == 0;                               // slots past the rows become zeros

@@ -101,3 +101,21 @@ def test_empty_pools_have_scales_that_attention_takes(T):
         assert (s == 2.0 ** -60).all()
     k, v = cached(pool, i32([0, 1, 2]).view(1, 3), 0, 192, layer=0)
     assert (k == 0).all() and (v == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_tokens_of_scale_zero_stay_zeros(T, dtype):
+    """Rows written behind the tokens of a page whose scale is 0: those stay zeros, whatever their bytes are, when the page
+    gets a scale."""
+    pool = T.PagePool.empty(1, 2, 3, 64)
+    for x in (pool.k, pool.v):
+        x.copy_(encode(torch.randn(x.shape, generator=gen(1), device="cuda") * 60))
+    pool.k_scale.zero_(), pool.v_scale.zero_()
+    x = torch.randn((5, 2, 3, 64), generator=gen(2), device="cuda").to(dtype)
+    table = i32([1]).view(1, 1)
+    T.tadm_page_write(pool, 0, x[:, 0], x[:, 1], i32([0, 5]), i32([30]), table, 5)
+    k, v = (torch.empty((35, 3, 64), dtype=dtype, device="cuda") for _ in range(2))
+    T.tadm_page_read(pool, 0, k, v, i32([0, 35]), i32([0]), table, 35)
+    for got, new in ((k, x[:, 0]), (v, x[:, 1])):
+        assert (got[:30] == 0).all()
+        assert ((got[30:] - new).abs() <= 2.0 ** -4 * new.abs().max()).all()

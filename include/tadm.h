@@ -510,8 +510,9 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  * of the same sequence that do not.
  *
  * Arithmetic: fp32 scores, softmax sums and accumulators.  bf16 calls round
- * the probabilities to 8 (tadm_attention_packed) or 11 significant bits
- * (tadm_page_attention) before they multiply V.  tadm_page_attention takes
+ * the probabilities to 8 (tadm_attention_packed; 16 in the tiles of 128 keys that
+ * the mask or the sequence's end cuts) or 11 significant bits (tadm_page_attention)
+ * before they multiply V.  tadm_page_attention takes
  * bf16 q exactly where it is within 2^-12 of the largest finite value of its row
  * and head, and to 2^-20 of that below.  Results repeat from call to
  * call; the last bits of a row may depend on the other sequences' lengths

@@ -16,20 +16,21 @@
 // P (bf16) lies in TMEM over the scores that it was made from, V is read as it
 // lies in memory (a key per line, an MN-major operand).  The reference maximum
 // of a row moves only when a tile exceeds it by 2^8; O is rescaled then.
-// Where a causal row of a tile sees fewer than 256 keys in all, key tiles that
-// the mask cuts keep P in two bf16 terms, whose 128 columns are those of the
-// scores: with few visible keys single probabilities weigh most, and these
-// rows do not feel their rounding to 8 bits.
+// Key tiles that the mask cuts keep P in two bf16 terms, whose 128 columns are
+// those of the scores: a row that sees few keys, or weighs most those next to it,
+// does not feel the rounding of single probabilities to 8 bits, 2^-8 of each (one
+// term where every row sees 256 keys or more: 129 us instead of 133 under a window
+// of 1024, and a row that is all on its own key off by 1.3 times 2^-8).
 // What a tile holds behind the sequence's end belongs to its neighbour: those
 // scores are masked, and those lines of V are zeroed in shared memory.
 //
 // Bound: the tensor pipe, 1024 cycles per 128 x 128 tile at hd 128 (the
 // exponentials take 512).  Measured: about 1450 per tile, 1.34 PFLOP/s over an
-// 8111-token prompt of 32 / 16 heads (448 us with its neighbours; 461 where
-// each block starts and ends by itself, and a window of 1024 over 8900 rows 129
+// 8111-token prompt of 32 / 16 heads (450 us with its neighbours; 461 where
+// each block starts and ends by itself, and a window of 1024 over 8900 rows 133
 // and 157; with 64-key tiles and two S per row tile 587 and 155); prompts of a few hundred tokens are bound by the latency of
 // cut tiles and of the first pair, whose code and rows come from memory (24
-// prompts, 6400 tokens, 16 / 8 heads: 31 us; 43 with the code of cut tiles
+// prompts, 6400 tokens, 16 / 8 heads: 32 us; 43 with the code of cut tiles
 // unrolled over the 128 columns, 36 with the sequences' work in their order).
 #include "ragged.cuh"
 #include "serve.h"
@@ -216,13 +217,6 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     return make_int2(a.window > 0 ? hi - a.window + 1 : 0, a.causal ? lo + 1 : w.n);
   };
   auto partial = [](int2 c, int j) { return (j + 1) * TK > c.y || j * TK < c.x; };
-  // whether tile h keeps P in two terms in cut key tiles: a causal row of it sees fewer than 256 keys; without the causal
-  // rule only a sequence's end and a window's edge cut
-  auto few = [&](const Work& w, int h) {
-    const int seen = w.tok0 + h * a.tq + 1;
-    return !a.causal || (a.window > 0 ? min(seen, a.window) : seen) < 256;
-  };
-
   if (warp < 4) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == 0) {
     // --------------------------------------------------------------- producer
@@ -323,7 +317,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       const int n_keys = uniform(w.n);
       if (n_keys == 0) break;
       const int2 rA = uniform(range(w, 0)), rB = uniform(range(w, 1)), cA = uniform(common(w, 0)), cB = uniform(common(w, 1));
-      const bool fA = uniform(few(w, 0)), fB = uniform(few(w, 1)), two = rB.y > 0;
+      const bool two = rB.y > 0;
       const int j0 = rA.x, j1 = two ? rB.y : rA.y;            // A's keys begin and end no later than B's
       bool ok = early || (wait(&q_full[0], t & 1) && wait(&full[sk.at], sk.parity));
       if (!ok) break;
@@ -353,7 +347,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         }
         tc_fence_after();
         if (j < rA.y) {
-          ok = values(0, sv, nA + j - j0, j == j0, fA && partial(cA, j));
+          ok = values(0, sv, nA + j - j0, j == j0, partial(cA, j));
           if (!ok) break;
           if (j == rA.y - 1) umma_commit(&o_done[0]);
         }
@@ -372,7 +366,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
             }
           }
           if (j >= rB.x) {                                    // (j < rB.y: B's keys end last)
-            ok = values(1, sv, nB + j - rB.x, j == rB.x, fB && partial(cB, j));
+            ok = values(1, sv, nB + j - rB.x, j == rB.x, partial(cB, j));
             if (!ok) break;
             if (j == rB.y - 1) umma_commit(&o_done[1]);
           }
@@ -426,7 +420,6 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         l_run *= factor;
       };
       const int2 all = common(w, h);
-      const bool few_keys = few(w, h);
       for (int j = r.x; j < r.y; ++j, ++n) {
         if (!warp_wait_bounded(&s_full[h], n & 1, abort_flag, nullptr)) { ok = false; break; }
         tc_fence_after();
@@ -446,7 +439,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         if (partial(all, j)) {
           // A cut tile: 32 columns at a time, twice (the maximum, the exponentials), and those that no row of the warp sees
           // are left out.  Rolled, because it runs once or twice per tile of rows and would wait for its instructions.
-          // P goes over the scores that it was made from: two terms of 16 columns for 32, or one closed up.
+          // P goes over the scores that it was made from: two terms of 16 columns for 32.
           const int lim = see_hi - j * TK, lo = see_lo - j * TK;   // visible columns of this tile: [lo, lim)
           uint32_t s[32], pk[16], rest[16];
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -473,12 +466,8 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
 #pragma unroll
               for (int k = 0; k < 16; ++k) pk[k] = rest[k] = 0;
             }
-            if (few_keys) {
-              tmem_st16(t_s + 32 * c, pk);
-              tmem_st16(t_s + 32 * c + 16, rest);
-            } else {
-              tmem_st16(t_s + 16 * c, pk);
-            }
+            tmem_st16(t_s + 32 * c, pk);
+            tmem_st16(t_s + 32 * c + 16, rest);
           }
         } else {
           // the row's scores stay in registers: P is written over them in TMEM

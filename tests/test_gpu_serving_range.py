@@ -119,3 +119,19 @@ def test_tokens_of_scale_zero_stay_zeros(T, dtype):
     for got, new in ((k, x[:, 0]), (v, x[:, 1])):
         assert (got[:30] == 0).all()
         assert ((got[30:] - new).abs() <= 2.0 ** -4 * new.abs().max()).all()
+
+
+# ------------------------------------------------------------------ packed rows that weigh few keys
+@pytest.mark.parametrize("heads", [(8, 8, 128), (4, 4, 64), (8, 4, 128)])
+@pytest.mark.parametrize("n", [300, 1000])
+@pytest.mark.parametrize("window", [0, 200])
+def test_packed_rows_on_their_own_key(T, heads, n, window):
+    """Rows of long prompts whose weight is nearly all on the key at their own position: what is left is the rounding of
+    the output, 2^-8 of it, because the probabilities of the last keys are not rounded to 8 bits."""
+    Hq, Hkv, hd = heads
+    k, v = (torch.randn((n, Hkv, hd), generator=gen(i), device="cuda").bfloat16() for i in range(2))
+    q = (k.float() * (1.0 if hd == 128 else 1.4)).bfloat16().repeat_interleave(Hq // Hkv, 1)
+    o = torch.empty_like(q)
+    T.tadm_attention_packed(q, k, v, o, i32([0, n]), n, window=window)
+    ref, absum = attend64(q.double(), k.double(), v.double(), torch.arange(n, device="cuda"), True, window)
+    close(o, ref, absum, torch.bfloat16, float(v.abs().max()))

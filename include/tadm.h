@@ -504,10 +504,10 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  *
  * Visibility.  Keys j of a row's own sequence; causal: only j <= p, p the
  * row's position; window > 0: only j with p - j < window.  A row that sees no
- * key gets zeros.  K and V of one sequence never reach another one's rows,
- * whatever they hold, nor do keys that no row of their sequence sees reach
- * any; an infinity or NaN in V of a key that one row sees may spread to rows
- * of the same sequence that do not.
+ * key gets zeros, and so does one whose scores are all minus infinity.  K and V
+ * of one sequence never reach another one's rows, whatever they hold, nor do
+ * keys that no row of their sequence sees reach any; an infinity or NaN in V of
+ * a key that one row sees may spread to rows of the same sequence that do not.
  *
  * Arithmetic: fp32 scores, softmax sums and accumulators.  bf16 calls round
  * the probabilities to 8 (tadm_attention_packed; 16 in the tiles of 128 keys that

@@ -434,7 +434,8 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
             m_ref = m_tile;
           }
           if (__any_sync(0xffffffffu, factor != 1.0f)) rescale(factor);
-          return f2_pack(-m_ref, -m_ref);
+          const float negm = m_ref == -INFINITY ? 0.0f : -m_ref;   // (scores of minus infinity alone weigh nothing)
+          return f2_pack(negm, negm);
         };
         if (partial(all, j)) {
           // A cut tile: 32 columns at a time, twice (the maximum, the exponentials), and those that no row of the warp sees

@@ -159,8 +159,9 @@ __global__ void __launch_bounds__(NT) attn_rows_kernel(const RowsAttnArgs a) {
         const bool see1 = v < n_virt && k0 + lane + 32 >= lo && k0 + lane + 32 < hi;
         const float x0 = see0 ? s[i][0] * a.scale : -INFINITY, x1 = see1 ? s[i][1] * a.scale : -INFINITY;
         const float mn = fmaxf(m[i], warp_max(fmaxf(x0, x1)));
-        const float f = m[i] == -INFINITY ? 0.0f : expf(m[i] - mn);
-        const float p0 = see0 ? expf(x0 - mn) : 0.0f, p1 = see1 ? expf(x1 - mn) : 0.0f;
+        const float ref = mn == -INFINITY ? 0.0f : mn;  // (scores of minus infinity alone weigh nothing)
+        const float f = m[i] == -INFINITY ? 0.0f : expf(m[i] - ref);
+        const float p0 = see0 ? expf(x0 - ref) : 0.0f, p1 = see1 ? expf(x1 - ref) : 0.0f;
         sP[(warp + 8 * i) * KT + lane] = p0;
         sP[(warp + 8 * i) * KT + lane + 32] = p1;
         l[i] = l[i] * f + p0 + p1;                     // this lane's keys; the lanes' sums meet at the end

@@ -135,3 +135,60 @@ def test_packed_rows_on_their_own_key(T, heads, n, window):
     T.tadm_attention_packed(q, k, v, o, i32([0, n]), n, window=window)
     ref, absum = attend64(q.double(), k.double(), v.double(), torch.arange(n, device="cuda"), True, window)
     close(o, ref, absum, torch.bfloat16, float(v.abs().max()))
+
+
+# ------------------------------------------------------------------ scores of minus infinity
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads", [(4, 2, 64), (16, 8, 128)])
+@pytest.mark.parametrize("n,hidden", [(300, 200), (300, 128), (300, 64), (700, 513), (40, 40)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 150)])
+def test_packed_scores_of_minus_infinity(T, dtype, heads, n, hidden, causal, window):
+    """The first keys' scores are all minus infinity, over whole key tiles: they weigh nothing, and a row that sees no other
+    key gets zeros as if it saw none."""
+    Hq, Hkv, hd = heads
+    q, k, v = (torch.randn((n, h, hd), generator=gen(h + 1), device="cuda") for h in (Hq, Hkv, Hkv))
+    q[..., 3], k[:hidden, :, 3] = q[..., 3].abs() + 0.1, -math.inf
+    q, k, v = q.to(dtype), k.to(dtype), v.to(dtype)
+    o = torch.empty_like(q)
+    T.tadm_attention_packed(q, k, v, o, i32([0, n]), n, causal=causal, window=window)
+    pos, j = torch.arange(n, device="cuda")[:, None], torch.arange(n, device="cuda")
+    see = (j >= hidden).expand(n, n)
+    if causal:
+        see = see & (j <= pos)
+    if window:
+        see = see & (pos - j < window)
+    kk, vv = (x.double().repeat_interleave(Hq // Hkv, 1) for x in (k, v))
+    kk[:hidden, :, 3] = 0.0
+    x = (torch.einsum("rhd,nhd->hrn", q.double(), kk) / math.sqrt(hd)).masked_fill(~see, -math.inf)
+    w = torch.exp(x - x.amax(-1, keepdim=True).clamp_min(-1e300))
+    w = w / w.sum(-1, keepdim=True).clamp_min(1e-300)
+    close(o, torch.einsum("hrn,nhd->rhd", w, vv), torch.einsum("hrn,nhd->rhd", w, vv.abs()), dtype, float(v.abs().max()))
+    assert (o[~see.any(1)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("causal", [True, False])
+def test_page_scores_of_minus_infinity(T, dtype, causal):
+    """The same over the cache, with K of -448 2^60 (its largest) against a query that takes the scores past fp32."""
+    Hq, Hkv, hd, n, length, hidden = 8, 4, 128, 5, 700, 384
+    pool, table, _ = filled(T, [length], Hkv, hd, 2, nan_tail=False)
+    at = table[0, :hidden // 64].long()
+    pool.k[1, :, :, :, 7] = 0
+    pool.k[1, at, :, :, :] = 0
+    pool.k[1, at, :, :, 7] = 0xFE                               # -448
+    pool.k_scale[1, at] = 2.0 ** 60
+    k, v = cached(pool, table, 0, length)
+    q = torch.randn((n, Hq, hd), generator=gen(3), device="cuda")
+    q[..., 7] = 2.0 ** 70
+    q = q.to(dtype)
+    o = run_paged(T, pool, table, q, [0, n], [length], n, length, causal, 0)
+    pos = torch.arange(length - n, length, device="cuda") - hidden
+    qq = q.double()
+    qq[..., 7] = 0.0
+    ref, absum = attend64(qq, k[hidden:], v[hidden:], pos, causal, 0)
+    if dtype == torch.float32:
+        close(o, ref, absum, dtype, float(v.abs().max()))
+    else:                                                      # q's other channels are below 2^-60 of its largest: no score of theirs is left
+        flat = v[hidden:].repeat_interleave(Hq // Hkv, 1)
+        mean = torch.stack([flat[:int(p) + 1 if causal else None].mean(0) for p in pos])
+        close(o, mean, mean.abs().max().expand_as(mean), dtype, float(v.abs().max()))

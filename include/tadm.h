@@ -600,7 +600,8 @@ TADM_API tadm_status tadm_page_attention(const void* q, const tadm_page_pool* po
  * a fixed order, free pages are taken lowest id first, and status (int32 [1])
  * tells the outcome: 0 done; TADM_PAGES_SHORT not enough free pages;
  * TADM_PAGES_BAD an index out of range, a sequence listed twice, or tables
- * and refs that contradict each other.  If it is not 0, the out arrays are
+ * and refs that contradict each other (pages of the listed sequences and of
+ * the sources of a fork; the others' are not looked at).  If it is not 0, the out arrays are
  * copies of the inputs and no page is written.  scratch: at least
  * tadm_pages_scratch_size() bytes, 16-byte aligned, as above. */
 #define TADM_PAGES_SHORT 1

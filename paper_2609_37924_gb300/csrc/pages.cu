@@ -466,6 +466,10 @@ __global__ void __launch_bounds__(PB) plan_reserve_kernel(const SeqArgs a) {
     for (int i = threadIdx.x >> 5; i < a.n; i += PB / 32) {
       const int have = held(a, a.list[i]), want = a.list2[i];
       if (want < 0 || pages_of(want) > a.ld) ok = false;
+      // a page that it holds and that counts as free would be handed out a second time
+      const int32_t* row = a.tables + static_cast<int64_t>(a.list[i]) * a.ld;
+      for (int j = threadIdx.x & 31; j < have; j += 32)
+        if (row[j] >= a.pages || a.refs[row[j]] <= 0) ok = false;
       if ((threadIdx.x & 31) == 0) {
         a.sc.first[i] = have;
         a.sc.count[i] = max(0, pages_of(max(want, 0)) - have);

@@ -5,7 +5,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_serving import T, attend64, close, cum, filled, gen, i32, run_paged  # noqa: E402, F401
+from test_gpu_serving import Device, Pages, T, attend64, close, cum, filled, gen, i32, run_paged  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -192,3 +192,25 @@ def test_page_scores_of_minus_infinity(T, dtype, causal):
         flat = v[hidden:].repeat_interleave(Hq // Hkv, 1)
         mean = torch.stack([flat[:int(p) + 1 if causal else None].mean(0) for p in pos])
         close(o, mean, mean.abs().max().expand_as(mean), dtype, float(v.abs().max()))
+
+
+# ------------------------------------------------------------------ bookkeeping
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("wrong", ["free", "past", "negative"])
+def test_reserve_finds_contradictions(T, in_place, wrong):
+    """A listed sequence that holds a page which the references call free (it would be handed out a second time), or an id
+    that is no page: refused, nothing changes."""
+    d = Device(T, 20, 6, 40, in_place)
+    assert d.call("tadm_pages_reserve", i32([0, 3]), i32([200, 700]), lens=False) == 0
+    d.lens = i32([130, 0, 0, 700, 0, 0])
+    if wrong == "free":
+        d.refs[int(d.table[3, 9])] = 0
+    elif wrong == "past":
+        d.table[3, 10] = 20
+    else:
+        d.refs[int(d.table[3, 2])] = -1
+    m = Pages(d.table.tolist(), d.lens.tolist(), d.refs.tolist())
+    for seqs, new in (([3], [900]), ([1, 3], [64, 10]), ([3, 0], [64, 64])):
+        assert d.call("tadm_pages_reserve", i32(seqs), i32(new), lens=False) == 2
+        d.same(m)
+    assert d.call("tadm_pages_reserve", i32([0]), i32([300]), lens=False) == 0      # others go on

@@ -166,6 +166,7 @@ def serve(layers=4, prompts=6, branches=3, block=32, blocks=2, tokens=4, heads=1
     live = s.compact()
     for _ in range(tokens):
         x = s.step(rand(len(first)), first, 1, causal=True)
+    T.tadm_ragged_sync_status()
     assert s.lens.tolist() == [n + blocks * block + tokens for n in lens] + [0] * len(others)
     return x, peak, live, s.worst
 

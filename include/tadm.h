@@ -518,6 +518,13 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  * call; the last bits of a row may depend on the other sequences' lengths
  * (tadm_page_attention splits long contexts by the whole call's work). */
 
+/* Waits inside the bf16 attention kernels are bounded: after 4 s without
+ * progress a call gives up.  Rows of it are then not written, or NaN where they
+ * were computed in parts.  This call waits for `stream` and returns
+ * TADM_ERR_TIMEOUT if an attention call of this section gave up on the current
+ * device, on any stream, since it last said so. */
+TADM_API tadm_status tadm_ragged_sync_status(tadm_stream stream);
+
 /* softmax(Q K^T / sqrt(head_dim)) V of whole prompts: row r of a sequence is
  * at position r.  q, o: [total_rows, n_heads, head_dim]; k, v: [total_rows,
  * n_kv_heads, head_dim].  Query head h reads KV head h / (n_heads /

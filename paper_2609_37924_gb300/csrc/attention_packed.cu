@@ -67,6 +67,7 @@ struct PackedArgs {
   int64_t ldo;
   int causal, window;
   float scale_log2;
+  int* status;
 };
 
 // A pair of row tiles: KV head, first row and row count of the sequence (0: no pair is left), first row of the pair in it.
@@ -227,7 +228,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     bool ok = true, asking = false;
     volatile int never = 0;
     for (;; ++t) {
-      if (!warp_wait_bounded(&w_empty[t & 1], ((t >> 1) & 1) ^ 1, abort_flag, nullptr)) break;
+      if (!warp_wait_bounded(&w_empty[t & 1], ((t >> 1) & 1) ^ 1, abort_flag, a.status)) break;
       if (lane == 0) s_work[t & 1] = w;
       warp_arrive(&w_full[t & 1]);
       if (w.n == 0) break;
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       const bool two = rB.y > 0;
       if (lane == 0) {
         for (int h = 0; ok && h < (two ? 2 : 1); ++h) {       // rows behind the sequence's end are other rows, unused
-          ok = mbar_wait_bounded(&q_empty[h], (qn[h] & 1) ^ 1, abort_flag, nullptr);
+          ok = mbar_wait_bounded(&q_empty[h], (qn[h] & 1) ^ 1, abort_flag, a.status);
           if (!ok) break;
           ++qn[h];
           mbar_arrive_expect_tx(&q_full[h], HD / 64 * a.rows * 128);
@@ -245,7 +246,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         for (int j = rA.x; ok && j < (two ? rB.y : rA.y); ++j)
           for (int m = 0; m < 2; ++m, ++g) {
             const int sl = g % NS;
-            if (!mbar_wait_bounded(&empty[sl], ((g / NS) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
+            if (!mbar_wait_bounded(&empty[sl], ((g / NS) & 1) ^ 1, abort_flag, a.status)) { ok = false; break; }
             mbar_arrive_expect_tx(&full[sl], C::TILE_BYTES);
             for (int s = 0; s < HD / 64; ++s)
               tma_load_3d(sKV + sl * C::TILE_BYTES + s * 16384, m ? &tmV : &tmK, &full[sl], 64 * s, w.hk, w.first + j * TK);
@@ -259,7 +260,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         ask_block(s_asked, asked);
       }
       asking = true;
-      if (!warp_wait_bounded(asked, t & 1, abort_flag, nullptr)) break;
+      if (!warp_wait_bounded(asked, t & 1, abort_flag, a.status)) break;
       asking = false;
       const int block = next_block(s_asked);
       fence_proxy_async_smem();                               // the next answer is written there
@@ -268,10 +269,10 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     }
     // every copy started here has landed before the CTA may exit
     if (lane == 0) {
-      if (asking) mbar_wait_bounded(asked, t & 1, &never, nullptr);
+      if (asking) mbar_wait_bounded(asked, t & 1, &never, a.status);
       for (int h = 0; h < 2; ++h)
-        if (qn[h] > 0) mbar_wait_bounded(&q_full[h], (qn[h] - 1) & 1, &never, nullptr);
-      for (int i = max(0, g - NS); i < g; ++i) mbar_wait_bounded(&full[i % NS], (i / NS) & 1, &never, nullptr);
+        if (qn[h] > 0) mbar_wait_bounded(&q_full[h], (qn[h] - 1) & 1, &never, a.status);
+      for (int i = max(0, g - NS); i < g; ++i) mbar_wait_bounded(&full[i % NS], (i / NS) & 1, &never, a.status);
     }
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     };
     auto after = [](Slot s) { return s.at + 1 == NS ? Slot{0, s.parity ^ 1} : Slot{s.at + 1, s.parity}; };
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, nullptr);
+      return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, a.status);
     };
     const uint32_t q_lo = desc_k(smem_u32(sQ)), kv_lo = smem_u32(sKV);
     auto scores = [&](int h, Slot s, bool last) {             // S_h = Q_h K^T, the pair's last ones release Q_h
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     }
     umma_commit(drain);
     volatile int never = 0;
-    warp_wait_bounded(drain, 0, &never, nullptr);
+    warp_wait_bounded(drain, 0, &never, a.status);
   } else if (warp >= 4) {
     // --------------------------------------------------------------- softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::REGS));
@@ -393,7 +394,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
     uint8_t* stage = sO + h * C::STAGE_BYTES;
     int n = 0, used = 0;                                      // scores so far, pairs with this tile
     for (int t = 0;; ++t) {
-      bool ok = warp_wait_bounded(&w_full[t & 1], (t >> 1) & 1, abort_flag, nullptr);
+      bool ok = warp_wait_bounded(&w_full[t & 1], (t >> 1) & 1, abort_flag, a.status);
       if (vote_group<128>(1 + h, !ok)) break;                   // the four warps of a tile leave together
       const Work w = s_work[t & 1];
       warp_arrive(&w_empty[t & 1]);
@@ -421,7 +422,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
       };
       const int2 all = common(w, h);
       for (int j = r.x; j < r.y; ++j, ++n) {
-        if (!warp_wait_bounded(&s_full[h], n & 1, abort_flag, nullptr)) { ok = false; break; }
+        if (!warp_wait_bounded(&s_full[h], n & 1, abort_flag, a.status)) { ok = false; break; }
         tc_fence_after();
         uint64_t ps2[2] = {0, 0};
         // the new reference, from the tile's largest score; O and the sum follow
@@ -505,7 +506,7 @@ __global__ void __launch_bounds__(PackedCfg<HD_, NT_>::THREADS, PackedCfg<HD_, N
         if (partial(all, j)) warp_arrive(&p_full[2 * h]);
         warp_arrive(&p_full[2 * h + 1]);
       }
-      ok = ok && warp_wait_bounded(&o_done[h], used & 1, abort_flag, nullptr);
+      ok = ok && warp_wait_bounded(&o_done[h], used & 1, abort_flag, a.status);
       if (vote_group<128>(1 + h, !ok)) break;
       ++used;
       // O leaves 64 dims at a time.  A tile of whole rows of the sequence is one tensor store, else its rows are copied
@@ -592,7 +593,7 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
       !rows_map(&mk, c.k, HD, c.n_kv, c.total, c.ldk, 1, TK) || !rows_map(&mv, c.v, HD, c.n_kv, c.total, c.ldv, 1, TK))
     return "attention tensor map encode failed";
   const PackedArgs a{static_cast<bf16*>(c.o), c.cu, c.batch, c.total, c.max_rows, group, c.n_kv, tq, tq * group, 65536u / group + 1,
-                     c.ldo, c.causal, c.window, 1.4426950408889634f / sqrtf(static_cast<float>(HD))};
+                     c.ldo, c.causal, c.window, 1.4426950408889634f / sqrtf(static_cast<float>(HD)), c.status};
   // at most one CTA per NT tiles of rows and one more per sequence
   const int64_t blocks = (static_cast<int64_t>(c.total) / (NT * tq) + c.batch) * c.n_kv;
   const cudaError_t e = launch_pdl(attn_packed_kernel<HD, NT>, dim3(static_cast<unsigned>(blocks)), C::THREADS, C::SMEM, s, mq, mk, mv, mo, a);

@@ -79,6 +79,7 @@ struct PagedArgs {
   float* part_o;                           // [2 * CTAs][N][HD]
   float2* part_ml;                         // [2 * CTAs][N]: (reference in log2 units, sum)
   struct Place* place;                     // [CTAs] where each CTA's units begin
+  int* status;
 };
 
 // ------------------------------------------------------------------ work items
@@ -430,6 +431,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
   }
   pdl_enter();
   if (warp == 0) {
+    // what the merge reads of a part that a CTA which gave up a wait did not finish
+    for (int i = lane; i < 2 * N; i += 32) a.part_ml[2LL * blockIdx.x * N + i] = make_float2(NAN, NAN);
     const Place pl = locate<N>(a, blockIdx.x, gridDim.x);
     if (lane == 0) {
       *s_place = pl;
@@ -493,7 +496,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       for (int i = 0; i < now.n; ++i, ++g) {
         const int p0 = __shfl_sync(0xffffffffu, now.id, 2 * i), p1 = __shfl_sync(0xffffffffu, now.id, 2 * i + 1);
         const int st = g % NST;
-        if (!warp_wait_bounded(&kv_empty[st], ((g / NST) & 1) ^ 1, abort_flag, nullptr)) { ok = false; break; }
+        if (!warp_wait_bounded(&kv_empty[st], ((g / NST) & 1) ^ 1, abort_flag, a.status)) { ok = false; break; }
         // the converters are done with tile g - NST, so the softmax is with tile g - 16
         if ((lane >> 1) == i) s_scale[(g & 15) * 2 + (lane & 1)] = now.sc;
         __syncwarp();
@@ -515,13 +518,13 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
     // every copy started here has landed before the CTA may exit (g tiles were issued in ring order)
     volatile int never = 0;
-    for (int i = max(0, g - NST); i < g; ++i) mbar_wait_bounded(&kv_full[i % NST], (i / NST) & 1, &never, nullptr);
+    for (int i = max(0, g - NST); i < g; ++i) mbar_wait_bounded(&kv_full[i % NST], (i / NST) & 1, &never, a.status);
   } else if (warp == 1) {
     // --------------------------------------------------------------- MMA issuer
     constexpr uint32_t idesc_hi = idesc_f8_f32(128, N, false), idesc_lo = idesc_f8_f32(128, N, true), idesc_o = idesc_f16_f32(128, N, true);
     const uint32_t q_lo = desc_k(smem_u32(sQ)), k_lo = desc_k(smem_u32(sKV)), p_lo = desc_mn(smem_u32(sP));
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, nullptr);
+      return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || warp_wait_bounded(bar, parity, abort_flag, a.status);
     };
     uint32_t st = 0, turn = 0, tile = 0;                      // ring place and its parity; tiles so far
     int seg = 0;
@@ -562,7 +565,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     }
     umma_commit(drain);
     volatile int never = 0;
-    warp_wait_bounded(drain, 0, &never, nullptr);
+    warp_wait_bounded(drain, 0, &never, a.status);
   } else if (warp >= 4 && warp < 8) {
     // --------------------------------------------------------------- converters
     const int row = (warp & 3) * 32 + lane;                   // dim of V^T
@@ -575,9 +578,9 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         const int st = g % NST, sb = g & 1;
         const uint32_t again = ((g >> 1) & 1) ^ 1;
         const uint8_t* base = sKV + st * C::STAGE_BYTES;
-        if (!warp_wait_bounded(&kv_full[st], (g / NST) & 1, abort_flag, nullptr)) { ok = false; break; }
+        if (!warp_wait_bounded(&kv_full[st], (g / NST) & 1, abort_flag, a.status)) { ok = false; break; }
         {
-          if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, nullptr)) { ok = false; break; }
+          if (!warp_wait_bounded(&vt_empty[sb], again, abort_flag, a.status)) { ok = false; break; }
           tc_fence_after();
           if (HD == 128 || row < 64) {                        // hd 64: lanes 64 .. 127 of V^T stay as they are, unread
             const int valid = keys - i * TK;                  // keys of this tile that exist
@@ -642,7 +645,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
     };
     while (more) {
       const int qb = seg & 1, rows = fetch();
-      bool ok = warp_wait_bounded(raw_full, seg & 1, abort_flag, nullptr);
+      bool ok = warp_wait_bounded(raw_full, seg & 1, abort_flag, a.status);
       // the largest magnitude of each row, infinities and NaN (an exponent of ones) aside: 64 / N threads per row, which
       // begin at different groups (and banks)
       constexpr int TPR = 64 / N;
@@ -661,7 +664,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       const int e_max = max(static_cast<int>(top >> 23), 40) - 127;      // 2^e_max <= the largest
       s_unit[(seg & 3) * N + own] = static_cast<uint8_t>((e_max - 7 + 127) >> 1);
       asm volatile("barrier.cta.sync 8, 64;" ::: "memory");
-      ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, nullptr) && ok;
+      ok = warp_wait_bounded(&q_empty[qb], ((seg >> 1) & 1) ^ 1, abort_flag, a.status) && ok;
 #pragma unroll 4
       for (int i = 0; i < QV; ++i) {
         const int c = i * 64 + tid, r = c / CPR, ch = c % CPR;
@@ -707,7 +710,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       while (more && w.nt == 0) more = w.next(a);
     }
     volatile int never = 0;                                   // the rows have landed (a warp that gave up)
-    if (seg > 0) mbar_wait_bounded(raw_full, (seg - 1) & 1, &never, nullptr);
+    if (seg > 0) mbar_wait_bounded(raw_full, (seg - 1) & 1, &never, a.status);
   } else {
     // --------------------------------------------------------------- softmax
     constexpr int RN = C::RN;
@@ -751,7 +754,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       const int nt = w.nt, t0 = w.t0;
       for (int i = 0; i < nt; ++i) {
         const int t = g + i, sb = t & 1, tile = t0 + i;
-        if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, nullptr)) { ok = false; }
+        if (!warp_wait_bounded(&s_full[sb], (t >> 1) & 1, abort_flag, a.status)) { ok = false; }
         // the warps vote below: all of them leave together
         tc_fence_after();
         const float4 sc = s_scale[(t & 15) * 2 + (key_lane >> 6)];
@@ -812,7 +815,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
           if (i > 0) {
             // O holds the segment's tiles up to i - 1 once their PV is complete (all but the last are: S of this tile
             // was issued behind them)
-            if (!warp_wait_bounded(o_full, (t - 1) & 1, abort_flag, nullptr)) ok = false;
+            if (!warp_wait_bounded(o_full, (t - 1) & 1, abort_flag, a.status)) ok = false;
             tc_fence_after();
 #pragma unroll
             for (int c = 0; c < RN / 16; ++c) {
@@ -871,7 +874,7 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
         }
       }
       // o_done, not o_full: the PV ahead of the last one may still be running as well
-      ok = warp_wait_bounded(o_done, seg & 1, abort_flag, nullptr);
+      ok = warp_wait_bounded(o_done, seg & 1, abort_flag, a.status);
       ++seg;
       tc_fence_after();
       bar_group<128>(1 + grp);
@@ -1026,7 +1029,7 @@ const char* launch(const RaggedCall& c, cudaStream_t s) {
                     c.ldq, c.ldo, c.causal, c.window,
                     1.4426950408889634f / sqrtf(static_cast<float>(HD)), part,
                     reinterpret_cast<float2*>(part + 2LL * ctas * N * HD),
-                    reinterpret_cast<Place*>(part + 2LL * ctas * N * (HD + 2))};
+                    reinterpret_cast<Place*>(part + 2LL * ctas * N * (HD + 2)), c.status};
   cudaError_t e = launch_pdl(attn_paged_kernel<HD, N>, ctas, C::THREADS, C::SMEM, s, mq, mk, mv, a);
   if (e == cudaSuccess && ctas > 1)
     e = launch_pdl(merge_paged_kernel<HD, N>, dim3(ctas - 1, N / 4), 128, 0, s, a, ctas);

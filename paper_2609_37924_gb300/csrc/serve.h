@@ -44,10 +44,12 @@ struct RaggedCall {
   int64_t ldq, ldk, ldv, ldo;
   int causal, window, bf16;
   void* scratch;
+  int* status;           // this device's status word
 };
 const char* attention_rows(const RaggedCall& c, cudaStream_t s);      // CUDA cores, fp32
 const char* attention_packed(const RaggedCall& c, cudaStream_t s);    // tcgen05, bf16 rows over themselves
 const char* attention_paged(const RaggedCall& c, cudaStream_t s);     // tcgen05, bf16 rows over a pool
 size_t attention_paged_scratch(int max_rows, int group, int head_dim);
+int* ragged_status();                                                 // of the current device; null: it cannot be had
 
 }  // namespace tadm

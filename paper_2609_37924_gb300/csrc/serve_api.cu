@@ -3,9 +3,36 @@
 // and the choice of kernel.
 #include <cstdint>
 
+#include "per_device.h"
 #include "serve.h"
 
 using namespace tadm;
+
+// Set by an attention kernel that gave up a bounded wait, cleared by tadm_ragged_sync_status().
+__device__ int g_ragged_status;
+
+namespace tadm {
+int* ragged_status() {
+  struct Word {
+    int* at[PerDevice::kMax] = {};
+  };
+  static Word word;
+  static PerDevice ready;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= PerDevice::kMax) return nullptr;
+  const int ok = ready.get(dev, [&] {
+    // (no work on a stream: allowed while one is captured)
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) return 0;
+    void* p = nullptr;
+    const bool got = cudaGetSymbolAddress(&p, g_ragged_status) == cudaSuccess;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    word.at[dev] = static_cast<int*>(p);
+    return got ? 1 : 0;
+  });
+  return ok > 0 ? word.at[dev] : nullptr;
+}
+}  // namespace tadm
 
 namespace {
 
@@ -92,6 +119,7 @@ tadm_status tadm_attention_packed(const void* q, const void* k, const void* v, v
   c.n_heads = n_heads, c.n_kv = n_kv_heads, c.head_dim = head_dim;
   c.ldq = ldq, c.ldk = ldk, c.ldv = ldv, c.ldo = ldo;
   c.causal = causal, c.window = window < c.max_rows ? window : 0, c.bf16 = dtype;   // none where no distance reaches it
+  if (dtype && !(c.status = ragged_status())) return TADM_ERR_CUDA;
   return (dtype ? attention_packed(c, stream) : attention_rows(c, stream)) ? TADM_ERR_CUDA : TADM_OK;
 }
 
@@ -143,7 +171,17 @@ tadm_status tadm_page_attention(const void* q, const tadm_page_pool* pool, int l
   c.n_heads = n_heads, c.n_kv = pool->n_kv_heads, c.head_dim = pool->head_dim;
   c.ldq = ldq, c.ldo = ldo, c.causal = causal, c.bf16 = dtype, c.scratch = scratch;
   c.window = window < max_len ? window : 0;                   // none where no distance reaches it
+  if (dtype && !(c.status = ragged_status())) return TADM_ERR_CUDA;
   return (dtype ? attention_paged(c, stream) : attention_rows(c, stream)) ? TADM_ERR_CUDA : TADM_OK;
+}
+
+tadm_status tadm_ragged_sync_status(tadm_stream stream) {
+  int* word = ragged_status();
+  int st = 0;
+  if (!word || cudaStreamSynchronize(stream) != cudaSuccess ||
+      cudaMemcpy(&st, word, sizeof st, cudaMemcpyDeviceToHost) != cudaSuccess || (st && cudaMemset(word, 0, sizeof st) != cudaSuccess))
+    return TADM_ERR_CUDA;
+  return st ? TADM_ERR_TIMEOUT : TADM_OK;
 }
 
 tadm_status tadm_pages_scratch_size(int pages, int n_seqs, size_t* bytes) {

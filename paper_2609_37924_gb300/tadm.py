@@ -26,7 +26,7 @@ ABI_FUNCTIONS = [
     "tadm_head_confidence", "tadm_head_confidence_static", "tadm_probe_breakdown",
     "tadm_remdm_schedule", "tadm_remdm_uniforms", "tadm_remdm_update", "tadm_generate_remdm",
     "tadm_eb_update", "tadm_eb_scratch_bytes", "tadm_generate_entropy_bound",
-    "tadm_attention_packed", "tadm_page_write", "tadm_page_read", "tadm_page_attention_scratch_size",
+    "tadm_ragged_sync_status", "tadm_attention_packed", "tadm_page_write", "tadm_page_read", "tadm_page_attention_scratch_size",
     "tadm_page_attention", "tadm_pages_scratch_size", "tadm_pages_reserve", "tadm_pages_fork", "tadm_pages_free",
     "tadm_pages_compact", "tadm_pages_copy",
 ]
@@ -121,6 +121,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "tadm_eb_scratch_bytes": (I, [P, I, I, I, ctypes.POINTER(SZ)]),
         "tadm_generate_entropy_bound": (I, [P, P, I, I, P, I, I, I, ctypes.c_double, ctypes.c_double,
                                             ctypes.c_double, I, ctypes.c_uint64, P, SZ, P]),
+        "tadm_ragged_sync_status": (I, [P]),
         "tadm_attention_packed": (I, [P] * 5 + [I] * 6 + [I64] * 4 + [I] * 3 + [P]),
         "tadm_page_write": (I, [P, I, P, P, P, P, I, I, I, I64, I64, P, I, I, P]),
         "tadm_page_read": (I, [P, I, P, P, P, P, I, I, I, I64, I64, P, I, I, P]),
@@ -409,6 +410,11 @@ def _scratch_of(t):
     if not t.is_contiguous() or t.get_device() != _device():
         raise TadmError(1, "scratch must be a contiguous tensor on the current device")
     return t.data_ptr(), t.nbytes
+
+
+def tadm_ragged_sync_status(stream=None):
+    """Waits for the stream; an error if an attention call below gave up a bounded wait since the last such error."""
+    _check(load_library().tadm_ragged_sync_status(_stream(stream)))
 
 
 def tadm_attention_packed(q, k, v, o, cu_rows, max_rows: int, causal: bool = True, window: int = 0, stream=None):

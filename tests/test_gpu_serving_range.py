@@ -214,3 +214,26 @@ def test_reserve_finds_contradictions(T, in_place, wrong):
         assert d.call("tadm_pages_reserve", i32(seqs), i32(new), lens=False) == 2
         d.same(m)
     assert d.call("tadm_pages_reserve", i32([0]), i32([300]), lens=False) == 0      # others go on
+
+
+# ------------------------------------------------------------------ status
+def test_no_call_gave_up(T):
+    """What the tests of this file and the calls below left on the device's status word: nothing, on any stream, also
+    where the calls were captured into a graph."""
+    q = torch.randn((40, 4, 64), generator=gen(1), device="cuda").bfloat16()
+    pool, table, _ = filled(T, [300], 2, 64, 1)
+    o, scratch = torch.empty_like(q), torch.empty(T.tadm_page_attention_scratch_size(1, 40, 40, 300, 4, 2, 64, 1), dtype=torch.uint8, device="cuda")
+    cu, lens, s = i32([0, 40]), i32([300]), torch.cuda.Stream()
+
+    def once(stream=None):
+        T.tadm_attention_packed(q, q[:, :2], q[:, 2:], o, cu, 40, stream=stream)
+        T.tadm_page_attention(q, pool, 1, o, cu, lens, table, 40, 300, scratch, stream=stream)
+
+    torch.cuda.synchronize()
+    once(s)
+    T.tadm_ragged_sync_status(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once()
+    graph.replay()
+    T.tadm_ragged_sync_status()

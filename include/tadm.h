@@ -494,7 +494,7 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  * where: sequence b has the rows cu_rows[b] .. cu_rows[b + 1] - 1.  A sequence
  * may have no row.  Rows outside every sequence are neither read nor written.
  * max_rows is at least the longest sequence's row count; rows of a sequence
- * past it are left out.  Row t, head h of an operand starts at element
+ * past it are left out, as if the sequence had no more.  Row t, head h of an operand starts at element
  * t * ld + h * head_dim, ld >= heads * head_dim, so that q, k and v may be
  * slices of one QKV projection's output.  dtype: 0 fp32, 1 bf16, of every row
  * operand of the call.  Pointers are 16-byte aligned and ld * element size is
@@ -509,14 +509,16 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  * keys that no row of their sequence sees reach any; an infinity or NaN in V of
  * a key that one row sees may spread to rows of the same sequence that do not.
  *
- * Arithmetic: fp32 scores, softmax sums and accumulators.  bf16 calls round
- * the probabilities to 8 (tadm_attention_packed; 16 in the tiles of 128 keys that
- * the mask or the sequence's end cuts) or 11 significant bits (tadm_page_attention)
- * before they multiply V.  tadm_page_attention takes
- * bf16 q exactly where it is within 2^-12 of the largest finite value of its row
- * and head, and to 2^-20 of that below.  Results repeat from call to
- * call; the last bits of a row may depend on the other sequences' lengths
- * (tadm_page_attention splits long contexts by the whole call's work). */
+ * Arithmetic: fp32 scores, softmax sums and accumulators.  bf16 calls of
+ * tadm_attention_packed round the probabilities to 8 significant bits before
+ * they multiply V (to 16 in tiles of 128 keys that the mask or the sequence's
+ * end cuts).  bf16 calls of tadm_page_attention take q exactly where it is
+ * within 2^-12 of the largest finite value of its row and head, and to 2^-20 of
+ * that below; they round a key's weight, its probability times its page's V
+ * scale, to 11 significant bits where it is within 2^-21 of its row's largest
+ * weight, and to 2^-32 of that below.  Results repeat from call to call; the last
+ * bits of a row may depend on the other sequences' lengths (tadm_page_attention
+ * splits long contexts by the whole call's work). */
 
 /* Waits inside the bf16 attention kernels are bounded: after 4 s without
  * progress a call gives up.  Rows of it are then not written, or NaN where they
@@ -585,7 +587,7 @@ TADM_API tadm_status tadm_page_read(const tadm_page_pool* pool, int layer, void*
  * ones: row r of n is at position lens[b] - n + r.  A decode step has one row per
  * sequence, a block step block_len rows and causal = 0, a chunk of a prompt
  * many rows and causal = 1.  lens[b] <= max_len <= ld_table * 64; tokens past
- * max_len are left out.  Scales that bf16 calls meet lie within 2^-60 ..
+ * max_len are left out, as if there were no more of them.  Scales that bf16 calls meet lie within 2^-60 ..
  * 2^60, as tadm_page_write makes them, or are 0 (a page of zeros).  scratch: at least
  * tadm_page_attention_scratch_size() bytes (for the current device), 16-byte
  * aligned; it needs no initialisation, and calls that overlap on the GPU need

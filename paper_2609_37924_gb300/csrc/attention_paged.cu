@@ -30,10 +30,11 @@
 // per tile, a large row took the bits of the others); the two terms hold a bf16
 // value exactly if it is within 2^-12 of its row's largest, and to 2^-20 of that
 // below (e5m2, because its steps go down to 2^-16, e4m3's to 2^-9).  K and V are
-// exact, the probabilities
-// times the page's V scale are rounded to f16 (11 bits) with the row's
-// reference at 2^7 to 2^15, so that a probability 2^-21 of the largest still
-// has all of them; scores, sums and O are fp32.
+// exact.  A key's weight, its probability times its page's V scale, is rounded to
+// f16 (11 bits) with the row's largest weight at 2^7 to 2^15, so that a weight of
+// 2^-21 of the largest still has all of them and one below 2^-32 is lost: with
+// equal probabilities, a page whose V scale is that far below another page's.
+// Scores, sums and O are fp32.
 //
 // Bound: the bytes of the cache.  Measured: 4 tokens over 386,544 cached ones (8
 // KV heads of 128) 135 us, 5.9 TB/s; with 64 virtual rows a tile takes 1.1 us

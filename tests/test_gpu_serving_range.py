@@ -237,3 +237,67 @@ def test_no_call_gave_up(T):
         once()
     graph.replay()
     T.tadm_ragged_sync_status()
+
+
+# ------------------------------------------------------------------ pages of different scales
+def by_dim(o, q, k8, v8, ks, vs, dtype):
+    """Each output value against its own dim: what multiplies V in the bf16 form is p s, p the probability and s the page's
+    scale, rounded to f16 (2^-11 of it) or, where it is below 2^-21 of the row's largest p s, to 2^-32 of that; the output to
+    bf16 (2^-8); the rest is fp32."""
+    group = q.shape[1] // k8.shape[1]
+    k8, v8 = k8.repeat_interleave(group, 1), v8.repeat_interleave(group, 1)
+    ks, vs = ks.repeat_interleave(group, 1), vs.repeat_interleave(group, 1)
+    x = torch.einsum("rhd,nhd->hrn", q.double(), k8 * ks[..., None]) / math.sqrt(q.shape[2])
+    w = torch.softmax(x, -1) * vs.T[:, None]
+    ref, absum = torch.einsum("hrn,nhd->rhd", w, v8), torch.einsum("hrn,nhd->rhd", w, v8.abs())
+    tol = 1e-4 * absum
+    if dtype == torch.bfloat16:
+        tol = tol + (2.0 ** -8 + 2.0 ** -11) * absum + 2.0 ** -32 * w.amax(-1).T[..., None] * v8.abs().sum(0)
+    err = (o.double() - ref).abs()
+    assert torch.isfinite(o).all() and (err <= tol).all(), (float((err / tol.clamp_min(1e-300)).max()))
+
+
+def parts(pool, table, n):
+    """Bytes and scales of the first n tokens of the one sequence: k8, v8 [n, heads, hd], ks, vs [n, heads]."""
+    at = table[0, :-(-n // 64)].long()
+    k, v = (x[1, at].view(torch.float8_e4m3fn).double() for x in (pool.k, pool.v))
+    s = [x[1, at].double().repeat_interleave(64, 0)[:n] for x in (pool.k_scale, pool.v_scale)]
+    return k.permute(0, 2, 1, 3).flatten(0, 1)[:n], v.permute(0, 3, 1, 2).flatten(0, 1)[:n], *s
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 4, 33])
+@pytest.mark.parametrize("ratio", [2.0 ** 12, 2.0 ** 18, 2.0 ** 24])
+def test_page_attention_one_large_dim(T, dtype, n, ratio):
+    """The page in the middle has a V scale `ratio` times the others' and zeros in all dims but one: the other dims are the
+    other pages' alone and keep their bits."""
+    Hq, Hkv, hd, length = 8, 4, 128, 600
+    pool, table, _ = filled(T, [length], Hkv, hd, 3, spread=0)
+    page = int(table[0, 4])
+    pool.v[1, page, :, 1:] = 0
+    pool.v_scale[1, page] *= ratio
+    q = (torch.randn((n, Hq, hd), generator=gen(4), device="cuda") * 0.2).to(dtype)
+    o = run_paged(T, pool, table, q, [0, n], [length], n, length, False, 0)
+    by_dim(o, q, *parts(pool, table, length), dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 4, 33])
+@pytest.mark.parametrize("page", [0, 3, 8])
+def test_page_attention_scales_far_apart(T, dtype, n, page):
+    """One page's V scale is 2^40 times the others' and its keys weigh 2^-40 of theirs: both count alike, all are seen at
+    once, and every dim is judged by its own sum."""
+    Hq, Hkv, hd, length = 8, 4, 128, 600
+    pool, table, _ = filled(T, [length], Hkv, hd, 3, spread=0)
+    q = torch.randn((n, Hq, hd), generator=gen(4), device="cuda") * 0.2
+    q[..., 0] = 8.0
+    q = q.to(dtype)
+    at = int(table[0, page])
+    pool.k[1, :, :, :, 0] = 0
+    pool.k_scale[1, at] = 2.0 ** -3
+    pool.k[1, at, :, :, 0] = encode(torch.tensor(-40.0 * math.log(2.0) * math.sqrt(hd) / 8.0 * 8.0)).item()   # score -40 ln 2
+    pool.v_scale[1, at] *= 2.0 ** 40
+    if at == int(table[0, length // 64]):                      # (the page that ends inside: its tail holds NaN)
+        pool.k[1, at, :, length % 64:] = 0x7F
+    o = run_paged(T, pool, table, q, [0, n], [length], n, length, False, 0)
+    by_dim(o, q, *parts(pool, table, length), dtype)

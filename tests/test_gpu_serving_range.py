@@ -301,3 +301,40 @@ def test_page_attention_scales_far_apart(T, dtype, n, page):
         pool.k[1, at, :, length % 64:] = 0x7F
     o = run_paged(T, pool, table, q, [0, n], [length], n, length, False, 0)
     by_dim(o, q, *parts(pool, table, length), dtype)
+
+
+def test_page_moves_past_32_bits(T):
+    """fork and compact on a pool whose K and V are over 4 GB each: page contents and scales of both layers."""
+    Hkv, hd, pages = 8, 128, 34000
+    k = torch.empty((2, pages, Hkv, 64, hd), dtype=torch.uint8, device="cuda")
+    v = torch.empty((2, pages, Hkv, hd, 64), dtype=torch.uint8, device="cuda")
+    scales = [torch.ones((2, pages, Hkv), dtype=torch.float32, device="cuda") for _ in range(2)]
+    assert k.numel() > 1 << 32
+    pool = T.PagePool(k, v, *scales)
+    own = [pages - 1, pages - 3, pages - 4]
+    for i, x in enumerate((k, v)):
+        x[:, own] = torch.randint(0, 256, (2, 3, Hkv) + tuple(x.shape[3:]), generator=gen(i), device="cuda").to(torch.uint8)
+    for i, s in enumerate(scales):
+        s[:, own] = torch.rand((2, 3, Hkv), generator=gen(9 + i), device="cuda")
+    before = [x[:, own].clone() for x in (k, v, *scales)]
+    refs = torch.ones(pages, dtype=torch.int32, device="cuda")
+    refs[pages - 2] = 0                                        # the only free page
+    tables = torch.full((2, 3), -1, dtype=torch.int32, device="cuda")
+    tables[0] = i32(own)
+    lens, status = i32([150, 0]), i32([7])
+    scratch = torch.empty(T.tadm_pages_scratch_size(pages, 2), dtype=torch.uint8, device="cuda")
+    T.tadm_pages_fork(pool, tables, lens, refs, i32([0]), i32([1]), tables, lens, refs, status, scratch)
+    assert int(status) == 0 and tables.tolist() == [own, own[:2] + [pages - 2]] and lens.tolist() == [150, 150]
+    assert refs[own].tolist() == [2, 2, 1] and int(refs[pages - 2]) == 1
+    for x, b in zip((k, v, *scales), before):
+        assert torch.equal(x[:, pages - 2], b[:, 2]) and torch.equal(x[:, own], b)
+    refs.zero_()
+    refs[own], refs[pages - 2] = i32([2, 2, 1]), 1
+    refs[0] = refs[33000] = 1                                  # pages of nobody else's table: 0 stays, 33000 moves too
+    T.tadm_pages_compact(pool, tables, refs, tables, refs, status, scratch)
+    # in use: 0, 33000, then the four in ascending order; they take 1 .. 5
+    to = {33000: 1, pages - 4: 2, pages - 3: 3, pages - 2: 4, pages - 1: 5}
+    assert int(status) == 6 and tables.tolist() == [[to[p] for p in own], [to[p] for p in own[:2]] + [to[pages - 2]]]
+    assert refs[:6].tolist() == [1, 1, 1, 2, 1, 2] and int(refs.sum()) == 8
+    for x, b in zip((k, v, *scales), before):
+        assert torch.equal(x[:, [to[p] for p in own]], b) and torch.equal(x[:, 4], b[:, 2])

@@ -140,3 +140,17 @@ def test_strides_of_single_rows_and_heads_do_not_matter(lib):
     assert leading.pop() == (64, 64, 64, 64)
     with pytest.raises(tadm.TadmError):
         tadm.tadm_attention_packed(*[Cuda(torch.zeros((2, 5, 64), dtype=torch.bfloat16).transpose(0, 1)) for _ in range(4)], ints(2), 5)
+
+
+def test_stream_and_device_without_torchs_private_functions(monkeypatch):
+    """The quick lookups of the current stream and device are not part of torch's interface: where a version lacks them, its
+    public ones serve."""
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    monkeypatch.setattr(torch.cuda, "init", lambda: None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: type("S", (), {"cuda_stream": 77})())
+    monkeypatch.setattr(tadm, "_raw_stream", None)
+    monkeypatch.setattr(tadm, "_current_device", None)
+    assert tadm._stream() == 77 and tadm._device() == 3
+    assert tadm._stream(type("S", (), {"cuda_stream": 5})()) == 5

@@ -587,9 +587,10 @@ TADM_API tadm_status tadm_page_read(const tadm_page_pool* pool, int layer, void*
  * ones: row r of n is at position lens[b] - n + r.  A decode step has one row per
  * sequence, a block step block_len rows and causal = 0, a chunk of a prompt
  * many rows and causal = 1.  lens[b] <= max_len <= ld_table * 64; tokens past
- * max_len are left out, as if there were no more of them.  Scales that bf16 calls meet lie within 2^-60 ..
- * 2^60, as tadm_page_write makes them, or are 0 (a page of zeros).  scratch: at least
- * tadm_page_attention_scratch_size() bytes (for the current device), 16-byte
+ * max_len are left out, as if there were no more of them.  Scales that bf16
+ * calls meet lie within 2^-60 .. 2^60, as tadm_page_write makes them, or are 0 (a
+ * page of zeros).  scratch: at least tadm_page_attention_scratch_size() bytes
+ * (for the current device; batch and max_len do not change them), 16-byte
  * aligned; it needs no initialisation, and calls that overlap on the GPU need
  * one each. */
 TADM_API tadm_status tadm_page_attention_scratch_size(int batch, int total_rows, int max_rows, int max_len,

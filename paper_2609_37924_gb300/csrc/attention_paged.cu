@@ -115,9 +115,10 @@ __device__ __forceinline__ int2 tile_range(const PagedArgs& a, const SeqInfo& s,
   return tiles_of(key_range<N>(a, s, rt));
 }
 // An item's units: its tiles, then kItemUnits for its start and end (Q, the
-// first references, the sums, O), measured in tiles (32 block steps over 1 to
-// 2000 tokens: 49 us with 3, 43.6 with 5, 42.4 with 8); a row tile that sees
-// nothing has zeros to write there.
+// first references, the sums, O), measured in tiles (32 block steps of 32 rows over
+// 1 to 2000 tokens / 8 over 3000 to 30,000: 46.4 / 105 us with 3, 43.1 / 102.7
+// with 5, 43.3 / 103.2 with 6, 43.3 / 104.4 with 8, 44.2 / 106 with 10; the middle
+// of what serves both); a row tile that sees nothing has zeros to write there.
 constexpr int kItemUnits = 6;
 // Units of a sequence and KV head.
 template <int N>
@@ -270,7 +271,7 @@ struct PagedCfg {
   static constexpr int QT_BYTES = N * HD, Q_BYTES = 2 * QT_BYTES;   // two terms of N rows; two buffers
   static constexpr int RAW_BYTES = N * HD * 2;               // Q as it is in memory
   static constexpr int P_BYTES = TK * 128;                   // a 128-byte line of up to 64 rows per key, f16
-  static constexpr int RN = 16, GROUPS = N / RN;   // rows per softmax thread, groups of four softmax warps
+  static constexpr int RN = 16, GROUPS = N / RN;   // rows per softmax thread (its loads from TMEM have 16 columns), groups of four softmax warps
   static constexpr int SM_THREADS = 128 * GROUPS;
   static constexpr int THREADS = 256 + SM_THREADS;
   static constexpr int MISC = 3328 + N * 44;
@@ -286,7 +287,7 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
       "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
       : "memory");
 }
-// D(tmem) (+)= A(tmem) * B(smem)^T for f16 operands is umma_bf16_ts with another instruction descriptor.
+// A and B: f16, B K-major or MN-major
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool b_mn_major) {
   return (1u << 4) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
@@ -818,14 +819,11 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
             // was issued behind them)
             if (!warp_wait_bounded(o_full, (t - 1) & 1, abort_flag, a.status)) ok = false;
             tc_fence_after();
+            float y[RN];
+            tmem_ld16(tmem + lane_off + C::O_COL + row0, y);
 #pragma unroll
-            for (int c = 0; c < RN / 16; ++c) {
-              float y[16];
-              tmem_ld16(tmem + lane_off + C::O_COL + row0 + 16 * c, y);
-#pragma unroll
-              for (int k = 0; k < 16; ++k) y[k] *= s_fac[row0 + 16 * c + k];
-              tmem_st16(tmem + lane_off + C::O_COL + row0 + 16 * c, y);
-            }
+            for (int r = 0; r < RN; ++r) y[r] *= s_fac[row0 + r];
+            tmem_st16(tmem + lane_off + C::O_COL + row0, y);
             tmem_wait_st();
 #pragma unroll
             for (int r = 0; r < RN; ++r) l[r] *= s_fac[row0 + r];
@@ -856,14 +854,8 @@ __global__ void __launch_bounds__(PagedCfg<HD_, N_>::THREADS, 1)
       if (!ok) break;
       g += nt;
       // ---- the rows' sums, then O
-#pragma unroll
-      for (int c = 0; c < RN; c += 16) {
-        float y[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) y[k] = l[c + k];
-        const float s = sum_rows(y);
-        if (lane < 16) my_red[c + lane] = s;
-      }
+      const float l_row = sum_rows(l);
+      if (lane < RN) my_red[lane] = l_row;
       bar_group<128>(1 + grp);
       if (tid < RN) {
         const float s = (s_red[own] + s_red[N + own]) + (s_red[2 * N + own] + s_red[3 * N + own]);

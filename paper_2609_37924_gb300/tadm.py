@@ -372,42 +372,40 @@ def _torch_types():
     return _DTYPES
 
 
-def _rows_of(*tensors):
-    """The dtype code of row operands [rows, heads, hd]: fp32 or bf16, each row's heads dense, on the current device."""
-    kind, device = tensors[0].dtype, _device()
+def _rows_of(device, *tensors):
+    """The dtype code of row operands [rows, heads, hd] (fp32 or bf16, each row's heads dense, on the device), and for each the
+    elements from one row to the next.  The strides of a single row or head do not matter."""
+    kind = tensors[0].dtype
     dtype = (_DTYPES or _torch_types()).get(kind)
     if dtype not in (0, 1):
         raise TadmError(1, f"rows must be fp32 or bf16, not {kind}")
+    ld = []
     for t in tensors:
         s, n = t.stride(), t.shape
         if len(s) != 3 or s[2] != 1 or (s[1] != n[2] and n[1] != 1) or t.dtype is not kind or t.get_device() != device:
             raise TadmError(1, "rows must be tensors [rows, heads, head_dim] of one type with dense heads on the current device")
-    return dtype
+        ld.append(s[0] if n[0] != 1 else n[1] * n[2])
+    return dtype, ld
 
 
-def _ld(t) -> int:
-    """Elements from one row to the next (a single row may have any stride)."""
-    return t.stride(0) if t.shape[0] != 1 else t.shape[1] * t.shape[2]
-
-
-def _ints_of(*tensors):
-    types, device = _DTYPES or _torch_types(), _device()
+def _ints_of(device, *tensors):
+    types = _DTYPES or _torch_types()
     for t in tensors:
         if types.get(t.dtype) != "int32" or not t.is_contiguous() or t.get_device() != device:
             raise TadmError(1, "lengths, tables and lists must be contiguous int32 tensors on the current device")
 
 
-def _pool_of(pool):
-    if pool.index != _device():
+def _pool_of(device, pool):
+    if pool.index != device:
         raise TadmError(1, "the page pool is not on the current device")
     return pool.ref
 
 
-def _scratch_of(t):
+def _scratch_of(device, t):
     """Address and size of scratch memory; none at all is no address."""
     if t is None:
         return None, 0
-    if not t.is_contiguous() or t.get_device() != _device():
+    if not t.is_contiguous() or t.get_device() != device:
         raise TadmError(1, "scratch must be a contiguous tensor on the current device")
     return t.data_ptr(), t.nbytes
 
@@ -421,23 +419,25 @@ def tadm_attention_packed(q, k, v, o, cu_rows, max_rows: int, causal: bool = Tru
     """Attention of whole prompts packed one after the other: q, o [rows,
     heads, hd], k, v [rows, kv heads, hd] (fp32 or bf16, rows may be strided),
     cu_rows int32 [batch + 1]."""
-    dtype = _rows_of(q, k, v, o)
-    _ints_of(cu_rows)
+    device = _device()
+    dtype, ld = _rows_of(device, q, k, v, o)
+    _ints_of(device, cu_rows)
     shape, kv = q.shape, k.shape
     rows, heads, hd = shape
     if o.shape != shape or kv != v.shape or kv[0] != rows or kv[2] != hd:
         raise TadmError(1, "shapes of q, k, v and o do not agree")
     status = load_library().tadm_attention_packed(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), cu_rows.data_ptr(), cu_rows.shape[0] - 1, rows,
-        max_rows, heads, kv[1], hd, _ld(q), _ld(k), _ld(v), _ld(o), 1 if causal else 0, window,
+        max_rows, heads, kv[1], hd, *ld, 1 if causal else 0, window,
         dtype, _stream(stream))
     if status:
         _check(status)
 
 
 def _page_rows(call, pool, layer, k, v, cu_rows, start, table, max_rows, stream):
-    dtype = _rows_of(k, v)
-    _ints_of(cu_rows, start, table)
+    device = _device()
+    dtype, ld = _rows_of(device, k, v)
+    _ints_of(device, cu_rows, start, table)
     shape = k.shape
     rows, heads, hd = shape
     if shape != v.shape or heads != pool.n_kv_heads or hd != pool.head_dim:
@@ -446,8 +446,8 @@ def _page_rows(call, pool, layer, k, v, cu_rows, start, table, max_rows, stream)
     seqs, width = table.shape
     if start.shape[0] != batch or seqs < batch:
         raise TadmError(1, "start and table need an entry per sequence")
-    status = call(_pool_of(pool), layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, rows, max_rows,
-                  _ld(k), _ld(v), table.data_ptr(), width, dtype, _stream(stream))
+    status = call(_pool_of(device, pool), layer, k.data_ptr(), v.data_ptr(), cu_rows.data_ptr(), start.data_ptr(), batch, rows, max_rows,
+                  *ld, table.data_ptr(), width, dtype, _stream(stream))
     if status:
         _check(status)
 
@@ -474,8 +474,9 @@ def tadm_page_attention(q, pool, layer: int, o, cu_rows, lens, table, max_rows: 
                         causal: bool = False, window: int = 0, stream=None):
     """Attention of packed rows q, o [rows, heads, hd] over the cache: sequence b
     sees its first lens[b] tokens, its rows are the last ones of them."""
-    dtype = _rows_of(q, o)
-    _ints_of(cu_rows, lens, table)
+    device = _device()
+    dtype, ld = _rows_of(device, q, o)
+    _ints_of(device, cu_rows, lens, table)
     shape = q.shape
     rows, heads, hd = shape
     batch = cu_rows.shape[0] - 1
@@ -483,9 +484,9 @@ def tadm_page_attention(q, pool, layer: int, o, cu_rows, lens, table, max_rows: 
     if o.shape != shape or hd != pool.head_dim or lens.shape[0] != batch or seqs < batch:
         raise TadmError(1, "shapes of q, o, lens, table and the pool do not agree")
     status = load_library().tadm_page_attention(
-        q.data_ptr(), _pool_of(pool), layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
-        max_len, heads, _ld(q), _ld(o), table.data_ptr(), width, 1 if causal else 0, window, dtype,
-        *_scratch_of(scratch), _stream(stream))
+        q.data_ptr(), _pool_of(device, pool), layer, o.data_ptr(), cu_rows.data_ptr(), lens.data_ptr(), batch, rows, max_rows,
+        max_len, heads, *ld, table.data_ptr(), width, 1 if causal else 0, window, dtype,
+        *_scratch_of(device, scratch), _stream(stream))
     if status:
         _check(status)
 
@@ -497,59 +498,62 @@ def tadm_pages_scratch_size(pages: int, n_seqs: int) -> int:
 
 
 def _seqs_of(tables, tables_out, per_seq, refs, refs_out, lists, status):
-    _ints_of(tables, tables_out, refs, refs_out, status, *per_seq, *lists)
+    device = _device()
+    _ints_of(device, tables, tables_out, refs, refs_out, status, *per_seq, *lists)
     if tables_out.shape != tables.shape or refs_out.shape != refs.shape or any(
             t.shape[0] != tables.shape[0] for t in per_seq) or any(t.shape != lists[0].shape for t in lists):
         raise TadmError(1, "shapes of tables, lens, refs and lists do not agree")
     if status.numel() < 1:
         raise TadmError(1, "the outcome needs an element")
+    return device
 
 
 def tadm_pages_reserve(tables, refs, seqs, new_len, tables_out, refs_out, status, scratch, stream=None):
     """The pages that sequences seqs lack for new_len tokens, lowest free ids first."""
-    _seqs_of(tables, tables_out, (), refs, refs_out, (seqs, new_len), status)
+    device = _seqs_of(tables, tables_out, (), refs, refs_out, (seqs, new_len), status)
     _check(load_library().tadm_pages_reserve(
         tables.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1], seqs.data_ptr(),
         new_len.data_ptr(), seqs.shape[0], tables_out.data_ptr(), refs_out.data_ptr(), status.data_ptr(),
-        *_scratch_of(scratch), _stream(stream)))
+        *_scratch_of(device, scratch), _stream(stream)))
 
 
 def tadm_pages_fork(pool, tables, lens, refs, src, dst, tables_out, lens_out, refs_out, status, scratch, stream=None):
     """Sequences dst become copies of src: full pages shared, the last page copied."""
-    _seqs_of(tables, tables_out, (lens, lens_out), refs, refs_out, (src, dst), status)
+    device = _seqs_of(tables, tables_out, (lens, lens_out), refs, refs_out, (src, dst), status)
     if refs.shape[0] != pool.pages:
         raise TadmError(1, "refs needs an entry per page")
     _check(load_library().tadm_pages_fork(
-        _pool_of(pool), tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1],
+        _pool_of(device, pool), tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1],
         src.data_ptr(), dst.data_ptr(), src.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
-        status.data_ptr(), *_scratch_of(scratch), _stream(stream)))
+        status.data_ptr(), *_scratch_of(device, scratch), _stream(stream)))
 
 
 def tadm_pages_free(tables, lens, refs, seqs, tables_out, lens_out, refs_out, status, scratch, stream=None):
     """Sequences seqs give their pages back."""
-    _seqs_of(tables, tables_out, (lens, lens_out), refs, refs_out, (seqs,), status)
+    device = _seqs_of(tables, tables_out, (lens, lens_out), refs, refs_out, (seqs,), status)
     _check(load_library().tadm_pages_free(
         tables.data_ptr(), lens.data_ptr(), refs.data_ptr(), refs.shape[0], tables.shape[0], tables.shape[1],
         seqs.data_ptr(), seqs.shape[0], tables_out.data_ptr(), lens_out.data_ptr(), refs_out.data_ptr(),
-        status.data_ptr(), *_scratch_of(scratch), _stream(stream)))
+        status.data_ptr(), *_scratch_of(device, scratch), _stream(stream)))
 
 
 def tadm_pages_compact(pool, tables, refs, tables_out, refs_out, n_live, scratch, stream=None):
     """Pages in use move to the lowest ids; n_live int32 [1] gets their number."""
-    _seqs_of(tables, tables_out, (), refs, refs_out, (), n_live)
+    device = _seqs_of(tables, tables_out, (), refs, refs_out, (), n_live)
     if refs.shape[0] != pool.pages:
         raise TadmError(1, "refs needs an entry per page")
     _check(load_library().tadm_pages_compact(
-        _pool_of(pool), tables.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1], tables_out.data_ptr(),
-        refs_out.data_ptr(), n_live.data_ptr(), *_scratch_of(scratch), _stream(stream)))
+        _pool_of(device, pool), tables.data_ptr(), refs.data_ptr(), tables.shape[0], tables.shape[1], tables_out.data_ptr(),
+        refs_out.data_ptr(), n_live.data_ptr(), *_scratch_of(device, scratch), _stream(stream)))
 
 
 def tadm_pages_copy(pool, src, dst, stream=None):
     """Page src[i] onto page dst[i] in every layer."""
-    _ints_of(src, dst)
+    device = _device()
+    _ints_of(device, src, dst)
     if src.shape != dst.shape:
         raise TadmError(1, "src and dst differ in length")
-    _check(load_library().tadm_pages_copy(_pool_of(pool), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream(stream)))
+    _check(load_library().tadm_pages_copy(_pool_of(device, pool), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream(stream)))
 
 
 # ---------------------------------------------------------------------------- model handle

@@ -24,7 +24,8 @@
  *    weight [n_out, n_in] (y = x W^T).
  *  - Calls that take a stream only enqueue work on it and return at once;
  *    kernels that give up a bounded wait set a device status word that
- *    tadm_sync_status() turns into TADM_ERR_TIMEOUT.  Argument errors are
+ *    tadm_sync_status() turns into TADM_ERR_TIMEOUT (those of attention over
+ *    packed rows and pages: tadm_ragged_sync_status()).  Argument errors are
  *    detected on the host, before anything is enqueued.
  *  - No call throws, aborts or exits.  On error the returned status is
  *    non-zero and tadm_last_error() describes it.
@@ -492,7 +493,7 @@ TADM_API tadm_status tadm_generate_entropy_bound(tadm_handle* h, const int32_t* 
  * Packed rows.  The rows of `batch` sequences lie one after the other;
  * cu_rows (int32 [batch + 1], not decreasing, within 0 .. total_rows) says
  * where: sequence b has the rows cu_rows[b] .. cu_rows[b + 1] - 1.  A sequence
- * may have no row.  Rows outside every sequence are neither read nor written.
+ * may have no row.  Rows outside every sequence reach none and are not written.
  * max_rows is at least the longest sequence's row count; rows of a sequence
  * past it are left out, as if the sequence had no more.  Row t, head h of an operand starts at element
  * t * ld + h * head_dim, ld >= heads * head_dim, so that q, k and v may be

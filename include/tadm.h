@@ -657,6 +657,84 @@ TADM_API tadm_status tadm_pages_compact(const tadm_page_pool* pool, const int32_
 TADM_API tadm_status tadm_pages_copy(const tadm_page_pool* pool, const int32_t* src, const int32_t* dst, int n,
                                      tadm_stream stream);
 
+/* ------------------------------------------------ requests with settings of their own --
+ * What lies around attention in a serving step, for rows of many requests at
+ * once: tokens drawn with each row's own settings, projections with each
+ * request's own adapter, the norms between the blocks of a layer.  Packed rows
+ * are those of the section above: sequence b has the rows cu_rows[b] ..
+ * cu_rows[b + 1] - 1, rows outside every sequence reach none and are not
+ * written.  No handle; all pointers are device pointers, and every call only
+ * enqueues work. */
+
+/* One token per row of logits [rows, vocab] (row stride ld elements; dtype 0
+ * fp32, 1 bf16), which are read only.
+ *  - Candidates of a row: ids other than mask_id (-1: none is masked) whose logit
+ *    is not -infinity; NaN counts as -infinity.  A row without one gets token -1
+ *    and probability 0.
+ *  - Order: falling logit, equal ones by rising id.  w_v = exp((l_v - max) / T);
+ *    where the maximum is +infinity, the ids that have it weigh 1 and the others 0.
+ *  - Kept, each a first part of the order: with top_k[row] > 0 the first top_k
+ *    ids; with min_p[row] > 0 those with w >= min(min_p, 1); with top_p[row] < 1
+ *    those with less than top_p of the mass (of what top_k and min_p leave) in
+ *    front of them; always the first.
+ *  - The token is the first kept id, in the order of ids, whose cumulative weight
+ *    exceeds u[row] times the kept ids' mass.  u in [0, 1); 1 and above take the
+ *    last kept id that weighs anything, NaN and values below 0 count as 0.
+ *  - temperature[row] <= 2^-100 or NaN: the first of the order, whatever the
+ *    other settings.  temperature NULL: 1; top_k, top_p, min_p NULL: off.
+ *  - prob (optional): the token's weight over the kept ids' mass.
+ * Weights are whole multiples of 2^-44 of the largest (smaller ones are none), right to about 2^-35, their sums
+ * exact: results repeat, do not depend on the other rows, and are those of
+ * exact arithmetic unless u or a cut lies that close to a border.  vocab is
+ * at most 400,000 (TADM_ERR_UNSUPPORTED above).  Rows may start at any element. */
+TADM_API tadm_status tadm_sample(const void* logits, int64_t ld, int rows, int vocab, int mask_id,
+                                 const float* temperature, const int32_t* top_k, const float* top_p,
+                                 const float* min_p, const float* u, int32_t* tok, float* prob, int dtype,
+                                 tadm_stream stream);
+
+/* y[t] = W x[t] + lora_scale[a] B_a (A_a x[t]) for the rows t of each sequence,
+ * a = adapter[b] of its sequence (int32 [batch]; outside 0 .. n_adapters - 1:
+ * no adapter, y = W x).  x: [total_rows, n_in], W: [n_out, n_in], y:
+ * [total_rows, n_out] (row strides ldx, ldw, ldy in elements); lora_a:
+ * [n_adapters, rank, n_in], lora_b: [n_adapters, n_out, rank], both contiguous;
+ * lora_scale: fp32 [n_adapters].  dtype: 0 fp32, 1 bf16, of x, W, lora_a and
+ * lora_b; y_dtype 0 or 1 for bf16 calls, 0 for fp32 ones.  x, W, lora_a and
+ * lora_b are 16-byte aligned, n_in, ldx and ldw times the element size multiples
+ * of 16, rank a multiple of 8 up to 256 (adapters of a lower rank: zeros behind
+ * their rows of A and columns of B).  y must not overlap the inputs.
+ *
+ * Sums are fp32.  bf16 calls carry A_a x (times the scale) to 16 significant
+ * bits.  W and the adapters that the call uses hold finite values; other adapters
+ * are not read, and x of a row, whatever it holds, reaches that row alone.
+ * scratch: at least tadm_lora_scratch_size() bytes, 16-byte aligned; it needs no
+ * initialisation, and calls that overlap on the GPU need one each.  Waits are
+ * bounded as in the attention calls above: tadm_ragged_sync_status() tells. */
+TADM_API tadm_status tadm_lora_scratch_size(int batch, int total_rows, int n_in, int n_out, int n_adapters, int rank,
+                                            int dtype, size_t* bytes);
+TADM_API tadm_status tadm_lora_project(const void* x, const void* w, void* y, const int32_t* cu_rows,
+                                       const int32_t* adapter, int batch, int total_rows, int n_in, int n_out,
+                                       int64_t ldx, int64_t ldw, int64_t ldy, const void* lora_a, const void* lora_b,
+                                       const float* lora_scale, int n_adapters, int rank, int dtype, int y_dtype,
+                                       void* scratch, size_t scratch_bytes, tadm_stream stream);
+
+/* The norms around a block of a layer and its residual add, per row of width d:
+ *   u     = y * rsqrt(mean(y^2) + eps) * post_gain     (post_gain NULL: u = y)
+ *   x_out = residual_scale * x + gate[b] * u           (gate NULL: without it)
+ *   n_out = x_out * rsqrt(mean(x_out^2) + eps) * pre_gain  (pre_gain NULL: no gain; n_out NULL: not wanted)
+ * gate: [batch, d], a row per sequence (row stride ldg).  cu_rows NULL: every
+ * row is in sequence 0 (batch 1).  x_dtype: type of x and x_out; y_dtype: of y;
+ * dtype: of post_gain, gate, pre_gain and n_out (each 0 fp32, 1 bf16).  All
+ * arithmetic is fp32; n_out is made from x_out before it is rounded to its type.
+ * x_out may be x (with its stride) and n_out may be y (of the same type and
+ * stride); other overlaps are not allowed.  Any d up to 49152
+ * (TADM_ERR_UNSUPPORTED above), any strides of at least d, any alignment;
+ * widths that are a multiple of 8 with rows on 16 bytes are the fast ones. */
+TADM_API tadm_status tadm_residual_norm(const void* x, const void* y, void* x_out, void* n_out, const int32_t* cu_rows,
+                                        int batch, int total_rows, int d, int64_t ldx, int64_t ldy, int64_t ldxo,
+                                        int64_t ldn, const void* post_gain, const void* gate, int64_t ldg,
+                                        const void* pre_gain, float residual_scale, float eps, int x_dtype,
+                                        int y_dtype, int dtype, tadm_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,6 +14,23 @@ __device__ __forceinline__ SeqRows seq_rows(const int32_t* cu, int b, int total,
   return {c0, min(c1 - c0, max_rows)};
 }
 
+// The sequence of row `row`: cu[b] <= row < cu[b + 1]; -1: it is in none.  Warp-collective, for a row that the warp's lanes
+// share; 32 boundaries per step, so that 1024 sequences take two reads one after the other.
+__device__ __forceinline__ int seq_of_row(const int32_t* cu, int batch, int row) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = batch + 1;                                  // the boundaries <= row end in lo .. lo + n
+  while (n > 0) {
+    const int step = (n + 31) / 32, at = lo + lane * step;
+    const bool le = at < lo + n && cu[at] <= row;
+    const int hits = __popc(__ballot_sync(0xffffffffu, le));
+    if (hits == 0) return lo - 1;
+    const int last = lo + (hits - 1) * step;                  // a boundary <= row; the next one asked about is not
+    n = min(lo + n, last + step) - (last + 1);
+    lo = last + 1;
+  }
+  return lo - 1 < batch ? lo - 1 : -1;
+}
+
 // Row tile `tile` of all sequences' tiles, sequence by sequence; tiles_of(b)
 // says how many sequence b has.  Returns the sequence (-1: there are fewer
 // tiles) and the tile's index in it.  Warp-collective, 32 sequences per step.

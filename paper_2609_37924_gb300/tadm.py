@@ -29,6 +29,7 @@ ABI_FUNCTIONS = [
     "tadm_ragged_sync_status", "tadm_attention_packed", "tadm_page_write", "tadm_page_read", "tadm_page_attention_scratch_size",
     "tadm_page_attention", "tadm_pages_scratch_size", "tadm_pages_reserve", "tadm_pages_fork", "tadm_pages_free",
     "tadm_pages_compact", "tadm_pages_copy",
+    "tadm_sample", "tadm_lora_scratch_size", "tadm_lora_project", "tadm_residual_norm",
 ]
 
 
@@ -133,6 +134,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "tadm_pages_free": (I, [P, P, P, I, I, I, P, I, P, P, P, P, P, SZ, P]),
         "tadm_pages_compact": (I, [P, P, P, I, I, P, P, P, P, SZ, P]),
         "tadm_pages_copy": (I, [P, P, P, I, P]),
+        "tadm_sample": (I, [P, I64, I, I, I] + [P] * 7 + [I, P]),
+        "tadm_lora_scratch_size": (I, [I] * 7 + [ctypes.POINTER(SZ)]),
+        "tadm_lora_project": (I, [P] * 5 + [I] * 4 + [I64] * 3 + [P] * 3 + [I] * 4 + [P, SZ, P]),
+        "tadm_residual_norm": (I, [P] * 5 + [I] * 3 + [I64] * 4 + [P, P, I64, P, ctypes.c_float, ctypes.c_float] + [I] * 3 + [P]),
         "tadm_probe_breakdown": (I, [P, I, ctypes.POINTER(I64), ctypes.POINTER(ctypes.c_double),
                                      ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]),
         "tadm_probe_read": (I, [P, ctypes.POINTER(I64), ctypes.POINTER(ctypes.c_double),
@@ -554,6 +559,111 @@ def tadm_pages_copy(pool, src, dst, stream=None):
     if src.shape != dst.shape:
         raise TadmError(1, "src and dst differ in length")
     _check(load_library().tadm_pages_copy(_pool_of(device, pool), src.data_ptr(), dst.data_ptr(), src.shape[0], _stream(stream)))
+
+
+# ------------------------------------------------ requests with settings of their own
+def _matrix_of(device, t, what):
+    """The dtype code (fp32 or bf16) of a matrix with dense rows on the device, and the elements from one row to the next."""
+    code = (_DTYPES or _torch_types()).get(t.dtype)
+    s, n = t.stride(), t.shape
+    if code not in (0, 1) or len(s) != 2 or (s[1] != 1 and n[1] != 1) or t.get_device() != device:
+        raise TadmError(1, f"{what} must be an fp32 or bf16 matrix with dense rows on the current device")
+    return code, s[0] if n[0] != 1 else n[1]
+
+
+def _per_row(device, t, rows, kind, what):
+    """Address of a vector of a value per row (None: none)."""
+    if t is None:
+        return None
+    if (_DTYPES or _torch_types()).get(t.dtype) != kind or tuple(t.shape) != (rows,) or not t.is_contiguous() or t.get_device() != device:
+        raise TadmError(1, f"{what} must be a dense vector of {rows} {'int32' if kind == 'int32' else 'fp32'} values on the current device")
+    return t.data_ptr()
+
+
+def tadm_sample(logits, u, tok, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, mask_id: int = -1,
+                stream=None):
+    """One token per row of logits [rows, vocab] (fp32 or bf16, rows may be strided) into tok (int32 [rows]), drawn with the
+    row's temperature, top_k (int32), top_p and min_p (fp32 [rows] each, None: off) from its random number u (fp32
+    [rows], 0 <= u < 1); prob (fp32 [rows]) gets the token's probability among the ids kept."""
+    device = _device()
+    dtype, ld = _matrix_of(device, logits, "logits")
+    rows, vocab = logits.shape
+    status = load_library().tadm_sample(
+        logits.data_ptr(), ld, rows, vocab, mask_id, _per_row(device, temperature, rows, 0, "temperature"),
+        _per_row(device, top_k, rows, "int32", "top_k"), _per_row(device, top_p, rows, 0, "top_p"),
+        _per_row(device, min_p, rows, 0, "min_p"), _per_row(device, u, rows, 0, "u"),
+        _per_row(device, tok, rows, "int32", "tok"), _per_row(device, prob, rows, 0, "prob"), dtype, _stream(stream))
+    if status:
+        _check(status)
+
+
+def tadm_lora_scratch_size(batch: int, total_rows: int, n_in: int, n_out: int, n_adapters: int, rank: int, dtype: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().tadm_lora_scratch_size(batch, total_rows, n_in, n_out, n_adapters, rank, dtype, ctypes.byref(n)))
+    return n.value
+
+
+def tadm_lora_project(x, w, y, cu_rows, adapter, lora_a, lora_b, lora_scale, scratch, stream=None):
+    """y [rows, n_out] = x [rows, n_in] W^T (W [n_out, n_in]) plus, for the rows of sequence b, lora_scale[a] B_a (A_a x)
+    with a = adapter[b] (int32 [batch]; -1: none); lora_a [adapters, rank, n_in], lora_b [adapters, n_out, rank]."""
+    device = _device()
+    dtype, ldx = _matrix_of(device, x, "x")
+    w_dtype, ldw = _matrix_of(device, w, "w")
+    y_dtype, ldy = _matrix_of(device, y, "y")
+    _ints_of(device, cu_rows, adapter)
+    (rows, n_in), (n_out, k) = x.shape, w.shape
+    (n, rank, a_in), batch = lora_a.shape, cu_rows.shape[0] - 1
+    if k != n_in or tuple(y.shape) != (rows, n_out) or a_in != n_in or tuple(lora_b.shape) != (n, n_out, rank) or \
+            adapter.shape[0] != batch:
+        raise TadmError(1, "shapes of x, w, y, the adapters and the sequences do not agree")
+    for t in (lora_a, lora_b):
+        if t.dtype is not x.dtype or not t.is_contiguous() or t.get_device() != device:
+            raise TadmError(1, "adapters must be contiguous, of x's type, on the current device")
+    if w_dtype != dtype:
+        raise TadmError(1, "w must have x's type")
+    status = load_library().tadm_lora_project(
+        x.data_ptr(), w.data_ptr(), y.data_ptr(), cu_rows.data_ptr(), adapter.data_ptr(), batch, rows, n_in, n_out, ldx, ldw,
+        ldy, lora_a.data_ptr(), lora_b.data_ptr(), _per_row(device, lora_scale, n, 0, "lora_scale"), n, rank, dtype, y_dtype,
+        *_scratch_of(device, scratch), _stream(stream))
+    if status:
+        _check(status)
+
+
+def tadm_residual_norm(x, y, x_out, n_out=None, cu_rows=None, post_gain=None, gate=None, pre_gain=None,
+                       residual_scale: float = 1.0, eps: float = 1e-6, stream=None):
+    """x_out = residual_scale x + gate[b] u with u = y or, with post_gain, its RMS norm times the gain, and n_out = the RMS
+    norm of x_out times pre_gain, for rows [rows, d]; gate [batch, d] has a row per sequence of cu_rows (int32 [batch + 1])."""
+    device = _device()
+    x_dtype, ldx = _matrix_of(device, x, "x")
+    xo_dtype, ldxo = _matrix_of(device, x_out, "x_out")
+    y_dtype, ldy = _matrix_of(device, y, "y")
+    rows, d = shape = x.shape
+    batch = 1
+    if cu_rows is not None:
+        _ints_of(device, cu_rows)
+        batch = cu_rows.shape[0] - 1
+    if xo_dtype != x_dtype or x_out.shape != shape or y.shape != shape or (n_out is not None and n_out.shape != shape):
+        raise TadmError(1, "x, y, x_out and n_out must have one shape, x and x_out one type")
+    dtype, ldn, ldg = None, d, d
+    if n_out is not None:
+        dtype, ldn = _matrix_of(device, n_out, "n_out")
+    if gate is not None:
+        g_dtype, ldg = _matrix_of(device, gate, "gate")
+        if tuple(gate.shape) != (batch, d) or dtype not in (None, g_dtype):
+            raise TadmError(1, "gate must be [batch, d], of n_out's type")
+        dtype = g_dtype
+    for t in (post_gain, pre_gain):
+        if t is not None:
+            code = (_DTYPES or _torch_types()).get(t.dtype)
+            if code not in (0, 1) or tuple(t.shape) != (d,) or not t.is_contiguous() or t.get_device() != device or \
+                    dtype not in (None, code):
+                raise TadmError(1, "gains must be dense vectors of d values of n_out's type on the current device")
+            dtype = code
+    status = load_library().tadm_residual_norm(
+        x.data_ptr(), y.data_ptr(), x_out.data_ptr(), _ptr(n_out), _ptr(cu_rows), batch, rows, d, ldx, ldy, ldxo, ldn,
+        _ptr(post_gain), _ptr(gate), ldg, _ptr(pre_gain), residual_scale, eps, x_dtype, y_dtype, dtype or 0, _stream(stream))
+    if status:
+        _check(status)
 
 
 # ---------------------------------------------------------------------------- model handle

@@ -11,7 +11,7 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "libtadm.so")
 SOURCES = ["gemm_tc.cu", "gemm_simt.cu", "attention.cu", "rowops.cu", "sampler.cu", "tadm_api.cu", "head_static.cu", "splitk.cu",
            "pages.cu", "attention_rows.cu", "attention_packed.cu", "attention_paged.cu", "serve_api.cu",
-           "sample_rows.cu", "adapters_rows.cu", "residual_norm.cu", "requests_api.cu"]
+           "sample_rows.cu", "adapters.cu", "adapters_rows.cu", "residual_norm.cu", "requests_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "-Xcompiler", "-ffp-contract=off"]   # host fp64 arithmetic exactly as written (no fused multiply-add)

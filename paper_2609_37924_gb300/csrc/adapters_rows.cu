@@ -140,14 +140,12 @@ cudaError_t launch(const LoraRowsArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-size_t lora_scratch(int batch, int total, int n_in, int n_out, int n_adapters, int rank, int bf16) {
-  return static_cast<size_t>(total) * rank * sizeof(float);
-}
+size_t lora_rows_scratch(int total, int rank) { return static_cast<size_t>(total) * rank * sizeof(float); }
 
-const char* lora_project(const LoraCall& c, cudaStream_t s) {
+const char* lora_rows(const LoraCall& c, cudaStream_t s) {
   const LoraRowsArgs a{c.x, c.w, c.a, c.b, c.y, c.cu, c.adapter, c.scale, static_cast<float*>(c.scratch),
                        c.batch, c.total, c.n_in, c.n_out, c.n_adapters, c.rank, c.ldx, c.ldw, c.ldy};
-  const cudaError_t e = !c.bf16 ? launch<float, float>(a, s) : c.y_bf16 ? launch<bf16, bf16>(a, s) : launch<bf16, float>(a, s);
+  const cudaError_t e = launch<float, float>(a, s);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 

@@ -35,7 +35,9 @@ struct LoraCall {
 };
 constexpr int kLoraMaxRank = 256;
 size_t lora_scratch(int batch, int total, int n_in, int n_out, int n_adapters, int rank, int bf16);
-const char* lora_project(const LoraCall& c, cudaStream_t s);
+const char* lora_project(const LoraCall& c, cudaStream_t s);          // tcgen05 (bf16), or
+size_t lora_rows_scratch(int total, int rank);
+const char* lora_rows(const LoraCall& c, cudaStream_t s);             // CUDA cores (fp32)
 
 struct NormCall {
   const void *x, *y;

@@ -14,19 +14,18 @@
 // 16 columns of B (so it has 16 significant bits: y then is as near as from an
 // fp32 h, for 2 x 16 more steps of K per 16 ranks).
 //
-// Three launches:
-//   lora_plan_kernel    a block per tile: each row's adapter, the tile's list
-//                       of adapters in the order of their first rows;
-//   lora_down_kernel    x A^T for 128 rows and eight groups of 16 ranks of the
-//                       tile's list (M = 128, N = 128), K split over the blocks of a
-//                       cluster, whose partial sums are added in the order of
-//                       K through distributed shared memory; scale, mask, hi, lo;
+// Two launches:
+//   lora_down_kernel    each cluster finds the adapters of its tile's rows, then x A^T for
+//                       128 rows and eight groups of 16 ranks of the tile's
+//                       list (M = 128, N = 128), K split over the blocks of the
+//                       cluster, whose partial sums are added in the order of K
+//                       through distributed shared memory; scale, mask, hi, lo;
 //   lora_gemm_kernel    the product, CTA pairs (M = 256): persistent over tiles,
-//                       or, where there are few, K (the blocks of h and B
-//                       included) split over the pairs of a cluster likewise.
-// lora_gemm_kernel needs of its predecessor only h: its loads of x and W run
-// ahead of the grid dependency (what wrote x, W and the plan lies two launches
-// back and has completed).
+//                       or, where there are few, K (and the blocks of h and B)
+//                       split over the two pairs of a cluster likewise.
+// lora_gemm_kernel needs of its predecessor only h and the lists: its blocks of
+// x and W run ahead of the grid dependency (when it starts, every block of
+// its predecessor has waited for what came before, so x and W are there).
 #include <algorithm>
 #include <cstdint>
 
@@ -42,16 +41,14 @@ constexpr int TR = 256;                    // rows of a tile
 constexpr int BK = 64;
 constexpr int G = 16;                      // ranks of a group
 constexpr int KB_BYTES = TR * BK * 2;      // a block of h: 256 rows x (hi, lo of two groups)
-constexpr int TABLE = 4096;
 
-// What the plan leaves for a call, and its place in the scratch memory.
+// What the first kernel leaves for the second, and its place in the scratch memory.
 struct Plan {
-  int32_t* row_ad;                         // [tiles * TR] a row's adapter; -1: none or in no sequence
   int32_t* n_ad;                           // [tiles] adapters of the tile
   int32_t* base;                           // [tiles] first block of h
   int32_t* list;                           // [tiles][cap]
   bf16* h;                                 // [slots][TR][64]
-  int tiles, cap, slots, groups;           // groups: of 16 ranks per adapter
+  int tiles, cap, slots, groups;           // cap: most adapters of a tile; groups: of 16 ranks per adapter
   int by_seq;                              // where a tile's blocks of h begin: by its first sequence, or by the tile
 };
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
@@ -71,73 +68,12 @@ Plan make_plan(int batch, int total, int n_adapters, int rank, uint8_t* scratch,
     at = up(at + n, 1024);
     return scratch + here;
   };
-  p.row_ad = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles * TR));
   p.n_ad = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles));
   p.base = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles));
   p.list = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles * static_cast<size_t>(p.cap)));
   p.h = reinterpret_cast<bf16*>(take(static_cast<size_t>(p.slots) * KB_BYTES));
   if (bytes) *bytes = at + 1024;           // the blocks start on 1024 bytes, scratch on 16
   return p;
-}
-
-// ------------------------------------------------------------------ plan
-struct PlanArgs {
-  Plan p;
-  const int32_t *cu, *adapter;
-  int batch, total, n_adapters;
-};
-
-__global__ void __launch_bounds__(TR) lora_plan_kernel(const PlanArgs a) {
-  constexpr int CACHE = 2048;
-  __shared__ int32_t s_cu[CACHE + 1], s_first[TABLE], s_ad[TR], s_part[TR / 32], s_base;
-  const int tile = blockIdx.x, i = threadIdx.x, row = tile * TR + i, warp = i >> 5, lane = i & 31;
-  const bool cached = a.batch <= CACHE, table = a.n_adapters <= TABLE;
-  if (table)
-    for (int j = i; j < a.n_adapters; j += TR) s_first[j] = TR;
-  pdl_enter();
-  if (cached)
-    for (int j = i; j <= a.batch; j += TR) s_cu[j] = a.cu[j];
-  __syncthreads();
-  const int32_t* cu = cached ? s_cu : a.cu;
-  int lo = 0, hi = a.batch + 1;            // boundaries <= row: in lo .. hi
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= row) lo = mid + 1;
-    else hi = mid;
-  }
-  const int b = lo - 1;
-  int ad = -1;
-  if (row < a.total && b >= 0 && b < a.batch) {
-    ad = a.adapter[b];
-    if (ad < 0 || ad >= a.n_adapters) ad = -1;
-  }
-  if (i == 0) s_base = a.p.by_seq ? (max(b, 0) + tile) * ((a.p.groups + 1) / 2) : tile * ((a.p.cap * a.p.groups + 1) / 2);
-  s_ad[i] = ad;
-  a.p.row_ad[row] = ad;
-  if (table && ad >= 0) atomicMin(&s_first[ad], i);
-  __syncthreads();
-  bool first = ad >= 0;
-  if (table) {
-    first = first && s_first[ad] == i;
-  } else {
-    for (int j = 0; j < i && first; ++j) first = s_ad[j] != ad;
-  }
-  const unsigned have = __ballot_sync(0xffffffffu, first);
-  if (lane == 0) s_part[warp] = __popc(have);
-  __syncthreads();
-  int before = 0, n = 0;
-  for (int w = 0; w < TR / 32; ++w) {
-    if (w < warp) before += s_part[w];
-    n += s_part[w];
-  }
-  const int at = before + __popc(have & ((1u << lane) - 1));
-  if (first && at < a.p.cap) a.p.list[static_cast<int64_t>(tile) * a.p.cap + at] = ad;
-  if (i == 0) {
-    // (sequences that overlap or run backwards may ask for more than there is: no block past the last one is touched)
-    const int base = min(s_base, a.p.slots), room = 2 * (a.p.slots - base) / a.p.groups;
-    a.p.n_ad[tile] = min(min(n, a.p.cap), room);
-    a.p.base[tile] = base;
-  }
 }
 
 // ------------------------------------------------------------------ shared pieces
@@ -153,6 +89,8 @@ __device__ __forceinline__ float4 remote_f4(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
+// Waits for the kernel before this one, without letting the next one start.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // K-major bf16 tile with rows of 16 elements, 32-byte swizzle: 256 bytes from one 8-row group to the next
 __device__ __forceinline__ uint64_t sdesc_rows32(uint32_t saddr) {
   return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | 1ull << 16 | static_cast<uint64_t>(256 >> 4) << 32 | 1ull << 46 | 6ull << 61;
@@ -161,26 +99,81 @@ __device__ __forceinline__ uint64_t sdesc_rows32(uint32_t saddr) {
 // ------------------------------------------------------------------ h = scale A x
 constexpr int D_STAGES = 4, D_GROUPS = 8, D_N = D_GROUPS * G;
 constexpr int D_X_BYTES = 128 * BK * 2, D_A_BYTES = D_N * BK * 2, D_STAGE_BYTES = D_X_BYTES + D_A_BYTES;
-constexpr int D_THREADS = 192;
-constexpr int D_SMEM = 1024 + D_STAGES * D_STAGE_BYTES + 128 * D_N * 4 + 256;
+constexpr int D_THREADS = 192, TABLE = 4096, CACHE = 4096;
+static_assert((TABLE + CACHE + 1) * 4 <= 128 * D_N * 4, "the lists are made where the sums come later");
+constexpr int D_SMEM = 1024 + D_STAGES * D_STAGE_BYTES + 128 * D_N * 4 + 2 * TR * 4 + 256;
 
 struct DownArgs {
   Plan p;
+  const int32_t *cu, *adapter;
   const float* scale;
-  int total, kblocks, rank;
+  int batch, total, n_adapters, kblocks;
   int* status;
 };
 
+// The adapters of tile `tile`'s rows (s_row: -1 none) and the list of them in the order of their first rows (s_list); returns
+// how many.  Block-collective; `room`: scratch of TABLE + CACHE + 1 words.
+__device__ __forceinline__ int make_lists(const DownArgs& a, int tile, int32_t* room, int32_t* s_row, int32_t* s_list, int* first_seq) {
+  int32_t *s_first = room, *s_cu = room + TABLE;
+  const bool cached = a.batch <= CACHE, table = a.n_adapters <= TABLE;
+  if (table)
+    for (int j = threadIdx.x; j < a.n_adapters; j += D_THREADS) s_first[j] = TR;
+  if (cached)
+    for (int j = threadIdx.x; j <= a.batch; j += D_THREADS) s_cu[j] = a.cu[j];
+  __syncthreads();
+  for (int i = threadIdx.x; i < TR; i += D_THREADS) {
+    const int row = tile * TR + i;
+    const int32_t* cu = cached ? s_cu : a.cu;
+    int lo = 0, hi = a.batch + 1;          // boundaries <= row: in lo .. hi
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (cu[mid] <= row) lo = mid + 1;
+      else hi = mid;
+    }
+    const int b = lo - 1;
+    int ad = -1;
+    if (row < a.total && b >= 0 && b < a.batch) {
+      ad = a.adapter[b];
+      if (ad < 0 || ad >= a.n_adapters) ad = -1;
+    }
+    if (i == 0) *first_seq = max(b, 0);
+    s_row[i] = ad;
+    if (table && ad >= 0) atomicMin(&s_first[ad], i);
+  }
+  __syncthreads();
+  // every warp counts all, the first one writes the list
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int n = 0;
+  for (int i = lane; i < TR; i += 32) {
+    const int ad = s_row[i];
+    bool first = ad >= 0;
+    if (table) {
+      first = first && s_first[ad] == i;
+    } else {
+      for (int j = 0; j < i && first; ++j) first = s_row[j] != ad;
+    }
+    const unsigned have = __ballot_sync(0xffffffffu, first);
+    const int at = n + __popc(have & ((1u << lane) - 1));
+    if (warp == 0 && first) s_list[at] = ad;
+    n += __popc(have);
+  }
+  __syncthreads();
+  return min(n, a.p.cap);
+}
+
+// A cluster has a half of a tile (128 rows) and every so many of its eights of groups.
 template <int CS>
 __global__ void __launch_bounds__(D_THREADS, 1)
     lora_down_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmA, const DownArgs a) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   float4* s_d = reinterpret_cast<float4*>(smem + D_STAGES * D_STAGE_BYTES);   // [D_N / 4][128 rows]
-  uint64_t* full = reinterpret_cast<uint64_t*>(s_d + 128 * D_N / 4);
+  int32_t *s_row = reinterpret_cast<int32_t*>(s_d + 128 * D_N / 4), *s_list = s_row + TR;
+  uint64_t* full = reinterpret_cast<uint64_t*>(s_list + TR);
   uint64_t *empty = full + D_STAGES, *done = empty + D_STAGES;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* s_seq = reinterpret_cast<int*>(tmem_slot + 2);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CS > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   if (threadIdx.x == 0) {
@@ -207,106 +200,112 @@ __global__ void __launch_bounds__(D_THREADS, 1)
   int stage = 0, loads = 0;
   uint32_t phase = 0, done_phase = 0;
   bool any = false;
-  auto chunks_of = [&](int t) {            // of a tile: its groups in eights, for each of its halves
-    return (static_cast<int64_t>(a.p.n_ad[t]) * a.p.groups + D_GROUPS - 1) / D_GROUPS * (t * TR + 128 < a.total ? 2 : 1);
-  };
-  for (int64_t unit = blockIdx.x / CS;; unit += gridDim.x / CS) {
-    int within;
-    const int t = find_tile(a.p.tiles, unit, chunks_of, &within);
-    if (t < 0) break;
-    const int all = a.p.n_ad[t] * a.p.groups, halves = t * TR + 128 < a.total ? 2 : 1;
-    const int half = within % halves, g0 = within / halves * D_GROUPS, ng = min(D_GROUPS, all - g0), row0 = t * TR + half * 128;
-    const int32_t* list = a.p.list + static_cast<int64_t>(t) * a.p.cap;
-    if (warp == 0) {
-      // (lane i: group i)
-      const int ad = lane < ng ? list[(g0 + lane) / a.p.groups] : 0, at = (g0 + lane) % a.p.groups * G;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!warp_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status)) break;
-        uint8_t* sx = smem + stage * D_STAGE_BYTES;
-        if (lane == 0) {
-          mbar_arrive_expect_tx(&full[stage], D_X_BYTES + ng * G * BK * 2);
-          tma_load_2d(sx, &tmX, &full[stage], kb * BK, row0);
-        }
-        __syncwarp();
-        if (lane < ng) tma_load_3d(sx + D_X_BYTES + lane * G * BK * 2, &tmA, &full[stage], kb * BK, at, ad);
-        loads = min(loads + 1, D_STAGES);
-        if (++stage == D_STAGES) { stage = 0; phase ^= 1; }
+  const int clusters = gridDim.x / CS, halves = (a.total + 127) / 128, per = max(1, clusters / halves);   // clusters of a half
+  for (int th = blockIdx.x / CS % (per * halves) % halves, c0 = blockIdx.x / CS / halves; th < halves && c0 < per; th += clusters) {
+    const int t = th >> 1, half = th & 1, row0 = th * 128;
+    const int n_list = make_lists(a, t, reinterpret_cast<int32_t*>(s_d), s_row, s_list, s_seq);
+    const int base = min(a.p.by_seq ? (*s_seq + t) * ((a.p.groups + 1) / 2) : t * ((a.p.cap * a.p.groups + 1) / 2), a.p.slots);
+    // (sequences that overlap or run backwards may ask for more blocks of h than there are: none past the last is touched)
+    const int n_ad = min(n_list, 2 * (a.p.slots - base) / a.p.groups), all = n_ad * a.p.groups;
+    if (half == 0 && c0 == 0 && rank == 0) {
+      if (threadIdx.x == 0) {
+        a.p.n_ad[t] = n_ad;
+        a.p.base[t] = base;
       }
-    } else if (warp == 1) {
-      const uint32_t idesc = idesc_bf16_f32(128, ng * G);
-      bool ok = true;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!(ok = warp_wait_bounded(&full[stage], phase, abort_flag, a.status))) break;
-        tc_fence_after();
-        const uint64_t x0 = sdesc_kmajor_sw128(smem_u32(smem + stage * D_STAGE_BYTES));
-        const uint64_t a0 = sdesc_kmajor_sw128(smem_u32(smem + stage * D_STAGE_BYTES + D_X_BYTES));
-#pragma unroll
-        for (int k = 0; k < BK / 16; ++k) umma_bf16(tmem, x0 + 2 * k, a0 + 2 * k, idesc, kb != kb0 || k != 0);
-        umma_commit(&empty[stage]);
-        if (++stage == D_STAGES) { stage = 0; phase ^= 1; }
-      }
-      umma_commit(done);
-    } else {
-      const int quad = warp & 3;
-      const bool waited = warp_wait_bounded(done, done_phase, abort_flag, a.status), ok = waited && !*abort_flag && kb1 > kb0;
-      tc_fence_after();
-      for (int c = 0; c < ng; ++c) {
-        float v[16];
-        __syncwarp();
-        if (ok) {
-          tmem_ld16(tmem + c * G + (static_cast<uint32_t>(quad * 32) << 16), v);
-        } else {
-          for (int e = 0; e < 16; ++e) v[e] = kb1 > kb0 ? NAN : 0.0f;
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          s_d[(c * 4 + q) * 128 + quad * 32 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-      }
-      tc_fence_before();
+      for (int i = threadIdx.x; i < n_ad; i += D_THREADS) a.p.list[static_cast<int64_t>(t) * a.p.cap + i] = s_list[i];
     }
-    done_phase ^= 1;
-    any = true;
-    __syncwarp();
-    if constexpr (CS > 1) cluster_sync();
-    else __syncthreads();
-    if (warp >= 2) {
-      // this block's share of the groups: the sum in the order of K, then a row's 32 + 32 bytes of hi and lo
-      const int r = (warp - 2) * 32 + lane, row = row0 + r;
-      const int mine = row < a.total ? a.p.row_ad[row] : -1;
-      for (int c = rank; c < ng; c += CS) {
-        float v[16];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-          for (int p = 0; p < CS; ++p) {
-            const float4 x = CS > 1 ? remote_f4(cluster_addr(&s_d[(c * 4 + q) * 128 + r], p)) : s_d[(c * 4 + q) * 128 + r];
-            s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+    for (int g0 = c0 * D_GROUPS; g0 < all; g0 += per * D_GROUPS) {
+      const int ng = min(D_GROUPS, all - g0);
+      if (warp == 0) {
+        // (lane i: group i)
+        const int ad = lane < ng ? s_list[(g0 + lane) / a.p.groups] : 0, at = (g0 + lane) % a.p.groups * G;
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!warp_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status)) break;
+          uint8_t* sx = smem + stage * D_STAGE_BYTES;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(&full[stage], D_X_BYTES + ng * G * BK * 2);
+            tma_load_2d(sx, &tmX, &full[stage], kb * BK, row0);
           }
-          v[4 * q] = s.x, v[4 * q + 1] = s.y, v[4 * q + 2] = s.z, v[4 * q + 3] = s.w;
+          __syncwarp();
+          if (lane < ng) tma_load_3d(sx + D_X_BYTES + lane * G * BK * 2, &tmA, &full[stage], kb * BK, at, ad);
+          loads = min(loads + 1, D_STAGES);
+          if (++stage == D_STAGES) { stage = 0; phase ^= 1; }
         }
-        const int ad = list[(g0 + c) / a.p.groups];
-        const float scale = a.scale[ad];
-        uint32_t hi[8], lo[8];
+      } else if (warp == 1) {
+        const uint32_t idesc = idesc_bf16_f32(128, ng * G);
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!warp_wait_bounded(&full[stage], phase, abort_flag, a.status)) break;
+          tc_fence_after();
+          const uint64_t x0 = sdesc_kmajor_sw128(smem_u32(smem + stage * D_STAGE_BYTES));
+          const uint64_t a0 = sdesc_kmajor_sw128(smem_u32(smem + stage * D_STAGE_BYTES + D_X_BYTES));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = mine == ad ? v[2 * e] * scale : 0.0f, y = mine == ad ? v[2 * e + 1] * scale : 0.0f;
-          const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-          const __nv_bfloat162 l = __floats2bfloat162_rn(x - __low2float(h), y - __high2float(h));
-          hi[e] = *reinterpret_cast<const uint32_t*>(&h);
-          lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+          for (int k = 0; k < BK / 16; ++k) umma_bf16(tmem, x0 + 2 * k, a0 + 2 * k, idesc, kb != kb0 || k != 0);
+          umma_commit(&empty[stage]);
+          if (++stage == D_STAGES) { stage = 0; phase ^= 1; }
         }
-        const int g = g0 + c;
-        uint4* out = reinterpret_cast<uint4*>(a.p.h + (static_cast<int64_t>(a.p.base[t] + g / 2) * TR + half * 128 + r) * BK + g % 2 * 32);
-        out[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        out[1] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
-        out[2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        out[3] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+        umma_commit(done);
+      } else {
+        const int quad = warp & 3;
+        const bool ok = warp_wait_bounded(done, done_phase, abort_flag, a.status) && !*abort_flag;
+        tc_fence_after();
+        for (int c = 0; c < ng; ++c) {
+          float v[16];
+          __syncwarp();
+          if (ok && kb1 > kb0) {
+            tmem_ld16(tmem + c * G + (static_cast<uint32_t>(quad * 32) << 16), v);
+          } else {
+            for (int e = 0; e < 16; ++e) v[e] = ok ? 0.0f : NAN;
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            s_d[(c * 4 + q) * 128 + quad * 32 + lane] = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+        }
+        tc_fence_before();
       }
+      done_phase ^= 1;
+      any = true;
+      __syncwarp();
+      if constexpr (CS > 1) cluster_sync();
+      else __syncthreads();
+      if (warp >= 2) {
+        // this block's share of the groups: the sum in the order of K, then a row's 32 + 32 bytes of hi and lo
+        const int r = (warp - 2) * 32 + lane, mine = s_row[half * 128 + r];
+        for (int c = rank; c < ng; c += CS) {
+          float v[16];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int p = 0; p < CS; ++p) {
+              const float4 x = CS > 1 ? remote_f4(cluster_addr(&s_d[(c * 4 + q) * 128 + r], p)) : s_d[(c * 4 + q) * 128 + r];
+              s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+            }
+            v[4 * q] = s.x, v[4 * q + 1] = s.y, v[4 * q + 2] = s.z, v[4 * q + 3] = s.w;
+          }
+          const int ad = s_list[(g0 + c) / a.p.groups];
+          const float scale = a.scale[ad];
+          uint32_t hi[8], lo[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float x = mine == ad ? v[2 * e] * scale : 0.0f, y = mine == ad ? v[2 * e + 1] * scale : 0.0f;
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+            const __nv_bfloat162 l = __floats2bfloat162_rn(x - __low2float(h), y - __high2float(h));
+            hi[e] = *reinterpret_cast<const uint32_t*>(&h);
+            lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+          }
+          const int g = g0 + c;
+          uint4* out = reinterpret_cast<uint4*>(a.p.h + (static_cast<int64_t>(base + g / 2) * TR + half * 128 + r) * BK + g % 2 * 32);
+          out[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          out[1] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+          out[2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          out[3] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+        }
+      }
+      __syncwarp();
+      if constexpr (CS > 1) cluster_sync();                   // the partial sums may be written again, blocks may leave
+      else __syncthreads();
     }
-    __syncwarp();
-    if constexpr (CS > 1) cluster_sync();                     // the partial sums may be written again, blocks may leave
-    else __syncthreads();
+    __syncthreads();                                          // (the lists are read no more)
   }
   // (after a wait that gave up: the copies have landed and the MMAs are through before the block ends)
   volatile int never = 0;
@@ -438,7 +437,13 @@ __global__ void __launch_bounds__(G_THREADS, 1)
       nt = u - mt * a.n_tiles_n;
     }
   };
-  auto blocks_of = [&](int mt) { return a.kblocks + (a.p.n_ad[mt] * a.p.groups + 1) / 2; };
+  const int k0 = a.kblocks * pair / KS, k1 = a.kblocks * (pair + 1) / KS;   // this pair's blocks of x and W (at least one)
+  auto share = [&](int mt, int& e0, int& e1) {                // and of h and B; returns the tile's groups
+    const int groups = a.p.n_ad[mt] * a.p.groups, blocks = (groups + 1) / 2;
+    e0 = blocks * pair / KS;
+    e1 = blocks * (pair + 1) / KS;
+    return groups;
+  };
 
   if (warp == 0) {
     if (lane == 0) {
@@ -449,29 +454,33 @@ __global__ void __launch_bounds__(G_THREADS, 1)
       for (int u = u0; u < units && !*abort_flag; u += ustep) {
         int mt, nt;
         place(u, mt, nt);
-        const int all = blocks_of(mt), k0 = all * pair / KS, k1 = all * (pair + 1) / KS;
-        const int n0 = nt * BN + half * (BN / 2), ng_all = a.p.n_ad[mt] * a.p.groups;
-        const int32_t* list = a.p.list + static_cast<int64_t>(mt) * a.p.cap;
+        const int n0 = nt * BN + half * (BN / 2);
         bool ok = true;
         for (int kb = k0; kb < k1; ++kb) {
           if (!mbar_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status)) { ok = false; break; }
           const uint32_t bar = full_l + 8u * stage;
-          if (kb < a.kblocks) {
-            if (!half) mbar_arrive_expect_tx(&full[stage], 2 * C::STAGE_BYTES);
-            tma_load_2d_pair(sB + stage * C::B_BYTES, &tmW, bar, kb * BK, n0);
-            tma_load_2d_pair(sA + stage * C::A_BYTES, &tmX, bar, kb * BK, mt * TR + half * 128);
-          } else {
-            if (!waited) {                 // h comes from the kernel before
-              pdl_enter();
-              waited = true;
-            }
-            const int g0 = 2 * (kb - a.kblocks), ng = min(2, ng_all - g0);
-            if (!half) mbar_arrive_expect_tx(&full[stage], 2 * (C::A_BYTES + ng * C::EXT_BYTES));
-            tma_load_2d_pair(sA + stage * C::A_BYTES, &tmH, bar, 0, (a.p.base[mt] + kb - a.kblocks) * TR + half * 128);
-            for (int i = 0; i < ng; ++i)
-              tma_load_3d_pair(sB + stage * C::B_BYTES + i * C::EXT_BYTES, &tmB, bar, (g0 + i) % a.p.groups * G, n0,
-                               list[(g0 + i) / a.p.groups]);
-          }
+          if (!half) mbar_arrive_expect_tx(&full[stage], 2 * C::STAGE_BYTES);
+          tma_load_2d_pair(sB + stage * C::B_BYTES, &tmW, bar, kb * BK, n0);
+          tma_load_2d_pair(sA + stage * C::A_BYTES, &tmX, bar, kb * BK, mt * TR + half * 128);
+          if (++stage == NST) { stage = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        if (!waited) {                     // h and the lists come from the kernel before
+          pdl_enter();
+          waited = true;
+        }
+        int e0, e1;
+        const int groups = share(mt, e0, e1), base = a.p.base[mt];
+        const int32_t* list = a.p.list + static_cast<int64_t>(mt) * a.p.cap;
+        for (int kb = e0; kb < e1; ++kb) {
+          if (!mbar_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status)) { ok = false; break; }
+          const uint32_t bar = full_l + 8u * stage;
+          const int ng = min(2, groups - 2 * kb);
+          if (!half) mbar_arrive_expect_tx(&full[stage], 2 * (C::A_BYTES + ng * C::EXT_BYTES));
+          tma_load_2d_pair(sA + stage * C::A_BYTES, &tmH, bar, 0, (base + kb) * TR + half * 128);
+          for (int i = 0; i < ng; ++i)
+            tma_load_3d_pair(sB + stage * C::B_BYTES + i * C::EXT_BYTES, &tmB, bar, (2 * kb + i) % a.p.groups * G, n0,
+                             list[(2 * kb + i) / a.p.groups]);
           if (++stage == NST) { stage = 0; phase ^= 1; }
         }
         if (!ok) break;
@@ -491,7 +500,6 @@ __global__ void __launch_bounds__(G_THREADS, 1)
       for (int u = u0; u < units; u += ustep) {
         int mt, nt;
         place(u, mt, nt);
-        const int all = blocks_of(mt), k0 = all * pair / KS, k1 = all * (pair + 1) / KS, ng_all = a.p.n_ad[mt] * a.p.groups;
         if (!warp_wait_bounded(&tempty[acc], acc_phase ^ 1, abort_flag, a.status)) break;
         tc_fence_after();
         const uint32_t d = tmem + acc * BN;
@@ -500,17 +508,25 @@ __global__ void __launch_bounds__(G_THREADS, 1)
           if (!warp_wait_bounded(&full[stage], phase, abort_flag, a.status)) { ok = false; break; }
           tc_fence_after();
           const uint64_t a0 = sdesc_kmajor_sw128(smem_u32(sA + stage * C::A_BYTES));
-          if (kb < a.kblocks) {
-            const uint64_t b0 = sdesc_kmajor_sw128(smem_u32(sB + stage * C::B_BYTES));
+          const uint64_t b0 = sdesc_kmajor_sw128(smem_u32(sB + stage * C::B_BYTES));
 #pragma unroll
-            for (int k = 0; k < BK / 16; ++k) umma_bf16_pair(d, a0 + 2 * k, b0 + 2 * k, idesc, kb != k0 || k != 0);
-          } else {
-            const int ng = min(2, ng_all - 2 * (kb - a.kblocks));
-            for (int i = 0; i < ng; ++i) {
-              const uint64_t b0 = sdesc_rows32(smem_u32(sB + stage * C::B_BYTES + i * C::EXT_BYTES));
-              umma_bf16_pair(d, a0 + 4 * i, b0, idesc, kb != k0 || i != 0);
-              umma_bf16_pair(d, a0 + 4 * i + 2, b0, idesc, 1);
-            }
+          for (int k = 0; k < BK / 16; ++k) umma_bf16_pair(d, a0 + 2 * k, b0 + 2 * k, idesc, kb != k0 || k != 0);
+          umma_commit_pair_mc(&empty[stage], 0x3 << lead);
+          if (++stage == NST) { stage = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        grid_wait();
+        int e0, e1;
+        const int groups = share(mt, e0, e1);
+        for (int kb = e0; kb < e1; ++kb) {
+          if (!warp_wait_bounded(&full[stage], phase, abort_flag, a.status)) { ok = false; break; }
+          tc_fence_after();
+          const uint64_t a0 = sdesc_kmajor_sw128(smem_u32(sA + stage * C::A_BYTES));
+          const int ng = min(2, groups - 2 * kb);
+          for (int i = 0; i < ng; ++i) {
+            const uint64_t b0 = sdesc_rows32(smem_u32(sB + stage * C::B_BYTES + i * C::EXT_BYTES));
+            umma_bf16_pair(d, a0 + 4 * i, b0, idesc, 1);      // hi
+            umma_bf16_pair(d, a0 + 4 * i + 2, b0, idesc, 1);  // lo
           }
           umma_commit_pair_mc(&empty[stage], 0x3 << lead);
           if (++stage == NST) { stage = 0; phase ^= 1; }
@@ -555,15 +571,14 @@ __global__ void __launch_bounds__(G_THREADS, 1)
         if (++acc == 2) { acc = 0; acc_phase ^= 1; }
       } else {
         // this pair's share of the sum, for the others: [columns / 4][128 rows] over the stages, which all have been read
-        const int all = blocks_of(mt), k0 = all * pair / KS, k1 = all * (pair + 1) / KS;
         float4* s_d = reinterpret_cast<float4*>(smem);
         if (row0 < r_hi && row0 + 32 > r_lo) {
           for (int c = part * (BN / 64); c < (part + 1) * (BN / 64); ++c) {
             __syncwarp();
-            if (ok && k1 > k0) {
+            if (ok) {
               tmem_ld32(d + 32 * c, v);
             } else {
-              for (int e = 0; e < 32; ++e) v[e] = ok ? 0.0f : NAN;
+              for (int e = 0; e < 32; ++e) v[e] = NAN;
             }
 #pragma unroll
             for (int q = 0; q < 8; ++q)
@@ -726,38 +741,31 @@ const char* lora_project(const LoraCall& c, cudaStream_t s) {
   const int sms = current_sms(&dev);
   uint8_t* scratch = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(c.scratch) + 1023) & ~uintptr_t(1023));
   const Plan p = make_plan(c.batch, c.total, c.n_adapters, c.rank, scratch, nullptr);
-  cudaError_t e = launch_pdl(lora_plan_kernel, p.tiles, TR, 0, s, PlanArgs{p, c.cu, c.adapter, c.batch, c.total, c.n_adapters});
-  if (e != cudaSuccess) return cudaGetErrorString(e);
   const int kblocks = (c.n_in + BK - 1) / BK;
   Maps m;
   CUtensorMap ta;
   if (!rows_map(&m.x, c.x, c.total, c.n_in, c.ldx, 128) || !rows_map(&m.h, p.h, static_cast<int64_t>(p.slots) * TR, BK, BK, 128) ||
       !(c.n_adapters > 0 ? adapter_map(&ta, c.a, c.n_adapters, c.rank, c.n_in, BK, G) : rows_map(&ta, c.x, c.total, c.n_in, c.ldx, 128)))
     return "tensor map encode failed";
-  // h: the units of the call at most; K is split over a cluster's blocks while SMs would stay idle
-  const int halves = c.total > (p.tiles - 1) * TR + 128 ? 2 * p.tiles : 2 * p.tiles - 1;
-  const int64_t most = c.n_adapters > 0 ? static_cast<int64_t>(halves) * ((static_cast<int64_t>(p.cap) * p.groups + D_GROUPS - 1) / D_GROUPS) : 1;
+  // h: at most so many products of 128 rows and 128 ranks; K is split over a cluster's blocks while SMs would stay idle
+  const int halves = (c.total + 127) / 128;
+  const int64_t most = halves * ((static_cast<int64_t>(c.n_adapters > 0 ? p.cap : 0) * p.groups + D_GROUPS - 1) / D_GROUPS);
   int cs = 1;
   while (cs < 8 && most * cs * 2 <= sms && kblocks >= 4 * cs) cs *= 2;
-  const int clusters = static_cast<int>(std::min<int64_t>(most, sms / cs));
-  const DownArgs d{p, c.scale, c.total, kblocks, c.rank, c.status};
-  e = cs == 1 ? launch_down<1>(m.x, ta, d, clusters, dev, s) : cs == 2 ? launch_down<2>(m.x, ta, d, clusters, dev, s)
-    : cs == 4 ? launch_down<4>(m.x, ta, d, clusters, dev, s) : launch_down<8>(m.x, ta, d, clusters, dev, s);
+  const int clusters = static_cast<int>(std::min<int64_t>(std::max<int64_t>(most, halves), sms / cs));
+  const DownArgs d{p, c.cu, c.adapter, c.scale, c.batch, c.total, c.n_adapters, kblocks, c.status};
+  cudaError_t e = cs == 1 ? launch_down<1>(m.x, ta, d, clusters, dev, s) : cs == 2 ? launch_down<2>(m.x, ta, d, clusters, dev, s)
+                : cs == 4 ? launch_down<4>(m.x, ta, d, clusters, dev, s) : launch_down<8>(m.x, ta, d, clusters, dev, s);
   if (e != cudaSuccess) return cudaGetErrorString(e);
   GemmArgs a{};
   a.p = p, a.cu = c.cu, a.y = c.y, a.ldy = c.ldy, a.batch = c.batch, a.total = c.total, a.n_out = c.n_out, a.kblocks = kblocks;
   a.y_bf16 = c.y_bf16, a.status = c.status;
   a.y_vec = (reinterpret_cast<uintptr_t>(c.y) & 15) == 0 && c.ldy * (c.y_bf16 ? 2 : 4) % 16 == 0;
   a.m_fast = static_cast<int64_t>(c.n_out) > c.total;         // the larger operand's tiles are shared through L2
-  const int pairs = sms / 2;
-  const int64_t t256 = static_cast<int64_t>(p.tiles) * ((c.n_out + 255) / 256), t192 = static_cast<int64_t>(p.tiles) * ((c.n_out + 191) / 192),
-                t128 = static_cast<int64_t>(p.tiles) * ((c.n_out + 127) / 128);
-  auto rounds = [&](int64_t t) { return (t + pairs - 1) / pairs; };
-  if (kblocks >= 8 && t128 * 4 <= pairs) e = launch_gemm<128, 4>(c, m, a, dev, sms, s);
-  else if (kblocks >= 8 && t256 * 4 <= pairs) e = launch_gemm<256, 4>(c, m, a, dev, sms, s);
-  else if (kblocks >= 8 && t256 * 2 <= pairs) e = launch_gemm<256, 2>(c, m, a, dev, sms, s);
-  else if (rounds(t128) * 140 < rounds(t256) * 256 && rounds(t128) * 140 < rounds(t192) * 200) e = launch_gemm<128, 1>(c, m, a, dev, sms, s);
-  else if (rounds(t192) * 200 < rounds(t256) * 256) e = launch_gemm<192, 1>(c, m, a, dev, sms, s);
+  const int64_t t256 = static_cast<int64_t>(p.tiles) * ((c.n_out + 255) / 256), t128 = static_cast<int64_t>(p.tiles) * ((c.n_out + 127) / 128);
+  const bool split = kblocks >= 8;
+  if (split && t128 <= gemm_clusters<128, 2>(dev, sms, &e)) e = launch_gemm<128, 2>(c, m, a, dev, sms, s);
+  else if (split && t256 <= gemm_clusters<256, 2>(dev, sms, &e)) e = launch_gemm<256, 2>(c, m, a, dev, sms, s);
   else e = launch_gemm<256, 1>(c, m, a, dev, sms, s);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }

@@ -100,7 +100,7 @@ __device__ __forceinline__ uint64_t sdesc_rows32(uint32_t saddr) {
 constexpr int D_STAGES = 4, D_GROUPS = 8, D_N = D_GROUPS * G;
 constexpr int D_X_BYTES = 128 * BK * 2, D_A_BYTES = D_N * BK * 2, D_STAGE_BYTES = D_X_BYTES + D_A_BYTES;
 constexpr int D_THREADS = 192, TABLE = 4096, CACHE = 4096;
-static_assert((TABLE + CACHE + 1) * 4 <= 128 * D_N * 4, "the lists are made where the sums come later");
+static_assert((TABLE + 2 * CACHE + 1) * 4 <= 128 * D_N * 4, "the lists are made where the sums come later");
 constexpr int D_SMEM = 1024 + D_STAGES * D_STAGE_BYTES + 128 * D_N * 4 + 2 * TR * 4 + 256;
 
 struct DownArgs {
@@ -112,14 +112,17 @@ struct DownArgs {
 };
 
 // The adapters of tile `tile`'s rows (s_row: -1 none) and the list of them in the order of their first rows (s_list); returns
-// how many.  Block-collective; `room`: scratch of TABLE + CACHE + 1 words.
+// how many.  Block-collective; `room`: scratch of TABLE + 2 CACHE + 1 words.
 __device__ __forceinline__ int make_lists(const DownArgs& a, int tile, int32_t* room, int32_t* s_row, int32_t* s_list, int* first_seq) {
-  int32_t *s_first = room, *s_cu = room + TABLE;
+  int32_t *s_first = room, *s_ad = room + TABLE, *s_cu = s_ad + CACHE;
   const bool cached = a.batch <= CACHE, table = a.n_adapters <= TABLE;
   if (table)
     for (int j = threadIdx.x; j < a.n_adapters; j += D_THREADS) s_first[j] = TR;
   if (cached)
-    for (int j = threadIdx.x; j <= a.batch; j += D_THREADS) s_cu[j] = a.cu[j];
+    for (int j = threadIdx.x; j <= a.batch; j += D_THREADS) {
+      s_cu[j] = a.cu[j];
+      if (j < a.batch) s_ad[j] = a.adapter[j];
+    }
   __syncthreads();
   for (int i = threadIdx.x; i < TR; i += D_THREADS) {
     const int row = tile * TR + i;
@@ -133,7 +136,7 @@ __device__ __forceinline__ int make_lists(const DownArgs& a, int tile, int32_t* 
     const int b = lo - 1;
     int ad = -1;
     if (row < a.total && b >= 0 && b < a.batch) {
-      ad = a.adapter[b];
+      ad = cached ? s_ad[b] : a.adapter[b];
       if (ad < 0 || ad >= a.n_adapters) ad = -1;
     }
     if (i == 0) *first_seq = max(b, 0);
@@ -216,6 +219,7 @@ __global__ void __launch_bounds__(D_THREADS, 1)
     }
     for (int g0 = c0 * D_GROUPS; g0 < all; g0 += per * D_GROUPS) {
       const int ng = min(D_GROUPS, all - g0);
+      float scale = 0.0f;                  // lane i of the summing warps: of group i
       if (warp == 0) {
         // (lane i: group i)
         const int ad = lane < ng ? s_list[(g0 + lane) / a.p.groups] : 0, at = (g0 + lane) % a.p.groups * G;
@@ -246,6 +250,7 @@ __global__ void __launch_bounds__(D_THREADS, 1)
         umma_commit(done);
       } else {
         const int quad = warp & 3;
+        if (lane < ng) scale = a.scale[s_list[(g0 + lane) / a.p.groups]];
         const bool ok = warp_wait_bounded(done, done_phase, abort_flag, a.status) && !*abort_flag;
         tc_fence_after();
         for (int c = 0; c < ng; ++c) {
@@ -283,11 +288,11 @@ __global__ void __launch_bounds__(D_THREADS, 1)
             v[4 * q] = s.x, v[4 * q + 1] = s.y, v[4 * q + 2] = s.z, v[4 * q + 3] = s.w;
           }
           const int ad = s_list[(g0 + c) / a.p.groups];
-          const float scale = a.scale[ad];
+          const float by = __shfl_sync(0xffffffffu, scale, c);
           uint32_t hi[8], lo[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float x = mine == ad ? v[2 * e] * scale : 0.0f, y = mine == ad ? v[2 * e + 1] * scale : 0.0f;
+            const float x = mine == ad ? v[2 * e] * by : 0.0f, y = mine == ad ? v[2 * e + 1] * by : 0.0f;
             const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
             const __nv_bfloat162 l = __floats2bfloat162_rn(x - __low2float(h), y - __high2float(h));
             hi[e] = *reinterpret_cast<const uint32_t*>(&h);
@@ -446,51 +451,56 @@ __global__ void __launch_bounds__(G_THREADS, 1)
   };
 
   if (warp == 0) {
-    if (lane == 0) {
-      const uint32_t full_l = cluster_addr(full, lead);
-      int stage = 0;
-      uint32_t phase = 0;
-      bool waited = false;
-      for (int u = u0; u < units && !*abort_flag; u += ustep) {
-        int mt, nt;
-        place(u, mt, nt);
-        const int n0 = nt * BN + half * (BN / 2);
-        bool ok = true;
-        for (int kb = k0; kb < k1; ++kb) {
-          if (!mbar_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status)) { ok = false; break; }
+    const uint32_t full_l = cluster_addr(full, lead);
+    int stage = 0;
+    uint32_t phase = 0;
+    bool waited = false;
+    for (int u = u0; u < units && !*abort_flag; u += ustep) {
+      int mt, nt;
+      place(u, mt, nt);
+      const int n0 = nt * BN + half * (BN / 2);
+      bool ok = true;
+      for (int kb = k0; kb < k1; ++kb) {
+        if (!(ok = warp_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status))) break;
+        if (lane == 0) {
           const uint32_t bar = full_l + 8u * stage;
           if (!half) mbar_arrive_expect_tx(&full[stage], 2 * C::STAGE_BYTES);
           tma_load_2d_pair(sB + stage * C::B_BYTES, &tmW, bar, kb * BK, n0);
           tma_load_2d_pair(sA + stage * C::A_BYTES, &tmX, bar, kb * BK, mt * TR + half * 128);
-          if (++stage == NST) { stage = 0; phase ^= 1; }
         }
-        if (!ok) break;
-        if (!waited) {                     // h and the lists come from the kernel before
-          pdl_enter();
-          waited = true;
-        }
-        int e0, e1;
-        const int groups = share(mt, e0, e1), base = a.p.base[mt];
-        const int32_t* list = a.p.list + static_cast<int64_t>(mt) * a.p.cap;
-        for (int kb = e0; kb < e1; ++kb) {
-          if (!mbar_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status)) { ok = false; break; }
-          const uint32_t bar = full_l + 8u * stage;
-          const int ng = min(2, groups - 2 * kb);
-          if (!half) mbar_arrive_expect_tx(&full[stage], 2 * (C::A_BYTES + ng * C::EXT_BYTES));
-          tma_load_2d_pair(sA + stage * C::A_BYTES, &tmH, bar, 0, (base + kb) * TR + half * 128);
-          for (int i = 0; i < ng; ++i)
-            tma_load_3d_pair(sB + stage * C::B_BYTES + i * C::EXT_BYTES, &tmB, bar, (2 * kb + i) % a.p.groups * G, n0,
-                             list[(2 * kb + i) / a.p.groups]);
-          if (++stage == NST) { stage = 0; phase ^= 1; }
-        }
-        if (!ok) break;
-      }
-      if (!waited) pdl_enter();            // (every block waits before it lets the next kernel start)
-      // every stage released: all copies into this block's memory have landed and been read
-      for (int i = 0; i < NST; ++i) {
-        mbar_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status);
         if (++stage == NST) { stage = 0; phase ^= 1; }
       }
+      if (!ok) break;
+      if (!waited) {                       // h and the lists come from the kernel before
+        pdl_enter();
+        waited = true;
+      }
+      int e0, e1;
+      const int groups = share(mt, e0, e1), base = a.p.base[mt];
+      const int32_t* list = a.p.list + static_cast<int64_t>(mt) * a.p.cap;
+      int ad = 0;                          // lane i: the adapter of group i of the next 32
+      for (int kb = e0; kb < e1; ++kb) {
+        if ((kb - e0) % 16 == 0) ad = 2 * kb + lane < groups ? list[(2 * kb + lane) / a.p.groups] : 0;
+        const int mine = __shfl_sync(0xffffffffu, ad, 2 * ((kb - e0) % 16) + (lane & 1));
+        if (!(ok = warp_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status))) break;
+        const uint32_t bar = full_l + 8u * stage;
+        const int ng = min(2, groups - 2 * kb);
+        if (lane == 0) {
+          if (!half) mbar_arrive_expect_tx(&full[stage], 2 * (C::A_BYTES + ng * C::EXT_BYTES));
+          tma_load_2d_pair(sA + stage * C::A_BYTES, &tmH, bar, 0, (base + kb) * TR + half * 128);
+        }
+        __syncwarp();
+        if (lane < ng)
+          tma_load_3d_pair(sB + stage * C::B_BYTES + lane * C::EXT_BYTES, &tmB, bar, (2 * kb + lane) % a.p.groups * G, n0, mine);
+        if (++stage == NST) { stage = 0; phase ^= 1; }
+      }
+      if (!ok) break;
+    }
+    if (!waited) pdl_enter();              // (every block waits before it lets the next kernel start)
+    // every stage released: all copies into this block's memory have landed and been read
+    for (int i = 0; i < NST; ++i) {
+      warp_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status);
+      if (++stage == NST) { stage = 0; phase ^= 1; }
     }
   } else if (warp == 1) {
     if (!half) {

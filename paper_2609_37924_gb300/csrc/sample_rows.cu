@@ -20,11 +20,18 @@
 //
 // A cluster of 1 to 8 blocks holds the row in shared memory: the logits leave
 // HBM once, whatever the settings ask for.  Block c has the c-th part of the
-// ids, warp w of it the w-th segment of that part.  A cut is narrowed down by
-// histograms of 512 bins, first over the value, then over the key, until 128
-// elements or one key are left.  What the blocks know together goes through
-// distributed shared memory; every block reads all parts and comes to the same
-// decisions.
+// ids, warp w of it the w-th segment of that part.  What the blocks know
+// together goes through distributed shared memory; every block reads all
+// parts and comes to the same decisions.
+//
+// Whole rows are summed by bulk(): the same weights in pairs of fp32 sums, a
+// third of weight()'s instructions.  The nucleus takes two passes: one sums
+// the row and counts it by value in 512 bins, which places the cut within
+// three of them; one sums what lies above those and lists what lies in them.
+// top-k begins with the lanes' maxima, the k-th largest of which is a lower
+// bound.  Listed elements are narrowed down by histograms over the key until
+// 128 elements or one key are left.  Where a list overflows or a guess was
+// wrong, the same histograms go over the whole row.
 #include <cstdint>
 
 #include "common.cuh"
@@ -147,6 +154,10 @@ __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, 
   return down <= 0 ? w << -down : (w + (1ull << (down - 1))) >> down;
 }
 
+// 2^f - 1 = f (A1 + f (A2 + f (A3 + f A4))) for |f| <= 1/32: ln2^n / n!, the last two eased to spread the error of the next
+// term (Chebyshev)
+constexpr float A1 = 0.693147182f, A2 = 0.240226507f, A3 = 0.0555057377f, A4 = 0.00961835496f;
+
 // ------------------------------------------------------------------ the cluster's shared memory
 __device__ __forceinline__ uint32_t remote_u32(uint32_t addr) {
   uint32_t v;
@@ -189,36 +200,48 @@ __device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, F&& pred
   return lo;
 }
 
+constexpr int CAP = 2048;                  // elements that a block lists
 struct Shared {
   uint64_t pow[32];
   uint64_t mass[2][NB];                    // histograms, two in turn
   uint32_t count[2][NB];
   uint64_t sums[2][NW];                    // per warp
-  uint64_t scan_mass[NW];
-  uint32_t scan_count[NW];
-  uint32_t found_id[2];                    // what pick() found
-  uint64_t found_w[2];
-  float2 top;                              // maximum and, of the finite ones, minimum of the block
-  uint32_t list_n[2];
-  uint32_t list_key[2][LIST], list_id[2][LIST];
+  uint64_t above[NW];                      // per warp: of what lies above the list
+  uint64_t scan[NW];
+  float scan_f[NW];
+  float2 top;                              // largest and smallest of the lanes' maxima in the block
+  float2 wtop[NW];
+  uint32_t list_n, few_n;
+  uint16_t list[CAP];                      // places in the block's part
+  uint32_t few_key[LIST], few_id[LIST];
   uint64_t all_w[LIST];
   uint32_t all_key[LIST], all_id[LIST];
+  uint32_t found_id[2];                    // what pick() found
+  uint64_t found_w[2];
   uint64_t part[NW];
-  float wmax[NW];
-  float fhi, flo;
+  float2 pow16[16];                        // bulk(): 2^(j/16) 2^-(M - Mh) in two fp32 terms
+  float c_hi, c_lo, low;                   // log2(e) / T; the row's least logit that min-p keeps, less the maximum
+  double low64;
+  float mh;
   // what one thread decides for its block
-  uint64_t d_mass;
   uint32_t d_bin, d_count, d_key, d_id;
   uint64_t d_above;
-  uint32_t d_above_n;
 };
-
 static_assert((sizeof(Shared) + 15) / 16 * 16 + (kSampleMaxVocab + MAXC * NW * 128 - 1) / (MAXC * NW * 128) * 128 * NW * 4 <= 232448, "shared memory");
 
 struct Cut {
   uint32_t key;
   int id;                                  // ids of that key up to this one are kept
 };
+constexpr int ALL = 0x7fffffff;
+constexpr float kFlat = 1e-30f;            // log2(e) / T above which a finite logit can stand for one that weighs nothing (bulk)
+
+__device__ __forceinline__ uint64_t pair(float x) { return f2_pack(x, x); }
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 template <class T, int CS>
 struct Row {
@@ -228,6 +251,7 @@ struct Row {
   int first, seg, rank;                    // id of the part's first element
   Scale s;
   int turn;                                // of the arrays that pick() uses in turn: a sync lies between two uses of one
+  bool listed;                             // each() goes over the list
 
   __device__ __forceinline__ uint64_t w(float l) const { return weight(s, sh.pow, l); }
   __device__ __forceinline__ static bool kept(const Cut& c, uint32_t key, int id) { return key > c.key || (key == c.key && id <= c.id); }
@@ -235,9 +259,19 @@ struct Row {
     if constexpr (CS > 1) cluster_sync();
     else __syncthreads();
   }
-  // f(logit, id) of this warp's elements whose logit is at least `least`
+  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(data)[i]); }
+  // f(logit, id) of this warp's elements (listed: of this thread's listed ones) whose logit is at least `least`
   template <class F>
   __device__ __forceinline__ void each(float least, F&& f) const {
+    if (listed) {
+      const int n = sh.list_n;
+      for (int i = threadIdx.x; i < n; i += NT) {
+        const int p = sh.list[i];
+        const float v = at(p);
+        if (v >= least) f(v, first + p);
+      }
+      return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint4* p = data + warp * (seg / V::N);
     for (int i = lane; i < seg / V::N; i += 32) {
@@ -248,16 +282,111 @@ struct Row {
         if (v[e] >= least) f(v[e], first + warp * seg + i * V::N + e);
     }
   }
-  // Sum of f over the elements with a logit of at least `least`; with `id`, also the first element in the order of ids with
-  // which the sum exceeds target(whole sum), and its f.
+
+  // Sum of the weights of this warp's elements above `cut` (a logit, exclusive), in units of ONE^-1, in lane 0.  With
+  // BINS also a histogram by value, in bins of width 1 / per below the maximum (none past the last bin): an element adds its
+  // weight over that of its bin's middle, linear in its place within the bin, in 2^-14.
+  //
+  // t = c x - M (c = log2(e) / T, M = c max; x a logit, less the maximum where c max is large) without the rounding of a
+  // difference: j = 16 t to the nearest whole number, f = c x - Mh - j / 16 by one fma, Mh the multiple of 1/16 next to M,
+  // plus c's second term; 2^f - 1 by a polynomial of degree 4 (error 2^-36 for |f| <= 1/32, coefficients below); times the
+  // table's 2^(j/16) 2^(Mh - M) in two terms.  The sum is split at 2^-17: multiples of that add without rounding (at most
+  // 104 of them a lane), the rest carries errors of about 2^-37 a lane.
+  template <bool BINS>
+  __device__ uint64_t bulk(float cut, float per, uint32_t* hist) const {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool far = fabsf(s.max * s.hi) >= 92.0f;            // then logits that weigh anything are near the maximum
+    const float shift = far ? s.max : 0.0f, mh = sh.mh;
+    const float none = fmaxf(s.max - shift - 60.0f / s.hi, -3.0e38f);   // stands for elements that are not summed: 2^-60
+    const uint64_t k_shift = pair(-shift), k_hi16 = pair(16.0f * s.hi), k_c = pair(12582912.0f - 16.0f * mh), k_back = pair(-12582912.0f);
+    const uint64_t k_n16 = pair(-0.0625f), k_nmh = pair(-mh), k_hi = pair(s.hi), k_lo = pair(s.lo), k_minus = pair(-1.0f);
+    const uint64_t k_up = pair(96.0f), k_down = pair(-96.0f);
+    const uint64_t a1 = pair(A1), a2 = pair(A2), a3 = pair(A3), a4 = pair(A4);
+    const uint64_t b_per = pair(-per), b_c = pair(fmaf(s.max, per, 12582912.0f)), b_slope = pair(-16384.0f * 0.693147181f * s.hi / per);
+    const uint64_t b_one = pair(12582912.0f + 16384.0f);
+    uint64_t big = 0, small = 0;
+    cut = fmaxf(cut, fminf(s.max - 60.0f / s.hi, below(s.max)));
+    auto two = [&](float v0, float v1) {
+      const bool in0 = v0 > cut, in1 = v1 > cut;
+      if constexpr (BINS) {
+        const uint64_t v = f2_pack(v0, v1), q = f2_fma(v, b_per, b_c);
+        const uint64_t d = f2_fma(v, b_per, f2_fma(q, k_minus, b_c));     // from the bin's middle, in bins
+        float q0, q1, m0, m1;
+        f2_unpack(q, q0, q1);
+        f2_unpack(f2_fma(d, b_slope, b_one), m0, m1);
+        const uint32_t i0 = __float_as_uint(q0) - 0x4b400000u, i1 = __float_as_uint(q1) - 0x4b400000u;
+        if (in0 && i0 < NB - 1) atomicAdd(&hist[i0], __float_as_uint(m0) - 0x4b400000u);
+        if (in1 && i1 < NB - 1) atomicAdd(&hist[i1], __float_as_uint(m1) - 0x4b400000u);
+      }
+      float x0, x1;
+      f2_unpack(f2_add(f2_pack(v0, v1), k_shift), x0, x1);
+      const uint64_t x = f2_pack(in0 ? x0 : none, in1 ? x1 : none);
+      const uint64_t q = f2_fma(x, k_hi16, k_c), j = f2_add(q, k_back);
+      const uint64_t g = f2_fma(x, k_lo, f2_fma(x, k_hi, f2_fma(j, k_n16, k_nmh)));
+      const uint64_t r = f2_mul(g, f2_fma(g, f2_fma(g, f2_fma(g, a4, a3), a2), a1));
+      float q0, q1;
+      f2_unpack(q, q0, q1);
+      const uint32_t b0 = __float_as_uint(q0), b1 = __float_as_uint(q1);
+      const float2 t0 = sh.pow16[b0 & 15], t1 = sh.pow16[b1 & 15];
+      // 2^n, n = floor(j / 16): the magic number's bits drop out of the shifted word
+      constexpr uint32_t BIAS = (127u << 23) - (0x4b400000u >> 4 << 23);
+      const uint64_t p2 = f2_pack(__uint_as_float((b0 >> 4 << 23) + BIAS), __uint_as_float((b1 >> 4 << 23) + BIAS));
+      const uint64_t a = f2_mul(f2_pack(t0.x, t1.x), p2), al = f2_mul(f2_pack(t0.y, t1.y), p2);
+      const uint64_t t = f2_fma(a, r, al), h = f2_add(a, t), l = f2_add(f2_fma(h, k_minus, a), t);
+      const uint64_t up = f2_add(f2_add(h, k_up), k_down);
+      big = f2_add(big, up);
+      small = f2_add(small, f2_add(f2_fma(up, k_minus, h), l));
+    };
+    const uint4* p = data + warp * (seg / V::N);
+#pragma unroll 2
+    for (int i = lane; i < seg / V::N; i += 32) {
+      float v[V::N];
+      V::get(p[i], v);
+#pragma unroll
+      for (int e = 0; e < V::N; e += 2) two(v[e], v[e + 1]);
+    }
+    float h0, h1, l0, l1;
+    f2_unpack(big, h0, h1);
+    f2_unpack(small, l0, l1);
+    const int64_t whole = static_cast<int64_t>(__float2int_rn(h0 * 131072.0f)) + __float2int_rn(h1 * 131072.0f);
+    return warp_sum_u64(static_cast<uint64_t>((whole << 27) + __float2ll_rn((l0 + l1) * 17592186044416.0f)));
+  }
+  // the largest logit below `v`
+  __device__ __forceinline__ static float below(float v) {
+    return v == 0.0f ? -1.4e-45f : Key<float>::value(Key<float>::of(v) - 1);
+  }
+  // Per warp into sums[turn]: the weights of what `cut` keeps.
+  __device__ void sums_kept(const Cut& cut) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (listed) {                                             // all of it is on the list
+      if (threadIdx.x < NW) sh.sums[turn][threadIdx.x] = sh.above[threadIdx.x];
+      __syncthreads();
+      each(Key<T>::value(cut.key), [&](float l, int id) {
+        if (kept(cut, Key<T>::of(l), id))
+          atomicAdd(reinterpret_cast<unsigned long long*>(&sh.sums[turn][(id - first) / seg]), static_cast<unsigned long long>(w(l)));
+      });
+      return;
+    }
+    const float v = Key<T>::value(cut.key);
+    uint64_t mine = s.hi > kFlat ? bulk<false>(cut.id == ALL ? below(v) : v, 0.0f, nullptr) : 0;
+    if (cut.id != ALL) {
+      uint64_t ties = 0;
+      each(v, [&](float l, int id) { ties += l == v && id <= cut.id ? 1 : 0; });
+      mine += warp_sum_u64(ties) * w(v);
+    }
+    if (__shfl_sync(0xffffffffu, mine, 0) < 2ull * seg) {     // nearly nothing: exactly what weight() gives, so that it can be drawn from
+      mine = 0;
+      each(v, [&](float l, int id) { mine += kept(cut, Key<T>::of(l), id) ? w(l) : 0; });
+      mine = warp_sum_u64(mine);
+    }
+    if (lane == 0) sh.sums[turn][warp] = mine;
+  }
+
+  // From the warps' sums[turn]: their sum over the cluster; with `id`, also the first element in the order of ids with which
+  // the sum of f exceeds target(whole sum), and its f.  (The warps' sums may differ from f's in the last bits.)
   template <class F, class G>
   __device__ uint64_t pick(float least, F&& f, G&& target, int* id, uint64_t* value) {
-    turn ^= 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint64_t mine = 0;
-    each(least, [&](float l, int i) { mine += f(l, i); });
-    mine = warp_sum_u64(mine);
-    if (lane == 0) sh.sums[turn][warp] = mine;
     sync();
     // every warp: lane l has the sums of CS * NW / 32 consecutive warps
     constexpr int PER = CS * NW >= 32 ? CS * NW / 32 : 1, LANES = CS * NW / PER;
@@ -269,14 +398,13 @@ struct Row {
       own += part[i];
     }
     const uint64_t incl = warp_scan_u64(own), total = __shfl_sync(0xffffffffu, incl, 31);
-    if (!id) return total;
-    const uint64_t t = target(total);
-    const unsigned past = __ballot_sync(0xffffffffu, incl > t);
-    if (!past) {                                              // (t is below a sum that is not zero)
-      *id = -1;
+    if (!id) {
+      turn ^= 1;
       return total;
     }
-    const int src = __ffs(past) - 1;
+    const uint64_t t = target(total);
+    const unsigned past = __ballot_sync(0xffffffffu, incl > t);
+    const int src = past ? __ffs(past) - 1 : 31;
     uint64_t left = t - (incl - own);
     int at = lane * PER;
 #pragma unroll
@@ -306,16 +434,19 @@ struct Row {
       a = warp_sum_u64(a);
       if (lane == 0) sh.part[warp] = a;
       __syncthreads();
-      const uint64_t x = lane < NW ? sh.part[lane] : 0, inc = warp_scan_u64(x);
-      const int who = __ffs(__ballot_sync(0xffffffffu, inc > left)) - 1;
+      const uint64_t x = lane < NW ? sh.part[lane] : 0, inc = warp_scan_u64(x), all = __shfl_sync(0xffffffffu, inc, 31);
+      left = min(left, all - 1);
+      const unsigned over = __ballot_sync(0xffffffffu, inc > left);
+      if (!over && threadIdx.x == 0) sh.found_id[turn] = 0xffffffffu, sh.found_w[turn] = 0;
+      const int who = __ffs(over) - 1;
       if (who == warp) {
         left -= __shfl_sync(0xffffffffu, inc - x, who);
         for (int c = c0; c < c1; ++c) {
-          const uint64_t mine2 = lane_sum(c), in = warp_scan_u64(mine2);
+          const uint64_t mine = lane_sum(c), in = warp_scan_u64(mine);
           const unsigned hit = __ballot_sync(0xffffffffu, in > left);
           if (hit) {
             if (lane == __ffs(hit) - 1) {
-              uint64_t rem = left - (in - mine2);
+              uint64_t rem = left - (in - mine);
               float v[V::N];
               V::get(p[c * 32 + lane], v);
               bool open = true;
@@ -340,25 +471,68 @@ struct Row {
     sync();
     *id = static_cast<int>(remote_u32(cluster_addr(&sh.found_id[turn], at / NW)));
     if (value) *value = remote_u64(cluster_addr(&sh.found_w[turn], at / NW));
+    turn ^= 1;
     return total;
+  }
+  // Sums of f, which is 0 or 1, into the warps' sums.
+  template <class F>
+  __device__ void sums_of(float least, F&& f) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool l = listed;
+    listed = false;
+    uint64_t mine = 0;
+    each(least, [&](float v, int i) { mine += f(v, i); });
+    listed = l;
+    mine = warp_sum_u64(mine);
+    if (lane == 0) sh.sums[turn][warp] = mine;
+  }
+
+  // Lists the elements from `least` to `most` that `from` keeps.  False (in every block): one of the lists is too short for them.
+  __device__ bool make_list(const Cut& from, float least, float most) {
+    listed = false;
+    if (threadIdx.x == 0) sh.list_n = 0;
+    if (threadIdx.x < NW) sh.above[threadIdx.x] = 0;
+    __syncthreads();
+    each(least, [&](float l, int id) {
+      if (l > most || !kept(from, Key<T>::of(l), id)) return;
+      const uint32_t i = atomicAdd(&sh.list_n, 1u);
+      if (i < CAP) sh.list[i] = static_cast<uint16_t>(id - first);
+    });
+    sync();
+    uint32_t n = 0;
+#pragma unroll
+    for (int r = 0; r < CS; ++r) n = max(n, remote_u32(cluster_addr(&sh.list_n, r)));
+    listed = n <= CAP;
+    return listed;
+  }
+
+  // Sum over the threads up to this one and over all (block-collective); the arrays may be used again after a __syncthreads.
+  __device__ __forceinline__ uint64_t scan_block(uint64_t own) const {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint64_t incl = warp_scan_u64(own);
+    if (lane == 31) sh.scan[warp] = incl;
+    __syncthreads();
+    const uint64_t x = warp_scan_u64(lane < NW ? sh.scan[lane] : 0);
+    return warp > 0 ? incl + __shfl_sync(0xffffffffu, x, warp - 1) : incl;
   }
 
   // The cut that keeps, of the elements that `from` keeps, the first ones of the order: `target` of them (BY_MASS: as many
   // as have less than `target` of mass in front of them).  At least one element is kept by `from`, target >= 1 and at most
-  // all of them (their mass).  lo: a key below which nothing needs to be looked at.
+  // all of them (their mass).  Keys outside lo .. hi need not be looked at; `above`: what lies above hi counts.  False: the cut is not
+  // between lo and hi.
   template <bool BY_MASS>
-  __device__ Cut narrow(Cut from, uint32_t lo, uint32_t hi, uint64_t target) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint64_t above = 0;                    // what lies above the window counts: elements or mass
+  __device__ bool narrow(const Cut& from, uint32_t lo, uint32_t hi, uint64_t above, uint64_t target, Cut* cut) {
+    const uint64_t start = above;
     uint32_t inside = 0xffffffffu;         // elements in the window
+    bool by_value = hi == Key<T>::of(s.max);   // first by value, in steps of equal ratios of weights; then by key
     for (int level = 0; lo < hi && inside > LIST; ++level) {
       const int buf = level & 1;
       sh.count[buf][threadIdx.x] = 0;
       sh.mass[buf][threadIdx.x] = 0;
+      if (threadIdx.x == 0) sh.d_count = 0;
       __syncthreads();
-      // first by value, in steps of equal ratios of weights; then by key
       const float range = s.max - Key<T>::value(lo);
-      const bool by_value = level == 0 && range < 3e38f;
+      by_value = by_value && range < 3e38f;
       const float per = by_value ? (NB - 1) / range : 0.0f;
       int shift = 0;
       while (((hi - lo) >> shift) >= NB) ++shift;
@@ -380,12 +554,7 @@ struct Row {
         n += remote_u32(cluster_addr(&sh.count[buf][threadIdx.x], r));
         if (BY_MASS) m += remote_u64(cluster_addr(&sh.mass[buf][threadIdx.x], r));
       }
-      const uint64_t own = BY_MASS ? m : n;
-      uint64_t incl = warp_scan_u64(own);
-      if (lane == 31) sh.scan_mass[warp] = incl;
-      __syncthreads();
-      const uint64_t x = warp_scan_u64(lane < NW ? sh.scan_mass[lane] : 0);
-      if (warp > 0) incl += __shfl_sync(0xffffffffu, x, warp - 1);
+      const uint64_t own = BY_MASS ? m : n, incl = scan_block(own);
       if (above + incl >= target && above + incl - own < target) {
         sh.d_bin = threadIdx.x;
         sh.d_count = n;
@@ -394,12 +563,14 @@ struct Row {
       __syncthreads();
       const uint32_t bin = sh.d_bin;
       inside = sh.d_count;
+      if (inside == 0) return false;
       above = sh.d_above;
       if (by_value) {
         const int b = static_cast<int>(bin);
         const uint32_t lo2 = first_key(lo, hi, [&](uint32_t k) { return value_bin(Key<T>::value(k)) <= b; });
         if (b > 0) hi = first_key(lo2, hi, [&](uint32_t k) { return value_bin(Key<T>::value(k)) <= b - 1; }) - 1;
         lo = lo2;
+        by_value = false;
       } else {
         const uint32_t top = hi - (bin << shift);
         lo = max(lo, top - min(top, (1u << shift) - 1));
@@ -409,44 +580,47 @@ struct Row {
     }
     const float least = Key<T>::value(lo), most = Key<T>::value(hi);
     if (lo >= hi) {
+      if (above >= target) return false;
       // one key: of its ids the first ones, in the order of ids
       uint64_t need = target - above;
       if (BY_MASS) {
         const uint64_t each_w = w(least);
+        if (each_w == 0) return false;
         need = (need + each_w - 1) / each_w;
       }
+      auto one = [&](float l, int i) { return l == least && kept(from, Key<T>::of(l), i) ? 1ull : 0ull; };
       int id;
-      pick(least, [&](float l, int i) { return l == least && kept(from, Key<T>::of(l), i) ? 1ull : 0ull; },
-           [&](uint64_t) { return need - 1; }, &id, nullptr);
-      return {lo, id};
+      sums_of(least, one);
+      if (pick(least, one, [&](uint64_t all) { return min(all, need) - 1; }, &id, nullptr) < need && above == start) return false;
+      *cut = {lo, id};
+      return true;
     }
     // a few elements: each of them finds what is in front of it
-    if (threadIdx.x == 0) sh.list_n[0] = 0;
+    if (threadIdx.x == 0) sh.few_n = 0, sh.d_id = 0xffffffffu;
     __syncthreads();
     each(least, [&](float l, int id) {
       const uint32_t key = Key<T>::of(l);
       if (l > most || !kept(from, key, id)) return;
-      const uint32_t at = atomicAdd(&sh.list_n[0], 1u);
-      sh.list_key[0][at] = key;
-      sh.list_id[0][at] = id;
+      const uint32_t i = atomicAdd(&sh.few_n, 1u);
+      sh.few_key[i] = key;
+      sh.few_id[i] = id;
     });
     sync();
-    uint32_t before = 0, n_all = 0, off = 0;
+    uint32_t n_all = 0, off = 0;
     int src = -1;
 #pragma unroll
     for (int r = 0; r < CS; ++r) {
-      const uint32_t n = remote_u32(cluster_addr(&sh.list_n[0], r));
-      if (threadIdx.x >= before && threadIdx.x < before + n) {
+      const uint32_t n = remote_u32(cluster_addr(&sh.few_n, r));
+      if (threadIdx.x >= n_all && threadIdx.x < n_all + n) {
         src = r;
-        off = threadIdx.x - before;
+        off = threadIdx.x - n_all;
       }
-      before += n;
+      n_all += n;
     }
-    n_all = before;
     if (src >= 0) {
-      const uint32_t key = remote_u32(cluster_addr(&sh.list_key[0][off], src));
+      const uint32_t key = remote_u32(cluster_addr(&sh.few_key[off], src));
       sh.all_key[threadIdx.x] = key;
-      sh.all_id[threadIdx.x] = remote_u32(cluster_addr(&sh.list_id[0][off], src));
+      sh.all_id[threadIdx.x] = remote_u32(cluster_addr(&sh.few_id[off], src));
       sh.all_w[threadIdx.x] = BY_MASS ? w(Key<T>::value(key)) : 1;
     }
     __syncthreads();
@@ -466,8 +640,85 @@ struct Row {
         sh.d_id = sh.all_id[i];
       }
     }
-    sync();                                                   // (the lists have been read by all)
-    return {sh.d_key, static_cast<int>(sh.d_id)};
+    sync();                                                   // (the few have been read by all)
+    *cut = {sh.d_key, static_cast<int>(sh.d_id)};
+    return cut->id >= 0;
+  }
+
+  // A key below which no element is among the first k: the lanes' maxima, `mine` of each, are counted by value.
+  __device__ uint32_t bound_k(uint32_t lo, uint32_t hi, float mine, float least_mine, uint64_t k) {
+    const float range = s.max - least_mine;
+    if (!(range > 0.0f && range < 3e38f)) return lo;
+    const float per = (NB - 1) / range;
+    auto value_bin = [&](float l) { return min(NB - 1, static_cast<int>((s.max - l) * per)); };
+    sh.count[0][threadIdx.x] = 0;
+    if (threadIdx.x == 0) sh.d_bin = NB;
+    __syncthreads();
+    if (mine >= least_mine) atomicAdd(&sh.count[0][value_bin(mine)], 1u);
+    sync();
+    uint32_t n = 0;
+#pragma unroll
+    for (int r = 0; r < CS; ++r) n += remote_u32(cluster_addr(&sh.count[0][threadIdx.x], r));
+    const uint64_t incl = scan_block(n);
+    if (incl >= k && incl - n < k) sh.d_bin = threadIdx.x;
+    __syncthreads();
+    const int b = static_cast<int>(sh.d_bin);
+    sync();                                                   // (the counts may be written again)
+    if (b >= NB - 1) return lo;
+    return max(lo, first_key(lo, hi, [&](uint32_t key) { return value_bin(Key<T>::value(key)) <= b; }));
+  }
+
+  // The nucleus of a row that is not listed: p of the mass of what `from` keeps.
+  __device__ Cut nucleus(const Cut& from, float p, int vocab) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t khi = Key<T>::of(s.max);
+    auto nothing = [](float, int) { return 0ull; };
+    auto any = [](uint64_t) { return 0ull; };
+    auto target_of = [&](uint64_t mass) {
+      const uint64_t t = static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(mass)));
+      return min(max(t, static_cast<uint64_t>(1)), mass);
+    };
+    Cut cut{};
+    // Ids that weigh less than (1 - p) / vocab of the maximum together weigh less than 1 - p of the mass: none is kept.
+    const float depth = (__log2f(static_cast<float>(vocab) / (1.0f - p)) + 0.5f) / s.hi;
+    const uint32_t low = max(from.key, Key<T>::of(s.max - depth));
+    if (from.id == ALL && from.key < khi && s.hi > kFlat) {
+      const float cutv = below(Key<T>::value(from.key)), per = (NB - 2) / depth;
+      sh.count[0][threadIdx.x] = 0;
+      if (threadIdx.x == 0) sh.d_bin = NB;
+      __syncthreads();
+      const uint64_t mine = bulk<true>(cutv, per, sh.count[0]);
+      if (lane == 0) sh.sums[turn][warp] = mine;
+      const uint64_t mass = pick(0.0f, nothing, any, nullptr, nullptr);
+      const uint64_t target = target_of(mass);
+      uint32_t n = 0;
+#pragma unroll
+      for (int r = 0; r < CS; ++r) n += remote_u32(cluster_addr(&sh.count[0][threadIdx.x], r));
+      // a bin's mass, about, in 2^-32 of the maximum's
+      const float b_c = fmaf(s.max, per, 12582912.0f), off = fmaf(-s.max, per, b_c - 12582912.0f);   // (of the maximum from its bin's middle)
+      const float mid = ex2_approx((off - static_cast<float>(threadIdx.x)) / per * s.hi) * 262144.0f;
+      const uint64_t guess = static_cast<uint64_t>(static_cast<float>(n) * mid), incl = scan_block(guess);
+      if (incl >= target >> 12 && incl - guess < target >> 12) sh.d_bin = threadIdx.x;
+      __syncthreads();
+      const int b = static_cast<int>(sh.d_bin);
+      if (b < NB - 2) {
+        // the keys of the bins b - 1 .. b + 1
+        auto bin = [&](uint32_t k) { return static_cast<int>(__float_as_uint(fmaf(Key<T>::value(k), -per, b_c)) - 0x4b400000u); };
+        const uint32_t lo = first_key(low, khi, [&](uint32_t k) { return bin(k) <= b + 1; });
+        const uint32_t hi = b > 1 ? first_key(lo, khi, [&](uint32_t k) { return bin(k) <= b - 2; }) - 1 : khi;
+        if (make_list(from, Key<T>::value(lo), Key<T>::value(hi))) {
+          const uint64_t over = hi < khi ? bulk<false>(Key<T>::value(hi), 0.0f, nullptr) : 0;
+          if (lane == 0) sh.above[warp] = sh.sums[turn][warp] = over;
+          const uint64_t above = pick(0.0f, nothing, any, nullptr, nullptr);
+          if (above < target && narrow<true>(from, lo, hi, above, target, &cut)) return cut;
+          listed = false;
+        }
+      }
+    }
+    sums_kept(from);
+    const uint64_t mass = pick(0.0f, nothing, any, nullptr, nullptr);
+    if (!narrow<true>(from, low, khi, 0, target_of(mass), &cut)) cut = from;
+    return cut;
   }
 };
 
@@ -485,13 +736,10 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SampleArgs a) {
   const int first = rank * NW * a.seg;
   const T* src = static_cast<const T*>(a.logits) + row * a.ld;
   const float ninf = __int_as_float(0xff800000);
+  const float t = a.temperature ? a.temperature[row] : 1.0f, p = a.top_p ? a.top_p[row] : 1.0f, mp = a.min_p ? a.min_p[row] : 0.0f;
+  const int k = !(t > 0x1p-100f) || p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
+  const float u0 = a.u[row];
   float top = ninf;
-  if (threadIdx.x == 0) {
-    const float t = a.temperature ? a.temperature[row] : 1.0f;
-    const double c = 1.4426950408889634074 / static_cast<double>(t);
-    sh.fhi = static_cast<float>(c);
-    sh.flo = static_cast<float>(c - static_cast<double>(sh.fhi));
-  }
   {
     const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
     const int base = first + warp * a.seg, n = a.seg / V::N;
@@ -499,12 +747,16 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SampleArgs a) {
     auto take = [&](int i, const uint4& q) {
       float v[V::N];
       V::get(q, v);
+      const int id = base + i * V::N;
 #pragma unroll
-      for (int e = 0; e < V::N; ++e) {
-        const int id = base + i * V::N + e;
-        v[e] = v[e] != v[e] || id == a.mask_id || id >= a.vocab ? ninf : v[e] + 0.0f;
-        top = fmaxf(top, v[e]);
+      for (int e = 0; e < V::N; ++e) v[e] = fmaxf(v[e] + 0.0f, ninf);   // NaN: -inf
+      if (static_cast<uint32_t>(a.mask_id - id) < V::N) {
+#pragma unroll
+        for (int e = 0; e < V::N; ++e)
+          if (id + e == a.mask_id) v[e] = ninf;
       }
+#pragma unroll
+      for (int e = 0; e < V::N; ++e) top = fmaxf(top, v[e]);
       dst[i] = V::put(v);
     };
     auto one = [&](int i) {                                   // element by element: the row's end, and rows off 16 bytes
@@ -529,15 +781,31 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SampleArgs a) {
         if (i0 + 32 * k < n) take(i0 + 32 * k, q[k]);
     }
   }
-  top = warp_max(top);
-  if (lane == 0) sh.wmax[warp] = top;
+  const float lane_top = top;
+  {
+    const float hi = warp_max(top), lo = -warp_max(top > ninf ? -top : ninf);
+    if (lane == 0) sh.wtop[warp] = make_float2(hi, lo);
+  }
+  if (threadIdx.x == 0) {                                     // (double precision is slow here: one thread, for all)
+    const double c = 1.4426950408889634074 / static_cast<double>(t);
+    sh.c_hi = static_cast<float>(c);
+    sh.c_lo = static_cast<float>(c - static_cast<double>(sh.c_hi));
+    if (mp > 0.0f) sh.low64 = mp >= 1.0f ? 0.0 : static_cast<double>(t) * log(static_cast<double>(mp));
+  }
   __syncthreads();
-  top = warp_max(lane < NW ? sh.wmax[lane] : ninf);
-  if (threadIdx.x == 0) sh.top.x = top;
-  Row<T, CS> r{sh, data, first, a.seg, rank, {}, 0};
+  if (warp == 0) {
+    const float2 x = lane < NW ? sh.wtop[lane] : make_float2(ninf, -ninf);
+    const float hi = warp_max(x.x), lo = -warp_max(-x.y);
+    if (lane == 0) sh.top = make_float2(hi, lo);
+  }
+  Row<T, CS> r{sh, data, first, a.seg, rank, {}, 0, false};
   r.sync();
+  float least_top = -ninf;
 #pragma unroll
-  for (int k = 0; k < CS; ++k) top = fmaxf(top, __uint_as_float(remote_u32(cluster_addr(&sh.top, k))));
+  for (int i = 0; i < CS; ++i) {
+    top = fmaxf(top, __uint_as_float(remote_u32(cluster_addr(&sh.top.x, i))));
+    least_top = fminf(least_top, __uint_as_float(remote_u32(cluster_addr(&sh.top.y, i))));
+  }
   const bool writer = rank == 0 && threadIdx.x == 0;
   if (top == ninf) {                                          // nothing to draw from
     if (writer) {
@@ -547,41 +815,78 @@ __global__ void __launch_bounds__(NT) sample_kernel(const SampleArgs a) {
     r.sync();
     return;
   }
-  r.s = {top, sh.fhi, sh.flo};
   const uint32_t khi = Key<T>::of(top);
-  const float t = a.temperature ? a.temperature[row] : 1.0f;
-  const int k = !(t > 0x1p-100f) ? 1 : a.top_k ? a.top_k[row] : 0;
-  const float p = a.top_p ? a.top_p[row] : 1.0f, mp = a.min_p ? a.min_p[row] : 0.0f;
   int id = -1;
-  if (k == 1 || p <= 0.0f) {
-    // the first of the order: the lowest id of the maximum
-    r.pick(top, [&](float, int) { return 1ull; }, [](uint64_t) { return 0ull; }, &id, nullptr);
+  if (k == 1 || top == -ninf) {
+    // the first of the order, the lowest id of the maximum; or, of an infinite maximum, ids of equal weight
+    auto of_max = [&](float l, int) { return l == top ? 1ull : 0ull; };
+    r.sums_of(top, of_max);
+    uint64_t n = 1;
+    r.pick(top, of_max, [&](uint64_t all) {
+      if (k == 1) return static_cast<uint64_t>(0);
+      n = k > 0 ? min(all, static_cast<uint64_t>(k)) : all;
+      if (p < 1.0f) n = min(n, max(static_cast<uint64_t>(1), static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(n)))));
+      const double x = (u0 > 0.0f ? static_cast<double>(u0) : 0.0) * static_cast<double>(n);
+      return x >= static_cast<double>(n) ? n - 1 : static_cast<uint64_t>(x);
+    }, &id, nullptr);
     if (writer) {
       a.tok[row] = id;
-      if (a.prob) a.prob[row] = 1.0f;
+      if (a.prob) a.prob[row] = 1.0f / static_cast<float>(n);
     }
     r.sync();
     return;
   }
-  // ---- the cut: weights that count at all, min-p, top-k, top-p
-  uint64_t least_w = 1;
-  if (mp > 0.0f) least_w = mp >= 1.0f ? ONE : max(static_cast<uint64_t>(1), static_cast<uint64_t>(ceil(static_cast<double>(mp) * static_cast<double>(ONE))));
-  const uint32_t kinf = Key<T>::of(ninf) + 1;
-  Cut cut{first_key(kinf, khi, [&](uint32_t key) { return r.w(Key<T>::value(key)) >= least_w; }), 0x7fffffff};
-  if (k > 0 && k < a.vocab) {
-    const uint64_t n = r.pick(Key<T>::value(cut.key), [&](float, int) { return 1ull; }, [](uint64_t) { return 0ull; }, nullptr, nullptr);
-    if (n > static_cast<uint64_t>(k)) cut = r.template narrow<false>(cut, cut.key, khi, k);
+  r.s = {top, sh.c_hi, sh.c_lo};
+  // ---- what bulk() needs of the row: M = c max (max less itself where it is large) to 1/16, and the table with the rest of it
+  if (threadIdx.x < 16) {
+    const float xm = fabsf(top * r.s.hi) >= 92.0f ? 0.0f : top;
+    const float m = xm * r.s.hi, e = fmaf(xm, r.s.lo, fmaf(xm, r.s.hi, -m));
+    const float mh = rintf(16.0f * m) * 0.0625f, rest = (m - mh) + e;      // |rest| <= 1/32
+    const double f = -static_cast<double>(rest) * 0.693147180559945309417;
+    const double x = 1.0 + f * (1.0 + f * (0.5 + f * (1.0 / 6 + f * (1.0 / 24 + f * (1.0 / 120 + f / 720)))));
+    const double v = x * (static_cast<double>(sh.pow[2 * threadIdx.x]) * 0x1p-43);
+    const float h = static_cast<float>(v);
+    sh.pow16[threadIdx.x] = make_float2(h, static_cast<float>(v - static_cast<double>(h)));
+    sh.mh = mh;
+    if (threadIdx.x == 0) {                                   // the least logit that min-p keeps, rounded up
+      const double least = mp > 0.0f ? static_cast<double>(top) + sh.low64 : -INFINITY;
+      sh.low = __double2float_ru(least);
+    }
   }
-  auto kept_w = [&](float l, int i) { return r.kept(cut, Key<T>::of(l), i) ? r.w(l) : 0ull; };
+  if (threadIdx.x < NW) sh.above[threadIdx.x] = 0;
+  __syncthreads();
+  // ---- the cut: min-p, top-k, top-p
+  Cut cut{Key<T>::of(ninf) + 1, ALL};
+  if (mp > 0.0f) {
+    const float low = fminf(sh.low, top) + 0.0f;
+    const uint32_t key = Key<T>::of(low);
+    cut.key = max(cut.key, Key<T>::value(key) < low ? key + 1 : key);
+  }
+  if (k > 0 || mp > 0.0f) {
+    const uint32_t lo = k > 0 && k < a.vocab ? r.bound_k(cut.key, khi, lane_top, least_top, k) : cut.key;
+    r.make_list(cut, Key<T>::value(lo), top);
+    if (k > 0 && k < a.vocab) {
+      // (fewer than k: all of them)
+      Cut to{};
+      if (r.template narrow<false>(cut, lo, khi, 0, k, &to)) cut = to;
+    }
+  }
   if (p < 1.0f) {
-    const uint64_t mass = r.pick(Key<T>::value(cut.key), kept_w, [](uint64_t) { return 0ull; }, nullptr, nullptr);
-    const uint64_t target = max(static_cast<uint64_t>(1), static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(mass))));
-    cut = r.template narrow<true>(cut, cut.key, khi, min(target, mass));
+    if (r.listed) {
+      r.sums_kept(cut);
+      const uint64_t mass = r.pick(0.0f, [](float, int) { return 0ull; }, [](uint64_t) { return 0ull; }, nullptr, nullptr);
+      const uint64_t target = max(static_cast<uint64_t>(1), static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(mass))));
+      Cut to{};
+      if (r.template narrow<true>(cut, cut.key, khi, 0, min(target, mass), &to)) cut = to;
+    } else {
+      cut = r.nucleus(cut, p, a.vocab);
+    }
   }
   // ---- the draw
   uint64_t value = 0;
-  const float u0 = a.u[row];
-  const uint64_t mass = r.pick(Key<T>::value(cut.key), kept_w, [&](uint64_t all) {
+  r.sums_kept(cut);
+  const uint64_t mass = r.pick(Key<T>::value(cut.key), [&](float l, int i) { return r.kept(cut, Key<T>::of(l), i) ? r.w(l) : 0ull; },
+                               [&](uint64_t all) {
     const double u = u0 > 0.0f ? static_cast<double>(u0) : 0.0;
     const double x = u * static_cast<double>(all);
     return x >= static_cast<double>(all) ? all - 1 : min(all - 1, static_cast<uint64_t>(x));

@@ -683,14 +683,18 @@ TADM_API tadm_status tadm_pages_copy(const tadm_page_pool* pool, const int32_t* 
  *  - temperature[row] <= 2^-100 or NaN: the first of the order, whatever the
  *    other settings.  temperature NULL: 1; top_k, top_p, min_p NULL: off.
  *  - prob (optional): the token's weight over the kept ids' mass.
- * Weights are whole multiples of 2^-44 of the largest (smaller ones are none), right to about 2^-35, their sums
- * exact: results repeat, do not depend on the other rows, and are those of
- * exact arithmetic unless u or a cut lies that close to a border.  vocab is
- * at most 400,000 (TADM_ERR_UNSUPPORTED above).  Rows may start at any element. */
+ * Weights count in units of 2^-44 of the largest (smaller ones are none), right to about 2^-30 without a bias:
+ * results repeat, do not depend on the other rows, and are those of exact
+ * arithmetic unless u or a cut lies within some 2^-34 of the mass of a border.  vocab is
+ * at most 2^19 (TADM_ERR_UNSUPPORTED above).  Rows may start at any element.
+ * scratch: at least tadm_sample_scratch_size() bytes (none for small
+ * vocabularies), 256-byte aligned; it needs no initialisation, and calls that
+ * overlap on the GPU need one each. */
+TADM_API tadm_status tadm_sample_scratch_size(int rows, int vocab, size_t* bytes);
 TADM_API tadm_status tadm_sample(const void* logits, int64_t ld, int rows, int vocab, int mask_id,
                                  const float* temperature, const int32_t* top_k, const float* top_p,
                                  const float* min_p, const float* u, int32_t* tok, float* prob, int dtype,
-                                 tadm_stream stream);
+                                 void* scratch, size_t scratch_bytes, tadm_stream stream);
 
 /* y[t] = W x[t] + lora_scale[a] B_a (A_a x[t]) for the rows t of each sequence,
  * a = adapter[b] of its sequence (int32 [batch]; outside 0 .. n_adapters - 1:

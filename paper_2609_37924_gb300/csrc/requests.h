@@ -17,8 +17,10 @@ struct SampleCall {
   const float* u;
   int32_t* tok;
   float* prob;                     // null: not wanted
+  void* scratch;
 };
-constexpr int kSampleMaxVocab = 400000;   // fp32 rows in the shared memory of 8 blocks
+constexpr int kSampleMaxVocab = 1 << 19;
+size_t sample_scratch(int rows, int vocab);
 const char* sample_rows(const SampleCall& c, cudaStream_t s);
 
 struct LoraCall {

@@ -16,16 +16,24 @@ int es(int dtype) { return dtype ? 2 : 4; }
 
 extern "C" {
 
+tadm_status tadm_sample_scratch_size(int rows, int vocab, size_t* bytes) {
+  if (rows < 0 || vocab < 1 || !bytes) return TADM_ERR_INVALID_ARG;
+  *bytes = vocab > kSampleMaxVocab ? 0 : sample_scratch(rows, vocab);
+  return TADM_OK;
+}
+
 tadm_status tadm_sample(const void* logits, int64_t ld, int rows, int vocab, int mask_id, const float* temperature,
                         const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* tok,
-                        float* prob, int dtype, tadm_stream stream) {
+                        float* prob, int dtype, void* scratch, size_t scratch_bytes, tadm_stream stream) {
   if (!is_type(dtype) || rows < 0 || vocab < 1 || ld < vocab || mask_id < -1 || mask_id >= vocab) return TADM_ERR_INVALID_ARG;
   if (rows == 0) return TADM_OK;
   if (!logits || !u || !tok || !aligned(logits, es(dtype)) || !aligned(u, 4) || !aligned(tok, 4) || !aligned(temperature, 4) ||
       !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(prob, 4))
     return TADM_ERR_INVALID_ARG;
-  if (vocab > kSampleMaxVocab || rows > (1 << 27)) return TADM_ERR_UNSUPPORTED;   // shared memory; a grid of 8 blocks a row
-  const SampleCall c{logits, ld, rows, vocab, mask_id, dtype, temperature, top_k, top_p, min_p, u, tok, prob};
+  if (vocab > kSampleMaxVocab || rows > (1 << 24)) return TADM_ERR_UNSUPPORTED;   // a row's parts, a grid of up to 64 blocks a row
+  const size_t need = sample_scratch(rows, vocab);
+  if (need > 0 && (!scratch || !aligned(scratch, 256) || scratch_bytes < need)) return TADM_ERR_INVALID_ARG;
+  const SampleCall c{logits, ld, rows, vocab, mask_id, dtype, temperature, top_k, top_p, min_p, u, tok, prob, scratch};
   return sample_rows(c, stream) ? TADM_ERR_CUDA : TADM_OK;
 }
 

@@ -11,27 +11,26 @@
 // Every set is a first part of the order, so it is one cut: a key (the logit's
 // bits as an ordered integer) and, among the ids of that key, a last id.
 //
-// Weights are whole numbers of 2^-44, accurate to about 2^-35 (weight() says
-// how), and all sums are 64-bit integers.  So a sum does not depend on its
-// order, cuts and draws repeat, and they differ from those of exact
-// arithmetic only where a border lies within some 2^-40 of the mass: with
-// fp32 weights a row of 10^5 like tokens draws another one every few thousand
-// rows.
+// A cut or a draw next to a border must not depend on rounding: with weights
+// of fp32 a row of 10^5 like tokens draws another one every few thousand
+// rows.  Weights are right to about 2^-30 without a bias, and their sums are
+// 64-bit integers in units of 2^-44, or pairs of fp32 sums good to 2^-37 a lane
+// (bulk), so that a border has to lie within some 2^-35 of the mass.
 //
-// A cluster of 1 to 8 blocks holds the row in shared memory: the logits leave
-// HBM once, whatever the settings ask for.  Block c has the c-th part of the
-// ids, warp w of it the w-th segment of that part.  What the blocks know
-// together goes through distributed shared memory; every block reads all
-// parts and comes to the same decisions.
-//
-// Whole rows are summed by bulk(): the same weights in pairs of fp32 sums, a
-// third of weight()'s instructions.  The nucleus takes two passes: one sums
-// the row and counts it by value in 512 bins, which places the cut within
-// three of them; one sums what lies above those and lists what lies in them.
-// top-k begins with the lanes' maxima, the k-th largest of which is a lower
-// bound.  Listed elements are narrowed down by histograms over the key until
-// 128 elements or one key are left.  Where a list overflows or a guess was
-// wrong, the same histograms go over the whole row.
+// Rows of up to 4096 ids: one block a row, sample_finish_kernel.  Longer ones:
+//   sample_scan_kernel     per 8192 ids: maximum, mass per 512 ids, histogram of
+//                          the mass by value in 512 bins;
+//   sample_plan_kernel     per row: from those the mass to be kept, and between
+//                          which values the cut lies (three bins); where few ids are
+//                          kept at all, a value below the cut;
+//   sample_collect_kernel  per 8192 ids: the mass above those values per 512
+//                          ids, and a list of the ids in between;
+//   sample_finish_kernel   per row: the cut within the list, by histograms over the
+//                          key until 128 elements or one key are left; the 512
+//                          ids in which the draw falls; the token.
+// Where a list overflows or the guess was wrong, the last one takes the whole
+// row by the same histograms (logits beyond 2^18 T, cuts of thousands of ids
+// under two settings at once).
 #include <cstdint>
 
 #include "common.cuh"
@@ -40,18 +39,42 @@
 namespace tadm {
 namespace {
 
-constexpr int NT = 512, NW = NT / 32, NB = NT, LIST = 128, MAXC = 8;
+constexpr int NT = 512, NW = NT / 32, NB = 512, LIST = 128;
+constexpr int PER = 16;                    // ids of a lane
+constexpr int CHUNK = NT * PER, SEG = 32 * PER;   // ids of a block, of a warp
+constexpr int CAP = 4096;                  // ids on a row's list
+constexpr int SEGS = (kSampleMaxVocab + SEG - 1) / SEG;
 constexpr uint64_t ONE = 1ull << 44;
 
 struct SampleArgs {
   const void* logits;
   int64_t ld;
-  int vocab, mask_id, seg;                 // seg: ids of a warp
+  int rows, vocab, mask_id, chunks;
   const float* temperature;
   const int32_t* top_k;
   const float *top_p, *min_p, *u;
   int32_t* tok;
   float* prob;
+  // scratch
+  struct ChunkInfo* info;                  // [rows][chunks]
+  uint64_t* seg;                           // [rows][chunks * NW] mass of a warp's ids
+  uint32_t* hist;                          // [rows][chunks][NB]
+  struct RowPlan* plan;                    // [rows]
+  uint2* list;                             // [rows][CAP] key, id
+};
+// Maximum of a chunk; its weights count from 2^(mj / 16), its bins from gj down; far: neither fits, the row is taken whole.
+struct ChunkInfo {
+  float max;
+  int mj, gj, far;
+};
+enum Mode : int { kEmpty, kAll, kListed, kWindow, kWhole };
+// kAll: every id is kept, the masses are the scan's.  kListed: what may be kept is on the list.  kWindow: what lies above
+// the list is kept, too; of the mass, `target` is.  kWhole: the last kernel takes the row by itself.
+struct RowPlan {
+  float max, lo, hi;                       // the list: lo <= logit <= hi
+  int mode, mj, listed;
+  int more;                                // ids below lo may be kept, too
+  uint64_t target;
 };
 
 // ------------------------------------------------------------------ keys
@@ -76,7 +99,7 @@ struct Key<bf16> {
   }
 };
 
-// 16 bytes of logits: NaN and the masked id count as -inf, -0 as 0
+// 16 bytes of logits
 template <class T>
 struct Vec;
 template <>
@@ -84,9 +107,6 @@ struct Vec<float> {
   static constexpr int N = 4;
   static __device__ __forceinline__ void get(const uint4& q, float (&v)[4]) {
     v[0] = __uint_as_float(q.x), v[1] = __uint_as_float(q.y), v[2] = __uint_as_float(q.z), v[3] = __uint_as_float(q.w);
-  }
-  static __device__ __forceinline__ uint4 put(const float (&v)[4]) {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
   }
 };
 template <>
@@ -100,75 +120,183 @@ struct Vec<bf16> {
       v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
-  static __device__ __forceinline__ uint4 put(const float (&v)[8]) {   // (the values are bf16)
-    uint32_t w[4];
+};
+
+// The logits of a row: NaN and the masked id count as -inf, -0 as 0.
+template <class T>
+struct Logits {
+  using V = Vec<T>;
+  const T* p;
+  int vocab, mask_id;
+  bool vec;                                // rows on 16 bytes
+  __device__ __forceinline__ Logits(const SampleArgs& a, int row)
+      : p(static_cast<const T*>(a.logits) + row * a.ld), vocab(a.vocab), mask_id(a.mask_id),
+        vec((reinterpret_cast<uintptr_t>(p) & 15) == 0) {}
+  __device__ __forceinline__ float one(int id) const {
+    const float ninf = __int_as_float(0xff800000);
+    return id < vocab && id != mask_id ? fmaxf(to_f32(p[id]) + 0.0f, ninf) : ninf;
+  }
+  // V::N ids from id on, a multiple of V::N
+  __device__ __forceinline__ uint4 load(int id) const {
+    if (vec && id + V::N <= vocab) return __ldg(reinterpret_cast<const uint4*>(p + id));
+    T v[V::N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[2 * i]) >> 16 | __float_as_uint(v[2 * i + 1]);
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    for (int e = 0; e < V::N; ++e) v[e] = id + e < vocab ? p[id + e] : from_f32<T>(__int_as_float(0xff800000));
+    return *reinterpret_cast<const uint4*>(v);
+  }
+  __device__ __forceinline__ void get(const uint4& q, int id, float* v) const {
+    const float ninf = __int_as_float(0xff800000);
+    float x[V::N];
+    V::get(q, x);
+#pragma unroll
+    for (int e = 0; e < V::N; ++e) v[e] = fmaxf(x[e] + 0.0f, ninf);
+    if (static_cast<uint32_t>(mask_id - id) < V::N) {
+#pragma unroll
+      for (int e = 0; e < V::N; ++e)
+        if (id + e == mask_id) v[e] = ninf;
+    }
   }
 };
 
 // ------------------------------------------------------------------ weights
-struct Scale {
-  float max, hi, lo;                       // the row's maximum; log2(e) / T in two terms
-};
-// 2^(j/32) in units of 2^-43, rounded
-__constant__ const uint64_t kPow[32] = {
-    0x80000000000ull, 0x82cd8698ac3ull, 0x85aac367cc5ull, 0x88980e8092eull,
-    0x8b95c1e3ea9ull, 0x8ea4398b45dull, 0x91c3d373ab1ull, 0x94f4efa8fefull,
-    0x9837f0518dcull, 0x9b8d39b9d55ull, 0x9ef5326091aull, 0xa27043030c5ull,
-    0xa5fed6a9b15ull, 0xa9a15ab4ea8ull, 0xad583eea42aull, 0xb123f581d2bull,
-    0xb504f333f9eull, 0xb8fbaf47630ull, 0xbd08a39f581ull, 0xc12c4cca667ull,
-    0xc5672a11550ull, 0xc9b9bd866e3ull, 0xce248c151f8ull, 0xd2a81d91f13ull,
-    0xd744fccad6aull, 0xdbfbb797dafull, 0xe0ccdeec2a9ull, 0xe5b906e77c8ull,
-    0xeac0c6e7dd2ull, 0xefe4b99bdceull, 0xf5257d15248ull, 0xfa83b2db723ull};
+// 2^(j/16) in units of 2^-43, rounded, and in two fp32 terms
+__constant__ const uint64_t kPow[16] = {
+    0x80000000000ull, 0x85aac367cc5ull, 0x8b95c1e3ea9ull, 0x91c3d373ab1ull,
+    0x9837f0518dcull, 0x9ef5326091aull, 0xa5fed6a9b15ull, 0xad583eea42aull,
+    0xb504f333f9eull, 0xbd08a39f581ull, 0xc5672a11550ull, 0xce248c151f8ull,
+    0xd744fccad6aull, 0xe0ccdeec2a9ull, 0xeac0c6e7dd2ull, 0xf5257d15248ull};
+__constant__ const float2 kPow2[16] = {
+    {1.0f, 0.0f}, {1.04427373f, 4.83347016e-08f}, {1.09050775f, -1.30775399e-08f}, {1.13878858f, 5.38622231e-08f},
+    {1.18920708f, 3.79763527e-08f}, {1.24185777f, 4.4968381e-08f}, {1.29683959f, -4.01899953e-08f}, {1.35425556f, -1.01233493e-08f},
+    {1.41421354f, 2.4203235e-08f}, {1.47682619f, -4.50089885e-08f}, {1.54221082f, 8.07090483e-09f}, {1.61049032f, 9.83621717e-09f},
+    {1.68179286f, -2.47553267e-08f}, {1.75625217f, -9.23577037e-09f}, {1.8340081f, -1.1239278e-08f}, {1.91520655f, 9.84532811e-09f}};
+// 2^f - 1 = f (A1 + f (A2 + f (A3 + f A4))) for |f| <= 1/32: ln2^n / n!, eased so that the neglected terms spread (Chebyshev); error
+// 2^-37
+constexpr float A1 = 0.693147182f, A2 = 0.240226507f, A3 = 0.0555057377f, A4 = 0.00961835496f;
+constexpr float kMagic = 12582912.0f;      // 1.5 * 2^23: added to a number, leaves the nearest whole one in the low bits
+constexpr int kMagicBits = 0x4b400000;
+constexpr int kFar = 1 << 22;              // |mj|, |gj| below this
 
-// exp((l - max) / T) * ONE, rounded.  t = (l - max) log2(e) / T in two fp32 terms p + e (the difference and the product are
-// taken with their errors); p = n + j/32 + f with |f| <= 1/64; 2^f - 1 = f ln 2 + ... with the first term in two pieces,
-// which go into 36 fraction bits; times 2^e = 1 + e ln 2, and 2^(j/32) from a table; shifted by n.  Errors: 2^-36 of the
-// fraction's two roundings, 2^-38 of the neglected e^2, half a unit of the last shift.
+// Settings of a row.
+struct Row {
+  float hi, lo;                            // log2(e) / T in two terms
+  int k;
+  float p, mp, t;
+};
+__device__ __forceinline__ Row row_of(const SampleArgs& a, int row, float* s_c) {
+  Row r;
+  r.t = a.temperature ? a.temperature[row] : 1.0f;
+  r.p = a.top_p ? a.top_p[row] : 1.0f;
+  r.mp = a.min_p ? a.min_p[row] : 0.0f;
+  r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
+  if (r.k < 0 || r.k >= a.vocab) r.k = 0;
+  if (threadIdx.x == 0) {                  // (double precision is slow here: one thread, for all)
+    const double c = 1.4426950408889634074 / static_cast<double>(r.t);
+    s_c[0] = static_cast<float>(c);
+    s_c[1] = static_cast<float>(c - static_cast<double>(s_c[0]));
+  }
+  return r;
+}
+// Ids of less than 2^-depth of the maximum are of no account: too light for a nucleus (those that weigh less than
+// (1 - p) / vocab together weigh less than 1 - p of the mass), or for any draw.
+__device__ __forceinline__ float depth_of(const SampleArgs& a, const Row& r) {
+  return r.k == 0 && r.mp <= 0.0f && r.p < 1.0f ? fminf(44.0f, __log2f(static_cast<float>(a.vocab) / (1.0f - r.p)) + 0.5f) : 44.0f;
+}
+
+// What weights count from: 2^(mj / 16), next to the weight of a maximum.  t = c x - mj / 16 without the rounding of a
+// difference: j = 16 t to the nearest whole number, f = c x - (mj + j) / 16 by one fma (whose product is exact), plus c's
+// second term.  shift: the maximum where it is far from zero (then mj = 0, and logits that weigh anything are near it).
+struct Scale {
+  float hi, lo, hi16, k_c, mh, shift;
+  __device__ __forceinline__ Scale(float c_hi, float c_lo, int mj, float from)
+      : hi(c_hi), lo(c_lo), hi16(16.0f * c_hi), k_c(kMagic - static_cast<float>(mj)), mh(static_cast<float>(mj) * 0.0625f), shift(from) {}
+};
+__device__ __forceinline__ int mj_of(float c_hi, float c_lo, float max) {
+  const float m = 16.0f * max * c_hi;
+  return fabsf(m) < static_cast<float>(kFar) - 2.0f ? __float2int_rn(m) : kFar;
+}
+
+// The weight of a logit in units of 2^-44, rounded: 2^f - 1 (2^-30 of rounding) in 36 fraction bits, times 2^(j/16) from
+// the table, shifted.
 __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, float l) {
-  if (l == s.max) return ONE;
-  const float d = l - s.max, bb = d - l;
-  const float dl = (l - (d - bb)) - (s.max + bb);
-  const float p = d * s.hi;
-  if (!(p > -46.0f)) return 0;
-  float e = fmaf(d, s.hi, -p);
-  e = fmaf(d, s.lo, e);
-  e = fmaf(dl, s.hi, e);
-  const float q = fmaf(p, 32.0f, 12582912.0f);                // 1.5 * 2^23: the nearest integer in the low bits
-  const int j = __float_as_int(q) - 0x4b400000;
-  const float f = fmaf(q - 12582912.0f, -0.03125f, p);
-  constexpr float L = 0.693147180559945f, LL = static_cast<float>(0.6931471805599453094 - static_cast<double>(0.693147180559945f));
-  const float r = f * L;
-  float rest = fmaf(f, L, -r);
-  rest = fmaf(f, LL, rest);
-  rest = fmaf(e * L, 1.0f + r, rest);
-  const float c = fmaf(f, fmaf(f, 0.00961812911f, 0.0555041087f), 0.240226507f);   // ln2^4/24, ln2^3/6, ln2^2/2
-  rest = fmaf(f * f, c, rest);
-  const int64_t frac = static_cast<int64_t>(__float2int_rn(r * 68719476736.0f)) + __float2int_rn(rest * 68719476736.0f);
-  const uint64_t t = pow[j & 31];
-  // t (1 + frac 2^-36) with the low 12 bits of t left out of the second product
-  const uint64_t w = t + static_cast<uint64_t>((static_cast<int64_t>(t >> 12) * frac) >> 24);
-  const int down = -(j >> 5) - 1;                             // w counts 2^-44 of 2^(n + 1)
+  const float x = l - s.shift;
+  if (!(fmaf(x, s.hi, -s.mh) > -46.0f)) return 0;
+  const float q = fmaf(x, s.hi16, s.k_c), jf = q - kMagic;
+  const int j = __float_as_int(q) - kMagicBits;
+  const float g = fmaf(x, s.lo, fmaf(x, s.hi, fmaf(jf, -0.0625f, -s.mh)));
+  const float r = g * fmaf(g, fmaf(g, fmaf(g, A4, A3), A2), A1);
+  const uint64_t t = pow[j & 15];
+  const uint64_t w = t + static_cast<uint64_t>((static_cast<int64_t>(t >> 12) * __float2int_rn(r * 68719476736.0f)) >> 24);
+  const int down = -(j >> 4) - 1;          // w counts 2^-44 of 2^(n + 1)
   return down <= 0 ? w << -down : (w + (1ull << (down - 1))) >> down;
 }
 
-// 2^f - 1 = f (A1 + f (A2 + f (A3 + f A4))) for |f| <= 1/32: ln2^n / n!, the last two eased to spread the error of the next
-// term (Chebyshev)
-constexpr float A1 = 0.693147182f, A2 = 0.240226507f, A3 = 0.0555057377f, A4 = 0.00961835496f;
+__device__ __forceinline__ uint64_t pair(float x) { return f2_pack(x, x); }
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
-// ------------------------------------------------------------------ the cluster's shared memory
-__device__ __forceinline__ uint32_t remote_u32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
+// Sum of the weights of the values above `cut` (exclusive) that a warp's lanes hold, in units of 2^-44, in every lane.  The
+// same arithmetic as weight()'s, two values at a time, with the table in two fp32 terms.  A weight is split at 2^-17:
+// multiples of that add without rounding, the rest carries errors of about 2^-37 a lane.
+// BINS: also a histogram by value, bins counted down from gj / per; a value adds its weight over that of its bin's
+// middle, linear in its place within the bin, in 2^-14.
+template <bool BINS>
+__device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, const float2* pow, float max, float cut, float per, int gj,
+                                         uint32_t* hist) {
+  const float none = fmaxf(max - 60.0f / s.hi, -3.0e38f);     // stands for values that are not summed: 2^-60
+  cut = fmaxf(cut, none);
+  const uint64_t k_hi16 = pair(s.hi16), k_c = pair(s.k_c), k_back = pair(-kMagic);
+  const uint64_t k_n16 = pair(-0.0625f), k_nmh = pair(-s.mh), k_hi = pair(s.hi), k_lo = pair(s.lo), k_minus = pair(-1.0f);
+  const uint64_t k_up = pair(96.0f), k_down = pair(-96.0f);
+  const uint64_t a1 = pair(A1), a2 = pair(A2), a3 = pair(A3), a4 = pair(A4);
+  const uint64_t b_per = pair(-per), b_c = pair(kMagic + static_cast<float>(gj)), b_slope = pair(-16384.0f * 0.693147181f * s.hi / per);
+  const uint64_t b_one = pair(kMagic + 16384.0f);
+  uint64_t big = 0, small = 0;
+#pragma unroll
+  for (int e = 0; e < PER; e += 2) {
+    const float v0 = v[e], v1 = v[e + 1];
+    const bool in0 = v0 > cut, in1 = v1 > cut;
+    const uint64_t x = f2_pack(in0 ? v0 : none, in1 ? v1 : none);
+    if constexpr (BINS) {
+      const uint64_t q = f2_fma(x, b_per, b_c), d = f2_fma(x, b_per, f2_fma(q, k_minus, b_c));   // d: from the bin's middle, in bins
+      float q0, q1, m0, m1;
+      f2_unpack(q, q0, q1);
+      f2_unpack(f2_fma(d, b_slope, b_one), m0, m1);
+      const uint32_t i0 = __float_as_uint(q0) - kMagicBits, i1 = __float_as_uint(q1) - kMagicBits;
+      if (in0 && i0 < NB) atomicAdd(&hist[i0], __float_as_uint(m0) - kMagicBits);
+      if (in1 && i1 < NB) atomicAdd(&hist[i1], __float_as_uint(m1) - kMagicBits);
+    }
+    const uint64_t q = f2_fma(x, k_hi16, k_c), j = f2_add(q, k_back);
+    const uint64_t g = f2_fma(x, k_lo, f2_fma(x, k_hi, f2_fma(j, k_n16, k_nmh)));
+    const uint64_t r = f2_mul(g, f2_fma(g, f2_fma(g, f2_fma(g, a4, a3), a2), a1));
+    float q0, q1;
+    f2_unpack(q, q0, q1);
+    const uint32_t b0 = __float_as_uint(q0), b1 = __float_as_uint(q1);
+    const float2 t0 = pow[b0 & 15], t1 = pow[b1 & 15];
+    // 2^n, n = floor(j / 16): the magic number's bits drop out of the shifted word
+    constexpr uint32_t BIAS = (127u << 23) - (static_cast<uint32_t>(kMagicBits) >> 4 << 23);
+    const uint64_t p2 = f2_pack(__uint_as_float((b0 >> 4 << 23) + BIAS), __uint_as_float((b1 >> 4 << 23) + BIAS));
+    const uint64_t a = f2_mul(f2_pack(t0.x, t1.x), p2), al = f2_mul(f2_pack(t0.y, t1.y), p2);
+    const uint64_t t = f2_fma(a, r, al), h = f2_add(a, t), l = f2_add(f2_fma(h, k_minus, a), t);
+    const uint64_t up = f2_add(f2_add(h, k_up), k_down);
+    big = f2_add(big, up);
+    small = f2_add(small, f2_add(f2_fma(up, k_minus, h), l));
+  }
+  float h0, h1, l0, l1;
+  f2_unpack(big, h0, h1);
+  f2_unpack(small, l0, l1);
+  const int64_t whole = static_cast<int64_t>(__float2int_rn((h0 + h1) * 131072.0f)) << 27;
+  uint64_t sum = static_cast<uint64_t>(whole + __float2ll_rn((l0 + l1) * 17592186044416.0f));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
 }
-__device__ __forceinline__ uint64_t remote_u64(uint32_t addr) {
-  uint64_t v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
-  return v;
-}
+// the largest logit below `v`
+__device__ __forceinline__ float below(float v) { return v == 0.0f ? -1.4e-45f : Key<float>::value(Key<float>::of(v) - 1); }
+
 __device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -200,364 +328,343 @@ __device__ __forceinline__ uint32_t first_key(uint32_t lo, uint32_t hi, F&& pred
   return lo;
 }
 
-constexpr int CAP = 2048;                  // elements that a block lists
-struct Shared {
-  uint64_t pow[32];
-  uint64_t mass[2][NB];                    // histograms, two in turn
-  uint32_t count[2][NB];
-  uint64_t sums[2][NW];                    // per warp
-  uint64_t above[NW];                      // per warp: of what lies above the list
-  uint64_t scan[NW];
-  float scan_f[NW];
-  float2 top;                              // largest and smallest of the lanes' maxima in the block
-  float2 wtop[NW];
-  uint32_t list_n, few_n;
-  uint16_t list[CAP];                      // places in the block's part
-  uint32_t few_key[LIST], few_id[LIST];
-  uint64_t all_w[LIST];
-  uint32_t all_key[LIST], all_id[LIST];
-  uint32_t found_id[2];                    // what pick() found
-  uint64_t found_w[2];
-  uint64_t part[NW];
-  float2 pow16[16];                        // bulk(): 2^(j/16) 2^-(M - Mh) in two fp32 terms
-  float c_hi, c_lo, low;                   // log2(e) / T; the row's least logit that min-p keeps, less the maximum
-  double low64;
-  float mh;
-  // what one thread decides for its block
-  uint32_t d_bin, d_count, d_key, d_id;
-  uint64_t d_above;
-};
-static_assert((sizeof(Shared) + 15) / 16 * 16 + (kSampleMaxVocab + MAXC * NW * 128 - 1) / (MAXC * NW * 128) * 128 * NW * 4 <= 232448, "shared memory");
+// Sum over the block's threads up to this one, and over all.  Block-collective; `room` may be used again after a __syncthreads.
+__device__ __forceinline__ uint64_t scan_block(uint64_t own, uint64_t* room, uint64_t* all = nullptr) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint64_t incl = warp_scan_u64(own);
+  if (lane == 31) room[warp] = incl;
+  __syncthreads();
+  const uint64_t x = warp_scan_u64(lane < NW ? room[lane] : 0);
+  if (all) *all = __shfl_sync(0xffffffffu, x, 31);
+  const uint64_t before = __shfl_sync(0xffffffffu, x, warp > 0 ? warp - 1 : 0);
+  return warp > 0 ? incl + before : incl;
+}
 
+// ------------------------------------------------------------------ the passes over the logits
+// This lane's ids: PER of its warp's 512, V::N next to each other, 32 V::N from piece to piece.
+template <class T>
+__device__ __forceinline__ void load_chunk(const Logits<T>& l, int base, float (&v)[PER]) {
+  constexpr int N = Vec<T>::N;
+  const int lane = threadIdx.x & 31;
+  uint4 q[PER / N];
+#pragma unroll
+  for (int i = 0; i < PER / N; ++i) q[i] = l.load(base + (i * 32 + lane) * N);
+#pragma unroll
+  for (int i = 0; i < PER / N; ++i) l.get(q[i], base + (i * 32 + lane) * N, &v[i * N]);
+}
+__device__ __forceinline__ bool wants_mass(const Row& r) { return r.k == 0; }          // draws or cuts by the mass of everything
+__device__ __forceinline__ bool wants_bins(const Row& r) { return r.k > 1 || (r.k == 0 && (r.p < 1.0f || r.mp > 0.0f)); }
+
+template <class T>
+__global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) {
+  __shared__ uint32_t s_hist[NB];
+  __shared__ float2 s_pow[16];
+  __shared__ float s_max[NW], s_c[2];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
+  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow2[threadIdx.x];
+  s_hist[threadIdx.x] = 0;
+  pdl_enter();
+  const Logits<T> l(a, row);
+  float v[PER];
+  load_chunk(l, chunk * CHUNK + warp * SEG, v);
+  Row r = row_of(a, row, s_c);
+  float top = v[0];
+#pragma unroll
+  for (int e = 1; e < PER; ++e) top = fmaxf(top, v[e]);
+  top = warp_max(top);
+  if (lane == 0) s_max[warp] = top;
+  __syncthreads();
+  top = warp_max(s_max[lane & (NW - 1)]);
+  r.hi = s_c[0], r.lo = s_c[1];
+  const float per = r.hi * ((NB - 2) / depth_of(a, r));
+  const float ninf = __int_as_float(0xff800000);
+  ChunkInfo info{top, 0, 0, 0};
+  if (top > ninf) {
+    const float g = top * per;
+    info.mj = mj_of(r.hi, r.lo, top);
+    info.gj = fabsf(g) < static_cast<float>(kFar) ? __float2int_rn(g) : kFar;
+    info.far = info.mj == kFar || info.gj == kFar || !(r.hi > 1e-30f);
+    uint64_t sum = 0;
+    if (!info.far && r.k != 1) {
+      const Scale s(r.hi, r.lo, info.mj, 0.0f);
+      sum = wants_bins(r) ? bulk<true>(v, s, s_pow, top, ninf, per, info.gj, s_hist) : bulk<false>(v, s, s_pow, top, ninf, 0.0f, 0, nullptr);
+    }
+    if (lane == 0) a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = sum;
+  } else if (lane == 0) {
+    a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = 0;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) a.info[static_cast<int64_t>(row) * a.chunks + chunk] = info;
+  if (wants_bins(r)) a.hist[(static_cast<int64_t>(row) * a.chunks + chunk) * NB + threadIdx.x] = s_hist[threadIdx.x];
+}
+
+// a number of units of 2^(from / 16) in units of 2^(to / 16), from <= to
+__device__ __forceinline__ uint64_t rescale(uint64_t sum, int from, int to) {
+  const int d = from - to, n = d >> 4;                        // 2^n 2^(j/16), n <= 0
+  const uint64_t t = kPow[d & 15];                            // 2^-43
+  // sum * t: 128 bits, down by 43 - n
+  const uint64_t hi = __umul64hi(sum, t), lo = sum * t;
+  const int down = 43 - n;
+  if (down >= 128) return 0;
+  if (down >= 64) return hi >> (down - 64);
+  return (hi << (64 - down)) | (lo >> down);
+}
+
+template <class T>
+__global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
+  __shared__ uint64_t s_room[NW];
+  __shared__ float s_max[NW], s_c[2];
+  __shared__ int s_bin, s_low;
+  __shared__ uint64_t s_front;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
+  if (threadIdx.x == 0) s_bin = NB, s_low = NB;
+  pdl_enter();
+  Row r = row_of(a, row, s_c);
+  const ChunkInfo* info = a.info + static_cast<int64_t>(row) * a.chunks;
+  uint64_t* seg = a.seg + static_cast<int64_t>(row) * a.chunks * NW;
+  const float ninf = __int_as_float(0xff800000);
+  const ChunkInfo mine = threadIdx.x < a.chunks ? info[threadIdx.x] : ChunkInfo{ninf, 0, 0, 0};   // (a row has fewer chunks than threads)
+  float top = warp_max(mine.max);
+  if (lane == 0) s_max[warp] = top;
+  __syncthreads();
+  top = warp_max(s_max[lane & (NW - 1)]);
+  r.hi = s_c[0], r.lo = s_c[1];
+  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0};
+  const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
+  if (top > ninf && (r.k == 1 || top == -ninf)) {
+    plan.mode = kListed;                                      // the ids of the maximum
+    plan.mj = far ? kFar : mj_of(r.hi, r.lo, top);
+  } else if (top > ninf && far) {
+    plan.mode = kWhole;
+    plan.mj = kFar;
+  } else if (top > ninf) {
+    const int mj = mj_of(r.hi, r.lo, top);
+    const float per = r.hi * ((NB - 2) / depth_of(a, r));
+    const int gj = __float2int_rn(top * per);
+    plan.mj = mj;
+    // every mass in the units of the row's maximum
+    uint64_t mass = 0;
+    if (wants_mass(r)) {
+      uint64_t own = 0;
+      for (int i = threadIdx.x; i < a.chunks * NW; i += NT) {
+        const ChunkInfo c = info[i / NW];
+        const uint64_t x = c.max > ninf && !c.far ? rescale(seg[i], c.mj, mj) : 0;
+        seg[i] = x;
+        own += x;
+      }
+      scan_block(own, s_room, &mass);
+      __syncthreads();
+    }
+    plan.mode = kAll;
+    plan.lo = ninf, plan.hi = -ninf;
+    if (wants_bins(r)) {
+      // a bin per thread: its number of ids, about, and its mass in 2^-32
+      uint64_t n = 0;
+      for (int c = 0; c < a.chunks; ++c) {
+        const ChunkInfo x = info[c];
+        const int bin = static_cast<int>(threadIdx.x) - (gj - x.gj);
+        if (x.max > ninf && !x.far && bin >= 0 && bin < NB) n += a.hist[(static_cast<int64_t>(row) * a.chunks + c) * NB + bin];
+      }
+      auto edge = [&](float bin) { return (static_cast<float>(gj) - bin) / per; };
+      const uint64_t count = (n + 8192) >> 14, in_front = scan_block(count, s_room);
+      __syncthreads();
+      int b = NB;
+      if (r.k > 1) {
+        if (in_front >= static_cast<uint64_t>(r.k) && in_front - count < static_cast<uint64_t>(r.k)) s_bin = threadIdx.x;
+      } else if (r.p < 1.0f && r.mp <= 0.0f) {
+        plan.target = min(max(static_cast<uint64_t>(ceil(static_cast<double>(r.p) * static_cast<double>(mass))), static_cast<uint64_t>(1)), mass);
+        const float mid = ex2_approx(fmaf(edge(static_cast<float>(threadIdx.x)), r.hi, -0.0625f * static_cast<float>(mj))) * 262144.0f;
+        const uint64_t guess = static_cast<uint64_t>(static_cast<float>(n) * mid), incl = scan_block(guess, s_room);
+        if (incl >= plan.target >> 12 && incl - guess < plan.target >> 12) s_bin = threadIdx.x;
+      }
+      float lo = ninf;
+      if (r.mp > 0.0f) {                                      // the least logit that min-p keeps, rounded up
+        const double x = r.mp >= 1.0f ? 0.0 : static_cast<double>(r.t) * log(static_cast<double>(r.mp));
+        lo = fminf(__double2float_ru(static_cast<double>(top) + x), top) + 0.0f;
+      }
+      __syncthreads();
+      b = s_bin;
+      plan.mode = kListed;
+      if (b < NB - 2) {
+        plan.more = edge(b + 1.5f) > lo;
+        lo = fmaxf(lo, edge(b + 1.5f));
+        if (r.k == 0) plan.hi = edge(b - 1.5f);
+      } else if (r.k == 0 && r.mp <= 0.0f) {
+        plan.mode = kWhole;
+      } else {
+        lo = fmaxf(lo, edge(NB - 0.5f));                      // (k: nothing below counts; min-p: or is kept)
+      }
+      // ids from lo on: on the list, all of them, if they are few
+      const int low = min(NB - 1, max(0, static_cast<int>(static_cast<float>(gj) - lo * per) + 1));
+      if (threadIdx.x == low) s_front = in_front;
+      __syncthreads();
+      if (s_front < CAP * 3 / 4) {
+        plan.hi = -ninf;
+      } else if (plan.mode == kListed && r.k == 0) {
+        if (r.mp <= 0.0f) {
+          plan.mode = kWindow;
+        } else if (r.p >= 1.0f && lo * r.hi > (top * r.hi - 44.0f)) {
+          plan.mode = kWindow;                                // min-p alone: everything from lo on lies above an empty list
+          plan.hi = below(lo);
+          lo = -ninf;
+        } else {
+          plan.mode = kWhole;
+        }
+      } else {
+        plan.mode = kWhole;
+      }
+      plan.lo = lo;
+    }
+  }
+  if (threadIdx.x == 0) a.plan[row] = plan;
+}
+
+template <class T>
+__global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs a) {
+  __shared__ float2 s_pow[16];
+  __shared__ float s_c[2];
+  __shared__ int s_n, s_at;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
+  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow2[threadIdx.x];
+  if (threadIdx.x == 0) s_n = 0;
+  pdl_enter();
+  const RowPlan plan = a.plan[row];
+  if (plan.mode != kListed && plan.mode != kWindow) return;
+  uint64_t* seg = a.seg + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
+  const bool above = plan.mode == kWindow;
+  if (a.info[static_cast<int64_t>(row) * a.chunks + chunk].max < (above ? fminf(plan.lo, plan.hi) : plan.lo)) {
+    if (above && lane == 0) *seg = 0;
+    return;
+  }
+  const Logits<T> l(a, row);
+  const int base = chunk * CHUNK + warp * SEG;
+  float v[PER];
+  load_chunk(l, base, v);
+  Row r = row_of(a, row, s_c);
+  uint32_t in = 0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) in |= v[e] >= plan.lo && v[e] <= plan.hi ? 1u << e : 0u;
+  __syncthreads();
+  const int mine = __popc(in);
+  int at = 0;
+  if (__any_sync(0xffffffffu, mine > 0)) {
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += x;
+    }
+    int first = 0;
+    if (lane == 31) first = atomicAdd(&s_n, incl);
+    at = __shfl_sync(0xffffffffu, first, 31) + incl - mine;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0 && s_n > 0) s_at = atomicAdd(&a.plan[row].listed, s_n);
+  __syncthreads();
+  if (mine > 0) {
+    uint2* list = a.list + static_cast<int64_t>(row) * CAP;
+    at += s_at;
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      if (in >> e & 1) {
+        if (at < CAP) list[at] = make_uint2(Key<T>::of(v[e]), base + ((e / N) * 32 + lane) * N + e % N);
+        ++at;
+      }
+  }
+  if (above) {
+    const Scale s(s_c[0], s_c[1], plan.mj, 0.0f);
+    const uint64_t sum = bulk<false>(v, s, s_pow, plan.max, plan.hi, 0.0f, 0, nullptr);
+    if (lane == 0) *seg = sum;
+  }
+}
+
+// ------------------------------------------------------------------ the cut and the draw
 struct Cut {
   uint32_t key;
   int id;                                  // ids of that key up to this one are kept
 };
 constexpr int ALL = 0x7fffffff;
-constexpr float kFlat = 1e-30f;            // log2(e) / T above which a finite logit can stand for one that weighs nothing (bulk)
 
-__device__ __forceinline__ uint64_t pair(float x) { return f2_pack(x, x); }
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
+struct Finish {
+  uint64_t pow[16];
+  uint64_t mass[NB], seg[(SEGS + NT - 1) / NT * NT], room[NW];
+  uint64_t all_w[LIST];
+  uint32_t count[NB];
+  uint32_t key[CAP], id[CAP];
+  uint32_t few_key[LIST], few_id[LIST];
+  float max[NW], c[2];
+  int n, few;
+  // what one thread decides
+  uint64_t d_above, d_left, d_w, d_best;
+  uint32_t d_bin, d_count, d_key, d_id;
+};
 
-template <class T, int CS>
-struct Row {
-  using V = Vec<T>;
-  Shared& sh;
-  const uint4* data;                       // this block's part
-  int first, seg, rank;                    // id of the part's first element
+template <class T>
+struct Finisher {
+  Finish& sh;
+  Logits<T> l;
   Scale s;
-  int turn;                                // of the arrays that pick() uses in turn: a sync lies between two uses of one
-  bool listed;                             // each() goes over the list
+  float max;
+  bool whole;                              // the row itself, not its list
 
-  __device__ __forceinline__ uint64_t w(float l) const { return weight(s, sh.pow, l); }
+  __device__ __forceinline__ uint64_t w(float v) const {
+    return max == __int_as_float(0x7f800000) ? (v == max ? ONE : 0) : weight(s, sh.pow, v);
+  }
   __device__ __forceinline__ static bool kept(const Cut& c, uint32_t key, int id) { return key > c.key || (key == c.key && id <= c.id); }
-  __device__ __forceinline__ void sync() const {
-    if constexpr (CS > 1) cluster_sync();
-    else __syncthreads();
-  }
-  __device__ __forceinline__ float at(int i) const { return to_f32(reinterpret_cast<const T*>(data)[i]); }
-  // f(logit, id) of this warp's elements (listed: of this thread's listed ones) whose logit is at least `least`
+  // f(key, id) of this thread's candidates
   template <class F>
-  __device__ __forceinline__ void each(float least, F&& f) const {
-    if (listed) {
-      const int n = sh.list_n;
-      for (int i = threadIdx.x; i < n; i += NT) {
-        const int p = sh.list[i];
-        const float v = at(p);
-        if (v >= least) f(v, first + p);
-      }
+  __device__ __forceinline__ void each(F&& f) const {
+    if (!whole) {
+      for (int i = threadIdx.x; i < sh.n; i += NT) f(sh.key[i], static_cast<int>(sh.id[i]));
       return;
     }
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint4* p = data + warp * (seg / V::N);
-    for (int i = lane; i < seg / V::N; i += 32) {
-      float v[V::N];
-      V::get(p[i], v);
+    constexpr int N = Vec<T>::N;
+    for (int id = threadIdx.x * N; id < l.vocab; id += NT * N) {
+      float v[N];
+      l.get(l.load(id), id, v);
 #pragma unroll
-      for (int e = 0; e < V::N; ++e)
-        if (v[e] >= least) f(v[e], first + warp * seg + i * V::N + e);
+      for (int e = 0; e < N; ++e)
+        if (v[e] > __int_as_float(0xff800000)) f(Key<T>::of(v[e]), id + e);
     }
   }
-
-  // Sum of the weights of this warp's elements above `cut` (a logit, exclusive), in units of ONE^-1, in lane 0.  With
-  // BINS also a histogram by value, in bins of width 1 / per below the maximum (none past the last bin): an element adds its
-  // weight over that of its bin's middle, linear in its place within the bin, in 2^-14.
-  //
-  // t = c x - M (c = log2(e) / T, M = c max; x a logit, less the maximum where c max is large) without the rounding of a
-  // difference: j = 16 t to the nearest whole number, f = c x - Mh - j / 16 by one fma, Mh the multiple of 1/16 next to M,
-  // plus c's second term; 2^f - 1 by a polynomial of degree 4 (error 2^-36 for |f| <= 1/32, coefficients below); times the
-  // table's 2^(j/16) 2^(Mh - M) in two terms.  The sum is split at 2^-17: multiples of that add without rounding (at most
-  // 104 of them a lane), the rest carries errors of about 2^-37 a lane.
-  template <bool BINS>
-  __device__ uint64_t bulk(float cut, float per, uint32_t* hist) const {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool far = fabsf(s.max * s.hi) >= 92.0f;            // then logits that weigh anything are near the maximum
-    const float shift = far ? s.max : 0.0f, mh = sh.mh;
-    const float none = fmaxf(s.max - shift - 60.0f / s.hi, -3.0e38f);   // stands for elements that are not summed: 2^-60
-    const uint64_t k_shift = pair(-shift), k_hi16 = pair(16.0f * s.hi), k_c = pair(12582912.0f - 16.0f * mh), k_back = pair(-12582912.0f);
-    const uint64_t k_n16 = pair(-0.0625f), k_nmh = pair(-mh), k_hi = pair(s.hi), k_lo = pair(s.lo), k_minus = pair(-1.0f);
-    const uint64_t k_up = pair(96.0f), k_down = pair(-96.0f);
-    const uint64_t a1 = pair(A1), a2 = pair(A2), a3 = pair(A3), a4 = pair(A4);
-    const uint64_t b_per = pair(-per), b_c = pair(fmaf(s.max, per, 12582912.0f)), b_slope = pair(-16384.0f * 0.693147181f * s.hi / per);
-    const uint64_t b_one = pair(12582912.0f + 16384.0f);
-    uint64_t big = 0, small = 0;
-    cut = fmaxf(cut, fminf(s.max - 60.0f / s.hi, below(s.max)));
-    auto two = [&](float v0, float v1) {
-      const bool in0 = v0 > cut, in1 = v1 > cut;
-      if constexpr (BINS) {
-        const uint64_t v = f2_pack(v0, v1), q = f2_fma(v, b_per, b_c);
-        const uint64_t d = f2_fma(v, b_per, f2_fma(q, k_minus, b_c));     // from the bin's middle, in bins
-        float q0, q1, m0, m1;
-        f2_unpack(q, q0, q1);
-        f2_unpack(f2_fma(d, b_slope, b_one), m0, m1);
-        const uint32_t i0 = __float_as_uint(q0) - 0x4b400000u, i1 = __float_as_uint(q1) - 0x4b400000u;
-        if (in0 && i0 < NB - 1) atomicAdd(&hist[i0], __float_as_uint(m0) - 0x4b400000u);
-        if (in1 && i1 < NB - 1) atomicAdd(&hist[i1], __float_as_uint(m1) - 0x4b400000u);
-      }
-      float x0, x1;
-      f2_unpack(f2_add(f2_pack(v0, v1), k_shift), x0, x1);
-      const uint64_t x = f2_pack(in0 ? x0 : none, in1 ? x1 : none);
-      const uint64_t q = f2_fma(x, k_hi16, k_c), j = f2_add(q, k_back);
-      const uint64_t g = f2_fma(x, k_lo, f2_fma(x, k_hi, f2_fma(j, k_n16, k_nmh)));
-      const uint64_t r = f2_mul(g, f2_fma(g, f2_fma(g, f2_fma(g, a4, a3), a2), a1));
-      float q0, q1;
-      f2_unpack(q, q0, q1);
-      const uint32_t b0 = __float_as_uint(q0), b1 = __float_as_uint(q1);
-      const float2 t0 = sh.pow16[b0 & 15], t1 = sh.pow16[b1 & 15];
-      // 2^n, n = floor(j / 16): the magic number's bits drop out of the shifted word
-      constexpr uint32_t BIAS = (127u << 23) - (0x4b400000u >> 4 << 23);
-      const uint64_t p2 = f2_pack(__uint_as_float((b0 >> 4 << 23) + BIAS), __uint_as_float((b1 >> 4 << 23) + BIAS));
-      const uint64_t a = f2_mul(f2_pack(t0.x, t1.x), p2), al = f2_mul(f2_pack(t0.y, t1.y), p2);
-      const uint64_t t = f2_fma(a, r, al), h = f2_add(a, t), l = f2_add(f2_fma(h, k_minus, a), t);
-      const uint64_t up = f2_add(f2_add(h, k_up), k_down);
-      big = f2_add(big, up);
-      small = f2_add(small, f2_add(f2_fma(up, k_minus, h), l));
-    };
-    const uint4* p = data + warp * (seg / V::N);
-#pragma unroll 2
-    for (int i = lane; i < seg / V::N; i += 32) {
-      float v[V::N];
-      V::get(p[i], v);
-#pragma unroll
-      for (int e = 0; e < V::N; e += 2) two(v[e], v[e + 1]);
-    }
-    float h0, h1, l0, l1;
-    f2_unpack(big, h0, h1);
-    f2_unpack(small, l0, l1);
-    const int64_t whole = static_cast<int64_t>(__float2int_rn(h0 * 131072.0f)) + __float2int_rn(h1 * 131072.0f);
-    return warp_sum_u64(static_cast<uint64_t>((whole << 27) + __float2ll_rn((l0 + l1) * 17592186044416.0f)));
-  }
-  // the largest logit below `v`
-  __device__ __forceinline__ static float below(float v) {
-    return v == 0.0f ? -1.4e-45f : Key<float>::value(Key<float>::of(v) - 1);
-  }
-  // Per warp into sums[turn]: the weights of what `cut` keeps.
-  __device__ void sums_kept(const Cut& cut) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (listed) {                                             // all of it is on the list
-      if (threadIdx.x < NW) sh.sums[turn][threadIdx.x] = sh.above[threadIdx.x];
-      __syncthreads();
-      each(Key<T>::value(cut.key), [&](float l, int id) {
-        if (kept(cut, Key<T>::of(l), id))
-          atomicAdd(reinterpret_cast<unsigned long long*>(&sh.sums[turn][(id - first) / seg]), static_cast<unsigned long long>(w(l)));
-      });
-      return;
-    }
-    const float v = Key<T>::value(cut.key);
-    uint64_t mine = s.hi > kFlat ? bulk<false>(cut.id == ALL ? below(v) : v, 0.0f, nullptr) : 0;
-    if (cut.id != ALL) {
-      uint64_t ties = 0;
-      each(v, [&](float l, int id) { ties += l == v && id <= cut.id ? 1 : 0; });
-      mine += warp_sum_u64(ties) * w(v);
-    }
-    if (__shfl_sync(0xffffffffu, mine, 0) < 2ull * seg) {     // nearly nothing: exactly what weight() gives, so that it can be drawn from
-      mine = 0;
-      each(v, [&](float l, int id) { mine += kept(cut, Key<T>::of(l), id) ? w(l) : 0; });
-      mine = warp_sum_u64(mine);
-    }
-    if (lane == 0) sh.sums[turn][warp] = mine;
-  }
-
-  // From the warps' sums[turn]: their sum over the cluster; with `id`, also the first element in the order of ids with which
-  // the sum of f exceeds target(whole sum), and its f.  (The warps' sums may differ from f's in the last bits.)
-  template <class F, class G>
-  __device__ uint64_t pick(float least, F&& f, G&& target, int* id, uint64_t* value) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    sync();
-    // every warp: lane l has the sums of CS * NW / 32 consecutive warps
-    constexpr int PER = CS * NW >= 32 ? CS * NW / 32 : 1, LANES = CS * NW / PER;
-    uint64_t part[PER], own = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int at = lane * PER + i;
-      part[i] = lane < LANES ? remote_u64(cluster_addr(&sh.sums[turn][at % NW], at / NW)) : 0;
-      own += part[i];
-    }
-    const uint64_t incl = warp_scan_u64(own), total = __shfl_sync(0xffffffffu, incl, 31);
-    if (!id) {
-      turn ^= 1;
-      return total;
-    }
-    const uint64_t t = target(total);
-    const unsigned past = __ballot_sync(0xffffffffu, incl > t);
-    const int src = past ? __ffs(past) - 1 : 31;
-    uint64_t left = t - (incl - own);
-    int at = lane * PER;
-#pragma unroll
-    for (int i = 0; i + 1 < PER; ++i)
-      if (left >= part[i] && at == lane * PER + i) {
-        left -= part[i];
-        ++at;
-      }
-    left = __shfl_sync(0xffffffffu, left, src);
-    at = __shfl_sync(0xffffffffu, at, src);
-    // the block that has it: its warps take the chunks of that segment
-    if (at / NW == rank) {
-      const int chunks = seg / (32 * V::N), per = (chunks + NW - 1) / NW, c0 = warp * per, c1 = min(chunks, c0 + per);
-      const uint4* p = data + (at % NW) * (seg / V::N);
-      const int base = first + (at % NW) * seg;
-      auto lane_sum = [&](int c) {
-        float v[V::N];
-        V::get(p[c * 32 + lane], v);
-        uint64_t a = 0;
-#pragma unroll
-        for (int e = 0; e < V::N; ++e)
-          if (v[e] >= least) a += f(v[e], base + (c * 32 + lane) * V::N + e);
-        return a;
-      };
-      uint64_t a = 0;
-      for (int c = c0; c < c1; ++c) a += lane_sum(c);
-      a = warp_sum_u64(a);
-      if (lane == 0) sh.part[warp] = a;
-      __syncthreads();
-      const uint64_t x = lane < NW ? sh.part[lane] : 0, inc = warp_scan_u64(x), all = __shfl_sync(0xffffffffu, inc, 31);
-      left = min(left, all - 1);
-      const unsigned over = __ballot_sync(0xffffffffu, inc > left);
-      if (!over && threadIdx.x == 0) sh.found_id[turn] = 0xffffffffu, sh.found_w[turn] = 0;
-      const int who = __ffs(over) - 1;
-      if (who == warp) {
-        left -= __shfl_sync(0xffffffffu, inc - x, who);
-        for (int c = c0; c < c1; ++c) {
-          const uint64_t mine = lane_sum(c), in = warp_scan_u64(mine);
-          const unsigned hit = __ballot_sync(0xffffffffu, in > left);
-          if (hit) {
-            if (lane == __ffs(hit) - 1) {
-              uint64_t rem = left - (in - mine);
-              float v[V::N];
-              V::get(p[c * 32 + lane], v);
-              bool open = true;
-#pragma unroll
-              for (int e = 0; e < V::N; ++e) {
-                const int i = base + (c * 32 + lane) * V::N + e;
-                const uint64_t x2 = open && v[e] >= least ? f(v[e], i) : 0;
-                if (open && x2 > rem) {
-                  sh.found_id[turn] = static_cast<uint32_t>(i);
-                  sh.found_w[turn] = x2;
-                  open = false;
-                }
-                rem -= x2;
-              }
-            }
-            break;
-          }
-          left -= __shfl_sync(0xffffffffu, in, 31);
-        }
-      }
-    }
-    sync();
-    *id = static_cast<int>(remote_u32(cluster_addr(&sh.found_id[turn], at / NW)));
-    if (value) *value = remote_u64(cluster_addr(&sh.found_w[turn], at / NW));
-    turn ^= 1;
-    return total;
-  }
-  // Sums of f, which is 0 or 1, into the warps' sums.
-  template <class F>
-  __device__ void sums_of(float least, F&& f) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const bool l = listed;
-    listed = false;
-    uint64_t mine = 0;
-    each(least, [&](float v, int i) { mine += f(v, i); });
-    listed = l;
-    mine = warp_sum_u64(mine);
-    if (lane == 0) sh.sums[turn][warp] = mine;
-  }
-
-  // Lists the elements from `least` to `most` that `from` keeps.  False (in every block): one of the lists is too short for them.
-  __device__ bool make_list(const Cut& from, float least, float most) {
-    listed = false;
-    if (threadIdx.x == 0) sh.list_n = 0;
-    if (threadIdx.x < NW) sh.above[threadIdx.x] = 0;
+  __device__ __forceinline__ uint64_t sum(uint64_t own) const {
+    uint64_t all;
+    scan_block(own, sh.room, &all);
     __syncthreads();
-    each(least, [&](float l, int id) {
-      if (l > most || !kept(from, Key<T>::of(l), id)) return;
-      const uint32_t i = atomicAdd(&sh.list_n, 1u);
-      if (i < CAP) sh.list[i] = static_cast<uint16_t>(id - first);
-    });
-    sync();
-    uint32_t n = 0;
-#pragma unroll
-    for (int r = 0; r < CS; ++r) n = max(n, remote_u32(cluster_addr(&sh.list_n, r)));
-    listed = n <= CAP;
-    return listed;
+    return all;
   }
 
-  // Sum over the threads up to this one and over all (block-collective); the arrays may be used again after a __syncthreads.
-  __device__ __forceinline__ uint64_t scan_block(uint64_t own) const {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    uint64_t incl = warp_scan_u64(own);
-    if (lane == 31) sh.scan[warp] = incl;
-    __syncthreads();
-    const uint64_t x = warp_scan_u64(lane < NW ? sh.scan[lane] : 0);
-    return warp > 0 ? incl + __shfl_sync(0xffffffffu, x, warp - 1) : incl;
-  }
-
-  // The cut that keeps, of the elements that `from` keeps, the first ones of the order: `target` of them (BY_MASS: as many
-  // as have less than `target` of mass in front of them).  At least one element is kept by `from`, target >= 1 and at most
-  // all of them (their mass).  Keys outside lo .. hi need not be looked at; `above`: what lies above hi counts.  False: the cut is not
-  // between lo and hi.
+  // The cut that keeps, of the candidates that `from` keeps, the first ones of the order: `target` of them (BY_MASS: as many
+  // as have less than `target` of mass in front of them; `above`: mass of what is kept beside the candidates).  Keys outside
+  // lo .. hi are not looked at.  False: the cut is not there.
   template <bool BY_MASS>
   __device__ bool narrow(const Cut& from, uint32_t lo, uint32_t hi, uint64_t above, uint64_t target, Cut* cut) {
-    const uint64_t start = above;
-    uint32_t inside = 0xffffffffu;         // elements in the window
-    bool by_value = hi == Key<T>::of(s.max);   // first by value, in steps of equal ratios of weights; then by key
-    for (int level = 0; lo < hi && inside > LIST; ++level) {
-      const int buf = level & 1;
-      sh.count[buf][threadIdx.x] = 0;
-      sh.mass[buf][threadIdx.x] = 0;
+    uint32_t inside = 0xffffffffu;         // candidates in the window
+    if (above >= target) return false;
+    bool by_value = hi == Key<T>::of(max); // first by value, in steps of equal ratios of weights; then by key
+    while (lo < hi && inside > LIST) {
+      sh.count[threadIdx.x] = 0;
+      sh.mass[threadIdx.x] = 0;
       if (threadIdx.x == 0) sh.d_count = 0;
       __syncthreads();
-      const float range = s.max - Key<T>::value(lo);
+      const float range = max - Key<T>::value(lo);
       by_value = by_value && range < 3e38f;
       const float per = by_value ? (NB - 1) / range : 0.0f;
       int shift = 0;
       while (((hi - lo) >> shift) >= NB) ++shift;
-      auto value_bin = [&](float l) { return min(NB - 1, static_cast<int>((s.max - l) * per)); };
-      const float least = Key<T>::value(lo), most = Key<T>::value(hi);
-      each(least, [&](float l, int id) {
-        const uint32_t key = Key<T>::of(l);
-        if (l > most || !kept(from, key, id)) return;
-        const int bin = by_value ? value_bin(l) : static_cast<int>((hi - key) >> shift);
-        atomicAdd(&sh.count[buf][bin], 1u);
-        if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[buf][bin]), static_cast<unsigned long long>(w(l)));
+      auto value_bin = [&](uint32_t key) { return min(NB - 1, static_cast<int>((max - Key<T>::value(key)) * per)); };
+      each([&](uint32_t key, int id) {
+        if (key < lo || key > hi || !kept(from, key, id)) return;
+        const int bin = by_value ? value_bin(key) : static_cast<int>((hi - key) >> shift);
+        atomicAdd(&sh.count[bin], 1u);
+        if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[bin]), static_cast<unsigned long long>(w(Key<T>::value(key))));
       });
-      sync();
-      // a bin per thread, all blocks' together
-      uint32_t n = 0;
-      uint64_t m = 0;
-#pragma unroll
-      for (int r = 0; r < CS; ++r) {
-        n += remote_u32(cluster_addr(&sh.count[buf][threadIdx.x], r));
-        if (BY_MASS) m += remote_u64(cluster_addr(&sh.mass[buf][threadIdx.x], r));
-      }
-      const uint64_t own = BY_MASS ? m : n, incl = scan_block(own);
+      __syncthreads();
+      const uint64_t own = BY_MASS ? sh.mass[threadIdx.x] : sh.count[threadIdx.x], incl = scan_block(own, sh.room);
       if (above + incl >= target && above + incl - own < target) {
         sh.d_bin = threadIdx.x;
-        sh.d_count = n;
+        sh.d_count = sh.count[threadIdx.x];
         sh.d_above = above + incl - own;
       }
       __syncthreads();
@@ -567,384 +674,334 @@ struct Row {
       above = sh.d_above;
       if (by_value) {
         const int b = static_cast<int>(bin);
-        const uint32_t lo2 = first_key(lo, hi, [&](uint32_t k) { return value_bin(Key<T>::value(k)) <= b; });
-        if (b > 0) hi = first_key(lo2, hi, [&](uint32_t k) { return value_bin(Key<T>::value(k)) <= b - 1; }) - 1;
+        const uint32_t lo2 = first_key(lo, hi, [&](uint32_t k) { return value_bin(k) <= b; });
+        if (b > 0) hi = first_key(lo2, hi, [&](uint32_t k) { return value_bin(k) <= b - 1; }) - 1;
         lo = lo2;
         by_value = false;
       } else {
         const uint32_t top = hi - (bin << shift);
-        lo = max(lo, top - min(top, (1u << shift) - 1));
+        lo = ::max(lo, top - min(top, (1u << shift) - 1));
         hi = top;
       }
-      __syncthreads();                                        // (d_bin is written again)
+      __syncthreads();                     // (d_bin and the histogram are written again)
     }
-    const float least = Key<T>::value(lo), most = Key<T>::value(hi);
     if (lo >= hi) {
-      if (above >= target) return false;
       // one key: of its ids the first ones, in the order of ids
       uint64_t need = target - above;
       if (BY_MASS) {
-        const uint64_t each_w = w(least);
-        if (each_w == 0) return false;
-        need = (need + each_w - 1) / each_w;
+        const uint64_t one = w(Key<T>::value(lo));
+        if (one == 0) return false;
+        need = (need + one - 1) / one;
       }
-      auto one = [&](float l, int i) { return l == least && kept(from, Key<T>::of(l), i) ? 1ull : 0ull; };
-      int id;
-      sums_of(least, one);
-      if (pick(least, one, [&](uint64_t all) { return min(all, need) - 1; }, &id, nullptr) < need && above == start) return false;
-      *cut = {lo, id};
+      // by id as above by key
+      uint32_t first = 0, last = static_cast<uint32_t>(l.vocab - 1), front = 0;
+      while (first < last) {
+        sh.count[threadIdx.x] = 0;
+        if (threadIdx.x == 0) sh.d_count = 0;
+        __syncthreads();
+        int shift = 0;
+        while (((last - first) >> shift) >= NB) ++shift;
+        each([&](uint32_t key, int id) {
+          if (key == lo && kept(from, key, id) && static_cast<uint32_t>(id) >= first && static_cast<uint32_t>(id) <= last)
+            atomicAdd(&sh.count[(id - first) >> shift], 1u);
+        });
+        __syncthreads();
+        const uint64_t own = sh.count[threadIdx.x], incl = scan_block(own, sh.room);
+        if (front + incl >= need && front + incl - own < need) {
+          sh.d_bin = threadIdx.x;
+          sh.d_count = static_cast<uint32_t>(own);
+          sh.d_above = front + incl - own;
+        }
+        __syncthreads();
+        if (sh.d_count == 0) return false; // fewer than that
+        front = static_cast<uint32_t>(sh.d_above);
+        first += sh.d_bin << shift;
+        last = min(last, first + (1u << shift) - 1);
+        __syncthreads();
+      }
+      *cut = {lo, static_cast<int>(first)};
       return true;
     }
-    // a few elements: each of them finds what is in front of it
-    if (threadIdx.x == 0) sh.few_n = 0, sh.d_id = 0xffffffffu;
+    // a few candidates: each of them finds what is in front of it
+    if (threadIdx.x == 0) sh.few = 0, sh.d_id = 0xffffffffu;
     __syncthreads();
-    each(least, [&](float l, int id) {
-      const uint32_t key = Key<T>::of(l);
-      if (l > most || !kept(from, key, id)) return;
-      const uint32_t i = atomicAdd(&sh.few_n, 1u);
+    each([&](uint32_t key, int id) {
+      if (key < lo || key > hi || !kept(from, key, id)) return;
+      const int i = atomicAdd(&sh.few, 1);
       sh.few_key[i] = key;
       sh.few_id[i] = id;
+      sh.all_w[i] = BY_MASS ? w(Key<T>::value(key)) : 1;
     });
-    sync();
-    uint32_t n_all = 0, off = 0;
-    int src = -1;
-#pragma unroll
-    for (int r = 0; r < CS; ++r) {
-      const uint32_t n = remote_u32(cluster_addr(&sh.few_n, r));
-      if (threadIdx.x >= n_all && threadIdx.x < n_all + n) {
-        src = r;
-        off = threadIdx.x - n_all;
-      }
-      n_all += n;
+    __syncthreads();
+    // four threads a candidate
+    const int i = threadIdx.x >> 2, n = sh.few;
+    uint64_t front = 0;
+    if (i < n) {
+      const uint32_t key = sh.few_key[i], id = sh.few_id[i];
+      for (int j = threadIdx.x & 3; j < n; j += 4)
+        if (sh.few_key[j] > key || (sh.few_key[j] == key && sh.few_id[j] < id)) front += sh.all_w[j];
     }
-    if (src >= 0) {
-      const uint32_t key = remote_u32(cluster_addr(&sh.few_key[off], src));
-      sh.all_key[threadIdx.x] = key;
-      sh.all_id[threadIdx.x] = remote_u32(cluster_addr(&sh.few_id[off], src));
-      sh.all_w[threadIdx.x] = BY_MASS ? w(Key<T>::value(key)) : 1;
+    front += __shfl_xor_sync(0xffffffffu, front, 1);
+    front += __shfl_xor_sync(0xffffffffu, front, 2);
+    if (i < n && (threadIdx.x & 3) == 0 && above + front < target && above + front + sh.all_w[i] >= target) {
+      sh.d_key = sh.few_key[i];
+      sh.d_id = sh.few_id[i];
     }
     __syncthreads();
-    // four threads an element
-    {
-      const uint32_t i = threadIdx.x >> 2, part = threadIdx.x & 3;
-      uint64_t front = 0;
-      if (i < n_all) {
-        const uint32_t key = sh.all_key[i], id = sh.all_id[i];
-        for (uint32_t j = part; j < n_all; j += 4)
-          if (sh.all_key[j] > key || (sh.all_key[j] == key && sh.all_id[j] < id)) front += sh.all_w[j];
-      }
-      front += __shfl_xor_sync(0xffffffffu, front, 1);
-      front += __shfl_xor_sync(0xffffffffu, front, 2);
-      if (i < n_all && part == 0 && above + front < target && above + front + sh.all_w[i] >= target) {
-        sh.d_key = sh.all_key[i];
-        sh.d_id = sh.all_id[i];
-      }
-    }
-    sync();                                                   // (the few have been read by all)
     *cut = {sh.d_key, static_cast<int>(sh.d_id)};
-    return cut->id >= 0;
-  }
-
-  // A key below which no element is among the first k: the lanes' maxima, `mine` of each, are counted by value.
-  __device__ uint32_t bound_k(uint32_t lo, uint32_t hi, float mine, float least_mine, uint64_t k) {
-    const float range = s.max - least_mine;
-    if (!(range > 0.0f && range < 3e38f)) return lo;
-    const float per = (NB - 1) / range;
-    auto value_bin = [&](float l) { return min(NB - 1, static_cast<int>((s.max - l) * per)); };
-    sh.count[0][threadIdx.x] = 0;
-    if (threadIdx.x == 0) sh.d_bin = NB;
+    const bool found = sh.d_id != 0xffffffffu;
     __syncthreads();
-    if (mine >= least_mine) atomicAdd(&sh.count[0][value_bin(mine)], 1u);
-    sync();
-    uint32_t n = 0;
-#pragma unroll
-    for (int r = 0; r < CS; ++r) n += remote_u32(cluster_addr(&sh.count[0][threadIdx.x], r));
-    const uint64_t incl = scan_block(n);
-    if (incl >= k && incl - n < k) sh.d_bin = threadIdx.x;
-    __syncthreads();
-    const int b = static_cast<int>(sh.d_bin);
-    sync();                                                   // (the counts may be written again)
-    if (b >= NB - 1) return lo;
-    return max(lo, first_key(lo, hi, [&](uint32_t key) { return value_bin(Key<T>::value(key)) <= b; }));
-  }
-
-  // The nucleus of a row that is not listed: p of the mass of what `from` keeps.
-  __device__ Cut nucleus(const Cut& from, float p, int vocab) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t khi = Key<T>::of(s.max);
-    auto nothing = [](float, int) { return 0ull; };
-    auto any = [](uint64_t) { return 0ull; };
-    auto target_of = [&](uint64_t mass) {
-      const uint64_t t = static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(mass)));
-      return min(max(t, static_cast<uint64_t>(1)), mass);
-    };
-    Cut cut{};
-    // Ids that weigh less than (1 - p) / vocab of the maximum together weigh less than 1 - p of the mass: none is kept.
-    const float depth = (__log2f(static_cast<float>(vocab) / (1.0f - p)) + 0.5f) / s.hi;
-    const uint32_t low = max(from.key, Key<T>::of(s.max - depth));
-    if (from.id == ALL && from.key < khi && s.hi > kFlat) {
-      const float cutv = below(Key<T>::value(from.key)), per = (NB - 2) / depth;
-      sh.count[0][threadIdx.x] = 0;
-      if (threadIdx.x == 0) sh.d_bin = NB;
-      __syncthreads();
-      const uint64_t mine = bulk<true>(cutv, per, sh.count[0]);
-      if (lane == 0) sh.sums[turn][warp] = mine;
-      const uint64_t mass = pick(0.0f, nothing, any, nullptr, nullptr);
-      const uint64_t target = target_of(mass);
-      uint32_t n = 0;
-#pragma unroll
-      for (int r = 0; r < CS; ++r) n += remote_u32(cluster_addr(&sh.count[0][threadIdx.x], r));
-      // a bin's mass, about, in 2^-32 of the maximum's
-      const float b_c = fmaf(s.max, per, 12582912.0f), off = fmaf(-s.max, per, b_c - 12582912.0f);   // (of the maximum from its bin's middle)
-      const float mid = ex2_approx((off - static_cast<float>(threadIdx.x)) / per * s.hi) * 262144.0f;
-      const uint64_t guess = static_cast<uint64_t>(static_cast<float>(n) * mid), incl = scan_block(guess);
-      if (incl >= target >> 12 && incl - guess < target >> 12) sh.d_bin = threadIdx.x;
-      __syncthreads();
-      const int b = static_cast<int>(sh.d_bin);
-      if (b < NB - 2) {
-        // the keys of the bins b - 1 .. b + 1
-        auto bin = [&](uint32_t k) { return static_cast<int>(__float_as_uint(fmaf(Key<T>::value(k), -per, b_c)) - 0x4b400000u); };
-        const uint32_t lo = first_key(low, khi, [&](uint32_t k) { return bin(k) <= b + 1; });
-        const uint32_t hi = b > 1 ? first_key(lo, khi, [&](uint32_t k) { return bin(k) <= b - 2; }) - 1 : khi;
-        if (make_list(from, Key<T>::value(lo), Key<T>::value(hi))) {
-          const uint64_t over = hi < khi ? bulk<false>(Key<T>::value(hi), 0.0f, nullptr) : 0;
-          if (lane == 0) sh.above[warp] = sh.sums[turn][warp] = over;
-          const uint64_t above = pick(0.0f, nothing, any, nullptr, nullptr);
-          if (above < target && narrow<true>(from, lo, hi, above, target, &cut)) return cut;
-          listed = false;
-        }
-      }
-    }
-    sums_kept(from);
-    const uint64_t mass = pick(0.0f, nothing, any, nullptr, nullptr);
-    if (!narrow<true>(from, low, khi, 0, target_of(mass), &cut)) cut = from;
-    return cut;
+    return found;
   }
 };
 
-template <class T, int CS>
-__global__ void __launch_bounds__(NT) sample_kernel(const SampleArgs a) {
-  using V = Vec<T>;
+// DIRECT: rows of up to CAP ids, nothing ran ahead.
+template <class T, bool DIRECT>
+__global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
   extern __shared__ __align__(16) uint8_t smem[];
-  Shared& sh = *reinterpret_cast<Shared*>(smem);
-  uint4* data = reinterpret_cast<uint4*>(smem + (sizeof(Shared) + 15) / 16 * 16);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = CS > 1 ? static_cast<int>(cluster_ctarank()) : 0, row = blockIdx.x / CS;
-  if (threadIdx.x < 32) sh.pow[threadIdx.x] = kPow[threadIdx.x];
-  pdl_enter();
-  // ---- the row into shared memory, its maximum
-  const int first = rank * NW * a.seg;
-  const T* src = static_cast<const T*>(a.logits) + row * a.ld;
+  Finish& sh = *reinterpret_cast<Finish*>(smem);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
   const float ninf = __int_as_float(0xff800000);
-  const float t = a.temperature ? a.temperature[row] : 1.0f, p = a.top_p ? a.top_p[row] : 1.0f, mp = a.min_p ? a.min_p[row] : 0.0f;
-  const int k = !(t > 0x1p-100f) || p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
-  const float u0 = a.u[row];
-  float top = ninf;
-  {
-    const bool vec = (reinterpret_cast<uintptr_t>(src) & 15) == 0;
-    const int base = first + warp * a.seg, n = a.seg / V::N;
-    uint4* dst = data + warp * n;
-    auto take = [&](int i, const uint4& q) {
-      float v[V::N];
-      V::get(q, v);
-      const int id = base + i * V::N;
-#pragma unroll
-      for (int e = 0; e < V::N; ++e) v[e] = fmaxf(v[e] + 0.0f, ninf);   // NaN: -inf
-      if (static_cast<uint32_t>(a.mask_id - id) < V::N) {
-#pragma unroll
-        for (int e = 0; e < V::N; ++e)
-          if (id + e == a.mask_id) v[e] = ninf;
+  if (threadIdx.x < 16) sh.pow[threadIdx.x] = kPow[threadIdx.x];
+  if (threadIdx.x == 0) sh.n = 0;
+  pdl_enter();
+  const Logits<T> l(a, row);
+  Row r = row_of(a, row, sh.c);
+  const float u = a.u[row];
+  RowPlan plan;
+  if constexpr (DIRECT) {
+    float top = ninf;
+    for (int id = threadIdx.x; id < a.vocab; id += NT) top = fmaxf(top, l.one(id));
+    top = warp_max(top);
+    if (lane == 0) sh.max[warp] = top;
+    __syncthreads();
+    top = warp_max(sh.max[lane & (NW - 1)]);
+    for (int id = threadIdx.x; id < a.vocab; id += NT) {
+      const float v = l.one(id);
+      if (v > ninf && (r.k != 1 || v == top)) {
+        const int i = atomicAdd(&sh.n, 1);
+        sh.key[i] = Key<T>::of(v);
+        sh.id[i] = id;
       }
-#pragma unroll
-      for (int e = 0; e < V::N; ++e) top = fmaxf(top, v[e]);
-      dst[i] = V::put(v);
-    };
-    auto one = [&](int i) {                                   // element by element: the row's end, and rows off 16 bytes
-      float v[V::N];
-#pragma unroll
-      for (int e = 0; e < V::N; ++e) {
-        const int id = base + i * V::N + e;
-        v[e] = id < a.vocab ? to_f32(src[id]) : ninf;
-      }
-      return V::put(v);
-    };
-    constexpr int U = 4;
-    for (int i0 = lane; i0 < n; i0 += 32 * U) {
-      uint4 q[U];
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int i = i0 + 32 * k, id = base + i * V::N;
-        if (i < n) q[k] = vec && id + V::N <= a.vocab ? __ldcs(reinterpret_cast<const uint4*>(src + id)) : one(i);
-      }
-#pragma unroll
-      for (int k = 0; k < U; ++k)
-        if (i0 + 32 * k < n) take(i0 + 32 * k, q[k]);
     }
-  }
-  const float lane_top = top;
-  {
-    const float hi = warp_max(top), lo = -warp_max(top > ninf ? -top : ninf);
-    if (lane == 0) sh.wtop[warp] = make_float2(hi, lo);
-  }
-  if (threadIdx.x == 0) {                                     // (double precision is slow here: one thread, for all)
-    const double c = 1.4426950408889634074 / static_cast<double>(t);
-    sh.c_hi = static_cast<float>(c);
-    sh.c_lo = static_cast<float>(c - static_cast<double>(sh.c_hi));
-    if (mp > 0.0f) sh.low64 = mp >= 1.0f ? 0.0 : static_cast<double>(t) * log(static_cast<double>(mp));
+    const int mj = mj_of(sh.c[0], sh.c[1], top);
+    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, sh.c[0] > 1e-30f ? mj : kFar, 0, 0, 0};
+  } else {
+    plan = a.plan[row];
+    const uint2* list = a.list + static_cast<int64_t>(row) * CAP;
+    if (plan.mode == kListed || plan.mode == kWindow) {
+      if (plan.listed > CAP) plan.mode = kWhole;
+      else
+        for (int i = threadIdx.x; i < plan.listed; i += NT) {
+          const uint2 x = list[i];
+          sh.key[i] = x.x;
+          sh.id[i] = x.y;
+        }
+    }
+    if (threadIdx.x == 0) sh.n = plan.listed;
   }
   __syncthreads();
-  if (warp == 0) {
-    const float2 x = lane < NW ? sh.wtop[lane] : make_float2(ninf, -ninf);
-    const float hi = warp_max(x.x), lo = -warp_max(-x.y);
-    if (lane == 0) sh.top = make_float2(hi, lo);
-  }
-  Row<T, CS> r{sh, data, first, a.seg, rank, {}, 0, false};
-  r.sync();
-  float least_top = -ninf;
-#pragma unroll
-  for (int i = 0; i < CS; ++i) {
-    top = fmaxf(top, __uint_as_float(remote_u32(cluster_addr(&sh.top.x, i))));
-    least_top = fminf(least_top, __uint_as_float(remote_u32(cluster_addr(&sh.top.y, i))));
-  }
-  const bool writer = rank == 0 && threadIdx.x == 0;
-  if (top == ninf) {                                          // nothing to draw from
-    if (writer) {
+  if (plan.mode == kEmpty) {
+    if (threadIdx.x == 0) {
       a.tok[row] = -1;
       if (a.prob) a.prob[row] = 0.0f;
     }
-    r.sync();
     return;
   }
-  const uint32_t khi = Key<T>::of(top);
-  int id = -1;
-  if (k == 1 || top == -ninf) {
-    // the first of the order, the lowest id of the maximum; or, of an infinite maximum, ids of equal weight
-    auto of_max = [&](float l, int) { return l == top ? 1ull : 0ull; };
-    r.sums_of(top, of_max);
-    uint64_t n = 1;
-    r.pick(top, of_max, [&](uint64_t all) {
-      if (k == 1) return static_cast<uint64_t>(0);
-      n = k > 0 ? min(all, static_cast<uint64_t>(k)) : all;
-      if (p < 1.0f) n = min(n, max(static_cast<uint64_t>(1), static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(n)))));
-      const double x = (u0 > 0.0f ? static_cast<double>(u0) : 0.0) * static_cast<double>(n);
-      return x >= static_cast<double>(n) ? n - 1 : static_cast<uint64_t>(x);
-    }, &id, nullptr);
-    if (writer) {
-      a.tok[row] = id;
-      if (a.prob) a.prob[row] = 1.0f / static_cast<float>(n);
+  r.hi = sh.c[0], r.lo = sh.c[1];
+  const bool far = plan.mj == kFar;
+  Finisher<T> f{sh, l, Scale(r.hi, r.lo, far ? 0 : plan.mj, far ? plan.max : 0.0f), plan.max, plan.mode == kWhole};
+  const uint32_t khi = Key<T>::of(plan.max), kinf = Key<T>::of(ninf) + 1;
+  if (r.k == 1) {                          // the lowest id of the maximum
+    if (threadIdx.x == 0) sh.d_id = 0xffffffffu;
+    __syncthreads();
+    f.each([&](uint32_t key, int id) {
+      if (key == khi) atomicMin(&sh.d_id, static_cast<uint32_t>(id));
+    });
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      a.tok[row] = static_cast<int>(sh.d_id);
+      if (a.prob) a.prob[row] = 1.0f;
     }
-    r.sync();
     return;
   }
-  r.s = {top, sh.c_hi, sh.c_lo};
-  // ---- what bulk() needs of the row: M = c max (max less itself where it is large) to 1/16, and the table with the rest of it
-  if (threadIdx.x < 16) {
-    const float xm = fabsf(top * r.s.hi) >= 92.0f ? 0.0f : top;
-    const float m = xm * r.s.hi, e = fmaf(xm, r.s.lo, fmaf(xm, r.s.hi, -m));
-    const float mh = rintf(16.0f * m) * 0.0625f, rest = (m - mh) + e;      // |rest| <= 1/32
-    const double f = -static_cast<double>(rest) * 0.693147180559945309417;
-    const double x = 1.0 + f * (1.0 + f * (0.5 + f * (1.0 / 6 + f * (1.0 / 24 + f * (1.0 / 120 + f / 720)))));
-    const double v = x * (static_cast<double>(sh.pow[2 * threadIdx.x]) * 0x1p-43);
-    const float h = static_cast<float>(v);
-    sh.pow16[threadIdx.x] = make_float2(h, static_cast<float>(v - static_cast<double>(h)));
-    sh.mh = mh;
-    if (threadIdx.x == 0) {                                   // the least logit that min-p keeps, rounded up
-      const double least = mp > 0.0f ? static_cast<double>(top) + sh.low64 : -INFINITY;
-      sh.low = __double2float_ru(least);
-    }
-  }
-  if (threadIdx.x < NW) sh.above[threadIdx.x] = 0;
-  __syncthreads();
   // ---- the cut: min-p, top-k, top-p
-  Cut cut{Key<T>::of(ninf) + 1, ALL};
-  if (mp > 0.0f) {
-    const float low = fminf(sh.low, top) + 0.0f;
-    const uint32_t key = Key<T>::of(low);
-    cut.key = max(cut.key, Key<T>::value(key) < low ? key + 1 : key);
+  const uint64_t* seg = DIRECT ? nullptr : a.seg + static_cast<int64_t>(row) * a.chunks * NW;
+  const int segs = (a.vocab + SEG - 1) / SEG;
+  uint64_t above = 0;
+  if (!DIRECT && plan.mode == kWindow) {
+    uint64_t own = 0;
+    for (int i = threadIdx.x; i < segs; i += NT) own += seg[i];
+    above = f.sum(own);
   }
-  if (k > 0 || mp > 0.0f) {
-    const uint32_t lo = k > 0 && k < a.vocab ? r.bound_k(cut.key, khi, lane_top, least_top, k) : cut.key;
-    r.make_list(cut, Key<T>::value(lo), top);
-    if (k > 0 && k < a.vocab) {
-      // (fewer than k: all of them)
+  Cut low{kinf, ALL};
+  if (r.mp > 0.0f) {                       // the least logit that min-p keeps, rounded up
+    const double x = r.mp >= 1.0f ? 0.0 : static_cast<double>(r.t) * log(static_cast<double>(r.mp));
+    const float least = fminf(__double2float_ru(static_cast<double>(plan.max) + x), plan.max) + 0.0f;
+    const uint32_t key = Key<T>::of(least);
+    low.key = ::max(low.key, Key<T>::value(key) < least ? key + 1 : key);
+  }
+  Cut cut = low;
+  bool window = plan.mode == kWindow;
+  if (plan.mode != kAll) {
+    for (;;) {                             // the list; where that fails, the row
+      bool ok = true;
+      cut = low;
       Cut to{};
-      if (r.template narrow<false>(cut, lo, khi, 0, k, &to)) cut = to;
+      if (window) {
+        if (r.p < 1.0f && r.mp <= 0.0f) {
+          ok = f.template narrow<true>(cut, ::max(cut.key, Key<T>::of(plan.lo)), Key<T>::of(plan.hi), above, plan.target, &to);
+          if (ok) cut = to;
+        }
+      } else {
+        if (r.k > 0) {
+          if (f.template narrow<false>(cut, cut.key, khi, 0, r.k, &to)) cut = to;
+          else ok = f.whole || !plan.more; // (fewer than k candidates: all of them)
+        }
+        if (ok && r.p < 1.0f) {
+          uint64_t target = plan.target;
+          if (DIRECT || f.whole || far || r.k > 0 || r.mp > 0.0f) {
+            uint64_t own = 0;
+            f.each([&](uint32_t key, int id) { own += f.kept(cut, key, id) ? f.w(Key<T>::value(key)) : 0; });
+            const uint64_t mass = f.sum(own);
+            target = min(::max(static_cast<uint64_t>(ceil(static_cast<double>(r.p) * static_cast<double>(mass))), static_cast<uint64_t>(1)), mass);
+          }
+          uint32_t lo = cut.key;
+          if (r.hi > 1e-30f) lo = ::max(lo, Key<T>::of(plan.max - 46.0f / r.hi));
+          ok = f.template narrow<true>(cut, min(lo, khi), khi, 0, target, &to);
+          if (ok) cut = to;
+          ok = ok || f.whole;
+        }
+      }
+      if (ok) break;
+      f.whole = true;
+      window = false;
     }
   }
-  if (p < 1.0f) {
-    if (r.listed) {
-      r.sums_kept(cut);
-      const uint64_t mass = r.pick(0.0f, [](float, int) { return 0ull; }, [](uint64_t) { return 0ull; }, nullptr, nullptr);
-      const uint64_t target = max(static_cast<uint64_t>(1), static_cast<uint64_t>(ceil(static_cast<double>(p) * static_cast<double>(mass))));
-      Cut to{};
-      if (r.template narrow<true>(cut, cut.key, khi, 0, min(target, mass), &to)) cut = to;
-    } else {
-      cut = r.nucleus(cut, p, a.vocab);
+  // ---- the draw: the masses of 512 ids each
+  for (int i = threadIdx.x; i < static_cast<int>(sizeof(sh.seg) / 8); i += NT)
+    sh.seg[i] = !DIRECT && (window || plan.mode == kAll) && i < segs ? seg[i] : 0;
+  __syncthreads();
+  if (f.whole) {
+    constexpr int N = Vec<T>::N;
+    for (int i = warp; i < segs; i += NW) {
+      uint64_t own = 0;
+      for (int id = i * SEG + lane * N; id < (i + 1) * SEG; id += 32 * N) {
+        float v[N];
+        l.get(l.load(id), id, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (v[e] > ninf && f.kept(cut, Key<T>::of(v[e]), id + e)) own += f.w(v[e]);
+      }
+      own = warp_sum_u64(own);
+      if (lane == 0) sh.seg[i] = own;
+    }
+  } else if (plan.mode != kAll) {
+    f.each([&](uint32_t key, int id) {
+      if (f.kept(cut, key, id))
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.seg[id / SEG]), static_cast<unsigned long long>(f.w(Key<T>::value(key))));
+    });
+  }
+  __syncthreads();
+  constexpr int EACH = (SEGS + NT - 1) / NT;                  // a thread's segments
+  uint64_t own = 0, mass;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) own += sh.seg[threadIdx.x * EACH + i];
+  const uint64_t incl = scan_block(own, sh.room, &mass);
+  const double at = (u > 0.0f ? static_cast<double>(u) : 0.0) * static_cast<double>(mass);
+  const uint64_t target = at >= static_cast<double>(mass) ? mass - 1 : min(mass - 1, static_cast<uint64_t>(at));
+  if (incl > target && incl - own <= target) {
+    uint64_t left = target - (incl - own);
+    int i = 0;
+    while (i + 1 < EACH && left >= sh.seg[threadIdx.x * EACH + i]) left -= sh.seg[threadIdx.x * EACH + i++];
+    sh.d_bin = threadIdx.x * EACH + i;
+    sh.d_left = left;
+  }
+  if (threadIdx.x == 0) sh.d_best = 0, sh.d_w = 0;
+  __syncthreads();
+  // its ids, one a thread.  (Their weights may add up to a little less than the segment's mass.)
+  static_assert(SEG == NT, "one id a thread");
+  const int id = static_cast<int>(sh.d_bin) * SEG + threadIdx.x;
+  const float v = l.one(id);
+  const uint32_t key = Key<T>::of(v);
+  const bool in = v > ninf && f.kept(cut, key, id);
+  const uint64_t x = in ? f.w(v) : 0;
+  uint64_t all;
+  const uint64_t upto = scan_block(x, sh.room, &all);
+  if (all == 0) {                          // ids that weigh next to nothing: the heaviest of them
+    if (in) atomicMax(reinterpret_cast<unsigned long long*>(&sh.d_best), static_cast<unsigned long long>(key) << 32 | (0xffffffffu - id));
+  } else {
+    const uint64_t left = min(sh.d_left, all - 1);
+    if (upto > left && upto - x <= left) {
+      sh.d_best = 0xffffffffu - id;
+      sh.d_w = x;
     }
   }
-  // ---- the draw
-  uint64_t value = 0;
-  r.sums_kept(cut);
-  const uint64_t mass = r.pick(Key<T>::value(cut.key), [&](float l, int i) { return r.kept(cut, Key<T>::of(l), i) ? r.w(l) : 0ull; },
-                               [&](uint64_t all) {
-    const double u = u0 > 0.0f ? static_cast<double>(u0) : 0.0;
-    const double x = u * static_cast<double>(all);
-    return x >= static_cast<double>(all) ? all - 1 : min(all - 1, static_cast<uint64_t>(x));
-  }, &id, &value);
-  if (writer) {
-    a.tok[row] = id;
-    if (a.prob) a.prob[row] = static_cast<float>(static_cast<double>(value) / static_cast<double>(mass));
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.tok[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sh.d_best));
+    if (a.prob) a.prob[row] = static_cast<float>(static_cast<double>(sh.d_w) / static_cast<double>(mass));
   }
-  r.sync();                                                   // no block leaves while another reads its memory
 }
 
-template <class T, int CS>
-cudaError_t launch(const SampleArgs& a, int rows, size_t smem, cudaStream_t s) {
-  cudaError_t e = cudaSuccess;
+template <class... KArgs, class... Args>
+cudaError_t start(void (*kernel)(KArgs...), int64_t grid, size_t smem, cudaStream_t s, Args&&... args) {
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(grid)), dim3(NT), smem, s, args...);
+}
+
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+int chunks_of(int vocab) { return vocab <= CAP ? 0 : (vocab + CHUNK - 1) / CHUNK; }
+// The scratch memory's parts; returns its size.
+size_t place(SampleArgs* a, int rows, int vocab, uint8_t* base) {
+  const size_t chunks = chunks_of(vocab), n = static_cast<size_t>(rows);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += up(bytes);
+    return base + here;
+  };
+  a->info = reinterpret_cast<ChunkInfo*>(take(n * chunks * sizeof(ChunkInfo)));
+  a->seg = reinterpret_cast<uint64_t*>(take(n * chunks * NW * sizeof(uint64_t)));
+  a->hist = reinterpret_cast<uint32_t*>(take(n * chunks * NB * sizeof(uint32_t)));
+  a->plan = reinterpret_cast<RowPlan*>(take(n * sizeof(RowPlan)));
+  a->list = reinterpret_cast<uint2*>(take(n * CAP * sizeof(uint2)));
+  return at;
+}
+
+template <class T>
+cudaError_t run(const SampleArgs& a, cudaStream_t s) {
   static PerDevice ready;
   int dev = 0;
   cudaGetDevice(&dev);
+  cudaError_t e = cudaSuccess;
+  const int smem = static_cast<int>(sizeof(Finish));
   if (ready.get(dev, [&] {
-        e = cudaFuncSetAttribute(sample_kernel<T, CS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448);
+        e = cudaFuncSetAttribute(sample_finish_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_finish_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         return e == cudaSuccess ? 1 : 0;
       }) <= 0)
     return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(rows) * CS);
-  cfg.blockDim = dim3(NT);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = CS, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, sample_kernel<T, CS>, a);
+  if (a.chunks == 0) return start(sample_finish_kernel<T, true>, a.rows, smem, s, a);
+  const int64_t blocks = static_cast<int64_t>(a.rows) * a.chunks;
+  if ((e = start(sample_scan_kernel<T>, blocks, 0, s, a)) != cudaSuccess) return e;
+  if ((e = start(sample_plan_kernel<T>, a.rows, 0, s, a)) != cudaSuccess) return e;
+  if ((e = start(sample_collect_kernel<T>, blocks, 0, s, a)) != cudaSuccess) return e;
+  return start(sample_finish_kernel<T, false>, a.rows, smem, s, a);
 }
 
 }  // namespace
 
+size_t sample_scratch(int rows, int vocab) {
+  SampleArgs a;
+  return chunks_of(vocab) ? place(&a, rows, vocab, nullptr) : 0;
+}
+
 const char* sample_rows(const SampleCall& c, cudaStream_t s) {
-  int dev = 0;
-  const int sms = current_sms(&dev), es = c.bf16 ? 2 : 4, chunk = 32 * (16 / es);
-  // Blocks of a row: as few as let two of them share an SM (one loads while the other searches), and more while SMs would
-  // stay idle and every warp still has a few loads of its own.
-  auto seg_of = [&](int cs) { return (c.vocab + cs * NW * chunk - 1) / (cs * NW * chunk) * chunk; };
-  int cs = 1;
-  while (cs < MAXC && static_cast<int64_t>(seg_of(cs)) * NW * es > 90 * 1024) cs *= 2;
-  while (cs < MAXC && static_cast<int64_t>(c.rows) * cs * 2 <= sms && seg_of(cs) > 2 * chunk) cs *= 2;
-  const SampleArgs a{c.logits, c.ld, c.vocab, c.mask_id, seg_of(cs), c.temperature, c.top_k, c.top_p, c.min_p, c.u, c.tok, c.prob};
-  const size_t smem = (sizeof(Shared) + 15) / 16 * 16 + static_cast<size_t>(a.seg) * NW * es;
-  cudaError_t e;
-  if (c.bf16) {
-    e = cs == 1 ? launch<bf16, 1>(a, c.rows, smem, s) : cs == 2 ? launch<bf16, 2>(a, c.rows, smem, s)
-      : cs == 4 ? launch<bf16, 4>(a, c.rows, smem, s) : launch<bf16, 8>(a, c.rows, smem, s);
-  } else {
-    e = cs == 1 ? launch<float, 1>(a, c.rows, smem, s) : cs == 2 ? launch<float, 2>(a, c.rows, smem, s)
-      : cs == 4 ? launch<float, 4>(a, c.rows, smem, s) : launch<float, 8>(a, c.rows, smem, s);
-  }
+  SampleArgs a{};
+  a.logits = c.logits, a.ld = c.ld, a.rows = c.rows, a.vocab = c.vocab, a.mask_id = c.mask_id, a.chunks = chunks_of(c.vocab);
+  a.temperature = c.temperature, a.top_k = c.top_k, a.top_p = c.top_p, a.min_p = c.min_p, a.u = c.u, a.tok = c.tok, a.prob = c.prob;
+  if (a.chunks) place(&a, c.rows, c.vocab, static_cast<uint8_t*>(c.scratch));
+  const cudaError_t e = c.bf16 ? run<bf16>(a, s) : run<float>(a, s);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 

@@ -29,7 +29,7 @@ ABI_FUNCTIONS = [
     "tadm_ragged_sync_status", "tadm_attention_packed", "tadm_page_write", "tadm_page_read", "tadm_page_attention_scratch_size",
     "tadm_page_attention", "tadm_pages_scratch_size", "tadm_pages_reserve", "tadm_pages_fork", "tadm_pages_free",
     "tadm_pages_compact", "tadm_pages_copy",
-    "tadm_sample", "tadm_lora_scratch_size", "tadm_lora_project", "tadm_residual_norm",
+    "tadm_sample_scratch_size", "tadm_sample", "tadm_lora_scratch_size", "tadm_lora_project", "tadm_residual_norm",
 ]
 
 
@@ -134,7 +134,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "tadm_pages_free": (I, [P, P, P, I, I, I, P, I, P, P, P, P, P, SZ, P]),
         "tadm_pages_compact": (I, [P, P, P, I, I, P, P, P, P, SZ, P]),
         "tadm_pages_copy": (I, [P, P, P, I, P]),
-        "tadm_sample": (I, [P, I64, I, I, I] + [P] * 7 + [I, P]),
+        "tadm_sample_scratch_size": (I, [I, I, ctypes.POINTER(SZ)]),
+        "tadm_sample": (I, [P, I64, I, I, I] + [P] * 7 + [I, P, SZ, P]),
         "tadm_lora_scratch_size": (I, [I] * 7 + [ctypes.POINTER(SZ)]),
         "tadm_lora_project": (I, [P] * 5 + [I] * 4 + [I64] * 3 + [P] * 3 + [I] * 4 + [P, SZ, P]),
         "tadm_residual_norm": (I, [P] * 5 + [I] * 3 + [I64] * 4 + [P, P, I64, P, ctypes.c_float, ctypes.c_float] + [I] * 3 + [P]),
@@ -580,19 +581,38 @@ def _per_row(device, t, rows, kind, what):
     return t.data_ptr()
 
 
+def tadm_sample_scratch_size(rows: int, vocab: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().tadm_sample_scratch_size(rows, vocab, ctypes.byref(n)))
+    return n.value
+
+
+def _scratch_on(stream, nbytes: int):
+    """Scratch memory for work on `stream` (None: the current one), from torch's allocator."""
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
 def tadm_sample(logits, u, tok, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, mask_id: int = -1,
-                stream=None):
+                scratch=None, stream=None):
     """One token per row of logits [rows, vocab] (fp32 or bf16, rows may be strided) into tok (int32 [rows]), drawn with the
     row's temperature, top_k (int32), top_p and min_p (fp32 [rows] each, None: off) from its random number u (fp32
-    [rows], 0 <= u < 1); prob (fp32 [rows]) gets the token's probability among the ids kept."""
+    [rows], 0 <= u < 1); prob (fp32 [rows]) gets the token's probability among the ids kept.  scratch: a device buffer of
+    at least tadm_sample_scratch_size(rows, vocab) bytes; None: torch's allocator gives it for the call."""
     device = _device()
     dtype, ld = _matrix_of(device, logits, "logits")
     rows, vocab = logits.shape
+    if scratch is None and vocab > 4096:
+        scratch = _scratch_on(stream, tadm_sample_scratch_size(rows, vocab))
     status = load_library().tadm_sample(
         logits.data_ptr(), ld, rows, vocab, mask_id, _per_row(device, temperature, rows, 0, "temperature"),
         _per_row(device, top_k, rows, "int32", "top_k"), _per_row(device, top_p, rows, 0, "top_p"),
         _per_row(device, min_p, rows, 0, "min_p"), _per_row(device, u, rows, 0, "u"),
-        _per_row(device, tok, rows, "int32", "tok"), _per_row(device, prob, rows, 0, "prob"), dtype, _stream(stream))
+        _per_row(device, tok, rows, "int32", "tok"), _per_row(device, prob, rows, 0, "prob"), dtype,
+        *_scratch_of(device, scratch), _stream(stream))
     if status:
         _check(status)
 

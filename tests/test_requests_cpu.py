@@ -19,7 +19,7 @@ def T():
 
 
 SAMPLE = dict(logits=P, ld=1000, rows=4, vocab=1000, mask_id=-1, temperature=P, top_k=P, top_p=P, min_p=P, u=P, tok=P, prob=P,
-              dtype=0, stream=None)
+              dtype=0, scratch=None, scratch_bytes=0, stream=None)
 
 
 @pytest.mark.parametrize("over", [
@@ -34,9 +34,23 @@ def test_sample_refuses(T, over):
 def test_sample_sizes(T):
     f = T.load_library().tadm_sample
     assert f(*{**SAMPLE, "rows": 0, "logits": None, "u": None, "tok": None}.values()) == 0
-    big = 400001
+    big = (1 << 19) + 1
     assert f(*{**SAMPLE, "vocab": big, "ld": big}.values()) == UNSUPPORTED
-    assert f(*{**SAMPLE, "rows": (1 << 27) + 1}.values()) == UNSUPPORTED
+    assert f(*{**SAMPLE, "rows": (1 << 24) + 1}.values()) == UNSUPPORTED
+
+
+def test_sample_scratch(T):
+    size = T.tadm_sample_scratch_size
+    assert size(4, 4096) == 0 and size(0, 100000) == 0
+    need = size(4, 100000)
+    assert 0 < need <= size(5, 100000) and need <= size(4, 200000)
+    call = {**SAMPLE, "vocab": 100000, "ld": 100000, "scratch": P, "scratch_bytes": need}
+    for over in (dict(scratch=None), dict(scratch=P + 128), dict(scratch_bytes=need - 1)):
+        assert T.load_library().tadm_sample(*{**call, **over}.values()) == INVALID
+    n = ctypes.c_size_t()
+    for bad in ((-1, 100), (4, 0)):
+        assert T.load_library().tadm_sample_scratch_size(*bad, ctypes.byref(n)) == INVALID
+    assert T.load_library().tadm_sample_scratch_size(4, 100, None) == INVALID
 
 
 LORA = dict(x=P, w=P, y=P, cu=P, adapter=P, batch=3, total=10, n_in=64, n_out=40, ldx=64, ldw=64, ldy=40, a=P, b=P, scale=P,
@@ -113,7 +127,7 @@ def b16(*shape, device=0):
 
 def sample_args(**over):
     return {**dict(logits=f32(4, 100), u=f32(4), tok=ints(4), temperature=f32(4), top_k=ints(4), top_p=f32(4), min_p=f32(4),
-                   prob=f32(4)), **over}
+                   prob=f32(4), scratch=scratch()), **over}
 
 
 def lora_args(**over):

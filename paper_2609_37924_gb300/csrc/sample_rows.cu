@@ -74,6 +74,7 @@ struct RowPlan {
   float max, lo, hi;                       // the list: lo <= logit <= hi
   int mode, mj, listed;
   int more;                                // ids below lo may be kept, too
+  uint32_t low;                            // the least key that min-p keeps
   uint64_t target;
 };
 
@@ -183,20 +184,33 @@ struct Row {
   int k;
   float p, mp, t;
 };
-__device__ __forceinline__ Row row_of(const SampleArgs& a, int row, float* s_c) {
+__device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   Row r;
   r.t = a.temperature ? a.temperature[row] : 1.0f;
   r.p = a.top_p ? a.top_p[row] : 1.0f;
   r.mp = a.min_p ? a.min_p[row] : 0.0f;
   r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
   if (r.k < 0 || r.k >= a.vocab) r.k = 0;
-  if (threadIdx.x == 0) {                  // (double precision is slow here: one thread, for all)
-    const double c = 1.4426950408889634074 / static_cast<double>(r.t);
-    s_c[0] = static_cast<float>(c);
-    s_c[1] = static_cast<float>(c - static_cast<double>(s_c[0]));
-  }
+  constexpr double kLog2e = 1.4426950408889634074;
+  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
+  r.hi = L / r.t;
+  r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, r.t, L) + LL) / r.t : 0.0f;   // the division's remainder
   return r;
 }
+// f m rounded down (UP: up), for 0 <= f < 1: f's 24 bits times m's 64, shifted.
+template <bool UP>
+__device__ __forceinline__ uint64_t times(float f, uint64_t m) {
+  const uint32_t b = __float_as_uint(f), e = b >> 23;
+  const uint64_t mant = e ? (b & 0x7fffffu) | 0x800000u : b & 0x7fffffu;
+  const int down = 150 - static_cast<int>(e ? e : 1);         // f = mant 2^-down, down >= 24
+  const uint64_t lo = mant * m, hi = __umul64hi(mant, m);
+  if (down >= 128) return UP && mant != 0 && m != 0;
+  const uint64_t q = down >= 64 ? hi >> (down - 64) : (hi << (64 - down)) | (lo >> down);
+  const bool rest = down >= 64 ? lo != 0 || (down > 64 && hi << (128 - down) != 0) : lo << (64 - down) != 0;
+  return q + (UP && rest);
+}
+// Which part of `mass` is kept: at least a unit, at most all of it.
+__device__ __forceinline__ uint64_t target_of(float p, uint64_t mass) { return min(max(times<true>(p, mass), static_cast<uint64_t>(1)), mass); }
 // Ids of less than 2^-depth of the maximum are of no account: too light for a nucleus (those that weigh less than
 // (1 - p) / vocab together weigh less than 1 - p of the mass), or for any draw.
 __device__ __forceinline__ float depth_of(const SampleArgs& a, const Row& r) {
@@ -359,7 +373,7 @@ template <class T>
 __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) {
   __shared__ uint32_t s_hist[NB];
   __shared__ float2 s_pow[16];
-  __shared__ float s_max[NW], s_c[2];
+  __shared__ float s_max[NW];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
   if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow2[threadIdx.x];
   s_hist[threadIdx.x] = 0;
@@ -367,7 +381,7 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
   const Logits<T> l(a, row);
   float v[PER];
   load_chunk(l, chunk * CHUNK + warp * SEG, v);
-  Row r = row_of(a, row, s_c);
+  const Row r = row_of(a, row);
   float top = v[0];
 #pragma unroll
   for (int e = 1; e < PER; ++e) top = fmaxf(top, v[e]);
@@ -375,7 +389,6 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
-  r.hi = s_c[0], r.lo = s_c[1];
   const float per = r.hi * ((NB - 2) / depth_of(a, r));
   const float ninf = __int_as_float(0xff800000);
   ChunkInfo info{top, 0, 0, 0};
@@ -410,26 +423,39 @@ __device__ __forceinline__ uint64_t rescale(uint64_t sum, int from, int to) {
   return (hi << (64 - down)) | (lo >> down);
 }
 
+// The least key whose weight is at least min-p of the maximum's.  Warp-collective.
+template <class T>
+__device__ __forceinline__ uint32_t low_key(const Row& r, const Scale& s, const uint64_t* pow, float max) {
+  const uint32_t top = Key<T>::of(max), bottom = Key<T>::of(__int_as_float(0xff800000)) + 1;
+  if (!(r.mp > 0.0f)) return bottom;
+  if (r.mp >= 1.0f || !(max < __int_as_float(0x7f800000))) return top;
+  const uint64_t least = ::max(times<true>(r.mp, weight(s, pow, max)), static_cast<uint64_t>(1));
+  return first_key(bottom, top, [&](uint32_t key) { return weight(s, pow, Key<T>::value(key)) >= least; });
+}
+
 template <class T>
 __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
   __shared__ uint64_t s_room[NW];
-  __shared__ float s_max[NW], s_c[2];
-  __shared__ int s_bin, s_low;
-  __shared__ uint64_t s_front;
+  __shared__ float s_max[NW];
+  __shared__ int s_bin, s_three;
+  __shared__ float s_part;
+  __shared__ uint64_t s_front, s_pow[16];
+  __shared__ ChunkInfo s_info[(kSampleMaxVocab + CHUNK - 1) / CHUNK];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
-  if (threadIdx.x == 0) s_bin = NB, s_low = NB;
+  if (threadIdx.x == 0) s_bin = NB, s_three = 0;
+  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow[threadIdx.x];
   pdl_enter();
-  Row r = row_of(a, row, s_c);
+  const Row r = row_of(a, row);
   const ChunkInfo* info = a.info + static_cast<int64_t>(row) * a.chunks;
   uint64_t* seg = a.seg + static_cast<int64_t>(row) * a.chunks * NW;
   const float ninf = __int_as_float(0xff800000);
   const ChunkInfo mine = threadIdx.x < a.chunks ? info[threadIdx.x] : ChunkInfo{ninf, 0, 0, 0};   // (a row has fewer chunks than threads)
+  if (threadIdx.x < a.chunks) s_info[threadIdx.x] = mine;
   float top = warp_max(mine.max);
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
-  r.hi = s_c[0], r.lo = s_c[1];
-  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0};
+  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0, 0};
   const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {
     plan.mode = kListed;                                      // the ids of the maximum
@@ -447,7 +473,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
     if (wants_mass(r)) {
       uint64_t own = 0;
       for (int i = threadIdx.x; i < a.chunks * NW; i += NT) {
-        const ChunkInfo c = info[i / NW];
+        const ChunkInfo c = s_info[i / NW];
         const uint64_t x = c.max > ninf && !c.far ? rescale(seg[i], c.mj, mj) : 0;
         seg[i] = x;
         own += x;
@@ -455,13 +481,15 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
       scan_block(own, s_room, &mass);
       __syncthreads();
     }
+    plan.low = low_key<T>(r, Scale(r.hi, r.lo, mj, 0.0f), s_pow, top);
     plan.mode = kAll;
     plan.lo = ninf, plan.hi = -ninf;
     if (wants_bins(r)) {
       // a bin per thread: its number of ids, about, and its mass in 2^-32
       uint64_t n = 0;
+#pragma unroll 4
       for (int c = 0; c < a.chunks; ++c) {
-        const ChunkInfo x = info[c];
+        const ChunkInfo x = s_info[c];
         const int bin = static_cast<int>(threadIdx.x) - (gj - x.gj);
         if (x.max > ninf && !x.far && bin >= 0 && bin < NB) n += a.hist[(static_cast<int64_t>(row) * a.chunks + c) * NB + bin];
       }
@@ -472,23 +500,30 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
       if (r.k > 1) {
         if (in_front >= static_cast<uint64_t>(r.k) && in_front - count < static_cast<uint64_t>(r.k)) s_bin = threadIdx.x;
       } else if (r.p < 1.0f && r.mp <= 0.0f) {
-        plan.target = min(max(static_cast<uint64_t>(ceil(static_cast<double>(r.p) * static_cast<double>(mass))), static_cast<uint64_t>(1)), mass);
+        plan.target = target_of(r.p, mass);
         const float mid = ex2_approx(fmaf(edge(static_cast<float>(threadIdx.x)), r.hi, -0.0625f * static_cast<float>(mj))) * 262144.0f;
         const uint64_t guess = static_cast<uint64_t>(static_cast<float>(n) * mid), incl = scan_block(guess, s_room);
-        if (incl >= plan.target >> 12 && incl - guess < plan.target >> 12) s_bin = threadIdx.x;
+        if (incl >= plan.target >> 12 && incl - guess < plan.target >> 12) {
+          s_bin = threadIdx.x;
+          s_part = static_cast<float>((plan.target >> 12) - (incl - guess)) / static_cast<float>(guess);
+        }
       }
       float lo = ninf;
-      if (r.mp > 0.0f) {                                      // the least logit that min-p keeps, rounded up
-        const double x = r.mp >= 1.0f ? 0.0 : static_cast<double>(r.t) * log(static_cast<double>(r.mp));
-        lo = fminf(__double2float_ru(static_cast<double>(top) + x), top) + 0.0f;
-      }
+      if (r.mp > 0.0f) lo = Key<T>::value(plan.low);
       __syncthreads();
       b = s_bin;
       plan.mode = kListed;
-      if (b < NB - 2) {
+      if (b < NB - 2 && r.k > 0) {
         plan.more = edge(b + 1.5f) > lo;
         lo = fmaxf(lo, edge(b + 1.5f));
-        if (r.k == 0) plan.hi = edge(b - 1.5f);
+      } else if (b < NB - 2) {
+        // three bins, or as many as the list takes around the place within the bin (the guess is good to a hundredth of one)
+        if (threadIdx.x == max(0, b - 1) || threadIdx.x == b || threadIdx.x == b + 1) atomicAdd(&s_three, static_cast<int>(min(count, static_cast<uint64_t>(1 << 24))));
+        __syncthreads();
+        const float most = CAP * 0.6f, three = static_cast<float>(s_three);
+        const float half = three <= most ? 1.5f : fmaxf(0.05f, 1.5f * most / three), mid = three <= most ? b : b - 0.5f + s_part;
+        lo = edge(mid + half);
+        plan.hi = edge(mid - half);
       } else if (r.k == 0 && r.mp <= 0.0f) {
         plan.mode = kWhole;
       } else {
@@ -522,7 +557,6 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
 template <class T>
 __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs a) {
   __shared__ float2 s_pow[16];
-  __shared__ float s_c[2];
   __shared__ int s_n, s_at;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
   if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow2[threadIdx.x];
@@ -540,7 +574,7 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   const int base = chunk * CHUNK + warp * SEG;
   float v[PER];
   load_chunk(l, base, v);
-  Row r = row_of(a, row, s_c);
+  const Row r = row_of(a, row);
   uint32_t in = 0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) in |= v[e] >= plan.lo && v[e] <= plan.hi ? 1u << e : 0u;
@@ -573,7 +607,7 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
       }
   }
   if (above) {
-    const Scale s(s_c[0], s_c[1], plan.mj, 0.0f);
+    const Scale s(r.hi, r.lo, plan.mj, 0.0f);
     const uint64_t sum = bulk<false>(v, s, s_pow, plan.max, plan.hi, 0.0f, 0, nullptr);
     if (lane == 0) *seg = sum;
   }
@@ -588,12 +622,19 @@ constexpr int ALL = 0x7fffffff;
 
 struct Finish {
   uint64_t pow[16];
-  uint64_t mass[NB], seg[(SEGS + NT - 1) / NT * NT], room[NW];
+  // mass by bin: whole rows 64 bits; lists, whose counts allow it, three words of 16 bits' sums (64-bit additions to shared
+  // memory are loops)
+  union {
+    uint64_t mass[NB];
+    uint32_t mass3[3][NB];
+  };
+  uint64_t seg[(SEGS + NT - 1) / NT * NT], room[NW];
+  uint32_t seg2[2][(SEGS + NT - 1) / NT * NT];                // of lists: 22 bits, and the others
   uint64_t all_w[LIST];
   uint32_t count[NB];
   uint32_t key[CAP], id[CAP];
   uint32_t few_key[LIST], few_id[LIST];
-  float max[NW], c[2];
+  float max[NW];
   int n, few;
   // what one thread decides
   uint64_t d_above, d_left, d_w, d_best;
@@ -645,7 +686,8 @@ struct Finisher {
     bool by_value = hi == Key<T>::of(max); // first by value, in steps of equal ratios of weights; then by key
     while (lo < hi && inside > LIST) {
       sh.count[threadIdx.x] = 0;
-      sh.mass[threadIdx.x] = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) sh.mass3[i][threadIdx.x] = 0;
       if (threadIdx.x == 0) sh.d_count = 0;
       __syncthreads();
       const float range = max - Key<T>::value(lo);
@@ -658,10 +700,23 @@ struct Finisher {
         if (key < lo || key > hi || !kept(from, key, id)) return;
         const int bin = by_value ? value_bin(key) : static_cast<int>((hi - key) >> shift);
         atomicAdd(&sh.count[bin], 1u);
-        if (BY_MASS) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[bin]), static_cast<unsigned long long>(w(Key<T>::value(key))));
+        if (BY_MASS) {
+          const uint64_t x = w(Key<T>::value(key));
+          if (whole) {
+            atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[bin]), static_cast<unsigned long long>(x));
+          } else {
+            atomicAdd(&sh.mass3[0][bin], static_cast<uint32_t>(x) & 0xffffu);
+            atomicAdd(&sh.mass3[1][bin], static_cast<uint32_t>(x >> 16) & 0xffffu);
+            atomicAdd(&sh.mass3[2][bin], static_cast<uint32_t>(x >> 32));
+          }
+        }
       });
       __syncthreads();
-      const uint64_t own = BY_MASS ? sh.mass[threadIdx.x] : sh.count[threadIdx.x], incl = scan_block(own, sh.room);
+      uint64_t own = sh.count[threadIdx.x];
+      if (BY_MASS)
+        own = whole ? sh.mass[threadIdx.x]
+                    : sh.mass3[0][threadIdx.x] + (static_cast<uint64_t>(sh.mass3[1][threadIdx.x]) << 16) + (static_cast<uint64_t>(sh.mass3[2][threadIdx.x]) << 32);
+      const uint64_t incl = scan_block(own, sh.room);
       if (above + incl >= target && above + incl - own < target) {
         sh.d_bin = threadIdx.x;
         sh.d_count = sh.count[threadIdx.x];
@@ -766,7 +821,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
   if (threadIdx.x == 0) sh.n = 0;
   pdl_enter();
   const Logits<T> l(a, row);
-  Row r = row_of(a, row, sh.c);
+  const Row r = row_of(a, row);
   const float u = a.u[row];
   RowPlan plan;
   if constexpr (DIRECT) {
@@ -784,8 +839,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
         sh.id[i] = id;
       }
     }
-    const int mj = mj_of(sh.c[0], sh.c[1], top);
-    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, sh.c[0] > 1e-30f ? mj : kFar, 0, 0, 0};
+    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0};
   } else {
     plan = a.plan[row];
     const uint2* list = a.list + static_cast<int64_t>(row) * CAP;
@@ -808,7 +862,6 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
     }
     return;
   }
-  r.hi = sh.c[0], r.lo = sh.c[1];
   const bool far = plan.mj == kFar;
   Finisher<T> f{sh, l, Scale(r.hi, r.lo, far ? 0 : plan.mj, far ? plan.max : 0.0f), plan.max, plan.mode == kWhole};
   const uint32_t khi = Key<T>::of(plan.max), kinf = Key<T>::of(ninf) + 1;
@@ -834,13 +887,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
     for (int i = threadIdx.x; i < segs; i += NT) own += seg[i];
     above = f.sum(own);
   }
-  Cut low{kinf, ALL};
-  if (r.mp > 0.0f) {                       // the least logit that min-p keeps, rounded up
-    const double x = r.mp >= 1.0f ? 0.0 : static_cast<double>(r.t) * log(static_cast<double>(r.mp));
-    const float least = fminf(__double2float_ru(static_cast<double>(plan.max) + x), plan.max) + 0.0f;
-    const uint32_t key = Key<T>::of(least);
-    low.key = ::max(low.key, Key<T>::value(key) < least ? key + 1 : key);
-  }
+  const Cut low{DIRECT || far || plan.mode == kWhole ? low_key<T>(r, f.s, sh.pow, plan.max) : ::max(plan.low, kinf), ALL};
   Cut cut = low;
   bool window = plan.mode == kWindow;
   if (plan.mode != kAll) {
@@ -864,7 +911,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
             uint64_t own = 0;
             f.each([&](uint32_t key, int id) { own += f.kept(cut, key, id) ? f.w(Key<T>::value(key)) : 0; });
             const uint64_t mass = f.sum(own);
-            target = min(::max(static_cast<uint64_t>(ceil(static_cast<double>(r.p) * static_cast<double>(mass))), static_cast<uint64_t>(1)), mass);
+            target = target_of(r.p, mass);
           }
           uint32_t lo = cut.key;
           if (r.hi > 1e-30f) lo = ::max(lo, Key<T>::of(plan.max - 46.0f / r.hi));
@@ -880,7 +927,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
   }
   // ---- the draw: the masses of 512 ids each
   for (int i = threadIdx.x; i < static_cast<int>(sizeof(sh.seg) / 8); i += NT)
-    sh.seg[i] = !DIRECT && (window || plan.mode == kAll) && i < segs ? seg[i] : 0;
+    sh.seg[i] = !DIRECT && (window || plan.mode == kAll) && i < segs ? seg[i] : 0, sh.seg2[0][i] = sh.seg2[1][i] = 0;
   __syncthreads();
   if (f.whole) {
     constexpr int N = Vec<T>::N;
@@ -898,18 +945,23 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
     }
   } else if (plan.mode != kAll) {
     f.each([&](uint32_t key, int id) {
-      if (f.kept(cut, key, id))
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.seg[id / SEG]), static_cast<unsigned long long>(f.w(Key<T>::value(key))));
+      if (!f.kept(cut, key, id)) return;
+      const uint64_t x = f.w(Key<T>::value(key));
+      atomicAdd(&sh.seg2[0][id / SEG], static_cast<uint32_t>(x) & 0x3fffffu);
+      atomicAdd(&sh.seg2[1][id / SEG], static_cast<uint32_t>(x >> 22));
     });
   }
   __syncthreads();
   constexpr int EACH = (SEGS + NT - 1) / NT;                  // a thread's segments
   uint64_t own = 0, mass;
 #pragma unroll
-  for (int i = 0; i < EACH; ++i) own += sh.seg[threadIdx.x * EACH + i];
+  for (int i = 0; i < EACH; ++i) {
+    const int at = threadIdx.x * EACH + i;
+    sh.seg[at] += sh.seg2[0][at] + (static_cast<uint64_t>(sh.seg2[1][at]) << 22);
+    own += sh.seg[at];
+  }
   const uint64_t incl = scan_block(own, sh.room, &mass);
-  const double at = (u > 0.0f ? static_cast<double>(u) : 0.0) * static_cast<double>(mass);
-  const uint64_t target = at >= static_cast<double>(mass) ? mass - 1 : min(mass - 1, static_cast<uint64_t>(at));
+  const uint64_t target = u >= 1.0f ? mass - 1 : min(mass - 1, times<false>(u > 0.0f ? u : 0.0f, mass));
   if (incl > target && incl - own <= target) {
     uint64_t left = target - (incl - own);
     int i = 0;

@@ -27,6 +27,12 @@ struct NormArgs {
   float alpha, eps;
 };
 
+// `bytes` (a multiple of 16) of global memory into shared memory, counted on the mbarrier
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+               "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
 // eight consecutive elements, 16-byte aligned
 __device__ __forceinline__ void ld8(const float* p, float (&v)[8]) {
   const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
@@ -143,6 +149,101 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) norm_reg_kernel(const Norm
   }
 }
 
+// Many rows: blocks that stay, each with the rows of its next RING turns on the way into shared memory by bulk copies, so
+// that the loads go on while a row waits for its sums.  (11512 rows of 5376, fp32 x and bf16 y: a block per row, which loads,
+// sums, and stores one after the other, 157 us.)
+constexpr int RT = 256, RING = 3, kRingBytes = 112 * 1024;   // two blocks an SM
+template <class XT, class YT>
+__host__ __device__ constexpr int ring_stage(int d) { return d * static_cast<int>(sizeof(XT) + sizeof(YT)); }
+
+template <class XT, class YT, class T, int NV>
+__global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ float red[2][32];
+  __shared__ __align__(8) uint64_t full[RING];
+  const int nvec = a.d / 8, stage_bytes = ring_stage<XT, YT>(a.d), step = gridDim.x;
+  const uint32_t xb = a.d * sizeof(XT), yb = a.d * sizeof(YT);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < RING; ++i) mbar_init(&full[i], 1);
+    fence_mbar_init();
+  }
+  __syncthreads();
+  pdl_enter();
+  auto ask = [&](int row, int i) {         // thread 0
+    uint8_t* to = smem + i * stage_bytes;
+    mbar_arrive_expect_tx(&full[i], xb + yb);
+    bulk_load(to, static_cast<const XT*>(a.x) + row * a.ldx, xb, &full[i]);
+    bulk_load(to + xb, static_cast<const YT*>(a.y) + row * a.ldy, yb, &full[i]);
+  };
+  if (threadIdx.x == 0)
+    for (int i = 0; i < RING; ++i)
+      if (static_cast<int>(blockIdx.x) + i * step < a.total) ask(blockIdx.x + i * step, i);
+  const T *post = static_cast<const T*>(a.post), *pre = static_cast<const T*>(a.pre), *gate = static_cast<const T*>(a.gate);
+  int stage = 0;
+  uint32_t phase = 0;
+  for (int row = blockIdx.x; row < a.total; row += step) {
+    const int b = a.cu ? seq_of_row(a.cu, a.batch, row) : 0;
+    while (!mbar_try_wait_suspend(&full[stage], phase, 1000000u)) {}        // (a copy that was asked for arrives)
+    const XT* x = reinterpret_cast<const XT*>(smem + stage * stage_bytes);
+    const YT* y = reinterpret_cast<const YT*>(smem + stage * stage_bytes + xb);
+    float v[NV][8], w[8];
+    float r = 1.0f, s = 0.0f;
+    if (post) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = threadIdx.x + i * RT;
+        if (c < nvec) {
+          ld8(y + 8 * c, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s = fmaf(w[e], w[e], s);
+        }
+      }
+      r = rsqrtf(row_sum<true>(s, red[0]) / static_cast<float>(a.d) + a.eps);
+      s = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = threadIdx.x + i * RT;
+      if (c < nvec) {
+        float u[8];
+        ld8(y + 8 * c, u);
+        ld8(x + 8 * c, v[i]);
+        if (post) {
+          ld8(post + 8 * c, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) u[e] = u[e] * r * w[e];
+        }
+        if (gate && b >= 0) {
+          ld8(gate + b * a.ldg + 8 * c, w);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) u[e] *= w[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[i][e] = fmaf(a.alpha, v[i][e], u[e]);
+          s = fmaf(v[i][e], v[i][e], s);
+        }
+      }
+    }
+    const float q = rsqrtf(row_sum<true>(s, red[1]) / static_cast<float>(a.d) + a.eps);   // (its barrier: the stage has been read)
+    if (threadIdx.x == 0 && row + RING * step < a.total) ask(row + RING * step, stage);
+    if (++stage == RING) { stage = 0; phase ^= 1; }
+    if (b < 0) continue;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = threadIdx.x + i * RT;
+      if (c < nvec) {
+        st8(static_cast<XT*>(a.xo) + row * a.ldxo + 8 * c, v[i]);
+        if (!a.no) continue;
+        if (pre) ld8(pre + 8 * c, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = pre ? v[i][e] * q * w[e] : v[i][e] * q;
+        st8(static_cast<T*>(a.no) + row * a.ldn + 8 * c, v[i]);
+      }
+    }
+  }
+}
+
 // Any width, stride and alignment: a row per block, x' in shared memory.
 template <class XT, class YT, class T>
 __global__ void __launch_bounds__(512) norm_any_kernel(const NormArgs a) {
@@ -180,9 +281,30 @@ __global__ void __launch_bounds__(512) norm_any_kernel(const NormArgs a) {
   }
 }
 
+template <class XT, class YT, class T, int NV>
+cudaError_t launch_ring(const NormArgs& a, int dev, int sms, cudaStream_t s) {
+  static PerDevice ready;
+  cudaError_t e = cudaSuccess;
+  if (ready.get(dev, [&] {
+        e = cudaFuncSetAttribute(norm_ring_kernel<XT, YT, T, NV>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+        return e == cudaSuccess ? 1 : 0;
+      }) <= 0)
+    return e;
+  return launch_pdl(norm_ring_kernel<XT, YT, T, NV>, 2 * sms, RT, RING * ring_stage<XT, YT>(a.d), s, a);
+}
+
 template <class XT, class YT, class T>
 cudaError_t launch(const NormArgs& a, bool vec, cudaStream_t s) {
   const int nvec = a.d / 8;
+  int dev = 0;
+  const int sms = current_sms(&dev);
+  // rows enough for a few turns of every block, and wide enough for a block (narrow ones: a warp each, many at once)
+  if (vec && nvec > 128 && a.total >= 8 * sms && RING * ring_stage<XT, YT>(a.d) <= kRingBytes) {
+    if (nvec <= RT) return launch_ring<XT, YT, T, 1>(a, dev, sms, s);
+    if (nvec <= 2 * RT) return launch_ring<XT, YT, T, 2>(a, dev, sms, s);
+    if (nvec <= 3 * RT) return launch_ring<XT, YT, T, 3>(a, dev, sms, s);
+    return launch_ring<XT, YT, T, 6>(a, dev, sms, s);
+  }
   if (vec && nvec <= 128) {
     const int rows = 8, grid = (a.total + rows - 1) / rows;
     if (nvec <= 32) return launch_pdl(norm_reg_kernel<XT, YT, T, 1, false>, grid, 32 * rows, 0, s, a);
@@ -195,8 +317,6 @@ cudaError_t launch(const NormArgs& a, bool vec, cudaStream_t s) {
     return launch_pdl(norm_reg_kernel<XT, YT, T, 2, true>, a.total, two, 0, s, a);
   }
   static PerDevice ready;
-  int dev = 0;
-  cudaGetDevice(&dev);
   cudaError_t e = cudaSuccess;
   if (ready.get(dev, [&] {
         e = cudaFuncSetAttribute(norm_any_kernel<XT, YT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormMaxWidth * 4);

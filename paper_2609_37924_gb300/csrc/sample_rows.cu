@@ -145,12 +145,13 @@ struct Logits {
     for (int e = 0; e < V::N; ++e) v[e] = id + e < vocab ? p[id + e] : from_f32<T>(__int_as_float(0xff800000));
     return *reinterpret_cast<const uint4*>(v);
   }
+  template <bool ZERO = true>              // false: -0 stays
   __device__ __forceinline__ void get(const uint4& q, int id, float* v) const {
     const float ninf = __int_as_float(0xff800000);
     float x[V::N];
     V::get(q, x);
 #pragma unroll
-    for (int e = 0; e < V::N; ++e) v[e] = fmaxf(x[e] + 0.0f, ninf);
+    for (int e = 0; e < V::N; ++e) v[e] = fmaxf(ZERO ? x[e] + 0.0f : x[e], ninf);
     if (static_cast<uint32_t>(mask_id - id) < V::N) {
 #pragma unroll
       for (int e = 0; e < V::N; ++e)
@@ -160,17 +161,17 @@ struct Logits {
 };
 
 // ------------------------------------------------------------------ weights
-// 2^(j/16) in units of 2^-43, rounded, and in two fp32 terms
+// 2^(j/16) in units of 2^-43, rounded; and over 1 + j/16 in fp32, with what the product of the two leaves over itself
 __constant__ const uint64_t kPow[16] = {
     0x80000000000ull, 0x85aac367cc5ull, 0x8b95c1e3ea9ull, 0x91c3d373ab1ull,
     0x9837f0518dcull, 0x9ef5326091aull, 0xa5fed6a9b15ull, 0xad583eea42aull,
     0xb504f333f9eull, 0xbd08a39f581ull, 0xc5672a11550ull, 0xce248c151f8ull,
     0xd744fccad6aull, 0xe0ccdeec2a9ull, 0xeac0c6e7dd2ull, 0xf5257d15248ull};
-__constant__ const float2 kPow2[16] = {
-    {1.0f, 0.0f}, {1.04427373f, 4.83347016e-08f}, {1.09050775f, -1.30775399e-08f}, {1.13878858f, 5.38622231e-08f},
-    {1.18920708f, 3.79763527e-08f}, {1.24185777f, 4.4968381e-08f}, {1.29683959f, -4.01899953e-08f}, {1.35425556f, -1.01233493e-08f},
-    {1.41421354f, 2.4203235e-08f}, {1.47682619f, -4.50089885e-08f}, {1.54221082f, 8.07090483e-09f}, {1.61049032f, 9.83621717e-09f},
-    {1.68179286f, -2.47553267e-08f}, {1.75625217f, -9.23577037e-09f}, {1.8340081f, -1.1239278e-08f}, {1.91520655f, 9.84532811e-09f}};
+__constant__ const float2 kPowF[16] = {
+    {1.0f, 0.0f}, {0.982845902f, 4.62854715e-08f}, {0.969340205f, -1.19921575e-08f}, {0.958979905f, 4.72978243e-08f},
+    {0.951365709f, 3.19341815e-08f}, {0.946177363f, 3.62105723e-08f}, {0.943156064f, -3.09907193e-08f}, {0.942090809f, -7.47521334e-09f},
+    {0.942809045f, 1.71142709e-08f}, {0.945168734f, -3.04768335e-08f}, {0.949052811f, 5.23333421e-09f}, {0.954364657f, 6.10759177e-09f},
+    {0.961024463f, -1.47196051e-08f}, {0.968966722f, -5.25879518e-09f}, {0.978137672f, -6.12825968e-09f}, {0.988493681f, 5.14060927e-09f}};
 // 2^f - 1 = f (A1 + f (A2 + f (A3 + f A4))) for |f| <= 1/32: ln2^n / n!, eased so that the neglected terms spread (Chebyshev); error
 // 2^-37
 constexpr float A1 = 0.693147182f, A2 = 0.240226507f, A3 = 0.0555057377f, A4 = 0.00961835496f;
@@ -245,68 +246,52 @@ __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, 
   return down <= 0 ? w << -down : (w + (1ull << (down - 1))) >> down;
 }
 
-__device__ __forceinline__ uint64_t pair(float x) { return f2_pack(x, x); }
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
+// Adds to a word of shared memory.
+__device__ __forceinline__ void add_shared(uint32_t at, uint32_t x) { asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory"); }
 
-// Sum of the weights of the values above `cut` (exclusive) that a warp's lanes hold, in units of 2^-44, in every lane.  The
-// same arithmetic as weight()'s, two values at a time, with the table in two fp32 terms.  A weight is split at 2^-17:
-// multiples of that add without rounding, the rest carries errors of about 2^-37 a lane.
+// Sum of the weights of the values that a warp's lanes hold, in units of 2^-44, in every lane; CUT: of those above `cut`
+// (exclusive).  weight()'s arithmetic, with the table's rest added to 2^f - 1: a weight is a + a r, a in fp32, r good to
+// 2^-30; h the sum's rounding, l what that lost.  The sum of h begins at 96, so that what its roundings (2^-17) lose is
+// had by two subtractions; the lost parts' sum carries errors of about 2^-38 a lane.
 // BINS: also a histogram by value, bins counted down from gj / per; a value adds its weight over that of its bin's
-// middle, linear in its place within the bin, in 2^-14.
-template <bool BINS>
+// middle, linear in its place within the bin, in 2^-14.  NB words, and 32 for what lies past them.
+template <bool CUT, bool BINS>
 __device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, const float2* pow, float max, float cut, float per, int gj,
-                                         uint32_t* hist) {
-  const float none = fmaxf(max - 60.0f / s.hi, -3.0e38f);     // stands for values that are not summed: 2^-60
-  cut = fmaxf(cut, none);
-  const uint64_t k_hi16 = pair(s.hi16), k_c = pair(s.k_c), k_back = pair(-kMagic);
-  const uint64_t k_n16 = pair(-0.0625f), k_nmh = pair(-s.mh), k_hi = pair(s.hi), k_lo = pair(s.lo), k_minus = pair(-1.0f);
-  const uint64_t k_up = pair(96.0f), k_down = pair(-96.0f);
-  const uint64_t a1 = pair(A1), a2 = pair(A2), a3 = pair(A3), a4 = pair(A4);
-  const uint64_t b_per = pair(-per), b_c = pair(kMagic + static_cast<float>(gj)), b_slope = pair(-16384.0f * 0.693147181f * s.hi / per);
-  const uint64_t b_one = pair(kMagic + 16384.0f);
-  uint64_t big = 0, small = 0;
+                                         uint32_t hist) {
+  const float none = fmaxf(max - 60.0f / s.hi, -3.0e38f);     // stands for values that are not summed: 2^-60, in no bin
+  if (CUT) cut = fmaxf(cut, none);
+  const float back = kMagic * 0.0625f - s.mh;
+  const float b_c = kMagic + static_cast<float>(gj), b_slope = -16384.0f * 0.693147181f * s.hi / per;
+  const uint32_t past = hist + 4u * (NB + (threadIdx.x & 31));   // (a word per lane: no branch, no conflicts)
+  hist -= 4u * static_cast<uint32_t>(kMagicBits);
+  float big = 96.0f, small = 0.0f;
 #pragma unroll
-  for (int e = 0; e < PER; e += 2) {
-    const float v0 = v[e], v1 = v[e + 1];
-    const bool in0 = v0 > cut, in1 = v1 > cut;
-    const uint64_t x = f2_pack(in0 ? v0 : none, in1 ? v1 : none);
+  for (int e = 0; e < PER; ++e) {
+    const float x = CUT ? (v[e] > cut ? v[e] : none) : fmaxf(v[e], none);
     if constexpr (BINS) {
-      const uint64_t q = f2_fma(x, b_per, b_c), d = f2_fma(x, b_per, f2_fma(q, k_minus, b_c));   // d: from the bin's middle, in bins
-      float q0, q1, m0, m1;
-      f2_unpack(q, q0, q1);
-      f2_unpack(f2_fma(d, b_slope, b_one), m0, m1);
-      const uint32_t i0 = __float_as_uint(q0) - kMagicBits, i1 = __float_as_uint(q1) - kMagicBits;
-      if (in0 && i0 < NB) atomicAdd(&hist[i0], __float_as_uint(m0) - kMagicBits);
-      if (in1 && i1 < NB) atomicAdd(&hist[i1], __float_as_uint(m1) - kMagicBits);
+      const float q = fmaf(x, -per, b_c), d = fmaf(x, -per, b_c - q);       // d: from the bin's middle, in bins
+      const uint32_t at = hist + 4u * __float_as_uint(q);
+      add_shared(q < kMagic + NB ? at : past, __float_as_uint(fmaf(d, b_slope, kMagic + 16384.0f)) - kMagicBits);
     }
-    const uint64_t q = f2_fma(x, k_hi16, k_c), j = f2_add(q, k_back);
-    const uint64_t g = f2_fma(x, k_lo, f2_fma(x, k_hi, f2_fma(j, k_n16, k_nmh)));
-    const uint64_t r = f2_mul(g, f2_fma(g, f2_fma(g, f2_fma(g, a4, a3), a2), a1));
-    float q0, q1;
-    f2_unpack(q, q0, q1);
-    const uint32_t b0 = __float_as_uint(q0), b1 = __float_as_uint(q1);
-    const float2 t0 = pow[b0 & 15], t1 = pow[b1 & 15];
-    // 2^n, n = floor(j / 16): the magic number's bits drop out of the shifted word
-    constexpr uint32_t BIAS = (127u << 23) - (static_cast<uint32_t>(kMagicBits) >> 4 << 23);
-    const uint64_t p2 = f2_pack(__uint_as_float((b0 >> 4 << 23) + BIAS), __uint_as_float((b1 >> 4 << 23) + BIAS));
-    const uint64_t a = f2_mul(f2_pack(t0.x, t1.x), p2), al = f2_mul(f2_pack(t0.y, t1.y), p2);
-    const uint64_t t = f2_fma(a, r, al), h = f2_add(a, t), l = f2_add(f2_fma(h, k_minus, a), t);
-    const uint64_t up = f2_add(f2_add(h, k_up), k_down);
-    big = f2_add(big, up);
-    small = f2_add(small, f2_add(f2_fma(up, k_minus, h), l));
+    const float q = fmaf(x, s.hi16, s.k_c);
+    const uint32_t b = __float_as_uint(q);
+    const float g = fmaf(x, s.lo, fmaf(x, s.hi, fmaf(q, -0.0625f, back)));
+    const float2 t = pow[b & 15];
+    const float r = fmaf(g, fmaf(g, fmaf(g, fmaf(g, A4, A3), A2), A1), t.y);
+    // 2^n (1 + i/16), j = 16 n + i: j with its last four bits at the top of the fraction (the magic number's drop out)
+    const float a = __uint_as_float(b * (1u << 19) + ((127u << 23) - (static_cast<uint32_t>(kMagicBits) << 19))) * t.x;
+    const float h = fmaf(a, r, a), l = fmaf(a, r, a - h);
+    const float next = big + h;
+    small += (h - (next - big)) + l;
+    big = next;
   }
-  float h0, h1, l0, l1;
-  f2_unpack(big, h0, h1);
-  f2_unpack(small, l0, l1);
-  const int64_t whole = static_cast<int64_t>(__float2int_rn((h0 + h1) * 131072.0f)) << 27;
-  uint64_t sum = static_cast<uint64_t>(whole + __float2ll_rn((l0 + l1) * 17592186044416.0f));
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum;
+  // 16 weights of up to 1.03 a lane in units of 2^-17: 2^26 over the warp; the rest 2^30 a lane
+  const uint32_t whole = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(__float2int_rn((big - 96.0f) * 131072.0f)));
+  const int rest = __float2int_rn(small * 17592186044416.0f);
+  const int high = __reduce_add_sync(0xffffffffu, rest >> 16);
+  const uint32_t low = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(rest) & 0xffffu);
+  const int64_t sum = (static_cast<int64_t>(whole) << 27) + (static_cast<int64_t>(high) << 16) + low;
+  return sum > 0 ? static_cast<uint64_t>(sum) : 0;
 }
 // the largest logit below `v`
 __device__ __forceinline__ float below(float v) { return v == 0.0f ? -1.4e-45f : Key<float>::value(Key<float>::of(v) - 1); }
@@ -361,21 +346,40 @@ __device__ __forceinline__ void load_chunk(const Logits<T>& l, int base, float (
   constexpr int N = Vec<T>::N;
   const int lane = threadIdx.x & 31;
   uint4 q[PER / N];
+  if (l.vec && base + SEG <= l.vocab && static_cast<uint32_t>(l.mask_id - base) >= SEG) {   // a whole segment, nothing masked in it
+    const uint4* p = reinterpret_cast<const uint4*>(l.p + base) + lane;
 #pragma unroll
-  for (int i = 0; i < PER / N; ++i) q[i] = l.load(base + (i * 32 + lane) * N);
+    for (int i = 0; i < PER / N; ++i) q[i] = __ldg(p + i * 32);
 #pragma unroll
-  for (int i = 0; i < PER / N; ++i) l.get(q[i], base + (i * 32 + lane) * N, &v[i * N]);
+    for (int i = 0; i < PER / N; ++i) {
+      float x[N];
+      Vec<T>::get(q[i], x);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[i * N + e] = fmaxf(x[e], __int_as_float(0xff800000));
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < PER / N; ++i) {
+      float x[N];
+      l.template get<false>(l.load(base + (i * 32 + lane) * N), base + (i * 32 + lane) * N, x);
+#pragma unroll
+      for (int k = 0; k < PER / N; ++k)
+        if (k == i)
+#pragma unroll
+          for (int e = 0; e < N; ++e) v[k * N + e] = x[e];
+    }
+  }
 }
 __device__ __forceinline__ bool wants_mass(const Row& r) { return r.k == 0; }          // draws or cuts by the mass of everything
 __device__ __forceinline__ bool wants_bins(const Row& r) { return r.k > 1 || (r.k == 0 && (r.p < 1.0f || r.mp > 0.0f)); }
 
 template <class T>
 __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) {
-  __shared__ uint32_t s_hist[NB];
+  __shared__ uint32_t s_hist[NB + 32];
   __shared__ float2 s_pow[16];
   __shared__ float s_max[NW];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
-  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow2[threadIdx.x];
+  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPowF[threadIdx.x];
   s_hist[threadIdx.x] = 0;
   pdl_enter();
   const Logits<T> l(a, row);
@@ -400,7 +404,8 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
     uint64_t sum = 0;
     if (!info.far && r.k != 1) {
       const Scale s(r.hi, r.lo, info.mj, 0.0f);
-      sum = wants_bins(r) ? bulk<true>(v, s, s_pow, top, ninf, per, info.gj, s_hist) : bulk<false>(v, s, s_pow, top, ninf, 0.0f, 0, nullptr);
+      sum = wants_bins(r) ? bulk<false, true>(v, s, s_pow, top, ninf, per, info.gj, smem_u32(s_hist))
+                          : bulk<false, false>(v, s, s_pow, top, ninf, 1.0f, 0, 0);
     }
     if (lane == 0) a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = sum;
   } else if (lane == 0) {
@@ -533,7 +538,8 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
       const int low = min(NB - 1, max(0, static_cast<int>(static_cast<float>(gj) - lo * per) + 1));
       if (threadIdx.x == low) s_front = in_front;
       __syncthreads();
-      if (s_front < CAP * 3 / 4) {
+      // (a nucleus beyond some hundred ids: the three bins are the shorter list)
+      if (s_front < (r.k == 0 && r.mp <= 0.0f ? LIST * 4 : CAP * 3 / 4)) {
         plan.hi = -ninf;
       } else if (plan.mode == kListed && r.k == 0) {
         if (r.mp <= 0.0f) {
@@ -559,7 +565,7 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   __shared__ float2 s_pow[16];
   __shared__ int s_n, s_at;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
-  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow2[threadIdx.x];
+  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPowF[threadIdx.x];
   if (threadIdx.x == 0) s_n = 0;
   pdl_enter();
   const RowPlan plan = a.plan[row];
@@ -599,16 +605,15 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
     uint2* list = a.list + static_cast<int64_t>(row) * CAP;
     at += s_at;
     constexpr int N = Vec<T>::N;
-#pragma unroll
-    for (int e = 0; e < PER; ++e)
-      if (in >> e & 1) {
-        if (at < CAP) list[at] = make_uint2(Key<T>::of(v[e]), base + ((e / N) * 32 + lane) * N + e % N);
-        ++at;
-      }
+    for (; in; in &= in - 1) {             // (few: read once more)
+      const int e = __ffs(in) - 1, id = base + ((e / N) * 32 + lane) * N + e % N;
+      if (at < CAP) list[at] = make_uint2(Key<T>::of(l.one(id)), id);
+      ++at;
+    }
   }
   if (above) {
     const Scale s(r.hi, r.lo, plan.mj, 0.0f);
-    const uint64_t sum = bulk<false>(v, s, s_pow, plan.max, plan.hi, 0.0f, 0, nullptr);
+    const uint64_t sum = bulk<true, false>(v, s, s_pow, plan.max, plan.hi, 1.0f, 0, 0);
     if (lane == 0) *seg = sum;
   }
 }

@@ -61,6 +61,17 @@ __device__ __forceinline__ void st8(bf16* p, const float (&v)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// eight parameters as they lie in memory
+template <class T>
+struct Raw8 {
+  uint4 q[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const { ld8(reinterpret_cast<const T*>(q), v); }
+};
+
 // Sum over the threads that share a row: a warp (WARPS 1) or the block.
 template <bool BLOCK>
 __device__ __forceinline__ float row_sum(float v, float* red) {
@@ -152,7 +163,7 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) norm_reg_kernel(const Norm
 // Many rows: blocks that stay, each with the rows of its next RING turns on the way into shared memory by bulk copies, so
 // that the loads go on while a row waits for its sums.  (11512 rows of 5376, fp32 x and bf16 y: a block per row, which loads,
 // sums, and stores one after the other, 157 us.)
-constexpr int RT = 256, RING = 3, kRingBytes = 112 * 1024;   // two blocks an SM
+constexpr int RT = 512, RING = 3, kRingBytes = 112 * 1024;   // two blocks an SM
 template <class XT, class YT>
 __host__ __device__ constexpr int ring_stage(int d) { return d * static_cast<int>(sizeof(XT) + sizeof(YT)); }
 
@@ -179,6 +190,13 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
     for (int i = 0; i < RING; ++i)
       if (static_cast<int>(blockIdx.x) + i * step < a.total) ask(blockIdx.x + i * step, i);
   const T *post = static_cast<const T*>(a.post), *pre = static_cast<const T*>(a.pre), *gate = static_cast<const T*>(a.gate);
+  Raw8<T> g_post[NV], g_pre[NV];           // the same for every row
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = threadIdx.x + i * RT;
+    if (c < nvec && post) g_post[i].load(post + 8 * c);
+    if (c < nvec && pre) g_pre[i].load(pre + 8 * c);
+  }
   int stage = 0;
   uint32_t phase = 0;
   for (int row = blockIdx.x; row < a.total; row += step) {
@@ -209,7 +227,7 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
         ld8(y + 8 * c, u);
         ld8(x + 8 * c, v[i]);
         if (post) {
-          ld8(post + 8 * c, w);
+          g_post[i].get(w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) u[e] = u[e] * r * w[e];
         }
@@ -235,7 +253,7 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
       if (c < nvec) {
         st8(static_cast<XT*>(a.xo) + row * a.ldxo + 8 * c, v[i]);
         if (!a.no) continue;
-        if (pre) ld8(pre + 8 * c, w);
+        if (pre) g_pre[i].get(w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[i][e] = pre ? v[i][e] * q * w[e] : v[i][e] * q;
         st8(static_cast<T*>(a.no) + row * a.ldn + 8 * c, v[i]);
@@ -299,12 +317,8 @@ cudaError_t launch(const NormArgs& a, bool vec, cudaStream_t s) {
   int dev = 0;
   const int sms = current_sms(&dev);
   // rows enough for a few turns of every block, and wide enough for a block (narrow ones: a warp each, many at once)
-  if (vec && nvec > 128 && a.total >= 8 * sms && RING * ring_stage<XT, YT>(a.d) <= kRingBytes) {
-    if (nvec <= RT) return launch_ring<XT, YT, T, 1>(a, dev, sms, s);
-    if (nvec <= 2 * RT) return launch_ring<XT, YT, T, 2>(a, dev, sms, s);
-    if (nvec <= 3 * RT) return launch_ring<XT, YT, T, 3>(a, dev, sms, s);
-    return launch_ring<XT, YT, T, 6>(a, dev, sms, s);
-  }
+  if (vec && nvec > 128 && nvec <= 2 * RT && a.total >= 8 * sms && RING * ring_stage<XT, YT>(a.d) <= kRingBytes)
+    return nvec <= RT ? launch_ring<XT, YT, T, 1>(a, dev, sms, s) : launch_ring<XT, YT, T, 2>(a, dev, sms, s);
   if (vec && nvec <= 128) {
     const int rows = 8, grid = (a.total + rows - 1) / rows;
     if (nvec <= 32) return launch_pdl(norm_reg_kernel<XT, YT, T, 1, false>, grid, 32 * rows, 0, s, a);

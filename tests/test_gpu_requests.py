@@ -425,6 +425,32 @@ def test_residual_norm(T, xt, yt, t, d, form):
             assert (o[:cu[0]] == 9).all() and (o[cu[-1]:] == 9).all()
 
 
+@pytest.mark.parametrize("xt,yt,t", [(F32, F32, BF16), (F32, BF16, BF16), (BF16, BF16, BF16), (BF16, F32, F32)])
+@pytest.mark.parametrize("d", [1032, 2048, 5376, 8192, 16384])
+def test_residual_norm_of_many_rows(T, xt, yt, t, d):
+    """More rows than blocks at a time, strided and in place, rows in front of and behind the sequences."""
+    g = gen(d)
+    lens, spare, first = [700, 0, 1, 1500, 133], 9, 4
+    cu = cum(lens, first)
+    total = cu[-1] + spare
+    wide = randn(g, total, d + 16).to(xt)
+    x = wide[:, 8:8 + d]
+    y, x0, around = (3 * randn(g, total, d)).to(yt), x.clone(), wide.clone()
+    post, gate, pre = (1 + randn(g, d)).to(t), randn(g, 5, d).to(t), (1 + randn(g, d)).to(t)
+    no = torch.full((total, d), 9.0, device="cuda").to(t)
+    T.tadm_residual_norm(x, y, x, no, cu_rows=i32(cu), post_gain=post, gate=gate, pre_gain=pre, residual_scale=0.7)
+    at = slice(cu[0], cu[-1])
+    seq = torch.repeat_interleave(torch.arange(5, device="cuda"), torch.tensor(lens, device="cuda"))
+    want = norm64(x0[at], y[at], post, gate, pre, np.float32(0.7), np.float32(1e-6), seq)
+    check_norm((x[at], no[at]), want[:2], want[2], want[3])
+    around[at, 8:8 + d] = x[at]
+    assert torch.equal(wide, around) and (no[:cu[0]] == 9).all() and (no[cu[-1]:] == 9).all()
+    plain = torch.empty_like(no)
+    T.tadm_residual_norm(x0.clone(), y, torch.empty_like(x0), plain)
+    want = norm64(x0, y, None, None, None, 1.0, np.float32(1e-6), None)
+    check_norm((want[0], plain), want[:2], want[2], want[3])
+
+
 def test_residual_norm_in_place_and_strided(T):
     g = gen(20)
     for d, left, width in ((512, 8, 1024), (512, 3, 1025), (1500, 0, 1501)):

@@ -563,21 +563,23 @@ def tadm_pages_copy(pool, src, dst, stream=None):
 
 
 # ------------------------------------------------ requests with settings of their own
-def _matrix_of(device, t, what):
-    """The dtype code (fp32 or bf16) of a matrix with dense rows on the device, and the elements from one row to the next."""
-    code = (_DTYPES or _torch_types()).get(t.dtype)
-    s, n = t.stride(), t.shape
-    if code not in (0, 1) or len(s) != 2 or (s[1] != 1 and n[1] != 1) or t.get_device() != device:
-        raise TadmError(1, f"{what} must be an fp32 or bf16 matrix with dense rows on the current device")
+def _matrix_of(device, t, what, shape=None):
+    """The dtype code (fp32 or bf16) of a matrix with dense rows on the device (of `shape`), and the elements from one row to
+    the next."""
+    code, s, n = (_DTYPES or _torch_types()).get(t.dtype), t.stride(), t.shape
+    if code not in (0, 1) or len(s) != 2 or (s[1] != 1 and n[1] != 1) or t.get_device() != device or (shape is not None and n != shape):
+        raise TadmError(1, f"{what} must be an fp32 or bf16 matrix with dense rows on the current device" +
+                        ("" if shape is None else f", {tuple(shape)}"))
     return code, s[0] if n[0] != 1 else n[1]
 
 
-def _per_row(device, t, rows, kind, what):
-    """Address of a vector of a value per row (None: none)."""
+def _vector_of(device, t, shape, kind, what):
+    """Address of a dense vector (None: none); kind: its dtype code."""
     if t is None:
         return None
-    if (_DTYPES or _torch_types()).get(t.dtype) != kind or tuple(t.shape) != (rows,) or not t.is_contiguous() or t.get_device() != device:
-        raise TadmError(1, f"{what} must be a dense vector of {rows} {'int32' if kind == 'int32' else 'fp32'} values on the current device")
+    if (_DTYPES or _torch_types()).get(t.dtype) != kind or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise TadmError(1, f"{what} must be a dense vector of {shape[0]} {('fp32', 'bf16').__getitem__(kind) if kind in (0, 1) else kind} "
+                        "values on the current device")
     return t.data_ptr()
 
 
@@ -587,13 +589,16 @@ def tadm_sample_scratch_size(rows: int, vocab: int) -> int:
     return n.value
 
 
-def _scratch_on(stream, nbytes: int):
+_sample_scratch = {}
+
+
+def _scratch_on(device, stream, nbytes: int):
     """Scratch memory for work on `stream` (None: the current one), from torch's allocator."""
     import torch
     if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def tadm_sample(logits, u, tok, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, mask_id: int = -1,
@@ -604,15 +609,22 @@ def tadm_sample(logits, u, tok, temperature=None, top_k=None, top_p=None, min_p=
     at least tadm_sample_scratch_size(rows, vocab) bytes; None: torch's allocator gives it for the call."""
     device = _device()
     dtype, ld = _matrix_of(device, logits, "logits")
-    rows, vocab = logits.shape
-    if scratch is None and vocab > 4096:
-        scratch = _scratch_on(stream, tadm_sample_scratch_size(rows, vocab))
-    status = load_library().tadm_sample(
-        logits.data_ptr(), ld, rows, vocab, mask_id, _per_row(device, temperature, rows, 0, "temperature"),
-        _per_row(device, top_k, rows, "int32", "top_k"), _per_row(device, top_p, rows, 0, "top_p"),
-        _per_row(device, min_p, rows, 0, "min_p"), _per_row(device, u, rows, 0, "u"),
-        _per_row(device, tok, rows, "int32", "tok"), _per_row(device, prob, rows, 0, "prob"), dtype,
-        *_scratch_of(device, scratch), _stream(stream))
+    shape = logits.shape
+    rows, vocab = shape
+    one = shape[:1]
+    args = (_vector_of(device, temperature, one, 0, "temperature"), _vector_of(device, top_k, one, "int32", "top_k"),
+            _vector_of(device, top_p, one, 0, "top_p"), _vector_of(device, min_p, one, 0, "min_p"),
+            _vector_of(device, u, one, 0, "u"), _vector_of(device, tok, one, "int32", "tok"), _vector_of(device, prob, one, 0, "prob"))
+    if scratch is None:
+        need = _sample_scratch.get(shape)
+        if need is None:
+            if len(_sample_scratch) > 4096:
+                _sample_scratch.clear()
+            need = _sample_scratch[shape] = tadm_sample_scratch_size(rows, vocab)
+        if need:
+            scratch = _scratch_on(device, stream, need)
+    status = load_library().tadm_sample(logits.data_ptr(), ld, rows, vocab, mask_id, *args, dtype, *_scratch_of(device, scratch),
+                                        _stream(stream))
     if status:
         _check(status)
 
@@ -629,12 +641,11 @@ def tadm_lora_project(x, w, y, cu_rows, adapter, lora_a, lora_b, lora_scale, scr
     device = _device()
     dtype, ldx = _matrix_of(device, x, "x")
     w_dtype, ldw = _matrix_of(device, w, "w")
-    y_dtype, ldy = _matrix_of(device, y, "y")
-    _ints_of(device, cu_rows, adapter)
     (rows, n_in), (n_out, k) = x.shape, w.shape
+    y_dtype, ldy = _matrix_of(device, y, "y", (rows, n_out))
+    _ints_of(device, cu_rows, adapter)
     (n, rank, a_in), batch = lora_a.shape, cu_rows.shape[0] - 1
-    if k != n_in or tuple(y.shape) != (rows, n_out) or a_in != n_in or tuple(lora_b.shape) != (n, n_out, rank) or \
-            adapter.shape[0] != batch:
+    if k != n_in or a_in != n_in or lora_b.shape != (n, n_out, rank) or adapter.shape[0] != batch:
         raise TadmError(1, "shapes of x, w, y, the adapters and the sequences do not agree")
     for t in (lora_a, lora_b):
         if t.dtype is not x.dtype or not t.is_contiguous() or t.get_device() != device:
@@ -643,7 +654,7 @@ def tadm_lora_project(x, w, y, cu_rows, adapter, lora_a, lora_b, lora_scale, scr
         raise TadmError(1, "w must have x's type")
     status = load_library().tadm_lora_project(
         x.data_ptr(), w.data_ptr(), y.data_ptr(), cu_rows.data_ptr(), adapter.data_ptr(), batch, rows, n_in, n_out, ldx, ldw,
-        ldy, lora_a.data_ptr(), lora_b.data_ptr(), _per_row(device, lora_scale, n, 0, "lora_scale"), n, rank, dtype, y_dtype,
+        ldy, lora_a.data_ptr(), lora_b.data_ptr(), _vector_of(device, lora_scale, (n,), 0, "lora_scale"), n, rank, dtype, y_dtype,
         *_scratch_of(device, scratch), _stream(stream))
     if status:
         _check(status)
@@ -654,34 +665,38 @@ def tadm_residual_norm(x, y, x_out, n_out=None, cu_rows=None, post_gain=None, ga
     """x_out = residual_scale x + gate[b] u with u = y or, with post_gain, its RMS norm times the gain, and n_out = the RMS
     norm of x_out times pre_gain, for rows [rows, d]; gate [batch, d] has a row per sequence of cu_rows (int32 [batch + 1])."""
     device = _device()
+    shape = x.shape
     x_dtype, ldx = _matrix_of(device, x, "x")
-    xo_dtype, ldxo = _matrix_of(device, x_out, "x_out")
-    y_dtype, ldy = _matrix_of(device, y, "y")
-    rows, d = shape = x.shape
-    batch = 1
+    xo_dtype, ldxo = _matrix_of(device, x_out, "x_out", shape) if x_out is not x else (x_dtype, ldx)
+    y_dtype, ldy = _matrix_of(device, y, "y", shape)
+    rows, d = shape
+    if xo_dtype != x_dtype:
+        raise TadmError(1, "x and x_out must have one type")
+    batch, cu = 1, None
     if cu_rows is not None:
         _ints_of(device, cu_rows)
-        batch = cu_rows.shape[0] - 1
-    if xo_dtype != x_dtype or x_out.shape != shape or y.shape != shape or (n_out is not None and n_out.shape != shape):
-        raise TadmError(1, "x, y, x_out and n_out must have one shape, x and x_out one type")
-    dtype, ldn, ldg = None, d, d
+        batch, cu = cu_rows.shape[0] - 1, cu_rows.data_ptr()
+    dtype, ldn, ldg, n_ptr, g_ptr = None, d, d, None, None
     if n_out is not None:
-        dtype, ldn = _matrix_of(device, n_out, "n_out")
+        dtype, ldn = _matrix_of(device, n_out, "n_out", shape)
+        n_ptr = n_out.data_ptr()
     if gate is not None:
-        g_dtype, ldg = _matrix_of(device, gate, "gate")
-        if tuple(gate.shape) != (batch, d) or dtype not in (None, g_dtype):
-            raise TadmError(1, "gate must be [batch, d], of n_out's type")
-        dtype = g_dtype
-    for t in (post_gain, pre_gain):
-        if t is not None:
-            code = (_DTYPES or _torch_types()).get(t.dtype)
-            if code not in (0, 1) or tuple(t.shape) != (d,) or not t.is_contiguous() or t.get_device() != device or \
-                    dtype not in (None, code):
-                raise TadmError(1, "gains must be dense vectors of d values of n_out's type on the current device")
-            dtype = code
+        g_dtype, ldg = _matrix_of(device, gate, "gate", (batch, d))
+        if dtype is None:
+            dtype = g_dtype
+        if dtype != g_dtype:
+            raise TadmError(1, "gate must have n_out's type")
+        g_ptr = gate.data_ptr()
+    if dtype is None:
+        first = post_gain if post_gain is not None else pre_gain
+        dtype = (_DTYPES or _torch_types()).get(first.dtype) if first is not None else 0
+        if dtype not in (0, 1):
+            raise TadmError(1, "gains must be fp32 or bf16")
+    one = shape[1:]
     status = load_library().tadm_residual_norm(
-        x.data_ptr(), y.data_ptr(), x_out.data_ptr(), _ptr(n_out), _ptr(cu_rows), batch, rows, d, ldx, ldy, ldxo, ldn,
-        _ptr(post_gain), _ptr(gate), ldg, _ptr(pre_gain), residual_scale, eps, x_dtype, y_dtype, dtype or 0, _stream(stream))
+        x.data_ptr(), y.data_ptr(), x_out.data_ptr(), n_ptr, cu, batch, rows, d, ldx, ldy, ldxo, ldn,
+        _vector_of(device, post_gain, one, dtype, "post_gain"), g_ptr, ldg, _vector_of(device, pre_gain, one, dtype, "pre_gain"),
+        residual_scale, eps, x_dtype, y_dtype, dtype, _stream(stream))
     if status:
         _check(status)
 

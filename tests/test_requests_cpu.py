@@ -103,6 +103,16 @@ def test_residual_norm_sizes(T):
     assert f(*{**NORM, **wide}.values()) == UNSUPPORTED
 
 
+def test_every_bounded_wait_of_the_adapters_names_the_status_word():
+    import os
+    import re
+    src = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_37924_gb300", "csrc", "adapters.cu")).read()
+    waits = re.findall(r"(?:mbar|warp)_wait_bounded\((.*)\)", src)
+    assert len(waits) > 8
+    for w in waits:
+        assert "a.status" in w and "nullptr" not in w, w
+
+
 # ------------------------------------------------------------------ the Python entry points
 torch = pytest.importorskip("torch")
 from paper_2609_37924_gb300 import tadm  # noqa: E402

@@ -35,7 +35,7 @@ struct LoraCall {
   void* scratch;
   int* status;                     // this device's status word
 };
-constexpr int kLoraMaxRank = 256;
+constexpr int kLoraMaxRank = 256, kLoraMaxRows = 1 << 20;
 size_t lora_scratch(int batch, int total, int n_in, int n_out, int n_adapters, int rank, int bf16);
 const char* lora_project(const LoraCall& c, cudaStream_t s);          // tcgen05 (bf16), or
 size_t lora_rows_scratch(int total, int rank);
@@ -50,6 +50,7 @@ struct NormCall {
   const void *post, *gate, *pre;
   float residual_scale, eps;
   int x_bf16, y_bf16, bf16;
+  int* status;                     // this device's status word
 };
 constexpr int kNormMaxWidth = 49152;
 const char* residual_norm(const NormCall& c, cudaStream_t s);

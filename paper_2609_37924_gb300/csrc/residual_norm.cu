@@ -25,6 +25,7 @@ struct NormArgs {
   int64_t ldx, ldy, ldxo, ldn, ldg;
   const void *post, *gate, *pre;
   float alpha, eps;
+  int* status;
 };
 
 // `bytes` (a multiple of 16) of global memory into shared memory, counted on the mbarrier
@@ -172,10 +173,12 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float red[2][32];
   __shared__ __align__(8) uint64_t full[RING];
+  __shared__ int abort_flag;
   const int nvec = a.d / 8, stage_bytes = ring_stage<XT, YT>(a.d), step = gridDim.x;
   const uint32_t xb = a.d * sizeof(XT), yb = a.d * sizeof(YT);
   if (threadIdx.x == 0) {
     for (int i = 0; i < RING; ++i) mbar_init(&full[i], 1);
+    abort_flag = 0;
     fence_mbar_init();
   }
   __syncthreads();
@@ -201,7 +204,7 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
   uint32_t phase = 0;
   for (int row = blockIdx.x; row < a.total; row += step) {
     const int b = a.cu ? seq_of_row(a.cu, a.batch, row) : 0;
-    while (!mbar_try_wait_suspend(&full[stage], phase, 1000000u)) {}        // (a copy that was asked for arrives)
+    if (__syncthreads_or(!mbar_wait_bounded(&full[stage], phase, &abort_flag, a.status))) break;
     const XT* x = reinterpret_cast<const XT*>(smem + stage * stage_bytes);
     const YT* y = reinterpret_cast<const YT*>(smem + stage * stage_bytes + xb);
     float v[NV][8], w[8];
@@ -258,6 +261,13 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
         for (int e = 0; e < 8; ++e) v[i][e] = pre ? v[i][e] * q * w[e] : v[i][e] * q;
         st8(static_cast<T*>(a.no) + row * a.ldn + 8 * c, v[i]);
       }
+    }
+  }
+  if (abort_flag && threadIdx.x == 0) {    // (a wait gave up: no copy is left in flight)
+    volatile int never = 0;
+    for (int i = 0; i < RING; ++i) {
+      mbar_wait_bounded(&full[stage], phase, &never, a.status);
+      if (++stage == RING) { stage = 0; phase ^= 1; }
     }
   }
 }
@@ -349,7 +359,7 @@ cudaError_t launch_out(const NormArgs& a, bool vec, bool bf, cudaStream_t s) {
 
 const char* residual_norm(const NormCall& c, cudaStream_t s) {
   const NormArgs a{c.x, c.y, c.x_out, c.n_out, c.cu, c.batch, c.total, c.d, c.ldx, c.ldy, c.ldxo, c.ldn, c.ldg,
-                   c.post, c.gate, c.pre, c.residual_scale, c.eps};
+                   c.post, c.gate, c.pre, c.residual_scale, c.eps, c.status};
   // 16-byte vectors of eight elements: widths, row strides and bases that allow them
   auto ok = [](const void* p, int64_t ld, int bf) {
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * (bf ? 2 : 4) % 16 == 0;

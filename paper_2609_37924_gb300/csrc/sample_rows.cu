@@ -69,13 +69,14 @@ struct ChunkInfo {
 };
 enum Mode : int { kEmpty, kAll, kListed, kWindow, kWhole };
 // kAll: every id is kept, the masses are the scan's.  kListed: what may be kept is on the list.  kWindow: what lies above
-// the list is kept, too; of the mass, `target` is.  kWhole: the last kernel takes the row by itself.
+// the list is kept, too; of the mass, `target` is, or, under min-p, top-p of `mass`, or the cut is by `count`.  kWhole: the last kernel takes the row by itself.
 struct RowPlan {
   float max, lo, hi;                       // the list: lo <= logit <= hi
   int mode, mj, listed;
   int more;                                // ids below lo may be kept, too
   uint32_t low;                            // the least key that min-p keeps
   uint64_t target;
+  unsigned long long mass, count;          // kWindow, where the cut is by them: mass that min-p leaves, ids above hi
 };
 
 // ------------------------------------------------------------------ keys
@@ -460,7 +461,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
-  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0, 0};
+  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0, 0, 0, 0};
   const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {
     plan.mode = kListed;                                      // the ids of the maximum
@@ -502,57 +503,77 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
       const uint64_t count = (n + 8192) >> 14, in_front = scan_block(count, s_room);
       __syncthreads();
       int b = NB;
-      if (r.k > 1) {
-        if (in_front >= static_cast<uint64_t>(r.k) && in_front - count < static_cast<uint64_t>(r.k)) s_bin = threadIdx.x;
-      } else if (r.p < 1.0f && r.mp <= 0.0f) {
-        plan.target = target_of(r.p, mass);
-        const float mid = ex2_approx(fmaf(edge(static_cast<float>(threadIdx.x)), r.hi, -0.0625f * static_cast<float>(mj))) * 262144.0f;
-        const uint64_t guess = static_cast<uint64_t>(static_cast<float>(n) * mid), incl = scan_block(guess, s_room);
-        if (incl >= plan.target >> 12 && incl - guess < plan.target >> 12) {
+      // the place in its bin, too: the guess of a mass is good to some 10^-4
+      auto cross = [&](uint64_t own, uint64_t incl, uint64_t target) {
+        if (incl >= target && incl - own < target) {
           s_bin = threadIdx.x;
-          s_part = static_cast<float>((plan.target >> 12) - (incl - guess)) / static_cast<float>(guess);
+          s_part = static_cast<float>(target - (incl - own)) / static_cast<float>(own);
         }
+      };
+      if (r.k > 1) {
+        cross(count, in_front, r.k);
+      } else if (r.p < 1.0f) {
+        const float mid = ex2_approx(fmaf(edge(static_cast<float>(threadIdx.x)), r.hi, -0.0625f * static_cast<float>(mj))) * 262144.0f;
+        uint64_t guess = static_cast<uint64_t>(static_cast<float>(n) * mid);
+        if (r.mp <= 0.0f) {
+          plan.target = target_of(r.p, mass);
+        } else {                           // of what min-p leaves: its part of its last bin
+          const float last = static_cast<float>(gj) - Key<T>::value(plan.low) * per + 0.5f - static_cast<float>(threadIdx.x);
+          guess = last >= 1.0f ? guess : last > 0.0f ? static_cast<uint64_t>(static_cast<float>(guess) * last) : 0;
+        }
+        uint64_t all;
+        const uint64_t incl = scan_block(guess, s_room, &all);
+        cross(guess, incl, r.mp <= 0.0f ? plan.target >> 12 : target_of(r.p, all));
       }
       float lo = ninf;
       if (r.mp > 0.0f) lo = Key<T>::value(plan.low);
       __syncthreads();
       b = s_bin;
       plan.mode = kListed;
-      if (b < NB - 2 && r.k > 0) {
-        plan.more = edge(b + 1.5f) > lo;
-        lo = fmaxf(lo, edge(b + 1.5f));
-      } else if (b < NB - 2) {
-        // three bins, or as many as the list takes around the place within the bin (the guess is good to a hundredth of one)
-        if (threadIdx.x == max(0, b - 1) || threadIdx.x == b || threadIdx.x == b + 1) atomicAdd(&s_three, static_cast<int>(min(count, static_cast<uint64_t>(1 << 24))));
+      // ids from a value on, about
+      auto ids_from = [&](float value) {
+        const int low = min(NB - 1, max(0, static_cast<int>(static_cast<float>(gj) - value * per) + 1));
         __syncthreads();
-        const float most = CAP * 0.6f, three = static_cast<float>(s_three);
-        const float half = three <= most ? 1.5f : fmaxf(0.05f, 1.5f * most / three), mid = three <= most ? b : b - 0.5f + s_part;
-        lo = edge(mid + half);
-        plan.hi = edge(mid - half);
-      } else if (r.k == 0 && r.mp <= 0.0f) {
-        plan.mode = kWhole;
-      } else {
-        lo = fmaxf(lo, edge(NB - 0.5f));                      // (k: nothing below counts; min-p: or is kept)
-      }
-      // ids from lo on: on the list, all of them, if they are few
-      const int low = min(NB - 1, max(0, static_cast<int>(static_cast<float>(gj) - lo * per) + 1));
-      if (threadIdx.x == low) s_front = in_front;
-      __syncthreads();
-      // (a nucleus beyond some hundred ids: the three bins are the shorter list)
-      if (s_front < (r.k == 0 && r.mp <= 0.0f ? LIST * 4 : CAP * 3 / 4)) {
-        plan.hi = -ninf;
-      } else if (plan.mode == kListed && r.k == 0) {
-        if (r.mp <= 0.0f) {
+        if (threadIdx.x == low) s_front = in_front;
+        __syncthreads();
+        return s_front;
+      };
+      const bool few_mp = r.mp > 0.0f && ids_from(lo) < CAP * 3 / 4;
+      if (few_mp || (r.k == 0 && r.p >= 1.0f)) {
+        // min-p alone cuts, or leaves a list
+        if (!few_mp) {                     // everything from lo on lies above an empty list
           plan.mode = kWindow;
-        } else if (r.p >= 1.0f && lo * r.hi > (top * r.hi - 44.0f)) {
-          plan.mode = kWindow;                                // min-p alone: everything from lo on lies above an empty list
           plan.hi = below(lo);
           lo = -ninf;
         } else {
-          plan.mode = kWhole;
+          plan.hi = -ninf;
         }
+      } else if (b >= NB - 2) {
+        if (r.k == 0) plan.mode = kWhole;
+        lo = fmaxf(lo, edge(NB - 0.5f));   // (k: nothing below counts)
+        plan.hi = -ninf;
+        if (ids_from(lo) >= CAP * 3 / 4) plan.mode = kWhole;
       } else {
-        plan.mode = kWhole;
+        // three bins; all from there on where those are few (or a second cut follows); else, of crowded bins, as many as the
+        // list takes around the place of the cut
+        const float edge_lo = fmaxf(lo, edge(b + 1.5f));
+        plan.more = edge_lo > lo;
+        const bool again = r.k > 0 && (r.p < 1.0f || r.mp > 0.0f);
+        if (ids_from(edge_lo) < (again ? CAP * 3 / 4 : LIST * 4)) {
+          if (r.k == 0 && r.mp > 0.0f) plan.mode = kWindow;   // (the mass is not the list's)
+          lo = edge_lo;
+          plan.hi = -ninf;
+        } else if (again) {
+          plan.mode = kWhole;
+        } else {
+          if (threadIdx.x == max(0, b - 1) || threadIdx.x == b || threadIdx.x == b + 1) atomicAdd(&s_three, static_cast<int>(min(count, static_cast<uint64_t>(1 << 24))));
+          __syncthreads();
+          const float most = CAP * 0.6f, three = static_cast<float>(s_three);
+          const float half = three <= most ? 1.5f : fmaxf(0.05f, 1.5f * most / three), mid = three <= most ? b : b - 0.5f + s_part;
+          plan.mode = kWindow;
+          lo = fmaxf(lo, edge(mid + half));
+          plan.hi = edge(mid - half);
+        }
       }
       plan.lo = lo;
     }
@@ -572,7 +593,11 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   if (plan.mode != kListed && plan.mode != kWindow) return;
   uint64_t* seg = a.seg + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
   const bool above = plan.mode == kWindow;
-  if (a.info[static_cast<int64_t>(row) * a.chunks + chunk].max < (above ? fminf(plan.lo, plan.hi) : plan.lo)) {
+  // (a chunk with nothing to list or to add; what min-p leaves may lie lower)
+  const Row r = row_of(a, row);
+  const bool left = above && r.k == 0 && r.mp > 0.0f && r.p < 1.0f;   // wants the mass that min-p leaves
+  const float low = Key<T>::value(plan.low), least = left ? low : above ? fminf(plan.lo, plan.hi) : plan.lo;
+  if (a.info[static_cast<int64_t>(row) * a.chunks + chunk].max < least) {
     if (above && lane == 0) *seg = 0;
     return;
   }
@@ -580,7 +605,6 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   const int base = chunk * CHUNK + warp * SEG;
   float v[PER];
   load_chunk(l, base, v);
-  const Row r = row_of(a, row);
   uint32_t in = 0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) in |= v[e] >= plan.lo && v[e] <= plan.hi ? 1u << e : 0u;
@@ -615,6 +639,16 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
     const Scale s(r.hi, r.lo, plan.mj, 0.0f);
     const uint64_t sum = bulk<true, false>(v, s, s_pow, plan.max, plan.hi, 1.0f, 0, 0);
     if (lane == 0) *seg = sum;
+    if (r.k > 0) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) n += v[e] > plan.hi;
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (lane == 0 && n) atomicAdd(&a.plan[row].count, static_cast<unsigned long long>(n));
+    } else if (left) {
+      const uint64_t x = bulk<true, false>(v, s, s_pow, plan.max, below(low), 1.0f, 0, 0);
+      if (lane == 0 && x) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(x));
+    }
   }
 }
 
@@ -844,7 +878,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
         sh.id[i] = id;
       }
     }
-    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0};
+    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0};
   } else {
     plan = a.plan[row];
     const uint2* list = a.list + static_cast<int64_t>(row) * CAP;
@@ -901,10 +935,10 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
       cut = low;
       Cut to{};
       if (window) {
-        if (r.p < 1.0f && r.mp <= 0.0f) {
-          ok = f.template narrow<true>(cut, ::max(cut.key, Key<T>::of(plan.lo)), Key<T>::of(plan.hi), above, plan.target, &to);
-          if (ok) cut = to;
-        }
+        const uint32_t lo = ::max(cut.key, Key<T>::of(plan.lo)), hi = Key<T>::of(plan.hi);
+        if (r.k > 0) ok = f.template narrow<false>(cut, lo, hi, plan.count, r.k, &to);
+        else if (r.p < 1.0f) ok = f.template narrow<true>(cut, lo, hi, above, r.mp > 0.0f ? target_of(r.p, plan.mass) : plan.target, &to);
+        if (ok && (r.k > 0 || r.p < 1.0f)) cut = to;
       } else {
         if (r.k > 0) {
           if (f.template narrow<false>(cut, cut.key, khi, 0, r.k, &to)) cut = to;

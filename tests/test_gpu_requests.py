@@ -138,6 +138,43 @@ def test_sample_large_vocabularies(T, dtype, vocab, rows):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("spread", [0.01, 1.0, 4.0])
+@pytest.mark.parametrize("vocab", [9000, 70001])
+def test_sample_cuts_of_thousands(T, dtype, spread, vocab):
+    """Cuts far down the order, one setting alone and several at once: more ids than any list takes."""
+    rows = 12
+    g = gen(vocab)
+    x = spread * randn(g, rows, vocab)
+    u, n = torch.rand(rows, generator=g, device="cuda"), torch.arange(rows, device="cuda")
+    k = (vocab * torch.tensor([0.05, 0.3, 0.7, 0.999], device="cuda")[n % 4]).to(torch.int32)
+    p = torch.tensor([0.9, 0.5, 0.99], device="cuda")[n % 3]
+    m = torch.tensor([1e-12, 0.01, 0.4], device="cuda")[n % 3]
+    x = x.to(dtype)
+    check_draws(T, x, u, k=k, mask_id=3)
+    check_draws(T, x, u, p=p)
+    check_draws(T, x, u, m=m, mask_id=vocab - 1)
+    check_draws(T, x, u, k=k, p=p.flip(0))
+    check_draws(T, x, u, p=p, m=m.roll(1))
+    check_draws(T, x, u, k=k, m=m, p=p)
+
+
+@pytest.mark.parametrize("vocab", [3000, 30000])
+def test_sample_far_from_zero_and_nearly_cold(T, vocab):
+    """Logits whose distance from zero, over the temperature, is past what the passes over a row count in."""
+    rows = 12
+    g = gen(vocab + 1)
+    x = randn(g, rows, vocab)
+    n = torch.arange(rows, device="cuda")
+    x += torch.tensor([0.0, 3e4, -3e4, 1e6], device="cuda")[n % 4][:, None]
+    t = torch.tensor([1.0, 1e-3, 3e-2], device="cuda")[n % 3]
+    u = torch.rand(rows, generator=g, device="cuda")
+    check_draws(T, x, u, t)
+    check_draws(T, x, u, t, p=f32([0.9] * rows), mask_id=7)
+    check_draws(T, x, u, t, k=i32([30] * rows), m=f32([0.01] * rows))
+    check_draws(T, 1e5 * x, u, 1e5 * t, p=f32([0.7] * rows))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("vocab", [7, 5000, 140000])
 def test_sample_equal_logits(T, dtype, vocab):
     """Ties everywhere: every cut falls among equal logits and goes by the id."""

@@ -78,6 +78,8 @@ def test_lora_scratch(T):
         need = T.tadm_lora_scratch_size(3, 10, 64, 40, 2, 16, dtype)
         call = {**LORA, "dtype": dtype, "y_dtype": 0}
         assert T.load_library().tadm_lora_project(*{**call, "scratch_bytes": need - 1}.values()) == INVALID
+    for over in (dict(total=(1 << 20) + 1), dict(n_out=(1 << 20) + 1, ldy=1 << 21)):
+        assert T.load_library().tadm_lora_project(*{**LORA, **over}.values()) == UNSUPPORTED
     for over in (dict(batch=0), dict(total=0)):
         assert T.load_library().tadm_lora_project(*{**LORA, **over}.values()) == 0
 

@@ -74,6 +74,7 @@ struct RowPlan {
   float max, lo, hi;                       // the list: lo <= logit <= hi
   int mode, mj, listed;
   int more;                                // ids below lo may be kept, too
+  int left;                                // kWindow: 1 where `mass` is wanted
   uint32_t low;                            // the least key that min-p keeps
   uint64_t target;
   unsigned long long mass, count;          // kWindow, where the cut is by them: mass that min-p leaves, ids above hi
@@ -341,7 +342,8 @@ __device__ __forceinline__ uint64_t scan_block(uint64_t own, uint64_t* room, uin
 }
 
 // ------------------------------------------------------------------ the passes over the logits
-// This lane's ids: PER of its warp's 512, V::N next to each other, 32 V::N from piece to piece.
+// This lane's ids: PER of its warp's 512, V::N next to each other, 32 V::N from piece to piece.  NaN may come as it is: maxima
+// leave it out, and no comparison holds for it.
 template <class T>
 __device__ __forceinline__ void load_chunk(const Logits<T>& l, int base, float (&v)[PER]) {
   constexpr int N = Vec<T>::N;
@@ -356,7 +358,7 @@ __device__ __forceinline__ void load_chunk(const Logits<T>& l, int base, float (
       float x[N];
       Vec<T>::get(q[i], x);
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[i * N + e] = fmaxf(x[e], __int_as_float(0xff800000));
+      for (int e = 0; e < N; ++e) v[i * N + e] = x[e];
     }
   } else {
 #pragma unroll 1
@@ -387,15 +389,15 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
   float v[PER];
   load_chunk(l, chunk * CHUNK + warp * SEG, v);
   const Row r = row_of(a, row);
-  float top = v[0];
+  const float ninf = __int_as_float(0xff800000);
+  float top = ninf;
 #pragma unroll
-  for (int e = 1; e < PER; ++e) top = fmaxf(top, v[e]);
+  for (int e = 0; e < PER; ++e) top = fmaxf(top, v[e]);
   top = warp_max(top);
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
   const float per = r.hi * ((NB - 2) / depth_of(a, r));
-  const float ninf = __int_as_float(0xff800000);
   ChunkInfo info{top, 0, 0, 0};
   if (top > ninf) {
     const float g = top * per;
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
-  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0, 0, 0, 0};
+  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0, 0, 0, 0, 0};
   const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {
     plan.mode = kListed;                                      // the ids of the maximum
@@ -576,6 +578,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
         }
       }
       plan.lo = lo;
+      plan.left = plan.mode == kWindow && r.k == 0 && r.mp > 0.0f && r.p < 1.0f;
     }
   }
   if (threadIdx.x == 0) a.plan[row] = plan;
@@ -594,9 +597,7 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   uint64_t* seg = a.seg + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
   const bool above = plan.mode == kWindow;
   // (a chunk with nothing to list or to add; what min-p leaves may lie lower)
-  const Row r = row_of(a, row);
-  const bool left = above && r.k == 0 && r.mp > 0.0f && r.p < 1.0f;   // wants the mass that min-p leaves
-  const float low = Key<T>::value(plan.low), least = left ? low : above ? fminf(plan.lo, plan.hi) : plan.lo;
+  const float low = Key<T>::value(plan.low), least = plan.left ? low : above ? fminf(plan.lo, plan.hi) : plan.lo;
   if (a.info[static_cast<int64_t>(row) * a.chunks + chunk].max < least) {
     if (above && lane == 0) *seg = 0;
     return;
@@ -605,6 +606,7 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   const int base = chunk * CHUNK + warp * SEG;
   float v[PER];
   load_chunk(l, base, v);
+  const Row r = row_of(a, row);
   uint32_t in = 0;
 #pragma unroll
   for (int e = 0; e < PER; ++e) in |= v[e] >= plan.lo && v[e] <= plan.hi ? 1u << e : 0u;
@@ -637,17 +639,19 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   }
   if (above) {
     const Scale s(r.hi, r.lo, plan.mj, 0.0f);
-    const uint64_t sum = bulk<true, false>(v, s, s_pow, plan.max, plan.hi, 1.0f, 0, 0);
-    if (lane == 0) *seg = sum;
+    // (a loop, so that bulk's code is there once)
+#pragma unroll 1
+    for (int turn = 0; turn < 1 + plan.left; ++turn) {
+      const uint64_t sum = bulk<true, false>(v, s, s_pow, plan.max, turn ? below(low) : plan.hi, 1.0f, 0, 0);
+      if (lane == 0 && turn == 0) *seg = sum;
+      if (lane == 0 && turn == 1 && sum) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(sum));
+    }
     if (r.k > 0) {
       uint32_t n = 0;
 #pragma unroll
       for (int e = 0; e < PER; ++e) n += v[e] > plan.hi;
       n = __reduce_add_sync(0xffffffffu, n);
       if (lane == 0 && n) atomicAdd(&a.plan[row].count, static_cast<unsigned long long>(n));
-    } else if (left) {
-      const uint64_t x = bulk<true, false>(v, s, s_pow, plan.max, below(low), 1.0f, 0, 0);
-      if (lane == 0 && x) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(x));
     }
   }
 }
@@ -878,7 +882,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
         sh.id[i] = id;
       }
     }
-    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0};
+    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0, 0};
   } else {
     plan = a.plan[row];
     const uint2* list = a.list + static_cast<int64_t>(row) * CAP;

@@ -8,7 +8,8 @@
 // x and y are read once, x' and n written once, everything between is fp32 in
 // registers; n is made from x' before it is rounded to its own type.
 //
-// Bound: HBM, (2 es_x + es_y + es_n) bytes per element.
+// Bound: HBM, (2 es_x + es_y + es_n) bytes per element: 11512 rows of 5376 (fp32 x, bf16 y) 134 us, 5.8 TB/s, 85 % of a
+// plain copy's rate; 1024 rows of 2048 in bf16 4.4 us out of L2; one row 3.5 us, the launch.
 #include <cstdint>
 
 #include "ragged.cuh"
@@ -163,7 +164,7 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) norm_reg_kernel(const Norm
 
 // Many rows: blocks that stay, each with the rows of its next RING turns on the way into shared memory by bulk copies, so
 // that the loads go on while a row waits for its sums.  (11512 rows of 5376, fp32 x and bf16 y: a block per row, which loads,
-// sums, and stores one after the other, 157 us.)
+// sums, and stores one after the other, 157 us; blocks of 256 threads 153; gains read for every row, 149; 134 as it is.)
 constexpr int RT = 512, RING = 3, kRingBytes = 112 * 1024;   // two blocks an SM
 template <class XT, class YT>
 __host__ __device__ constexpr int ring_stage(int d) { return d * static_cast<int>(sizeof(XT) + sizeof(YT)); }

@@ -29,8 +29,17 @@
 //                          key until 128 elements or one key are left; the 512
 //                          ids in which the draw falls; the token.
 // Where a list overflows or the guess was wrong, the last one takes the whole
-// row by the same histograms (logits beyond 2^18 T, cuts of thousands of ids
-// under two settings at once).
+// row by the same histograms (logits beyond 2^18 T; cuts of thousands of ids
+// by top-k under a second setting).
+//
+// Bound: of few rows the four kernels' latency, 4 to 6 us each (a row of 32768
+// ids 21 us); of many the instructions of the two passes over the logits, 54 and 40 an
+// id at 68 % and 55 % of the issue slots (512 rows of 128000, fp32, a nucleus
+// each: 292 us, of which scan 130, collect 124; one reading of the logits is
+// 39).  The row in the shared memory of a cluster of 8 blocks instead, read from
+// HBM once, took 691 us: 38 rows at a time, each some 45 us of passes that end
+// in a cluster barrier.  A pair of values per instruction (f32x2) executes as many
+// instructions as one.
 #include <cstdint>
 
 #include "common.cuh"

@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
   if (top > ninf) {
     const float g = top * per;
     info.mj = mj_of(r.hi, r.lo, top);
-    info.gj = fabsf(g) < static_cast<float>(kFar) ? __float2int_rn(g) : kFar;
+    info.gj = fabsf(g) < static_cast<float>(kFar) ? __float2int_ru(g) : kFar;   // (up: no value rounds to a bin before the first)
     info.far = info.mj == kFar || info.gj == kFar || !(r.hi > 1e-30f);
     uint64_t sum = 0;
     if (!info.far && r.k != 1) {
@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
   } else if (top > ninf) {
     const int mj = mj_of(r.hi, r.lo, top);
     const float per = r.hi * ((NB - 2) / depth_of(a, r));
-    const int gj = __float2int_rn(top * per);
+    const int gj = __float2int_ru(top * per);
     plan.mj = mj;
     // every mass in the units of the row's maximum
     uint64_t mass = 0;

@@ -174,6 +174,43 @@ def test_sample_far_from_zero_and_nearly_cold(T, vocab):
     check_draws(T, 1e5 * x, u, 1e5 * t, p=f32([0.7] * rows))
 
 
+def half_way_tops(n):
+    """Logits that lie, in steps of which 510 span a weight of 2^-44, half-way between two whole numbers once their product
+    is rounded, and above that before."""
+    per = np.float32(1.4426950408889634) * (np.float32(510) / np.float32(44))
+    out = []
+    for at in (0.5, 100.5, -20.5, 2000.5, 1e5 + 0.5, 1e6 + 0.5, 3e6 + 0.5):
+        x = np.float32(at / np.float64(per))
+        found = 0
+        for _ in range(200000):
+            x = np.nextafter(x, np.float32(np.inf))
+            g = x * per
+            if np.float64(g) - math.floor(g) == 0.5 and math.floor(g) % 2 == 0 and np.float64(x) * np.float64(per) > g:
+                out.append(float(x))
+                found += 1
+                if found == n:
+                    break
+    return out
+
+
+@pytest.mark.parametrize("vocab", [5000, 30000])
+def test_sample_maxima_half_way_between_bins(T, vocab):
+    """Every 8192 ids count their values from their own maximum; it must not round to a place in front of the first."""
+    tops = half_way_tops(3)
+    assert len(tops) >= 12
+    rows = len(tops)
+    g = gen(vocab + 2)
+    x = torch.tensor(tops, device="cuda")[:, None] - 1.0 - 6.0 * torch.rand(rows, vocab, generator=g, device="cuda")
+    for first in range(0, vocab, 8192):
+        x[:, first + 77] = torch.tensor(tops, device="cuda")
+    u = torch.rand(rows, generator=g, device="cuda")
+    ones = torch.ones(rows, device="cuda")
+    check_draws(T, x, u, ones, k=i32([30] * rows))
+    check_draws(T, x, u, ones, k=i32([2] * rows))
+    check_draws(T, x, u, ones, m=f32([0.1] * rows))
+    check_draws(T, x, u, ones, m=f32([0.01] * rows), p=f32([0.9] * rows))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("vocab", [7, 5000, 140000])
 def test_sample_equal_logits(T, dtype, vocab):

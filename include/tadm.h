@@ -705,7 +705,7 @@ TADM_API tadm_status tadm_sample(const void* logits, int64_t ld, int rows, int v
  * lora_b; y_dtype 0 or 1 for bf16 calls, 0 for fp32 ones.  x, W, lora_a and
  * lora_b are 16-byte aligned, n_in, ldx and ldw times the element size multiples
  * of 16, rank a multiple of 8 up to 256 (adapters of a lower rank: zeros behind
- * their rows of A and columns of B), total_rows and n_out up to 2^20 (TADM_ERR_UNSUPPORTED above).  y must not overlap the
+ * their rows of A and columns of B), total_rows and n_out up to 2^20, batch up to 2^30 (TADM_ERR_UNSUPPORTED above).  y must not overlap the
  * inputs.
  *
  * Sums are fp32.  bf16 calls carry A_a x (times the scale) to 16 significant
@@ -731,8 +731,8 @@ TADM_API tadm_status tadm_lora_project(const void* x, const void* w, void* y, co
  * dtype: of post_gain, gate, pre_gain and n_out (each 0 fp32, 1 bf16).  All
  * arithmetic is fp32; n_out is made from x_out before it is rounded to its type.
  * x_out may be x (with its stride) and n_out may be y (of the same type and
- * stride); other overlaps are not allowed.  Any d up to 49152
- * (TADM_ERR_UNSUPPORTED above), any strides of at least d, any alignment;
+ * stride); other overlaps are not allowed.  Any d up to 49152, total_rows and
+ * batch up to 2^30 (TADM_ERR_UNSUPPORTED above), any strides of at least d, any alignment;
  * widths that are a multiple of 8 with rows on 16 bytes are the fast ones.
  * Waits are bounded as above: tadm_ragged_sync_status() tells. */
 TADM_API tadm_status tadm_residual_norm(const void* x, const void* y, void* x_out, void* n_out, const int32_t* cu_rows,

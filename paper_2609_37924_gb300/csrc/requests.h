@@ -52,7 +52,8 @@ struct NormCall {
   int x_bf16, y_bf16, bf16;
   int* status;                     // this device's status word
 };
-constexpr int kNormMaxWidth = 49152;
+constexpr int kNormMaxWidth = 49152, kNormMaxRows = 1 << 30;
+constexpr int kMaxSequences = 1 << 30;      // of adapters and norms
 const char* residual_norm(const NormCall& c, cudaStream_t s);
 
 }  // namespace tadm

@@ -62,7 +62,7 @@ tadm_status tadm_lora_project(const void* x, const void* w, void* y, const int32
   if (n_adapters > 0 && (!lora_a || !lora_b || !lora_scale || !aligned(lora_a, 16) || !aligned(lora_b, 16) || !aligned(lora_scale, 4)))
     return TADM_ERR_INVALID_ARG;
   if (need > 0 && (!scratch || !aligned(scratch, 16) || scratch_bytes < need)) return TADM_ERR_INVALID_ARG;
-  if (total_rows > kLoraMaxRows || n_out > kLoraMaxRows) return TADM_ERR_UNSUPPORTED;   // grids, counts of tiles
+  if (total_rows > kLoraMaxRows || n_out > kLoraMaxRows || batch > kMaxSequences) return TADM_ERR_UNSUPPORTED;   // grids, counts of tiles
   LoraCall c{};
   c.x = x, c.w = w, c.y = y, c.cu = cu_rows, c.adapter = adapter;
   c.batch = batch, c.total = total_rows, c.n_in = n_in, c.n_out = n_out, c.ldx = ldx, c.ldw = ldw, c.ldy = ldy;
@@ -84,7 +84,7 @@ tadm_status tadm_residual_norm(const void* x, const void* y, void* x_out, void* 
       !aligned(n_out, es(dtype)) || !aligned(post_gain, es(dtype)) || !aligned(gate, es(dtype)) || !aligned(pre_gain, es(dtype)) ||
       !aligned(cu_rows, 4))
     return TADM_ERR_INVALID_ARG;
-  if (d > kNormMaxWidth) return TADM_ERR_UNSUPPORTED;
+  if (d > kNormMaxWidth || total_rows > kNormMaxRows || batch > kMaxSequences) return TADM_ERR_UNSUPPORTED;
   const NormCall c{x, y, x_out, n_out, cu_rows, batch, total_rows, d, ldx, ldy, ldxo, ldn, ldg,
                    post_gain, gate, pre_gain, residual_scale, eps, x_dtype, y_dtype, dtype, ragged_status()};
   if (!c.status) return TADM_ERR_CUDA;

@@ -1,6 +1,9 @@
 """Sampling with settings per row, projections with an adapter per request, norms with gate and residual scale on the GPU,
 against plain definitions in 64 bits."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -639,3 +642,59 @@ def test_a_serving_step(T):
     T.tadm_gemm(last, head, logits, dtype=1)
     check_draws(T, logits, torch.rand(4, generator=g, device="cuda"), t=f32([0.0, 0.7, 1.0, 1.3]), k=i32([0, 50, 0, 0]),
                 p=f32([1.0, 0.9, 0.95, 1.0]), m=f32([0.0, 0.0, 0.0, 0.02]), mask_id=vocab - 1)
+
+
+FIRST_CALLS = """
+import torch
+from paper_2609_37924_gb300 import tadm as T
+s, dev = torch.cuda.Stream(), "cuda"
+x, w = torch.ones(40, 64, device=dev).bfloat16(), torch.eye(64, device=dev).bfloat16()
+a, b = torch.zeros(1, 16, 64, device=dev).bfloat16(), torch.zeros(1, 64, 16, device=dev).bfloat16()
+cu, ad = torch.tensor([0, 40], dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+y, scale = torch.zeros(40, 64, device=dev).bfloat16(), torch.ones(1, device=dev)
+room = torch.empty(T.tadm_lora_scratch_size(1, 40, 64, 64, 1, 16, 1), dtype=torch.uint8, device=dev)
+logits = torch.zeros(2, 9000, device=dev)
+logits[0, 8999] = logits[1, 17] = 1.0
+tok, u, k = torch.zeros(2, dtype=torch.int32, device=dev), torch.zeros(2, device=dev), torch.ones(2, dtype=torch.int32, device=dev)
+xo, no = torch.zeros(40, 64, device=dev), torch.zeros(40, 64, device=dev)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g, stream=s):
+    T.tadm_lora_project(x, w, y, cu, ad, a, b, scale, room)
+    T.tadm_residual_norm(torch.ones_like(xo), y, xo, no, cu_rows=cu)
+    T.tadm_sample(logits, u, tok, top_k=k)
+g.replay()
+torch.cuda.synchronize()
+T.tadm_ragged_sync_status()
+assert (y == 1).all() and (xo == 2).all() and ((no - 1).abs() < 1e-6).all() and tok.tolist() == [8999, 17]
+print("captured")
+"""
+
+
+def test_the_first_calls_of_a_process_can_be_captured(T):
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "captured", r.stderr[-2000:]
+
+
+def test_sample_rows_of_every_kind_in_one_call(T):
+    """Rows that are drawn from the whole, from a list, from a window, from nothing, and from one id, side by side: each as alone."""
+    g = gen(40)
+    rows, vocab = 24, 20000
+    x = 2.0 * randn(g, rows, vocab)
+    x[3], x[9, 5:] = -math.inf, -math.inf
+    x[4] = 0.5
+    x[11, 19999] = math.inf
+    x[12] += 1e6
+    n = torch.arange(rows, device="cuda")
+    t = torch.tensor([1.0, 0.5, 0.0, 5.0], device="cuda")[n % 4]
+    k = torch.tensor([0, 0, 50, 6000, 1], dtype=torch.int32, device="cuda")[n % 5]
+    p = torch.tensor([1.0, 0.9, 1.0, 0.3, 0.99, 0.999, 1.0], device="cuda")[n % 7]
+    m = torch.tensor([0.0, 0.0, 0.01], device="cuda")[n % 3]
+    u = torch.rand(rows, generator=g, device="cuda")
+    check_draws(T, x, u, t, k, p, m, mask_id=19998)
+    together, alone = (torch.empty(rows, dtype=torch.int32, device="cuda") for _ in range(2))
+    T.tadm_sample(x, u, together, t, k, p, m)
+    for r in range(rows):
+        T.tadm_sample(x[r:r + 1], u[r:r + 1], alone[r:r + 1], t[r:r + 1], k[r:r + 1], p[r:r + 1], m[r:r + 1])
+    assert torch.equal(together, alone)

@@ -78,7 +78,7 @@ def test_lora_scratch(T):
         need = T.tadm_lora_scratch_size(3, 10, 64, 40, 2, 16, dtype)
         call = {**LORA, "dtype": dtype, "y_dtype": 0}
         assert T.load_library().tadm_lora_project(*{**call, "scratch_bytes": need - 1}.values()) == INVALID
-    for over in (dict(total=(1 << 20) + 1), dict(n_out=(1 << 20) + 1, ldy=1 << 21)):
+    for over in (dict(total=(1 << 20) + 1), dict(batch=(1 << 30) + 1), dict(n_out=(1 << 20) + 1, ldy=1 << 21)):
         assert T.load_library().tadm_lora_project(*{**LORA, **over}.values()) == UNSUPPORTED
     for over in (dict(batch=0), dict(total=0)):
         assert T.load_library().tadm_lora_project(*{**LORA, **over}.values()) == 0
@@ -103,6 +103,8 @@ def test_residual_norm_sizes(T):
         assert f(*{**NORM, **over}.values()) == 0
     wide = dict(d=49153, ldx=49153, ldy=49153, ldxo=49153, ldn=49153, ldg=49153)
     assert f(*{**NORM, **wide}.values()) == UNSUPPORTED
+    for over in (dict(total=(1 << 30) + 1), dict(total=2 ** 31 - 1, d=8), dict(batch=(1 << 30) + 1)):
+        assert f(*{**NORM, **over}.values()) == UNSUPPORTED
 
 
 def test_every_bounded_wait_of_the_adapters_names_the_status_word():

@@ -260,33 +260,15 @@ __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, 
 // Adds to a word of shared memory.
 __device__ __forceinline__ void add_shared(uint32_t at, uint32_t x) { asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory"); }
 
-// Sum of the weights of the values that a warp's lanes hold, in units of 2^-44, in every lane; CUT: of those above `cut`
-// (exclusive).  weight()'s arithmetic, with the table's rest added to 2^f - 1: a weight is a + a r, a in fp32, r good to
-// 2^-30; h the sum's rounding, l what that lost.  The sum of h begins at 96, so that what its roundings (2^-17) lose is
-// had by two subtractions; the lost parts' sum carries errors of about 2^-38 a lane.
-// BINS: also a histogram by value, bins counted down from gj / per; a value adds its weight over that of its bin's
-// middle, linear in its place within the bin, in 2^-14.  NB words, and 32 for what lies past them.
-template <bool CUT, bool BINS>
-__device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, const float2* pow, float max, float cut, float per, int gj,
-                                         uint32_t hist) {
-  const float none = fmaxf(max - 60.0f / s.hi, -3.0e38f);     // stands for values that are not summed: 2^-60, in no bin
-  if (CUT) cut = fmaxf(cut, none);
-  const float back = kMagic * 0.0625f - s.mh;
-  const float b_c = kMagic + static_cast<float>(gj), b_slope = -16384.0f * 0.693147181f * s.hi / per;
-  const uint32_t past = hist + 4u * (NB + (threadIdx.x & 31));   // (a word per lane: no branch, no conflicts)
-  hist -= 4u * static_cast<uint32_t>(kMagicBits);
+// Sums the weights of a lane's values, in units of 2^-44.  weight()'s arithmetic, with the table's rest added to 2^f - 1: a
+// weight is a + a r, a in fp32, r good to 2^-30; h the sum's rounding, l what that lost.  The sum of h begins at 96, so that
+// what its roundings (2^-17) lose is had by two subtractions; the lost parts' sum carries errors of about 2^-38 a lane.
+struct Sums {
   float big = 96.0f, small = 0.0f;
-#pragma unroll
-  for (int e = 0; e < PER; ++e) {
-    const float x = CUT ? (v[e] > cut ? v[e] : none) : fmaxf(v[e], none);
-    if constexpr (BINS) {
-      const float q = fmaf(x, -per, b_c), d = fmaf(x, -per, b_c - q);       // d: from the bin's middle, in bins
-      const uint32_t at = hist + 4u * __float_as_uint(q);
-      add_shared(q < kMagic + NB ? at : past, __float_as_uint(fmaf(d, b_slope, kMagic + 16384.0f)) - kMagicBits);
-    }
+  __device__ __forceinline__ void add(float x, const Scale& s, const float2* pow) {
     const float q = fmaf(x, s.hi16, s.k_c);
     const uint32_t b = __float_as_uint(q);
-    const float g = fmaf(x, s.lo, fmaf(x, s.hi, fmaf(q, -0.0625f, back)));
+    const float g = fmaf(x, s.lo, fmaf(x, s.hi, fmaf(q, -0.0625f, kMagic * 0.0625f - s.mh)));
     const float2 t = pow[b & 15];
     const float r = fmaf(g, fmaf(g, fmaf(g, fmaf(g, A4, A3), A2), A1), t.y);
     // 2^n (1 + i/16), j = 16 n + i: j with its last four bits at the top of the fraction (the magic number's drop out)
@@ -296,13 +278,68 @@ __device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, 
     small += (h - (next - big)) + l;
     big = next;
   }
-  // 16 weights of up to 1.03 a lane in units of 2^-17: 2^26 over the warp; the rest 2^30 a lane
-  const uint32_t whole = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(__float2int_rn((big - 96.0f) * 131072.0f)));
-  const int rest = __float2int_rn(small * 17592186044416.0f);
-  const int high = __reduce_add_sync(0xffffffffu, rest >> 16);
-  const uint32_t low = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(rest) & 0xffffu);
-  const int64_t sum = (static_cast<int64_t>(whole) << 27) + (static_cast<int64_t>(high) << 16) + low;
-  return sum > 0 ? static_cast<uint64_t>(sum) : 0;
+  // over the warp, in every lane: 16 weights of up to 1.03 a lane in units of 2^-17: 2^26 over the warp; the rest 2^30 a lane
+  __device__ __forceinline__ uint64_t all() const {
+    const uint32_t whole = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(__float2int_rn((big - 96.0f) * 131072.0f)));
+    const int rest = __float2int_rn(small * 17592186044416.0f);
+    const int high = __reduce_add_sync(0xffffffffu, rest >> 16);
+    const uint32_t low = __reduce_add_sync(0xffffffffu, static_cast<uint32_t>(rest) & 0xffffu);
+    const int64_t sum = (static_cast<int64_t>(whole) << 27) + (static_cast<int64_t>(high) << 16) + low;
+    return sum > 0 ? static_cast<uint64_t>(sum) : 0;
+  }
+};
+// stands for a value that is not summed: 2^-60, in no bin
+__device__ __forceinline__ float none_of(const Scale& s, float max) { return fmaxf(max - 60.0f / s.hi, -3.0e38f); }
+
+// Sum of the weights of the values that a warp's lanes hold.
+// BINS: also a histogram by value, bins counted down from gj / per; a value adds its weight over that of its bin's
+// middle, linear in its place within the bin, in 2^-14.  NB words, and 32 for what lies past them.
+template <bool BINS>
+__device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, const float2* pow, float max, float per, int gj, uint32_t hist) {
+  const float none = none_of(s, max);
+  const float b_c = kMagic + static_cast<float>(gj), b_slope = -16384.0f * 0.693147181f * s.hi / per;
+  const uint32_t past = hist + 4u * (NB + (threadIdx.x & 31));   // (a word per lane: no branch, no conflicts)
+  hist -= 4u * static_cast<uint32_t>(kMagicBits);
+  Sums sums;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    const float x = fmaxf(v[e], none);
+    if constexpr (BINS) {
+      const float q = fmaf(x, -per, b_c), d = fmaf(x, -per, b_c - q);       // d: from the bin's middle, in bins
+      const uint32_t at = hist + 4u * __float_as_uint(q);
+      add_shared(q < kMagic + NB ? at : past, __float_as_uint(fmaf(d, b_slope, kMagic + 16384.0f)) - kMagicBits);
+    }
+    sums.add(x, s, pow);
+  }
+  return sums.all();
+}
+// Of those above `cut` alone: they are moved together first (room: SEG words of the warp's), since in a nucleus' or a top-k's
+// row they are few.
+__device__ __forceinline__ uint64_t bulk_above(const float (&v)[PER], const Scale& s, const float2* pow, float max, float cut, float* room) {
+  const int lane = threadIdx.x & 31;
+  const float none = none_of(s, max);
+  cut = fmaxf(cut, none);
+  int n = 0;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) n += v[e] > cut;
+  int incl = n;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  const int all = __shfl_sync(0xffffffffu, incl, 31);
+  if (all == 0) return 0;
+  float* to = room + incl - n;
+  __syncwarp();
+#pragma unroll
+  for (int e = 0; e < PER; ++e)
+    if (v[e] > cut) *to++ = v[e];
+  __syncwarp();
+  Sums sums;
+#pragma unroll 4
+  for (int i = 0; i < all; i += 32) sums.add(i + lane < all ? room[i + lane] : none, s, pow);
+  return sums.all();
 }
 // the largest logit below `v`
 __device__ __forceinline__ float below(float v) { return v == 0.0f ? -1.4e-45f : Key<float>::value(Key<float>::of(v) - 1); }
@@ -416,8 +453,7 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
     uint64_t sum = 0;
     if (!info.far && r.k != 1) {
       const Scale s(r.hi, r.lo, info.mj, 0.0f);
-      sum = wants_bins(r) ? bulk<false, true>(v, s, s_pow, top, ninf, per, info.gj, smem_u32(s_hist))
-                          : bulk<false, false>(v, s, s_pow, top, ninf, 1.0f, 0, 0);
+      sum = wants_bins(r) ? bulk<true>(v, s, s_pow, top, per, info.gj, smem_u32(s_hist)) : bulk<false>(v, s, s_pow, top, 1.0f, 0, 0);
     }
     if (lane == 0) a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = sum;
   } else if (lane == 0) {
@@ -596,6 +632,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
 template <class T>
 __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs a) {
   __shared__ float2 s_pow[16];
+  __shared__ float s_room[CHUNK];
   __shared__ int s_n, s_at;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
   if (threadIdx.x < 16) s_pow[threadIdx.x] = kPowF[threadIdx.x];
@@ -651,7 +688,7 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
     // (a loop, so that bulk's code is there once)
 #pragma unroll 1
     for (int turn = 0; turn < 1 + plan.left; ++turn) {
-      const uint64_t sum = bulk<true, false>(v, s, s_pow, plan.max, turn ? below(low) : plan.hi, 1.0f, 0, 0);
+      const uint64_t sum = bulk_above(v, s, s_pow, plan.max, turn ? below(low) : plan.hi, s_room + warp * SEG);
       if (lane == 0 && turn == 0) *seg = sum;
       if (lane == 0 && turn == 1 && sum) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(sum));
     }

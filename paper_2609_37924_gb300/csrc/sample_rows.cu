@@ -196,17 +196,21 @@ struct Row {
   int k;
   float p, mp, t;
 };
+// (t alone)
+__device__ __forceinline__ Row scaled(float t) {
+  Row r{0.0f, 0.0f, 0, 1.0f, 0.0f, t};
+  constexpr double kLog2e = 1.4426950408889634074;
+  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
+  r.hi = L / t;
+  r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, t, L) + LL) / t : 0.0f;   // the division's remainder
+  return r;
+}
 __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
-  Row r;
-  r.t = a.temperature ? a.temperature[row] : 1.0f;
+  Row r = scaled(a.temperature ? a.temperature[row] : 1.0f);
   r.p = a.top_p ? a.top_p[row] : 1.0f;
   r.mp = a.min_p ? a.min_p[row] : 0.0f;
   r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
   if (r.k < 0 || r.k >= a.vocab) r.k = 0;
-  constexpr double kLog2e = 1.4426950408889634074;
-  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
-  r.hi = L / r.t;
-  r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, r.t, L) + LL) / r.t : 0.0f;   // the division's remainder
   return r;
 }
 // f m rounded down (UP: up), for 0 <= f < 1: f's 24 bits times m's 64, shifted.
@@ -630,7 +634,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
 }
 
 template <class T>
-__global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs a) {
   __shared__ float2 s_pow[16];
   __shared__ float s_room[CHUNK];
   __shared__ int s_n, s_at;
@@ -638,13 +642,19 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   if (threadIdx.x < 16) s_pow[threadIdx.x] = kPowF[threadIdx.x];
   if (threadIdx.x == 0) s_n = 0;
   pdl_enter();
-  const RowPlan plan = a.plan[row];
-  if (plan.mode != kListed && plan.mode != kWindow) return;
+  // (what is read of the plan, the chunk and the settings is asked for at once)
+  const RowPlan& to = a.plan[row];
+  const float top = to.max, p_lo = to.lo, p_hi = to.hi, c_max = a.info[static_cast<int64_t>(row) * a.chunks + chunk].max;
+  const int mode = to.mode, mj = to.mj, left = to.left;
+  const uint32_t low_k = to.low;
+  const float t = a.temperature ? a.temperature[row] : 1.0f;
+  const int k = a.top_k ? a.top_k[row] : 0;
+  if (mode != kListed && mode != kWindow) return;
   uint64_t* seg = a.seg + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
-  const bool above = plan.mode == kWindow;
+  const bool above = mode == kWindow;
   // (a chunk with nothing to list or to add; what min-p leaves may lie lower)
-  const float low = Key<T>::value(plan.low), least = plan.left ? low : above ? fminf(plan.lo, plan.hi) : plan.lo;
-  if (a.info[static_cast<int64_t>(row) * a.chunks + chunk].max < least) {
+  const float low = Key<T>::value(low_k), least = left ? low : above ? fminf(p_lo, p_hi) : p_lo;
+  if (c_max < least) {
     if (above && lane == 0) *seg = 0;
     return;
   }
@@ -652,10 +662,9 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
   const int base = chunk * CHUNK + warp * SEG;
   float v[PER];
   load_chunk(l, base, v);
-  const Row r = row_of(a, row);
   uint32_t in = 0;
 #pragma unroll
-  for (int e = 0; e < PER; ++e) in |= v[e] >= plan.lo && v[e] <= plan.hi ? 1u << e : 0u;
+  for (int e = 0; e < PER; ++e) in |= v[e] >= p_lo && v[e] <= p_hi ? 1u << e : 0u;
   __syncthreads();
   const int mine = __popc(in);
   int at = 0;
@@ -671,7 +680,25 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
     at = __shfl_sync(0xffffffffu, first, 31) + incl - mine;
   }
   __syncthreads();
-  if (threadIdx.x == 0 && s_n > 0) s_at = atomicAdd(&a.plan[row].listed, s_n);
+  if (threadIdx.x == 0 && s_n > 0) s_at = atomicAdd(&a.plan[row].listed, s_n);   // (on its way while the sums are made)
+  if (above) {
+    const Row r = scaled(t);
+    const Scale s(r.hi, r.lo, mj, 0.0f);
+    // (a loop, so that the sums' code is there once)
+#pragma unroll 1
+    for (int turn = 0; turn < 1 + left; ++turn) {
+      const uint64_t sum = bulk_above(v, s, s_pow, top, turn ? below(low) : p_hi, s_room + warp * SEG);
+      if (lane == 0 && turn == 0) *seg = sum;
+      if (lane == 0 && turn == 1 && sum) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(sum));
+    }
+    if (k > 0) {
+      uint32_t n = 0;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) n += v[e] > p_hi;
+      n = __reduce_add_sync(0xffffffffu, n);
+      if (lane == 0 && n) atomicAdd(&a.plan[row].count, static_cast<unsigned long long>(n));
+    }
+  }
   __syncthreads();
   if (mine > 0) {
     uint2* list = a.list + static_cast<int64_t>(row) * CAP;
@@ -681,23 +708,6 @@ __global__ void __launch_bounds__(NT, 2) sample_collect_kernel(const SampleArgs 
       const int e = __ffs(in) - 1, id = base + ((e / N) * 32 + lane) * N + e % N;
       if (at < CAP) list[at] = make_uint2(Key<T>::of(l.one(id)), id);
       ++at;
-    }
-  }
-  if (above) {
-    const Scale s(r.hi, r.lo, plan.mj, 0.0f);
-    // (a loop, so that bulk's code is there once)
-#pragma unroll 1
-    for (int turn = 0; turn < 1 + plan.left; ++turn) {
-      const uint64_t sum = bulk_above(v, s, s_pow, plan.max, turn ? below(low) : plan.hi, s_room + warp * SEG);
-      if (lane == 0 && turn == 0) *seg = sum;
-      if (lane == 0 && turn == 1 && sum) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(sum));
-    }
-    if (r.k > 0) {
-      uint32_t n = 0;
-#pragma unroll
-      for (int e = 0; e < PER; ++e) n += v[e] > plan.hi;
-      n = __reduce_add_sync(0xffffffffu, n);
-      if (lane == 0 && n) atomicAdd(&a.plan[row].count, static_cast<unsigned long long>(n));
     }
   }
 }

@@ -81,6 +81,7 @@ enum Mode : int { kEmpty, kAll, kListed, kWindow, kWhole };
 // the list is kept, too; of the mass, `target` is, or, under min-p, top-p of `mass`, or the cut is by `count`.  kWhole: the last kernel takes the row by itself.
 struct RowPlan {
   float max, lo, hi;                       // the list: lo <= logit <= hi
+  float c_hi, c_lo, none;                  // the scale; see none_of()
   int mode, mj, listed;
   int more;                                // ids below lo may be kept, too
   int left;                                // kWindow: 1 where `mass` is wanted
@@ -196,21 +197,17 @@ struct Row {
   int k;
   float p, mp, t;
 };
-// (t alone)
-__device__ __forceinline__ Row scaled(float t) {
-  Row r{0.0f, 0.0f, 0, 1.0f, 0.0f, t};
-  constexpr double kLog2e = 1.4426950408889634074;
-  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
-  r.hi = L / t;
-  r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, t, L) + LL) / t : 0.0f;   // the division's remainder
-  return r;
-}
 __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
-  Row r = scaled(a.temperature ? a.temperature[row] : 1.0f);
+  Row r;
+  r.t = a.temperature ? a.temperature[row] : 1.0f;
   r.p = a.top_p ? a.top_p[row] : 1.0f;
   r.mp = a.min_p ? a.min_p[row] : 0.0f;
   r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
   if (r.k < 0 || r.k >= a.vocab) r.k = 0;
+  constexpr double kLog2e = 1.4426950408889634074;
+  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
+  r.hi = L / r.t;
+  r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, r.t, L) + LL) / r.t : 0.0f;   // the division's remainder
   return r;
 }
 // f m rounded down (UP: up), for 0 <= f < 1: f's 24 bits times m's 64, shifted.
@@ -292,17 +289,18 @@ struct Sums {
     return sum > 0 ? static_cast<uint64_t>(sum) : 0;
   }
 };
-// stands for a value that is not summed: 2^-60, in no bin
-__device__ __forceinline__ float none_of(const Scale& s, float max) { return fmaxf(max - 60.0f / s.hi, -3.0e38f); }
+// stands for a value that is not summed: 2^-60 of max, in no bin (deep: 60 / hi)
+__device__ __forceinline__ float none_of(float max, float deep) { return fmaxf(max - deep, -3.0e38f); }
+// A value's weight over that of its bin's middle, in 2^-14: as a float's bits where that float counts 2^-149.
+constexpr float kUnit = 0x1p-135f;         // 2^14 of them
+
 
 // Sum of the weights of the values that a warp's lanes hold.
 // BINS: also a histogram by value, bins counted down from gj / per; a value adds its weight over that of its bin's
 // middle, linear in its place within the bin, in 2^-14.  NB words, and 32 for what lies past them.
 template <bool BINS>
-__device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, const float2* pow, float max, float per, int gj, uint32_t hist) {
-  const float none = none_of(s, max);
-  const float b_c = kMagic + static_cast<float>(gj), b_slope = -16384.0f * 0.693147181f * s.hi / per;
-  const uint32_t past = hist + 4u * (NB + (threadIdx.x & 31));   // (a word per lane: no branch, no conflicts)
+__device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, const float2* pow, float none, float per, float slope, int gj, uint32_t hist) {
+  const float b_c = kMagic + static_cast<float>(gj), past = kMagic + static_cast<float>(NB + (threadIdx.x & 31));   // (a word per lane: no branch, no conflicts)
   hist -= 4u * static_cast<uint32_t>(kMagicBits);
   Sums sums;
 #pragma unroll
@@ -310,8 +308,7 @@ __device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, 
     const float x = fmaxf(v[e], none);
     if constexpr (BINS) {
       const float q = fmaf(x, -per, b_c), d = fmaf(x, -per, b_c - q);       // d: from the bin's middle, in bins
-      const uint32_t at = hist + 4u * __float_as_uint(q);
-      add_shared(q < kMagic + NB ? at : past, __float_as_uint(fmaf(d, b_slope, kMagic + 16384.0f)) - kMagicBits);
+      add_shared(hist + 4u * __float_as_uint(q < kMagic + NB ? q : past), __float_as_uint(fmaf(d, slope, kUnit)));
     }
     sums.add(x, s, pow);
   }
@@ -319,9 +316,8 @@ __device__ __forceinline__ uint64_t bulk(const float (&v)[PER], const Scale& s, 
 }
 // Of those above `cut` alone: they are moved together first (room: SEG words of the warp's), since in a nucleus' or a top-k's
 // row they are few.
-__device__ __forceinline__ uint64_t bulk_above(const float (&v)[PER], const Scale& s, const float2* pow, float max, float cut, float* room) {
+__device__ __forceinline__ uint64_t bulk_above(const float (&v)[PER], const Scale& s, const float2* pow, float none, float cut, float* room) {
   const int lane = threadIdx.x & 31;
-  const float none = none_of(s, max);
   cut = fmaxf(cut, none);
   int n = 0;
 #pragma unroll
@@ -426,11 +422,17 @@ __device__ __forceinline__ void load_chunk(const Logits<T>& l, int base, float (
 __device__ __forceinline__ bool wants_mass(const Row& r) { return r.k == 0; }          // draws or cuts by the mass of everything
 __device__ __forceinline__ bool wants_bins(const Row& r) { return r.k > 1 || (r.k == 0 && (r.p < 1.0f || r.mp > 0.0f)); }
 
+// What a block of the first pass needs of its row's settings; made by its first warp.
+struct ScanRow {
+  float hi, lo, per, slope, deep;          // per: bins per logit; slope: see bulk()
+  int sums;                                // 0: none, 1: the mass, 2: with bins
+};
 template <class T>
 __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) {
   __shared__ uint32_t s_hist[NB + 32];
   __shared__ float2 s_pow[16];
   __shared__ float s_max[NW];
+  __shared__ ScanRow s_row;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
   if (threadIdx.x < 16) s_pow[threadIdx.x] = kPowF[threadIdx.x];
   s_hist[threadIdx.x] = 0;
@@ -438,7 +440,11 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
   const Logits<T> l(a, row);
   float v[PER];
   load_chunk(l, chunk * CHUNK + warp * SEG, v);
-  const Row r = row_of(a, row);
+  if (warp == 0) {
+    const Row r = row_of(a, row);
+    const float depth = depth_of(a, r);
+    if (lane == 0) s_row = ScanRow{r.hi, r.lo, r.hi * ((NB - 2) / depth), kUnit * (-0.693147181f / (NB - 2)) * depth, 60.0f / r.hi, r.k == 1 ? 0 : wants_bins(r) ? 2 : 1};
+  }
   const float ninf = __int_as_float(0xff800000);
   float top = ninf;
 #pragma unroll
@@ -447,25 +453,24 @@ __global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) 
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
-  const float per = r.hi * ((NB - 2) / depth_of(a, r));
+  const ScanRow r = s_row;
   ChunkInfo info{top, 0, 0, 0};
+  uint64_t sum = 0;
   if (top > ninf) {
-    const float g = top * per;
+    const float g = top * r.per;
     info.mj = mj_of(r.hi, r.lo, top);
     info.gj = fabsf(g) < static_cast<float>(kFar) ? __float2int_ru(g) : kFar;   // (up: no value rounds to a bin before the first)
     info.far = info.mj == kFar || info.gj == kFar || !(r.hi > 1e-30f);
-    uint64_t sum = 0;
-    if (!info.far && r.k != 1) {
+    if (!info.far && r.sums > 0) {
       const Scale s(r.hi, r.lo, info.mj, 0.0f);
-      sum = wants_bins(r) ? bulk<true>(v, s, s_pow, top, per, info.gj, smem_u32(s_hist)) : bulk<false>(v, s, s_pow, top, 1.0f, 0, 0);
+      const float none = none_of(top, r.deep);
+      sum = r.sums == 2 ? bulk<true>(v, s, s_pow, none, r.per, r.slope, info.gj, smem_u32(s_hist)) : bulk<false>(v, s, s_pow, none, 1.0f, 0.0f, 0, 0);
     }
-    if (lane == 0) a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = sum;
-  } else if (lane == 0) {
-    a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = 0;
   }
+  if (lane == 0) a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = sum;
   __syncthreads();
   if (threadIdx.x == 0) a.info[static_cast<int64_t>(row) * a.chunks + chunk] = info;
-  if (wants_bins(r)) a.hist[(static_cast<int64_t>(row) * a.chunks + chunk) * NB + threadIdx.x] = s_hist[threadIdx.x];
+  if (r.sums == 2) a.hist[(static_cast<int64_t>(row) * a.chunks + chunk) * NB + threadIdx.x] = s_hist[threadIdx.x];
 }
 
 // a number of units of 2^(from / 16) in units of 2^(to / 16), from <= to
@@ -512,7 +517,7 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
   if (lane == 0) s_max[warp] = top;
   __syncthreads();
   top = warp_max(s_max[lane & (NW - 1)]);
-  RowPlan plan{top, top, top, kEmpty, 0, 0, 0, 0, 0, 0, 0, 0};
+  RowPlan plan{top, top, top, r.hi, r.lo, none_of(top, 60.0f / r.hi), kEmpty, 0, 0, 0, 0, 0, 0, 0, 0};
   const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {
     plan.mode = kListed;                                      // the ids of the maximum
@@ -644,11 +649,11 @@ __global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs 
   pdl_enter();
   // (what is read of the plan, the chunk and the settings is asked for at once)
   const RowPlan& to = a.plan[row];
-  const float top = to.max, p_lo = to.lo, p_hi = to.hi, c_max = a.info[static_cast<int64_t>(row) * a.chunks + chunk].max;
+  const float p_lo = to.lo, p_hi = to.hi, none = to.none, c_max = a.info[static_cast<int64_t>(row) * a.chunks + chunk].max;
   const int mode = to.mode, mj = to.mj, left = to.left;
   const uint32_t low_k = to.low;
-  const float t = a.temperature ? a.temperature[row] : 1.0f;
   const int k = a.top_k ? a.top_k[row] : 0;
+  const Scale s(to.c_hi, to.c_lo, mj, 0.0f);
   if (mode != kListed && mode != kWindow) return;
   uint64_t* seg = a.seg + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
   const bool above = mode == kWindow;
@@ -682,12 +687,10 @@ __global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs 
   __syncthreads();
   if (threadIdx.x == 0 && s_n > 0) s_at = atomicAdd(&a.plan[row].listed, s_n);   // (on its way while the sums are made)
   if (above) {
-    const Row r = scaled(t);
-    const Scale s(r.hi, r.lo, mj, 0.0f);
     // (a loop, so that the sums' code is there once)
 #pragma unroll 1
     for (int turn = 0; turn < 1 + left; ++turn) {
-      const uint64_t sum = bulk_above(v, s, s_pow, top, turn ? below(low) : p_hi, s_room + warp * SEG);
+      const uint64_t sum = bulk_above(v, s, s_pow, none, turn ? below(low) : p_hi, s_room + warp * SEG);
       if (lane == 0 && turn == 0) *seg = sum;
       if (lane == 0 && turn == 1 && sum) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(sum));
     }
@@ -938,7 +941,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
         sh.id[i] = id;
       }
     }
-    plan = RowPlan{top, ninf, -ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0, 0};
+    plan = RowPlan{top, ninf, -ninf, r.hi, r.lo, ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0, 0};
   } else {
     plan = a.plan[row];
     const uint2* list = a.list + static_cast<int64_t>(row) * CAP;

@@ -428,7 +428,7 @@ struct ScanRow {
   int sums;                                // 0: none, 1: the mass, 2: with bins
 };
 template <class T>
-__global__ void __launch_bounds__(NT, 2) sample_scan_kernel(const SampleArgs a) {
+__global__ void __launch_bounds__(NT, 3) sample_scan_kernel(const SampleArgs a) {
   __shared__ uint32_t s_hist[NB + 32];
   __shared__ float2 s_pow[16];
   __shared__ float s_max[NW];

@@ -30,15 +30,18 @@
 //                          ids in which the draw falls; the token.
 // Where a list overflows or the guess was wrong, the last one takes the whole
 // row by the same histograms (logits beyond 2^18 T; cuts of thousands of ids
-// by top-k under a second setting).
+// by top-k under a second setting).  Of few rows the last three are one kernel,
+// sample_rest_kernel.
 //
-// Bound: of few rows the four kernels' latency, 4 to 6 us each (a row of 32768
-// ids 21 us); of many the instructions of the two passes over the logits, 54 and 40 an
-// id at 68 % and 55 % of the issue slots (512 rows of 128000, fp32, a nucleus
-// each: 292 us, of which scan 130, collect 124; one reading of the logits is
-// 39).  The row in the shared memory of a cluster of 8 blocks instead, read from
-// HBM once, took 691 us: 38 rows at a time, each some 45 us of passes that end
-// in a cluster barrier.  A pair of values per instruction (f32x2) executes as many
+// Bound: of few rows the chain of small steps, each a barrier or two (a row of 32768
+// ids 16 to 20 us, of which the scan 4); of many the instructions of the two passes
+// over the logits (512 rows of 128000, fp32, a nucleus each: 231 us, of which scan
+// 111 with 46 instructions an id at 71 % of the issue slots, collect 89 with 37 at
+// 74 %; one reading of the logits is 39).  Weights above the cut summed where they
+// lie, without moving them together, 292 us with two blocks an SM.  The row in the
+// shared memory of a cluster of 8 blocks instead, read from HBM once, took 691
+// us: 38 rows at a time, each some 45 us of passes that end in a cluster
+// barrier.  A pair of values per instruction (f32x2) executes as many
 // instructions as one.
 #include <cstdint>
 
@@ -66,7 +69,7 @@ struct SampleArgs {
   float* prob;
   // scratch
   struct ChunkInfo* info;                  // [rows][chunks]
-  uint64_t* seg;                           // [rows][chunks * NW] mass of a warp's ids
+  uint64_t *seg, *kept;                    // [rows][chunks * NW] mass of a warp's ids: as scanned; kAll: in the row's units, kWindow: above the list
   uint32_t* hist;                          // [rows][chunks][NB]
   struct RowPlan* plan;                    // [rows]
   uint2* list;                             // [rows][CAP] key, id
@@ -88,6 +91,7 @@ struct RowPlan {
   uint32_t low;                            // the least key that min-p keeps
   uint64_t target;
   unsigned long long mass, count;          // kWindow, where the cut is by them: mass that min-p leaves, ids above hi
+  int done;                                // chunks that are through (the kernels of few rows)
 };
 
 // ------------------------------------------------------------------ keys
@@ -202,13 +206,21 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   r.t = a.temperature ? a.temperature[row] : 1.0f;
   r.p = a.top_p ? a.top_p[row] : 1.0f;
   r.mp = a.min_p ? a.min_p[row] : 0.0f;
-  r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : a.top_k ? a.top_k[row] : 0;
+  const int k = a.top_k ? a.top_k[row] : 0;                   // (asked for with the others)
+  r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : k;
   if (r.k < 0 || r.k >= a.vocab) r.k = 0;
   constexpr double kLog2e = 1.4426950408889634074;
   constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
   r.hi = L / r.t;
   r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, r.t, L) + LL) / r.t : 0.0f;   // the division's remainder
   return r;
+}
+// p / q, right to an ulp of fp32 (a quotient of doubles takes four times as long).
+__device__ __forceinline__ float ratio(uint64_t p, uint64_t q) {
+  const float ph = __ull2float_rn(p), qh = __ull2float_rn(q);
+  const float pl = static_cast<float>(static_cast<int64_t>(p - static_cast<uint64_t>(ph))), ql = static_cast<float>(static_cast<int64_t>(q - static_cast<uint64_t>(qh)));
+  const float x = ph / qh;
+  return x + (fmaf(-x, qh, ph) + fmaf(-x, ql, pl)) / qh;
 }
 // f m rounded down (UP: up), for 0 <= f < 1: f's 24 bits times m's 64, shifted.
 template <bool UP>
@@ -469,7 +481,10 @@ __global__ void __launch_bounds__(NT, 3) sample_scan_kernel(const SampleArgs a) 
   }
   if (lane == 0) a.seg[(static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) a.info[static_cast<int64_t>(row) * a.chunks + chunk] = info;
+  if (threadIdx.x == 0) {
+    a.info[static_cast<int64_t>(row) * a.chunks + chunk] = info;
+    if (chunk == 0) a.plan[row].listed = 0, a.plan[row].mass = 0, a.plan[row].count = 0, a.plan[row].done = 0;
+  }
   if (r.sums == 2) a.hist[(static_cast<int64_t>(row) * a.chunks + chunk) * NB + threadIdx.x] = s_hist[threadIdx.x];
 }
 
@@ -492,32 +507,36 @@ __device__ __forceinline__ uint32_t low_key(const Row& r, const Scale& s, const 
   if (!(r.mp > 0.0f)) return bottom;
   if (r.mp >= 1.0f || !(max < __int_as_float(0x7f800000))) return top;
   const uint64_t least = ::max(times<true>(r.mp, weight(s, pow, max)), static_cast<uint64_t>(1));
-  return first_key(bottom, top, [&](uint32_t key) { return weight(s, pow, Key<T>::value(key)) >= least; });
+  auto enough = [&](uint32_t key) { return weight(s, pow, Key<T>::value(key)) >= least; };
+  // (near max + T ln(min-p), if it is there)
+  const uint32_t near = Key<T>::of(max + __log2f(r.mp) / r.hi), from = ::max(bottom, near - ::min(near, 400u)), to = ::min(top, near + 400u);
+  if (from < to && enough(to) && (from == bottom || !enough(from - 1))) return first_key(from, to, enough);
+  return first_key(bottom, top, enough);
 }
 
+struct Planner {
+  uint64_t room[NW], front, pow[16];
+  float max[NW], part;
+  int bin, three;
+  ChunkInfo info[(kSampleMaxVocab + CHUNK - 1) / CHUNK];
+};
+// A row's plan, in every thread; `writes`: this block leaves the masses of kAll.  Block-collective.
 template <class T>
-__global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
-  __shared__ uint64_t s_room[NW];
-  __shared__ float s_max[NW];
-  __shared__ int s_bin, s_three;
-  __shared__ float s_part;
-  __shared__ uint64_t s_front, s_pow[16];
-  __shared__ ChunkInfo s_info[(kSampleMaxVocab + CHUNK - 1) / CHUNK];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
-  if (threadIdx.x == 0) s_bin = NB, s_three = 0;
-  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPow[threadIdx.x];
-  pdl_enter();
-  const Row r = row_of(a, row);
+__device__ __forceinline__ RowPlan plan_row(const SampleArgs& a, int row, const Row& r, Planner& sh, bool writes) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) sh.bin = NB, sh.three = 0;
+  if (threadIdx.x < 16) sh.pow[threadIdx.x] = kPow[threadIdx.x];
   const ChunkInfo* info = a.info + static_cast<int64_t>(row) * a.chunks;
-  uint64_t* seg = a.seg + static_cast<int64_t>(row) * a.chunks * NW;
+  const uint64_t* seg = a.seg + static_cast<int64_t>(row) * a.chunks * NW;
   const float ninf = __int_as_float(0xff800000);
   const ChunkInfo mine = threadIdx.x < a.chunks ? info[threadIdx.x] : ChunkInfo{ninf, 0, 0, 0};   // (a row has fewer chunks than threads)
-  if (threadIdx.x < a.chunks) s_info[threadIdx.x] = mine;
+  const uint64_t seg0 = static_cast<int>(threadIdx.x) < a.chunks * NW ? seg[threadIdx.x] : 0;   // (asked for with the others)
+  if (threadIdx.x < a.chunks) sh.info[threadIdx.x] = mine;
   float top = warp_max(mine.max);
-  if (lane == 0) s_max[warp] = top;
+  if (lane == 0) sh.max[warp] = top;
   __syncthreads();
-  top = warp_max(s_max[lane & (NW - 1)]);
-  RowPlan plan{top, top, top, r.hi, r.lo, none_of(top, 60.0f / r.hi), kEmpty, 0, 0, 0, 0, 0, 0, 0, 0};
+  top = warp_max(sh.max[lane & (NW - 1)]);
+  RowPlan plan{top, top, top, r.hi, r.lo, none_of(top, 60.0f / r.hi), kEmpty, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {
     plan.mode = kListed;                                      // the ids of the maximum
@@ -531,19 +550,20 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
     const int gj = __float2int_ru(top * per);
     plan.mj = mj;
     // every mass in the units of the row's maximum
+    auto mass_of = [&](int i) {
+      const ChunkInfo c = sh.info[i / NW];
+      return c.max > ninf && !c.far ? rescale(i < NT ? seg0 : seg[i], c.mj, mj) : 0;
+    };
     uint64_t mass = 0;
     if (wants_mass(r)) {
       uint64_t own = 0;
       for (int i = threadIdx.x; i < a.chunks * NW; i += NT) {
-        const ChunkInfo c = s_info[i / NW];
-        const uint64_t x = c.max > ninf && !c.far ? rescale(seg[i], c.mj, mj) : 0;
-        seg[i] = x;
-        own += x;
+        own += mass_of(i);
       }
-      scan_block(own, s_room, &mass);
+      scan_block(own, sh.room, &mass);
       __syncthreads();
     }
-    plan.low = low_key<T>(r, Scale(r.hi, r.lo, mj, 0.0f), s_pow, top);
+    plan.low = low_key<T>(r, Scale(r.hi, r.lo, mj, 0.0f), sh.pow, top);
     plan.mode = kAll;
     plan.lo = ninf, plan.hi = -ninf;
     if (wants_bins(r)) {
@@ -551,19 +571,19 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
       uint64_t n = 0;
 #pragma unroll 4
       for (int c = 0; c < a.chunks; ++c) {
-        const ChunkInfo x = s_info[c];
+        const ChunkInfo x = sh.info[c];
         const int bin = static_cast<int>(threadIdx.x) - (gj - x.gj);
         if (x.max > ninf && !x.far && bin >= 0 && bin < NB) n += a.hist[(static_cast<int64_t>(row) * a.chunks + c) * NB + bin];
       }
       auto edge = [&](float bin) { return (static_cast<float>(gj) - bin) / per; };
-      const uint64_t count = (n + 8192) >> 14, in_front = scan_block(count, s_room);
+      const uint64_t count = (n + 8192) >> 14, in_front = scan_block(count, sh.room);
       __syncthreads();
       int b = NB;
       // the place in its bin, too: the guess of a mass is good to some 10^-4
       auto cross = [&](uint64_t own, uint64_t incl, uint64_t target) {
         if (incl >= target && incl - own < target) {
-          s_bin = threadIdx.x;
-          s_part = static_cast<float>(target - (incl - own)) / static_cast<float>(own);
+          sh.bin = threadIdx.x;
+          sh.part = static_cast<float>(target - (incl - own)) / static_cast<float>(own);
         }
       };
       if (r.k > 1) {
@@ -578,21 +598,21 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
           guess = last >= 1.0f ? guess : last > 0.0f ? static_cast<uint64_t>(static_cast<float>(guess) * last) : 0;
         }
         uint64_t all;
-        const uint64_t incl = scan_block(guess, s_room, &all);
+        const uint64_t incl = scan_block(guess, sh.room, &all);
         cross(guess, incl, r.mp <= 0.0f ? plan.target >> 12 : target_of(r.p, all));
       }
       float lo = ninf;
       if (r.mp > 0.0f) lo = Key<T>::value(plan.low);
       __syncthreads();
-      b = s_bin;
+      b = sh.bin;
       plan.mode = kListed;
       // ids from a value on, about
       auto ids_from = [&](float value) {
         const int low = min(NB - 1, max(0, static_cast<int>(static_cast<float>(gj) - value * per) + 1));
         __syncthreads();
-        if (threadIdx.x == low) s_front = in_front;
+        if (threadIdx.x == low) sh.front = in_front;
         __syncthreads();
-        return s_front;
+        return sh.front;
       };
       const bool few_mp = r.mp > 0.0f && ids_from(lo) < CAP * 3 / 4;
       if (few_mp || (r.k == 0 && r.p >= 1.0f)) {
@@ -622,10 +642,10 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
         } else if (again) {
           plan.mode = kWhole;
         } else {
-          if (threadIdx.x == max(0, b - 1) || threadIdx.x == b || threadIdx.x == b + 1) atomicAdd(&s_three, static_cast<int>(min(count, static_cast<uint64_t>(1 << 24))));
+          if (threadIdx.x == max(0, b - 1) || threadIdx.x == b || threadIdx.x == b + 1) atomicAdd(&sh.three, static_cast<int>(min(count, static_cast<uint64_t>(1 << 24))));
           __syncthreads();
-          const float most = CAP * 0.6f, three = static_cast<float>(s_three);
-          const float half = three <= most ? 1.5f : fmaxf(0.05f, 1.5f * most / three), mid = three <= most ? b : b - 0.5f + s_part;
+          const float most = CAP * 0.6f, three = static_cast<float>(sh.three);
+          const float half = three <= most ? 1.5f : fmaxf(0.05f, 1.5f * most / three), mid = three <= most ? b : b - 0.5f + sh.part;
           plan.mode = kWindow;
           lo = fmaxf(lo, edge(mid + half));
           plan.hi = edge(mid - half);
@@ -634,31 +654,34 @@ __global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
       plan.lo = lo;
       plan.left = plan.mode == kWindow && r.k == 0 && r.mp > 0.0f && r.p < 1.0f;
     }
+    if (plan.mode == kAll && writes) {
+      uint64_t* kept = a.kept + static_cast<int64_t>(row) * a.chunks * NW;
+      for (int i = threadIdx.x; i < a.chunks * NW; i += NT) kept[i] = mass_of(i);
+    }
   }
-  if (threadIdx.x == 0) a.plan[row] = plan;
+  return plan;
+}
+template <class T>
+__global__ void __launch_bounds__(NT) sample_plan_kernel(const SampleArgs a) {
+  __shared__ Planner sh;
+  pdl_enter();
+  const RowPlan plan = plan_row<T>(a, blockIdx.x, row_of(a, blockIdx.x), sh, true);
+  if (threadIdx.x == 0) a.plan[blockIdx.x] = plan;
 }
 
+struct Collector {
+  float2 pow[16];
+  int n, at;
+};
+// A chunk's part, by plan `to`; c_max: the chunk's maximum; room: CHUNK words.  Block-collective.
 template <class T>
-__global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs a) {
-  __shared__ float2 s_pow[16];
-  __shared__ float s_room[CHUNK];
-  __shared__ int s_n, s_at;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
-  if (threadIdx.x < 16) s_pow[threadIdx.x] = kPowF[threadIdx.x];
-  if (threadIdx.x == 0) s_n = 0;
-  pdl_enter();
-  // (what is read of the plan, the chunk and the settings is asked for at once)
-  const RowPlan& to = a.plan[row];
-  const float p_lo = to.lo, p_hi = to.hi, none = to.none, c_max = a.info[static_cast<int64_t>(row) * a.chunks + chunk].max;
-  const int mode = to.mode, mj = to.mj, left = to.left;
-  const uint32_t low_k = to.low;
-  const int k = a.top_k ? a.top_k[row] : 0;
-  const Scale s(to.c_hi, to.c_lo, mj, 0.0f);
-  if (mode != kListed && mode != kWindow) return;
-  uint64_t* seg = a.seg + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
-  const bool above = mode == kWindow;
+__device__ __forceinline__ void collect_chunk(const SampleArgs& a, int row, int chunk, const RowPlan& to, float c_max, int k, Collector& sh, float* room) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float p_lo = to.lo, p_hi = to.hi;
+  uint64_t* seg = a.kept + (static_cast<int64_t>(row) * a.chunks + chunk) * NW + warp;
+  const bool above = to.mode == kWindow;
   // (a chunk with nothing to list or to add; what min-p leaves may lie lower)
-  const float low = Key<T>::value(low_k), least = left ? low : above ? fminf(p_lo, p_hi) : p_lo;
+  const float low = Key<T>::value(to.low), least = to.left ? low : above ? fminf(p_lo, p_hi) : p_lo;
   if (c_max < least) {
     if (above && lane == 0) *seg = 0;
     return;
@@ -681,16 +704,17 @@ __global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs 
       if (lane >= o) incl += x;
     }
     int first = 0;
-    if (lane == 31) first = atomicAdd(&s_n, incl);
+    if (lane == 31) first = atomicAdd(&sh.n, incl);
     at = __shfl_sync(0xffffffffu, first, 31) + incl - mine;
   }
   __syncthreads();
-  if (threadIdx.x == 0 && s_n > 0) s_at = atomicAdd(&a.plan[row].listed, s_n);   // (on its way while the sums are made)
+  if (threadIdx.x == 0 && sh.n > 0) sh.at = atomicAdd(&a.plan[row].listed, sh.n);   // (on its way while the sums are made)
   if (above) {
+    const Scale s(to.c_hi, to.c_lo, to.mj, 0.0f);
     // (a loop, so that the sums' code is there once)
 #pragma unroll 1
-    for (int turn = 0; turn < 1 + left; ++turn) {
-      const uint64_t sum = bulk_above(v, s, s_pow, none, turn ? below(low) : p_hi, s_room + warp * SEG);
+    for (int turn = 0; turn < 1 + to.left; ++turn) {
+      const uint64_t sum = bulk_above(v, s, sh.pow, to.none, turn ? below(low) : p_hi, room + warp * SEG);
       if (lane == 0 && turn == 0) *seg = sum;
       if (lane == 0 && turn == 1 && sum) atomicAdd(&a.plan[row].mass, static_cast<unsigned long long>(sum));
     }
@@ -705,7 +729,7 @@ __global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs 
   __syncthreads();
   if (mine > 0) {
     uint2* list = a.list + static_cast<int64_t>(row) * CAP;
-    at += s_at;
+    at += sh.at;
     constexpr int N = Vec<T>::N;
     for (; in; in &= in - 1) {             // (few: read once more)
       const int e = __ffs(in) - 1, id = base + ((e / N) * 32 + lane) * N + e % N;
@@ -713,6 +737,23 @@ __global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs 
       ++at;
     }
   }
+}
+template <class T>
+__global__ void __launch_bounds__(NT, 3) sample_collect_kernel(const SampleArgs a) {
+  __shared__ Collector sh;
+  __shared__ float s_room[CHUNK];
+  const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
+  if (threadIdx.x < 16) sh.pow[threadIdx.x] = kPowF[threadIdx.x];
+  if (threadIdx.x == 0) sh.n = 0;
+  pdl_enter();
+  // (what is read of the plan, the chunk and the settings is asked for at once)
+  const RowPlan& from = a.plan[row];
+  RowPlan to;
+  to.mode = from.mode, to.lo = from.lo, to.hi = from.hi, to.none = from.none, to.c_hi = from.c_hi, to.c_lo = from.c_lo;
+  to.mj = from.mj, to.left = from.left, to.low = from.low;
+  const float c_max = a.info[static_cast<int64_t>(row) * a.chunks + chunk].max;
+  const int k = a.top_k ? a.top_k[row] : 0;
+  if (to.mode == kListed || to.mode == kWindow) collect_chunk<T>(a, row, chunk, to, c_max, k, sh, s_room);
 }
 
 // ------------------------------------------------------------------ the cut and the draw
@@ -783,9 +824,12 @@ struct Finisher {
   // lo .. hi are not looked at.  False: the cut is not there.
   template <bool BY_MASS>
   __device__ bool narrow(const Cut& from, uint32_t lo, uint32_t hi, uint64_t above, uint64_t target, Cut* cut) {
-    uint32_t inside = 0xffffffffu;         // candidates in the window
+    uint32_t inside = whole ? 0xffffffffu : sh.n;   // candidates in the window, at most
     if (above >= target) return false;
     bool by_value = hi == Key<T>::of(max); // first by value, in steps of equal ratios of weights; then by key
+    float per = 0.0f;
+    int only = -1;                         // the bin by value that the few candidates are in
+    auto value_bin = [&](uint32_t key) { return min(NB - 1, static_cast<int>((max - Key<T>::value(key)) * per)); };
     while (lo < hi && inside > LIST) {
       sh.count[threadIdx.x] = 0;
 #pragma unroll
@@ -794,10 +838,9 @@ struct Finisher {
       __syncthreads();
       const float range = max - Key<T>::value(lo);
       by_value = by_value && range < 3e38f;
-      const float per = by_value ? (NB - 1) / range : 0.0f;
+      per = by_value ? (NB - 1) / range : 0.0f;
       int shift = 0;
       while (((hi - lo) >> shift) >= NB) ++shift;
-      auto value_bin = [&](uint32_t key) { return min(NB - 1, static_cast<int>((max - Key<T>::value(key)) * per)); };
       each([&](uint32_t key, int id) {
         if (key < lo || key > hi || !kept(from, key, id)) return;
         const int bin = by_value ? value_bin(key) : static_cast<int>((hi - key) >> shift);
@@ -831,6 +874,10 @@ struct Finisher {
       above = sh.d_above;
       if (by_value) {
         const int b = static_cast<int>(bin);
+        if (inside <= LIST) {
+          only = b;
+          break;
+        }
         const uint32_t lo2 = first_key(lo, hi, [&](uint32_t k) { return value_bin(k) <= b; });
         if (b > 0) hi = first_key(lo2, hi, [&](uint32_t k) { return value_bin(k) <= b - 1; }) - 1;
         lo = lo2;
@@ -883,7 +930,7 @@ struct Finisher {
     if (threadIdx.x == 0) sh.few = 0, sh.d_id = 0xffffffffu;
     __syncthreads();
     each([&](uint32_t key, int id) {
-      if (key < lo || key > hi || !kept(from, key, id)) return;
+      if (key < lo || key > hi || !kept(from, key, id) || (only >= 0 && value_bin(key) != only)) return;
       const int i = atomicAdd(&sh.few, 1);
       sh.few_key[i] = key;
       sh.few_id[i] = id;
@@ -912,20 +959,14 @@ struct Finisher {
   }
 };
 
-// DIRECT: rows of up to CAP ids, nothing ran ahead.
+// The cut and the token.  DIRECT: rows of up to CAP ids, nothing ran ahead (and `plan` is made here); sh.n is 0 and sh.pow there.
+// What other blocks left is read from L2.  Block-collective.
 template <class T, bool DIRECT>
-__global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  Finish& sh = *reinterpret_cast<Finish*>(smem);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x;
+__device__ __forceinline__ void finish_row(const SampleArgs& a, int row, const Row& r, RowPlan plan, Finish& sh) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float ninf = __int_as_float(0xff800000);
-  if (threadIdx.x < 16) sh.pow[threadIdx.x] = kPow[threadIdx.x];
-  if (threadIdx.x == 0) sh.n = 0;
-  pdl_enter();
   const Logits<T> l(a, row);
-  const Row r = row_of(a, row);
   const float u = a.u[row];
-  RowPlan plan;
   if constexpr (DIRECT) {
     float top = ninf;
     for (int id = threadIdx.x; id < a.vocab; id += NT) top = fmaxf(top, l.one(id));
@@ -941,15 +982,15 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
         sh.id[i] = id;
       }
     }
-    plan = RowPlan{top, ninf, -ninf, r.hi, r.lo, ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0, 0};
+    plan = RowPlan{top, ninf, -ninf, r.hi, r.lo, ninf, top > ninf ? kListed : kEmpty, r.hi > 1e-30f ? mj_of(r.hi, r.lo, top) : kFar, 0, 0, 0, 0, 0, 0, 0, 0};
   } else {
-    plan = a.plan[row];
     const uint2* list = a.list + static_cast<int64_t>(row) * CAP;
     if (plan.mode == kListed || plan.mode == kWindow) {
+      uint2 x = __ldcg(list + threadIdx.x);                     // (asked for before its length is known)
       if (plan.listed > CAP) plan.mode = kWhole;
       else
         for (int i = threadIdx.x; i < plan.listed; i += NT) {
-          const uint2 x = list[i];
+          if (i >= NT) x = __ldcg(list + i);
           sh.key[i] = x.x;
           sh.id[i] = x.y;
         }
@@ -981,12 +1022,12 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
     return;
   }
   // ---- the cut: min-p, top-k, top-p
-  const uint64_t* seg = DIRECT ? nullptr : a.seg + static_cast<int64_t>(row) * a.chunks * NW;
+  const uint64_t* seg = DIRECT ? nullptr : a.kept + static_cast<int64_t>(row) * a.chunks * NW;
   const int segs = (a.vocab + SEG - 1) / SEG;
   uint64_t above = 0;
   if (!DIRECT && plan.mode == kWindow) {
     uint64_t own = 0;
-    for (int i = threadIdx.x; i < segs; i += NT) own += seg[i];
+    for (int i = threadIdx.x; i < segs; i += NT) own += __ldcg(seg + i);
     above = f.sum(own);
   }
   const Cut low{DIRECT || far || plan.mode == kWhole ? low_key<T>(r, f.s, sh.pow, plan.max) : ::max(plan.low, kinf), ALL};
@@ -997,30 +1038,31 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
       bool ok = true;
       cut = low;
       Cut to{};
-      if (window) {
-        const uint32_t lo = ::max(cut.key, Key<T>::of(plan.lo)), hi = Key<T>::of(plan.hi);
-        if (r.k > 0) ok = f.template narrow<false>(cut, lo, hi, plan.count, r.k, &to);
-        else if (r.p < 1.0f) ok = f.template narrow<true>(cut, lo, hi, above, r.mp > 0.0f ? target_of(r.p, plan.mass) : plan.target, &to);
-        if (ok && (r.k > 0 || r.p < 1.0f)) cut = to;
-      } else {
-        if (r.k > 0) {
-          if (f.template narrow<false>(cut, cut.key, khi, 0, r.k, &to)) cut = to;
-          else ok = f.whole || !plan.more; // (fewer than k candidates: all of them)
-        }
-        if (ok && r.p < 1.0f) {
-          uint64_t target = plan.target;
+      uint32_t lo = window ? ::max(cut.key, Key<T>::of(plan.lo)) : cut.key;
+      const uint32_t hi = window ? Key<T>::of(plan.hi) : khi;
+      if (r.k > 0) {
+        ok = f.template narrow<false>(cut, lo, hi, window ? plan.count : 0, r.k, &to);
+        if (ok) cut = to;
+        else ok = !window && (f.whole || !plan.more);           // (fewer than k candidates: all of them)
+      }
+      if (ok && r.p < 1.0f && !(window && r.k > 0)) {           // (a window is there for one cut)
+        uint64_t target = plan.target;
+        if (window) {
+          if (r.mp > 0.0f) target = target_of(r.p, plan.mass);
+        } else {
           if (DIRECT || f.whole || far || r.k > 0 || r.mp > 0.0f) {
             uint64_t own = 0;
             f.each([&](uint32_t key, int id) { own += f.kept(cut, key, id) ? f.w(Key<T>::value(key)) : 0; });
             const uint64_t mass = f.sum(own);
             target = target_of(r.p, mass);
           }
-          uint32_t lo = cut.key;
+          lo = cut.key;
           if (r.hi > 1e-30f) lo = ::max(lo, Key<T>::of(plan.max - 46.0f / r.hi));
-          ok = f.template narrow<true>(cut, min(lo, khi), khi, 0, target, &to);
-          if (ok) cut = to;
-          ok = ok || f.whole;
+          lo = min(lo, khi);
         }
+        ok = f.template narrow<true>(cut, lo, hi, window ? above : 0, target, &to);
+        if (ok) cut = to;
+        else ok = f.whole;
       }
       if (ok) break;
       f.whole = true;
@@ -1029,7 +1071,7 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
   }
   // ---- the draw: the masses of 512 ids each
   for (int i = threadIdx.x; i < static_cast<int>(sizeof(sh.seg) / 8); i += NT)
-    sh.seg[i] = !DIRECT && (window || plan.mode == kAll) && i < segs ? seg[i] : 0, sh.seg2[0][i] = sh.seg2[1][i] = 0;
+    sh.seg[i] = !DIRECT && (window || plan.mode == kAll) && i < segs ? __ldcg(seg + i) : 0, sh.seg2[0][i] = sh.seg2[1][i] = 0;
   __syncthreads();
   if (f.whole) {
     constexpr int N = Vec<T>::N;
@@ -1094,8 +1136,54 @@ __global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
   __syncthreads();
   if (threadIdx.x == 0) {
     a.tok[row] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(sh.d_best));
-    if (a.prob) a.prob[row] = static_cast<float>(static_cast<double>(sh.d_w) / static_cast<double>(mass));
+    if (a.prob) a.prob[row] = ratio(sh.d_w, mass);
   }
+}
+template <class T, bool DIRECT>
+__global__ void __launch_bounds__(NT) sample_finish_kernel(const SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Finish& sh = *reinterpret_cast<Finish*>(smem);
+  if (threadIdx.x < 16) sh.pow[threadIdx.x] = kPow[threadIdx.x];
+  if (threadIdx.x == 0) sh.n = 0;
+  pdl_enter();
+  finish_row<T, DIRECT>(a, blockIdx.x, row_of(a, blockIdx.x), DIRECT ? RowPlan{} : a.plan[blockIdx.x], sh);
+}
+
+// Few rows: plan, collect and finish in one launch.  Every block plans its row for itself; the one that is through last with its
+// chunk finishes the row.  (No block waits for another.)
+template <class T>
+__global__ void __launch_bounds__(NT, 2) sample_rest_kernel(const SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  Finish& sh = *reinterpret_cast<Finish*>(smem);
+  static_assert(sizeof(Planner) <= sizeof(Finish) && CHUNK * 4 <= sizeof(Finish), "the parts take turns");
+  __shared__ Collector s_c;
+  __shared__ int s_last;
+  const int row = blockIdx.x / a.chunks, chunk = blockIdx.x - row * a.chunks;
+  if (threadIdx.x < 16) s_c.pow[threadIdx.x] = kPowF[threadIdx.x];
+  if (threadIdx.x == 0) s_c.n = 0;
+  pdl_enter();
+  const Row r = row_of(a, row);
+  RowPlan plan = plan_row<T>(a, row, r, *reinterpret_cast<Planner*>(smem), chunk == 0);
+  __syncthreads();
+  if (plan.mode == kListed || plan.mode == kWindow) {
+    const float c_max = a.info[static_cast<int64_t>(row) * a.chunks + chunk].max;
+    collect_chunk<T>(a, row, chunk, plan, c_max, r.k, s_c, reinterpret_cast<float*>(smem));
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) s_last = atomicAdd(&a.plan[row].done, 1) == a.chunks - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    plan.listed = __ldcg(&a.plan[row].listed);
+    plan.mass = __ldcg(&a.plan[row].mass);
+    plan.count = __ldcg(&a.plan[row].count);
+  } else if (chunk != 0) {
+    return;
+  }
+  if (threadIdx.x < 16) sh.pow[threadIdx.x] = kPow[threadIdx.x];
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+  finish_row<T, false>(a, row, r, plan, sh);
 }
 
 template <class... KArgs, class... Args>
@@ -1116,6 +1204,7 @@ size_t place(SampleArgs* a, int rows, int vocab, uint8_t* base) {
   };
   a->info = reinterpret_cast<ChunkInfo*>(take(n * chunks * sizeof(ChunkInfo)));
   a->seg = reinterpret_cast<uint64_t*>(take(n * chunks * NW * sizeof(uint64_t)));
+  a->kept = reinterpret_cast<uint64_t*>(take(n * chunks * NW * sizeof(uint64_t)));
   a->hist = reinterpret_cast<uint32_t*>(take(n * chunks * NB * sizeof(uint32_t)));
   a->plan = reinterpret_cast<RowPlan*>(take(n * sizeof(RowPlan)));
   a->list = reinterpret_cast<uint2*>(take(n * CAP * sizeof(uint2)));
@@ -1126,11 +1215,12 @@ template <class T>
 cudaError_t run(const SampleArgs& a, cudaStream_t s) {
   static PerDevice ready;
   int dev = 0;
-  cudaGetDevice(&dev);
+  const int sms = current_sms(&dev);
   cudaError_t e = cudaSuccess;
   const int smem = static_cast<int>(sizeof(Finish));
   if (ready.get(dev, [&] {
         e = cudaFuncSetAttribute(sample_finish_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_rest_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_finish_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         return e == cudaSuccess ? 1 : 0;
       }) <= 0)
@@ -1138,6 +1228,9 @@ cudaError_t run(const SampleArgs& a, cudaStream_t s) {
   if (a.chunks == 0) return start(sample_finish_kernel<T, true>, a.rows, smem, s, a);
   const int64_t blocks = static_cast<int64_t>(a.rows) * a.chunks;
   if ((e = start(sample_scan_kernel<T>, blocks, 0, s, a)) != cudaSuccess) return e;
+  // a block an SM: two launches for four (3 us less of the host's time per call), and every block's own plan costs no more than
+  // one per row.  4 rows of 32768 ids and 9 of 128000 18.3 -> 17.3 and 27 -> 26 us; at three blocks an SM 32.6 -> 33 and 34 -> 39.
+  if (blocks <= sms) return start(sample_rest_kernel<T>, blocks, smem, s, a);
   if ((e = start(sample_plan_kernel<T>, a.rows, 0, s, a)) != cudaSuccess) return e;
   if ((e = start(sample_collect_kernel<T>, blocks, 0, s, a)) != cudaSuccess) return e;
   return start(sample_finish_kernel<T, false>, a.rows, smem, s, a);

@@ -677,10 +677,11 @@ def test_the_first_calls_of_a_process_can_be_captured(T):
     assert r.returncode == 0 and r.stdout.strip() == "captured", r.stderr[-2000:]
 
 
-def test_sample_rows_of_every_kind_in_one_call(T):
+@pytest.mark.parametrize("rows", [24, 120])
+def test_sample_rows_of_every_kind_in_one_call(T, rows):
     """Rows that are drawn from the whole, from a list, from a window, from nothing, and from one id, side by side: each as alone."""
     g = gen(40)
-    rows, vocab = 24, 20000
+    vocab = 20000
     x = 2.0 * randn(g, rows, vocab)
     x[3], x[9, 5:] = -math.inf, -math.inf
     x[4] = 0.5

@@ -141,7 +141,7 @@ __device__ __forceinline__ int make_lists(const DownArgs& a, int tile, int32_t* 
     const int32_t* cu = cached ? s_cu : a.cu;
     int lo = 0, hi = a.batch + 1;          // boundaries <= row: in lo .. hi
     while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
+      const int mid = lo + (hi - lo) / 2;
       if (cu[mid] <= row) lo = mid + 1;
       else hi = mid;
     }

@@ -5,10 +5,14 @@
 //
 // The second product runs in the tile of the first: after the k-blocks of W
 // come, for each adapter that a row of the tile has, k-blocks of B_a against
-// h with the other rows' h taken as zero.  Bound: shared-memory reads of the
-// 2 x 2 products per thread, and for few rows the latency of a k-block (four
-// prompts of 228 rows, 256 -> 768, rank 8: 16 us; tiles of 64 x 64, 48 blocks
-// of them, 57).
+// h with the other rows' h taken as zero.  W's blocks run while h is made: the
+// kernel waits for its predecessor before the first block of h (x, W and the
+// sequences were there when that one had waited for what came before it).
+// Bound: the latency of the steps in front of the first products (where the
+// rows lie, their adapters, the first blocks), then shared-memory reads of the
+// 2 x 2 products per thread (four prompts of 228 rows, 256 -> 768, rank 8: 10.9
+// us; blocks fetched one ahead into registers, a warp per row for its adapter and
+// no overlap, 15.8; tiles of 64 x 64, 48 blocks of them, 57).
 #include <cstdint>
 
 #include "ragged.cuh"
@@ -47,6 +51,7 @@ __global__ void __launch_bounds__(256) lora_down_kernel(const LoraRowsArgs a) {
   const float4* x = reinterpret_cast<const float4*>(a.x + row * a.ldx);
   const float4* p = reinterpret_cast<const float4*>(a.a + (static_cast<int64_t>(ad) * a.rank + r0) * a.n_in);
   const int n4 = a.n_in / 4;
+  const float by = a.scale[ad];
   float s[8] = {};
 #pragma unroll 2
   for (int k = lane; k < n4; k += 32) {
@@ -63,91 +68,103 @@ __global__ void __launch_bounds__(256) lora_down_kernel(const LoraRowsArgs a) {
     float mine = 0.0f;
 #pragma unroll
     for (int r = 0; r < 8; ++r) mine = lane == r ? s[r] : mine;
-    a.h[static_cast<int64_t>(row) * a.rank + r0 + lane] = mine * a.scale[ad];
+    a.h[static_cast<int64_t>(row) * a.rank + r0 + lane] = mine * by;
   }
 }
 
-// Tiles of 32 x 32 outputs (a few short prompts give many of them), K in blocks of 64 that are fetched one ahead: 256
-// threads with 2 x 2 outputs and a float4 of each operand for each half of the block.
-constexpr int TM = 32, TN = 32, TKB = 64;
+// Tiles of 32 x 32 outputs (a few short prompts give many of them), K in blocks of 64 that come in a ring of asynchronous
+// copies: 256 threads with 2 x 2 outputs and two 16-byte pieces of each operand per block.
+constexpr int TM = 32, TN = 32, TKB = 64, RING = 3, LD = TKB + 4;
+constexpr int R_SMEM = RING * (TM + TN) * LD * 4;
+
+// 16 bytes into shared memory, zeros where not `in`
+__device__ __forceinline__ void copy16(float* to, const float* from, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(in ? 16 : 0) : "memory");
+}
 
 __global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
-  __shared__ __align__(16) float sx[2][TM][TKB + 4], sw[2][TN][TKB + 4];
+  extern __shared__ __align__(16) float smem[];
+  float(*sx)[TM][LD] = reinterpret_cast<float(*)[TM][LD]>(smem);
+  float(*sw)[TN][LD] = reinterpret_cast<float(*)[TN][LD]>(smem + RING * TM * LD);
   __shared__ int s_ad[TM], s_list[TM], s_n;
   const int m0 = blockIdx.y * TM, n0 = blockIdx.x * TN, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_enter();
   const int lr = threadIdx.x >> 3, lk = (threadIdx.x & 7) * 4;   // a row of either operand, its elements lk .. and 32 + lk ..
-  const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  const float* px = a.x + (m0 + lr) * a.ldx;
-  const float* pw = a.w + (n0 + lr) * a.ldw;
   const bool x_in = m0 + lr < a.total, w_in = n0 + lr < a.n_out;
-  float4 fx[2], fw[2];
-  auto fetch = [&](int k0) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int k = k0 + 32 * i + lk;
-      fx[i] = x_in && k < a.n_in ? *reinterpret_cast<const float4*>(px + k) : zero;
-      fw[i] = w_in && k < a.n_in ? *reinterpret_cast<const float4*>(pw + k) : zero;
+  const float* px = a.x + static_cast<int64_t>(x_in ? m0 + lr : 0) * a.ldx;
+  const float* pw = a.w + static_cast<int64_t>(w_in ? n0 + lr : 0) * a.ldw;
+  const int main = (a.n_in + TKB - 1) / TKB, per = (a.rank + TKB - 1) / TKB;   // blocks of x and W; of h and B, per adapter
+  bool waited = false;
+  int blocks = main;
+  // block i of K into its place of the ring; past the last one nothing
+  auto ask = [&](int i) {
+    if (i >= main && !waited) {            // h comes from the kernel before; x, W and the sequences were there when that one ran
+      pdl_enter();
+      waited = true;
     }
+    if (i < blocks) {
+      const bool ext = i >= main;
+      const int e = i - main, ad = ext ? s_list[e / per] : 0, k0 = (ext ? e % per : i) * TKB, width = ext ? a.rank : a.n_in;
+      const float* x = ext ? a.h + static_cast<int64_t>(x_in ? m0 + lr : 0) * a.rank : px;
+      const float* w = ext ? a.b + (static_cast<int64_t>(ad) * a.n_out + (w_in ? n0 + lr : 0)) * a.rank : pw;
+      const bool x_on = ext ? s_ad[lr] == ad : x_in;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int k = k0 + 32 * p + lk;
+        copy16(&sx[i % RING][lr][32 * p + lk], k < width ? x + k : x, x_on && k < width);
+        copy16(&sw[i % RING][lr][32 * p + lk], k < width ? w + k : w, w_in && k < width);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  fetch(0);
-  for (int i = warp; i < TM; i += 8) {
-    const int ad = adapter_of(a, m0 + i);
-    if (lane == 0) s_ad[i] = ad;
-  }
-  __syncthreads();
-  if (warp == 0) {                               // the tile's adapters, in the order of their first rows
-    const int ad = s_ad[lane];
-    bool first = ad >= 0;
-    for (int j = 0; j < lane; ++j) first = first && s_ad[j] != ad;
+  static_assert(RING == 3, "two blocks ahead");
+  ask(0);
+  if (main > 1) ask(1);
+  if (warp == 0) {
+    // a row per lane: its adapter (-1 none, -2: it is in no sequence), and the list of them in the order of their first rows
+    const int row = m0 + lane;
+    int lo = 0, hi = a.batch + 1;                // boundaries <= row: in lo .. hi
+    while (lo < hi) {
+      const int mid = lo + (hi - lo) / 2;
+      if (a.cu[mid] <= row) lo = mid + 1;
+      else hi = mid;
+    }
+    int ad = -2;
+    if (row < a.total && lo >= 1 && lo <= a.batch) {
+      ad = a.adapter[lo - 1];
+      if (ad < 0 || ad >= a.n_adapters) ad = -1;
+    }
+    s_ad[lane] = ad;
+    const unsigned same = __match_any_sync(0xffffffffu, ad);    // (every lane calls it)
+    const bool first = ad >= 0 && __ffs(same) - 1 == lane;
     const unsigned have = __ballot_sync(0xffffffffu, first);
     if (first) s_list[__popc(have & ((1u << lane) - 1))] = ad;
     if (lane == 0) s_n = __popc(have);
   }
+  __syncthreads();
+  blocks = main + s_n * per;
+  if (main == 1) ask(1);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   float acc[2][2] = {};
-  int buf = 0;
-  auto put = [&]() {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      *reinterpret_cast<float4*>(&sx[buf][lr][32 * i + lk]) = fx[i];
-      *reinterpret_cast<float4*>(&sw[buf][lr][32 * i + lk]) = fw[i];
-    }
-    __syncthreads();
-  };
-  auto multiply = [&]() {
-#pragma unroll
-    for (int k = 0; k < TKB; k += 4) {
-      const float4 x0 = *reinterpret_cast<const float4*>(&sx[buf][ty][k]), x1 = *reinterpret_cast<const float4*>(&sx[buf][ty + 16][k]);
-      const float4 w0 = *reinterpret_cast<const float4*>(&sw[buf][tx][k]), w1 = *reinterpret_cast<const float4*>(&sw[buf][tx + 16][k]);
+  for (int i = 0; i < blocks; ++i) {
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncthreads();                             // (the block is there; the one before has been read)
+    ask(i + 2);
+    const auto &x = sx[i % RING], &w = sw[i % RING];
+    auto step = [&](int k) {
+      const float4 x0 = *reinterpret_cast<const float4*>(&x[ty][k]), x1 = *reinterpret_cast<const float4*>(&x[ty + 16][k]);
+      const float4 w0 = *reinterpret_cast<const float4*>(&w[tx][k]), w1 = *reinterpret_cast<const float4*>(&w[tx + 16][k]);
       auto dot = [](const float4& p, const float4& q, float s) { return fmaf(p.w, q.w, fmaf(p.z, q.z, fmaf(p.y, q.y, fmaf(p.x, q.x, s)))); };
       acc[0][0] = dot(x0, w0, acc[0][0]);
       acc[0][1] = dot(x0, w1, acc[0][1]);
       acc[1][0] = dot(x1, w0, acc[1][0]);
       acc[1][1] = dot(x1, w1, acc[1][1]);
-    }
-    buf ^= 1;                                    // (the other buffer's readers have passed the barrier in put())
-  };
-  for (int k0 = 0; k0 < a.n_in; k0 += TKB) {
-    put();
-    if (k0 + TKB < a.n_in) fetch(k0 + TKB);
-    multiply();
-  }
-  __syncthreads();
-  for (int i = 0; i < s_n; ++i) {
-    const int ad = s_list[i];
-    const bool mine = s_ad[lr] == ad;
-    const float* ph = a.h + static_cast<int64_t>(m0 + lr) * a.rank;
-    const float* pb = a.b + (static_cast<int64_t>(ad) * a.n_out + n0 + lr) * a.rank;
-    for (int k0 = 0; k0 < a.rank; k0 += TKB) {
+    };
+    const int left = i < main ? TKB : a.rank - (i - main) % per * TKB;   // (ranks come in eights)
+    if (left >= TKB) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = k0 + 32 * h + lk;
-        fx[h] = mine && k < a.rank ? *reinterpret_cast<const float4*>(ph + k) : zero;
-        fw[h] = w_in && k < a.rank ? *reinterpret_cast<const float4*>(pb + k) : zero;
-      }
-      put();
-      multiply();
+      for (int k = 0; k < TKB; k += 4) step(k);
+    } else {
+      for (int k = 0; k < left; k += 8) step(k), step(k + 4);
     }
   }
 #pragma unroll
@@ -169,8 +186,17 @@ const char* lora_rows(const LoraCall& c, cudaStream_t s) {
   const LoraRowsArgs a{f(c.x), f(c.w), f(c.a), f(c.b), static_cast<float*>(c.y), c.cu, c.adapter, c.scale, static_cast<float*>(c.scratch),
                        c.batch, c.total, c.n_in, c.n_out, c.n_adapters, c.rank, c.ldx, c.ldw, c.ldy};
   const int64_t items = static_cast<int64_t>(c.total) * (c.rank / 8);
-  cudaError_t e = launch_pdl(lora_down_kernel, static_cast<unsigned>((items + 7) / 8), 256, 0, s, a);
-  if (e == cudaSuccess) e = launch_pdl(lora_rows_kernel, dim3((c.n_out + TN - 1) / TN, (c.total + TM - 1) / TM), 256, 0, s, a);
+  static PerDevice ready;
+  int dev = 0;
+  cudaGetDevice(&dev);
+  cudaError_t e = cudaSuccess;
+  if (ready.get(dev, [&] {
+        e = cudaFuncSetAttribute(lora_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R_SMEM);
+        return e == cudaSuccess ? 1 : 0;
+      }) <= 0)
+    return cudaGetErrorString(e);
+  e = launch_pdl(lora_down_kernel, static_cast<unsigned>((items + 7) / 8), 256, 0, s, a);
+  if (e == cudaSuccess) e = launch_pdl(lora_rows_kernel, dim3((c.n_out + TN - 1) / TN, (c.total + TM - 1) / TM), 256, R_SMEM, s, a);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 

@@ -444,14 +444,18 @@ __global__ void __launch_bounds__(G_THREADS, 1)
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const int units = a.p.tiles * a.n_tiles_n, u0 = blockIdx.x / (2 * KS), ustep = gridDim.x / (2 * KS);
+  // tiles with rows of a sequence (buffers may be longer)
+  const int r_lo = max(a.cu[0], 0), r_hi = min(a.cu[a.batch], a.total), t0 = r_lo / TR;
+  const int tiles = r_hi > r_lo ? (r_hi + TR - 1) / TR - t0 : 0;
+  const int units = tiles * a.n_tiles_n, u0 = blockIdx.x / (2 * KS), ustep = gridDim.x / (2 * KS);
   auto place = [&](int u, int& mt, int& nt) {
     if (a.m_fast) {
-      nt = u / a.p.tiles;
-      mt = u - nt * a.p.tiles;
+      nt = u / tiles;
+      mt = t0 + u - nt * tiles;
     } else {
       mt = u / a.n_tiles_n;
       nt = u - mt * a.n_tiles_n;
+      mt += t0;
     }
   };
   const int k0 = a.kblocks * pair / KS, k1 = a.kblocks * (pair + 1) / KS;   // this pair's blocks of x and W (at least one)
@@ -565,7 +569,6 @@ __global__ void __launch_bounds__(G_THREADS, 1)
     const int quad = warp & 3, part = (warp - 2) / 4;         // 32 rows, half of the columns
     uint8_t* box = boxes + (warp - 2) * BOX_BYTES;
     const uint32_t tempty_l = cluster_addr(tempty, lead), lanes = static_cast<uint32_t>(quad * 32) << 16;
-    const int r_lo = max(a.cu[0], 0), r_hi = min(a.cu[a.batch], a.total);
     int acc = 0;
     uint32_t acc_phase = 0;
     for (int u = u0; u < units; u += ustep) {
@@ -621,7 +624,6 @@ __global__ void __launch_bounds__(G_THREADS, 1)
       int mt, nt;
       place(u0, mt, nt);
       const int quad = warp & 3, part = (warp - 2) / 4, row0 = mt * TR + half * 128 + quad * 32;
-      const int r_lo = max(a.cu[0], 0), r_hi = min(a.cu[a.batch], a.total);
       uint8_t* box = boxes + (warp - 2) * BOX_BYTES;
       const float4* s_d = reinterpret_cast<const float4*>(smem);
       if (row0 < r_hi && row0 + 32 > r_lo) {

@@ -138,9 +138,15 @@ __global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
     const bool first = ad >= 0 && __ffs(same) - 1 == lane;
     const unsigned have = __ballot_sync(0xffffffffu, first);
     if (first) s_list[__popc(have & ((1u << lane) - 1))] = ad;
-    if (lane == 0) s_n = __popc(have);
+    const unsigned rows = __ballot_sync(0xffffffffu, ad > -2);
+    if (lane == 0) s_n = rows ? __popc(have) : -1;
   }
   __syncthreads();
+  if (s_n < 0) {                                 // rows of no sequence (buffers may be longer than what is in use)
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    pdl_enter();                                 // (no block is through before the kernel in front)
+    return;
+  }
   blocks = main + s_n * per;
   if (main == 1) ask(1);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;

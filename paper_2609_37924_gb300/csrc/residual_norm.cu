@@ -8,7 +8,7 @@
 // x and y are read once, x' and n written once, everything between is fp32 in
 // registers; n is made from x' before it is rounded to its own type.
 //
-// Bound: HBM, (2 es_x + es_y + es_n) bytes per element: 11512 rows of 5376 (fp32 x, bf16 y) 134 us, 5.5 TB/s, 82 % of a
+// Bound: HBM, (2 es_x + es_y + es_n) bytes per element: 11512 rows of 5376 (fp32 x, bf16 y) 123 us, 6.0 TB/s, 89 % of a
 // plain copy's rate; 1024 rows of 2048 in bf16 4.4 us out of L2; one row 3.5 us, the launch.
 #include <cstdint>
 
@@ -63,15 +63,30 @@ __device__ __forceinline__ void st8(bf16* p, const float (&v)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// eight parameters as they lie in memory
+// four consecutive elements: what 32 lanes store at once are whole lines
+__device__ __forceinline__ void ld4(const float* p, float (&v)[4]) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+}
+__device__ __forceinline__ void ld4(const bf16* p, float (&v)[4]) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
+  v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
+}
+__device__ __forceinline__ void st4(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void st4(bf16* p, const float (&v)[4]) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+  *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+// four parameters as they lie in memory
 template <class T>
-struct Raw8 {
-  uint4 q[sizeof(T) / 2];
+struct Raw4 {
+  alignas(sizeof(T) * 4) uint32_t q[sizeof(T)];
   __device__ __forceinline__ void load(const T* p) {
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4*>(q) = *reinterpret_cast<const uint4*>(p);
+    else *reinterpret_cast<uint2*>(q) = *reinterpret_cast<const uint2*>(p);
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const { ld8(reinterpret_cast<const T*>(q), v); }
+  __device__ __forceinline__ void get(float (&v)[4]) const { ld4(reinterpret_cast<const T*>(q), v); }
 };
 
 // Sum over the threads that share a row: a warp (WARPS 1) or the block.
@@ -164,7 +179,8 @@ __global__ void __launch_bounds__(BLOCK ? 1024 : 256) norm_reg_kernel(const Norm
 
 // Many rows: blocks that stay, each with the rows of its next RING turns on the way into shared memory by bulk copies, so
 // that the loads go on while a row waits for its sums.  (11512 rows of 5376, fp32 x and bf16 y: a block per row, which loads,
-// sums, and stores one after the other, 157 us; blocks of 256 threads 153; gains read for every row, 149; 134 as it is.)
+// sums, and stores one after the other, 157 us; blocks of 256 threads 153; gains read for every row, 149; eight elements a
+// thread instead of four, whose 16-byte stores of fp32 fill half sectors, 134; 123 as it is.)
 constexpr int RT = 512, RING = 3, kRingBytes = 112 * 1024;   // two blocks an SM
 template <class XT, class YT>
 __host__ __device__ constexpr int ring_stage(int d) { return d * static_cast<int>(sizeof(XT) + sizeof(YT)); }
@@ -175,7 +191,7 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
   __shared__ float red[2][32];
   __shared__ __align__(8) uint64_t full[RING];
   __shared__ int abort_flag;
-  const int nvec = a.d / 8, stage_bytes = ring_stage<XT, YT>(a.d), step = gridDim.x;
+  const int nvec = a.d / 4, stage_bytes = ring_stage<XT, YT>(a.d), step = gridDim.x;
   const uint32_t xb = a.d * sizeof(XT), yb = a.d * sizeof(YT);
   if (threadIdx.x == 0) {
     for (int i = 0; i < RING; ++i) mbar_init(&full[i], 1);
@@ -194,12 +210,12 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
     for (int i = 0; i < RING; ++i)
       if (static_cast<int>(blockIdx.x) + i * step < a.total) ask(blockIdx.x + i * step, i);
   const T *post = static_cast<const T*>(a.post), *pre = static_cast<const T*>(a.pre), *gate = static_cast<const T*>(a.gate);
-  Raw8<T> g_post[NV], g_pre[NV];           // the same for every row
+  Raw4<T> g_post[NV], g_pre[NV];           // the same for every row
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = threadIdx.x + i * RT;
-    if (c < nvec && post) g_post[i].load(post + 8 * c);
-    if (c < nvec && pre) g_pre[i].load(pre + 8 * c);
+    if (c < nvec && post) g_post[i].load(post + 4 * c);
+    if (c < nvec && pre) g_pre[i].load(pre + 4 * c);
   }
   int stage = 0;
   uint32_t phase = 0;
@@ -208,16 +224,16 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
     if (__syncthreads_or(!mbar_wait_bounded(&full[stage], phase, &abort_flag, a.status))) break;
     const XT* x = reinterpret_cast<const XT*>(smem + stage * stage_bytes);
     const YT* y = reinterpret_cast<const YT*>(smem + stage * stage_bytes + xb);
-    float v[NV][8], w[8];
+    float v[NV][4], w[4];
     float r = 1.0f, s = 0.0f;
     if (post) {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         const int c = threadIdx.x + i * RT;
         if (c < nvec) {
-          ld8(y + 8 * c, w);
+          ld4(y + 4 * c, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s = fmaf(w[e], w[e], s);
+          for (int e = 0; e < 4; ++e) s = fmaf(w[e], w[e], s);
         }
       }
       r = rsqrtf(row_sum<true>(s, red[0]) / static_cast<float>(a.d) + a.eps);
@@ -227,21 +243,21 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
     for (int i = 0; i < NV; ++i) {
       const int c = threadIdx.x + i * RT;
       if (c < nvec) {
-        float u[8];
-        ld8(y + 8 * c, u);
-        ld8(x + 8 * c, v[i]);
+        float u[4];
+        ld4(y + 4 * c, u);
+        ld4(x + 4 * c, v[i]);
         if (post) {
           g_post[i].get(w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) u[e] = u[e] * r * w[e];
+          for (int e = 0; e < 4; ++e) u[e] = u[e] * r * w[e];
         }
         if (gate && b >= 0) {
-          ld8(gate + b * a.ldg + 8 * c, w);
+          ld4(gate + b * a.ldg + 4 * c, w);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) u[e] *= w[e];
+          for (int e = 0; e < 4; ++e) u[e] *= w[e];
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
           v[i][e] = fmaf(a.alpha, v[i][e], u[e]);
           s = fmaf(v[i][e], v[i][e], s);
         }
@@ -255,12 +271,12 @@ __global__ void __launch_bounds__(RT, 2) norm_ring_kernel(const NormArgs a) {
     for (int i = 0; i < NV; ++i) {
       const int c = threadIdx.x + i * RT;
       if (c < nvec) {
-        st8(static_cast<XT*>(a.xo) + row * a.ldxo + 8 * c, v[i]);
+        st4(static_cast<XT*>(a.xo) + row * a.ldxo + 4 * c, v[i]);
         if (!a.no) continue;
         if (pre) g_pre[i].get(w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = pre ? v[i][e] * q * w[e] : v[i][e] * q;
-        st8(static_cast<T*>(a.no) + row * a.ldn + 8 * c, v[i]);
+        for (int e = 0; e < 4; ++e) v[i][e] = pre ? v[i][e] * q * w[e] : v[i][e] * q;
+        st4(static_cast<T*>(a.no) + row * a.ldn + 4 * c, v[i]);
       }
     }
   }
@@ -329,7 +345,12 @@ cudaError_t launch(const NormArgs& a, bool vec, cudaStream_t s) {
   const int sms = current_sms(&dev);
   // rows enough for a few turns of every block, and wide enough for a block (narrow ones: a warp each, many at once)
   if (vec && nvec > 128 && nvec <= 2 * RT && a.total >= 8 * sms && RING * ring_stage<XT, YT>(a.d) <= kRingBytes)
-    return nvec <= RT ? launch_ring<XT, YT, T, 1>(a, dev, sms, s) : launch_ring<XT, YT, T, 2>(a, dev, sms, s);
+    switch ((a.d / 4 + RT - 1) / RT) {
+      case 1: return launch_ring<XT, YT, T, 1>(a, dev, sms, s);
+      case 2: return launch_ring<XT, YT, T, 2>(a, dev, sms, s);
+      case 3: return launch_ring<XT, YT, T, 3>(a, dev, sms, s);
+      default: return launch_ring<XT, YT, T, 4>(a, dev, sms, s);
+    }
   if (vec && nvec <= 128) {
     const int rows = 8, grid = (a.total + rows - 1) / rows;
     if (nvec <= 32) return launch_pdl(norm_reg_kernel<XT, YT, T, 1, false>, grid, 32 * rows, 0, s, a);

@@ -8,11 +8,12 @@
 // h with the other rows' h taken as zero.  W's blocks run while h is made: the
 // kernel waits for its predecessor before the first block of h (x, W and the
 // sequences were there when that one had waited for what came before it).
-// Bound: the latency of the steps in front of the first products (where the
-// rows lie, their adapters, the first blocks), then shared-memory reads of the
-// 2 x 2 products per thread (four prompts of 228 rows, 256 -> 768, rank 8: 10.9
-// us; blocks fetched one ahead into registers, a warp per row for its adapter and
-// no overlap, 15.8; tiles of 64 x 64, 48 blocks of them, 57).
+// Bound: of few rows the latency of the steps in front of the first products
+// (where the rows lie, their adapters, the first blocks) and the 2 x 2 products
+// per thread between reads of shared memory (four prompts of 228 rows, 256 ->
+// 768, rank 8: 10.9 us; blocks fetched one ahead into registers, a warp per row
+// for its adapter and no overlap, 15.8); of many the FMA and shared-memory
+// pipes (2020 rows, 768 -> 2304: 200 us, 37 TFLOP/s).
 #include <cstdint>
 
 #include "ragged.cuh"
@@ -72,26 +73,26 @@ __global__ void __launch_bounds__(256) lora_down_kernel(const LoraRowsArgs a) {
   }
 }
 
-// Tiles of 32 x 32 outputs (a few short prompts give many of them), K in blocks of 64 that come in a ring of asynchronous
-// copies: 256 threads with 2 x 2 outputs and two 16-byte pieces of each operand per block.
-constexpr int TM = 32, TN = 32, TKB = 64, RING = 3, LD = TKB + 4;
-constexpr int R_SMEM = RING * (TM + TN) * LD * 4;
+// Tiles of 16 R x 16 R outputs, K in blocks of 64 that come in a ring of asynchronous copies: 256 threads with R x R outputs
+// and R 16-byte pieces of each operand per block.  R = 2 gives the many tiles that few rows need, R = 4 reads half as much
+// shared memory per product.
+constexpr int TKB = 64, RING = 3, LD = TKB + 4;
+constexpr int ring_bytes(int R) { return RING * 2 * 16 * R * LD * 4; }
 
 // 16 bytes into shared memory, zeros where not `in`
 __device__ __forceinline__ void copy16(float* to, const float* from, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(in ? 16 : 0) : "memory");
 }
 
-__global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
+template <int R>
+__global__ void __launch_bounds__(256, R == 2 ? 4 : 2) lora_rows_kernel(const LoraRowsArgs a) {
+  constexpr int TM = 16 * R;
   extern __shared__ __align__(16) float smem[];
   float(*sx)[TM][LD] = reinterpret_cast<float(*)[TM][LD]>(smem);
-  float(*sw)[TN][LD] = reinterpret_cast<float(*)[TN][LD]>(smem + RING * TM * LD);
+  float(*sw)[TM][LD] = reinterpret_cast<float(*)[TM][LD]>(smem + RING * TM * LD);
   __shared__ int s_ad[TM], s_list[TM], s_n;
-  const int m0 = blockIdx.y * TM, n0 = blockIdx.x * TN, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int lr = threadIdx.x >> 3, lk = (threadIdx.x & 7) * 4;   // a row of either operand, its elements lk .. and 32 + lk ..
-  const bool x_in = m0 + lr < a.total, w_in = n0 + lr < a.n_out;
-  const float* px = a.x + static_cast<int64_t>(x_in ? m0 + lr : 0) * a.ldx;
-  const float* pw = a.w + static_cast<int64_t>(w_in ? n0 + lr : 0) * a.ldw;
+  const int m0 = blockIdx.y * TM, n0 = blockIdx.x * TM, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int lr = threadIdx.x >> 4, lk = (threadIdx.x & 15) * 4;   // rows lr, lr + 16 .. of either operand, their elements lk ..
   const int main = (a.n_in + TKB - 1) / TKB, per = (a.rank + TKB - 1) / TKB;   // blocks of x and W; of h and B, per adapter
   bool waited = false;
   int blocks = main;
@@ -103,15 +104,16 @@ __global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
     }
     if (i < blocks) {
       const bool ext = i >= main;
-      const int e = i - main, ad = ext ? s_list[e / per] : 0, k0 = (ext ? e % per : i) * TKB, width = ext ? a.rank : a.n_in;
-      const float* x = ext ? a.h + static_cast<int64_t>(x_in ? m0 + lr : 0) * a.rank : px;
-      const float* w = ext ? a.b + (static_cast<int64_t>(ad) * a.n_out + (w_in ? n0 + lr : 0)) * a.rank : pw;
-      const bool x_on = ext ? s_ad[lr] == ad : x_in;
+      const int e = i - main, ad = ext ? s_list[e / per] : 0, k = (ext ? e % per : i) * TKB + lk;
+      const bool k_in = k < (ext ? a.rank : a.n_in);
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int k = k0 + 32 * p + lk;
-        copy16(&sx[i % RING][lr][32 * p + lk], k < width ? x + k : x, x_on && k < width);
-        copy16(&sw[i % RING][lr][32 * p + lk], k < width ? w + k : w, w_in && k < width);
+      for (int p = 0; p < R; ++p) {
+        const int r = lr + 16 * p, m = m0 + r, n = n0 + r;
+        const bool x_on = k_in && m < a.total && (!ext || s_ad[r] == ad), w_on = k_in && n < a.n_out;
+        const float* x = ext ? a.h + static_cast<int64_t>(m) * a.rank : a.x + m * a.ldx;
+        const float* w = ext ? a.b + (static_cast<int64_t>(ad) * a.n_out + n) * a.rank : a.w + n * a.ldw;
+        copy16(&sx[i % RING][r][lk], x_on ? x + k : a.x, x_on);
+        copy16(&sw[i % RING][r][lk], w_on ? w + k : a.w, w_on);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -121,25 +123,32 @@ __global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
   if (main > 1) ask(1);
   if (warp == 0) {
     // a row per lane: its adapter (-1 none, -2: it is in no sequence), and the list of them in the order of their first rows
-    const int row = m0 + lane;
-    int lo = 0, hi = a.batch + 1;                // boundaries <= row: in lo .. hi
-    while (lo < hi) {
-      const int mid = lo + (hi - lo) / 2;
-      if (a.cu[mid] <= row) lo = mid + 1;
-      else hi = mid;
+    auto adapter_at = [&](int row) {
+      int lo = 0, hi = a.batch + 1;              // boundaries <= row: in lo .. hi
+      while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (a.cu[mid] <= row) lo = mid + 1;
+        else hi = mid;
+      }
+      if (row >= a.total || lo < 1 || lo > a.batch) return -2;
+      const int ad = a.adapter[lo - 1];
+      return ad >= 0 && ad < a.n_adapters ? ad : -1;
+    };
+    int n = 0;
+    bool any = false;
+    for (int r = 0; r < TM; r += 32) {
+      const int ad = adapter_at(m0 + r + lane);
+      s_ad[r + lane] = ad;
+      const unsigned same = __match_any_sync(0xffffffffu, ad);  // (every lane calls it)
+      bool first = ad >= 0 && __ffs(same) - 1 == lane;
+      for (int j = 0; j < n; ++j) first = first && s_list[j] != ad;
+      const unsigned have = __ballot_sync(0xffffffffu, first);
+      any = any || __any_sync(0xffffffffu, ad > -2);
+      if (first) s_list[n + __popc(have & ((1u << lane) - 1))] = ad;
+      n += __popc(have);
+      __syncwarp();
     }
-    int ad = -2;
-    if (row < a.total && lo >= 1 && lo <= a.batch) {
-      ad = a.adapter[lo - 1];
-      if (ad < 0 || ad >= a.n_adapters) ad = -1;
-    }
-    s_ad[lane] = ad;
-    const unsigned same = __match_any_sync(0xffffffffu, ad);    // (every lane calls it)
-    const bool first = ad >= 0 && __ffs(same) - 1 == lane;
-    const unsigned have = __ballot_sync(0xffffffffu, first);
-    if (first) s_list[__popc(have & ((1u << lane) - 1))] = ad;
-    const unsigned rows = __ballot_sync(0xffffffffu, ad > -2);
-    if (lane == 0) s_n = rows ? __popc(have) : -1;
+    if (lane == 0) s_n = any ? n : -1;
   }
   __syncthreads();
   if (s_n < 0) {                                 // rows of no sequence (buffers may be longer than what is in use)
@@ -150,20 +159,23 @@ __global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
   blocks = main + s_n * per;
   if (main == 1) ask(1);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  float acc[2][2] = {};
+  float acc[R][R] = {};
   for (int i = 0; i < blocks; ++i) {
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     __syncthreads();                             // (the block is there; the one before has been read)
     ask(i + 2);
     const auto &x = sx[i % RING], &w = sw[i % RING];
     auto step = [&](int k) {
-      const float4 x0 = *reinterpret_cast<const float4*>(&x[ty][k]), x1 = *reinterpret_cast<const float4*>(&x[ty + 16][k]);
-      const float4 w0 = *reinterpret_cast<const float4*>(&w[tx][k]), w1 = *reinterpret_cast<const float4*>(&w[tx + 16][k]);
-      auto dot = [](const float4& p, const float4& q, float s) { return fmaf(p.w, q.w, fmaf(p.z, q.z, fmaf(p.y, q.y, fmaf(p.x, q.x, s)))); };
-      acc[0][0] = dot(x0, w0, acc[0][0]);
-      acc[0][1] = dot(x0, w1, acc[0][1]);
-      acc[1][0] = dot(x1, w0, acc[1][0]);
-      acc[1][1] = dot(x1, w1, acc[1][1]);
+      float4 p[R], q[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        p[r] = *reinterpret_cast<const float4*>(&x[ty + 16 * r][k]);
+        q[r] = *reinterpret_cast<const float4*>(&w[tx + 16 * r][k]);
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < R; ++c) acc[r][c] = fmaf(p[r].w, q[c].w, fmaf(p[r].z, q[c].z, fmaf(p[r].y, q[c].y, fmaf(p[r].x, q[c].x, acc[r][c]))));
     };
     const int left = i < main ? TKB : a.rank - (i - main) % per * TKB;   // (ranks come in eights)
     if (left >= TKB) {
@@ -174,11 +186,11 @@ __global__ void __launch_bounds__(256) lora_rows_kernel(const LoraRowsArgs a) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < R; ++i) {
     const int m = m0 + ty + 16 * i;
     if (s_ad[ty + 16 * i] == -2) continue;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < R; ++j)
       if (n0 + tx + 16 * j < a.n_out) a.y[m * a.ldy + n0 + tx + 16 * j] = acc[i][j];
   }
 }
@@ -194,15 +206,22 @@ const char* lora_rows(const LoraCall& c, cudaStream_t s) {
   const int64_t items = static_cast<int64_t>(c.total) * (c.rank / 8);
   static PerDevice ready;
   int dev = 0;
-  cudaGetDevice(&dev);
+  const int sms = current_sms(&dev);
   cudaError_t e = cudaSuccess;
   if (ready.get(dev, [&] {
-        e = cudaFuncSetAttribute(lora_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, R_SMEM);
+        e = cudaFuncSetAttribute(lora_rows_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(2));
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(lora_rows_kernel<4>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(4));
         return e == cudaSuccess ? 1 : 0;
       }) <= 0)
     return cudaGetErrorString(e);
   e = launch_pdl(lora_down_kernel, static_cast<unsigned>((items + 7) / 8), 256, 0, s, a);
-  if (e == cudaSuccess) e = launch_pdl(lora_rows_kernel, dim3((c.n_out + TN - 1) / TN, (c.total + TM - 1) / TM), 256, R_SMEM, s, a);
+  auto grid = [&](int tile) { return dim3((c.n_out + tile - 1) / tile, (c.total + tile - 1) / tile); };
+  const dim3 wide = grid(64);
+  // 64 x 64 from a tile for every other SM on (84 tiles, 768 -> 768: 32 us instead of 45; 96 tiles, 256 -> 768: 24.5 instead of
+  // 22; 1152 tiles, 768 -> 2304: 200 instead of 318); fewer are quicker as 32 x 32 (48 tiles, 768 -> 768: 25 instead of 30)
+  if (e == cudaSuccess)
+    e = 2 * static_cast<int64_t>(wide.x) * wide.y >= sms ? launch_pdl(lora_rows_kernel<4>, wide, 256, ring_bytes(4), s, a)
+                                                         : launch_pdl(lora_rows_kernel<2>, grid(32), 256, ring_bytes(2), s, a);
   return e == cudaSuccess ? nullptr : cudaGetErrorString(e);
 }
 

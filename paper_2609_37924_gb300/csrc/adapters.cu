@@ -28,9 +28,8 @@
 // its predecessor has waited for what came before, so x and W are there).
 //
 // Bound: of prompts the tensor pipe (24 prompts, 5874 rows, 2048 -> 4096, 6
-// adapters of rank 16: 64 us, of which the product 62 at 84 % of the pipe; the
-// FLOP alone are 52; 384 tiles on 76 pairs are 5.05 rounds, taken in 6, tiles of
-// 192 columns 77 us, of 128 100); of few rows the chain of the two kernels: h
+// adapters of rank 16: 64 us, of which the product 59 at 83 % of the pipe; the
+// FLOP alone are 52; tiles of 192 columns 77 us, of 128 100); of few rows the chain of the two kernels: h
 // after 10 us (lists 2, x A^T 2 to 5, sums 3), then its blocks (64 tokens, 40 adapters:
 // 22 us; 256 rows, 5376 -> 8192, rank 64: 36, of which W's 88 MB are 13).  Blocks of
 // h and B cost 0.4 us each against 0.25 of x and W: B comes in rows of 32 bytes.

@@ -619,6 +619,45 @@ def test_calls_in_a_graph_and_on_streams(T):
         assert torch.equal(p, q) and torch.equal(p, r)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("lens", [[3, 1, 0, 9], [200, 1, 333, 50]])
+def test_a_chain_of_calls_is_that_of_calls_one_by_one(T, dtype, lens):
+    """Each call reads what the one before wrote, in buffers and scratch memory that all share, with nothing between them."""
+    g = gen(33)
+    d, n = 256, 3
+    cu, total = cum(lens), sum(lens)
+    cu_t, ad_t = i32(cu), i32([i % (n + 1) - 1 for i in range(len(lens))])
+    w, a, b = (randn(g, *sh).to(dtype) / 16 for sh in ((d, d), (n, 16, d), (n, d, 16)))
+    scale, gain = torch.ones(n, device="cuda"), (1 + 0.1 * randn(g, d)).to(dtype)
+    need = T.tadm_lora_scratch_size(len(lens), total, d, d, n, 16, 1 if dtype == BF16 else 0)
+    scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+    x0, u = randn(g, total, d).to(dtype), torch.rand(total, generator=g, device="cuda")
+    x, y, z = (torch.zeros((total, d), dtype=dtype, device="cuda") for _ in range(3))
+    wide, logits = (randn(g, 6000, d) / 4).to(dtype), torch.zeros((total, 6000), device="cuda")
+    tok = torch.zeros(total, dtype=torch.int32, device="cuda")
+    p = torch.full((total,), 0.9, device="cuda")
+    room = torch.empty(T.tadm_sample_scratch_size(total, 6000), dtype=torch.uint8, device="cuda")
+
+    def run(between):
+        toks = []
+        x.copy_(x0), z.zero_()
+        for _ in range(4):
+            T.tadm_residual_norm(x, z, x, y, cu_rows=cu_t, pre_gain=gain), between()
+            T.tadm_lora_project(y, w, z, cu_t, ad_t, a, b, scale, scratch), between()
+            T.tadm_residual_norm(x, z, x, y, cu_rows=cu_t, post_gain=gain, pre_gain=gain), between()
+            T.tadm_lora_project(y, w, z, cu_t, ad_t, a, b, scale, scratch), between()
+            T.tadm_gemm(z, wide, logits, dtype=1 if dtype == BF16 else 0), between()
+            T.tadm_sample(logits, u, tok, top_p=p, scratch=room), between()
+            toks.append(tok.clone())
+        return [x.clone(), y.clone(), z.clone()] + toks
+
+    want = run(torch.cuda.synchronize)
+    for _ in range(10):
+        for got, ref in zip(run(lambda: None), want):
+            assert torch.equal(got, ref)
+    T.tadm_ragged_sync_status()
+
+
 def test_a_serving_step(T):
     """A layer and a draw of ragged prompts as a server runs them: norm, QKV with adapters, packed attention, output
     projection with adapters, residual and norm, logits, sampling; each stage against 64 bits from what the one before gave."""

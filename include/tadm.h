@@ -708,8 +708,8 @@ TADM_API tadm_status tadm_sample(const void* logits, int64_t ld, int rows, int v
  * their rows of A and columns of B), total_rows and n_out up to 2^20, batch up to 2^30 (TADM_ERR_UNSUPPORTED above).  y must not overlap the
  * inputs.
  *
- * Sums are fp32.  bf16 calls carry A_a x (times the scale) to 16 significant
- * bits.  W and the adapters that the call uses hold finite values; other adapters
+ * Sums are fp32.  bf16 calls carry A_a x (times the scale) to 24 significant
+ * bits, in three bf16 terms.  W and the adapters that the call uses hold finite values; other adapters
  * are not read, and x of a row, whatever it holds, reaches that row alone.
  * scratch: at least tadm_lora_scratch_size() bytes, 16-byte aligned; it needs no
  * initialisation, and calls that overlap on the GPU need one each.  Waits are

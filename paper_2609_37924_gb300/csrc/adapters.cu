@@ -10,9 +10,13 @@
 //
 //   y_tile = [x | h_a1 | h_a2 ...] [W | B_a1 | B_a2 ...]^T
 //
-// h is carried as two bf16 terms, hi and lo = h - hi, that multiply the same
-// 16 columns of B (so it has 16 significant bits: y then is as near as from an
-// fp32 h, for 2 x 16 more steps of K per 16 ranks).
+// h is carried as three bf16 terms, each the rounding of what the ones before
+// leave of it, that multiply the same 16 columns of B: 24 bits, h as fp32 has
+// it, for 3 x 16 more steps of K per 16 ranks.  (With two, 16 bits, y was off by
+// up to 2^-18 of an adapter's part: of the bf16 outputs of prompts 1.55 in 1000
+// were not the nearest to the exact value instead of 1.16, which are as many as
+// of rows without an adapter, from the matrix unit's sums, which truncate.)
+// The terms of four groups of 16 ranks lie one behind the other in three blocks.
 //
 // Two launches:
 //   lora_down_kernel    each cluster finds the adapters of its tile's rows, then x A^T for
@@ -51,7 +55,16 @@ namespace {
 constexpr int TR = 256;                    // rows of a tile
 constexpr int BK = 64;
 constexpr int G = 16;                      // ranks of a group
-constexpr int KB_BYTES = TR * BK * 2;      // a block of h: 256 rows x (hi, lo of two groups)
+constexpr int TERMS = 3;                   // of h
+constexpr int PLACES = BK / G;             // of a block of h: term i of group g is at place TERMS g + i of the tile's blocks
+constexpr int KB_BYTES = TR * BK * 2;      // a block of h
+__host__ __device__ constexpr int blocks_of(int groups) { return (TERMS * groups + PLACES - 1) / PLACES; }
+__host__ __device__ constexpr int first_group(int block) { return PLACES * block / TERMS; }
+__host__ __device__ constexpr int last_group(int block, int groups) {
+  const int last = (PLACES * block + PLACES - 1) / TERMS;
+  return last < groups ? last : groups - 1;
+}
+static_assert(PLACES <= TERMS + 1, "a block has terms of two groups at most");
 
 // What the first kernel leaves for the second, and its place in the scratch memory.
 struct Plan {
@@ -60,7 +73,7 @@ struct Plan {
   int32_t* list;                           // [tiles][cap]
   bf16* h;                                 // [slots][TR][64]
   int tiles, cap, slots, groups;           // cap: most adapters of a tile; groups: of 16 ranks per adapter
-  int by_seq;                              // where a tile's blocks of h begin: by its first sequence, or by the tile
+  int by_seq, step;                        // where a tile's blocks of h begin: `step` for each sequence in front, or for each tile
 };
 size_t up(size_t n, size_t to) { return (n + to - 1) / to * to; }
 Plan make_plan(int batch, int total, int n_adapters, int rank, uint8_t* scratch, size_t* bytes) {
@@ -69,9 +82,10 @@ Plan make_plan(int batch, int total, int n_adapters, int rank, uint8_t* scratch,
   p.groups = (rank + G - 1) / G;
   p.cap = std::max(1, std::min(std::min(TR, batch), n_adapters));
   // blocks of h: a tile has at most cap adapters; all tiles together at most as many as there are sequences and tiles
-  const int64_t per_tile = (static_cast<int64_t>(p.cap) * p.groups + 1) / 2, per_seq = (p.groups + 1) / 2;
-  const int64_t by_tile = p.tiles * per_tile, by_seq = (static_cast<int64_t>(batch) + p.tiles) * per_seq;
+  const int per_tile = blocks_of(p.cap * p.groups), per_seq = blocks_of(p.groups);
+  const int64_t by_tile = static_cast<int64_t>(p.tiles) * per_tile, by_seq = (static_cast<int64_t>(batch) + p.tiles) * per_seq;
   p.by_seq = by_seq < by_tile;
+  p.step = p.by_seq ? per_seq : per_tile;
   p.slots = static_cast<int>(std::min<int64_t>(std::min(by_tile, by_seq), INT32_MAX / TR));
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -218,9 +232,9 @@ __global__ void __launch_bounds__(D_THREADS, 1)
   for (int th = blockIdx.x / CS % (per * halves) % halves, c0 = blockIdx.x / CS / halves; th < halves && c0 < per; th += clusters) {
     const int t = th >> 1, half = th & 1, row0 = th * 128;
     const int n_list = make_lists(a, t, reinterpret_cast<int32_t*>(s_d), s_row, s_list, s_seq);
-    const int base = min(a.p.by_seq ? (*s_seq + t) * ((a.p.groups + 1) / 2) : t * ((a.p.cap * a.p.groups + 1) / 2), a.p.slots);
+    const int base = min((a.p.by_seq ? *s_seq + t : t) * a.p.step, a.p.slots);
     // (sequences that overlap or run backwards may ask for more blocks of h than there are: none past the last is touched)
-    const int n_ad = min(n_list, 2 * (a.p.slots - base) / a.p.groups), all = n_ad * a.p.groups;
+    const int n_ad = min(n_list, PLACES * (a.p.slots - base) / (TERMS * a.p.groups)), all = n_ad * a.p.groups;
     if (half == 0 && c0 == 0 && rank == 0) {
       if (threadIdx.x == 0) {
         a.p.n_ad[t] = n_ad;
@@ -284,7 +298,7 @@ __global__ void __launch_bounds__(D_THREADS, 1)
       if constexpr (CS > 1) cluster_sync();
       else __syncthreads();
       if (warp >= 2) {
-        // this block's share of the groups: the sum in the order of K, then a row's 32 + 32 bytes of hi and lo
+        // this block's share of the groups: the sum in the order of K, then a row's 32 bytes of each term
         const int r = (warp - 2) * 32 + lane, mine = s_row[half * 128 + r];
         for (int c = rank; c < ng; c += CS) {
           float v[16];
@@ -300,21 +314,22 @@ __global__ void __launch_bounds__(D_THREADS, 1)
           }
           const int ad = s_list[(g0 + c) / a.p.groups];
           const float by = __shfl_sync(0xffffffffu, scale, c);
-          uint32_t hi[8], lo[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float x = mine == ad ? v[2 * e] * by : 0.0f, y = mine == ad ? v[2 * e + 1] * by : 0.0f;
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-            const __nv_bfloat162 l = __floats2bfloat162_rn(x - __low2float(h), y - __high2float(h));
-            hi[e] = *reinterpret_cast<const uint32_t*>(&h);
-            lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+          for (int e = 0; e < 16; ++e) v[e] = mine == ad ? v[e] * by : 0.0f;
+#pragma unroll
+          for (int i = 0; i < TERMS; ++i) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+              v[2 * e] -= __low2float(h), v[2 * e + 1] -= __high2float(h);
+              w[e] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            const int place = TERMS * (g0 + c) + i;
+            uint4* out = reinterpret_cast<uint4*>(a.p.h + (static_cast<int64_t>(base + place / PLACES) * TR + half * 128 + r) * BK + place % PLACES * G);
+            out[0] = make_uint4(w[0], w[1], w[2], w[3]);
+            out[1] = make_uint4(w[4], w[5], w[6], w[7]);
           }
-          const int g = g0 + c;
-          uint4* out = reinterpret_cast<uint4*>(a.p.h + (static_cast<int64_t>(base + g / 2) * TR + half * 128 + r) * BK + g % 2 * 32);
-          out[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          out[1] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
-          out[2] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          out[3] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
         }
       }
       __syncwarp();
@@ -459,7 +474,7 @@ __global__ void __launch_bounds__(G_THREADS, 1)
   };
   const int k0 = a.kblocks * pair / KS, k1 = a.kblocks * (pair + 1) / KS;   // this pair's blocks of x and W (at least one)
   auto share = [&](int mt, int& e0, int& e1) {                // and of h and B; returns the tile's groups
-    const int groups = a.p.n_ad[mt] * a.p.groups, blocks = (groups + 1) / 2;
+    const int groups = a.p.n_ad[mt] * a.p.groups, blocks = blocks_of(groups);
     e0 = blocks * pair / KS;
     e1 = blocks * (pair + 1) / KS;
     return groups;
@@ -493,20 +508,23 @@ __global__ void __launch_bounds__(G_THREADS, 1)
       int e0, e1;
       const int groups = share(mt, e0, e1), base = a.p.base[mt];
       const int32_t* list = a.p.list + static_cast<int64_t>(mt) * a.p.cap;
-      int ad = 0;                          // lane i: the adapter of group i of the next 32
+      int ad = 0, g32 = -32;               // lane i: the adapter of group g32 + i
       for (int kb = e0; kb < e1; ++kb) {
-        if ((kb - e0) % 16 == 0) ad = 2 * kb + lane < groups ? list[(2 * kb + lane) / a.p.groups] : 0;
-        const int mine = __shfl_sync(0xffffffffu, ad, 2 * ((kb - e0) % 16) + (lane & 1));
+        const int g = first_group(kb), ng = last_group(kb, groups) - g + 1;
+        if (g + 1 >= g32 + 32) {
+          g32 = g;
+          ad = g + lane < groups ? list[(g + lane) / a.p.groups] : 0;
+        }
+        const int mine = __shfl_sync(0xffffffffu, ad, g - g32 + (lane & 1));
         if (!(ok = warp_wait_bounded(&empty[stage], phase ^ 1, abort_flag, a.status))) break;
         const uint32_t bar = full_l + 8u * stage;
-        const int ng = min(2, groups - 2 * kb);
         if (lane == 0) {
           if (!half) mbar_arrive_expect_tx(&full[stage], 2 * (C::A_BYTES + ng * C::EXT_BYTES));
           tma_load_2d_pair(sA + stage * C::A_BYTES, &tmH, bar, 0, (base + kb) * TR + half * 128);
         }
         __syncwarp();
         if (lane < ng)
-          tma_load_3d_pair(sB + stage * C::B_BYTES + lane * C::EXT_BYTES, &tmB, bar, (2 * kb + lane) % a.p.groups * G, n0, mine);
+          tma_load_3d_pair(sB + stage * C::B_BYTES + lane * C::EXT_BYTES, &tmB, bar, (g + lane) % a.p.groups * G, n0, mine);
         if (++stage == NST) { stage = 0; phase ^= 1; }
       }
       if (!ok) break;
@@ -547,12 +565,8 @@ __global__ void __launch_bounds__(G_THREADS, 1)
           if (!warp_wait_bounded(&full[stage], phase, abort_flag, a.status)) { ok = false; break; }
           tc_fence_after();
           const uint64_t a0 = sdesc_kmajor_sw128(smem_u32(sA + stage * C::A_BYTES));
-          const int ng = min(2, groups - 2 * kb);
-          for (int i = 0; i < ng; ++i) {
-            const uint64_t b0 = sdesc_rows32(smem_u32(sB + stage * C::B_BYTES + i * C::EXT_BYTES));
-            umma_bf16_pair(d, a0 + 4 * i, b0, idesc, 1);      // hi
-            umma_bf16_pair(d, a0 + 4 * i + 2, b0, idesc, 1);  // lo
-          }
+          for (int i = 0, place = PLACES * kb; i < PLACES && place < TERMS * groups; ++i, ++place)
+            umma_bf16_pair(d, a0 + 2 * i, sdesc_rows32(smem_u32(sB + stage * C::B_BYTES + (place / TERMS - first_group(kb)) * C::EXT_BYTES)), idesc, 1);
           umma_commit_pair_mc(&empty[stage], 0x3 << lead);
           if (++stage == NST) { stage = 0; phase ^= 1; }
         }

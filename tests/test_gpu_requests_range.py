@@ -1,0 +1,49 @@
+"""The operators for requests with settings of their own where their numbers are hard to keep: what an adapter's factor
+holds, long sums, logits at the limits of the temperature's range, against plain definitions in 64 bits."""
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from test_gpu_requests import BF16, T, gen, lora, lora_case, project64  # noqa: E402, F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ adapters
+@pytest.mark.parametrize("lens", [[1], [1] * 64, [32] * 8, [300, 1, 257, 63], [2048, 1, 1000]])
+@pytest.mark.parametrize("n_in,rank,n", [(64, 8, 1), (256, 24, 3), (512, 64, 7), (1000, 128, 40)])
+def test_lora_factor_in_fp32(T, lens, n_in, rank, n):
+    """W gives nothing, a row of x has one element, a row of B one column: an output is one product b h, h = s a x.  s a x
+    rounds once to fp32 (2^-24; a x has 16 bits); b times each part of h is exact, and what remains are two sums of them in
+    units that may truncate (2^-23 each) and that of the shares of K (2^-24; the others are zero): 3 x 2^-23 in all."""
+    g = gen(n_in + rank)
+    x, w, a, b, scale, cu, adapter = lora_case(g, lens, n_in, 200, rank, n, BF16, adapter=[i % n for i in range(len(lens))])
+    one = torch.randint(0, n_in, (x.shape[0], 1), generator=g, device="cuda")
+    x = torch.zeros_like(x).scatter_(1, one, x.gather(1, one))
+    only = torch.arange(200, device="cuda")[:, None] % rank
+    b = torch.zeros_like(b).scatter_(2, only.expand(n, 200, 1), b.gather(2, only.expand(n, 200, 1)))
+    y = torch.full((x.shape[0], 200), 7.5, device="cuda")
+    lora(T, x, torch.zeros_like(w), y, cu, adapter, a, b, scale)
+    T.tadm_ragged_sync_status()
+    ref = project64(x, torch.zeros_like(w), a, b, scale, cu, adapter)[0]
+    assert ((y.double() - ref).abs() <= 3 * 2.0 ** -23 * ref.abs()).all(), float(((y.double() - ref).abs() / ref.abs()).nan_to_num().max() * 2.0 ** 23)
+
+
+@pytest.mark.parametrize("lens", [[1] * 70, [300, 1, 257, 63]])
+@pytest.mark.parametrize("n_in,rank", [(1000, 16), (2048, 16), (5376, 64)])
+def test_lora_long_sums(T, lens, n_in, rank):
+    """Every 16 products a sum is rounded, by 2^-23 of it at most where the unit truncates; sums of products of both signs
+    stay within four times the root of their squares' sum.  The same for h, whose errors are as independent from rank to rank."""
+    x, w, a, b, scale, cu, adapter = lora_case(gen(n_in), lens, n_in, 264, rank, 5, BF16, adapter=[i % 5 for i in range(len(lens))])
+    y = torch.full((x.shape[0], 264), 7.5, device="cuda")
+    lora(T, x, w, y, cu, adapter, a, b, scale)
+    ref = project64(x, w, a, b, scale, cu, adapter)[0]
+    sq = lambda t: t.double().square()  # noqa: E731
+    of_y, of_h = sq(x) @ sq(w).T, torch.zeros_like(ref)
+    for i, ad in enumerate(adapter):
+        at, s2 = slice(cu[i], cu[i + 1]), float(scale[ad]) ** 2
+        of_y[at] += s2 * sq(x[at].double() @ a[ad].double().T) @ sq(b[ad]).T
+        of_h[at] = s2 * (sq(x[at]) @ sq(a[ad]).T) @ sq(b[ad]).T
+    tol = (n_in + 3 * rank) / 16 * 2.0 ** -21 * (of_y.sqrt() + of_h.sqrt())
+    err = (y.double() - ref).abs()
+    assert (err <= tol).all(), float((err / tol).max())

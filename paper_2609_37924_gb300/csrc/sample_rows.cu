@@ -535,7 +535,7 @@ __device__ __forceinline__ RowPlan plan_row(const SampleArgs& a, int row, const 
   float top = warp_max(mine.max);
   if (lane == 0) sh.max[warp] = top;
   __syncthreads();
-  top = warp_max(sh.max[lane & (NW - 1)]);
+  top = warp_max(sh.max[lane & (NW - 1)]) + 0.0f;             // (-0 as 0, which its ids' keys are of)
   RowPlan plan{top, top, top, r.hi, r.lo, none_of(top, 60.0f / r.hi), kEmpty, 0, 0, 0, 0, 0, 0, 0, 0, 0};
   const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {

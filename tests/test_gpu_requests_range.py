@@ -4,7 +4,7 @@ holds, long sums, logits at the limits of the temperature's range, against plain
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_requests import BF16, T, gen, lora, lora_case, project64  # noqa: E402, F401
+from test_gpu_requests import BF16, F32, T, check_draws, gen, i32, lora, lora_case, project64, randn  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +47,24 @@ def test_lora_long_sums(T, lens, n_in, rank):
     tol = (n_in + 3 * rank) / 16 * 2.0 ** -21 * (of_y.sqrt() + of_h.sqrt())
     err = (y.double() - ref).abs()
     assert (err <= tol).all(), float((err / tol).max())
+
+
+# ------------------------------------------------------------------ sampling
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab,rows", [(3000, 9), (30000, 6), (30000, 120)])
+def test_sample_maxima_of_minus_zero(T, dtype, vocab, rows):
+    """Rows without a positive logit whose largest ones are -0, which counts as 0."""
+    g = gen(vocab + rows)
+    x = -0.01 - 2 * randn(g, rows, vocab).abs()
+    for r in range(rows):
+        x[r, [7 + r, vocab // 2 + r, vocab - 1 - r][:r % 3 + 1]] = -0.0
+    x = x.to(dtype)
+    u = torch.rand(rows, generator=g, device="cuda")
+    ones = torch.ones(rows, device="cuda")
+    check_draws(T, x, u)
+    check_draws(T, x, u, 0 * ones)
+    check_draws(T, x, u, k=i32([1] * rows))
+    check_draws(T, x, u, k=i32([40, 2, 5000] * (rows // 3)), mask_id=7)
+    check_draws(T, x, u, 0.5 * ones, p=0.9 * ones)
+    check_draws(T, x, u, 0.5 * ones, m=0.3 * ones)
+    check_draws(T, x, u, k=i32([600] * rows), p=0.9 * ones, m=0.01 * ones)

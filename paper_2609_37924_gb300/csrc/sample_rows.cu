@@ -29,9 +29,9 @@
 //                          key until 128 elements or one key are left; the 512
 //                          ids in which the draw falls; the token.
 // Where a list overflows or the guess was wrong, the last one takes the whole
-// row by the same histograms (logits beyond 2^18 T; cuts of thousands of ids
-// by top-k under a second setting).  Of few rows the last three are one kernel,
-// sample_rest_kernel.
+// row by the same histograms (logits beyond some 2^17 T, where a chunk's weights
+// or bins are not counted; cuts of thousands of ids by top-k under a second
+// setting).  Of few rows the last three are one kernel, sample_rest_kernel.
 //
 // Bound: of few rows the chain of small steps, each a barrier or two (a row of 32768
 // ids 16 to 20 us, of which the scan 4); of many the instructions of the two passes
@@ -74,7 +74,8 @@ struct SampleArgs {
   struct RowPlan* plan;                    // [rows]
   uint2* list;                             // [rows][CAP] key, id
 };
-// Maximum of a chunk; its weights count from 2^(mj / 16), its bins from gj down; far: neither fits, the row is taken whole.
+// Maximum of a chunk; its weights count from 2^(mj / 16), its bins from gj down; far: one of them does not fit, the row is taken
+// whole if anything in the chunk counts.
 struct ChunkInfo {
   float max;
   int mj, gj, far;
@@ -537,7 +538,8 @@ __device__ __forceinline__ RowPlan plan_row(const SampleArgs& a, int row, const 
   __syncthreads();
   top = warp_max(sh.max[lane & (NW - 1)]) + 0.0f;             // (-0 as 0, which its ids' keys are of)
   RowPlan plan{top, top, top, r.hi, r.lo, none_of(top, 60.0f / r.hi), kEmpty, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-  const bool far = __syncthreads_or(mine.max == top && mine.far) != 0;
+  // (a chunk without masses counts if it lies within 2^-64 of the maximum, or that is not to be told: infinities)
+  const bool far = __syncthreads_or(mine.far && !((top - mine.max) * r.hi >= 64.0f)) != 0;
   if (top > ninf && (r.k == 1 || top == -ninf)) {
     plan.mode = kListed;                                      // the ids of the maximum
     plan.mj = far ? kFar : mj_of(r.hi, r.lo, top);

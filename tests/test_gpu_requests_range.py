@@ -1,10 +1,11 @@
 """The operators for requests with settings of their own where their numbers are hard to keep: what an adapter's factor
 holds, long sums, logits at the limits of the temperature's range, against plain definitions in 64 bits."""
+import math
 
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_requests import BF16, F32, T, check_draws, gen, i32, lora, lora_case, project64, randn  # noqa: E402, F401
+from test_gpu_requests import BF16, F32, T, check_draws, f32, gen, i32, lora, lora_case, project64, randn  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +69,28 @@ def test_sample_maxima_of_minus_zero(T, dtype, vocab, rows):
     check_draws(T, x, u, 0.5 * ones, p=0.9 * ones)
     check_draws(T, x, u, 0.5 * ones, m=0.3 * ones)
     check_draws(T, x, u, k=i32([600] * rows), p=0.9 * ones, m=0.01 * ones)
+
+
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("t", [1.0, 1e-4])
+@pytest.mark.parametrize("border,setting", [(2.0 ** 22 / 16 / math.log2(math.e), ""), (2.0 ** 22 / 16 / math.log2(math.e), "k"),
+                                            (2.0 ** 22 / 16 / math.log2(math.e), "m"), (101600.0, "p")])
+def test_sample_maxima_on_both_sides_of_a_limit(T, sign, t, border, setting):
+    """The passes over 8192 ids count weights from 2^(j / 16) and values in bins of a width of their own, while the numbers
+    of either stay below 2^22: rows whose maxima per 8192 ids lie on both sides of that, a little lower from one to the next."""
+    vocab, rows, step = 16384, 96, 2.0 ** -6
+    if setting == "p":                                         # 510 bins over the depth that top-p needs
+        border = 2.0 ** 22 * (math.log2(vocab / 0.1) + 0.5) / 510 / math.log2(math.e)
+    g = gen(int(border))
+    top = sign * border + step * (torch.arange(rows, device="cuda", dtype=torch.float64)[:, None] - rows / 2)
+    x = top - step * torch.randint(0, 64, (rows, vocab), generator=g, device="cuda")
+    u = torch.rand(rows, generator=g, device="cuda")
+    kw = {"k": dict(k=i32([40, 9000, 2] * 32)), "m": dict(m=f32([0.9, 0.3] * 48)), "p": dict(p=f32([0.9] * rows))}.get(setting, {})
+    for first, down in ((slice(8192, vocab), 0.25), (slice(0, 8192), 0.25), (slice(8192, vocab), 3.0)):
+        z = x.clone()
+        z[:, first] -= down
+        z = (z * t).float()
+        ts = torch.full((rows,), t, device="cuda")
+        check_draws(T, z, u, ts, **kw)                         # many rows
+        for r in range(0, rows, 8):                            # few
+            check_draws(T, z[r:r + 8], u[r:r + 8], ts[r:r + 8], **{n: v[r:r + 8] for n, v in kw.items()})

@@ -202,6 +202,13 @@ struct Row {
   int k;
   float p, mp, t;
 };
+// log2(e) / t in two terms
+__device__ __forceinline__ void log2e_over(float t, float& hi, float& lo) {
+  constexpr double kLog2e = 1.4426950408889634074;
+  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
+  hi = L / t;
+  lo = hi > 0.0f && hi < 3e38f ? (fmaf(-hi, t, L) + LL) / t : 0.0f;   // the division's remainder
+}
 __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   Row r;
   r.t = a.temperature ? a.temperature[row] : 1.0f;
@@ -210,10 +217,7 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int row) {
   const int k = a.top_k ? a.top_k[row] : 0;                   // (asked for with the others)
   r.k = !(r.t > 0x1p-100f) || r.p <= 0.0f ? 1 : k;
   if (r.k < 0 || r.k >= a.vocab) r.k = 0;
-  constexpr double kLog2e = 1.4426950408889634074;
-  constexpr float L = static_cast<float>(kLog2e), LL = static_cast<float>(kLog2e - static_cast<double>(L));
-  r.hi = L / r.t;
-  r.lo = r.hi > 0.0f && r.hi < 3e38f ? (fmaf(-r.hi, r.t, L) + LL) / r.t : 0.0f;   // the division's remainder
+  log2e_over(r.t, r.hi, r.lo);
   return r;
 }
 // p / q, right to an ulp of fp32 (a quotient of doubles takes four times as long).
@@ -245,21 +249,32 @@ __device__ __forceinline__ float depth_of(const SampleArgs& a, const Row& r) {
 
 // What weights count from: 2^(mj / 16), next to the weight of a maximum.  t = c x - mj / 16 without the rounding of a
 // difference: j = 16 t to the nearest whole number, f = c x - (mj + j) / 16 by one fma (whose product is exact), plus c's
-// second term.  shift: the maximum where it is far from zero (then mj = 0, and logits that weigh anything are near it).
+// second term.  shift: the maximum where it is far from zero (then mj = 0, and logits that weigh anything are near it).  by:
+// what logits are multiplied with, and temperatures, too.
 struct Scale {
-  float hi, lo, hi16, k_c, mh, shift;
-  __device__ __forceinline__ Scale(float c_hi, float c_lo, int mj, float from)
-      : hi(c_hi), lo(c_lo), hi16(16.0f * c_hi), k_c(kMagic - static_cast<float>(mj)), mh(static_cast<float>(mj) * 0.0625f), shift(from) {}
+  float hi, lo, hi16, k_c, mh, shift, by;
+  __device__ __forceinline__ Scale(float c_hi, float c_lo, int mj, float from, float factor = 1.0f)
+      : hi(c_hi), lo(c_lo), hi16(16.0f * c_hi), k_c(kMagic - static_cast<float>(mj)), mh(static_cast<float>(mj) * 0.0625f), shift(from), by(factor) {}
 };
 __device__ __forceinline__ int mj_of(float c_hi, float c_lo, float max) {
   const float m = 16.0f * max * c_hi;
   return fabsf(m) < static_cast<float>(kFar) - 2.0f ? __float2int_rn(m) : kFar;
 }
+// Of a row taken by itself.  Where its temperature is above 10^30 logits that count may lie further apart than the largest number,
+// and log2(e) / T has no second term: both are taken 2^-64 times.  (What a logit loses by that weighs nothing.)
+__device__ __forceinline__ Scale far_scale(const Row& r, float max) {
+  if (r.hi > 1e-30f) return Scale(r.hi, r.lo, 0, max);
+  constexpr float by = 0x1p-64f;
+  float hi, lo;
+  log2e_over(r.t * by, hi, lo);
+  const int mj = mj_of(hi, lo, max * by);
+  return mj == kFar ? Scale(hi, lo, 0, max * by, by) : Scale(hi, lo, mj, 0.0f, by);
+}
 
 // The weight of a logit in units of 2^-44, rounded: 2^f - 1 (2^-30 of rounding) in 36 fraction bits, times 2^(j/16) from
 // the table, shifted.
 __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, float l) {
-  const float x = l - s.shift;
+  const float x = fmaf(l, s.by, -s.shift);
   if (!(fmaf(x, s.hi, -s.mh) > -46.0f)) return 0;
   const float q = fmaf(x, s.hi16, s.k_c), jf = q - kMagic;
   const int j = __float_as_int(q) - kMagicBits;
@@ -1008,7 +1023,7 @@ __device__ __forceinline__ void finish_row(const SampleArgs& a, int row, const R
     return;
   }
   const bool far = plan.mj == kFar;
-  Finisher<T> f{sh, l, Scale(r.hi, r.lo, far ? 0 : plan.mj, far ? plan.max : 0.0f), plan.max, plan.mode == kWhole};
+  Finisher<T> f{sh, l, far ? far_scale(r, plan.max) : Scale(r.hi, r.lo, plan.mj, 0.0f), plan.max, plan.mode == kWhole};
   const uint32_t khi = Key<T>::of(plan.max), kinf = Key<T>::of(ninf) + 1;
   if (r.k == 1) {                          // the lowest id of the maximum
     if (threadIdx.x == 0) sh.d_id = 0xffffffffu;

@@ -2,6 +2,7 @@
 holds, long sums, logits at the limits of the temperature's range, against plain definitions in 64 bits."""
 import math
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -94,3 +95,22 @@ def test_sample_maxima_on_both_sides_of_a_limit(T, sign, t, border, setting):
         check_draws(T, z, u, ts, **kw)                         # many rows
         for r in range(0, rows, 8):                            # few
             check_draws(T, z[r:r + 8], u[r:r + 8], ts[r:r + 8], **{n: v[r:r + 8] for n, v in kw.items()})
+
+
+@pytest.mark.parametrize("vocab", [3000, 9000])
+def test_sample_logits_a_whole_range_apart(T, vocab):
+    """Temperatures at which logits count that lie further apart than the largest number."""
+    rows, top = 14, float(np.finfo(np.float32).max)
+    g = gen(vocab + 3)
+    x = top * (2 * torch.rand(rows, vocab, generator=g, device="cuda") - 1)
+    x[:, 5], x[:, 6] = top, -top
+    t = f32([1e37, 1e38, 3e38, math.inf, 1e36, 5e37, top] * 2)
+    x[7:] *= 0.25
+    u = torch.rand(rows, generator=g, device="cuda")
+    many = torch.arange(rows, device="cuda")
+    for y in (x, (1e31 * randn(g, rows, vocab)), x.bfloat16().clamp(-3e38, 3e38)):
+        s = t if y is x or y.dtype == BF16 else f32([1e31, 2e30, 1.4e30, 1.5e30, 1e32, 1e35, 1e29] * 2)
+        check_draws(T, y, u, s)
+        check_draws(T, y, u, s, k=(many * 100 + 3).int(), mask_id=5)
+        check_draws(T, y, u, s, p=f32([0.9, 0.3] * 7))
+        check_draws(T, y, u, s, m=f32([0.5, 0.01] * 7), p=f32([0.9, 0.3] * 7))

@@ -88,8 +88,8 @@ class Server:
         return int(self.status)
 
     # -- layers ----------------------------------------------------------------------------------
-    def lora(self, x, w, ab, cu, adapter):
-        y = torch.empty((x.shape[0], w.shape[0]), dtype=torch.bfloat16, device="cuda")
+    def lora(self, x, w, ab, cu, adapter, dtype=torch.bfloat16):
+        y = torch.empty((x.shape[0], w.shape[0]), dtype=dtype, device="cuda")
         a, b = ab
         need = T.tadm_lora_scratch_size(cu.numel() - 1, *x.shape, w.shape[0], a.shape[0], a.shape[1], 1)
         T.tadm_lora_project(x, w, y, cu, adapter, a, b, self.lora_scale, torch.empty(need, dtype=torch.uint8, device="cuda"))
@@ -109,7 +109,7 @@ class Server:
 
     def output(self, h, n, o, layer, cu, adapter):
         """Adds the attention's projection to the stream h and leaves the norm of that in n."""
-        y = self.lora(o.view(h.shape[0], -1), self.wo[layer], self.lora_o[layer], cu, adapter)
+        y = self.lora(o.view(h.shape[0], -1), self.wo[layer], self.lora_o[layer], cu, adapter, torch.float32)
         T.tadm_residual_norm(h, y, h, n, pre_gain=self.gain)
 
     def draw(self, n, u, **settings):

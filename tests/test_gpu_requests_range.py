@@ -1,6 +1,8 @@
 """The operators for requests with settings of their own where their numbers are hard to keep: what an adapter's factor
 holds, long sums, logits at the limits of the temperature's range, against plain definitions in 64 bits."""
+import importlib.util
 import math
+import os
 
 import numpy as np
 import pytest
@@ -114,3 +116,22 @@ def test_sample_logits_a_whole_range_apart(T, vocab):
         check_draws(T, y, u, s, k=(many * 100 + 3).int(), mask_id=5)
         check_draws(T, y, u, s, p=f32([0.9, 0.3] * 7))
         check_draws(T, y, u, s, m=f32([0.5, 0.01] * 7), p=f32([0.9, 0.3] * 7))
+
+
+# ------------------------------------------------------------------ the example
+def test_the_example_adds_its_projection_in_fp32(T):
+    """The output projection reaches the fp32 stream without a rounding to bf16: sums of 2048 products in fp32, each of
+    whose 128 steps rounds by 2^-23 of four times the root of the squares' sum at most (bf16 would be 2^-9 of the value)."""
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "ragged_server.py")
+    spec = importlib.util.spec_from_file_location("ragged_server", at)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    s = mod.Server(1, 16, 8, 128, seqs=4, max_len=128, pages=8, seed=1)
+    g = gen(50)
+    d, rows = 2048, 40
+    h, n = torch.zeros((rows, d), device="cuda"), torch.empty((rows, d), dtype=BF16, device="cuda")
+    o = randn(g, rows, 16, 128).bfloat16()
+    s.output(h, n, o, 0, i32([0, rows]), i32([-1]))
+    v, w = o.view(rows, d).double(), s.wo[0].double()
+    tol = 128 * 2.0 ** -21 * (v.square() @ w.square().T).sqrt()
+    assert ((h.double() - v @ w.T).abs() <= tol).all()

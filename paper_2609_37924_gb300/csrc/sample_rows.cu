@@ -157,7 +157,7 @@ struct Logits {
   // V::N ids from id on, a multiple of V::N
   __device__ __forceinline__ uint4 load(int id) const {
     if (vec && id + V::N <= vocab) return __ldg(reinterpret_cast<const uint4*>(p + id));
-    T v[V::N];
+    alignas(16) T v[V::N];
 #pragma unroll
     for (int e = 0; e < V::N; ++e) v[e] = id + e < vocab ? p[id + e] : from_f32<T>(__int_as_float(0xff800000));
     return *reinterpret_cast<const uint4*>(v);

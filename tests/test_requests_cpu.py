@@ -117,6 +117,22 @@ def test_every_bounded_wait_of_the_adapters_names_the_status_word():
         assert "a.status" in w and "nullptr" not in w, w
 
 
+def test_local_arrays_read_as_vectors_are_aligned_for_them():
+    """`T v[N]` read back through a pointer to 16 bytes: the array says so, whatever the compiler keeps it in."""
+    import os
+    import re
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_37924_gb300", "csrc")
+    found = 0
+    for name in ("sample_rows.cu", "adapters.cu", "adapters_rows.cu", "residual_norm.cu"):
+        src = open(os.path.join(at, name)).read()
+        for m in re.finditer(r"reinterpret_cast<(?:const )?(?:uint4|float4|uint2)\*>\(([a-z]+)\)(?!\[)", src):
+            decl = [d for d in re.finditer(r"^ *(?:alignas\([^;]*\) )?[\w:]+ " + m.group(1) + r"\[[^\]]+\];", src[:m.start()], re.M)]
+            if decl:
+                found += 1
+                assert "alignas" in decl[-1].group(0), (name, decl[-1].group(0))
+    assert found >= 2
+
+
 # ------------------------------------------------------------------ the Python entry points
 torch = pytest.importorskip("torch")
 from paper_2609_37924_gb300 import tadm  # noqa: E402

@@ -705,7 +705,8 @@ TADM_API tadm_status tadm_sample(const void* logits, int64_t ld, int rows, int v
  * lora_b; y_dtype 0 or 1 for bf16 calls, 0 for fp32 ones.  x, W, lora_a and
  * lora_b are 16-byte aligned, n_in, ldx and ldw times the element size multiples
  * of 16, rank a multiple of 8 up to 256 (adapters of a lower rank: zeros behind
- * their rows of A and columns of B), total_rows and n_out up to 2^20, batch up to 2^30 (TADM_ERR_UNSUPPORTED above).  y must not overlap the
+ * their rows of A and columns of B), total_rows and n_out up to 2^20, batch up to 2^30,
+ * for bf16 calls a scratch size up to 2^38 (TADM_ERR_UNSUPPORTED above).  y must not overlap the
  * inputs.
  *
  * Sums are fp32.  bf16 calls carry A_a x (times the scale) to 24 significant

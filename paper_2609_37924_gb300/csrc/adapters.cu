@@ -86,7 +86,8 @@ Plan make_plan(int batch, int total, int n_adapters, int rank, uint8_t* scratch,
   const int64_t by_tile = static_cast<int64_t>(p.tiles) * per_tile, by_seq = (static_cast<int64_t>(batch) + p.tiles) * per_seq;
   p.by_seq = by_seq < by_tile;
   p.step = p.by_seq ? per_seq : per_tile;
-  p.slots = static_cast<int>(std::min<int64_t>(std::min(by_tile, by_seq), INT32_MAX / TR));
+  const int64_t slots = std::min(by_tile, by_seq);
+  p.slots = static_cast<int>(std::min<int64_t>(slots, INT32_MAX / TR));   // (more of them are refused: kLoraMaxScratch)
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t here = at;
@@ -96,7 +97,7 @@ Plan make_plan(int batch, int total, int n_adapters, int rank, uint8_t* scratch,
   p.n_ad = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles));
   p.base = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles));
   p.list = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * p.tiles * static_cast<size_t>(p.cap)));
-  p.h = reinterpret_cast<bf16*>(take(static_cast<size_t>(p.slots) * KB_BYTES));
+  p.h = reinterpret_cast<bf16*>(take(static_cast<size_t>(slots) * KB_BYTES));
   if (bytes) *bytes = at + 1024;           // the blocks start on 1024 bytes, scratch on 16
   return p;
 }

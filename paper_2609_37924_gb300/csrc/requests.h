@@ -36,6 +36,7 @@ struct LoraCall {
   int* status;                     // this device's status word
 };
 constexpr int kLoraMaxRank = 256, kLoraMaxRows = 1 << 20;
+constexpr size_t kLoraMaxScratch = size_t{1} << 38;   // bf16: rows of 128 bytes, which tensor maps count in 31 bits
 size_t lora_scratch(int batch, int total, int n_in, int n_out, int n_adapters, int rank, int bf16);
 const char* lora_project(const LoraCall& c, cudaStream_t s);          // tcgen05 (bf16), or
 size_t lora_rows_scratch(int total, int rank);

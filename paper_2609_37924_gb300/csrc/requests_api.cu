@@ -61,6 +61,7 @@ tadm_status tadm_lora_project(const void* x, const void* w, void* y, const int32
     return TADM_ERR_INVALID_ARG;
   if (n_adapters > 0 && (!lora_a || !lora_b || !lora_scale || !aligned(lora_a, 16) || !aligned(lora_b, 16) || !aligned(lora_scale, 4)))
     return TADM_ERR_INVALID_ARG;
+  if (dtype && need > kLoraMaxScratch) return TADM_ERR_UNSUPPORTED;
   if (need > 0 && (!scratch || !aligned(scratch, 16) || scratch_bytes < need)) return TADM_ERR_INVALID_ARG;
   if (total_rows > kLoraMaxRows || n_out > kLoraMaxRows || batch > kMaxSequences) return TADM_ERR_UNSUPPORTED;   // grids, counts of tiles
   LoraCall c{};

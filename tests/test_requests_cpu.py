@@ -84,6 +84,14 @@ def test_lora_scratch(T):
         assert T.load_library().tadm_lora_project(*{**LORA, **over}.values()) == 0
 
 
+def test_lora_more_factors_than_are_counted(T):
+    """Every row an adapter of its own, at the highest rank: refused, none of them is left out."""
+    call = {**LORA, "batch": 1 << 20, "total": 1 << 20, "rank": 256, "scratch_bytes": 1 << 60}
+    assert T.tadm_lora_scratch_size(1 << 20, 1 << 20, 64, 40, 300, 256, 1) > 1 << 38
+    assert T.load_library().tadm_lora_project(*{**call, "n": 300}.values()) == UNSUPPORTED
+    assert T.tadm_lora_scratch_size(1 << 20, 1 << 20, 64, 40, 2, 256, 1) <= 1 << 38
+
+
 NORM = dict(x=P, y=P, x_out=P, n_out=P, cu=P, batch=3, total=10, d=64, ldx=64, ldy=64, ldxo=64, ldn=64, post=P, gate=P, ldg=64,
             pre=P, residual_scale=1.0, eps=1e-6, x_dtype=0, y_dtype=0, dtype=1, stream=None)
 

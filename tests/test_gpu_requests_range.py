@@ -8,7 +8,7 @@ import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_requests import BF16, F32, T, check_draws, f32, gen, i32, lora, lora_case, project64, randn  # noqa: E402, F401
+from test_gpu_requests import BF16, F32, T, check_draws, check_norm, f32, gen, i32, lora, lora_case, norm64, project64, randn  # noqa: E402, F401
 
 pytestmark = pytest.mark.gpu
 
@@ -116,6 +116,24 @@ def test_sample_logits_a_whole_range_apart(T, vocab):
         check_draws(T, y, u, s, k=(many * 100 + 3).int(), mask_id=5)
         check_draws(T, y, u, s, p=f32([0.9, 0.3] * 7))
         check_draws(T, y, u, s, m=f32([0.5, 0.01] * 7), p=f32([0.9, 0.3] * 7))
+
+
+# ------------------------------------------------------------------ norms
+@pytest.mark.parametrize("xt,yt,t", [(F32, F32, BF16), (F32, BF16, BF16), (BF16, BF16, BF16), (BF16, F32, F32)])
+@pytest.mark.parametrize("d", [1032, 2048, 4096, 5376, 8192])
+def test_residual_norm_of_many_rows_without_gains(T, xt, yt, t, d):
+    """Both outputs, and the residual add alone, where rows are many and no parameter is given."""
+    g = gen(d + 1)
+    total = 1500
+    x, y = randn(g, total, d).to(xt), (3 * randn(g, total, d)).to(yt)
+    xo, no = torch.full_like(x, 9.0), torch.full((total, d), 9.0, device="cuda").to(t)
+    T.tadm_residual_norm(x, y, xo, no)
+    want = norm64(x, y, None, None, None, 1.0, np.float32(1e-6), None)
+    check_norm((xo, no), want[:2], want[2], want[3])
+    alone = torch.full_like(x, 9.0)
+    T.tadm_residual_norm(x, y, alone, cu_rows=i32([0, 700, 700, total]))
+    assert torch.equal(alone, xo)
+    T.tadm_ragged_sync_status()
 
 
 # ------------------------------------------------------------------ the example

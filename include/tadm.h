@@ -683,10 +683,13 @@ TADM_API tadm_status tadm_pages_copy(const tadm_page_pool* pool, const int32_t* 
  *  - temperature[row] <= 2^-100 or NaN: the first of the order, whatever the
  *    other settings.  temperature NULL: 1; top_k, top_p, min_p NULL: off.
  *  - prob (optional): the token's weight over the kept ids' mass.
- * Weights count in units of 2^-44 of the largest (smaller ones are none), right to about 2^-30 without a bias:
+ * Weights count in units of 2^-44 of the largest (smaller ones are none).  Each
+ * is right to 2^-28, and to 2^-30.6 in the mean over logits, without a bias:
  * results repeat, do not depend on the other rows, and are those of exact
- * arithmetic unless u or a cut lies within some 2^-34 of the mass of a border.  vocab is
- * at most 2^19 (TADM_ERR_UNSUPPORTED above).  Rows may start at any element.
+ * arithmetic unless u or a cut lies next to a border: within some 2^-34 of the
+ * mass where a hundred or more distinct logits carry it, whose errors average
+ * out; within 2^-29 where a few do (ids with equal logits have one error).
+ * vocab is at most 2^19 (TADM_ERR_UNSUPPORTED above).  Rows may start at any element.
  * scratch: at least tadm_sample_scratch_size() bytes (none for small
  * vocabularies), 256-byte aligned; it needs no initialisation, and calls that
  * overlap on the GPU need one each. */

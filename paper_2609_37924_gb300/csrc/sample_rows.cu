@@ -13,9 +13,12 @@
 //
 // A cut or a draw next to a border must not depend on rounding: with weights
 // of fp32 a row of 10^5 like tokens draws another one every few thousand
-// rows.  Weights are right to about 2^-30 without a bias, and their sums are
-// 64-bit integers in units of 2^-44, or pairs of fp32 sums good to 2^-37 a lane
-// (bulk), so that a border has to lie within some 2^-35 of the mass.
+// rows.  Weights are right to 2^-28 (2^-30.6 in the mean over logits, without a
+// bias), and their sums are 64-bit integers in units of 2^-44, or pairs of fp32
+// sums good to 2^-37 a lane (bulk).  So a border has to lie within some 2^-34 of
+// the mass where a hundred distinct logits or more carry it; where a few do,
+// equal ones among them, whose errors are one, within 2^-29 (two values with
+// half of the mass each: a quarter of the difference of their errors).
 //
 // Rows of up to 4096 ids: one block a row, sample_finish_kernel.  Longer ones:
 //   sample_scan_kernel     per 8192 ids: maximum, mass per 512 ids, histogram of
@@ -189,8 +192,8 @@ __constant__ const float2 kPowF[16] = {
     {0.951365709f, 3.19341815e-08f}, {0.946177363f, 3.62105723e-08f}, {0.943156064f, -3.09907193e-08f}, {0.942090809f, -7.47521334e-09f},
     {0.942809045f, 1.71142709e-08f}, {0.945168734f, -3.04768335e-08f}, {0.949052811f, 5.23333421e-09f}, {0.954364657f, 6.10759177e-09f},
     {0.961024463f, -1.47196051e-08f}, {0.968966722f, -5.25879518e-09f}, {0.978137672f, -6.12825968e-09f}, {0.988493681f, 5.14060927e-09f}};
-// 2^f - 1 = f (A1 + f (A2 + f (A3 + f A4))) for |f| <= 1/32: ln2^n / n!, eased so that the neglected terms spread (Chebyshev); error
-// 2^-37
+// 2^f - 1 = f (A1 + f (A2 + f (A3 + f A4))) for |f| <= 1/32: ln2^n / n!, eased so that the neglected terms spread (Chebyshev);
+// with the coefficients in fp32 right to 2^-33.7, which is little beside what its evaluation rounds (2^-30.6, 2^-28.3 at most)
 constexpr float A1 = 0.693147182f, A2 = 0.240226507f, A3 = 0.0555057377f, A4 = 0.00961835496f;
 constexpr float kMagic = 12582912.0f;      // 1.5 * 2^23: added to a number, leaves the nearest whole one in the low bits
 constexpr int kMagicBits = 0x4b400000;
@@ -271,7 +274,7 @@ __device__ __forceinline__ Scale far_scale(const Row& r, float max) {
   return mj == kFar ? Scale(hi, lo, 0, max * by, by) : Scale(hi, lo, mj, 0.0f, by);
 }
 
-// The weight of a logit in units of 2^-44, rounded: 2^f - 1 (2^-30 of rounding) in 36 fraction bits, times 2^(j/16) from
+// The weight of a logit in units of 2^-44, rounded: 2^f - 1 (2^-28.3 of rounding at most) in 36 fraction bits, times 2^(j/16) from
 // the table, shifted.
 __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, float l) {
   const float x = fmaf(l, s.by, -s.shift);
@@ -290,7 +293,7 @@ __device__ __forceinline__ uint64_t weight(const Scale& s, const uint64_t* pow, 
 __device__ __forceinline__ void add_shared(uint32_t at, uint32_t x) { asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(at), "r"(x) : "memory"); }
 
 // Sums the weights of a lane's values, in units of 2^-44.  weight()'s arithmetic, with the table's rest added to 2^f - 1: a
-// weight is a + a r, a in fp32, r good to 2^-30; h the sum's rounding, l what that lost.  The sum of h begins at 96, so that
+// weight is a + a r, a in fp32, r as good as there; h the sum's rounding, l what that lost.  The sum of h begins at 96, so that
 // what its roundings (2^-17) lose is had by two subtractions; the lost parts' sum carries errors of about 2^-38 a lane.
 struct Sums {
   float big = 96.0f, small = 0.0f;

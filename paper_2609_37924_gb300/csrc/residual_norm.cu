@@ -343,14 +343,13 @@ cudaError_t launch(const NormArgs& a, bool vec, cudaStream_t s) {
   const int nvec = a.d / 8;
   int dev = 0;
   const int sms = current_sms(&dev);
-  // rows enough for a few turns of every block, and wide enough for a block (narrow ones: a warp each, many at once)
-  if (vec && nvec > 128 && nvec <= 2 * RT && a.total >= 8 * sms && RING * ring_stage<XT, YT>(a.d) <= kRingBytes)
-    switch ((a.d / 4 + RT - 1) / RT) {
-      case 1: return launch_ring<XT, YT, T, 1>(a, dev, sms, s);
-      case 2: return launch_ring<XT, YT, T, 2>(a, dev, sms, s);
-      case 3: return launch_ring<XT, YT, T, 3>(a, dev, sms, s);
-      default: return launch_ring<XT, YT, T, 4>(a, dev, sms, s);
-    }
+  // The ring for rows of more than 4096, two turns of every block or more.  Instead of a block per row, fp32 and bf16 x, bf16 y:
+  //   of 5376   304 rows 6.1 for 6.2 us and 5.5 for 5.1; 608 9.6 for 11.0 and 8.7 for 9.1; 4864 57 for 69 and 45 for 58
+  //   of 4096   1216 rows 12.2 for 12.8 and 11.3 for 9.8; 11512 101 for 85 and 78 for 65
+  //   of 2048   1216 rows 8.6 for 7.0 and 8.3 for 5.5; 11512 55 for 44 and 56 for 32
+  // (of narrow rows many are in flight at once as it is, and a turn of the ring ends in its barriers).
+  if (vec && nvec > RT && nvec <= 2 * RT && a.total >= 4 * sms && RING * ring_stage<XT, YT>(a.d) <= kRingBytes)
+    return a.d <= 3 * 4 * RT ? launch_ring<XT, YT, T, 3>(a, dev, sms, s) : launch_ring<XT, YT, T, 4>(a, dev, sms, s);
   if (vec && nvec <= 128) {
     const int rows = 8, grid = (a.total + rows - 1) / rows;
     if (nvec <= 32) return launch_pdl(norm_reg_kernel<XT, YT, T, 1, false>, grid, 32 * rows, 0, s, a);

@@ -524,7 +524,8 @@ template <class T>
 __device__ __forceinline__ uint32_t low_key(const Row& r, const Scale& s, const uint64_t* pow, float max) {
   const uint32_t top = Key<T>::of(max), bottom = Key<T>::of(__int_as_float(0xff800000)) + 1;
   if (!(r.mp > 0.0f)) return bottom;
-  if (r.mp >= 1.0f || !(max < __int_as_float(0x7f800000))) return top;
+  if (!(max < __int_as_float(0x7f800000))) return top;
+  if (r.mp >= 1.0f) return r.hi > 0.0f ? top : bottom;        // (T infinite: every id weighs as much as the first)
   const uint64_t least = ::max(times<true>(r.mp, weight(s, pow, max)), static_cast<uint64_t>(1));
   auto enough = [&](uint32_t key) { return weight(s, pow, Key<T>::value(key)) >= least; };
   // (near max + T ln(min-p), if it is there)

@@ -118,6 +118,19 @@ def test_sample_logits_a_whole_range_apart(T, vocab):
         check_draws(T, y, u, s, m=f32([0.5, 0.01] * 7), p=f32([0.9, 0.3] * 7))
 
 
+@pytest.mark.parametrize("vocab", [300, 9000])
+def test_sample_min_p_of_one(T, vocab):
+    """The ids of the maximum; at an infinite temperature, where every one weighs as much, all of them."""
+    rows = 12
+    g = gen(vocab + 4)
+    x = randn(g, rows, vocab)
+    x[:4] = torch.round(2 * x[:4]) / 2
+    x[11, [5, 8]] = math.inf
+    t, u = f32([1.0, math.inf, 0.5] * 4), torch.rand(rows, generator=g, device="cuda")
+    check_draws(T, x, u, t, m=f32([1.0, 1.0, 2.0, 2.0] * 3))
+    check_draws(T, x, u, t, m=f32([1.0, 1.0, 2.0, 2.0] * 3), p=f32([0.9] * rows), mask_id=3)
+
+
 # ------------------------------------------------------------------ norms
 @pytest.mark.parametrize("xt,yt,t", [(F32, F32, BF16), (F32, BF16, BF16), (BF16, BF16, BF16), (BF16, F32, F32)])
 @pytest.mark.parametrize("d", [1032, 2048, 4096, 5376, 8192])

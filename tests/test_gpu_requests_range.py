@@ -118,6 +118,23 @@ def test_sample_logits_a_whole_range_apart(T, vocab):
         check_draws(T, y, u, s, m=f32([0.5, 0.01] * 7), p=f32([0.9, 0.3] * 7))
 
 
+@pytest.mark.parametrize("vocab,rows", [(30000, 4), (30000, 80)])
+def test_sample_cuts_beside_a_token_s_mass(T, vocab, rows):
+    """A few tokens far apart above a tail: top-p ends within some 10^-6 of where one of them does, on either side."""
+    g = gen(vocab + rows + 7)
+    x = randn(g, rows, vocab)
+    at = torch.randint(0, vocab - 1, (rows, 5), generator=g, device="cuda")
+    x.scatter_(1, at, torch.tensor([16.0, 13.5, 12.0, 10.5, 9.0], device="cuda") + 0.2 * randn(g, rows, 5))
+    w = torch.sort(x.double(), 1, descending=True).values
+    w = torch.exp(w - w[:, :1])
+    mass = torch.cumsum(w, 1) / w.sum(1, keepdim=True)
+    u = torch.rand(rows, generator=g, device="cuda")
+    for j in range(6):
+        for off in (3e-6, -3e-6, 1e-4, -1e-4):
+            check_draws(T, x, u, p=(mass[:, j] + off).float())
+        check_draws(T, x, u, p=(mass[:, j] + 3e-6).float(), m=f32([1e-6] * rows), mask_id=vocab - 1)
+
+
 @pytest.mark.parametrize("vocab", [300, 9000])
 def test_sample_min_p_of_one(T, vocab):
     """The ids of the maximum; at an infinite temperature, where every one weighs as much, all of them."""

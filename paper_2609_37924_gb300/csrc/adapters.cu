@@ -32,12 +32,12 @@
 // its predecessor has waited for what came before, so x and W are there).
 //
 // Bound: of prompts the tensor pipe (24 prompts, 5874 rows, 2048 -> 4096, 6
-// adapters of rank 16: 64 us, of which the product 59 at 83 % of the pipe; the
-// FLOP alone are 52; tiles of 192 columns 77 us, of 128 100); of few rows the chain of the two kernels: h
+// adapters of rank 16: 74 us, of which the product 63 at 83 % of the pipe; the
+// FLOP alone are 52); of few rows the chain of the two kernels: h
 // after 10 us (lists 2, x A^T 2 to 5, sums 3), then its blocks (64 tokens, 40 adapters:
-// 22 us; 256 rows, 5376 -> 8192, rank 64: 36, of which W's 88 MB are 13).  Blocks of
+// 24.6 us; 256 rows, 5376 -> 8192, rank 64: 38.3, of which W's 88 MB are 13).  Blocks of
 // h and B cost 0.4 us each against 0.25 of x and W: B comes in rows of 32 bytes.
-// Tried: K over the four pairs of a cluster of 8 (only 15 of those run at once,
+// Tried, with h in two terms: tiles of 192 columns (prompts 77 us where 256 took 64), of 128 (100); K over the four pairs of a cluster of 8 (only 15 of those run at once,
 // 36 us for the tokens); h as the first units of the product's own kernel, with a
 // counter per tile that the others wait for (tokens 21, prompts 68, 256 rows 34 us: no
 // gain that is worth a wait between blocks).

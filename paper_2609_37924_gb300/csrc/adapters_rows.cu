@@ -13,7 +13,8 @@
 // per thread between reads of shared memory (four prompts of 228 rows, 256 ->
 // 768, rank 8: 10.9 us; blocks fetched one ahead into registers, a warp per row
 // for its adapter and no overlap, 15.8); of many the FMA and shared-memory
-// pipes (2020 rows, 768 -> 2304: 200 us, 37 TFLOP/s).
+// pipes (2020 rows, 768 -> 2304: 204 us with rank 16, 35 TFLOP/s; 222 with rank
+// 64, 251 with 128).
 #include <cstdint>
 
 #include "ragged.cuh"

@@ -10,6 +10,8 @@
 //
 // Bound: HBM, (2 es_x + es_y + es_n) bytes per element: 11512 rows of 5376 (fp32 x, bf16 y) 123 us, 6.0 TB/s, 89 % of a
 // plain copy's rate; 1024 rows of 2048 in bf16 4.4 us out of L2; one row 3.5 us, the launch.
+// Past the ring, a block per row: 11512 rows of 5376, fp32 x and y, 144 us (128 at a copy's rate), of 8192, bf16 y, 200 (167), 4096
+// of 16384 168 (119).  Other widths, element by element: 11512 rows of 5377 284 us (110), 1024 of 49152 760 (89).
 #include <cstdint>
 
 #include "ragged.cuh"

@@ -38,9 +38,11 @@
 //
 // Bound: of few rows the chain of small steps, each a barrier or two (a row of 32768
 // ids 16 to 20 us, of which the scan 4); of many the instructions of the two passes
-// over the logits (512 rows of 128000, fp32, a nucleus each: 231 us, of which scan
-// 111 with 46 instructions an id at 71 % of the issue slots, collect 89 with 37 at
-// 74 %; one reading of the logits is 39).  Weights above the cut summed where they
+// over the logits (512 rows of 128000, fp32, a nucleus each: 230 us, of which scan
+// 111 with 46 instructions an id at 73 % of the issue slots, collect 87 with 36 at
+// 73 %; one reading of the logits is 39).  Rows of up to 4096 ids: the same steps over all of
+// a row's ids (one row of 1024 9.0 us with top-p, 5.4 without; 512 of 4096 47 and 30; 4096
+// of 4096 294 and 200).  Weights above the cut summed where they
 // lie, without moving them together, 292 us with two blocks an SM.  The row in the
 // shared memory of a cluster of 8 blocks instead, read from HBM once, took 691
 // us: 38 rows at a time, each some 45 us of passes that end in a cluster
